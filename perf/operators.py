@@ -171,8 +171,11 @@ def prepare(case, seed):
             state["labels"][4] = -1
         if case["dir"] == "bwd":
             state["row_grad"] = (1 + 0.1 * normal(rows).abs()) / rows
-            zd = state["z"].double()
-            state["lse"] = torch.stack([torch.logsumexp(zd / case["temperature"], 1), torch.logsumexp(zd, 1)], 1).float()
+            # what the forward leaves: the largest logit and the logarithms of both sums of exp(difference to it)
+            most = state["z"].float().amax(1, keepdim=True)
+            d = state["z"].double() - most
+            state["stats"] = torch.cat([most, torch.logsumexp(d / case["temperature"], 1, keepdim=True).float(),
+                                        torch.logsumexp(d, 1, keepdim=True).float()], 1)
     return state
 
 
@@ -263,7 +266,8 @@ def _run_plain(s, case):
         return m + torch.log(torch.exp(v - m).sum(1, keepdim=True))
 
     if case["dir"] == "bwd":
-        lse_t, lse_1 = s["lse"][:, :1], s["lse"][:, 1:]
+        z = z - s["stats"][:, :1]
+        lse_t, lse_1 = s["stats"][:, 1:2], s["stats"][:, 2:]
         weight = s["row_grad"][:, None]
     else:
         lse_t = log_sum(z / temperature)
@@ -304,7 +308,7 @@ def _run_own(s, case):
         return P.bsr_layernorm_backward(s["dy"], s["x"], s["mean"], s["rstd"], s["gamma"], res=s.get("res"))
     how = dict(labels=s["labels"], temperature=case["temperature"], hard_weight=case["hard"])
     if case["dir"] == "bwd":
-        return P.bsr_distill_backward(s["z"], s["top_index"], s["top_logits"], s["lse"], s["row_grad"], **how)
+        return P.bsr_distill_backward(s["z"], s["top_index"], s["top_logits"], s["stats"], s["row_grad"], **how)
     if case["dir"] == "fwd":
         return P.bsr_distill_forward(s["z"], s["top_index"], s["top_logits"], **how)[0]
     return P.bsr_distill_forward_backward(s["z"], s["top_index"], s["top_logits"], grad_scale=1.0 / s["z"].shape[0], **how)
