@@ -464,6 +464,96 @@ int32_t bsr_attention_backward(const void* qkv, const void* out, const void* dou
                                int32_t* used_mfma, void* stream);
 
 /*
+ * Operators on the caller's own tensors (no context): LayerNorm, frozen linear layers in 8 bits, distillation from a teacher's top
+ * logits.  A program that tunes the norms of a frozen model against a teacher runs them one after the other
+ * (paper_2405_10951_amd/norm_tuning.py).  Rows are contiguous; between rows there is a stride ("ld...", in elements, at least the row's
+ * length) and the first may start anywhere.  Types are BSR_BF16 or BSR_FP32; statistics, sums over rows, products and losses are fp32 inside whatever
+ * the type.  Tensors without a stride are aligned to 16 bytes; rows of whole 16-byte pieces on 16-byte boundaries are the fast ones.  Zero rows are no error: nothing is
+ * launched but what zeroes a sum over them.  Results are bit-reproducible (no atomics).  All launches go to `stream`, nothing waits.
+ * Errors: INVALID_ARG (NULL or misaligned pointer, a negative row count, a length < 1, a stride shorter than a row, an unknown type), HIP.
+ *
+ * LayerNorm.
+ * bsr_layernorm_forward: y = (x - mean) rstd gamma + beta over rows of D, mean and biased variance per row, rstd = 1 / sqrt(var + eps).
+ *   x [M,D] stride ldx, y [M,D] stride ldy: of `type`; y may be NULL when values is given
+ *   gamma, beta   fp32 [D]
+ *   values, scales  both or neither: the result, unrounded, as 8-bit rows (below)
+ *   mean, rstd    fp32 [M], may be NULL
+ * bsr_layernorm_backward: dx = res + rstd (g - mean(g) - xhat mean(g xhat)), g = dy gamma, xhat = (x - mean) rstd; dgamma = sum over rows of
+ *   dy xhat, dbeta = sum of dy.  For a forward that left 8-bit rows the rounding counts as the identity.
+ *   dy, x, res, dx  [M,D] of `type`, with strides; res may be NULL (no residual gradient to add); dx may be NULL (parameters only), dy or res
+ *   dgamma, dbeta fp32 [D], both or neither
+ *   workspace     device fp32 scratch of bsr_layernorm_workspace_floats(D) floats, needed with dgamma
+ */
+size_t bsr_layernorm_workspace_floats(int32_t D);
+int32_t bsr_layernorm_forward(const void* x, int32_t type, int64_t M, int32_t D, int64_t ldx, const float* gamma, const float* beta, float eps,
+                              void* y, int64_t ldy, void* values, uint8_t* scales, float* mean, float* rstd, void* stream);
+int32_t bsr_layernorm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* res, int64_t ldr, int32_t type, int64_t M,
+                               int32_t D, const float* mean, const float* rstd, const float* gamma, void* dx, int64_t lddx, float* dgamma,
+                               float* dbeta, float* workspace, size_t workspace_floats, void* stream);
+
+/*
+ * Frozen linear layers in 8 bits.  A block of 128 holds e4m3 values (1 sign, 4 exponent, 3 mantissa bits, largest 448) and one scale, a power
+ * of two 2^e kept as the byte e + 127: e is the smallest integer >= -127 with max|x| 2^-e <= 448 (0 for a block of zeros), the values are x 2^-e rounded to
+ * nearest, ties to even.  Non-finite x do not count towards the maximum and become NaN.  Activations and gradients have a block for each 128
+ * columns of a row, weights for each 128 x 128.  K columns are stored as
+ *   values [rows, ldv]  ldv = K rounded up to 128, zeros behind column K
+ *   scales [rows, lds]  lds = number of blocks rounded up to 4 (one row of scales per 128 rows of a weight matrix)
+ * (bsr_block8_strides gives both).  The layer is frozen: there is an input gradient and no weight gradient.
+ * bsr_quantize8_rows: x [M,K] of `type`, stride ldx -> values, scales
+ * bsr_quantize8_weight: w [in,out] of `type`, stride ldw -> values [out, ldv(in)], scales [ceil(out/128), lds(in)] and, for the input gradient,
+ *   the same blocks as values_back [in, ldv(out)], scales_back [ceil(in/128), lds(out)] (both or neither)
+ * bsr_linear8_forward: y[M,out] = act(x . W + bias) (+ res)
+ *   x             x_scales given: 8-bit rows of `in` columns (x_type and ldx are ignored); NULL: [M,in] of x_type, stride ldx, brought to 8 bits on the way
+ *   workspace     device scratch, 16-byte aligned, of bsr_linear8_workspace_bytes(M, in), which is 0 where none is needed (a few rows); for x that is not in 8 bits yet
+ *   values, scales  the layer
+ *   bias          fp32 [out], may be NULL;  act 0: none, 1: exact-erf GELU
+ *   u_out, res, y [M,out] of y_type, contiguous; u_out (the pre-activation, act = 1) and res may be NULL
+ * bsr_linear8_dgrad: dx[M,in] = dy[M,out] . W^T, optionally times GELU'(u) element-wise; values, scales are the layer's values_back, scales_back
+ *   dy            as x above, of `out` columns;  workspace: bsr_linear8_workspace_bytes(M, out)
+ *   u, dx         [M,in] of dx_type, contiguous; u may be NULL
+ */
+void bsr_block8_strides(int32_t K, int64_t* ldv, int64_t* lds);
+int32_t bsr_quantize8_rows(const void* x, int32_t type, int64_t M, int32_t K, int64_t ldx, void* values, uint8_t* scales, void* stream);
+int32_t bsr_quantize8_weight(const void* w, int32_t type, int32_t in, int32_t out, int64_t ldw, void* values, uint8_t* scales, void* values_back,
+                             uint8_t* scales_back, void* stream);
+size_t bsr_linear8_workspace_bytes(int32_t M, int32_t K);
+int32_t bsr_linear8_forward(const void* x, int32_t x_type, int64_t ldx, const uint8_t* x_scales, int32_t M, int32_t in, int32_t out,
+                            const void* values, const uint8_t* scales, const float* bias, int32_t act, void* u_out, const void* res, void* y,
+                            int32_t y_type, void* workspace, size_t workspace_bytes, void* stream);
+int32_t bsr_linear8_dgrad(const void* dy, int32_t dy_type, int64_t lddy, const uint8_t* dy_scales, int32_t M, int32_t in, int32_t out,
+                          const void* values_back, const uint8_t* scales_back, const void* u, void* dx, int32_t dx_type, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * Distillation: loss of a classifier against a teacher's top logits, mixed with the label's cross-entropy.  Per row, with the student's logits
+ * z [classes], the teacher's entries (class c_j, logit t_j), temperature T > 0 and hard weight a in [0,1]:
+ *   p = softmax(t / T) over the entries,  q = softmax(z / T),  r = softmax(z)
+ *   loss = (1 - a) T^2 sum_j p_j (log p_j - log q_{c_j}) + a (-log r_label)
+ *   dz_v = g ((1 - a) T (q_v - sum_{j: c_j = v} p_j) + a (r_v - [v = label])),   g = grad_scale * row_grad[row]
+ * An entry whose class lies outside 0 .. classes-1 is absent, one whose logit is -inf has p = 0; a row without entries of p > 0 lacks the first part, one
+ * whose label lies outside 0 .. classes-1 the second; a row whose logits are all -inf has loss and gradient 0.  A class with z = -inf that the teacher
+ * gives weight makes the loss +inf and leaves the gradient finite.  NaN and +inf in z make a row NaN.
+ *   z            [rows, classes] of `type`, stride ldz
+ *   index        int32 [rows, top], stride ldi: c_j;  top <= 1024
+ *   logits       [rows, top] of logits_type, stride ldt: t_j
+ *   labels       int32 [rows], may be NULL
+ *   loss         fp32 [rows], may be NULL
+ *   stats        fp32 [rows, 3], may be NULL: m = max z, log sum exp((z - m) / T), log sum exp(z - m) (0 when a = 0 and T != 1), what the backward
+ *                needs; apart, because their sum would lose the logarithm where m is large
+ *   row_grad     fp32 [rows], may be NULL (1 for every row)
+ *   dz           [rows, classes] of `type`, stride ldd; may be z itself (same stride).  bsr_distill_forward: NULL for no gradient
+ * bsr_distill_forward gives loss, stats and, in the same launch, dz; bsr_distill_backward gives dz from stats.
+ */
+int32_t bsr_distill_forward(const void* z, int32_t type, int64_t rows, int32_t classes, int64_t ldz, const int32_t* index, int64_t ldi,
+                            const void* logits, int32_t logits_type, int64_t ldt, int32_t top, const int32_t* labels, float temperature,
+                            float hard_weight, float* loss, float* stats, const float* row_grad, float grad_scale, void* dz, int64_t ldd,
+                            void* stream);
+int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t classes, int64_t ldz, const int32_t* index, int64_t ldi,
+                             const void* logits, int32_t logits_type, int64_t ldt, int32_t top, const int32_t* labels, float temperature,
+                             float hard_weight, const float* stats, const float* row_grad, float grad_scale, void* dz, int64_t ldd,
+                             void* stream);
+
+/*
  * Profiling mode, for measurement only.  Between bsr_profile_begin and bsr_profile_end every launch
  * of the classes below is bracketed by a pair of HIP events on the call's stream (created on first
  * use and kept by the context).  bsr_profile_end WAITS for the recorded work, then adds up, per

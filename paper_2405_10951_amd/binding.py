@@ -130,6 +130,20 @@ def load_library():
     lib.bsr_attention_backward.restype = C.c_int32
     lib.bsr_attention_backward.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                            C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    p, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+    for name, args in {
+            "bsr_layernorm_forward": (p, i32, i64, i32, i64, p, p, f32, p, i64, p, p, p, p, p),
+            "bsr_layernorm_backward": (p, i64, p, i64, p, i64, i32, i64, i32, p, p, p, p, i64, p, p, p, C.c_size_t, p),
+            "bsr_quantize8_rows": (p, i32, i64, i32, i64, p, p, p),
+            "bsr_quantize8_weight": (p, i32, i32, i32, i64, p, p, p, p, p),
+            "bsr_linear8_forward": (p, i32, i64, p, i32, i32, i32, p, p, p, i32, p, p, p, i32, p, C.c_size_t, p),
+            "bsr_linear8_dgrad": (p, i32, i64, p, i32, i32, i32, p, p, p, p, i32, p, C.c_size_t, p),
+            "bsr_distill_forward": (p, i32, i64, i32, i64, p, i64, p, i32, i64, i32, p, f32, f32, p, p, p, f32, p, i64, p),
+            "bsr_distill_backward": (p, i32, i64, i32, i64, p, i64, p, i32, i64, i32, p, f32, f32, p, p, f32, p, i64, p)}.items():
+        getattr(lib, name).restype, getattr(lib, name).argtypes = i32, args
+    lib.bsr_block8_strides.restype, lib.bsr_block8_strides.argtypes = None, (i32, p, p)
+    lib.bsr_layernorm_workspace_floats.restype, lib.bsr_layernorm_workspace_floats.argtypes = C.c_size_t, (i32,)
+    lib.bsr_linear8_workspace_bytes.restype, lib.bsr_linear8_workspace_bytes.argtypes = C.c_size_t, (i32, i32)
     lib.bsr_profile_begin.argtypes = [C.c_void_p]
     lib.bsr_profile_end.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
     _lib = lib
@@ -330,13 +344,13 @@ def bsr_linear_wgrad_static(x, dy, dw=None, db=None):
     return dw, used.value
 
 
-def bsr_attention_forward(qkv, heads, want_lse=True, want_cls=True):
+def bsr_attention_forward(qkv, heads, want_stats=True, want_cls=True):
     """qkv [B,T,3D] bf16 -> (out [B,T,D] bf16, lse [B,H,T] | None, cls_prob [B,H,T] | None, used_mfma)."""
     import torch
     B, T, D3 = qkv.shape
     D = D3 // 3
     out = torch.empty((B, T, D), dtype=torch.bfloat16, device=qkv.device)
-    lse = torch.empty((B, heads, T), dtype=torch.float32, device=qkv.device) if want_lse else None
+    lse = torch.empty((B, heads, T), dtype=torch.float32, device=qkv.device) if want_stats else None
     cls = torch.empty((B, heads, T), dtype=torch.float32, device=qkv.device) if want_cls else None
     used = C.c_int32(-1)
     _check(load_library().bsr_attention_forward(_dp(qkv), B, T, heads, D // heads, _dp(out), _dp(lse), _dp(cls),
@@ -355,6 +369,256 @@ def bsr_attention_backward(qkv, out, dout, lse, heads):
     _check(load_library().bsr_attention_backward(_dp(qkv), _dp(out), _dp(dout), _dp(lse), B, T, heads, D // heads,
                                                  _dp(delta), _dp(dqkv), C.byref(used), _cur_stream(qkv)))
     return dqkv, used.value
+
+class Rows8:
+    """Rows in 8 bits: `values` uint8 [M, ldv] (e4m3), `scales` uint8 [M, lds], `cols` columns (see bsr.h)."""
+    __slots__ = ("values", "scales", "cols")
+
+    def __init__(self, values, scales, cols):
+        self.values, self.scales, self.cols = values, scales, int(cols)
+
+
+class Weight8:
+    """A frozen linear layer in 8 bits, laid out once: `values` / `scales` for the forward product, `values_back` / `scales_back`
+    (None without) for the input gradient; n_in, n_out (see bsr.h)."""
+    __slots__ = ("values", "scales", "values_back", "scales_back", "n_in", "n_out")
+
+    def __init__(self, values, scales, values_back, scales_back, n_in, n_out):
+        self.values, self.scales, self.values_back, self.scales_back = values, scales, values_back, scales_back
+        self.n_in, self.n_out = int(n_in), int(n_out)
+
+
+def _type_code(t, what):
+    import torch
+    code = {torch.bfloat16: BSR_BF16, torch.float32: BSR_FP32}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what}: bfloat16 or float32 is needed, got {t.dtype}")
+    return code
+
+
+def _rows_of(t, what, shape=None, dtype=None):
+    """A tensor of two dimensions whose rows are contiguous -> its row stride."""
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, {'two dimensions' if shape is None else tuple(shape)} expected")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what}: {dtype} is needed, got {t.dtype}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: the elements of a row have to lie together, stride {t.stride(1)}")
+    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if ld < t.shape[1]:
+        raise ValueError(f"{what}: rows overlap (stride {ld}, {t.shape[1]} columns)")
+    return ld
+
+
+def _flat(t, what, shape, dtype):
+    """An optional contiguous tensor of a known shape and type -> itself."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous {dtype} {tuple(shape)} expected, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+    return t
+
+
+def _together(first, *others):
+    """The current stream of the GPU that all tensors are on."""
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+    return _raw_stream(_gpu_index(first.device))
+
+
+def _blocks_of(n):
+    return -(-n // 128)
+
+
+def _rows8_new(M, K, device):
+    import torch
+    nk = _blocks_of(K)
+    return Rows8(torch.empty((M, nk * 128), dtype=torch.uint8, device=device),
+                 torch.empty((M, (nk + 3) // 4 * 4), dtype=torch.uint8, device=device), K)
+
+
+def bsr_quantize8_rows(x) -> Rows8:
+    """x [M,K] bf16 or fp32 (any row stride) -> 8-bit rows, a scale for each 128 columns."""
+    ld, code, stream = _rows_of(x, "x"), _type_code(x, "x"), _together(x)
+    M, K = x.shape
+    r = _rows8_new(M, K, x.device)
+    _check(load_library().bsr_quantize8_rows(_dp(x), code, M, K, ld, _dp(r.values), _dp(r.scales), stream))
+    return r
+
+
+def bsr_quantize8_weight(w, backward=True) -> Weight8:
+    """w [in,out] bf16 or fp32 (any row stride) -> a frozen 8-bit layer, a scale for each 128 x 128; backward: with the copy that the input
+    gradient reads."""
+    ld, code, stream = _rows_of(w, "w"), _type_code(w, "w"), _together(w)
+    n_in, n_out = w.shape
+
+    def new(rows, cols):
+        import torch
+        nk = _blocks_of(cols)
+        return (torch.empty((rows, nk * 128), dtype=torch.uint8, device=w.device),
+                torch.empty((_blocks_of(rows), (nk + 3) // 4 * 4), dtype=torch.uint8, device=w.device))
+
+    v, s = new(n_out, n_in)
+    vb, sb = new(n_in, n_out) if backward else (None, None)
+    _check(load_library().bsr_quantize8_weight(_dp(w), code, n_in, n_out, ld, _dp(v), _dp(s), _dp(vb), _dp(sb), stream))
+    return Weight8(v, s, vb, sb, n_in, n_out)
+
+
+def _linear8_rows(x, cols, what):
+    """-> (M, x pointer, type code, stride, scales pointer, workspace, its bytes)"""
+    import torch
+    if isinstance(x, Rows8):
+        if x.cols != cols:
+            raise ValueError(f"{what}: {x.cols} columns, the layer has {cols}")
+        return x.values.shape[0], _dp(x.values), BSR_BF16, 0, _dp(x.scales), None, 0
+    ld, code = _rows_of(x, what, (x.shape[0], cols)), _type_code(x, what)
+    M = x.shape[0]
+    size = load_library().bsr_linear8_workspace_bytes(M, cols)
+    ws = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
+    return M, _dp(x), code, ld, None, ws, size
+
+
+def bsr_linear8_forward(x, w: Weight8, bias=None, act=0, u_out=None, res=None, y=None, out_dtype=None):
+    """x [M,in] (Rows8, or bf16 / fp32 with any row stride) -> y [M,out] = act(x W + bias) (+ res), of out_dtype (that of x, bf16 for Rows8).
+    act 1: GELU, u_out [M,out] receives its input."""
+    import torch
+    t = x.values if isinstance(x, Rows8) else x
+    stream = _together(t, w.values, bias, u_out, res, y)
+    M, px, code, ld, ps, ws, size = _linear8_rows(x, w.n_in, "x")
+    if y is None:
+        y = torch.empty((M, w.n_out), dtype=out_dtype or (torch.bfloat16 if isinstance(x, Rows8) else x.dtype), device=t.device)
+    elif out_dtype is not None and y.dtype != out_dtype:
+        raise TypeError(f"y: {y.dtype}, out_dtype {out_dtype}")
+    _flat(y, "y", (M, w.n_out), y.dtype)
+    _flat(bias, "bias", (w.n_out,), torch.float32)
+    _flat(u_out, "u_out", (M, w.n_out), y.dtype)
+    _flat(res, "res", (M, w.n_out), y.dtype)
+    _check(load_library().bsr_linear8_forward(px, code, ld, ps, M, w.n_in, w.n_out, _dp(w.values), _dp(w.scales), _dp(bias), act, _dp(u_out),
+                                              _dp(res), _dp(y), _type_code(y, "y"), _dp(ws), size, stream))
+    return y
+
+
+def bsr_linear8_dgrad(dy, w: Weight8, u=None, dx=None, out_dtype=None):
+    """dy [M,out] (Rows8, or bf16 / fp32 with any row stride) -> dx [M,in] = dy W^T, times GELU'(u) where u [M,in] is given."""
+    import torch
+    if w.values_back is None:
+        raise ValueError("the layer was laid out without backward")
+    t = dy.values if isinstance(dy, Rows8) else dy
+    stream = _together(t, w.values_back, u, dx)
+    M, px, code, ld, ps, ws, size = _linear8_rows(dy, w.n_out, "dy")
+    if dx is None:
+        dx = torch.empty((M, w.n_in), dtype=out_dtype or (torch.bfloat16 if isinstance(dy, Rows8) else dy.dtype), device=t.device)
+    elif out_dtype is not None and dx.dtype != out_dtype:
+        raise TypeError(f"dx: {dx.dtype}, out_dtype {out_dtype}")
+    _flat(dx, "dx", (M, w.n_in), dx.dtype)
+    _flat(u, "u", (M, w.n_in), dx.dtype)
+    _check(load_library().bsr_linear8_dgrad(px, code, ld, ps, M, w.n_in, w.n_out, _dp(w.values_back), _dp(w.scales_back), _dp(u), _dp(dx),
+                                            _type_code(dx, "dx"), _dp(ws), size, stream))
+    return dx
+
+
+def _layernorm_forward(x, gamma, beta, eps, y, r8):
+    import torch
+    ld, code, stream = _rows_of(x, "x"), _type_code(x, "x"), _together(x, gamma, beta, y)
+    M, D = x.shape
+    _flat(gamma, "gamma", (D,), torch.float32)
+    _flat(beta, "beta", (D,), torch.float32)
+    ldy = _rows_of(y, "y", (M, D), x.dtype) if y is not None else 0
+    mean = torch.empty(M, dtype=torch.float32, device=x.device)
+    rstd = torch.empty(M, dtype=torch.float32, device=x.device)
+    _check(load_library().bsr_layernorm_forward(_dp(x), code, M, D, ld, _dp(gamma), _dp(beta), eps, _dp(y), ldy, _dp(r8.values) if r8 else None,
+                                                _dp(r8.scales) if r8 else None, _dp(mean), _dp(rstd), stream))
+    return mean, rstd
+
+
+def bsr_layernorm_forward(x, gamma, beta, eps=1e-6, y=None):
+    """x [M,D] bf16 or fp32 (any row stride), gamma, beta [D] fp32 -> (y [M,D], mean [M], rstd [M])."""
+    import torch
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    mean, rstd = _layernorm_forward(x, gamma, beta, eps, y, None)
+    return y, mean, rstd
+
+
+def bsr_layernorm_forward8(x, gamma, beta, eps=1e-6, y=None):
+    """The same with the result in 8 bits -> (Rows8, mean, rstd); y given: rounded to the type of x as well."""
+    r8 = _rows8_new(x.shape[0], x.shape[1], x.device)
+    mean, rstd = _layernorm_forward(x, gamma, beta, eps, y, r8)
+    return r8, mean, rstd
+
+
+def bsr_layernorm_backward(dy, x, mean, rstd, gamma, res=None, dx=None, need_dx=True, need_params=True):
+    """dy, x [M,D], mean, rstd [M] of the forward, gamma [D] -> (dx [M,D] | None, dgamma [D] | None, dbeta [D] | None).  res [M,D]: added to dx."""
+    import torch
+    lib = load_library()
+    ldx, code, stream = _rows_of(x, "x"), _type_code(x, "x"), _together(x, dy, mean, rstd, gamma, res, dx)
+    M, D = x.shape
+    lddy = _rows_of(dy, "dy", (M, D), x.dtype)
+    ldr = _rows_of(res, "res", (M, D), x.dtype) if res is not None else 0
+    _flat(mean, "mean", (M,), torch.float32)
+    _flat(rstd, "rstd", (M,), torch.float32)
+    _flat(gamma, "gamma", (D,), torch.float32)
+    if dx is None and need_dx:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    lddx = _rows_of(dx, "dx", (M, D), x.dtype) if dx is not None else 0
+    dg = db = ws = None
+    if need_params:
+        dg = torch.empty(D, dtype=torch.float32, device=x.device)
+        db = torch.empty(D, dtype=torch.float32, device=x.device)
+        ws = torch.empty(lib.bsr_layernorm_workspace_floats(D), dtype=torch.float32, device=x.device)
+    _check(lib.bsr_layernorm_backward(_dp(dy), lddy, _dp(x), ldx, _dp(res), ldr, code, M, D, _dp(mean), _dp(rstd), _dp(gamma), _dp(dx), lddx,
+                                      _dp(dg), _dp(db), _dp(ws), 0 if ws is None else ws.numel(), stream))
+    return dx, dg, db
+
+
+def _distill_common(z, index, logits, labels, row_grad, others):
+    import torch
+    stream = _together(z, index, logits, labels, row_grad, *others)
+    ldz, code = _rows_of(z, "z"), _type_code(z, "z")
+    rows, classes = z.shape
+    ldi = _rows_of(index, "index", (rows, index.shape[-1]), torch.int32)
+    ldt = _rows_of(logits, "logits", index.shape)
+    _flat(labels, "labels", (rows,), torch.int32)
+    _flat(row_grad, "row_grad", (rows,), torch.float32)
+    return stream, (_dp(z), code, rows, classes, ldz, _dp(index), ldi, _dp(logits), _type_code(logits, "logits"), ldt, index.shape[1], _dp(labels))
+
+
+def _distill_forward(z, index, logits, labels, temperature, hard_weight, row_grad, grad_scale, dz, want_stats):
+    import torch
+    stream, args = _distill_common(z, index, logits, labels, row_grad, (dz,))
+    ldd = _rows_of(dz, "dz", z.shape, z.dtype) if dz is not None else 0
+    loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
+    stats = torch.empty((z.shape[0], 3), dtype=torch.float32, device=z.device) if want_stats else None
+    _check(load_library().bsr_distill_forward(*args, temperature, hard_weight, _dp(loss), _dp(stats), _dp(row_grad), grad_scale, _dp(dz), ldd, stream))
+    return loss, stats
+
+
+def bsr_distill_forward(z, index, logits, labels=None, temperature=1.0, hard_weight=0.0):
+    """Student logits z [rows,classes] bf16 or fp32, the teacher's classes index [rows,top] int32 (-1: absent) and logits [rows,top], labels
+    [rows] int32 (-1: none) -> (loss [rows], stats [rows,3] for bsr_distill_backward)."""
+    return _distill_forward(z, index, logits, labels, temperature, hard_weight, None, 1.0, None, True)
+
+
+def bsr_distill_forward_backward(z, index, logits, labels=None, temperature=1.0, hard_weight=0.0, row_grad=None, grad_scale=1.0, dz=None):
+    """-> (loss [rows], dz [rows,classes] = grad_scale row_grad[row] dloss/dz) in one launch.  dz may be z."""
+    import torch
+    if dz is None:
+        dz = torch.empty(z.shape, dtype=z.dtype, device=z.device)
+    loss, _ = _distill_forward(z, index, logits, labels, temperature, hard_weight, row_grad, grad_scale, dz, False)
+    return loss, dz
+
+
+def bsr_distill_backward(z, index, logits, stats, row_grad=None, labels=None, temperature=1.0, hard_weight=0.0, grad_scale=1.0, dz=None):
+    """dz [rows,classes] = grad_scale row_grad[row] dloss/dz from the stats of bsr_distill_forward.  dz may be z."""
+    import torch
+    if dz is None:
+        dz = torch.empty(z.shape, dtype=z.dtype, device=z.device)
+    stream, args = _distill_common(z, index, logits, labels, row_grad, (stats, dz))
+    ldd = _rows_of(dz, "dz", z.shape, z.dtype)
+    _flat(stats, "stats", (z.shape[0], 3), torch.float32)
+    _check(load_library().bsr_distill_backward(*args, temperature, hard_weight, _dp(stats), _dp(row_grad), grad_scale, _dp(dz), ldd, stream))
+    return dz
 
 
 _PointerTable = C.c_uint64 * (C.sizeof(bsr_params) // 8)       # a bsr_params, which holds nothing but pointers, by position

@@ -13,6 +13,9 @@
 
 #include "../../include/bsr.h"
 #include "bsr_internal.h"
+#include "distill.h"
+#include "fp8.h"
+#include "norm_rows.h"
 
 using namespace bsr;
 
@@ -1752,6 +1755,187 @@ int32_t bsr_destroy(bsr_ctx* c) {
   }
   delete c;
   return BSR_OK;
+}
+
+// ---- operators on the caller's own tensors ------------------------------------------------------------------------------------------
+static bool known_type(int32_t t) { return t == BSR_BF16 || t == BSR_FP32; }
+// a matrix with a row stride: there, aligned to its elements, rows that do not overlap
+static bool rows_ok(const void* p, int32_t type, int64_t ld, int64_t row) {
+  return p && ((uintptr_t)p & (type == BSR_FP32 ? 3 : 1)) == 0 && ld >= row;
+}
+static bool aligned4(const void* p) { return p && ((uintptr_t)p & 3) == 0; }
+
+size_t bsr_layernorm_workspace_floats(int32_t D) { return D < 1 ? 0 : norm_rows_bwd_floats(D); }
+
+int32_t bsr_layernorm_forward(const void* x, int32_t type, int64_t M, int32_t D, int64_t ldx, const float* gamma, const float* beta, float eps,
+                              void* y, int64_t ldy, void* values, uint8_t* scales, float* mean, float* rstd, void* stream) {
+  const char* w = "bsr_layernorm_forward";
+  if (!known_type(type) || M < 0 || D < 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, D %d", w, type, (long long)M, D);
+  if (!aligned16(gamma) || !aligned16(beta)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: gamma or beta is NULL or not 16-byte aligned", w);
+  if (!(eps >= 0.f)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: eps %g", w, eps);
+  if (M == 0) return BSR_OK;                         // (and tensors without elements have no address)
+  if (!values != !scales || (!y && !values)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: y, or values and scales, or all three", w);
+  if (!rows_ok(x, type, ldx, D) || (y && !rows_ok(y, type, ldy, D)))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: x or y is NULL, misaligned or has rows closer than %d", w, D);
+  if ((values && !aligned16(values)) || (mean && !aligned4(mean)) || (rstd && !aligned4(rstd)))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: misaligned output", w);
+  NormRows a;
+  a.x = x; a.M = M; a.D = D; a.ldx = ldx; a.f32 = type == BSR_FP32; a.gamma = gamma; a.beta = beta; a.eps = eps;
+  a.y = y; a.ldy = ldy; a.q = values; a.scale = scales; a.mean = mean; a.rstd = rstd;
+  norm_rows_fwd(a, (hipStream_t)stream);
+  return check_hip(nullptr, w);
+}
+
+int32_t bsr_layernorm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* res, int64_t ldr, int32_t type, int64_t M,
+                               int32_t D, const float* mean, const float* rstd, const float* gamma, void* dx, int64_t lddx, float* dgamma,
+                               float* dbeta, float* workspace, size_t workspace_floats, void* stream) {
+  const char* w = "bsr_layernorm_backward";
+  if (!known_type(type) || M < 0 || D < 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, D %d", w, type, (long long)M, D);
+  if (!dgamma != !dbeta || (M > 0 && !dx && !dgamma)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dx, or dgamma and dbeta, or all three", w);
+  if (dgamma && (!aligned4(dgamma) || !aligned4(dbeta) || !aligned16(workspace)))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: misaligned dgamma or dbeta, or workspace NULL or not 16-byte aligned", w);
+  if (dgamma && workspace_floats < norm_rows_bwd_floats(D))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: workspace of %zu floats, %zu are needed", w, workspace_floats, norm_rows_bwd_floats(D));
+  if (!aligned16(gamma)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: gamma is NULL or not 16-byte aligned", w);
+  if (M > 0 && (!rows_ok(dy, type, lddy, D) || !rows_ok(x, type, ldx, D) || (res && !rows_ok(res, type, ldr, D)) || (dx && !rows_ok(dx, type, lddx, D))))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dy, x, res or dx is NULL, misaligned or has rows closer than %d", w, D);
+  if (M > 0 && (!aligned4(mean) || !aligned4(rstd))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: mean or rstd is NULL or misaligned", w);
+  if (M == 0 && !dgamma) return BSR_OK;
+  NormRowsBwd a;
+  a.dy = dy; a.x = x; a.res = res; a.lddy = lddy; a.ldx = ldx; a.ldr = ldr; a.M = M; a.D = D; a.f32 = type == BSR_FP32;
+  a.mean = mean; a.rstd = rstd; a.gamma = gamma; a.dx = dx; a.lddx = lddx; a.dgamma = dgamma; a.dbeta = dbeta; a.partial = workspace;
+  norm_rows_bwd(a, (hipStream_t)stream);
+  return check_hip(nullptr, w);
+}
+
+void bsr_block8_strides(int32_t K, int64_t* ldv, int64_t* lds) {
+  if (ldv) *ldv = K < 1 ? 0 : ld8(K);
+  if (lds) *lds = K < 1 ? 0 : ld8s(K);
+}
+
+int32_t bsr_quantize8_rows(const void* x, int32_t type, int64_t M, int32_t K, int64_t ldx, void* values, uint8_t* scales, void* stream) {
+  const char* w = "bsr_quantize8_rows";
+  if (!known_type(type) || M < 0 || K < 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, K %d", w, type, (long long)M, K);
+  if (M == 0) return BSR_OK;
+  if (!rows_ok(x, type, ldx, K)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: x is NULL, misaligned or has rows closer than %d", w, K);
+  if (!aligned16(values) || !aligned4(scales)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: values or scales is NULL or misaligned", w);
+  quantize8_rows(x, type == BSR_FP32, M, K, ldx, values, scales, (hipStream_t)stream);
+  return check_hip(nullptr, w);
+}
+
+int32_t bsr_quantize8_weight(const void* weight, int32_t type, int32_t in, int32_t out, int64_t ldw, void* values, uint8_t* scales, void* values_back,
+                             uint8_t* scales_back, void* stream) {
+  const char* w = "bsr_quantize8_weight";
+  if (!known_type(type) || in < 1 || out < 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, in %d, out %d", w, type, in, out);
+  if (!rows_ok(weight, type, ldw, out)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: w is NULL, misaligned or has rows closer than %d", w, out);
+  if (!aligned16(values) || !aligned4(scales) || !values_back != !scales_back || (values_back && (!aligned16(values_back) || !aligned4(scales_back))))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: values or scales is NULL or misaligned", w);
+  quantize8_weight(weight, type == BSR_FP32, in, out, ldw, values, scales, values_back, scales_back, (hipStream_t)stream);
+  return check_hip(nullptr, w);
+}
+
+static size_t rows8_values_bytes(int64_t M, int32_t K) { return (size_t)M * (size_t)ld8(K); }      // (a multiple of 128)
+size_t bsr_linear8_workspace_bytes(int32_t M, int32_t K) {
+  return M < 1 || K < 1 || gemm8_few_takes(M) ? 0 : rows8_values_bytes(M, K) + (size_t)M * (size_t)ld8s(K);
+}
+
+// the two products: rows of K columns against N rows of 8-bit weights
+static int32_t linear8(const char* w, const void* x, int32_t x_type, int64_t ldx, const uint8_t* x_scales, int32_t M, int32_t K, int32_t N,
+                       const void* values, const uint8_t* scales, Gemm8Desc& g, int32_t y_type, void* workspace, size_t workspace_bytes,
+                       void* stream) {
+  if (!known_type(y_type) || (!x_scales && !known_type(x_type)) || M < 0 || K < 1 || N < 1)
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: types %d and %d, M %d, in or out < 1", w, x_type, y_type, M);
+  if (!aligned16(values) || !aligned4(scales)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: values or scales is NULL or misaligned", w);
+  if ((g.bias && !aligned4(g.bias)) || (g.aux && !aligned16(g.aux)) || (g.res && !aligned16(g.res)))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: bias, u or res is misaligned", w);
+  if (M == 0) return BSR_OK;
+  if (!aligned16(g.C)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: the result is NULL or not 16-byte aligned", w);
+  if (x_scales ? !aligned16(x) || !aligned4(x_scales) : !rows_ok(x, x_type, ldx, K))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: the rows are NULL, misaligned or closer than %d", w, K);
+  g.M = M; g.K = K; g.N = N; g.ldc = N; g.out_f32 = y_type == BSR_FP32;
+  g.A = x; g.a_scale = x_scales; g.B = values; g.b_scale = scales;
+  if (!x_scales && gemm8_few_takes(M)) {
+    g.a_type = x_type == BSR_FP32 ? 1 : 0;
+    g.lda = ldx;
+  } else if (!x_scales) {
+    const size_t need = bsr_linear8_workspace_bytes(M, K);
+    if (!aligned16(workspace) || workspace_bytes < need)
+      return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: workspace NULL, misaligned or of %zu bytes, %zu are needed", w, workspace_bytes, need);
+    uint8_t* s8 = (uint8_t*)workspace + rows8_values_bytes(M, K);
+    quantize8_rows(x, x_type == BSR_FP32, M, K, ldx, workspace, s8, (hipStream_t)stream);
+    g.A = workspace;
+    g.a_scale = s8;
+  }
+  gemm8(g, (hipStream_t)stream);
+  return check_hip(nullptr, w);
+}
+
+int32_t bsr_linear8_forward(const void* x, int32_t x_type, int64_t ldx, const uint8_t* x_scales, int32_t M, int32_t in, int32_t out,
+                            const void* values, const uint8_t* scales, const float* bias, int32_t act, void* u_out, const void* res, void* y,
+                            int32_t y_type, void* workspace, size_t workspace_bytes, void* stream) {
+  if (act != 0 && act != 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "bsr_linear8_forward: act %d (0: none, 1: GELU)", act);
+  Gemm8Desc g;
+  g.bias = bias; g.act = act ? ACT_GELU : ACT_NONE; g.aux = act ? u_out : nullptr; g.res = res; g.C = y;
+  return linear8("bsr_linear8_forward", x, x_type, ldx, x_scales, M, in, out, values, scales, g, y_type, workspace, workspace_bytes, stream);
+}
+
+int32_t bsr_linear8_dgrad(const void* dy, int32_t dy_type, int64_t lddy, const uint8_t* dy_scales, int32_t M, int32_t in, int32_t out,
+                          const void* values_back, const uint8_t* scales_back, const void* u, void* dx, int32_t dx_type, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  Gemm8Desc g;
+  g.act = u ? ACT_GELU_BWD : ACT_NONE; g.aux = const_cast<void*>(u); g.C = dx;
+  return linear8("bsr_linear8_dgrad", dy, dy_type, lddy, dy_scales, M, out, in, values_back, scales_back, g, dx_type, workspace, workspace_bytes, stream);
+}
+
+// fills everything but the outputs
+static int32_t distill_args(const char* w, DistillArgs& a, const void* z, int32_t type, int64_t rows, int32_t classes, int64_t ldz, const int32_t* index,
+                            int64_t ldi, const void* logits, int32_t logits_type, int64_t ldt, int32_t top, const int32_t* labels,
+                            float temperature, float hard_weight, const float* row_grad, float grad_scale, void* dz, int64_t ldd) {
+  if (!known_type(type) || !known_type(logits_type) || rows < 0 || rows > INT32_MAX || classes < 1 || top < 1 || top > DISTILL_MAX_TOP)
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: types %d and %d, rows %lld, classes %d, top %d (1 .. %d)", w, type, logits_type, (long long)rows, classes, top,
+                DISTILL_MAX_TOP);
+  if (!(temperature > 0.f) || !(temperature <= 3.4e38f) || !(hard_weight >= 0.f && hard_weight <= 1.f))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: temperature %g, hard_weight %g", w, temperature, hard_weight);
+  if (rows > 0 && (!rows_ok(z, type, ldz, classes) || !rows_ok(index, BSR_FP32, ldi, top) || !rows_ok(logits, logits_type, ldt, top) ||
+                   (dz && !rows_ok(dz, type, ldd, classes))))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: z, index, logits or dz is NULL, misaligned or has rows too close", w);
+  if (rows > 0 && dz == z && ldd != ldz) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dz in the place of z needs its stride", w);
+  if ((labels && !aligned4(labels)) || (row_grad && !aligned4(row_grad))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: labels or row_grad is misaligned", w);
+  a.z = z; a.f32 = type == BSR_FP32; a.rows = rows; a.classes = classes; a.ldz = ldz; a.index = index; a.ldi = ldi;
+  a.top = logits; a.top_f32 = logits_type == BSR_FP32; a.ldt = ldt; a.k = top; a.labels = labels; a.temperature = temperature; a.hard = hard_weight;
+  a.row_grad = row_grad; a.grad_scale = grad_scale; a.dz = dz; a.ldd = ldd;
+  return BSR_OK;
+}
+
+int32_t bsr_distill_forward(const void* z, int32_t type, int64_t rows, int32_t classes, int64_t ldz, const int32_t* index, int64_t ldi,
+                            const void* logits, int32_t logits_type, int64_t ldt, int32_t top, const int32_t* labels, float temperature,
+                            float hard_weight, float* loss, float* stats, const float* row_grad, float grad_scale, void* dz, int64_t ldd,
+                            void* stream) {
+  DistillArgs a;
+  const int32_t rc = distill_args("bsr_distill_forward", a, z, type, rows, classes, ldz, index, ldi, logits, logits_type, ldt, top, labels, temperature,
+                                  hard_weight, row_grad, grad_scale, dz, ldd);
+  if (rc != BSR_OK) return rc;
+  if (rows > 0 && !loss && !stats && !dz) return fail(nullptr, BSR_ERR_INVALID_ARG, "bsr_distill_forward: nothing asked for");
+  if ((loss && !aligned4(loss)) || (stats && !aligned4(stats))) return fail(nullptr, BSR_ERR_INVALID_ARG, "bsr_distill_forward: loss or stats is misaligned");
+  if (rows == 0) return BSR_OK;
+  a.loss = loss; a.stats = stats;
+  distill_forward(a, (hipStream_t)stream);
+  return check_hip(nullptr, "bsr_distill_forward");
+}
+
+int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t classes, int64_t ldz, const int32_t* index, int64_t ldi,
+                             const void* logits, int32_t logits_type, int64_t ldt, int32_t top, const int32_t* labels, float temperature,
+                             float hard_weight, const float* stats, const float* row_grad, float grad_scale, void* dz, int64_t ldd,
+                             void* stream) {
+  DistillArgs a;
+  const int32_t rc = distill_args("bsr_distill_backward", a, z, type, rows, classes, ldz, index, ldi, logits, logits_type, ldt, top, labels, temperature,
+                                  hard_weight, row_grad, grad_scale, dz, ldd);
+  if (rc != BSR_OK) return rc;
+  if (rows > 0 && (!aligned4(stats) || !dz)) return fail(nullptr, BSR_ERR_INVALID_ARG, "bsr_distill_backward: stats or dz is NULL or misaligned");
+  if (rows == 0) return BSR_OK;
+  a.stats = const_cast<float*>(stats);
+  distill_backward(a, (hipStream_t)stream);
+  return check_hip(nullptr, "bsr_distill_backward");
 }
 
 const char* bsr_last_error(const bsr_ctx* c) { return c ? c->err : g_err; }

@@ -1,0 +1,60 @@
+// What the matrix-product kernels share: GELU, compile-time loops, the LDS chunk swizzle, the order of tiles over the XCDs, waits.
+#pragma once
+#include <utility>
+
+#include "bsr_internal.h"
+
+namespace bsr {
+
+constexpr int NXCD = 8;
+
+// GELU(u) = u Phi(u) and its derivative Phi(u) + u phi(u) with the exact (erf) Phi.  erf comes from
+// the rational-exponential form of Abramowitz & Stegun 7.1.26, |error| <= 1.5e-7 (below 1e-6 in
+// fp32 arithmetic): far below the resolution of the bf16 values these epilogues write, at a fraction
+// of the instructions of erff.  Its exp(-x^2) with x = u / sqrt(2) is the Gaussian that phi(u) needs
+// as well.  Its coefficients are halved, so that it is Phi that comes out: exact, and one product of 22 less.
+__device__ inline float phi_as(float u, float& gauss) {
+  const float x = u * 0.70710678118654752f, ax = fabsf(x);
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, ax, 1.0f));
+  float p = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+  p = fmaf(p, t, 0.5f * 1.421413741f);
+  p = fmaf(p, t, 0.5f * -0.284496736f);
+  p = fmaf(p, t, 0.5f * 0.254829592f);
+  gauss = __expf(-ax * ax);
+  return 0.5f + copysignf(fmaf(-p * t, gauss, 0.5f), x);
+}
+__device__ inline float gelu_f(float u) {
+  float gauss;
+  return u * phi_as(u, gauss);
+}
+__device__ inline float gelu_grad_f(float u) {
+  float gauss;
+  const float cdf = phi_as(u, gauss);
+  return fmaf(u * 0.39894228040143268f, gauss, cdf);
+}
+
+template <int V> struct IC { static constexpr int value = V; };   // compile-time flag for generic lambdas
+// f(IC<0>{}), ..., f(IC<N-1>{}): a loop whose index is a compile-time constant in the body
+template <class F, int... I> __device__ __forceinline__ void sfor_impl(F&& f, std::integer_sequence<int, I...>) { (f(IC<I>{}), ...); }
+template <int N, class F> __device__ __forceinline__ void sfor(F&& f) { sfor_impl(f, std::make_integer_sequence<int, N>{}); }
+
+// LDS chunk swizzle: 16 consecutive rows reading the same logical 16-byte chunk hit 16 different
+// (row parity, chunk position) pairs, i.e. all 64 banks once; 8 consecutive rows hit 8 positions.
+__device__ inline int swz(int row) { return (row & 7) ^ ((row >> 3) & 1); }
+
+// Logical tile id of this workgroup: XCD x owns the contiguous range [start(x), start(x+1)).
+__device__ inline int xcd_remap(int pid, int nblocks) {
+  const int base = nblocks / NXCD, rem = nblocks % NXCD;
+  const int x = pid % NXCD, local = pid / NXCD;
+  return x * base + min(x, rem) + local;
+}
+
+template <int N> __device__ __forceinline__ void wait_vmcnt() {
+  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+}
+__device__ __forceinline__ void wait_lgkmcnt0() { __builtin_amdgcn_s_waitcnt(0xF | (0x3 << 14) | (0x7 << 4)); }
+#define BSR_SCHED_FENCE() __builtin_amdgcn_sched_barrier(0)
+#define BSR_GLOBAL_PTR(p) ((const void __attribute__((address_space(1)))*)(p))
+#define BSR_LDS_VOID(p) ((void __attribute__((address_space(3)))*)(p))
+
+}  // namespace bsr

@@ -1,0 +1,497 @@
+// Products of 8-bit operands with a scale for each block of 128 (fp8.h): forward and input gradient of frozen linear layers.
+//
+// C(m,n) = epilogue(sum over blocks b of 2^(ea(m,b) + eb(n/128,b)) sum_{k in b} A(m,k) B(n,k)), fp32 accumulation, in
+// v_mfma_scale_f32_32x32x64_f8f6f4 (16x16x128 for few rows), which multiplies by the scales of its operands on the way: a scale is a byte that
+// each lane passes for its row.  A k-tile is one block of 128, so the bytes of a tile row (128) and the LDS layout are those of the bf16
+// products with their k-tiles of 64, and so is the way operands come: straight from global memory into LDS.  Any order of k within a block
+// is as good as another as long as both operands use it, the scale being one for all of it.
+//
+// How exactly that adds up (measured, one large product among small ones in an instruction): of the products that the 8-bit instructions add at
+// a time, those smaller than 2^-13 of the largest are cut to nothing and the others to that place; between such groups, and to the accumulator, the sum is fp32.
+// The result is off by about 3e-5 of its size, whatever K.  The bf16 instructions add the same products (exact in bf16: an e4m3 value times a
+// power of two is one) to 24 bits, at half the rate.  So there are two forms: EXACT brings the operands to bf16 on the way from LDS to the
+// instruction, for fp32 results, and for bf16 results of short sums (K < EXACT_BELOW), where an fp32 sum would be closer than the cut; longer sums for bf16 results
+// take the 8-bit instructions, whose error is then below the bound of an fp32 sum in any order (K 2^-24 sum |a b|) and 60 times below the rounding of the result.
+#include <algorithm>
+
+#include "fp8.h"
+#include "gemm_common.h"
+
+namespace bsr {
+
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> struct Eight;
+template <> struct Eight<bf16> {
+  bf16x8 v;
+  __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
+};
+template <> struct Eight<float> {
+  f32x4 lo, hi;
+  __device__ __forceinline__ float operator[](int i) const { return i < 4 ? lo[i] : hi[i - 4]; }
+};
+// up to eight consecutive values (n of them exist); vec: the address is aligned to 16 bytes and all eight exist
+template <typename T> __device__ __forceinline__ void get8(const T* p, int n, bool vec, float (&o)[8]) {
+  if (vec) {
+    const Eight<T> e = *(const Eight<T>*)p;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = e[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = i < n ? (float)p[i] : 0.f;
+  }
+}
+template <typename T> __device__ __forceinline__ void put8(T* p, int n, bool vec, const float (&v)[8]) {
+  if (vec) {
+    if constexpr (sizeof(T) == 2) {
+      bf16x8 o;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = (bf16)v[i];
+      *(bf16x8*)p = o;
+    } else {
+      *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+      *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = (T)v[i];
+  }
+}
+
+// bias, GELU (with its stored input) or GELU', residual on eight columns of row m, and out
+template <typename T, int ACT>
+__device__ __forceinline__ void finish8b(const Gemm8Desc& g, float (&v)[8], int64_t m, int col, bool vec) {
+  const int n = g.N - col;
+  vec = vec && n >= 8;
+  const int64_t at = m * g.ldc + col;
+  if (g.bias) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += i < n ? g.bias[col + i] : 0.f;
+  }
+  if (ACT == ACT_GELU) {
+    if (g.aux) put8((T*)g.aux + at, n, vec, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = gelu_f(v[i]);
+  } else if (ACT == ACT_GELU_BWD) {
+    float u[8];
+    get8((const T*)g.aux + at, n, vec, u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= gelu_grad_f(u[i]);
+  }
+  if (g.res) {
+    float r[8];
+    get8((const T*)g.res + at, n, vec, r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += r[i];
+  }
+  put8((T*)g.C + at, n, vec, v);
+}
+
+constexpr int EXACT_BELOW = 768;
+
+// eight e4m3 values (two dwords) times the power of two whose E8M0 byte is s8: exact in bf16
+__device__ __forceinline__ bf16x8 widen8(int lo, int hi, int s8) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const float s = __uint_as_float((unsigned)s8 << 23);
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ __forceinline__ i32x8 join8(i32x4 a, i32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// Block tile BM x BN x 128, WM x WN wavefronts, NST stages of LDS.  The weights are the first operand of the instruction, so an accumulator
+// holds the transposed output tile: lane l owns output row l % 32 and four runs of four columns.
+// A stage is (BM + BN) rows of 128 bytes (eight chunks of 16, chunk c of row r in slot c ^ swz(r)) and behind them a dword of scales for
+// each row: the scales of four k-tiles, of which each k-tile reads its byte (each k-tile fetches the dword anew, 1/32 more bytes, so that
+// every k-tile is the same number of loads and can be waited for by count).
+template <int BM, int BN, int WM, int WN, int NST, typename T, int ACT, bool EXACT>
+__global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, const void* hB, const void* hsa, const void* hsb, int hM, int hN, int hK,
+                                                                int tiles, Gemm8Desc g) {
+  constexpr int NW = WM * WN, NT = NW * 64, ROWS = BM + BN;
+  constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 32, NI = TN / 32, NMF = MI * NI, NFR = MI + NI;
+  constexpr int RPI = NT / 8;                        // tile rows that a load instruction of the workgroup fills
+  constexpr int AL = BM / RPI, BL = BN / RPI;
+  constexpr int SL = (ROWS + NT - 1) / NT;           // scale loads of a thread
+  constexpr int LPT = AL + BL + SL;
+  constexpr int SCALES = ROWS * 128;                 // where the scales of a stage start
+  constexpr int STAGE = SCALES + SL * NT * 4;
+  static_assert(BM % RPI == 0 && BN % RPI == 0 && RPI % 16 == 0, "a load instruction covers whole groups of 16 rows");
+  static_assert(NST >= 2 && NST <= 4 && (NST - 1) * LPT <= 60, "vmcnt has 6 bits");
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int M = hM, N = hN;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  const int tile = xcd_remap(blockIdx.x, tiles);
+  const int ntn = (N + BN - 1) / BN;
+  const int m0 = tile / ntn * BM, n0 = tile % ntn * BN;
+  const int nk = (hK + BLOCK8 - 1) / BLOCK8;
+  const unsigned ld = (unsigned)nk * BLOCK8, lds = (unsigned)(nk + 3) / 4 * 4;
+  const uint8_t* __restrict__ A = (const uint8_t*)hA + (int64_t)m0 * ld;
+  const uint8_t* __restrict__ B = (const uint8_t*)hB + (int64_t)n0 * ld;
+
+  // rows past the end repeat the last one: they only feed accumulators that are never stored
+  const int lrow = tid >> 3, chunk = ((tid & 7) ^ swz(lrow)) * 16;
+  unsigned off[AL + BL];
+#pragma unroll
+  for (int i = 0; i < AL; ++i) off[i] = (unsigned)(min(m0 + i * RPI + lrow, M - 1) - m0) * ld + chunk;
+#pragma unroll
+  for (int i = 0; i < BL; ++i) off[AL + i] = (unsigned)(min(n0 + i * RPI + lrow, N - 1) - n0) * ld + chunk;
+  const uint8_t* soff[SL];
+#pragma unroll
+  for (int i = 0; i < SL; ++i) {
+    const int r = i * NT + tid;
+    soff[i] = r < BM ? (const uint8_t*)hsa + (int64_t)min(m0 + r, M - 1) * lds
+                     : (const uint8_t*)hsb + (int64_t)(min(n0 + r - BM, N - 1) / BLOCK8) * lds;
+  }
+  auto issue1 = [&](auto I, int kt, int st) __attribute__((always_inline)) {
+    constexpr int i = decltype(I)::value;
+    unsigned char* base = smem + st * STAGE;
+    if constexpr (i < AL + BL) {
+      const uint8_t* src = (i < AL ? A : B) + (size_t)kt * BLOCK8;
+      unsigned char* dst = base + wave * 1024 + (i < AL ? i * RPI * 128 : BM * 128 + (i - AL) * RPI * 128);
+      __builtin_amdgcn_global_load_lds(BSR_GLOBAL_PTR(src + off[i]), BSR_LDS_VOID(dst), 16, 0, 0);
+    } else {
+      constexpr int j = i - AL - BL;
+      __builtin_amdgcn_global_load_lds(BSR_GLOBAL_PTR(soff[j] + (kt & ~3)), BSR_LDS_VOID(base + SCALES + (j * NT + wave * 64) * 4), 4, 0, 0);
+    }
+  };
+
+  f32x16 acc[MI][NI];
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[mi][ni][r] = 0.f;
+
+  // fragments in the order A0, B0 .. B(NI-1), A1 .. A(MI-1)
+  const int lr = lane & 31, lh = lane >> 5, sw = swz(lr);
+  int rowj[NFR];
+#pragma unroll
+  for (int j = 0; j < NFR; ++j) {
+    const bool isA = j == 0 || j > NI;
+    const int idx = j == 0 ? 0 : (j <= NI ? j - 1 : j - NI);
+    rowj[j] = isA ? wm * TM + idx * 32 + lr : BM + wn * TN + idx * 32 + lr;
+  }
+  i32x8 fr[2][NFR];
+  bf16x8 wide[EXACT ? NFR : 1][4];
+  int sc[NFR], scn[NFR];
+  auto widen = [&](auto SET) __attribute__((always_inline)) {
+    constexpr int set = decltype(SET)::value;
+    if constexpr (EXACT)
+#pragma unroll
+      for (int j = 0; j < NFR; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) wide[j][q] = widen8(fr[set][j][2 * q], fr[set][j][2 * q + 1], sc[j]);
+  };
+  auto rd1 = [&](auto SET, auto J, int st, int ks) __attribute__((always_inline)) {
+    constexpr int set = decltype(SET)::value, j = decltype(J)::value;
+    const unsigned char* p = smem + st * STAGE + rowj[j] * 128;
+    fr[set][j] = join8(*(const i32x4*)(p + (((ks * 4 + lh) ^ sw) << 4)), *(const i32x4*)(p + (((ks * 4 + 2 + lh) ^ sw) << 4)));
+  };
+  auto rds = [&](auto J, int st, int kt) __attribute__((always_inline)) {
+    constexpr int j = decltype(J)::value;
+    scn[j] = smem[st * STAGE + SCALES + rowj[j] * 4 + (kt & 3)];
+  };
+  auto mf1 = [&](auto SET, auto J) __attribute__((always_inline)) {
+    constexpr int set = decltype(SET)::value, j = decltype(J)::value, mi = j / NI, ni = j % NI;
+    constexpr int ja = mi == 0 ? 0 : NI + mi, jb = 1 + ni;
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide[jb][q], wide[ja][q], acc[mi][ni], 0, 0, 0);
+    } else {
+      acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fr[set][jb], fr[set][ja], acc[mi][ni], 0, 0, 0, sc[jb], 0, sc[ja]);
+    }
+  };
+  constexpr int PRE = NMF >= 8 ? 2 : 1;              // MFMAs of the second k-step in front of the barrier
+  constexpr int POST = NMF - PRE;
+  constexpr int SPAN = POST + (NST > 2 && NMF >= 4 ? NMF : 0);       // MFMAs that the loads of a k-tile are spread over
+  constexpr bool LATE = SPAN > POST;                 // some follow in the next k-tile
+  auto loads_at = [&](auto P, int kt, int st) __attribute__((always_inline)) {
+    constexpr int p = decltype(P)::value, lo = p >= SPAN ? LPT : (p * LPT + SPAN - 1) / SPAN, hi = p + 1 >= SPAN ? LPT : ((p + 1) * LPT + SPAN - 1) / SPAN;
+    sfor<hi - lo>([&](auto L) __attribute__((always_inline)) { issue1(IC<lo + decltype(L)::value>{}, kt, st); });
+  };
+  // the first k-step of a k-tile: MFMAs on set 0, the fragments of the second into set 1
+  auto kfirst = [&](auto LOADS, int st, int ktl, int stl) __attribute__((always_inline)) {
+    constexpr int RPM = (NFR + NMF - 1) / NMF;
+    widen(IC<0>{});
+    sfor<NMF>([&](auto J) __attribute__((always_inline)) {
+      constexpr int j = decltype(J)::value;
+      mf1(IC<0>{}, J);
+      sfor<RPM>([&](auto R) __attribute__((always_inline)) {
+        constexpr int r = j * RPM + decltype(R)::value;
+        if constexpr (r < NFR) rd1(IC<1>{}, IC<r>{}, st, 1);
+      });
+      if constexpr (decltype(LOADS)::value) loads_at(IC<POST + j>{}, ktl, stl);
+      BSR_SCHED_FENCE();
+    });
+  };
+  // the second, with the barrier.  VMW >= 0: loads that may stay in flight there (steady state, those of k-tile kt + NST follow it); VMW < 0:
+  // nothing is issued any more and the count follows from rem, the k-tiles behind this one
+  auto klast = [&](auto VMW, int kt, int st, int stn, int rem) __attribute__((always_inline)) {
+    constexpr int vmw = decltype(VMW)::value;
+    constexpr int RPP = (NFR + POST - 1) / POST;
+    if constexpr (EXACT) { wait_lgkmcnt0(); widen(IC<1>{}); }
+    sfor<PRE>([&](auto J) __attribute__((always_inline)) { mf1(IC<1>{}, J); BSR_SCHED_FENCE(); });
+    wait_lgkmcnt0();
+    if constexpr (vmw >= 0) wait_vmcnt<vmw>();
+    else if (rem >= 3) wait_vmcnt<2 * LPT>();
+    else if (rem == 2) wait_vmcnt<LPT>();
+    else wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();
+    BSR_SCHED_FENCE();
+    sfor<POST>([&](auto P) __attribute__((always_inline)) {
+      constexpr int p = decltype(P)::value;
+      mf1(IC<1>{}, IC<PRE + p>{});
+      sfor<RPP>([&](auto R) __attribute__((always_inline)) {
+        constexpr int r = p * RPP + decltype(R)::value;
+        if constexpr (r < NFR) { rds(IC<r>{}, stn, kt + 1); rd1(IC<0>{}, IC<r>{}, stn, 0); }
+      });
+      if constexpr (vmw >= 0) loads_at(P, kt + NST, st);
+      BSR_SCHED_FENCE();
+    });
+#pragma unroll
+    for (int j = 0; j < NFR; ++j) sc[j] = scn[j];
+  };
+
+#pragma unroll
+  for (int j = 0; j < NST; ++j)
+    if (j < nk) sfor<LPT>([&](auto I) __attribute__((always_inline)) { issue1(I, j, j); });
+  {
+    const int fl = min(nk, NST) - 1;
+    if (fl >= 3) wait_vmcnt<3 * LPT>(); else if (fl == 2) wait_vmcnt<2 * LPT>(); else if (fl == 1) wait_vmcnt<LPT>(); else wait_vmcnt<0>();
+  }
+  __builtin_amdgcn_s_barrier();
+  sfor<NFR>([&](auto J) __attribute__((always_inline)) { rds(J, 0, 0); rd1(IC<0>{}, J, 0, 0); });
+#pragma unroll
+  for (int j = 0; j < NFR; ++j) sc[j] = scn[j];
+  int st = 0, kt = 0;
+  auto ktile = [&](auto LOADS, auto VMW) __attribute__((always_inline)) {
+    const int stn = (st + 1 == NST) ? 0 : st + 1, stl = st == 0 ? NST - 1 : st - 1;
+    kfirst(LOADS, st, kt + NST - 1, stl);
+    klast(VMW, kt, st, stn, nk - 1 - kt);
+    st = stn;
+    ++kt;
+  };
+  constexpr IC<(NST - 2) * LPT> steady{};
+  if constexpr (LATE) {
+    if (kt + NST < nk) ktile(IC<0>{}, steady);                    // (the prologue's loads are all out)
+    while (kt + NST < nk) ktile(IC<1>{}, steady);
+    if (kt > 0) ktile(IC<1>{}, IC<-1>{});                         // the last late loads
+  } else {
+    while (kt + NST < nk) ktile(IC<0>{}, steady);
+  }
+  while (kt < nk) ktile(IC<0>{}, IC<-1>{});                       // nothing left to issue
+  // every wavefront is past the last barrier: the stages are free.  32 rows at a time go through a patch of the wavefront's own and come back with
+  // a lane owning eight columns of a row
+  constexpr int LDP = TN + 4, CPR = TN / 8, RPP = 64 / CPR, NPASS = 32 / RPP;
+  float* patch = (float*)smem + wave * 32 * LDP;
+  const bool vec = g.ldc * (int64_t)sizeof(T) % 16 == 0;
+  const int col = n0 + wn * TN + lane % CPR * 8;
+#pragma nounroll
+  for (int mi = 0; mi < MI; ++mi) {
+    sfor<MI>([&](auto I) __attribute__((always_inline)) {
+      constexpr int i = decltype(I)::value;
+      if (mi == i)
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+          for (int rg = 0; rg < 4; ++rg)
+            *(f32x4*)(patch + lr * LDP + ni * 32 + 8 * rg + 4 * lh) =
+                f32x4{acc[i][ni][4 * rg], acc[i][ni][4 * rg + 1], acc[i][ni][4 * rg + 2], acc[i][ni][4 * rg + 3]};
+    });
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int p = 0; p < NPASS; ++p) {
+      const int r = p * RPP + lane / CPR, m = m0 + wm * TM + mi * 32 + r;
+      float v[8];
+      const float* src = patch + r * LDP + lane % CPR * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = src[i];
+      if (m < M && col < N) finish8b<T, ACT>(g, v, m, col, vec);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Few rows: what counts is that the weights come once and at once.  A workgroup owns 16 columns and all rows (16 MI of them); its eight
+// wavefronts share the k-tiles, each with its own straight from global memory into registers (a weight row's 128 bytes of a k-tile are a
+// cache line that four lanes read whole), and their sums meet in LDS in wavefront order.  Rows of bf16 or fp32 are brought to 8 bits here
+// by every workgroup for itself: they are few, and it saves the launch.
+constexpr int FEW_WAVES = 8, FEW_ROWS = 64;
+template <typename TX, int MI, typename T, int ACT, bool EXACT>
+__global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void* hA, const void* hB, const void* hsa, const void* hsb, int hM, int hN,
+                                                                      int hK, int64_t lda, bool vec_x, Gemm8Desc g) {
+  constexpr bool E4 = sizeof(TX) == 1;
+  __shared__ float part[FEW_WAVES][MI * 16][16 + 1];
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = blockIdx.x * 16;
+  const int nk = (hK + BLOCK8 - 1) / BLOCK8;
+  const int64_t ld = (int64_t)nk * BLOCK8, lds = (nk + 3) / 4 * 4;
+  const uint8_t* wrow = (const uint8_t*)hB + (int64_t)min(n0 + lr, hN - 1) * ld + lg * 32;
+  const uint8_t* wscale = (const uint8_t*)hsb + (int64_t)(n0 / BLOCK8) * lds;       // (16 columns lie in one block)
+  f32x4 acc[MI];
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi) acc[mi] = f32x4{0.f, 0.f, 0.f, 0.f};
+  constexpr int AHEAD = 4;
+  for (int kt0 = wave; kt0 < nk; kt0 += FEW_WAVES * AHEAD) {
+    i32x8 w[AHEAD];
+    int ws[AHEAD];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int kt = min(kt0 + a * FEW_WAVES, nk - 1);
+      w[a] = join8(*(const i32x4*)(wrow + (int64_t)kt * BLOCK8), *(const i32x4*)(wrow + (int64_t)kt * BLOCK8 + 16));
+      ws[a] = wscale[kt];
+    }
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int kt = kt0 + a * FEW_WAVES;
+      if (kt < nk) {
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+          const int64_t m = min(mi * 16 + lr, hM - 1);
+          i32x8 x;
+          int xs;
+          if constexpr (E4) {
+            const uint8_t* p = (const uint8_t*)hA + m * ld + (int64_t)kt * BLOCK8 + lg * 32;
+            x = join8(*(const i32x4*)p, *(const i32x4*)(p + 16));
+            xs = ((const uint8_t*)hsa)[m * lds + kt];
+          } else {
+            const int k0 = kt * BLOCK8 + lg * 32;
+            const TX* p = (const TX*)hA + m * lda + k0;
+            float v[32];
+            if (vec_x && k0 + 32 <= hK) {
+              constexpr int V = Chunk<TX>::V;
+              typename Chunk<TX>::vec raw[32 / V];
+#pragma unroll
+              for (int i = 0; i < 32 / V; ++i) raw[i] = *(const typename Chunk<TX>::vec*)(p + i * V);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = (float)raw[i / V][i % V];
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = k0 + i < hK ? (float)p[i] : 0.f;
+            }
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) most = max(most, finite_bits(v[i]));
+            most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+            most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+            xs = (int)scale8_of(most);
+            const float inv = inverse_of(xs);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (int)pack8(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+          }
+          if constexpr (EXACT) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              acc[mi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[a][2 * q], w[a][2 * q + 1], ws[a]), widen8(x[2 * q], x[2 * q + 1], xs), acc[mi], 0, 0, 0);
+          } else {
+            acc[mi] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[a], x, acc[mi], 0, 0, 0, ws[a], 0, xs);
+          }
+        }
+      }
+    }
+  }
+  // lane l holds columns 4 (l / 16) .. + 3 of row l % 16
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) part[wave][mi * 16 + lr][4 * lg + e] = acc[mi][e];
+  __syncthreads();
+  for (int i = tid; i < MI * 16 * 16; i += FEW_WAVES * 64) {
+    const int m = i / 16, col = n0 + i % 16;
+    if (m >= hM || col >= hN) continue;
+    float v = part[0][m][i % 16];
+#pragma unroll
+    for (int w = 1; w < FEW_WAVES; ++w) v += part[w][m][i % 16];
+    const int64_t at = (int64_t)m * g.ldc + col;
+    if (g.bias) v += g.bias[col];
+    if (ACT == ACT_GELU) {
+      if (g.aux) ((T*)g.aux)[at] = (T)v;
+      v = gelu_f(v);
+    } else if (ACT == ACT_GELU_BWD) {
+      v *= gelu_grad_f((float)((const T*)g.aux)[at]);
+    }
+    if (g.res) v += (float)((const T*)g.res)[at];
+    ((T*)g.C)[at] = (T)v;
+  }
+}
+
+template <int BM, int BN, int WM, int WN, int NST, typename T, int ACT, bool EXACT>
+void launch_tiled(const Gemm8Desc& g, hipStream_t s) {
+  constexpr int NT = WM * WN * 64;
+  constexpr size_t stages = (size_t)NST * ((BM + BN) * 128 + (BM + BN + NT - 1) / NT * NT * 4);
+  constexpr size_t patches = (size_t)WM * WN * 32 * (BN / WN + 4) * 4;
+  static_assert(patches <= stages && stages <= 160 * 1024, "the epilogue patches live in the stages");
+  auto kern = gemm8_kernel<BM, BN, WM, WN, NST, T, ACT, EXACT>;
+  static bool attr_set = false;
+  if (!attr_set) {
+    (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)stages);
+    attr_set = true;
+  }
+  const int tiles = (int)((int64_t)((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN));
+  kern<<<tiles, NT, stages, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, tiles, g);
+}
+
+template <typename T, int ACT, bool EXACT>
+void tiled(const Gemm8Desc& g, hipStream_t s) {
+  const int64_t big = (int64_t)((g.M + 255) / 256) * ((g.N + 255) / 256), mid = (int64_t)((g.M + 127) / 128) * ((g.N + 127) / 128);
+  if constexpr (!EXACT)
+    if (big >= 256) return launch_tiled<256, 256, 2, 4, 2, T, ACT, false>(g, s);
+  if (mid >= 128) launch_tiled<128, 128, 2, 2, 3, T, ACT, EXACT>(g, s);
+  else launch_tiled<64, 64, 2, 1, 4, T, ACT, EXACT>(g, s);
+}
+
+template <typename TX, typename T, int ACT, bool EXACT>
+void few(const Gemm8Desc& g, hipStream_t s) {
+  const unsigned grid = (unsigned)((g.N + 15) / 16);
+  const int64_t lda = g.lda;
+  const bool vec = ((uintptr_t)g.A & 15) == 0 && lda * (int64_t)sizeof(TX) % 16 == 0;
+  auto go = [&](auto MI) {
+    gemm8_few_kernel<TX, decltype(MI)::value, T, ACT, EXACT><<<grid, FEW_WAVES * 64, 0, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, lda, vec, g);
+  };
+  if (g.M <= 16) go(IC<1>{});
+  else if (g.M <= 32) go(IC<2>{});
+  else go(IC<4>{});
+}
+
+template <typename T, int ACT, bool EXACT>
+void run(const Gemm8Desc& g, hipStream_t s) {
+  if (g.M > FEW_ROWS) tiled<T, ACT, EXACT>(g, s);
+  else if (g.a_type == 0) few<bf16, T, ACT, EXACT>(g, s);
+  else if (g.a_type == 1) few<float, T, ACT, EXACT>(g, s);
+  else few<uint8_t, T, ACT, EXACT>(g, s);
+}
+
+template <int ACT>
+void run_type(const Gemm8Desc& g, hipStream_t s) {
+  if (g.out_f32) run<float, ACT, true>(g, s);
+  else if (g.K < EXACT_BELOW) run<bf16, ACT, true>(g, s);
+  else run<bf16, ACT, false>(g, s);
+}
+
+}  // namespace
+
+bool gemm8_few_takes(int64_t M) { return M <= FEW_ROWS; }
+
+void gemm8(const Gemm8Desc& g, hipStream_t s) {
+  if (g.M <= 0) return;
+  if (g.act == ACT_GELU) run_type<ACT_GELU>(g, s);
+  else if (g.act == ACT_GELU_BWD) run_type<ACT_GELU_BWD>(g, s);
+  else run_type<ACT_NONE>(g, s);
+}
+
+}  // namespace bsr

@@ -1,0 +1,129 @@
+// Rows and weight matrices brought to 8 bits (fp8.h).  Bound by memory: 3 bytes move per bf16 element.
+#include "fp8.h"
+
+namespace bsr {
+
+namespace {
+
+__device__ __forceinline__ uint32_t umax_dpp(uint32_t v, uint32_t o) { return v > o ? v : o; }
+// maximum over each eight lanes (the pairs of eight_sum in rowops.h)
+__device__ __forceinline__ uint32_t eight_max(uint32_t v) {
+  v = umax_dpp(v, __float_as_uint(dpp_move<0xB1>(__uint_as_float(v))));
+  v = umax_dpp(v, __float_as_uint(dpp_move<0x4E>(__uint_as_float(v))));
+  return umax_dpp(v, __float_as_uint(dpp_move<0x141>(__uint_as_float(v))));
+}
+
+// Eight lanes take a block, 16 elements each; blocks count row after row, the padding of the scales included, so that a wavefront's
+// scales are consecutive bytes.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void quantize8_rows_kernel(const T* __restrict__ x, int64_t blocks, int K, int64_t ldx, int per_row,
+                                                             int real_blocks, uint8_t* __restrict__ q, uint8_t* __restrict__ scale) {
+  const int64_t b = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
+  if (b >= blocks) return;
+  const int64_t row = b / per_row;
+  const int kb = (int)(b - row * per_row), part = threadIdx.x & 7, k0 = kb * BLOCK8 + part * 16;
+  float v[16];
+  const T* src = x + row * ldx + k0;
+  if (VEC && k0 + 16 <= K) {
+    constexpr int V = Chunk<T>::V;
+    typename Chunk<T>::vec raw[16 / V];
+#pragma unroll
+    for (int i = 0; i < 16 / V; ++i) raw[i] = *(const typename Chunk<T>::vec*)(src + i * V);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = (float)raw[i / V][i % V];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = k0 + i < K ? (float)src[i] : 0.f;
+  }
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) most = umax_dpp(most, finite_bits(v[i]));
+  const uint32_t s8 = scale8_of(eight_max(most));
+  if (kb < real_blocks) {
+    const float inv = inverse_of(s8);
+    *(uint4*)(q + row * (int64_t)real_blocks * BLOCK8 + k0) =
+        make_uint4(pack8(v[0], v[1], v[2], v[3], inv), pack8(v[4], v[5], v[6], v[7], inv), pack8(v[8], v[9], v[10], v[11], inv),
+                   pack8(v[12], v[13], v[14], v[15], inv));
+  }
+  if (part == 0) scale[b] = (uint8_t)s8;
+}
+
+// A workgroup per block: thread t holds 64 columns of row t / 2; the transposed copy goes through LDS.  Once per weight matrix.
+template <typename T>
+__global__ __launch_bounds__(256) void quantize8_weight_kernel(const T* __restrict__ w, int in, int out, int64_t ldw, uint8_t* __restrict__ q,
+                                                               uint8_t* __restrict__ scale, uint8_t* __restrict__ q_back,
+                                                               uint8_t* __restrict__ scale_back) {
+  __shared__ uint8_t tile[BLOCK8][BLOCK8 + 4];
+  __shared__ uint32_t wave_most[4];
+  const int i0 = blockIdx.y * BLOCK8, n0 = blockIdx.x * BLOCK8;
+  const int r = threadIdx.x >> 1, c0 = (threadIdx.x & 1) * 64;
+  float v[64];
+  uint32_t most = 0;
+  const T* src = w + (int64_t)(i0 + r) * ldw + n0 + c0;
+#pragma unroll
+  for (int c = 0; c < 64; ++c) {
+    v[c] = i0 + r < in && n0 + c0 + c < out ? (float)src[c] : 0.f;
+    most = umax_dpp(most, finite_bits(v[c]));
+  }
+  // bits of non-negative floats order as the floats do
+  most = __float_as_uint(wave_max(__uint_as_float(most)));
+  if ((threadIdx.x & 63) == 0) wave_most[threadIdx.x >> 6] = most;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) most = umax_dpp(most, wave_most[i]);
+  const uint32_t s8 = scale8_of(most);
+  const float inv = inverse_of(s8);
+  const int64_t ldq = ld8(in), ldb = ld8(out), lds = ld8s(in), ldbs = ld8s(out);
+#pragma unroll
+  for (int c = 0; c < 64; c += 4) {
+    const uint32_t p = pack8(v[c], v[c + 1], v[c + 2], v[c + 3], inv);
+    *(uint32_t*)&tile[r][c0 + c] = p;
+    if (q_back && i0 + r < in) *(uint32_t*)(q_back + (int64_t)(i0 + r) * ldb + n0 + c0 + c) = p;
+  }
+  __syncthreads();
+  if (n0 + r < out)
+#pragma unroll
+    for (int c = 0; c < 64; c += 4) {
+      const uint32_t p = tile[c0 + c][r] | (uint32_t)tile[c0 + c + 1][r] << 8 | (uint32_t)tile[c0 + c + 2][r] << 16 |
+                         (uint32_t)tile[c0 + c + 3][r] << 24;
+      *(uint32_t*)(q + (int64_t)(n0 + r) * ldq + i0 + c0 + c) = p;
+    }
+  if (threadIdx.x == 0) {
+    const int bi = blockIdx.y, bn = blockIdx.x;
+    scale[bn * lds + bi] = (uint8_t)s8;
+    if (bi == (int)gridDim.y - 1)
+      for (int64_t p = bi + 1; p < lds; ++p) scale[bn * lds + p] = 127;
+    if (q_back) {
+      scale_back[bi * ldbs + bn] = (uint8_t)s8;
+      if (bn == (int)gridDim.x - 1)
+        for (int64_t p = bn + 1; p < ldbs; ++p) scale_back[bi * ldbs + p] = 127;
+    }
+  }
+}
+
+template <typename T>
+void rows_t(const void* x, int64_t M, int K, int64_t ldx, void* q, uint8_t* scale, hipStream_t s) {
+  const int per_row = (int)ld8s(K), real = (int)(ld8(K) / BLOCK8);
+  const int64_t blocks = M * per_row;
+  const unsigned grid = (unsigned)((blocks * 8 + 255) / 256);
+  const bool vec = ((uintptr_t)x & 15) == 0 && ldx * (int64_t)sizeof(T) % 16 == 0;
+  if (vec) quantize8_rows_kernel<T, true><<<grid, 256, 0, s>>>((const T*)x, blocks, K, ldx, per_row, real, (uint8_t*)q, scale);
+  else quantize8_rows_kernel<T, false><<<grid, 256, 0, s>>>((const T*)x, blocks, K, ldx, per_row, real, (uint8_t*)q, scale);
+}
+
+}  // namespace
+
+void quantize8_rows(const void* x, bool f32, int64_t M, int K, int64_t ldx, void* q, uint8_t* scale, hipStream_t s) {
+  if (M <= 0) return;
+  if (f32) rows_t<float>(x, M, K, ldx, q, scale, s);
+  else rows_t<bf16>(x, M, K, ldx, q, scale, s);
+}
+
+void quantize8_weight(const void* w, bool f32, int in, int out, int64_t ldw, void* q, uint8_t* scale, void* q_back, uint8_t* scale_back,
+                      hipStream_t s) {
+  const dim3 grid((out + BLOCK8 - 1) / BLOCK8, (in + BLOCK8 - 1) / BLOCK8);
+  if (f32) quantize8_weight_kernel<float><<<grid, 256, 0, s>>>((const float*)w, in, out, ldw, (uint8_t*)q, scale, (uint8_t*)q_back, scale_back);
+  else quantize8_weight_kernel<bf16><<<grid, 256, 0, s>>>((const bf16*)w, in, out, ldw, (uint8_t*)q, scale, (uint8_t*)q_back, scale_back);
+}
+
+}  // namespace bsr

@@ -1,0 +1,218 @@
+"""Distillation from a teacher's top logits against 64 bits.
+
+Tolerances, from the arithmetic: exp and log are good to a few 2^-24 plus 2^-24 of the size of their argument, logits here are below 100 in size
+(over the temperature), a sum of positive terms adds less than sqrt(n) 2^-24; so log-sum-exp is good to 3e-5 absolutely at worst, a loss to 1e-4 T^2 and a
+probability to 5e-5 relatively.  bf16 results add 2^-8 relatively."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a HIP device")
+    import paper_2405_10951_amd as P
+    return torch, P
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def log_softmax(z):
+    with np.errstate(all="ignore"):
+        m = z.max(1, keepdims=True)
+        return z - m - np.log(np.exp(z - m).sum(1, keepdims=True))
+
+
+def reference(z, index, t, labels, T, a, g):
+    """(loss [rows], dz, sizes of the numbers that dz is a difference of) row by row from the definition"""
+    rows, n = z.shape
+    loss, dz, size = np.zeros(rows), np.zeros((rows, n)), np.zeros((rows, n))
+    with np.errstate(all="ignore"):
+        for r in range(rows):
+            if (z[r] == -np.inf).all():
+                continue
+            lq, lr = log_softmax(z[r:r + 1] / T)[0], log_softmax(z[r:r + 1])[0]
+            ok = (index[r] >= 0) & (index[r] < n) & (t[r] > -np.inf)
+            if ok.any():
+                lp = log_softmax(t[r][ok][None] / T)[0]
+                p, c = np.exp(lp), index[r][ok]
+                loss[r] += (1 - a) * T * T * sum(pj * (lpj - lq[cj]) for pj, lpj, cj in zip(p, lp, c) if pj > 0)
+                d, q = np.exp(lq), np.zeros(n)
+                np.add.at(q, c, p)
+                dz[r] += g[r] * (1 - a) * T * (d - q)
+                size[r] += abs(g[r]) * (1 - a) * T * (d + q)
+            if a > 0 and labels is not None and 0 <= labels[r] < n:
+                loss[r] += -a * lr[labels[r]]
+                d, q = np.exp(lr), np.zeros(n)
+                q[labels[r]] = 1
+                dz[r] += g[r] * a * (d - q)
+                size[r] += abs(g[r]) * a * (d + q)
+    return loss, dz, size
+
+
+def make(torch, rows, n, k, dtype, seed, extra=0):
+    g = torch.Generator().manual_seed(seed + rows + 7 * n + 131 * k)
+    z = (3 * torch.randn(rows, n + extra, generator=g)).to({"bf16": torch.bfloat16, "f32": torch.float32}[dtype])[:, :n]
+    index = torch.stack([torch.randperm(n, generator=g)[:k] for _ in range(rows)]).to(torch.int32) if n <= 4096 else \
+        torch.randint(n, (rows, k), generator=g, dtype=torch.int32)
+    t = 3 * torch.randn(rows, k, generator=g)
+    labels = torch.randint(n, (rows,), generator=g, dtype=torch.int32)
+    return z.cuda(), index.cuda(), t.cuda(), labels.cuda()
+
+
+def check(torch, P, z, index, t, labels, T, a, dtype, weights=None, scale=1.0):
+    rows = z.shape[0]
+    g = (host(weights) if weights is not None else np.ones(rows)) * scale
+    ref_loss, ref_dz, size = reference(host(z), index.cpu().numpy(), host(t), None if labels is None else labels.cpu().numpy(), T, a, g)
+    how = dict(labels=labels, temperature=T, hard_weight=a)
+    loss, stats = P.bsr_distill_forward(z, index, t, **how)
+    both, dz = P.bsr_distill_forward_backward(z, index, t, row_grad=weights, grad_scale=scale, **how)
+    apart = P.bsr_distill_backward(z, index, t, stats, row_grad=weights, grad_scale=scale, **how)
+    zc = z.clone() if z.is_contiguous() else None
+    assert torch.equal(loss, both) or bool(torch.isnan(loss).any())
+    got = host(loss)
+    fine = np.isfinite(ref_loss)
+    assert np.array_equal(np.isfinite(got), fine) and np.array_equal(got[~fine], ref_loss[~fine], equal_nan=True)
+    assert (np.abs(got - ref_loss)[fine] <= 1e-4 * T * T + 1e-5 * np.abs(ref_loss)[fine]).all()
+    # a difference q - p of nearly equal numbers is as good as the numbers
+    with np.errstate(invalid="ignore"):
+        bound = 1e-4 * size + 1e-30 + (2.0 ** -8 * np.abs(ref_dz) + 1e-38 if dtype == "bf16" else 0)
+        for d, what in ((dz, "with the loss"), (apart, "apart")):
+            bad = ~(np.abs(host(d) - ref_dz) <= bound) & ~(np.isnan(host(d)) & np.isnan(ref_dz))
+            assert not bad.any(), f"dz {what}: {np.argwhere(bad)[:4]}, {host(d)[bad][:4]} for {ref_dz[bad][:4]}"
+    if zc is not None:
+        P.bsr_distill_forward_backward(zc, index, t, row_grad=weights, grad_scale=scale, dz=zc, **how)
+        assert torch.equal(zc.nan_to_num(), dz.nan_to_num())
+        zc = z.clone()
+        P.bsr_distill_backward(zc, index, t, stats, row_grad=weights, grad_scale=scale, dz=zc, **how)
+        assert torch.equal(zc.nan_to_num(), apart.nan_to_num())
+    return loss, dz
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,a", [(1.0, 0.0), (3.0, 0.0), (1.0, 0.4), (2.0, 0.4), (0.5, 1.0)])
+@pytest.mark.parametrize("rows,n,k,extra", [(1, 1, 1, 0), (3, 2, 2, 0), (5, 100, 10, 0), (4, 1000, 100, 24), (3, 1024, 64, 0), (3, 1025, 7, 0), (7, 4099, 33, 2), (2, 8192, 128, 0),
+                                            (3, 21841, 5, 0), (2, 40000, 1024, 8)])
+def test_loss_and_gradient(env, rows, n, k, extra, T, a, dtype):
+    torch, P = env
+    z, index, t, labels = make(torch, rows, n, k, dtype, 0, extra)
+    w = torch.linspace(0.5, 1.5, rows, device="cuda")
+    check(torch, P, z, index, t, labels, T, a, dtype, weights=w, scale=0.25)
+
+
+@pytest.mark.parametrize("n", [131072, 200003])
+def test_vocabularies(env, n):
+    torch, P = env
+    for dtype in ("bf16", "f32"):
+        z, index, t, labels = make(torch, 2, n, 64, dtype, 1)
+        check(torch, P, z, index, t, labels, 2.0, 0.1, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [50, 3001, 30001])
+def test_masks_and_empty_rows(env, n, dtype):
+    """absent entries, entries twice, labels absent, in the list and not, classes at -inf and at the type's lowest value, rows of nothing else, NaN"""
+    torch, P = env
+    rows, k = 16, 6
+    z, index, t, labels = make(torch, rows, n, k, dtype, 2)
+    low = torch.finfo(z.dtype).min
+    index[0, 3:] = -1
+    index[1] = -1
+    index[2, 1] = index[2, 0]                             # twice
+    index[3] = index[3, 0]                                # all the same
+    index[4, 0] = n                                       # outside
+    index[4, 1] = 2 ** 31 - 1
+    t[5, 2] = -float("inf")
+    t[6] = -float("inf")
+    labels[7] = -1
+    labels[8] = index[8, 2]
+    labels[9] = n
+    z[10] = -float("inf")                                 # nothing left
+    z[11] = low                                           # the lowest value everywhere: uniform
+    z[12, 1:] = -float("inf")                             # one class left; the teacher names others
+    index[12], labels[12] = torch.arange(1, k + 1), 0
+    z[13, n // 2:] = low
+    index[13], labels[13] = torch.arange(k), 3
+    z[14, 5] = float("nan")
+    keep = index[15].long().cpu().tolist() + [int(labels[15])]
+    hide = torch.ones(n, dtype=torch.bool)
+    hide[keep] = False
+    z[15, hide.cuda()] = -float("inf")
+    for T, a in ((1.0, 0.0), (2.0, 0.3), (1.0, 0.5)):
+        loss, dz = check(torch, P, z, index, t, labels, T, a, dtype)
+        loss, dz = loss.cpu(), dz.cpu()
+        assert loss[10] == 0 and not dz[10].any()
+        if a == 0:
+            assert loss[1] == 0 and not dz[1].any() and loss[6] == 0 and not dz[6].any()
+        assert loss[12] == float("inf") and bool(torch.isfinite(dz[12]).all())
+        assert bool(torch.isnan(loss[14])) and bool(torch.isnan(dz[14]).all())
+    check(torch, P, z, index, t, None, 2.0, 0.3, dtype)
+
+
+def test_large_logits(env):
+    """far from zero and far apart: differences to the maximum come first"""
+    torch, P = env
+    z, index, t, labels = make(torch, 6, 5000, 16, "f32", 3)
+    z = z * 10 + 64 * torch.arange(6, device="cuda")[:, None]
+    check(torch, P, z, index, 5 * t + 100, labels, 4.0, 0.5, "f32")
+    top = torch.full((1, 3), 3e38, device="cuda")
+    lowest = torch.full((1, 5000), torch.finfo(torch.float32).min, device="cuda")
+    lowest[0, 7] = 3e38
+    loss, dz = P.bsr_distill_forward_backward(lowest, torch.tensor([[7, 8, 9]], device="cuda", dtype=torch.int32), top)
+    assert float(loss) == float("inf") and abs(float(dz[0, 7]) - 2 / 3) < 1e-6
+
+
+def test_teacher_in_bf16(env):
+    torch, P = env
+    z, index, t, labels = make(torch, 9, 777, 20, "bf16", 4)
+    tb = t.bfloat16()
+    a, b = P.bsr_distill_forward_backward(z, index, tb, labels, 2.0, 0.2), P.bsr_distill_forward_backward(z, index, tb.float(), labels, 2.0, 0.2)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_against_differences(env):
+    """central differences of the 64-bit loss in random directions"""
+    torch, P = env
+    z, index, t, labels = make(torch, 4, 300, 12, "f32", 5)
+    _, dz = P.bsr_distill_forward_backward(z, index, t, labels, 2.0, 0.3)
+    zd, h = host(z), 1e-4
+    v = np.random.default_rng(0).standard_normal(zd.shape)
+    args = (index.cpu().numpy(), host(t), labels.cpu().numpy(), 2.0, 0.3, np.ones(4))
+    slope = (reference(zd + h * v, *args)[0] - reference(zd - h * v, *args)[0]) / (2 * h)
+    assert (np.abs(slope - (host(dz) * v).sum(1)) <= 1e-4 * np.linalg.norm(host(dz), axis=1) * np.linalg.norm(v, axis=1)).all()
+
+
+def test_whole_distribution_and_hard_part_alone(env):
+    """all classes as the teacher's list: the loss is 0 where the student agrees; hard weight 1: the cross-entropy"""
+    torch, P = env
+    z, _, _, labels = make(torch, 5, 64, 8, "f32", 6)
+    index = torch.arange(64, dtype=torch.int32, device="cuda").repeat(5, 1)
+    loss, dz = P.bsr_distill_forward_backward(z, index, z.clone(), temperature=2.0)
+    assert loss.abs().max() < 1e-5 and dz.abs().max() < 1e-6
+    loss, dz = P.bsr_distill_forward_backward(z, index, z.clone(), labels, 1.0, 1.0)
+    assert torch.allclose(loss.double(), torch.nn.functional.cross_entropy(z.double(), labels.long(), reduction="none"), atol=1e-5)
+
+
+def test_no_rows_and_refusals(env):
+    torch, P = env
+    z, index, t, labels = make(torch, 6, 40, 4, "f32", 7)
+    loss, dz = P.bsr_distill_forward_backward(z[:0], index[:0], t[:0], labels[:0])
+    assert loss.shape == (0,) and dz.shape == (0, 40)
+    for call in (lambda: P.bsr_distill_forward(z, index[:5], t), lambda: P.bsr_distill_forward(z, index, t[:, :3]), lambda: P.bsr_distill_forward(z.t(), index, t),
+                 lambda: P.bsr_distill_forward(z, index, t, labels.long()), lambda: P.bsr_distill_forward(z.cpu(), index, t),
+                 lambda: P.bsr_distill_backward(z, index, t, torch.zeros(6, 2, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: P.bsr_distill_forward(z.double(), index, t), lambda: P.bsr_distill_forward(z, index.long(), t)):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: P.bsr_distill_forward(z, index, t, temperature=0.0), lambda: P.bsr_distill_forward(z, index, t, temperature=float("nan")),
+                 lambda: P.bsr_distill_forward(z, index, t, hard_weight=1.5),
+                 lambda: P.bsr_distill_forward(z, torch.zeros(6, 1025, dtype=torch.int32, device="cuda"), torch.zeros(6, 1025, device="cuda"))):
+        with pytest.raises(P.BsrError):
+            call()

@@ -1,0 +1,90 @@
+"""The operators on a caller's own tensors without a GPU: exported, bound, and refusing bad arguments before anything is launched (the
+addresses below are never read)."""
+import ctypes as C
+
+import pytest
+
+import paper_2405_10951_amd as P
+from reference8 import blocks8, exponent, to_e4m3
+
+INVALID = -1
+A = 1 << 20                     # an aligned address
+
+
+def test_bound_under_their_c_names():
+    for n in ("bsr_layernorm_forward", "bsr_layernorm_forward8", "bsr_layernorm_backward", "bsr_quantize8_rows", "bsr_quantize8_weight",
+              "bsr_linear8_forward", "bsr_linear8_dgrad", "bsr_distill_forward", "bsr_distill_forward_backward", "bsr_distill_backward"):
+        assert hasattr(P, n)
+
+
+@pytest.mark.parametrize("k,ldv,lds", [(0, 0, 0), (1, 128, 4), (128, 128, 4), (129, 256, 4), (512, 512, 4), (513, 640, 8), (768, 768, 8)])
+def test_strides_of_8_bit_rows(k, ldv, lds):
+    v, s = C.c_int64(-1), C.c_int64(-1)
+    P.load_library().bsr_block8_strides(k, C.byref(v), C.byref(s))
+    assert (v.value, s.value) == (ldv, lds)
+
+
+def test_workspaces():
+    lib = P.load_library()
+    assert lib.bsr_layernorm_workspace_floats(0) == 0 and lib.bsr_layernorm_workspace_floats(768) >= 2 * 768
+    assert lib.bsr_linear8_workspace_bytes(1, 4096) == 0 and lib.bsr_linear8_workspace_bytes(0, 64) == 0
+    assert lib.bsr_linear8_workspace_bytes(6304, 768) >= 6304 * (768 + 8)
+
+
+def call(name, good, **bad):
+    """`good` is an ordered dict of valid arguments; any of them replaced"""
+    args = dict(good, **bad)
+    return getattr(P.load_library(), name)(*args.values())
+
+
+LN = dict(x=A, type=0, M=4, D=64, ldx=64, gamma=A, beta=A, eps=1e-6, y=A, ldy=64, values=None, scales=None, mean=A, rstd=A, stream=None)
+LNB = dict(dy=A, lddy=64, x=A, ldx=64, res=None, ldr=0, type=1, M=4, D=64, mean=A, rstd=A, gamma=A, dx=A, lddx=64, dgamma=A, dbeta=A, ws=A,
+           ws_floats=1 << 20, stream=None)
+QR = dict(x=A, type=0, M=4, K=64, ldx=64, values=A, scales=A, stream=None)
+QW = dict(w=A, type=0, n_in=64, n_out=32, ldw=32, values=A, scales=A, values_back=A, scales_back=A, stream=None)
+LF = dict(x=A, x_type=0, ldx=64, x_scales=None, M=400, n_in=64, n_out=32, values=A, scales=A, bias=None, act=0, u=None, res=None, y=A, y_type=0, ws=A,
+          ws_bytes=1 << 20, stream=None)
+LD = dict(dy=A, type=0, lddy=32, dy_scales=None, M=400, n_in=64, n_out=32, values=A, scales=A, u=None, dx=A, dx_type=0, ws=A, ws_bytes=1 << 20, stream=None)
+DF = dict(z=A, type=0, rows=4, classes=10, ldz=10, index=A, ldi=3, logits=A, logits_type=1, ldt=3, top=3, labels=None, T=1.0, a=0.0, loss=A, stats=A,
+          row_grad=None, scale=1.0, dz=None, ldd=0, stream=None)
+DB = dict(z=A, type=0, rows=4, classes=10, ldz=10, index=A, ldi=3, logits=A, logits_type=1, ldt=3, top=3, labels=None, T=1.0, a=0.0, stats=A,
+          row_grad=None, scale=1.0, dz=2 * A, ldd=10, stream=None)
+REFUSED = [
+    ("bsr_layernorm_forward", LN, [dict(x=None), dict(x=A + 1), dict(type=2), dict(M=-1), dict(D=0), dict(ldx=63), dict(gamma=A + 4), dict(beta=None),
+                                   dict(eps=float("nan")), dict(y=None), dict(ldy=8), dict(values=A), dict(scales=A), dict(values=A + 8, scales=A), dict(mean=A + 2)]),
+    ("bsr_layernorm_backward", LNB, [dict(dy=None), dict(x=A + 2), dict(lddy=1), dict(res=A, ldr=8), dict(type=7), dict(M=-5), dict(mean=None), dict(gamma=None),
+                                     dict(dgamma=None), dict(dx=None, dgamma=None, dbeta=None), dict(ws=None), dict(ws_floats=100), dict(lddx=60)]),
+    ("bsr_quantize8_rows", QR, [dict(x=None), dict(type=3), dict(M=-1), dict(K=0), dict(ldx=10), dict(values=None), dict(values=A + 8), dict(scales=None)]),
+    ("bsr_quantize8_weight", QW, [dict(w=None), dict(n_in=0), dict(n_out=-1), dict(ldw=31), dict(values=None), dict(scales_back=None), dict(values_back=A + 1)]),
+    ("bsr_linear8_forward", LF, [dict(x=None), dict(x_type=5), dict(ldx=63), dict(M=-1), dict(n_in=0), dict(n_out=0), dict(values=None), dict(scales=None), dict(act=2),
+                                 dict(y=None), dict(y=A + 2), dict(y_type=9), dict(ws=None), dict(ws_bytes=10), dict(res=A + 4), dict(act=1, u=A + 8),
+                                 dict(x_scales=A, x=A + 4), dict(bias=A + 2)]),
+    ("bsr_linear8_dgrad", LD, [dict(dy=None), dict(lddy=16), dict(u=A + 2), dict(dx=None), dict(ws_bytes=0), dict(values=A + 4), dict(dx_type=-1)]),
+    ("bsr_distill_forward", DF, [dict(z=None), dict(z=A + 1), dict(type=4), dict(logits_type=4), dict(rows=-1), dict(rows=1 << 31), dict(classes=0), dict(ldz=9), dict(top=0),
+                                 dict(top=1025, ldi=1025, ldt=1025), dict(index=None), dict(ldi=2), dict(logits=None), dict(T=0.0), dict(T=float("inf")), dict(T=float("nan")),
+                                 dict(a=-0.1), dict(a=1.1), dict(a=float("nan")), dict(loss=None, stats=None), dict(loss=A + 2), dict(labels=A + 1), dict(dz=A, ldd=11),
+                                 dict(dz=2 * A, ldd=4)]),
+    ("bsr_distill_backward", DB, [dict(stats=None), dict(dz=None), dict(row_grad=A + 1), dict(ldd=9)]),
+]
+
+
+@pytest.mark.parametrize("name,good,bad", [(n, g, b) for n, g, bads in REFUSED for b in bads])
+def test_refused_before_a_launch(name, good, bad):
+    assert call(name, good, **bad) == INVALID
+    text = P.load_library().bsr_last_error(None).decode()
+    assert text.startswith(name) and len(text) > len(name) + 8
+
+
+@pytest.mark.parametrize("name,good,rows", [(n, g, "rows" if "distill" in n else "M") for n, g, _ in REFUSED if "M" in g or "rows" in g])
+def test_no_rows_no_launch(name, good, rows):
+    """(the backward of a LayerNorm zeroes its sums, which is a launch: dx alone here)"""
+    more = dict(dgamma=None, dbeta=None) if name == "bsr_layernorm_backward" else {}
+    assert call(name, good, **{rows: 0}, **more) == 0
+
+
+def test_the_reference_of_8_bit_blocks():
+    """the numpy form that the GPU tests compare with, on values worked out by hand"""
+    assert [exponent(v) for v in (0.0, 448.0, 448.1, 1.0, 1.75, 1.7500001, 3.4e38, 1e-45)] == [0, 0, 1, -8, -8, -7, 120, -127]
+    assert list(to_e4m3([17.0, 19.0, 21.0, 2 ** -10, 3 * 2 ** -10, -17.0, 448.0, 0.0])) == [16.0, 20.0, 20.0, 0.0, 2 ** -8, -16.0, 448.0, 0.0]
+    v, e = blocks8([[896.0, 1.0, 3.1]], 1, 128)
+    assert e[0, 0] == 1 and list(v[0]) == [896.0, 1.0, 3.0]
