@@ -117,7 +117,7 @@ template <int BM, int BN, int WM, int WN, int NST, typename T, int ACT, bool EXA
 __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, const void* hB, const void* hsa, const void* hsb, int hM, int hN, int hK,
                                                                 int tiles, Gemm8Desc g) {
   constexpr int NW = WM * WN, NT = NW * 64, ROWS = BM + BN;
-  constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 32, NI = TN / 32, NMF = MI * NI, NFR = MI + NI;
+  constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 32, NI = TN / 32, NMF = MI * NI;
   constexpr int RPI = NT / 8;                        // tile rows that a load instruction of the workgroup fills
   constexpr int AL = BM / RPI, BL = BN / RPI;
   constexpr int SL = (ROWS + NT - 1) / NT;           // scale loads of a thread
@@ -141,11 +141,14 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
 
   // rows past the end repeat the last one: they only feed accumulators that are never stored
   const int lrow = tid >> 3, chunk = ((tid & 7) ^ swz(lrow)) * 16;
-  unsigned off[AL + BL];
-#pragma unroll
-  for (int i = 0; i < AL; ++i) off[i] = (unsigned)(min(m0 + i * RPI + lrow, M - 1) - m0) * ld + chunk;
-#pragma unroll
-  for (int i = 0; i < BL; ++i) off[AL + i] = (unsigned)(min(n0 + i * RPI + lrow, N - 1) - n0) * ld + chunk;
+  constexpr bool TIGHT = MI * NI >= 8;               // no registers to keep the offsets of the loads in: worked out at each
+  const int a_rows = M - 1 - m0, b_rows = N - 1 - n0;
+  auto row_off = [&](auto I, int row) __attribute__((always_inline)) {
+    constexpr int i = decltype(I)::value;
+    return (unsigned)min((i < AL ? i : i - AL) * RPI + row, i < AL ? a_rows : b_rows) * ld + chunk;
+  };
+  unsigned off[TIGHT ? 1 : AL + BL];
+  if constexpr (!TIGHT) sfor<AL + BL>([&](auto I) __attribute__((always_inline)) { off[decltype(I)::value] = row_off(I, lrow); });
   const uint8_t* soff[SL];
 #pragma unroll
   for (int i = 0; i < SL; ++i) {
@@ -159,7 +162,15 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
     if constexpr (i < AL + BL) {
       const uint8_t* src = (i < AL ? A : B) + (size_t)kt * BLOCK8;
       unsigned char* dst = base + wave * 1024 + (i < AL ? i * RPI * 128 : BM * 128 + (i - AL) * RPI * 128);
-      __builtin_amdgcn_global_load_lds(BSR_GLOBAL_PTR(src + off[i]), BSR_LDS_VOID(dst), 16, 0, 0);
+      unsigned o;
+      if constexpr (TIGHT) {
+        int row = lrow;
+        asm volatile("" : "+v"(row));                // (not before the loop)
+        o = row_off(I, row);
+      } else {
+        o = off[i];
+      }
+      __builtin_amdgcn_global_load_lds(BSR_GLOBAL_PTR(src + o), BSR_LDS_VOID(dst), 16, 0, 0);
     } else {
       constexpr int j = i - AL - BL;
       __builtin_amdgcn_global_load_lds(BSR_GLOBAL_PTR(soff[j] + (kt & ~3)), BSR_LDS_VOID(base + SCALES + (j * NT + wave * 64) * 4), 4, 0, 0);
@@ -174,46 +185,61 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[mi][ni][r] = 0.f;
 
-  // fragments in the order A0, B0 .. B(NI-1), A1 .. A(MI-1)
-  const int lr = lane & 31, lh = lane >> 5, sw = swz(lr);
-  int rowj[NFR];
+  // Fragments: rows of A one set, each read for the next k-step once its products are done; rows of B two sets, of k-steps in turn (a second set
+  // of A as well would spill in the largest tile).  Row r's bytes of k-step ks lie in chunks 4 ks + lh and 4 ks + 2 + lh, slot chunk ^ swz(r): the
+  // address of the lane's first chunk, bits flipped for the others.
+  const int lr = lane & 31, lh = lane >> 5;
+  const int slot0 = lr * 128 + ((lh ^ swz(lr)) << 4);
+  const int a_at = wm * TM * 128 + slot0, b_at = (BM + wn * TN) * 128 + slot0;
+  const int as_at = SCALES + (wm * TM + lr) * 4, bs_at = SCALES + (BM + wn * TN + lr) * 4;
+  i32x8 fa[MI], fb[2][NI];
+  bf16x8 wa[EXACT ? MI : 1][4], wb[EXACT ? NI : 1][4];
+  int sa[MI], sb[NI], sbn[NI];
+  auto frag = [&](int at, int ks) __attribute__((always_inline)) {
+    return join8(*(const i32x4*)(smem + (at ^ (ks << 6))), *(const i32x4*)(smem + (at ^ (ks << 6) ^ 32)));
+  };
+  auto rda = [&](auto I, int st, int ks) __attribute__((always_inline)) {
+    constexpr int i = decltype(I)::value;
+    fa[i] = frag(st * STAGE + i * 4096 + a_at, ks);
+  };
+  auto rdb = [&](auto SET, auto I, int st, int ks) __attribute__((always_inline)) {
+    constexpr int set = decltype(SET)::value, i = decltype(I)::value;
+    fb[set][i] = frag(st * STAGE + i * 4096 + b_at, ks);
+  };
+  auto rdsa = [&](auto I, int st, int kt) __attribute__((always_inline)) {
+    constexpr int i = decltype(I)::value;
+    sa[i] = smem[st * STAGE + as_at + i * 128 + (kt & 3)];
+  };
+  auto rdsb = [&](int st, int kt) __attribute__((always_inline)) {
 #pragma unroll
-  for (int j = 0; j < NFR; ++j) {
-    const bool isA = j == 0 || j > NI;
-    const int idx = j == 0 ? 0 : (j <= NI ? j - 1 : j - NI);
-    rowj[j] = isA ? wm * TM + idx * 32 + lr : BM + wn * TN + idx * 32 + lr;
-  }
-  i32x8 fr[2][NFR];
-  bf16x8 wide[EXACT ? NFR : 1][4];
-  int sc[NFR], scn[NFR];
+    for (int i = 0; i < NI; ++i) sbn[i] = smem[st * STAGE + bs_at + i * 128 + (kt & 3)];
+  };
+  auto next_scales = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) sb[i] = sbn[i];
+  };
   auto widen = [&](auto SET) __attribute__((always_inline)) {
     constexpr int set = decltype(SET)::value;
-    if constexpr (EXACT)
-#pragma unroll
-      for (int j = 0; j < NFR; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) wide[j][q] = widen8(fr[set][j][2 * q], fr[set][j][2 * q + 1], sc[j]);
-  };
-  auto rd1 = [&](auto SET, auto J, int st, int ks) __attribute__((always_inline)) {
-    constexpr int set = decltype(SET)::value, j = decltype(J)::value;
-    const unsigned char* p = smem + st * STAGE + rowj[j] * 128;
-    fr[set][j] = join8(*(const i32x4*)(p + (((ks * 4 + lh) ^ sw) << 4)), *(const i32x4*)(p + (((ks * 4 + 2 + lh) ^ sw) << 4)));
-  };
-  auto rds = [&](auto J, int st, int kt) __attribute__((always_inline)) {
-    constexpr int j = decltype(J)::value;
-    scn[j] = smem[st * STAGE + SCALES + rowj[j] * 4 + (kt & 3)];
-  };
-  auto mf1 = [&](auto SET, auto J) __attribute__((always_inline)) {
-    constexpr int set = decltype(SET)::value, j = decltype(J)::value, mi = j / NI, ni = j % NI;
-    constexpr int ja = mi == 0 ? 0 : NI + mi, jb = 1 + ni;
     if constexpr (EXACT) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide[jb][q], wide[ja][q], acc[mi][ni], 0, 0, 0);
-    } else {
-      acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fr[set][jb], fr[set][ja], acc[mi][ni], 0, 0, 0, sc[jb], 0, sc[ja]);
+      for (int q = 0; q < 4; ++q) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) wa[i][q] = widen8(fa[i][2 * q], fa[i][2 * q + 1], sa[i]);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) wb[i][q] = widen8(fb[set][i][2 * q], fb[set][i][2 * q + 1], sb[i]);
+      }
     }
   };
-  constexpr int PRE = NMF >= 8 ? 2 : 1;              // MFMAs of the second k-step in front of the barrier
+  auto mf1 = [&](auto SET, auto J) __attribute__((always_inline)) {
+    constexpr int set = decltype(SET)::value, mi = decltype(J)::value / NI, ni = decltype(J)::value % NI;
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[ni][q], wa[mi][q], acc[mi][ni], 0, 0, 0);
+    } else {
+      acc[mi][ni] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[set][ni], fa[mi], acc[mi][ni], 0, 0, 0, sb[ni], 0, sa[mi]);
+    }
+  };
+  constexpr int PRE = NI;                            // MFMAs of the second k-step in front of the barrier: those of the first rows
   constexpr int POST = NMF - PRE;
   constexpr int SPAN = POST + (NST > 2 && NMF >= 4 ? NMF : 0);       // MFMAs that the loads of a k-tile are spread over
   constexpr bool LATE = SPAN > POST;                 // some follow in the next k-tile
@@ -221,18 +247,23 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
     constexpr int p = decltype(P)::value, lo = p >= SPAN ? LPT : (p * LPT + SPAN - 1) / SPAN, hi = p + 1 >= SPAN ? LPT : ((p + 1) * LPT + SPAN - 1) / SPAN;
     sfor<hi - lo>([&](auto L) __attribute__((always_inline)) { issue1(IC<lo + decltype(L)::value>{}, kt, st); });
   };
-  // the first k-step of a k-tile: MFMAs on set 0, the fragments of the second into set 1
+  // what is read behind MFMA j of a k-step for the next one: B in the first MFMAs, the rows of A whose last product this was
+  auto reads_at = [&](auto SETN, auto J, int st, int ks, int kt) __attribute__((always_inline)) {
+    constexpr int j = decltype(J)::value;
+    if constexpr (j % NI == NI - 1) {
+      rda(IC<j / NI>{}, st, ks);
+      if constexpr (decltype(SETN)::value == 0) rdsa(IC<j / NI>{}, st, kt);
+    }
+    constexpr int from = PRE < NMF ? PRE : 0;        // (behind the barrier, where there is one)
+    if constexpr (j >= from && j - from < NI) rdb(SETN, IC<j - from>{}, st, ks);
+  };
+  // the first k-step of a k-tile: MFMAs on set 0 of B, the fragments of the second k-step
   auto kfirst = [&](auto LOADS, int st, int ktl, int stl) __attribute__((always_inline)) {
-    constexpr int RPM = (NFR + NMF - 1) / NMF;
     widen(IC<0>{});
     sfor<NMF>([&](auto J) __attribute__((always_inline)) {
-      constexpr int j = decltype(J)::value;
       mf1(IC<0>{}, J);
-      sfor<RPM>([&](auto R) __attribute__((always_inline)) {
-        constexpr int r = j * RPM + decltype(R)::value;
-        if constexpr (r < NFR) rd1(IC<1>{}, IC<r>{}, st, 1);
-      });
-      if constexpr (decltype(LOADS)::value) loads_at(IC<POST + j>{}, ktl, stl);
+      reads_at(IC<1>{}, J, st, 1, 0);
+      if constexpr (decltype(LOADS)::value) loads_at(IC<POST + decltype(J)::value>{}, ktl, stl);
       BSR_SCHED_FENCE();
     });
   };
@@ -240,8 +271,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
   // nothing is issued any more and the count follows from rem, the k-tiles behind this one
   auto klast = [&](auto VMW, int kt, int st, int stn, int rem) __attribute__((always_inline)) {
     constexpr int vmw = decltype(VMW)::value;
-    constexpr int RPP = (NFR + POST - 1) / POST;
-    if constexpr (EXACT) { wait_lgkmcnt0(); widen(IC<1>{}); }
+    if constexpr (EXACT) widen(IC<1>{});
     sfor<PRE>([&](auto J) __attribute__((always_inline)) { mf1(IC<1>{}, J); BSR_SCHED_FENCE(); });
     wait_lgkmcnt0();
     if constexpr (vmw >= 0) wait_vmcnt<vmw>();
@@ -250,18 +280,19 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
     else wait_vmcnt<0>();
     __builtin_amdgcn_s_barrier();
     BSR_SCHED_FENCE();
-    sfor<POST>([&](auto P) __attribute__((always_inline)) {
-      constexpr int p = decltype(P)::value;
-      mf1(IC<1>{}, IC<PRE + p>{});
-      sfor<RPP>([&](auto R) __attribute__((always_inline)) {
-        constexpr int r = p * RPP + decltype(R)::value;
-        if constexpr (r < NFR) { rds(IC<r>{}, stn, kt + 1); rd1(IC<0>{}, IC<r>{}, stn, 0); }
-      });
-      if constexpr (vmw >= 0) loads_at(P, kt + NST, st);
+    rda(IC<0>{}, stn, 0);                            // (its products were in front of the barrier)
+    rdsa(IC<0>{}, stn, kt + 1);
+    rdsb(stn, kt + 1);
+    if constexpr (POST == 0) sfor<NI>([&](auto I) __attribute__((always_inline)) { rdb(IC<0>{}, I, stn, 0); });
+    sfor<POST>([&](auto Q) __attribute__((always_inline)) {
+      constexpr int q = decltype(Q)::value;
+      mf1(IC<1>{}, IC<PRE + q>{});
+      reads_at(IC<0>{}, IC<PRE + q>{}, stn, 0, kt + 1);
+      if constexpr (vmw >= 0) loads_at(Q, kt + NST, st);
       BSR_SCHED_FENCE();
     });
-#pragma unroll
-    for (int j = 0; j < NFR; ++j) sc[j] = scn[j];
+    if constexpr (POST == 0 && vmw >= 0) sfor<LPT>([&](auto I) __attribute__((always_inline)) { issue1(I, kt + NST, st); });
+    next_scales();
   };
 
 #pragma unroll
@@ -272,9 +303,10 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
     if (fl >= 3) wait_vmcnt<3 * LPT>(); else if (fl == 2) wait_vmcnt<2 * LPT>(); else if (fl == 1) wait_vmcnt<LPT>(); else wait_vmcnt<0>();
   }
   __builtin_amdgcn_s_barrier();
-  sfor<NFR>([&](auto J) __attribute__((always_inline)) { rds(J, 0, 0); rd1(IC<0>{}, J, 0, 0); });
-#pragma unroll
-  for (int j = 0; j < NFR; ++j) sc[j] = scn[j];
+  rdsb(0, 0);
+  sfor<MI>([&](auto I) __attribute__((always_inline)) { rda(I, 0, 0); rdsa(I, 0, 0); });
+  sfor<NI>([&](auto I) __attribute__((always_inline)) { rdb(IC<0>{}, I, 0, 0); });
+  next_scales();
   int st = 0, kt = 0;
   auto ktile = [&](auto LOADS, auto VMW) __attribute__((always_inline)) {
     const int stn = (st + 1 == NST) ? 0 : st + 1, stl = st == 0 ? NST - 1 : st - 1;
