@@ -32,21 +32,20 @@ template <typename T> struct Eight;
 template <> struct Eight<bf16> {
   bf16x8 v;
   __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
+  __device__ __forceinline__ void set(int i, bf16 x) { v[i] = x; }
 };
 template <> struct Eight<float> {
   f32x4 lo, hi;
   __device__ __forceinline__ float operator[](int i) const { return i < 4 ? lo[i] : hi[i - 4]; }
+  __device__ __forceinline__ void set(int i, float x) { if (i < 4) lo[i] = x; else hi[i - 4] = x; }
 };
 // up to eight consecutive values (n of them exist); vec: the address is aligned to 16 bytes and all eight exist
-template <typename T> __device__ __forceinline__ void get8(const T* p, int n, bool vec, float (&o)[8]) {
-  if (vec) {
-    const Eight<T> e = *(const Eight<T>*)p;
+template <typename T> __device__ __forceinline__ Eight<T> get8(const T* p, int n, bool vec) {
+  if (vec) return *(const Eight<T>*)p;
+  Eight<T> o;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = e[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = i < n ? (float)p[i] : 0.f;
-  }
+  for (int i = 0; i < 8; ++i) o.set(i, i < n ? p[i] : (T)0.f);
+  return o;
 }
 template <typename T> __device__ __forceinline__ void put8(T* p, int n, bool vec, const float (&v)[8]) {
   if (vec) {
@@ -66,33 +65,99 @@ template <typename T> __device__ __forceinline__ void put8(T* p, int n, bool vec
   }
 }
 
-// bias, GELU (with its stored input) or GELU', residual on eight columns of row m, and out
-template <typename T, int ACT>
-__device__ __forceinline__ void finish8b(const Gemm8Desc& g, float (&v)[8], int64_t m, int col, bool vec) {
-  const int n = g.N - col;
-  vec = vec && n >= 8;
-  const int64_t at = m * g.ldc + col;
-  if (g.bias) {
+// What follows the products of a wave tile: bias, GELU (with its stored input) or GELU', residual.  Bias and GELU are finished where the
+// accumulators are; 32 rows at a time then go through a patch of LDS, rounded where nothing is to be added any more, and come back with a lane owning
+// eight columns of a row.  bias: that of the wave tile's columns, in LDS.  What is added or multiplied there is asked for ahead of the patch.  The row blocks are a loop: code that is written out once is fetched once.
+template <int MI, int NI, typename T, int ACT>
+__device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][NI], int row0, int col0, int lane, unsigned char* patch,
+                                          const float* bias) {
+  constexpr int TN = NI * 32, CPR = TN / 8, RPP = 64 / CPR, NPASS = 32 / RPP, LDF = (TN + 4) * 4, LDT = TN * (int)sizeof(T) + 16;
+  const int lr = lane & 31, lh = lane >> 5, my_row = lane / CPR, col = col0 + lane % CPR * 8, n = g.N - col;
+  const bool vec = g.ldc * (int64_t)sizeof(T) % 16 == 0 && n >= 8;
+  auto fence = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  // the row block in blk, rounded, to dst
+  auto out = [&](const f32x16 (&blk)[NI], T* dst, int mi) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += i < n ? g.bias[col + i] : 0.f;
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg) {
+        vec4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (T)blk[ni][4 * rg + e];
+        *(vec4*)(patch + lr * LDT + (ni * 32 + 8 * rg + 4 * lh) * (int)sizeof(T)) = o;
+      }
+    fence();
+#pragma unroll
+    for (int p = 0; p < NPASS; ++p) {
+      const int r = p * RPP + my_row, m = row0 + mi * 32 + r;
+      const T* src = (const T*)(patch + r * LDT) + lane % CPR * 8;
+      if (m < g.M && n > 0) {
+        T* to = dst + (int64_t)m * g.ldc + col;
+        if (vec) *(Eight<T>*)to = *(const Eight<T>*)src;
+        else
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i < n) to[i] = src[i];
+      }
+    }
+    fence();
+  };
+  const T* extra = (const T*)(ACT == ACT_GELU_BWD ? g.aux : g.res);
+#pragma nounroll
+  for (int mi = 0; mi < MI; ++mi) {
+    f32x16 blk[NI];
+    sfor<MI>([&](auto I) __attribute__((always_inline)) {
+      constexpr int i = decltype(I)::value;
+      if (mi == i)
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) blk[ni] = acc[i][ni];
+    });
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg) {
+        const f32x4 b = *(const f32x4*)(bias + ni * 32 + 8 * rg + 4 * lh);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) blk[ni][4 * rg + e] += b[e];
+      }
+    if constexpr (ACT == ACT_GELU) {
+      if (g.aux) out(blk, (T*)g.aux, mi);
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) blk[ni][r] = gelu_f(blk[ni][r]);
+    }
+    if (ACT != ACT_GELU_BWD && !g.res) {
+      out(blk, (T*)g.C, mi);
+      continue;
+    }
+    Eight<T> more[NPASS];
+#pragma unroll
+    for (int p = 0; p < NPASS; ++p) {
+      const int m = row0 + mi * 32 + p * RPP + my_row;
+      if (m < g.M && n > 0) more[p] = get8(extra + (int64_t)m * g.ldc + col, n, vec);
+    }
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg)
+        *(f32x4*)(patch + lr * LDF + (ni * 32 + 8 * rg + 4 * lh) * 4) = f32x4{blk[ni][4 * rg], blk[ni][4 * rg + 1], blk[ni][4 * rg + 2], blk[ni][4 * rg + 3]};
+    fence();
+#pragma unroll
+    for (int p = 0; p < NPASS; ++p) {
+      const int r = p * RPP + my_row, m = row0 + mi * 32 + r;
+      float v[8];
+      const float* src = (const float*)(patch + r * LDF) + lane % CPR * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = ACT == ACT_GELU_BWD ? src[i] * gelu_grad_f(more[p][i]) : src[i] + more[p][i];
+      if (m < g.M && n > 0) put8((T*)g.C + (int64_t)m * g.ldc + col, n, vec, v);
+    }
+    fence();
   }
-  if (ACT == ACT_GELU) {
-    if (g.aux) put8((T*)g.aux + at, n, vec, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = gelu_f(v[i]);
-  } else if (ACT == ACT_GELU_BWD) {
-    float u[8];
-    get8((const T*)g.aux + at, n, vec, u);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= gelu_grad_f(u[i]);
-  }
-  if (g.res) {
-    float r[8];
-    get8((const T*)g.res + at, n, vec, r);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += r[i];
-  }
-  put8((T*)g.C + at, n, vec, v);
 }
 
 constexpr int EXACT_BELOW = 768;
@@ -295,6 +360,12 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
     next_scales();
   };
 
+  // the bias goes behind the stages, ahead of the first k-tile: it has landed when that has
+  if (g.bias) {
+    if (wave < BN / 64) __builtin_amdgcn_global_load_lds(BSR_GLOBAL_PTR(g.bias + min(n0 + tid, N - 1)), BSR_LDS_VOID(smem + NST * STAGE + wave * 256), 4, 0, 0);
+  } else if (tid < BN) {
+    ((float*)(smem + NST * STAGE))[tid] = 0.f;
+  }
 #pragma unroll
   for (int j = 0; j < NST; ++j)
     if (j < nk) sfor<LPT>([&](auto I) __attribute__((always_inline)) { issue1(I, j, j); });
@@ -302,6 +373,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
     const int fl = min(nk, NST) - 1;
     if (fl >= 3) wait_vmcnt<3 * LPT>(); else if (fl == 2) wait_vmcnt<2 * LPT>(); else if (fl == 1) wait_vmcnt<LPT>(); else wait_vmcnt<0>();
   }
+  wait_lgkmcnt0();
   __builtin_amdgcn_s_barrier();
   rdsb(0, 0);
   sfor<MI>([&](auto I) __attribute__((always_inline)) { rda(I, 0, 0); rdsa(I, 0, 0); });
@@ -324,38 +396,9 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
     while (kt + NST < nk) ktile(IC<0>{}, steady);
   }
   while (kt < nk) ktile(IC<0>{}, IC<-1>{});                       // nothing left to issue
-  // every wavefront is past the last barrier: the stages are free.  32 rows at a time go through a patch of the wavefront's own and come back with
-  // a lane owning eight columns of a row
-  constexpr int LDP = TN + 4, CPR = TN / 8, RPP = 64 / CPR, NPASS = 32 / RPP;
-  float* patch = (float*)smem + wave * 32 * LDP;
-  const bool vec = g.ldc * (int64_t)sizeof(T) % 16 == 0;
-  const int col = n0 + wn * TN + lane % CPR * 8;
-#pragma nounroll
-  for (int mi = 0; mi < MI; ++mi) {
-    sfor<MI>([&](auto I) __attribute__((always_inline)) {
-      constexpr int i = decltype(I)::value;
-      if (mi == i)
-#pragma unroll
-        for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-          for (int rg = 0; rg < 4; ++rg)
-            *(f32x4*)(patch + lr * LDP + ni * 32 + 8 * rg + 4 * lh) =
-                f32x4{acc[i][ni][4 * rg], acc[i][ni][4 * rg + 1], acc[i][ni][4 * rg + 2], acc[i][ni][4 * rg + 3]};
-    });
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int p = 0; p < NPASS; ++p) {
-      const int r = p * RPP + lane / CPR, m = m0 + wm * TM + mi * 32 + r;
-      float v[8];
-      const float* src = patch + r * LDP + lane % CPR * 8;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = src[i];
-      if (m < M && col < N) finish8b<T, ACT>(g, v, m, col, vec);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
+  // every wavefront is past the last barrier: the stages are free, a patch of them for each wavefront
+  epilogue8<MI, NI, T, ACT>(g, acc, m0 + wm * TM, n0 + wn * TN, lane, smem + wave * (32 * (TN + 4) * 4),
+                            (const float*)(smem + NST * STAGE) + wn * TN);
 }
 
 // Few rows: what counts is that the weights come once and at once.  A workgroup owns 16 columns and all rows (16 MI of them); its eight
@@ -465,7 +508,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
 template <int BM, int BN, int WM, int WN, int NST, typename T, int ACT, bool EXACT>
 void launch_tiled(const Gemm8Desc& g, hipStream_t s) {
   constexpr int NT = WM * WN * 64;
-  constexpr size_t stages = (size_t)NST * ((BM + BN) * 128 + (BM + BN + NT - 1) / NT * NT * 4);
+  constexpr size_t stages = (size_t)NST * ((BM + BN) * 128 + (BM + BN + NT - 1) / NT * NT * 4) + BN * 4;
+  static_assert(BN <= NT, "a thread for each column of the bias");
   constexpr size_t patches = (size_t)WM * WN * 32 * (BN / WN + 4) * 4;
   static_assert(patches <= stages && stages <= 160 * 1024, "the epilogue patches live in the stages");
   auto kern = gemm8_kernel<BM, BN, WM, WN, NST, T, ACT, EXACT>;
