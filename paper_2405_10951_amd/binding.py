@@ -388,9 +388,15 @@ class Weight8:
         self.n_in, self.n_out = int(n_in), int(n_out)
 
 
+# The wrappers below are on the path of calls that take the GPU a few microseconds, so what they look at they look at once and cheaply.
+_types: dict = {}                  # torch type -> type code
+
+
 def _type_code(t, what):
-    import torch
-    code = {torch.bfloat16: BSR_BF16, torch.float32: BSR_FP32}.get(t.dtype)
+    if not _types:
+        import torch
+        _types.update({torch.bfloat16: BSR_BF16, torch.float32: BSR_FP32})
+    code = _types.get(t.dtype)
     if code is None:
         raise TypeError(f"{what}: bfloat16 or float32 is needed, got {t.dtype}")
     return code
@@ -398,52 +404,52 @@ def _type_code(t, what):
 
 def _rows_of(t, what, shape=None, dtype=None):
     """A tensor of two dimensions whose rows are contiguous -> its row stride."""
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, {'two dimensions' if shape is None else tuple(shape)} expected")
-    if dtype is not None and t.dtype != dtype:
+    s = t.shape
+    if len(s) != 2 or (shape is not None and s != shape):
+        raise ValueError(f"{what}: shape {tuple(s)}, {'two dimensions' if shape is None else tuple(shape)} expected")
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{what}: {dtype} is needed, got {t.dtype}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{what}: the elements of a row have to lie together, stride {t.stride(1)}")
-    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if ld < t.shape[1]:
-        raise ValueError(f"{what}: rows overlap (stride {ld}, {t.shape[1]} columns)")
+    ld, step = t.stride()
+    cols = s[1]
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what}: the elements of a row have to lie together, stride {step}")
+    if ld < cols:
+        if s[0] > 1:
+            raise ValueError(f"{what}: rows overlap (stride {ld}, {cols} columns)")
+        ld = cols
     return ld
 
 
 def _flat(t, what, shape, dtype):
-    """An optional contiguous tensor of a known shape and type -> itself."""
-    if t is None:
-        return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+    """The address of a contiguous tensor of a known shape and type."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
         raise ValueError(f"{what}: contiguous {dtype} {tuple(shape)} expected, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
-    return t
+    return t.data_ptr()
 
 
 def _together(first, *others):
     """The current stream of the GPU that all tensors are on."""
+    gpu = first.get_device()
+    if gpu < 0:
+        raise ValueError(f"tensors on a GPU are needed, these are on {first.device}")
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != gpu:
             raise ValueError(f"tensors on {first.device} and {t.device}")
-    return _raw_stream(_gpu_index(first.device))
+    return _raw_stream(gpu)
 
 
-def _blocks_of(n):
-    return -(-n // 128)
-
-
-def _rows8_new(M, K, device):
+def _rows8_new(M, K, like):
     import torch
-    nk = _blocks_of(K)
-    return Rows8(torch.empty((M, nk * 128), dtype=torch.uint8, device=device),
-                 torch.empty((M, (nk + 3) // 4 * 4), dtype=torch.uint8, device=device), K)
+    nk = -(-K // 128)
+    return Rows8(like.new_empty((M, nk * 128), dtype=torch.uint8), like.new_empty((M, (nk + 3) // 4 * 4), dtype=torch.uint8), K)
 
 
 def bsr_quantize8_rows(x) -> Rows8:
     """x [M,K] bf16 or fp32 (any row stride) -> 8-bit rows, a scale for each 128 columns."""
     ld, code, stream = _rows_of(x, "x"), _type_code(x, "x"), _together(x)
     M, K = x.shape
-    r = _rows8_new(M, K, x.device)
-    _check(load_library().bsr_quantize8_rows(_dp(x), code, M, K, ld, _dp(r.values), _dp(r.scales), stream))
+    r = _rows8_new(M, K, x)
+    _check(load_library().bsr_quantize8_rows(x.data_ptr(), code, M, K, ld, r.values.data_ptr(), r.scales.data_ptr(), stream))
     return r
 
 
@@ -455,9 +461,8 @@ def bsr_quantize8_weight(w, backward=True) -> Weight8:
 
     def new(rows, cols):
         import torch
-        nk = _blocks_of(cols)
-        return (torch.empty((rows, nk * 128), dtype=torch.uint8, device=w.device),
-                torch.empty((_blocks_of(rows), (nk + 3) // 4 * 4), dtype=torch.uint8, device=w.device))
+        nk = -(-cols // 128)
+        return w.new_empty((rows, nk * 128), dtype=torch.uint8), w.new_empty((-(-rows // 128), (nk + 3) // 4 * 4), dtype=torch.uint8)
 
     v, s = new(n_out, n_in)
     vb, sb = new(n_in, n_out) if backward else (None, None)
@@ -465,159 +470,175 @@ def bsr_quantize8_weight(w, backward=True) -> Weight8:
     return Weight8(v, s, vb, sb, n_in, n_out)
 
 
-def _linear8_rows(x, cols, what):
-    """-> (M, x pointer, type code, stride, scales pointer, workspace, its bytes)"""
-    import torch
-    if isinstance(x, Rows8):
+def _linear8(x, cols, what, *others):
+    """-> (the rows' tensor, M, (pointer, type, stride, scales' pointer), workspace, its bytes, stream)"""
+    if type(x) is Rows8:
         if x.cols != cols:
             raise ValueError(f"{what}: {x.cols} columns, the layer has {cols}")
-        return x.values.shape[0], _dp(x.values), BSR_BF16, 0, _dp(x.scales), None, 0
-    ld, code = _rows_of(x, what, (x.shape[0], cols)), _type_code(x, what)
-    M = x.shape[0]
-    size = load_library().bsr_linear8_workspace_bytes(M, cols)
-    ws = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
-    return M, _dp(x), code, ld, None, ws, size
+        t = x.values
+        return t, t.shape[0], (t.data_ptr(), BSR_BF16, 0, x.scales.data_ptr()), None, 0, _together(t, x.scales, *others)
+    ld = _rows_of(x, what)
+    M, k = x.shape
+    if k != cols:
+        raise ValueError(f"{what}: {k} columns, the layer has {cols}")
+    stream = _together(x, *others)
+    size, ws = load_library().bsr_linear8_workspace_bytes(M, cols), None
+    if size:
+        import torch
+        ws = x.new_empty(size, dtype=torch.uint8)
+    return x, M, (x.data_ptr(), _type_code(x, what), ld, None), ws, size, stream
+
+
+def _linear8_out(x, t, y, what, shape, out_dtype):
+    if y is None:
+        if out_dtype is None:
+            import torch
+            out_dtype = torch.bfloat16 if type(x) is Rows8 else x.dtype
+        return t.new_empty(shape, dtype=out_dtype)
+    if out_dtype is not None and y.dtype is not out_dtype:
+        raise TypeError(f"{what}: {y.dtype}, out_dtype {out_dtype}")
+    return y
 
 
 def bsr_linear8_forward(x, w: Weight8, bias=None, act=0, u_out=None, res=None, y=None, out_dtype=None):
     """x [M,in] (Rows8, or bf16 / fp32 with any row stride) -> y [M,out] = act(x W + bias) (+ res), of out_dtype (that of x, bf16 for Rows8).
     act 1: GELU, u_out [M,out] receives its input."""
-    import torch
-    t = x.values if isinstance(x, Rows8) else x
-    stream = _together(t, w.values, bias, u_out, res, y)
-    M, px, code, ld, ps, ws, size = _linear8_rows(x, w.n_in, "x")
-    if y is None:
-        y = torch.empty((M, w.n_out), dtype=out_dtype or (torch.bfloat16 if isinstance(x, Rows8) else x.dtype), device=t.device)
-    elif out_dtype is not None and y.dtype != out_dtype:
-        raise TypeError(f"y: {y.dtype}, out_dtype {out_dtype}")
-    _flat(y, "y", (M, w.n_out), y.dtype)
-    _flat(bias, "bias", (w.n_out,), torch.float32)
-    _flat(u_out, "u_out", (M, w.n_out), y.dtype)
-    _flat(res, "res", (M, w.n_out), y.dtype)
-    _check(load_library().bsr_linear8_forward(px, code, ld, ps, M, w.n_in, w.n_out, _dp(w.values), _dp(w.scales), _dp(bias), act, _dp(u_out),
-                                              _dp(res), _dp(y), _type_code(y, "y"), _dp(ws), size, stream))
+    t, M, rows, ws, size, stream = _linear8(x, w.n_in, "x", w.values, bias, u_out, res, y)
+    shape = (M, w.n_out)
+    y = _linear8_out(x, t, y, "y", shape, out_dtype)
+    if bias is not None:
+        import torch
+        _flat(bias, "bias", shape[1:], torch.float32)
+    pu = None if u_out is None else _flat(u_out, "u_out", shape, y.dtype)
+    pr = None if res is None else _flat(res, "res", shape, y.dtype)
+    _check(load_library().bsr_linear8_forward(*rows, M, w.n_in, w.n_out, w.values.data_ptr(), w.scales.data_ptr(), _dp(bias), act, pu, pr,
+                                              _flat(y, "y", shape, y.dtype), _type_code(y, "y"), _dp(ws), size, stream))
     return y
 
 
 def bsr_linear8_dgrad(dy, w: Weight8, u=None, dx=None, out_dtype=None):
     """dy [M,out] (Rows8, or bf16 / fp32 with any row stride) -> dx [M,in] = dy W^T, times GELU'(u) where u [M,in] is given."""
-    import torch
     if w.values_back is None:
         raise ValueError("the layer was laid out without backward")
-    t = dy.values if isinstance(dy, Rows8) else dy
-    stream = _together(t, w.values_back, u, dx)
-    M, px, code, ld, ps, ws, size = _linear8_rows(dy, w.n_out, "dy")
-    if dx is None:
-        dx = torch.empty((M, w.n_in), dtype=out_dtype or (torch.bfloat16 if isinstance(dy, Rows8) else dy.dtype), device=t.device)
-    elif out_dtype is not None and dx.dtype != out_dtype:
-        raise TypeError(f"dx: {dx.dtype}, out_dtype {out_dtype}")
-    _flat(dx, "dx", (M, w.n_in), dx.dtype)
-    _flat(u, "u", (M, w.n_in), dx.dtype)
-    _check(load_library().bsr_linear8_dgrad(px, code, ld, ps, M, w.n_in, w.n_out, _dp(w.values_back), _dp(w.scales_back), _dp(u), _dp(dx),
-                                            _type_code(dx, "dx"), _dp(ws), size, stream))
+    t, M, rows, ws, size, stream = _linear8(dy, w.n_out, "dy", w.values_back, u, dx)
+    shape = (M, w.n_in)
+    dx = _linear8_out(dy, t, dx, "dx", shape, out_dtype)
+    pu = None if u is None else _flat(u, "u", shape, dx.dtype)
+    _check(load_library().bsr_linear8_dgrad(*rows, M, w.n_in, w.n_out, w.values_back.data_ptr(), w.scales_back.data_ptr(), pu,
+                                            _flat(dx, "dx", shape, dx.dtype), _type_code(dx, "dx"), _dp(ws), size, stream))
     return dx
 
 
 def _layernorm_forward(x, gamma, beta, eps, y, r8):
-    import torch
     ld, code, stream = _rows_of(x, "x"), _type_code(x, "x"), _together(x, gamma, beta, y)
     M, D = x.shape
-    _flat(gamma, "gamma", (D,), torch.float32)
-    _flat(beta, "beta", (D,), torch.float32)
-    ldy = _rows_of(y, "y", (M, D), x.dtype) if y is not None else 0
-    mean = torch.empty(M, dtype=torch.float32, device=x.device)
-    rstd = torch.empty(M, dtype=torch.float32, device=x.device)
-    _check(load_library().bsr_layernorm_forward(_dp(x), code, M, D, ld, _dp(gamma), _dp(beta), eps, _dp(y), ldy, _dp(r8.values) if r8 else None,
-                                                _dp(r8.scales) if r8 else None, _dp(mean), _dp(rstd), stream))
+    import torch
+    f32 = torch.float32
+    pg, pb = _flat(gamma, "gamma", (D,), f32), _flat(beta, "beta", (D,), f32)
+    ldy = 0 if y is None else _rows_of(y, "y", x.shape, x.dtype)
+    mean, rstd = gamma.new_empty(M), gamma.new_empty(M)
+    pq, ps = (None, None) if r8 is None else (r8.values.data_ptr(), r8.scales.data_ptr())
+    _check(load_library().bsr_layernorm_forward(x.data_ptr(), code, M, D, ld, pg, pb, eps, _dp(y), ldy, pq, ps, mean.data_ptr(),
+                                                rstd.data_ptr(), stream))
     return mean, rstd
 
 
 def bsr_layernorm_forward(x, gamma, beta, eps=1e-6, y=None):
     """x [M,D] bf16 or fp32 (any row stride), gamma, beta [D] fp32 -> (y [M,D], mean [M], rstd [M])."""
-    import torch
     if y is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = x.new_empty(x.shape)
     mean, rstd = _layernorm_forward(x, gamma, beta, eps, y, None)
     return y, mean, rstd
 
 
 def bsr_layernorm_forward8(x, gamma, beta, eps=1e-6, y=None):
     """The same with the result in 8 bits -> (Rows8, mean, rstd); y given: rounded to the type of x as well."""
-    r8 = _rows8_new(x.shape[0], x.shape[1], x.device)
+    _rows_of(x, "x")
+    r8 = _rows8_new(*x.shape, x)
     mean, rstd = _layernorm_forward(x, gamma, beta, eps, y, r8)
     return r8, mean, rstd
 
 
 def bsr_layernorm_backward(dy, x, mean, rstd, gamma, res=None, dx=None, need_dx=True, need_params=True):
     """dy, x [M,D], mean, rstd [M] of the forward, gamma [D] -> (dx [M,D] | None, dgamma [D] | None, dbeta [D] | None).  res [M,D]: added to dx."""
-    import torch
     lib = load_library()
     ldx, code, stream = _rows_of(x, "x"), _type_code(x, "x"), _together(x, dy, mean, rstd, gamma, res, dx)
-    M, D = x.shape
-    lddy = _rows_of(dy, "dy", (M, D), x.dtype)
-    ldr = _rows_of(res, "res", (M, D), x.dtype) if res is not None else 0
-    _flat(mean, "mean", (M,), torch.float32)
-    _flat(rstd, "rstd", (M,), torch.float32)
-    _flat(gamma, "gamma", (D,), torch.float32)
-    if dx is None and need_dx:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    lddx = _rows_of(dx, "dx", (M, D), x.dtype) if dx is not None else 0
+    shape, dtype = x.shape, x.dtype
+    M, D = shape
+    import torch
+    f32 = torch.float32
+    lddy = _rows_of(dy, "dy", shape, dtype)
+    ldr = 0 if res is None else _rows_of(res, "res", shape, dtype)
+    pm, ps, pg = _flat(mean, "mean", (M,), f32), _flat(rstd, "rstd", (M,), f32), _flat(gamma, "gamma", (D,), f32)
+    if dx is None:
+        lddx = D
+        if need_dx:
+            dx = x.new_empty(shape)
+    else:
+        lddx = _rows_of(dx, "dx", shape, dtype)
     dg = db = ws = None
+    floats = 0
     if need_params:
-        dg = torch.empty(D, dtype=torch.float32, device=x.device)
-        db = torch.empty(D, dtype=torch.float32, device=x.device)
-        ws = torch.empty(lib.bsr_layernorm_workspace_floats(D), dtype=torch.float32, device=x.device)
-    _check(lib.bsr_layernorm_backward(_dp(dy), lddy, _dp(x), ldx, _dp(res), ldr, code, M, D, _dp(mean), _dp(rstd), _dp(gamma), _dp(dx), lddx,
-                                      _dp(dg), _dp(db), _dp(ws), 0 if ws is None else ws.numel(), stream))
+        floats = lib.bsr_layernorm_workspace_floats(D)
+        dg, db, ws = gamma.new_empty(D), gamma.new_empty(D), gamma.new_empty(floats)
+    _check(lib.bsr_layernorm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, _dp(res), ldr, code, M, D, pm, ps, pg, _dp(dx), lddx, _dp(dg), _dp(db),
+                                      _dp(ws), floats, stream))
     return dx, dg, db
 
 
-def _distill_common(z, index, logits, labels, row_grad, others):
+def _distill_args(z, index, logits, labels, temperature, hard_weight):
     import torch
-    stream = _together(z, index, logits, labels, row_grad, *others)
     ldz, code = _rows_of(z, "z"), _type_code(z, "z")
     rows, classes = z.shape
-    ldi = _rows_of(index, "index", (rows, index.shape[-1]), torch.int32)
-    ldt = _rows_of(logits, "logits", index.shape)
-    _flat(labels, "labels", (rows,), torch.int32)
-    _flat(row_grad, "row_grad", (rows,), torch.float32)
-    return stream, (_dp(z), code, rows, classes, ldz, _dp(index), ldi, _dp(logits), _type_code(logits, "logits"), ldt, index.shape[1], _dp(labels))
+    shape = (rows, index.shape[-1])
+    ldi = _rows_of(index, "index", shape, torch.int32)
+    ldt = _rows_of(logits, "logits", shape)
+    pl = None if labels is None else _flat(labels, "labels", (rows,), torch.int32)
+    return (z.data_ptr(), code, rows, classes, ldz, index.data_ptr(), ldi, logits.data_ptr(), _type_code(logits, "logits"), ldt, shape[1], pl,
+            temperature, hard_weight)
 
 
-def _distill_forward(z, index, logits, labels, temperature, hard_weight, row_grad, grad_scale, dz, want_stats):
-    import torch
-    stream, args = _distill_common(z, index, logits, labels, row_grad, (dz,))
-    ldd = _rows_of(dz, "dz", z.shape, z.dtype) if dz is not None else 0
-    loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
-    stats = torch.empty((z.shape[0], 3), dtype=torch.float32, device=z.device) if want_stats else None
-    _check(load_library().bsr_distill_forward(*args, temperature, hard_weight, _dp(loss), _dp(stats), _dp(row_grad), grad_scale, _dp(dz), ldd, stream))
-    return loss, stats
+def _distill_dz(z, row_grad, dz):
+    """-> (row_grad's address, dz, its row stride)"""
+    pg = None
+    if row_grad is not None:
+        import torch
+        pg = _flat(row_grad, "row_grad", z.shape[:1], torch.float32)
+    if dz is None:
+        return pg, z.new_empty(z.shape), z.shape[1]
+    return pg, dz, _rows_of(dz, "dz", z.shape, z.dtype)
 
 
 def bsr_distill_forward(z, index, logits, labels=None, temperature=1.0, hard_weight=0.0):
     """Student logits z [rows,classes] bf16 or fp32, the teacher's classes index [rows,top] int32 (-1: absent) and logits [rows,top], labels
     [rows] int32 (-1: none) -> (loss [rows], stats [rows,3] for bsr_distill_backward)."""
-    return _distill_forward(z, index, logits, labels, temperature, hard_weight, None, 1.0, None, True)
+    import torch
+    stream = _together(z, index, logits, labels)
+    args = _distill_args(z, index, logits, labels, temperature, hard_weight)
+    loss, stats = z.new_empty(z.shape[0], dtype=torch.float32), z.new_empty((z.shape[0], 3), dtype=torch.float32)
+    _check(load_library().bsr_distill_forward(*args, loss.data_ptr(), stats.data_ptr(), None, 1.0, None, 0, stream))
+    return loss, stats
 
 
 def bsr_distill_forward_backward(z, index, logits, labels=None, temperature=1.0, hard_weight=0.0, row_grad=None, grad_scale=1.0, dz=None):
     """-> (loss [rows], dz [rows,classes] = grad_scale row_grad[row] dloss/dz) in one launch.  dz may be z."""
     import torch
-    if dz is None:
-        dz = torch.empty(z.shape, dtype=z.dtype, device=z.device)
-    loss, _ = _distill_forward(z, index, logits, labels, temperature, hard_weight, row_grad, grad_scale, dz, False)
+    stream = _together(z, index, logits, labels, row_grad, dz)
+    args = _distill_args(z, index, logits, labels, temperature, hard_weight)
+    pg, dz, ldd = _distill_dz(z, row_grad, dz)
+    loss = z.new_empty(z.shape[0], dtype=torch.float32)
+    _check(load_library().bsr_distill_forward(*args, loss.data_ptr(), None, pg, grad_scale, dz.data_ptr(), ldd, stream))
     return loss, dz
 
 
 def bsr_distill_backward(z, index, logits, stats, row_grad=None, labels=None, temperature=1.0, hard_weight=0.0, grad_scale=1.0, dz=None):
     """dz [rows,classes] = grad_scale row_grad[row] dloss/dz from the stats of bsr_distill_forward.  dz may be z."""
     import torch
-    if dz is None:
-        dz = torch.empty(z.shape, dtype=z.dtype, device=z.device)
-    stream, args = _distill_common(z, index, logits, labels, row_grad, (stats, dz))
-    ldd = _rows_of(dz, "dz", z.shape, z.dtype)
-    _flat(stats, "stats", (z.shape[0], 3), torch.float32)
-    _check(load_library().bsr_distill_backward(*args, temperature, hard_weight, _dp(stats), _dp(row_grad), grad_scale, _dp(dz), ldd, stream))
+    stream = _together(z, index, logits, labels, stats, row_grad, dz)
+    args = _distill_args(z, index, logits, labels, temperature, hard_weight)
+    ps = _flat(stats, "stats", (z.shape[0], 3), torch.float32)
+    pg, dz, ldd = _distill_dz(z, row_grad, dz)
+    _check(load_library().bsr_distill_backward(*args, ps, pg, grad_scale, dz.data_ptr(), ldd, stream))
     return dz
 
 

@@ -13,6 +13,7 @@
 // instruction, for fp32 results, and for bf16 results of short sums (K < EXACT_BELOW), where an fp32 sum would be closer than the cut; longer sums for bf16 results
 // take the 8-bit instructions, whose error is then below the bound of an fp32 sum in any order (K 2^-24 sum |a b|) and 60 times below the rounding of the result.
 #include <algorithm>
+#include <type_traits>
 
 #include "fp8.h"
 #include "gemm_common.h"
@@ -23,6 +24,7 @@ namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -401,15 +403,80 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
                             (const float*)(smem + NST * STAGE) + wn * TN);
 }
 
+// maximum over lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ uint32_t quarters_max(uint32_t v) {
+  const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  v = max((uint32_t)h[0], (uint32_t)h[1]);
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return max((uint32_t)r[0], (uint32_t)r[1]);
+}
+// 32 values of a block whose other three quarters lanes l ^ 16, l ^ 32 and l ^ 48 hold -> 8 bits, and the block's scale byte.  The maximum is taken of
+// the bits (two bf16 at a time), which non-finite values top: blocks that hold one go through the values again.
+template <typename T>
+__device__ __forceinline__ int quantize32(const typename Chunk<T>::vec (&v)[32 / Chunk<T>::V], i32x8& q) {
+  constexpr int V = Chunk<T>::V;
+  uint32_t most;
+  if constexpr (sizeof(T) == 2) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t d = __builtin_bit_cast(u32x4, v[i / 4])[i % 4] & 0x7fff7fffu;
+      m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, d));
+    }
+    most = quarters_max((uint32_t)max(m[0], m[1]) << 16);
+  } else {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = max(m, __float_as_uint(v[i / V][i % V]) & 0x7fffffffu);
+    most = quarters_max(m);
+  }
+  if (most >= 0x7f800000u) {
+    most = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) most = max(most, finite_bits((float)v[i / V][i % V]));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+    const float inv = inverse_of(scale8_of(most));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float a = (float)v[4 * i / V][4 * i % V], b = (float)v[4 * i / V][(4 * i + 1) % V], c = (float)v[4 * i / V][(4 * i + 2) % V], d = (float)v[4 * i / V][(4 * i + 3) % V];
+      q[i] = (int)pack8(a, b, c, d, inv);
+    }
+    return (int)scale8_of(most);
+  }
+  const int s8 = (int)scale8_of(most);
+  const float s = __uint_as_float((uint32_t)s8 << 23);        // 2^e, what the instruction divides by
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    s16x2 r = {0, 0};
+    if constexpr (sizeof(T) == 2) {
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, bf16x2{v[i / 2][4 * (i % 2)], v[i / 2][4 * (i % 2) + 1]}, s, false);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, bf16x2{v[i / 2][4 * (i % 2) + 2], v[i / 2][4 * (i % 2) + 3]}, s, true);
+    } else {
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, v[i][0], v[i][1], s, false);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, v[i][2], v[i][3], s, true);
+    }
+    q[i] = __builtin_bit_cast(int, r);
+  }
+  return s8;
+}
+
 // Few rows: what counts is that the weights come once and at once.  A workgroup owns 16 columns and all rows (16 MI of them); its eight
 // wavefronts share the k-tiles, each with its own straight from global memory into registers (a weight row's 128 bytes of a k-tile are a
-// cache line that four lanes read whole), and their sums meet in LDS in wavefront order.  Rows of bf16 or fp32 are brought to 8 bits here
-// by every workgroup for itself: they are few, and it saves the launch.
+// cache line that four lanes read whole), AHEAD of them asked for before the first is looked at, and their sums meet in LDS in wavefront
+// order.  Rows of bf16 or fp32 (X: X_VEC where they are whole, aligned pieces of 32 values) are brought to 8 bits here by every workgroup for itself: they are few, and
+// it saves the launch.  Bound by the latency of one trip to memory, then by the weights' bytes.
+enum { X_E4, X_BF16, X_BF16_VEC, X_F32, X_F32_VEC };
 constexpr int FEW_WAVES = 8, FEW_ROWS = 64;
-template <typename TX, int MI, typename T, int ACT, bool EXACT>
+template <int X, int MI, bool EXACT>
 __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void* hA, const void* hB, const void* hsa, const void* hsb, int hM, int hN,
-                                                                      int hK, int64_t lda, bool vec_x, Gemm8Desc g) {
-  constexpr bool E4 = sizeof(TX) == 1;
+                                                                      int hK, int64_t lda, Gemm8Desc g) {
+  constexpr bool VEC = X == X_BF16_VEC || X == X_F32_VEC, F32 = X == X_F32 || X == X_F32_VEC;
+  typedef typename std::conditional<F32, float, bf16>::type TX;
+  constexpr int V = Chunk<TX>::V, AHEAD = X == X_E4 ? (MI < 4 ? 4 : 2) : 4 / MI;
   __shared__ float part[FEW_WAVES][MI * 16][16 + 1];
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -421,61 +488,59 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
   f32x4 acc[MI];
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi) acc[mi] = f32x4{0.f, 0.f, 0.f, 0.f};
-  constexpr int AHEAD = 4;
   for (int kt0 = wave; kt0 < nk; kt0 += FEW_WAVES * AHEAD) {
-    i32x8 w[AHEAD];
-    int ws[AHEAD];
+    i32x8 w[AHEAD], x8[X == X_E4 ? AHEAD : 1][MI];
+    int ws[AHEAD], xs[X == X_E4 ? AHEAD : 1][MI];
+    typename Chunk<TX>::vec raw[VEC ? AHEAD : 1][MI][32 / V];
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
+    for (int a = 0; a < AHEAD; ++a) {                      // (past the end: the last k-tile again, not used)
       const int kt = min(kt0 + a * FEW_WAVES, nk - 1);
       w[a] = join8(*(const i32x4*)(wrow + (int64_t)kt * BLOCK8), *(const i32x4*)(wrow + (int64_t)kt * BLOCK8 + 16));
       ws[a] = wscale[kt];
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) {
+        const int64_t m = min(mi * 16 + lr, hM - 1);
+        if constexpr (X == X_E4) {
+          const uint8_t* p = (const uint8_t*)hA + m * ld + (int64_t)kt * BLOCK8 + lg * 32;
+          x8[a][mi] = join8(*(const i32x4*)p, *(const i32x4*)(p + 16));
+          xs[a][mi] = ((const uint8_t*)hsa)[m * lds + kt];
+        } else if constexpr (VEC) {
+          const TX* p = (const TX*)hA + m * lda + min(kt * BLOCK8 + lg * 32, hK - 32);
+#pragma unroll
+          for (int i = 0; i < 32 / V; ++i) raw[a][mi][i] = *(const typename Chunk<TX>::vec*)(p + i * V);
+        }
+      }
     }
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
       const int kt = kt0 + a * FEW_WAVES;
-      if (kt < nk) {
+      if (kt >= nk) break;
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-          const int64_t m = min(mi * 16 + lr, hM - 1);
-          i32x8 x;
-          int xs;
-          if constexpr (E4) {
-            const uint8_t* p = (const uint8_t*)hA + m * ld + (int64_t)kt * BLOCK8 + lg * 32;
-            x = join8(*(const i32x4*)p, *(const i32x4*)(p + 16));
-            xs = ((const uint8_t*)hsa)[m * lds + kt];
+      for (int mi = 0; mi < MI; ++mi) {
+        i32x8 x;
+        int s8;
+        if constexpr (X == X_E4) {
+          x = x8[a][mi];
+          s8 = xs[a][mi];
+        } else {
+          const int k0 = kt * BLOCK8 + lg * 32;
+          typename Chunk<TX>::vec v[32 / V];
+          if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < 32 / V; ++i) v[i] = k0 < hK ? raw[a][mi][i] : typename Chunk<TX>::vec{};
           } else {
-            const int k0 = kt * BLOCK8 + lg * 32;
-            const TX* p = (const TX*)hA + m * lda + k0;
-            float v[32];
-            if (vec_x && k0 + 32 <= hK) {
-              constexpr int V = Chunk<TX>::V;
-              typename Chunk<TX>::vec raw[32 / V];
+            const TX* p = (const TX*)hA + (int64_t)min(mi * 16 + lr, hM - 1) * lda + k0;
 #pragma unroll
-              for (int i = 0; i < 32 / V; ++i) raw[i] = *(const typename Chunk<TX>::vec*)(p + i * V);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = (float)raw[i / V][i % V];
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = k0 + i < hK ? (float)p[i] : 0.f;
-            }
-            uint32_t most = 0;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) most = max(most, finite_bits(v[i]));
-            most = max(most, (uint32_t)__shfl_xor((int)most, 16));
-            most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-            xs = (int)scale8_of(most);
-            const float inv = inverse_of(xs);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = (int)pack8(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+            for (int i = 0; i < 32; ++i) v[i / V][i % V] = k0 + i < hK ? p[i] : (TX)0.f;
           }
-          if constexpr (EXACT) {
+          s8 = quantize32<TX>(v, x);
+        }
+        if constexpr (EXACT) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              acc[mi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[a][2 * q], w[a][2 * q + 1], ws[a]), widen8(x[2 * q], x[2 * q + 1], xs), acc[mi], 0, 0, 0);
-          } else {
-            acc[mi] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[a], x, acc[mi], 0, 0, 0, ws[a], 0, xs);
-          }
+          for (int q = 0; q < 4; ++q)
+            acc[mi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[a][2 * q], w[a][2 * q + 1], ws[a]), widen8(x[2 * q], x[2 * q + 1], s8), acc[mi], 0, 0, 0);
+        } else {
+          acc[mi] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[a], x, acc[mi], 0, 0, 0, ws[a], 0, s8);
         }
       }
     }
@@ -486,6 +551,11 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
 #pragma unroll
     for (int e = 0; e < 4; ++e) part[wave][mi * 16 + lr][4 * lg + e] = acc[mi][e];
   __syncthreads();
+  auto get = [&](const void* p, int64_t at) __attribute__((always_inline)) { return g.out_f32 ? ((const float*)p)[at] : (float)((const bf16*)p)[at]; };
+  auto put = [&](void* p, int64_t at, float v) __attribute__((always_inline)) {
+    if (g.out_f32) ((float*)p)[at] = v;
+    else ((bf16*)p)[at] = (bf16)v;
+  };
   for (int i = tid; i < MI * 16 * 16; i += FEW_WAVES * 64) {
     const int m = i / 16, col = n0 + i % 16;
     if (m >= hM || col >= hN) continue;
@@ -494,14 +564,14 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
     for (int w = 1; w < FEW_WAVES; ++w) v += part[w][m][i % 16];
     const int64_t at = (int64_t)m * g.ldc + col;
     if (g.bias) v += g.bias[col];
-    if (ACT == ACT_GELU) {
-      if (g.aux) ((T*)g.aux)[at] = (T)v;
+    if (g.act == ACT_GELU) {
+      if (g.aux) put(g.aux, at, v);
       v = gelu_f(v);
-    } else if (ACT == ACT_GELU_BWD) {
-      v *= gelu_grad_f((float)((const T*)g.aux)[at]);
+    } else if (g.act == ACT_GELU_BWD) {
+      v *= gelu_grad_f(get(g.aux, at));
     }
-    if (g.res) v += (float)((const T*)g.res)[at];
-    ((T*)g.C)[at] = (T)v;
+    if (g.res) v += get(g.res, at);
+    put(g.C, at, v);
   }
 }
 
@@ -531,32 +601,31 @@ void tiled(const Gemm8Desc& g, hipStream_t s) {
   else launch_tiled<64, 64, 2, 1, 4, T, ACT, EXACT>(g, s);
 }
 
-template <typename TX, typename T, int ACT, bool EXACT>
-void few(const Gemm8Desc& g, hipStream_t s) {
+template <int X, bool EXACT>
+void few_as(const Gemm8Desc& g, hipStream_t s) {
   const unsigned grid = (unsigned)((g.N + 15) / 16);
-  const int64_t lda = g.lda;
-  const bool vec = ((uintptr_t)g.A & 15) == 0 && lda * (int64_t)sizeof(TX) % 16 == 0;
   auto go = [&](auto MI) {
-    gemm8_few_kernel<TX, decltype(MI)::value, T, ACT, EXACT><<<grid, FEW_WAVES * 64, 0, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, lda, vec, g);
+    gemm8_few_kernel<X, decltype(MI)::value, EXACT><<<grid, FEW_WAVES * 64, 0, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, g.lda, g);
   };
   if (g.M <= 16) go(IC<1>{});
   else if (g.M <= 32) go(IC<2>{});
   else go(IC<4>{});
 }
-
-template <typename T, int ACT, bool EXACT>
-void run(const Gemm8Desc& g, hipStream_t s) {
-  if (g.M > FEW_ROWS) tiled<T, ACT, EXACT>(g, s);
-  else if (g.a_type == 0) few<bf16, T, ACT, EXACT>(g, s);
-  else if (g.a_type == 1) few<float, T, ACT, EXACT>(g, s);
-  else few<uint8_t, T, ACT, EXACT>(g, s);
+template <bool EXACT>
+void few(const Gemm8Desc& g, hipStream_t s) {
+  const bool vec = ((uintptr_t)g.A & 15) == 0 && g.lda * (g.a_type == 1 ? 4 : 2) % 16 == 0 && g.K % 32 == 0;
+  if (g.a_type == 2) few_as<X_E4, EXACT>(g, s);
+  else if (g.a_type == 1 && vec) few_as<X_F32_VEC, EXACT>(g, s);
+  else if (g.a_type == 1) few_as<X_F32, EXACT>(g, s);
+  else if (vec) few_as<X_BF16_VEC, EXACT>(g, s);
+  else few_as<X_BF16, EXACT>(g, s);
 }
 
-template <int ACT>
-void run_type(const Gemm8Desc& g, hipStream_t s) {
-  if (g.out_f32) run<float, ACT, true>(g, s);
-  else if (g.K < EXACT_BELOW) run<bf16, ACT, true>(g, s);
-  else run<bf16, ACT, false>(g, s);
+template <typename T, bool EXACT>
+void tiled_act(const Gemm8Desc& g, hipStream_t s) {
+  if (g.act == ACT_GELU) tiled<T, ACT_GELU, EXACT>(g, s);
+  else if (g.act == ACT_GELU_BWD) tiled<T, ACT_GELU_BWD, EXACT>(g, s);
+  else tiled<T, ACT_NONE, EXACT>(g, s);
 }
 
 }  // namespace
@@ -565,9 +634,11 @@ bool gemm8_few_takes(int64_t M) { return M <= FEW_ROWS; }
 
 void gemm8(const Gemm8Desc& g, hipStream_t s) {
   if (g.M <= 0) return;
-  if (g.act == ACT_GELU) run_type<ACT_GELU>(g, s);
-  else if (g.act == ACT_GELU_BWD) run_type<ACT_GELU_BWD>(g, s);
-  else run_type<ACT_NONE>(g, s);
+  const bool exact = g.out_f32 || g.K < EXACT_BELOW;
+  if (g.M <= FEW_ROWS) exact ? few<true>(g, s) : few<false>(g, s);
+  else if (g.out_f32) tiled_act<float, true>(g, s);
+  else if (exact) tiled_act<bf16, true>(g, s);
+  else tiled_act<bf16, false>(g, s);
 }
 
 }  // namespace bsr

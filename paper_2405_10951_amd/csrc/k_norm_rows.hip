@@ -16,7 +16,15 @@ namespace {
 
 constexpr int FINAL_WAVES = 16;
 
-// sums of a and b over the threads of a row: a wavefront, or the four of a workgroup (red: two floats a wavefront; a second buffer in turn, so that
+// A piece of a row: V values, V 16-byte chunks' worth or 1 (rows that are no whole chunks, or are not aligned to them)
+template <typename T, int V> struct Piece { typedef T vec __attribute__((ext_vector_type(V))); };
+template <typename T> struct Piece<T, 1> { struct vec { T v; __device__ __forceinline__ T& operator[](int) { return v; } __device__ __forceinline__ T operator[](int) const { return v; } }; };
+template <int V> __device__ __forceinline__ void params(const float* p, float (&o)[V]) {
+  if constexpr (V == 1) o[0] = *p;
+  else load_params<V>(p, o);
+}
+
+// sums of a and b over the threads of a row: a wavefront, or all of a workgroup (red: two floats a wavefront; a second buffer in turn, so that
 // one barrier a row is enough)
 template <int TPR>
 __device__ __forceinline__ void row_sums(float& a, float& b, float (*red)[2]) {
@@ -39,23 +47,34 @@ template <int N> __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
   return v;
 }
 
-template <typename T, int TPR, int MAXC, bool OUT, bool OUT8>
-__global__ __launch_bounds__(256) void rows_fwd_kernel(const T* __restrict__ x, int64_t M, int D, int64_t ldx, const float* __restrict__ gamma,
-                                                       const float* __restrict__ beta, float eps, T* __restrict__ y, int64_t ldy,
-                                                       uint8_t* __restrict__ q, uint8_t* __restrict__ scale, float* __restrict__ mean,
-                                                       float* __restrict__ rstd) {
-  constexpr int V = Chunk<T>::V;
-  typedef typename Chunk<T>::vec vec;
-  __shared__ float red[2][4][2];
+template <int TPR> constexpr int block_threads() { return TPR > 256 ? TPR : 256; }
+
+template <typename T, int V, int TPR, int MAXC, bool OUT, bool OUT8>
+__global__ __launch_bounds__(block_threads<TPR>()) void rows_fwd_kernel(const T* __restrict__ x, int64_t M, int D, int64_t ldx,
+                                                                        const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
+                                                                        T* __restrict__ y, int64_t ldy, uint8_t* __restrict__ q,
+                                                                        uint8_t* __restrict__ scale, float* __restrict__ mean,
+                                                                        float* __restrict__ rstd) {
+  typedef typename Piece<T, V>::vec vec;
+  constexpr int NT = block_threads<TPR>();
+  constexpr bool AHEAD = V * MAXC <= 16;                   // gamma and beta asked for with the row (more would cost wavefronts)
+  __shared__ float red[2][NT / WAVE][2];
   const int t = threadIdx.x % TPR;
-  const int64_t m = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  const int64_t m = (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
   if (m >= M) return;                                     // (whole wavefronts, or the whole workgroup)
   const int nch = D / V;
   const T* xr = x + m * ldx;
   vec raw[MAXC];
-  float v[MAXC][V];
+  float v[MAXC][V], g[AHEAD ? MAXC : 1][V], b[AHEAD ? MAXC : 1][V];
 #pragma unroll
   for (int i = 0; i < MAXC; ++i) raw[i] = *(const vec*)(xr + min(t + i * TPR, nch - 1) * V);
+  if constexpr (AHEAD)
+#pragma unroll
+    for (int i = 0; i < MAXC; ++i) {
+      const int c = min(t + i * TPR, nch - 1) * V;
+      params<V>(gamma + c, g[i]);
+      params<V>(beta + c, b[i]);
+    }
   float s = 0.f, none = 0.f;
 #pragma unroll
   for (int i = 0; i < MAXC; ++i)
@@ -75,16 +94,18 @@ __global__ __launch_bounds__(256) void rows_fwd_kernel(const T* __restrict__ x, 
     if (rstd) rstd[m] = rs;
   }
   const int64_t ldq = ld8(D), lds = ld8s(D);
+  float o1[OUT8 && V == 1 ? MAXC : 1];
 #pragma unroll
   for (int i = 0; i < MAXC; ++i) {
     const int c = t + i * TPR;
     float o[V];
     if (c < nch) {
-      float g[V], b[V];
-      load_params<V>(gamma + c * V, g);
-      load_params<V>(beta + c * V, b);
+      if constexpr (!AHEAD) {
+        params<V>(gamma + c * V, g[0]);
+        params<V>(beta + c * V, b[0]);
+      }
 #pragma unroll
-      for (int e = 0; e < V; ++e) o[e] = (v[i][e] - mu) * rs * g[e] + b[e];
+      for (int e = 0; e < V; ++e) o[e] = (v[i][e] - mu) * rs * g[AHEAD ? i : 0][e] + b[AHEAD ? i : 0][e];
     } else {
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] = 0.f;
@@ -95,7 +116,19 @@ __global__ __launch_bounds__(256) void rows_fwd_kernel(const T* __restrict__ x, 
       for (int e = 0; e < V; ++e) w[e] = (T)o[e];
       *(vec*)(y + m * ldy + c * V) = w;
     }
-    if constexpr (OUT8) {                                 // BLOCK8 / V neighbouring lanes hold a block
+    if constexpr (OUT8 && V == 1) {                       // two pieces of a wavefront hold a block
+      static_assert(TPR == WAVE && MAXC % 2 == 0, "");
+      o1[i] = o[0];
+      if (i % 2 == 1 && (i - 1) * TPR < ldq) {
+        const uint32_t s8 = scale8_of(__float_as_uint(wave_max(__uint_as_float(max(finite_bits(o1[i - 1]), finite_bits(o1[i]))))));
+        const float inv = inverse_of(s8);
+        uint8_t* to = q + m * ldq + (i - 1) * TPR + t;
+        const uint32_t two = pack8(o1[i - 1], o1[i], 0.f, 0.f, inv);
+        to[0] = (uint8_t)two;
+        to[TPR] = (uint8_t)(two >> 8);
+        if (t == 0) scale[m * lds + i / 2] = (uint8_t)s8;
+      }
+    } else if constexpr (OUT8) {                          // BLOCK8 / V neighbouring lanes hold a block
       if (i * TPR * V < ldq) {
         uint32_t most = 0;
 #pragma unroll
@@ -155,26 +188,32 @@ __global__ __launch_bounds__(256) void rows_fwd_any_kernel(const T* __restrict__
   if (OUT8 && lane < lds - ldq / BLOCK8) scale[m * lds + ldq / BLOCK8 + lane] = 127;
 }
 
-// Backward, with the next row's loads in flight.  256 / TPR rows of a workgroup at a time; each walks every gridDim.x (256 / TPR)-th row and keeps
+// Backward, with the next row's loads in flight.  Each group of TPR threads walks every gridDim.x (NT / TPR)-th row and keeps
 // its sums for dgamma and dbeta in registers; the wavefronts of a workgroup then add theirs in a fixed order and leave them in
 // partial[blockIdx.x] = [dgamma | dbeta].
-template <typename T, int TPR, int MAXC, bool DX, bool PARAMS>
-__global__ __launch_bounds__(256) void rows_bwd_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx,
-                                                       const T* __restrict__ res, int64_t ldr, int64_t M, int D, const float* __restrict__ mean,
-                                                       const float* __restrict__ rstd, const float* __restrict__ gamma, T* __restrict__ dx,
-                                                       int64_t lddx, float* __restrict__ partial) {
-  constexpr int V = Chunk<T>::V, RPB = 256 / TPR;
-  typedef typename Chunk<T>::vec vec;
-  extern __shared__ float lds_sums[];                     // [RPB - 1][2][D]
-  __shared__ float red[2][4][2];
+template <typename T, int V, int TPR, int MAXC, bool DX, bool PARAMS, bool RES>
+__global__ __launch_bounds__(block_threads<TPR>(), TPR == 512 ? 4 : 1) void rows_bwd_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx,
+                                                                        const T* __restrict__ res, int64_t ldr, int64_t M, int D,
+                                                                        const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                                        const float* __restrict__ gamma, T* __restrict__ dx, int64_t lddx,
+                                                                        float* __restrict__ partial) {
+  constexpr int NT = block_threads<TPR>(), RPB = NT / TPR;
+  typedef typename Piece<T, V>::vec vec;
+  constexpr bool KEEP = NT <= 256;                        // gamma in registers (larger workgroups: more wavefronts on the CU count for more)
+  constexpr bool RES_EARLY = TPR < 512;                   // (as the residual row a row ahead)
+  extern __shared__ __attribute__((aligned(16))) float lds_sums[];                     // [RPB / 2][2][D]
+  __shared__ float red[2][NT / WAVE][2];
   const int t = threadIdx.x % TPR, r = threadIdx.x / TPR, nch = D / V;
   const int64_t stride = (int64_t)gridDim.x * RPB;
-  float dg[MAXC][V], db[MAXC][V];
+  float dg[PARAMS ? MAXC : 1][V], db[PARAMS ? MAXC : 1][V], gk[KEEP ? MAXC : 1][V];
 #pragma unroll
-  for (int i = 0; i < MAXC; ++i)
+  for (int i = 0; i < (PARAMS ? MAXC : 1); ++i)
 #pragma unroll
     for (int e = 0; e < V; ++e) dg[i][e] = db[i][e] = 0.f;
-  vec na[MAXC], nx[MAXC];
+  if constexpr (KEEP)
+#pragma unroll
+    for (int i = 0; i < MAXC; ++i) params<V>(gamma + min(t + i * TPR, nch - 1) * V, gk[i]);
+  vec na[MAXC], nx[MAXC], nr[RES && RES_EARLY ? MAXC : 1];
   float nmu = 0.f, nrs = 0.f;
   auto prefetch = [&](int64_t m) __attribute__((always_inline)) {
     if (m >= M) return;
@@ -183,6 +222,7 @@ __global__ __launch_bounds__(256) void rows_bwd_kernel(const T* __restrict__ dy,
       const int c = min(t + i * TPR, nch - 1) * V;
       na[i] = *(const vec*)(dy + m * lddy + c);
       nx[i] = *(const vec*)(x + m * ldx + c);
+      if constexpr (RES && RES_EARLY) nr[i] = *(const vec*)(res + m * ldr + c);
     }
     nmu = mean[m];
     nrs = rstd[m];
@@ -190,9 +230,13 @@ __global__ __launch_bounds__(256) void rows_bwd_kernel(const T* __restrict__ dy,
   int64_t m = (int64_t)blockIdx.x * RPB + r;
   prefetch(m);
   for (int turn = 0; m < M; m += stride, turn ^= 1) {
-    vec a[MAXC], b[MAXC];
+    vec a[MAXC], b[MAXC], c[RES ? MAXC : 1];
 #pragma unroll
-    for (int i = 0; i < MAXC; ++i) { a[i] = na[i]; b[i] = nx[i]; }
+    for (int i = 0; i < MAXC; ++i) {
+      a[i] = na[i];
+      b[i] = nx[i];
+      if constexpr (RES && RES_EARLY) c[i] = nr[i];
+    }
     const float mu = nmu, rs = nrs;
     prefetch(m + stride);
     float s1 = 0.f, s2 = 0.f;
@@ -200,60 +244,75 @@ __global__ __launch_bounds__(256) void rows_bwd_kernel(const T* __restrict__ dy,
     for (int i = 0; i < MAXC; ++i)
       if (t + i * TPR < nch) {
         float g[V];
-        load_params<V>(gamma + (t + i * TPR) * V, g);
+        if constexpr (!KEEP) params<V>(gamma + (t + i * TPR) * V, g);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const float d = (float)a[i][e], xh = ((float)b[i][e] - mu) * rs;
-          if (PARAMS) { dg[i][e] += d * xh; db[i][e] += d; }
-          s1 += d * g[e];
-          s2 += d * g[e] * xh;
+          const float d = (float)a[i][e], xh = ((float)b[i][e] - mu) * rs, gd = d * (KEEP ? gk[KEEP ? i : 0][e] : g[e]);
+          if constexpr (PARAMS) { dg[i][e] += d * xh; db[i][e] += d; }
+          s1 += gd;
+          s2 += gd * xh;
         }
       }
     if constexpr (DX) {
+      if constexpr (RES && !RES_EARLY)
+#pragma unroll
+        for (int i = 0; i < MAXC; ++i) c[i] = *(const vec*)(res + m * ldr + min(t + i * TPR, nch - 1) * V);
       row_sums<TPR>(s1, s2, red[turn]);
       const float m1 = s1 / (float)D, m2 = s2 / (float)D;
 #pragma unroll
       for (int i = 0; i < MAXC; ++i) {
-        const int c = t + i * TPR;
-        if (c < nch) {
+        const int ch = t + i * TPR;
+        if (ch < nch) {
           float g[V];
-          load_params<V>(gamma + c * V, g);
-          vec rr, o;
-          if (res) rr = *(const vec*)(res + m * ldr + c * V);
+          if constexpr (!KEEP) params<V>(gamma + ch * V, g);
+          vec o;
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             const float xh = ((float)b[i][e] - mu) * rs;
-            float v = rs * ((float)a[i][e] * g[e] - m1 - xh * m2);
-            if (res) v += (float)rr[e];
+            float v = rs * ((float)a[i][e] * (KEEP ? gk[KEEP ? i : 0][e] : g[e]) - m1 - xh * m2);
+            if constexpr (RES) v += (float)c[i][e];
             o[e] = (T)v;
           }
-          *(vec*)(dx + m * lddx + c * V) = o;
+          *(vec*)(dx + m * lddx + ch * V) = o;
         }
       }
     }
   }
   if constexpr (PARAMS) {
-    auto each = [&](auto f) __attribute__((always_inline)) {
+    // the sums to p = [dgamma | dbeta], or those at p added to them; four at a time where pieces are whole chunks
+    auto leave = [&](float* p) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < MAXC; ++i)
-        if (t + i * TPR < nch)
+        if (t + i * TPR < nch) {
+          float* to = p + (t + i * TPR) * V;
+          if constexpr (V == 1) { to[0] = dg[i][0]; to[D] = db[i][0]; }
+          else
 #pragma unroll
-          for (int e = 0; e < V; ++e) f((t + i * TPR) * V + e, i, e);
+            for (int e = 0; e < V; e += 4) {
+              *(float4*)(to + e) = make_float4(dg[i][e], dg[i][e + 1], dg[i][e + 2], dg[i][e + 3]);
+              *(float4*)(to + D + e) = make_float4(db[i][e], db[i][e + 1], db[i][e + 2], db[i][e + 3]);
+            }
+        }
     };
-    if constexpr (RPB > 1) {
-      if (r > 0) {
-        float* p = lds_sums + (size_t)(r - 1) * 2 * D;
-        each([&](int j, int i, int e) { p[j] = dg[i][e]; p[D + j] = db[i][e]; });
-      }
+    auto add = [&](const float* p) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < MAXC; ++i)
+        if (t + i * TPR < nch) {
+          float u[V], w[V];
+          params<V>(p + (t + i * TPR) * V, u);
+          params<V>(p + D + (t + i * TPR) * V, w);
+#pragma unroll
+          for (int e = 0; e < V; ++e) { dg[i][e] += u[e]; db[i][e] += w[e]; }
+        }
+    };
+#pragma unroll
+    for (int half = RPB / 2; half > 0; half /= 2) {       // (pairwise: a fixed tree)
+      if (r >= half && r < 2 * half) leave(lds_sums + (size_t)(r - half) * 2 * D);
       __syncthreads();
-      if (r > 0) return;
-      for (int k = 0; k < RPB - 1; ++k) {
-        const float* p = lds_sums + (size_t)k * 2 * D;
-        each([&](int j, int i, int e) { dg[i][e] += p[j]; db[i][e] += p[D + j]; });
-      }
+      if (r < half) add(lds_sums + (size_t)r * 2 * D);
+      __syncthreads();
     }
-    float* p = partial + (int64_t)blockIdx.x * 2 * D;
-    each([&](int j, int i, int e) { p[j] = dg[i][e]; p[D + j] = db[i][e]; });
+    if (r == 0) leave(partial + (int64_t)blockIdx.x * 2 * D);
   }
 }
 
@@ -315,8 +374,14 @@ __global__ __launch_bounds__(FINAL_WAVES * WAVE) void rows_bwd_final_kernel(cons
   const int64_t col = (int64_t)blockIdx.x * WAVE + lane;
   float s = 0.f;
   if (col < 2 * (int64_t)D) {
-#pragma unroll 8
-    for (int r = w; r < rows; r += FINAL_WAVES) s += partial[(int64_t)r * 2 * D + col];
+    // eight rows on their way at a time, those past the last one again and not counted (one by one they would each be a trip to memory)
+    for (int r0 = w; r0 < rows; r0 += 8 * FINAL_WAVES) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = partial[(int64_t)min(r0 + k * FINAL_WAVES, rows - 1) * 2 * D + col];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += r0 + k * FINAL_WAVES < rows ? v[k] : 0.f;
+    }
   }
   red[w][lane] = s;
   __syncthreads();
@@ -329,14 +394,25 @@ __global__ __launch_bounds__(FINAL_WAVES * WAVE) void rows_bwd_final_kernel(cons
   }
 }
 
-// f(threads per row, chunks per thread) for rows of n chunks; false: too long
-template <class F> bool with_row_shape(int n, F&& f) {
-  if (n <= 64) f(RowC<64>{}, RowC<1>{});
-  else if (n <= 128) f(RowC<64>{}, RowC<2>{});
-  else if (n <= 256) f(RowC<64>{}, RowC<4>{});
-  else if (n <= 512) f(RowC<256>{}, RowC<2>{});
-  else if (n <= 1024) f(RowC<256>{}, RowC<4>{});
-  else if (n <= 2048) f(RowC<256>{}, RowC<8>{});
+// f(values per piece, threads per row, pieces per thread) for a row of whole 16-byte chunks; false: too long.  Two chunks a thread leave registers for
+// four wavefronts a SIMD in the backward pass.
+template <typename T, class F> bool with_row_chunks_of(int D, F&& f) {
+  constexpr int V = Chunk<T>::V;
+  const int n = D / V;
+  if (n <= 64) f(RowC<V>{}, RowC<64>{}, RowC<1>{});
+  else if (n <= 128) f(RowC<V>{}, RowC<64>{}, RowC<2>{});
+  else if (n <= 256) f(RowC<V>{}, RowC<256>{}, RowC<1>{});
+  else if (n <= 512) f(RowC<V>{}, RowC<256>{}, RowC<2>{});
+  else if (n <= 1024) f(RowC<V>{}, RowC<512>{}, RowC<2>{});
+  else if (n <= 2048) f(RowC<V>{}, RowC<1024>{}, RowC<2>{});
+  else return false;
+  return true;
+}
+// the backward pass of rows that are no whole chunks: a value a piece
+template <class F> bool with_row_values(int D, F&& f) {
+  if (D <= 512) f(RowC<1>{}, RowC<64>{}, RowC<8>{});
+  else if (D <= 2048) f(RowC<1>{}, RowC<256>{}, RowC<8>{});
+  else if (D <= 8192) f(RowC<1>{}, RowC<1024>{}, RowC<8>{});
   else return false;
   return true;
 }
@@ -345,14 +421,21 @@ template <typename T> bool in_chunks(const void* p, int64_t ld) { return ((uintp
 
 template <typename T, bool OUT, bool OUT8>
 void fwd_as(const NormRows& a, hipStream_t s) {
-  constexpr int V = Chunk<T>::V;
-  const bool vec = a.D % V == 0 && in_chunks<T>(a.x, a.ldx) && (!OUT || in_chunks<T>(a.y, a.ldy)) &&
-                   with_row_shape(a.D / V, [&](auto TPR, auto C) {
-                     constexpr int tpr = decltype(TPR)::value, rpb = 256 / tpr;
-                     rows_fwd_kernel<T, tpr, decltype(C)::value, OUT, OUT8><<<(unsigned)((a.M + rpb - 1) / rpb), 256, 0, s>>>(
-                         (const T*)a.x, a.M, a.D, a.ldx, a.gamma, a.beta, a.eps, (T*)a.y, a.ldy, (uint8_t*)a.q, a.scale, a.mean, a.rstd);
-                   });
-  if (!vec)
+  const bool whole = a.D % Chunk<T>::V == 0 && in_chunks<T>(a.x, a.ldx) && (!OUT || in_chunks<T>(a.y, a.ldy));
+  auto go = [&](auto P, auto TPR, auto C) {
+    constexpr int v = decltype(P)::value, tpr = decltype(TPR)::value, nt = block_threads<tpr>(), rpb = nt / tpr;
+    rows_fwd_kernel<T, v, tpr, decltype(C)::value, OUT, OUT8><<<(unsigned)((a.M + rpb - 1) / rpb), nt, 0, s>>>(
+          (const T*)a.x, a.M, a.D, a.ldx, a.gamma, a.beta, a.eps, (T*)a.y, a.ldy, (uint8_t*)a.q, a.scale, a.mean, a.rstd);
+  };
+  bool done = true;
+  // (8-bit blocks are put together from neighbouring chunks, or from two values of every lane of a wavefront; with and without them a row is summed the
+  // same way)
+  if (whole) done = with_row_chunks_of<T>(a.D, go);
+  else if (a.D <= 512) go(RowC<1>{}, RowC<64>{}, RowC<8>{});
+  else if (a.D <= 2048) go(RowC<1>{}, RowC<64>{}, RowC<32>{});
+  else if (a.D <= 6144) go(RowC<1>{}, RowC<64>{}, RowC<96>{});
+  else done = false;
+  if (!done)
     rows_fwd_any_kernel<T, OUT, OUT8><<<(unsigned)((a.M + 3) / 4), 256, 0, s>>>((const T*)a.x, a.M, a.D, a.ldx, a.gamma, a.beta, a.eps, (T*)a.y, a.ldy,
                                                                               (uint8_t*)a.q, a.scale, a.mean, a.rstd);
 }
@@ -365,27 +448,31 @@ void fwd(const NormRows& a, hipStream_t s) {
 
 template <typename T>
 void bwd(const NormRowsBwd& a, hipStream_t s) {
-  constexpr int V = Chunk<T>::V;
   const bool params = a.dgamma != nullptr;
   int rows = 0;                                           // partial rows
   if (a.M > 0) {
-    const bool vec = a.D % V == 0 && in_chunks<T>(a.dy, a.lddy) && in_chunks<T>(a.x, a.ldx) && (!a.res || in_chunks<T>(a.res, a.ldr)) &&
-                     (!a.dx || in_chunks<T>(a.dx, a.lddx)) && with_row_shape(a.D / V, [&](auto TPR, auto C) {
-                       constexpr int tpr = decltype(TPR)::value, rpb = 256 / tpr, maxc = decltype(C)::value;
-                       const int64_t need = (a.M + rpb - 1) / rpb;
-                       auto go = [&](auto DX, auto PARAMS) {
-                         constexpr bool p = decltype(PARAMS)::value != 0;
-                         const unsigned grid = (unsigned)(p ? std::min<int64_t>(need, NORM_PARTIALS) : need);
-                         rows_bwd_kernel<T, tpr, maxc, decltype(DX)::value != 0, p><<<grid, 256, p ? (rpb - 1) * 2 * a.D * sizeof(float) : 0, s>>>(
-                             (const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, (const T*)a.res, a.ldr, a.M, a.D, a.mean, a.rstd, a.gamma, (T*)a.dx, a.lddx,
-                             a.partial);
-                         if (p) rows = (int)grid;
-                       };
-                       if (!params) go(RowC<1>{}, RowC<0>{});
-                       else if (a.dx) go(RowC<1>{}, RowC<1>{});
-                       else go(RowC<0>{}, RowC<1>{});
-                     });
-    if (!vec) {
+    const bool whole = a.D % Chunk<T>::V == 0 && in_chunks<T>(a.dy, a.lddy) && in_chunks<T>(a.x, a.ldx) && (!a.res || in_chunks<T>(a.res, a.ldr)) &&
+                       (!a.dx || in_chunks<T>(a.dx, a.lddx));
+    auto shaped = [&](auto P, auto TPR, auto C) {
+      constexpr int v = decltype(P)::value, tpr = decltype(TPR)::value, maxc = decltype(C)::value;
+      auto go = [&](auto DX, auto PARAMS, auto RES) {
+        constexpr bool p = decltype(PARAMS)::value != 0;
+        constexpr int nt = block_threads<tpr>(), rpb = nt / tpr;
+        const int64_t need = (a.M + rpb - 1) / rpb;
+        const unsigned grid = (unsigned)(p ? std::min<int64_t>(need, NORM_PARTIALS) : need);
+        rows_bwd_kernel<T, v, tpr, maxc, decltype(DX)::value != 0, p, decltype(RES)::value != 0>
+            <<<grid, nt, p ? rpb / 2 * 2 * a.D * sizeof(float) : 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, (const T*)a.res, a.ldr, a.M, a.D,
+                                                                       a.mean, a.rstd, a.gamma, (T*)a.dx, a.lddx, a.partial);
+        if (p) rows = (int)grid;
+      };
+      if (!a.dx) go(RowC<0>{}, RowC<1>{}, RowC<0>{});
+      else if (a.res && params) go(RowC<1>{}, RowC<1>{}, RowC<1>{});
+      else if (a.res) go(RowC<1>{}, RowC<0>{}, RowC<1>{});
+      else if (params) go(RowC<1>{}, RowC<1>{}, RowC<0>{});
+      else go(RowC<1>{}, RowC<0>{}, RowC<0>{});
+    };
+    const bool done = whole ? with_row_chunks_of<T>(a.D, shaped) : with_row_values(a.D, shaped);
+    if (!done) {
       if (a.dx)
         rows_bwd_dx_any_kernel<T><<<(unsigned)((a.M + 3) / 4), 256, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, (const T*)a.res, a.ldr, a.M,
                                                                           a.D, a.mean, a.rstd, a.gamma, (T*)a.dx, a.lddx);

@@ -51,9 +51,8 @@ def test_rows_to_8_bits(env, M, K, extra, dtype):
     check_blocks(host(x), (r.values, r.scales), 1)
 
 
-def test_rows_with_special_values(env):
+def special_rows(torch):
     """zeros, ties, the ends of the range, subnormals, infinities and NaN"""
-    torch, P = env
     x = torch.zeros(9, 256)
     x[1, 0] = 448.0
     x[1, 1:9] = torch.tensor([17.0, 19.0, 21.0, 1.0625, 2 ** -9, 2 ** -10, 3 * 2 ** -10, -17.0])      # halfway between neighbours
@@ -64,8 +63,36 @@ def test_rows_with_special_values(env):
     x[6, 3], x[6, 4], x[6, 5] = float("inf"), float("nan"), 2.5
     x[7, 128:] = float("-inf")
     x[8, :] = torch.finfo(torch.float32).min
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_with_special_values(env, dtype):
+    torch, P = env
+    x = special_rows(torch).to(dtypes(torch)[dtype])
     r = P.bsr_quantize8_rows(x.cuda())
     check_blocks(host(x), (r.values, r.scales), 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [256, 250])
+def test_special_values_on_the_way(env, K, dtype):
+    """few rows are brought to 8 bits inside the product: row i against a weight that picks columns out one by one gives the values themselves, the very
+    ones that the rows in 8 bits give (and NaN where a row has one: 0 times NaN)"""
+    torch, P = env
+    x = special_rows(torch)[:, :K].to(dtypes(torch)[dtype]).cuda()
+    x = torch.cat([x, torch.randn(5, K, device="cuda").to(x.dtype), 1e-3 * torch.randn(2, K, device="cuda").to(x.dtype)])
+    layer = P.bsr_quantize8_weight(torch.eye(K, device="cuda"))
+    a = P.bsr_linear8_forward(x, layer, out_dtype=torch.float32)
+    b = P.bsr_linear8_forward(P.bsr_quantize8_rows(x), layer, out_dtype=torch.float32)
+    assert torch.equal(a.nan_to_num(7.0, 8.0, 9.0), b.nan_to_num(7.0, 8.0, 9.0))
+    want, _ = blocks8(host(x), 1, 128)
+    with np.errstate(over="ignore"):
+        finite = np.isfinite(want.astype(np.float32)).all(1)         # (the largest fp32 values round up to 2^128)
+    assert 0 < finite.sum() < len(finite)
+    assert np.array_equal(np.isnan(host(a)).all(1), ~finite) and np.array_equal(np.isnan(host(a)).any(1), ~finite)
+    normal = finite & (np.abs(want).max(1) > 1e-30)
+    assert np.array_equal(host(a)[normal], want[normal])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
