@@ -200,7 +200,7 @@ __global__ __launch_bounds__(block_threads<TPR>(), TPR == 512 ? 4 : 1) void rows
   constexpr int NT = block_threads<TPR>(), RPB = NT / TPR;
   typedef typename Piece<T, V>::vec vec;
   constexpr bool KEEP = NT <= 256;                        // gamma in registers (larger workgroups: more wavefronts on the CU count for more)
-  constexpr bool RES_EARLY = TPR < 512;                   // (as the residual row a row ahead)
+  constexpr bool RES_EARLY = TPR < 512;                   // the residual a row ahead as well
   extern __shared__ __attribute__((aligned(16))) float lds_sums[];                     // [RPB / 2][2][D]
   __shared__ float red[2][NT / WAVE][2];
   const int t = threadIdx.x % TPR, r = threadIdx.x / TPR, nch = D / V;
@@ -254,10 +254,10 @@ __global__ __launch_bounds__(block_threads<TPR>(), TPR == 512 ? 4 : 1) void rows
         }
       }
     if constexpr (DX) {
+      row_sums<TPR>(s1, s2, red[turn]);
       if constexpr (RES && !RES_EARLY)
 #pragma unroll
         for (int i = 0; i < MAXC; ++i) c[i] = *(const vec*)(res + m * ldr + min(t + i * TPR, nch - 1) * V);
-      row_sums<TPR>(s1, s2, red[turn]);
       const float m1 = s1 / (float)D, m2 = s2 / (float)D;
 #pragma unroll
       for (int i = 0; i < MAXC; ++i) {
@@ -374,13 +374,14 @@ __global__ __launch_bounds__(FINAL_WAVES * WAVE) void rows_bwd_final_kernel(cons
   const int64_t col = (int64_t)blockIdx.x * WAVE + lane;
   float s = 0.f;
   if (col < 2 * (int64_t)D) {
-    // eight rows on their way at a time, those past the last one again and not counted (one by one they would each be a trip to memory)
-    for (int r0 = w; r0 < rows; r0 += 8 * FINAL_WAVES) {
-      float v[8];
+    // all rows of a wavefront on their way at once, those past the last one again and not counted (one by one they would each be a trip to memory)
+    constexpr int K = NORM_PARTIALS / FINAL_WAVES;
+    for (int r0 = w; r0 < rows; r0 += K * FINAL_WAVES) {
+      float v[K];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = partial[(int64_t)min(r0 + k * FINAL_WAVES, rows - 1) * 2 * D + col];
+      for (int k = 0; k < K; ++k) v[k] = partial[(int64_t)min(r0 + k * FINAL_WAVES, rows - 1) * 2 * D + col];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s += r0 + k * FINAL_WAVES < rows ? v[k] : 0.f;
+      for (int k = 0; k < K; ++k) s += r0 + k * FINAL_WAVES < rows ? v[k] : 0.f;
     }
   }
   red[w][lane] = s;
