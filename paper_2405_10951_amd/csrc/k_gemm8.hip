@@ -470,13 +470,13 @@ __device__ __forceinline__ int quantize32(const typename Chunk<T>::vec (&v)[32 /
 // order.  Rows of bf16 or fp32 (X: X_VEC where they are whole, aligned pieces of 32 values) are brought to 8 bits here by every workgroup for itself: they are few, and
 // it saves the launch.  Bound by the latency of one trip to memory, then by the weights' bytes.
 enum { X_E4, X_BF16, X_BF16_VEC, X_F32, X_F32_VEC };
-constexpr int FEW_WAVES = 8, FEW_ROWS = 64;
+constexpr int FEW_WAVES = 8, FEW_ROWS = 32;
 template <int X, int MI, bool EXACT>
 __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void* hA, const void* hB, const void* hsa, const void* hsb, int hM, int hN,
                                                                       int hK, int64_t lda, Gemm8Desc g) {
   constexpr bool VEC = X == X_BF16_VEC || X == X_F32_VEC, F32 = X == X_F32 || X == X_F32_VEC;
   typedef typename std::conditional<F32, float, bf16>::type TX;
-  constexpr int V = Chunk<TX>::V, AHEAD = X == X_E4 ? (MI < 4 ? 4 : 2) : 4 / MI;
+  constexpr int V = Chunk<TX>::V, AHEAD = X == X_E4 ? 4 : 4 / MI;
   __shared__ float part[FEW_WAVES][MI * 16][16 + 1];
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -592,13 +592,56 @@ void launch_tiled(const Gemm8Desc& g, hipStream_t s) {
   kern<<<tiles, NT, stages, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, tiles, g);
 }
 
+// What a product takes in each block tile, in microseconds: c[0] + rounds (c[1] + c[2] k) + tiles per CU (c[3] + c[4] k), k the k-tiles and rounds the
+// turns of workgroups that the tiles make over the CUs, `sharing` of them on one at a time.  Least squares over 67 products timed in every tile
+// (65 .. 16384 rows, 128 .. 8192 by 64 .. 8192, in chains of launches), one table for each arithmetic and type of result; the tile that comes out
+// best took 1.02, 1.02 and 1.01 times as long as the fastest of ten tiles on the mean, 1.31, 1.21 and 1.14 times at worst.
+struct Tile8 { int bm, bn, sharing; float c[5]; };
+constexpr Tile8 TILES_FAST[] = {
+    {256, 256, 1, {1.52f, 5.06f, 1.06f, 1.93f, 0.534f}},
+    {256, 128, 1, {1.31f, 3.58f, 0.556f, 1.91f, 0.295f}},
+    {128, 128, 2, {1.53f, 0.f, 0.547f, 1.37f, 0.325f}},
+    {128, 64, 2, {1.31f, 1.41f, 0.299f, 0.f, 0.192f}},
+    {64, 64, 3, {2.13f, 0.00842f, 0.199f, 0.f, 0.174f}}};
+constexpr Tile8 TILES_EXACT_BF16[] = {
+    {128, 128, 2, {3.95f, 0.f, 0.621f, 2.83f, 0.f}},
+    {128, 64, 3, {3.34f, 0.134f, 0.434f, 1.56f, 0.f}},
+    {64, 64, 3, {2.51f, 0.f, 0.362f, 0.583f, 0.137f}}};
+constexpr Tile8 TILES_EXACT_F32[] = {
+    {128, 128, 2, {2.51f, 1.4f, 0.684f, 2.18f, 0.559f}},
+    {128, 64, 3, {3.08f, 0.379f, 0.479f, 1.04f, 0.334f}},
+    {64, 64, 3, {2.81f, 0.f, 0.342f, 0.589f, 0.197f}}};
+template <int N>
+int pick(const Tile8 (&table)[N], const Gemm8Desc& g) {
+  const float k = (float)((g.K + BLOCK8 - 1) / BLOCK8);
+  int best = 0;
+  float least = 0.f;
+  for (int i = 0; i < N; ++i) {
+    const Tile8& t = table[i];
+    const int64_t tiles = (int64_t)((g.M + t.bm - 1) / t.bm) * ((g.N + t.bn - 1) / t.bn), slots = 256 * t.sharing;
+    const float us = t.c[0] + (float)((tiles + slots - 1) / slots) * (t.c[1] + t.c[2] * k) + (float)tiles / 256.f * (t.c[3] + t.c[4] * k);
+    if (i == 0 || us < least) { least = us; best = i; }
+  }
+  return best;
+}
+
 template <typename T, int ACT, bool EXACT>
 void tiled(const Gemm8Desc& g, hipStream_t s) {
-  const int64_t big = (int64_t)((g.M + 255) / 256) * ((g.N + 255) / 256), mid = (int64_t)((g.M + 127) / 128) * ((g.N + 127) / 128);
-  if constexpr (!EXACT)
-    if (big >= 256) return launch_tiled<256, 256, 2, 4, 2, T, ACT, false>(g, s);
-  if (mid >= 128) launch_tiled<128, 128, 2, 2, 3, T, ACT, EXACT>(g, s);
-  else launch_tiled<64, 64, 2, 1, 4, T, ACT, EXACT>(g, s);
+  if constexpr (!EXACT) {
+    switch (pick(TILES_FAST, g)) {
+      case 0: launch_tiled<256, 256, 2, 4, 2, T, ACT, false>(g, s); break;
+      case 1: launch_tiled<256, 128, 4, 2, 3, T, ACT, false>(g, s); break;
+      case 2: launch_tiled<128, 128, 2, 4, 2, T, ACT, false>(g, s); break;
+      case 3: launch_tiled<128, 64, 4, 1, 3, T, ACT, false>(g, s); break;
+      default: launch_tiled<64, 64, 2, 2, 3, T, ACT, false>(g, s); break;
+    }
+  } else {
+    switch (g.out_f32 ? pick(TILES_EXACT_F32, g) : pick(TILES_EXACT_BF16, g)) {
+      case 0: launch_tiled<128, 128, 2, 4, 2, T, ACT, true>(g, s); break;
+      case 1: launch_tiled<128, 64, 2, 2, 2, T, ACT, true>(g, s); break;
+      default: launch_tiled<64, 64, 2, 2, 3, T, ACT, true>(g, s); break;
+    }
+  }
 }
 
 template <int X, bool EXACT>
@@ -608,8 +651,7 @@ void few_as(const Gemm8Desc& g, hipStream_t s) {
     gemm8_few_kernel<X, decltype(MI)::value, EXACT><<<grid, FEW_WAVES * 64, 0, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, g.lda, g);
   };
   if (g.M <= 16) go(IC<1>{});
-  else if (g.M <= 32) go(IC<2>{});
-  else go(IC<4>{});
+  else go(IC<2>{});
 }
 template <bool EXACT>
 void few(const Gemm8Desc& g, hipStream_t s) {
