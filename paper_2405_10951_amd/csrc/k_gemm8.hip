@@ -67,50 +67,20 @@ template <typename T> __device__ __forceinline__ void put8(T* p, int n, bool vec
   }
 }
 
-// What follows the products of a wave tile: bias, GELU (with its stored input) or GELU', residual.  Bias and GELU are finished where the
-// accumulators are; 32 rows at a time then go through a patch of LDS, rounded where nothing is to be added any more, and come back with a lane owning
-// eight columns of a row.  bias: that of the wave tile's columns, in LDS.  What is added or multiplied there is asked for ahead of the patch.  The row blocks are a loop: code that is written out once is fetched once.
+// What follows the products of a wave tile: bias, GELU (with its stored input) or GELU', residual.  An accumulator holds, of output row lane % 32, four runs of
+// four columns, 8 apart, the other lane half those between them.  Two runs of the halves change places (v_permlane32_swap), and a lane has eight
+// consecutive columns, 16 bytes of bf16, to store: no LDS, so the stages are free for the next tile's loads meanwhile.  bias: that of the wave tile's columns,
+// in LDS.  The row blocks are a loop: code that is written out once is fetched once.
 template <int MI, int NI, typename T, int ACT>
-__device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][NI], int row0, int col0, int lane, unsigned char* patch,
-                                          const float* bias) {
-  constexpr int TN = NI * 32, CPR = TN / 8, RPP = 64 / CPR, NPASS = 32 / RPP, LDF = (TN + 4) * 4, LDT = TN * (int)sizeof(T) + 16;
-  const int lr = lane & 31, lh = lane >> 5, my_row = lane / CPR, col = col0 + lane % CPR * 8, n = g.N - col;
-  const bool vec = g.ldc * (int64_t)sizeof(T) % 16 == 0 && n >= 8;
-  auto fence = [&]() __attribute__((always_inline)) {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  };
-  typedef T vec4 __attribute__((ext_vector_type(4)));
-  // the row block in blk, rounded, to dst
-  auto out = [&](const f32x16 (&blk)[NI], T* dst, int mi) __attribute__((always_inline)) {
-#pragma unroll
-    for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-      for (int rg = 0; rg < 4; ++rg) {
-        vec4 o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (T)blk[ni][4 * rg + e];
-        *(vec4*)(patch + lr * LDT + (ni * 32 + 8 * rg + 4 * lh) * (int)sizeof(T)) = o;
-      }
-    fence();
-#pragma unroll
-    for (int p = 0; p < NPASS; ++p) {
-      const int r = p * RPP + my_row, m = row0 + mi * 32 + r;
-      const T* src = (const T*)(patch + r * LDT) + lane % CPR * 8;
-      if (m < g.M && n > 0) {
-        T* to = dst + (int64_t)m * g.ldc + col;
-        if (vec) *(Eight<T>*)to = *(const Eight<T>*)src;
-        else
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i < n) to[i] = src[i];
-      }
-    }
-    fence();
-  };
+__device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][NI], int row0, int col0, int lane, const float* bias) {
+  const int lr = lane & 31, lh = lane >> 5;
+  const bool aligned = g.ldc * (int64_t)sizeof(T) % 16 == 0;
   const T* extra = (const T*)(ACT == ACT_GELU_BWD ? g.aux : g.res);
+  const bool more = ACT == ACT_GELU_BWD || g.res;
 #pragma nounroll
   for (int mi = 0; mi < MI; ++mi) {
+    const int m = row0 + mi * 32 + lr;
+    const int64_t at = (int64_t)m * g.ldc + col0 + 8 * lh;             // piece q of eight columns: 16 q further
     f32x16 blk[NI];
     sfor<MI>([&](auto I) __attribute__((always_inline)) {
       constexpr int i = decltype(I)::value;
@@ -118,6 +88,13 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) blk[ni] = acc[i][ni];
     });
+    Eight<T> ex[2 * NI];
+    if (more)
+#pragma unroll
+      for (int q = 0; q < 2 * NI; ++q) {
+        const int n = g.N - (col0 + 16 * q + 8 * lh);
+        if (m < g.M && n > 0) ex[q] = get8(extra + at + 16 * q, n, aligned && n >= 8);
+      }
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
@@ -126,39 +103,39 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
 #pragma unroll
         for (int e = 0; e < 4; ++e) blk[ni][4 * rg + e] += b[e];
       }
+    // eight columns of piece q, in fp32
+    auto eight = [&](int q, float (&v)[8]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(blk[q / 2][8 * (q % 2) + e]), __float_as_uint(blk[q / 2][8 * (q % 2) + 4 + e]), false, false);
+        v[e] = __uint_as_float(x[0]);
+        v[4 + e] = __uint_as_float(x[1]);
+      }
+    };
+    auto out = [&](T* dst, auto&& finish) __attribute__((always_inline)) {
+#pragma unroll
+      for (int q = 0; q < 2 * NI; ++q) {
+        const int n = g.N - (col0 + 16 * q + 8 * lh);
+        float v[8];
+        eight(q, v);
+        finish(q, v);
+        if (m < g.M && n > 0) put8(dst + at + 16 * q, n, aligned && n >= 8, v);
+      }
+    };
     if constexpr (ACT == ACT_GELU) {
-      if (g.aux) out(blk, (T*)g.aux, mi);
+      if (g.aux) out((T*)g.aux, [](int, float (&)[8]) {});
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
         for (int r = 0; r < 16; ++r) blk[ni][r] = gelu_f(blk[ni][r]);
     }
-    if (ACT != ACT_GELU_BWD && !g.res) {
-      out(blk, (T*)g.C, mi);
-      continue;
-    }
-    Eight<T> more[NPASS];
+    if (more)
+      out((T*)g.C, [&](int q, float (&v)[8]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int p = 0; p < NPASS; ++p) {
-      const int m = row0 + mi * 32 + p * RPP + my_row;
-      if (m < g.M && n > 0) more[p] = get8(extra + (int64_t)m * g.ldc + col, n, vec);
-    }
-#pragma unroll
-    for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-      for (int rg = 0; rg < 4; ++rg)
-        *(f32x4*)(patch + lr * LDF + (ni * 32 + 8 * rg + 4 * lh) * 4) = f32x4{blk[ni][4 * rg], blk[ni][4 * rg + 1], blk[ni][4 * rg + 2], blk[ni][4 * rg + 3]};
-    fence();
-#pragma unroll
-    for (int p = 0; p < NPASS; ++p) {
-      const int r = p * RPP + my_row, m = row0 + mi * 32 + r;
-      float v[8];
-      const float* src = (const float*)(patch + r * LDF) + lane % CPR * 8;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = ACT == ACT_GELU_BWD ? src[i] * gelu_grad_f(more[p][i]) : src[i] + more[p][i];
-      if (m < g.M && n > 0) put8((T*)g.C + (int64_t)m * g.ldc + col, n, vec, v);
-    }
-    fence();
+        for (int i = 0; i < 8; ++i) v[i] = ACT == ACT_GELU_BWD ? v[i] * gelu_grad_f(ex[q][i]) : v[i] + ex[q][i];
+      });
+    else
+      out((T*)g.C, [](int, float (&)[8]) {});
   }
 }
 
@@ -398,9 +375,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
     while (kt + NST < nk) ktile(IC<0>{}, steady);
   }
   while (kt < nk) ktile(IC<0>{}, IC<-1>{});                       // nothing left to issue
-  // every wavefront is past the last barrier: the stages are free, a patch of them for each wavefront
-  epilogue8<MI, NI, T, ACT>(g, acc, m0 + wm * TM, n0 + wn * TN, lane, smem + wave * (32 * (TN + 4) * 4),
-                            (const float*)(smem + NST * STAGE) + wn * TN);
+  epilogue8<MI, NI, T, ACT>(g, acc, m0 + wm * TM, n0 + wn * TN, lane, (const float*)(smem + NST * STAGE) + wn * TN);
 }
 
 // maximum over lanes l, l ^ 16, l ^ 32, l ^ 48
@@ -580,8 +555,7 @@ void launch_tiled(const Gemm8Desc& g, hipStream_t s) {
   constexpr int NT = WM * WN * 64;
   constexpr size_t stages = (size_t)NST * ((BM + BN) * 128 + (BM + BN + NT - 1) / NT * NT * 4) + BN * 4;
   static_assert(BN <= NT, "a thread for each column of the bias");
-  constexpr size_t patches = (size_t)WM * WN * 32 * (BN / WN + 4) * 4;
-  static_assert(patches <= stages && stages <= 160 * 1024, "the epilogue patches live in the stages");
+  static_assert(stages <= 160 * 1024, "");
   auto kern = gemm8_kernel<BM, BN, WM, WN, NST, T, ACT, EXACT>;
   static bool attr_set = false;
   if (!attr_set) {
