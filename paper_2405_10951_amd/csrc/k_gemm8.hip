@@ -30,57 +30,70 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-template <typename T> struct Eight;
-template <> struct Eight<bf16> {
-  bf16x8 v;
-  __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
-  __device__ __forceinline__ void set(int i, bf16 x) { v[i] = x; }
-};
-template <> struct Eight<float> {
-  f32x4 lo, hi;
-  __device__ __forceinline__ float operator[](int i) const { return i < 4 ? lo[i] : hi[i - 4]; }
-  __device__ __forceinline__ void set(int i, float x) { if (i < 4) lo[i] = x; else hi[i - 4] = x; }
-};
-// up to eight consecutive values (n of them exist); vec: the address is aligned to 16 bytes and all eight exist
-template <typename T> __device__ __forceinline__ Eight<T> get8(const T* p, int n, bool vec) {
-  if (vec) return *(const Eight<T>*)p;
-  Eight<T> o;
+// 16 bytes of a row of results: PIECE columns
+template <typename T> struct Piece16 { static constexpr int N = 16 / sizeof(T); typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)))); };
+// a piece of which n columns exist; vec: all of them do, and the address is aligned to 16 bytes
+template <typename T> __device__ __forceinline__ typename Piece16<T>::vec get16(const T* p, int n, bool vec) {
+  typedef typename Piece16<T>::vec V;
+  if (vec) return *(const V*)p;
+  V o;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) o.set(i, i < n ? p[i] : (T)0.f);
+  for (int i = 0; i < Piece16<T>::N; ++i) o[i] = i < n ? p[i] : (T)0.f;
   return o;
 }
-template <typename T> __device__ __forceinline__ void put8(T* p, int n, bool vec, const float (&v)[8]) {
-  if (vec) {
-    if constexpr (sizeof(T) == 2) {
-      bf16x8 o;
+// past: past the caches, where rows lie on lines
+template <typename T> __device__ __forceinline__ void put16(T* p, int n, bool vec, bool past, typename Piece16<T>::vec v) {
+  if (vec && past) __builtin_nontemporal_store(__builtin_bit_cast(i32x4, v), (i32x4*)p);
+  else if (vec) *(i32x4*)p = __builtin_bit_cast(i32x4, v);
+  else
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = (bf16)v[i];
-      *(bf16x8*)p = o;
-    } else {
-      *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
-      *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = (T)v[i];
-  }
+    for (int i = 0; i < Piece16<T>::N; ++i)
+      if (i < n) p[i] = v[i];
 }
 
-// What follows the products of a wave tile: bias, GELU (with its stored input) or GELU', residual.  An accumulator holds, of output row lane % 32, four runs of
-// four columns, 8 apart, the other lane half those between them.  Two runs of the halves change places (v_permlane32_swap), and a lane has eight
-// consecutive columns, 16 bytes of bf16, to store: no LDS, so the stages are free for the next tile's loads meanwhile.  bias: that of the wave tile's columns,
-// in LDS.  The row blocks are a loop: code that is written out once is fetched once.
+// What follows the products of a wave tile: bias, GELU (with its stored input) or GELU', residual.  Bias and GELU are finished where the
+// accumulators are; 32 rows at a time then go through a patch of LDS, rounded where nothing is to be added any more, and come back with a lane owning
+// 16 bytes of a row.  bias: that of the wave tile's columns, in LDS.  What is added or multiplied there is asked for ahead of the patch.  The row blocks are a
+// loop: code that is written out once is fetched once.
+// Stores.  A row of a wave tile is one or two 128-byte lines, or half of one, where rows lie on lines; such stores go past the caches, which
+// otherwise lose the operands' panels to results that nobody reads here (16384 x 4096 x 8192: 509 -> 460 us; 6304 x 768 x 2304: 17.7 -> 15.7).  Smaller pieces of lines must not:
+// results stored 32 bytes of a row at a time straight from the accumulators took 509 us the ordinary way and 688 past the caches.
 template <int MI, int NI, typename T, int ACT>
-__device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][NI], int row0, int col0, int lane, const float* bias) {
-  const int lr = lane & 31, lh = lane >> 5;
-  const bool aligned = g.ldc * (int64_t)sizeof(T) % 16 == 0;
+__device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][NI], int row0, int col0, int lane, unsigned char* patch,
+                                          const float* bias) {
+  typedef typename Piece16<T>::vec vecT;
+  constexpr int P = Piece16<T>::N, TN = NI * 32, CPR = TN / P, RPP = 64 / CPR, NPASS = 32 / RPP, LDF = (TN + 4) * 4, LDT = TN * (int)sizeof(T) + 16;
+  const int lr = lane & 31, lh = lane >> 5, my_row = lane / CPR, col = col0 + lane % CPR * P, n = g.N - col;
+  const bool vec = g.ldc * (int64_t)sizeof(T) % 16 == 0 && n >= P;
+  const bool past = g.ldc * (int64_t)sizeof(T) % 128 == 0;
+  auto fence = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  // the row block in blk, rounded, to dst
+  auto out = [&](const f32x16 (&blk)[NI], T* dst, int mi) __attribute__((always_inline)) {
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg) {
+        vec4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (T)blk[ni][4 * rg + e];
+        *(vec4*)(patch + lr * LDT + (ni * 32 + 8 * rg + 4 * lh) * (int)sizeof(T)) = o;
+      }
+    fence();
+#pragma unroll
+    for (int p = 0; p < NPASS; ++p) {
+      const int r = p * RPP + my_row, m = row0 + mi * 32 + r;
+      const vecT v = *(const vecT*)(patch + r * LDT + lane % CPR * 16);
+      if (m < g.M && n > 0) put16(dst + (int64_t)m * g.ldc + col, n, vec, past, v);
+    }
+    fence();
+  };
   const T* extra = (const T*)(ACT == ACT_GELU_BWD ? g.aux : g.res);
-  const bool more = ACT == ACT_GELU_BWD || g.res;
 #pragma nounroll
   for (int mi = 0; mi < MI; ++mi) {
-    const int m = row0 + mi * 32 + lr;
-    const int64_t at = (int64_t)m * g.ldc + col0 + 8 * lh;             // piece q of eight columns: 16 q further
     f32x16 blk[NI];
     sfor<MI>([&](auto I) __attribute__((always_inline)) {
       constexpr int i = decltype(I)::value;
@@ -88,12 +101,13 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) blk[ni] = acc[i][ni];
     });
-    Eight<T> ex[2 * NI];
-    if (more)
+    vecT more[NPASS];
+    const bool add = ACT == ACT_GELU_BWD || g.res;
+    if (add)
 #pragma unroll
-      for (int q = 0; q < 2 * NI; ++q) {
-        const int n = g.N - (col0 + 16 * q + 8 * lh);
-        if (m < g.M && n > 0) ex[q] = get8(extra + at + 16 * q, n, aligned && n >= 8);
+      for (int p = 0; p < NPASS; ++p) {
+        const int m = row0 + mi * 32 + p * RPP + my_row;
+        if (m < g.M && n > 0) more[p] = get16(extra + (int64_t)m * g.ldc + col, n, vec);
       }
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
@@ -103,39 +117,33 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
 #pragma unroll
         for (int e = 0; e < 4; ++e) blk[ni][4 * rg + e] += b[e];
       }
-    // eight columns of piece q, in fp32
-    auto eight = [&](int q, float (&v)[8]) __attribute__((always_inline)) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(blk[q / 2][8 * (q % 2) + e]), __float_as_uint(blk[q / 2][8 * (q % 2) + 4 + e]), false, false);
-        v[e] = __uint_as_float(x[0]);
-        v[4 + e] = __uint_as_float(x[1]);
-      }
-    };
-    auto out = [&](T* dst, auto&& finish) __attribute__((always_inline)) {
-#pragma unroll
-      for (int q = 0; q < 2 * NI; ++q) {
-        const int n = g.N - (col0 + 16 * q + 8 * lh);
-        float v[8];
-        eight(q, v);
-        finish(q, v);
-        if (m < g.M && n > 0) put8(dst + at + 16 * q, n, aligned && n >= 8, v);
-      }
-    };
     if constexpr (ACT == ACT_GELU) {
-      if (g.aux) out((T*)g.aux, [](int, float (&)[8]) {});
+      if (g.aux) out(blk, (T*)g.aux, mi);
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
         for (int r = 0; r < 16; ++r) blk[ni][r] = gelu_f(blk[ni][r]);
     }
-    if (more)
-      out((T*)g.C, [&](int q, float (&v)[8]) __attribute__((always_inline)) {
+    if (!add) {
+      out(blk, (T*)g.C, mi);
+      continue;
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = ACT == ACT_GELU_BWD ? v[i] * gelu_grad_f(ex[q][i]) : v[i] + ex[q][i];
-      });
-    else
-      out((T*)g.C, [](int, float (&)[8]) {});
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg)
+        *(f32x4*)(patch + lr * LDF + (ni * 32 + 8 * rg + 4 * lh) * 4) = f32x4{blk[ni][4 * rg], blk[ni][4 * rg + 1], blk[ni][4 * rg + 2], blk[ni][4 * rg + 3]};
+    fence();
+#pragma unroll
+    for (int p = 0; p < NPASS; ++p) {
+      const int r = p * RPP + my_row, m = row0 + mi * 32 + r;
+      const float* src = (const float*)(patch + r * LDF) + lane % CPR * P;
+      vecT v;
+#pragma unroll
+      for (int i = 0; i < P; ++i) v[i] = (T)(ACT == ACT_GELU_BWD ? src[i] * gelu_grad_f((float)more[p][i]) : src[i] + (float)more[p][i]);
+      if (m < g.M && n > 0) put16((T*)g.C + (int64_t)m * g.ldc + col, n, vec, past, v);
+    }
+    fence();
   }
 }
 
@@ -151,6 +159,15 @@ __device__ __forceinline__ bf16x8 widen8(int lo, int hi, int s8) {
 }
 
 __device__ __forceinline__ i32x8 join8(i32x4 a, i32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// Row and column of tile t: column after column within bands of eight tile rows, so that the tiles that an XCD works on at a time (neighbours, by
+// xcd_remap) share rows and columns alike and its L2 reads each once.  16384 x 4096 x 8192: row after row, an XCD's 32 tiles read 33 panels a round, like this 12.
+constexpr int BAND = 8;
+__device__ __forceinline__ void place(int t, int ntm, int ntn, int& tm, int& tn) {
+  const int band = t / (BAND * ntn), first = band * BAND, high = min(BAND, ntm - first), in = t - first * ntn;
+  tm = first + in % high;
+  tn = in / high;
+}
 
 // Block tile BM x BN x 128, WM x WN wavefronts, NST stages of LDS.  The weights are the first operand of the instruction, so an accumulator
 // holds the transposed output tile: lane l owns output row l % 32 and four runs of four columns.
@@ -176,8 +193,9 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
   const int tile = xcd_remap(blockIdx.x, tiles);
-  const int ntn = (N + BN - 1) / BN;
-  const int m0 = tile / ntn * BM, n0 = tile % ntn * BN;
+  int tm, tn;
+  place(tile, (M + BM - 1) / BM, (N + BN - 1) / BN, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
   const int nk = (hK + BLOCK8 - 1) / BLOCK8;
   const unsigned ld = (unsigned)nk * BLOCK8, lds = (unsigned)(nk + 3) / 4 * 4;
   const uint8_t* __restrict__ A = (const uint8_t*)hA + (int64_t)m0 * ld;
@@ -375,7 +393,9 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, 
     while (kt + NST < nk) ktile(IC<0>{}, steady);
   }
   while (kt < nk) ktile(IC<0>{}, IC<-1>{});                       // nothing left to issue
-  epilogue8<MI, NI, T, ACT>(g, acc, m0 + wm * TM, n0 + wn * TN, lane, (const float*)(smem + NST * STAGE) + wn * TN);
+  // every wavefront is past the last barrier: the stages are free, a patch of them for each wavefront
+  epilogue8<MI, NI, T, ACT>(g, acc, m0 + wm * TM, n0 + wn * TN, lane, smem + wave * (32 * (TN + 4) * 4),
+                            (const float*)(smem + NST * STAGE) + wn * TN);
 }
 
 // maximum over lanes l, l ^ 16, l ^ 32, l ^ 48
@@ -555,7 +575,8 @@ void launch_tiled(const Gemm8Desc& g, hipStream_t s) {
   constexpr int NT = WM * WN * 64;
   constexpr size_t stages = (size_t)NST * ((BM + BN) * 128 + (BM + BN + NT - 1) / NT * NT * 4) + BN * 4;
   static_assert(BN <= NT, "a thread for each column of the bias");
-  static_assert(stages <= 160 * 1024, "");
+  constexpr size_t patches = (size_t)WM * WN * 32 * (BN / WN + 4) * 4;
+  static_assert(patches <= stages && stages <= 160 * 1024, "the epilogue patches live in the stages");
   auto kern = gemm8_kernel<BM, BN, WM, WN, NST, T, ACT, EXACT>;
   static bool attr_set = false;
   if (!attr_set) {
