@@ -590,22 +590,22 @@ void launch_tiled(const Gemm8Desc& g, hipStream_t s) {
 // What a product takes in each block tile, in microseconds: c[0] + rounds (c[1] + c[2] k) + tiles per CU (c[3] + c[4] k), k the k-tiles and rounds the
 // turns of workgroups that the tiles make over the CUs, `sharing` of them on one at a time.  Least squares over 67 products timed in every tile
 // (65 .. 16384 rows, 128 .. 8192 by 64 .. 8192, in chains of launches), one table for each arithmetic and type of result; the tile that comes out
-// best took 1.02, 1.02 and 1.01 times as long as the fastest of ten tiles on the mean, 1.31, 1.21 and 1.14 times at worst.
+// best took 1.01 times as long as the fastest of ten tiles on the mean, 1.20, 1.20 and 1.13 times at worst.
 struct Tile8 { int bm, bn, sharing; float c[5]; };
 constexpr Tile8 TILES_FAST[] = {
-    {256, 256, 1, {1.52f, 5.06f, 1.06f, 1.93f, 0.534f}},
-    {256, 128, 1, {1.31f, 3.58f, 0.556f, 1.91f, 0.295f}},
-    {128, 128, 2, {1.53f, 0.f, 0.547f, 1.37f, 0.325f}},
-    {128, 64, 2, {1.31f, 1.41f, 0.299f, 0.f, 0.192f}},
-    {64, 64, 3, {2.13f, 0.00842f, 0.199f, 0.f, 0.174f}}};
+    {256, 256, 1, {0.591f, 5.94f, 1.04f, 0.f, 0.544f}},
+    {256, 128, 1, {1.48f, 3.06f, 0.546f, 0.256f, 0.366f}},
+    {128, 128, 2, {2.04f, 0.f, 0.496f, 1.08f, 0.315f}},
+    {128, 64, 2, {1.32f, 1.44f, 0.315f, 0.f, 0.178f}},
+    {64, 64, 3, {1.77f, 0.697f, 0.19f, 0.0343f, 0.137f}}};
 constexpr Tile8 TILES_EXACT_BF16[] = {
-    {128, 128, 2, {3.95f, 0.f, 0.621f, 2.83f, 0.f}},
-    {128, 64, 3, {3.34f, 0.134f, 0.434f, 1.56f, 0.f}},
-    {64, 64, 3, {2.51f, 0.f, 0.362f, 0.583f, 0.137f}}};
+    {128, 128, 2, {3.25f, 0.781f, 0.701f, 2.1f, 0.f}},
+    {128, 64, 3, {2.78f, 0.613f, 0.441f, 1.39f, 0.f}},
+    {64, 64, 3, {2.58f, 0.f, 0.358f, 0.651f, 0.112f}}};
 constexpr Tile8 TILES_EXACT_F32[] = {
-    {128, 128, 2, {2.51f, 1.4f, 0.684f, 2.18f, 0.559f}},
-    {128, 64, 3, {3.08f, 0.379f, 0.479f, 1.04f, 0.334f}},
-    {64, 64, 3, {2.81f, 0.f, 0.342f, 0.589f, 0.197f}}};
+    {128, 128, 2, {1.04f, 3.67f, 0.718f, 0.695f, 0.478f}},
+    {128, 64, 3, {0.876f, 2.71f, 0.462f, 0.154f, 0.342f}},
+    {64, 64, 3, {2.61f, 0.152f, 0.335f, 0.525f, 0.186f}}};
 template <int N>
 int pick(const Tile8 (&table)[N], const Gemm8Desc& g) {
   const float k = (float)((g.K + BLOCK8 - 1) / BLOCK8);
@@ -632,7 +632,7 @@ void tiled(const Gemm8Desc& g, hipStream_t s) {
     }
   } else {
     switch (g.out_f32 ? pick(TILES_EXACT_F32, g) : pick(TILES_EXACT_BF16, g)) {
-      case 0: launch_tiled<128, 128, 2, 4, 2, T, ACT, true>(g, s); break;
+      case 0: launch_tiled<128, 128, 2, 2, 2, T, ACT, true>(g, s); break;
       case 1: launch_tiled<128, 64, 2, 2, 2, T, ACT, true>(g, s); break;
       default: launch_tiled<64, 64, 2, 2, 3, T, ACT, true>(g, s); break;
     }
