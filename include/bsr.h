@@ -542,12 +542,15 @@ int32_t bsr_linear8_dgrad(const void* dy, int32_t dy_type, int64_t lddy, const u
  *                needs; apart, because their sum would lose the logarithm where m is large
  *   row_grad     fp32 [rows], may be NULL (1 for every row)
  *   dz           [rows, classes] of `type`, stride ldd; may be z itself (same stride).  bsr_distill_forward: NULL for no gradient
- * bsr_distill_forward gives loss, stats and, in the same launch, dz; bsr_distill_backward gives dz from stats.
+ *   workspace    fp32 scratch of bsr_distill_workspace_floats() floats (0: none is needed), may be NULL: with it few rows of many classes are split over
+ *                several workgroups each and joined, without it a workgroup takes a row (sums in another order)
+ * bsr_distill_forward gives loss, stats and, in the same call, dz; bsr_distill_backward gives dz from stats.
  */
+size_t bsr_distill_workspace_floats(int32_t type, int64_t rows, int32_t classes);
 int32_t bsr_distill_forward(const void* z, int32_t type, int64_t rows, int32_t classes, int64_t ldz, const int32_t* index, int64_t ldi,
                             const void* logits, int32_t logits_type, int64_t ldt, int32_t top, const int32_t* labels, float temperature,
                             float hard_weight, float* loss, float* stats, const float* row_grad, float grad_scale, void* dz, int64_t ldd,
-                            void* stream);
+                            float* workspace, size_t workspace_floats, void* stream);
 int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t classes, int64_t ldz, const int32_t* index, int64_t ldi,
                              const void* logits, int32_t logits_type, int64_t ldt, int32_t top, const int32_t* labels, float temperature,
                              float hard_weight, const float* stats, const float* row_grad, float grad_scale, void* dz, int64_t ldd,

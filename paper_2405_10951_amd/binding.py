@@ -138,11 +138,12 @@ def load_library():
             "bsr_quantize8_weight": (p, i32, i32, i32, i64, p, p, p, p, p),
             "bsr_linear8_forward": (p, i32, i64, p, i32, i32, i32, p, p, p, i32, p, p, p, i32, p, C.c_size_t, p),
             "bsr_linear8_dgrad": (p, i32, i64, p, i32, i32, i32, p, p, p, p, i32, p, C.c_size_t, p),
-            "bsr_distill_forward": (p, i32, i64, i32, i64, p, i64, p, i32, i64, i32, p, f32, f32, p, p, p, f32, p, i64, p),
+            "bsr_distill_forward": (p, i32, i64, i32, i64, p, i64, p, i32, i64, i32, p, f32, f32, p, p, p, f32, p, i64, p, C.c_size_t, p),
             "bsr_distill_backward": (p, i32, i64, i32, i64, p, i64, p, i32, i64, i32, p, f32, f32, p, p, f32, p, i64, p)}.items():
         getattr(lib, name).restype, getattr(lib, name).argtypes = i32, args
     lib.bsr_block8_strides.restype, lib.bsr_block8_strides.argtypes = None, (i32, p, p)
     lib.bsr_layernorm_workspace_floats.restype, lib.bsr_layernorm_workspace_floats.argtypes = C.c_size_t, (i32,)
+    lib.bsr_distill_workspace_floats.restype, lib.bsr_distill_workspace_floats.argtypes = C.c_size_t, (i32, i64, i32)
     lib.bsr_linear8_workspace_bytes.restype, lib.bsr_linear8_workspace_bytes.argtypes = C.c_size_t, (i32, i32)
     lib.bsr_profile_begin.argtypes = [C.c_void_p]
     lib.bsr_profile_end.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
@@ -609,6 +610,16 @@ def _distill_dz(z, row_grad, dz):
     return pg, dz, _rows_of(dz, "dz", z.shape, z.dtype)
 
 
+def _distill_workspace(z, code):
+    """-> (scratch of the forward or None, its floats)"""
+    rows, classes = z.shape
+    floats = load_library().bsr_distill_workspace_floats(code, rows, classes)
+    if not floats:
+        return None, 0
+    import torch
+    return z.new_empty(floats, dtype=torch.float32), floats
+
+
 def bsr_distill_forward(z, index, logits, labels=None, temperature=1.0, hard_weight=0.0):
     """Student logits z [rows,classes] bf16 or fp32, the teacher's classes index [rows,top] int32 (-1: absent) and logits [rows,top], labels
     [rows] int32 (-1: none) -> (loss [rows], stats [rows,3] for bsr_distill_backward)."""
@@ -616,18 +627,20 @@ def bsr_distill_forward(z, index, logits, labels=None, temperature=1.0, hard_wei
     stream = _together(z, index, logits, labels)
     args = _distill_args(z, index, logits, labels, temperature, hard_weight)
     loss, stats = z.new_empty(z.shape[0], dtype=torch.float32), z.new_empty((z.shape[0], 3), dtype=torch.float32)
-    _check(load_library().bsr_distill_forward(*args, loss.data_ptr(), stats.data_ptr(), None, 1.0, None, 0, stream))
+    ws, floats = _distill_workspace(z, args[1])
+    _check(load_library().bsr_distill_forward(*args, loss.data_ptr(), stats.data_ptr(), None, 1.0, None, 0, _dp(ws), floats, stream))
     return loss, stats
 
 
 def bsr_distill_forward_backward(z, index, logits, labels=None, temperature=1.0, hard_weight=0.0, row_grad=None, grad_scale=1.0, dz=None):
-    """-> (loss [rows], dz [rows,classes] = grad_scale row_grad[row] dloss/dz) in one launch.  dz may be z."""
+    """-> (loss [rows], dz [rows,classes] = grad_scale row_grad[row] dloss/dz) in one pass.  dz may be z."""
     import torch
     stream = _together(z, index, logits, labels, row_grad, dz)
     args = _distill_args(z, index, logits, labels, temperature, hard_weight)
     pg, dz, ldd = _distill_dz(z, row_grad, dz)
     loss = z.new_empty(z.shape[0], dtype=torch.float32)
-    _check(load_library().bsr_distill_forward(*args, loss.data_ptr(), None, pg, grad_scale, dz.data_ptr(), ldd, stream))
+    ws, floats = _distill_workspace(z, args[1])
+    _check(load_library().bsr_distill_forward(*args, loss.data_ptr(), None, pg, grad_scale, dz.data_ptr(), ldd, _dp(ws), floats, stream))
     return loss, dz
 
 

@@ -1907,17 +1907,25 @@ static int32_t distill_args(const char* w, DistillArgs& a, const void* z, int32_
   return BSR_OK;
 }
 
+size_t bsr_distill_workspace_floats(int32_t type, int64_t rows, int32_t classes) {
+  return !known_type(type) || rows < 1 || classes < 1 ? 0 : distill_parts_floats(type == BSR_FP32, rows, classes);
+}
+
 int32_t bsr_distill_forward(const void* z, int32_t type, int64_t rows, int32_t classes, int64_t ldz, const int32_t* index, int64_t ldi,
                             const void* logits, int32_t logits_type, int64_t ldt, int32_t top, const int32_t* labels, float temperature,
                             float hard_weight, float* loss, float* stats, const float* row_grad, float grad_scale, void* dz, int64_t ldd,
-                            void* stream) {
+                            float* workspace, size_t workspace_floats, void* stream) {
   DistillArgs a;
   const int32_t rc = distill_args("bsr_distill_forward", a, z, type, rows, classes, ldz, index, ldi, logits, logits_type, ldt, top, labels, temperature,
                                   hard_weight, row_grad, grad_scale, dz, ldd);
   if (rc != BSR_OK) return rc;
   if (rows > 0 && !loss && !stats && !dz) return fail(nullptr, BSR_ERR_INVALID_ARG, "bsr_distill_forward: nothing asked for");
   if ((loss && !aligned4(loss)) || (stats && !aligned4(stats))) return fail(nullptr, BSR_ERR_INVALID_ARG, "bsr_distill_forward: loss or stats is misaligned");
+  const size_t parts = rows > 0 ? distill_parts_floats(a.f32, rows, classes) : 0;
+  if (workspace && (!aligned4(workspace) || workspace_floats < parts))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "bsr_distill_forward: workspace misaligned or of %zu floats, %zu are needed", workspace_floats, parts);
   if (rows == 0) return BSR_OK;
+  a.parts = parts ? workspace : nullptr;
   a.loss = loss; a.stats = stats;
   distill_forward(a, (hipStream_t)stream);
   return check_hip(nullptr, "bsr_distill_forward");

@@ -16,7 +16,10 @@ struct DistillArgs {
   const float* row_grad = nullptr;                      // [rows], null: 1 for each
   float grad_scale = 1.f;
   void* dz = nullptr; int64_t ldd = 0;                  // type of z; may be z itself
+  float* parts = nullptr;                               // forward: scratch of distill_parts_floats() floats, null: a row is not split
+  int segments = 1, writers = 1;                        // (set inside) workgroups that sum up a row, and that write it
 };
+size_t distill_parts_floats(bool f32, int64_t rows, int classes);      // 0: nothing to split
 void distill_forward(const DistillArgs& a, hipStream_t s);      // loss, stats and, where dz is given, the gradient
 void distill_backward(const DistillArgs& a, hipStream_t s);     // dz from stats
 

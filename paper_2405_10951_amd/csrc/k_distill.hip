@@ -7,6 +7,7 @@
 // Bound by memory: a workgroup takes a row, asks for all of it at once, keeps it in registers (rows of up to 131072 bf16 or 65536 fp32 values), takes the
 // maximum and both sums together and writes dz; longer rows are read a second time for dz.  The teacher's list is worked on while the row is on its way.  The few places that p and the label touch are
 // written again behind a barrier by a thread each, duplicates added in the order of the list: no atomics, the same bits every time.
+#include <algorithm>
 #include <cfloat>
 
 #include "distill.h"
@@ -67,19 +68,37 @@ template <typename T, int NT, int C> struct Row {
   }
 };
 
-// maximum m, sums of 2^((z - m) ct) and 2^((z - m) c1)
+// P: 0: one sum (temperature 1, or no hard part); 1: the sums at the temperature and at 1 by an exponential each; 2, 3, 4: that temperature, where
+// exp(d) is a power of exp(d / T) (4096 x 131072 bf16 at T = 2 with a hard part, forward and backward: 657 -> 597 us)
+template <int P> __device__ __forceinline__ float second(float e, float d) {
+  if constexpr (P == 2) return e * e;
+  else if constexpr (P == 3) return e * e * e;
+  else if constexpr (P == 4) return (e * e) * (e * e);
+  else return exp2_(d * LOG2E);
+}
+
+// maximum m, sums of exp((z - m) / T) and exp(z - m)
 struct Stats { float m, st, s1; };
-template <bool TWO> __device__ __forceinline__ void rescale(Stats& a, float m, float ct, float c1) {
+template <int P> __device__ __forceinline__ void count(Stats& a, float v, float ct) {
+  const float d = v - a.m, e = exp2_(d * ct);
+  a.st += e;
+  if (P) a.s1 += second<P>(e, d);
+}
+template <int P> __device__ __forceinline__ void rescale(Stats& a, float m, float ct) {
   const float d = a.m - m;
   a.st *= exp2_(d * ct);
-  if (TWO) a.s1 *= exp2_(d * c1);
+  if (P) a.s1 *= exp2_(d * LOG2E);
   a.m = m;
 }
-template <int NT, bool TWO>
-__device__ __forceinline__ void join(Stats& a, float ct, float c1, float (*red)[3]) {
-  rescale<TWO>(a, wave_max(a.m), ct, c1);
+// over a wavefront, and over the wavefronts of a workgroup
+template <int P> __device__ __forceinline__ void join_wave(Stats& a, float ct) {
+  rescale<P>(a, wave_max(a.m), ct);
   a.st = wave_sum(a.st);
-  if (TWO) a.s1 = wave_sum(a.s1);
+  if (P) a.s1 = wave_sum(a.s1);
+}
+template <int NT, int P>
+__device__ __forceinline__ void join(Stats& a, float ct, float (*red)[3]) {
+  join_wave<P>(a, ct);
   if constexpr (NT > WAVE) {
     const int w = threadIdx.x / WAVE;
     if (threadIdx.x % WAVE == 0) { red[w][0] = a.m; red[w][1] = a.st; red[w][2] = a.s1; }
@@ -87,15 +106,35 @@ __device__ __forceinline__ void join(Stats& a, float ct, float c1, float (*red)[
     float m = red[0][0];
 #pragma unroll
     for (int i = 1; i < NT / WAVE; ++i) m = fmaxf(m, red[i][0]);
-    float st = 0.f, s1 = 0.f;
+    Stats all{m, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NT / WAVE; ++i) {
-      const float d = red[i][0] - m;
-      st += red[i][1] * exp2_(d * ct);
-      if (TWO) s1 += red[i][2] * exp2_(d * c1);
+      Stats one{red[i][0], red[i][1], red[i][2]};
+      rescale<P>(one, m, ct);
+      all.st += one.st;
+      all.s1 += one.s1;
     }
-    a = Stats{m, st, s1};
+    a = all;
   }
+}
+template <typename T, int NT, int C, int P>
+__device__ __forceinline__ Stats row_stats(const Row<T, NT, C>& held, float ct, float (*red)[3]) {
+  constexpr int V = Chunk<T>::V;
+  Stats st{-FLT_MAX, 0.f, 0.f};
+  held.pass([&](int, float v) __attribute__((always_inline)) {
+              if (v > st.m) rescale<P>(st, v, ct);
+              count<P>(st, v, ct);
+            },
+            [&](int, const float (&v)[V]) __attribute__((always_inline)) {
+              float m = v[0];
+#pragma unroll
+              for (int e = 1; e < V; ++e) m = fmaxf(m, v[e]);
+              if (m > st.m) rescale<P>(st, m, ct);
+#pragma unroll
+              for (int e = 0; e < V; ++e) count<P>(st, v[e], ct);
+            });
+  join<NT, P>(st, ct, red);
+  return st;
 }
 
 // sum over the workgroup, in every thread
@@ -111,31 +150,64 @@ template <int NT> __device__ __forceinline__ float block_sum(float v, float* red
   return v;
 }
 
-// BWD: the statistics come from a.stats instead of a pass.  TWO: temperature other than 1 and a hard part, two sums
-template <typename T, int NT, int C, bool BWD, bool TWO>
+// Segment seg of `count` of a row: [lo, hi), all but the first and the last of whole chunks
+template <typename T> struct Segment {
+  int lo, hi, head;
+  __device__ __forceinline__ Segment(const DistillArgs& a, const T* z, int seg, int count) {
+    const int n = a.classes;
+    head = min(n, (int)((16 - ((uintptr_t)z & 15)) & 15) / (int)sizeof(T));
+    const int chunks = (n - head) / Chunk<T>::V, per = (chunks + count - 1) / count;
+    lo = seg == 0 ? 0 : head + min(chunks, seg * per) * Chunk<T>::V;
+    hi = seg == count - 1 ? n : head + min(chunks, (seg + 1) * per) * Chunk<T>::V;
+    if (seg > 0) head = 0;
+  }
+};
+
+// Few rows of many classes: several workgroups a row, each on a segment; what they find here, the kernel below joins.
+template <typename T, int NT, int C, int P>
+__global__ __launch_bounds__(NT) void distill_parts_kernel(DistillArgs a) {
+  __shared__ float red[NT / WAVE][3];
+  const int64_t row = blockIdx.x / (unsigned)a.segments;
+  const int seg = (int)(blockIdx.x % (unsigned)a.segments);
+  const T* z = (const T*)a.z + row * a.ldz;
+  const Segment<T> at(a, z, seg, a.segments);
+  Row<T, NT, C> held;
+  held.start(z + at.lo, at.hi - at.lo, at.head);
+  const Stats st = row_stats<T, NT, C, P>(held, LOG2E / a.temperature, red);
+  if (threadIdx.x == 0) {
+    float* o = a.parts + (int64_t)blockIdx.x * 3;
+    o[0] = st.m;
+    o[1] = st.st;
+    o[2] = st.s1;
+  }
+}
+
+// where a row's maximum and sums come from: a pass over it, the forward's (a.stats), or those of its segments (a.parts)
+enum { OWN, STATS, PARTS };
+template <typename T, int NT, int C, int FROM, int P>
 __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   extern __shared__ unsigned char dyn[];
   __shared__ float red[NT / WAVE][3], red_w[NT / WAVE], red_l[NT / WAVE];
+  constexpr int V = Chunk<T>::V;
   int* li = (int*)dyn;                              // [k] the classes, -1 where absent
   float* lp = (float*)(li + a.k);                   // [k] first t, then p
   float* lz = lp + a.k;                             // [k] the student's logits there
-  const int tid = threadIdx.x, n = a.classes;
-  const int64_t row = blockIdx.x;
+  constexpr int LIST = NT < 256 ? NT : 256;         // threads that go through the list: a sum over it is the same whatever NT
+  const int tid = threadIdx.x, n = a.classes, my_k = tid < LIST ? a.k : 0;
+  const int64_t row = FROM == OWN ? (int64_t)blockIdx.x : (int64_t)(blockIdx.x / (unsigned)a.writers);
+  const int seg = FROM == OWN ? 0 : (int)(blockIdx.x % (unsigned)a.writers);
   const T* z = (const T*)a.z + row * a.ldz;
   T* dz = a.dz ? (T*)a.dz + row * a.ldd : nullptr;
-  constexpr int V = Chunk<T>::V;
-  // (rows that lie differently within 16 bytes in z and dz go value by value: C = 0)
-  int head = min(n, (int)((16 - ((uintptr_t)z & 15)) & 15) / (int)sizeof(T));
-  if (C == 0 && dz && (((uintptr_t)z ^ (uintptr_t)dz) & 15)) head = n;
+  const Segment<T> at(a, z, seg, FROM == OWN ? 1 : a.writers);
   Row<T, NT, C> held;
-  held.start(z, n, head);
-  const float inv_t = 1.f / a.temperature, ct = LOG2E * inv_t, c1 = LOG2E;
+  if (FROM == OWN || dz) held.start(z + at.lo, at.hi - at.lo, at.head);
+  const float inv_t = 1.f / a.temperature, ct = LOG2E * inv_t;
   const int label = a.labels && a.hard > 0.f ? a.labels[row] : -1;
   const bool labelled = label >= 0 && label < n;
   const float zl = labelled ? (float)z[label] : 0.f;
   // the teacher's list; its maximum and its sum
   float tm = -FLT_MAX;
-  for (int j = tid; j < a.k; j += NT) {
+  for (int j = tid; j < my_k; j += LIST) {
     const int c = a.index[row * a.ldi + j];
     const bool there = c >= 0 && c < n;
     const float t = a.top_f32 ? ((const float*)a.top)[row * a.ldt + j] : (float)((const bf16*)a.top)[row * a.ldt + j];
@@ -144,26 +216,25 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
     lz[j] = there ? (float)z[c] : 0.f;
     if (there) tm = fmaxf(tm, t);
   }
-  Stats st{-FLT_MAX, 0.f, 0.f};
-  if constexpr (!BWD) {
-    held.pass([&](int, float v) __attribute__((always_inline)) {
-                      if (v > st.m) rescale<TWO>(st, v, ct, c1);
-                      st.st += exp2_((v - st.m) * ct);
-                      if (TWO) st.s1 += exp2_((v - st.m) * c1);
-                    },
-                    [&](int, const float (&v)[V]) __attribute__((always_inline)) {
-                      float m = v[0];
-#pragma unroll
-                      for (int e = 1; e < V; ++e) m = fmaxf(m, v[e]);
-                      if (m > st.m) rescale<TWO>(st, m, ct, c1);
-#pragma unroll
-                      for (int e = 0; e < V; ++e) {
-                        st.st += exp2_((v[e] - st.m) * ct);
-                        if (TWO) st.s1 += exp2_((v[e] - st.m) * c1);
-                      }
-                    });
-    join<NT, TWO>(st, ct, c1, red);
-    if (!TWO) st.s1 = st.st;                        // (temperature 1, or nobody asks)
+  Stats st{0.f, 0.f, 0.f};
+  // logarithms of the sums
+  float lt, l1;
+  if constexpr (FROM == STATS) {
+    st.m = a.stats[3 * row];
+    lt = a.stats[3 * row + 1];
+    l1 = a.stats[3 * row + 2];
+  } else {
+    if constexpr (FROM == OWN) {
+      st = row_stats<T, NT, C, P>(held, ct, red);
+    } else {                                         // (a lane for each segment)
+      const int lane = tid % WAVE;
+      const float* p = a.parts + (row * a.segments + min(lane, a.segments - 1)) * 3;
+      st = lane < a.segments ? Stats{p[0], p[1], p[2]} : Stats{-FLT_MAX, 0.f, 0.f};
+      join_wave<P>(st, ct);
+    }
+    if (!P) st.s1 = st.st;                          // (temperature 1, or nobody asks)
+    lt = logf(st.st);
+    l1 = logf(st.s1);
   }
   // p in place of t
   float tmax = wave_max(tm);
@@ -176,30 +247,19 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
     __syncthreads();
   }
   float w = 0.f;
-  for (int j = tid; j < a.k; j += NT)
+  for (int j = tid; j < my_k; j += LIST)
     if (li[j] >= 0) w += exp2_((lp[j] - tmax) * ct);
   w = block_sum<NT>(w, red_w);
-  const bool taught = w != 0.f;                      // (NaN goes on)
-  // log-sum-exp at the temperature and at 1, as (m, log of the sum): differences to m first, they are small
-  float lt, l1;
-  if (BWD) {
-    st.m = a.stats[3 * row];
-    lt = a.stats[3 * row + 1];
-    l1 = a.stats[3 * row + 2];
-  } else {
-    lt = logf(st.st);
-    l1 = logf(st.s1);
-  }
-  const bool empty = lt == -INFINITY;
+  const bool taught = w != 0.f, empty = lt == -INFINITY;            // (NaN goes on)
   float part = 0.f;
   const float lw = logf(w);
-  for (int j = tid; j < a.k; j += NT) {
+  for (int j = tid; j < my_k; j += LIST) {
     if (li[j] < 0) continue;
     const float lq = (lz[j] - st.m) * inv_t - lt, lpj = (lp[j] - tmax) * inv_t - lw, p = taught ? expf(lpj) : 0.f;
     if (p != 0.f) part += p * (lpj - lq);
     lp[j] = p;
   }
-  if constexpr (!BWD) {
+  if (FROM != STATS && seg == 0) {
     if (a.loss) {
       part = block_sum<NT>(part, red_l);
       float loss = (1.f - a.hard) * a.temperature * a.temperature * part;
@@ -209,35 +269,39 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
     if (a.stats && tid == 0) {
       a.stats[3 * row] = st.m;
       a.stats[3 * row + 1] = lt;
-      a.stats[3 * row + 2] = TWO || a.temperature == 1.f ? l1 : 0.f;
+      a.stats[3 * row + 2] = P || a.temperature == 1.f ? l1 : 0.f;
     }
   }
   if (!dz) return;
   __syncthreads();                                   // the list is whole; with dz = z, everybody has read its logits
   const float g = a.grad_scale * (a.row_grad ? a.row_grad[row] : 1.f);
   const float soft = taught && !empty ? (1.f - a.hard) * a.temperature * g : 0.f, mix = labelled && !empty ? a.hard * g : 0.f;
-  const float bt = lt * LOG2E, b1 = l1 * LOG2E;
+  // soft q + mix r, q = exp((z - m) / T) / sum, r = exp(z - m) / sum
+  const float by_q = (P ? soft : soft + mix) * exp2_(-lt * LOG2E), by_r = P ? mix * exp2_(-l1 * LOG2E) : 0.f;
   auto grad = [&](float v) __attribute__((always_inline)) {
-    const float d = v - st.m;
-    if (TWO) return soft * exp2_(d * ct - bt) + mix * exp2_(d * c1 - b1);
-    return (soft + mix) * exp2_(d * ct - bt);
+    const float d = v - st.m, e = exp2_(d * ct);
+    return P ? by_q * e + by_r * second<P>(e, d) : by_q * e;
   };
+  T* out = dz + at.lo;
+  const bool alike = (((uintptr_t)z ^ (uintptr_t)dz) & 15) == 0;     // (rows that lie differently within 16 bytes in z and dz leave value by value)
   if (empty) {
-    for (int i = tid; i < n; i += NT) dz[i] = (T)0.f;
+    for (int i = tid; i < at.hi - at.lo; i += NT) out[i] = (T)0.f;
     return;
   }
-  held.pass([&](int i, float v) __attribute__((always_inline)) { dz[i] = (T)grad(v); },
-                  [&](int i, const float (&v)[V]) __attribute__((always_inline)) {
-                    typename Chunk<T>::vec o;
+  held.pass([&](int i, float v) __attribute__((always_inline)) { out[i] = (T)grad(v); },
+            [&](int i, const float (&v)[V]) __attribute__((always_inline)) {
+              typename Chunk<T>::vec o;
 #pragma unroll
-                    for (int e = 0; e < V; ++e) o[e] = (T)grad(v[e]);
-                    *(typename Chunk<T>::vec*)(dz + i) = o;
-                  });
-  __syncthreads();                                   // the row is out: now the places that p and the label touch
-  bool label_listed = false;
-  for (int j = tid; j < a.k; j += NT) {
+              for (int e = 0; e < V; ++e) o[e] = (T)grad(v[e]);
+              if (alike) *(typename Chunk<T>::vec*)(out + i) = o;
+              else
+#pragma unroll
+                for (int e = 0; e < V; ++e) out[i + e] = o[e];
+            });
+  __syncthreads();                                   // the segment is out: now its places that p and the label touch
+  for (int j = tid; j < my_k; j += LIST) {
     const int c = li[j];
-    if (c < 0) continue;
+    if (c < at.lo || c >= at.hi) continue;
     float p = 0.f;
     bool first = true;
     for (int i = 0; i < a.k; ++i)
@@ -247,48 +311,85 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
       }
     if (first) dz[c] = (T)(grad(lz[j]) - soft * p - (labelled && c == label ? mix : 0.f));
   }
-  if (labelled && tid == 0) {
-    for (int i = 0; i < a.k; ++i) label_listed |= li[i] == label;
-    if (!label_listed) dz[label] = (T)(grad(zl) - mix);
+  if (labelled && label >= at.lo && label < at.hi && tid == 0) {
+    bool listed = false;
+    for (int i = 0; i < a.k; ++i) listed |= li[i] == label;
+    if (!listed) dz[label] = (T)(grad(zl) - mix);
   }
 }
 
-template <typename T, int NT, int C, bool BWD>
-void go(const DistillArgs& a, hipStream_t s) {
-  const size_t lds = (size_t)a.k * 12;
-  if (a.hard > 0.f && a.temperature != 1.f) distill_kernel<T, NT, C, BWD, true><<<(unsigned)a.rows, NT, lds, s>>>(a);
-  else distill_kernel<T, NT, C, BWD, false><<<(unsigned)a.rows, NT, lds, s>>>(a);
+template <class F> void with_power(const DistillArgs& a, F&& f) {
+  if (!(a.hard > 0.f) || a.temperature == 1.f) f(RowC<0>{});
+  else if (a.temperature == 2.f) f(RowC<2>{});
+  else if (a.temperature == 3.f) f(RowC<3>{});
+  else if (a.temperature == 4.f) f(RowC<4>{});
+  else f(RowC<1>{});
 }
-// Whether every row lies within 16 bytes in dz as it does in z
-bool alike(const DistillArgs& a) {
-  const int64_t e = a.f32 ? 4 : 2;
-  return !a.dz || ((((uintptr_t)a.z ^ (uintptr_t)a.dz) & 15) == 0 && (a.rows == 1 || (a.ldz - a.ldd) * e % 16 == 0));
+template <typename T, int NT, int C>
+void go_parts(const DistillArgs& a, hipStream_t s) {
+  with_power(a, [&](auto P) { distill_parts_kernel<T, NT, C, decltype(P)::value><<<(unsigned)(a.rows * a.segments), NT, 0, s>>>(a); });
+}
+template <typename T, int NT, int C, int FROM, int P>
+void go(const DistillArgs& a, hipStream_t s) {
+  distill_kernel<T, NT, C, FROM, P><<<(unsigned)(a.rows * a.writers), NT, (size_t)a.k * 12, s>>>(a);
+}
+template <typename T, int NT, int C, int FROM>
+void go(const DistillArgs& a, hipStream_t s) {
+  with_power(a, [&](auto P) { distill_kernel<T, NT, C, FROM, decltype(P)::value><<<(unsigned)(a.rows * a.writers), NT, (size_t)a.k * 12, s>>>(a); });
 }
 // Small workgroups: more rows at once on a CU, whose lists, sums and barriers then pass unseen behind one another's memory traffic.
-template <typename T, bool BWD>
+template <typename T, int FROM>
 void go_size(const DistillArgs& a, hipStream_t s) {
-  const int n = alike(a) ? (a.classes + Chunk<T>::V - 1) / Chunk<T>::V : INT32_MAX;        // chunks
-  if (n <= 128) go<T, 64, 2, BWD>(a, s);
-  else if (n <= 1024) go<T, 256, 4, BWD>(a, s);
-  else if (n <= 4096) go<T, 256, 16, BWD>(a, s);
-  else if (n <= 8192) go<T, 1024, 8, BWD>(a, s);
-  else if (n <= 16384) go<T, 1024, 16, BWD>(a, s);
-  else if (a.classes <= 1024) go<T, 64, 0, BWD>(a, s);
-  else go<T, 1024, 0, BWD>(a, s);
+  const int all = (a.classes + Chunk<T>::V - 1) / Chunk<T>::V, n = (all + a.writers - 1) / a.writers;        // chunks
+  if constexpr (FROM == PARTS) {
+    const int m = (all + a.segments - 1) / a.segments;
+    if (m <= 1024) go_parts<T, 256, 4>(a, s);
+    else if (m <= 4096) go_parts<T, 256, 16>(a, s);
+    else go_parts<T, 1024, 0>(a, s);
+  }
+  if constexpr (FROM != PARTS)
+    if (n <= 128) return go<T, 64, 2, FROM>(a, s);
+  if (n <= 1024) go<T, 256, 4, FROM>(a, s);
+  else if (n <= 4096) go<T, 256, 16, FROM>(a, s);
+  else if (n <= 8192) go<T, 512, 16, FROM>(a, s);
+  else if (n <= 16384) {
+    // (of one sum there is little to keep beside the row: 16 wavefronts fit; 4096 x 131072 bf16 forward and backward 485 us against 521, and 597 against 647 with two)
+    if (!(a.hard > 0.f) || a.temperature == 1.f) go<T, 1024, 16, FROM, 0>(a, s);
+    else go<T, 512, 32, FROM>(a, s);
+  }
+  else go<T, 1024, 0, FROM>(a, s);
 }
 
 }  // namespace
 
-void distill_forward(const DistillArgs& a, hipStream_t s) {
-  if (a.rows <= 0) return;
-  if (a.f32) go_size<float, false>(a, s);
-  else go_size<bf16, false>(a, s);
+// Segments of a row: as many as give the CUs two workgroups each, of 1024 chunks at least, a wavefront's lanes at most.  A forward split is two launches, which three
+// segments pay for.
+static int segments_of(const DistillArgs& a) {
+  const int64_t chunks = a.classes / (a.f32 ? 4 : 8);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({64, 512 / std::max<int64_t>(a.rows, 1), chunks / 1024}));
+}
+size_t distill_parts_floats(bool f32, int64_t rows, int classes) {
+  DistillArgs a;
+  a.f32 = f32; a.rows = rows; a.classes = classes;
+  const int n = segments_of(a);
+  return n < 3 ? 0 : (size_t)rows * n * 3;
 }
 
-void distill_backward(const DistillArgs& a, hipStream_t s) {
-  if (a.rows <= 0) return;
-  if (a.f32) go_size<float, true>(a, s);
-  else go_size<bf16, true>(a, s);
+void distill_forward(const DistillArgs& given, hipStream_t s) {
+  if (given.rows <= 0) return;
+  DistillArgs a = given;
+  a.segments = a.parts ? segments_of(a) : 1;
+  // (where dz takes the place of z, other segments' logits would be gone: one workgroup writes a row then, from the same parts)
+  a.writers = a.dz && a.dz != a.z ? a.segments : 1;
+  if (a.parts) a.f32 ? go_size<float, PARTS>(a, s) : go_size<bf16, PARTS>(a, s);
+  else a.f32 ? go_size<float, OWN>(a, s) : go_size<bf16, OWN>(a, s);
+}
+
+void distill_backward(const DistillArgs& given, hipStream_t s) {
+  if (given.rows <= 0) return;
+  DistillArgs a = given;
+  a.writers = a.dz != a.z ? segments_of(a) : 1;
+  a.f32 ? go_size<float, STATS>(a, s) : go_size<bf16, STATS>(a, s);
 }
 
 }  // namespace bsr

@@ -46,7 +46,7 @@ LF = dict(x=A, x_type=0, ldx=64, x_scales=None, M=400, n_in=64, n_out=32, values
           ws_bytes=1 << 20, stream=None)
 LD = dict(dy=A, type=0, lddy=32, dy_scales=None, M=400, n_in=64, n_out=32, values=A, scales=A, u=None, dx=A, dx_type=0, ws=A, ws_bytes=1 << 20, stream=None)
 DF = dict(z=A, type=0, rows=4, classes=10, ldz=10, index=A, ldi=3, logits=A, logits_type=1, ldt=3, top=3, labels=None, T=1.0, a=0.0, loss=A, stats=A,
-          row_grad=None, scale=1.0, dz=None, ldd=0, stream=None)
+          row_grad=None, scale=1.0, dz=None, ldd=0, ws=None, ws_floats=0, stream=None)
 DB = dict(z=A, type=0, rows=4, classes=10, ldz=10, index=A, ldi=3, logits=A, logits_type=1, ldt=3, top=3, labels=None, T=1.0, a=0.0, stats=A,
           row_grad=None, scale=1.0, dz=2 * A, ldd=10, stream=None)
 REFUSED = [
@@ -63,7 +63,7 @@ REFUSED = [
     ("bsr_distill_forward", DF, [dict(z=None), dict(z=A + 1), dict(type=4), dict(logits_type=4), dict(rows=-1), dict(rows=1 << 31), dict(classes=0), dict(ldz=9), dict(top=0),
                                  dict(top=1025, ldi=1025, ldt=1025), dict(index=None), dict(ldi=2), dict(logits=None), dict(T=0.0), dict(T=float("inf")), dict(T=float("nan")),
                                  dict(a=-0.1), dict(a=1.1), dict(a=float("nan")), dict(loss=None, stats=None), dict(loss=A + 2), dict(labels=A + 1), dict(dz=A, ldd=11),
-                                 dict(dz=2 * A, ldd=4)]),
+                                 dict(dz=2 * A, ldd=4), dict(ws=A + 2, ws_floats=100), dict(classes=1 << 20, ldz=1 << 20, ws=A, ws_floats=3)]),
     ("bsr_distill_backward", DB, [dict(stats=None), dict(dz=None), dict(row_grad=A + 1), dict(ldd=9)]),
 ]
 
