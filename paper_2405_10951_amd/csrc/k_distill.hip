@@ -293,7 +293,8 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
               typename Chunk<T>::vec o;
 #pragma unroll
               for (int e = 0; e < V; ++e) o[e] = (T)grad(v[e]);
-              if (alike) *(typename Chunk<T>::vec*)(out + i) = o;
+              // (past the caches: 2048 x 21841 bf16 backward 46 -> 36 us, 4096 x 131072 forward and backward 496 -> 455)
+              if (alike) __builtin_nontemporal_store(o, (typename Chunk<T>::vec*)(out + i));
               else
 #pragma unroll
                 for (int e = 0; e < V; ++e) out[i + e] = o[e];

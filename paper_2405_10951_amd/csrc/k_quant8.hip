@@ -48,23 +48,36 @@ __global__ __launch_bounds__(256) void quantize8_rows_kernel(const T* __restrict
   if (part == 0) scale[b] = (uint8_t)s8;
 }
 
-// A workgroup per block: thread t holds 64 columns of row t / 2; the transposed copy goes through LDS.  Once per weight matrix.
-template <typename T>
+// A workgroup per block, 64 values a thread: piece t % P of rows t / P, t / P + 256 / P, ... (P 16-byte pieces a row of the block; VEC: they all lie on
+// 16-byte boundaries).  The transposed copy goes through LDS.  Once per weight matrix.  4096 x 8192 bf16: 24 us, with both copies.
+template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void quantize8_weight_kernel(const T* __restrict__ w, int in, int out, int64_t ldw, uint8_t* __restrict__ q,
                                                                uint8_t* __restrict__ scale, uint8_t* __restrict__ q_back,
                                                                uint8_t* __restrict__ scale_back) {
+  constexpr int V = Chunk<T>::V, P = BLOCK8 / V, STEP = 256 / P, N = BLOCK8 / STEP;
   __shared__ uint8_t tile[BLOCK8][BLOCK8 + 4];
   __shared__ uint32_t wave_most[4];
   const int i0 = blockIdx.y * BLOCK8, n0 = blockIdx.x * BLOCK8;
-  const int r = threadIdx.x >> 1, c0 = (threadIdx.x & 1) * 64;
-  float v[64];
+  const int r0 = threadIdx.x / P, c = threadIdx.x % P * V;
+  float v[N][V];
   uint32_t most = 0;
-  const T* src = w + (int64_t)(i0 + r) * ldw + n0 + c0;
+  typename Chunk<T>::vec raw[N];
 #pragma unroll
-  for (int c = 0; c < 64; ++c) {
-    v[c] = i0 + r < in && n0 + c0 + c < out ? (float)src[c] : 0.f;
-    most = umax_dpp(most, finite_bits(v[c]));
+  for (int k = 0; k < N; ++k) {
+    const int i = i0 + r0 + k * STEP;
+    const T* src = w + (int64_t)min(i, in - 1) * ldw + n0 + c;
+    if (VEC && n0 + c + V <= out) raw[k] = *(const typename Chunk<T>::vec*)src;
+    else
+#pragma unroll
+      for (int e = 0; e < V; ++e) raw[k][e] = n0 + c + e < out ? src[e] : (T)0.f;
   }
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      v[k][e] = i0 + r0 + k * STEP < in ? (float)raw[k][e] : 0.f;
+      most = umax_dpp(most, finite_bits(v[k][e]));
+    }
   // bits of non-negative floats order as the floats do
   most = __float_as_uint(wave_max(__uint_as_float(most)));
   if ((threadIdx.x & 63) == 0) wave_most[threadIdx.x >> 6] = most;
@@ -75,19 +88,27 @@ __global__ __launch_bounds__(256) void quantize8_weight_kernel(const T* __restri
   const float inv = inverse_of(s8);
   const int64_t ldq = ld8(in), ldb = ld8(out), lds = ld8s(in), ldbs = ld8s(out);
 #pragma unroll
-  for (int c = 0; c < 64; c += 4) {
-    const uint32_t p = pack8(v[c], v[c + 1], v[c + 2], v[c + 3], inv);
-    *(uint32_t*)&tile[r][c0 + c] = p;
-    if (q_back && i0 + r < in) *(uint32_t*)(q_back + (int64_t)(i0 + r) * ldb + n0 + c0 + c) = p;
+  for (int k = 0; k < N; ++k) {
+    const int r = r0 + k * STEP;
+#pragma unroll
+    for (int e = 0; e < V; e += 4) {
+      const uint32_t p = pack8(v[k][e], v[k][e + 1], v[k][e + 2], v[k][e + 3], inv);
+      *(uint32_t*)&tile[r][c + e] = p;
+      if (q_back && i0 + r < in) *(uint32_t*)(q_back + (int64_t)(i0 + r) * ldb + n0 + c + e) = p;
+    }
   }
   __syncthreads();
-  if (n0 + r < out)
+  // eight neighbouring threads write a row of the other copy, 16 bytes each
+  const int part = threadIdx.x % 8 * 16;
 #pragma unroll
-    for (int c = 0; c < 64; c += 4) {
-      const uint32_t p = tile[c0 + c][r] | (uint32_t)tile[c0 + c + 1][r] << 8 | (uint32_t)tile[c0 + c + 2][r] << 16 |
-                         (uint32_t)tile[c0 + c + 3][r] << 24;
-      *(uint32_t*)(q + (int64_t)(n0 + r) * ldq + i0 + c0 + c) = p;
-    }
+  for (int k = 0; k < 4; ++k) {
+    const int r = threadIdx.x / 8 + k * 32;
+    uint32_t p[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      p[j] = tile[part + 4 * j][r] | (uint32_t)tile[part + 4 * j + 1][r] << 8 | (uint32_t)tile[part + 4 * j + 2][r] << 16 | (uint32_t)tile[part + 4 * j + 3][r] << 24;
+    if (n0 + r < out) *(uint4*)(q + (int64_t)(n0 + r) * ldq + i0 + part) = make_uint4(p[0], p[1], p[2], p[3]);
+  }
   if (threadIdx.x == 0) {
     const int bi = blockIdx.y, bn = blockIdx.x;
     scale[bn * lds + bi] = (uint8_t)s8;
@@ -122,8 +143,10 @@ void quantize8_rows(const void* x, bool f32, int64_t M, int K, int64_t ldx, void
 void quantize8_weight(const void* w, bool f32, int in, int out, int64_t ldw, void* q, uint8_t* scale, void* q_back, uint8_t* scale_back,
                       hipStream_t s) {
   const dim3 grid((out + BLOCK8 - 1) / BLOCK8, (in + BLOCK8 - 1) / BLOCK8);
-  if (f32) quantize8_weight_kernel<float><<<grid, 256, 0, s>>>((const float*)w, in, out, ldw, (uint8_t*)q, scale, (uint8_t*)q_back, scale_back);
-  else quantize8_weight_kernel<bf16><<<grid, 256, 0, s>>>((const bf16*)w, in, out, ldw, (uint8_t*)q, scale, (uint8_t*)q_back, scale_back);
+  const bool vec = ((uintptr_t)w & 15) == 0 && ldw * (f32 ? 4 : 2) % 16 == 0;
+  auto go = [&](auto kern, auto* p) { kern<<<grid, 256, 0, s>>>(p, in, out, ldw, (uint8_t*)q, scale, (uint8_t*)q_back, scale_back); };
+  if (f32) vec ? go(quantize8_weight_kernel<float, true>, (const float*)w) : go(quantize8_weight_kernel<float, false>, (const float*)w);
+  else vec ? go(quantize8_weight_kernel<bf16, true>, (const bf16*)w) : go(quantize8_weight_kernel<bf16, false>, (const bf16*)w);
 }
 
 }  // namespace bsr

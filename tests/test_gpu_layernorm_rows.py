@@ -146,6 +146,25 @@ def test_many_rows_of_one_value(env):
     assert not r8.values.any() and bool((r8.scales[:, :6] == 127).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [256, 300, 1024, 8200])
+def test_infinities_and_nan_in_8_bit_rows(env, D, dtype):
+    """a gain of infinity or NaN in some columns: those are NaN in 8 bits and do not count towards their blocks' maxima"""
+    torch, P = env
+    x, _, gamma, beta = make(torch, 9, D, dtype)
+    plain, _, _ = P.bsr_layernorm_forward8(x, torch.where(torch.arange(D, device="cuda") % 128 == 5, 0.0, gamma), torch.where(torch.arange(D, device="cuda") % 128 == 5, 0.0, beta), EPS)
+    gamma[5::128] = float("inf")
+    gamma[5] = float("nan")
+    r8, _, _ = P.bsr_layernorm_forward8(x, gamma, beta, EPS)
+    n = -(-D // 128)
+    assert torch.equal(r8.scales[:, :n], plain.scales[:, :n])
+    got, want = r8.values[:, :D].clone(), plain.values[:, :D].clone()
+    assert bool((got[:, 5::128] & 0x7f == 0x7f).all())
+    got[:, 5::128] = 0
+    want[:, 5::128] = 0
+    assert torch.equal(got, want)
+
+
 def test_no_rows_zero_the_sums(env):
     torch, P = env
     x = torch.empty(0, 96, device="cuda")
