@@ -3,6 +3,7 @@ as device memory, the stream is torch's current HIP stream.  Same names as the C
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 MAX_BLOCKS = 16
@@ -439,6 +440,20 @@ def _together(first, *others):
     return _raw_stream(gpu)
 
 
+@functools.lru_cache(maxsize=256)
+def _scratch_size(which, *sizes):
+    """A size that the library names (a call costs as much as a look-up of a few of them)."""
+    return getattr(load_library(), which)(*sizes)
+
+
+def _like(t):
+    """A new contiguous tensor of the shape and type of one."""
+    if t.is_contiguous():
+        import torch
+        return torch.empty_like(t)
+    return t.new_empty(t.shape)
+
+
 def _rows8_new(M, K, like):
     import torch
     nk = -(-K // 128)
@@ -483,7 +498,7 @@ def _linear8(x, cols, what, *others):
     if k != cols:
         raise ValueError(f"{what}: {k} columns, the layer has {cols}")
     stream = _together(x, *others)
-    size, ws = load_library().bsr_linear8_workspace_bytes(M, cols), None
+    size, ws = _scratch_size("bsr_linear8_workspace_bytes", M, cols), None
     if size:
         import torch
         ws = x.new_empty(size, dtype=torch.uint8)
@@ -493,9 +508,11 @@ def _linear8(x, cols, what, *others):
 def _linear8_out(x, t, y, what, shape, out_dtype):
     if y is None:
         if out_dtype is None:
+            if type(x) is not Rows8:
+                return t.new_empty(shape)
             import torch
-            out_dtype = torch.bfloat16 if type(x) is Rows8 else x.dtype
-        return t.new_empty(shape, dtype=out_dtype)
+            out_dtype = torch.bfloat16
+        return t.new_empty(shape) if t.dtype is out_dtype else t.new_empty(shape, dtype=out_dtype)
     if out_dtype is not None and y.dtype is not out_dtype:
         raise TypeError(f"{what}: {y.dtype}, out_dtype {out_dtype}")
     return y
@@ -547,7 +564,7 @@ def _layernorm_forward(x, gamma, beta, eps, y, r8):
 def bsr_layernorm_forward(x, gamma, beta, eps=1e-6, y=None):
     """x [M,D] bf16 or fp32 (any row stride), gamma, beta [D] fp32 -> (y [M,D], mean [M], rstd [M])."""
     if y is None:
-        y = x.new_empty(x.shape)
+        y = _like(x)
     mean, rstd = _layernorm_forward(x, gamma, beta, eps, y, None)
     return y, mean, rstd
 
@@ -574,13 +591,13 @@ def bsr_layernorm_backward(dy, x, mean, rstd, gamma, res=None, dx=None, need_dx=
     if dx is None:
         lddx = D
         if need_dx:
-            dx = x.new_empty(shape)
+            dx = _like(x)
     else:
         lddx = _rows_of(dx, "dx", shape, dtype)
     dg = db = ws = None
     floats = 0
     if need_params:
-        floats = lib.bsr_layernorm_workspace_floats(D)
+        floats = _scratch_size("bsr_layernorm_workspace_floats", D)
         dg, db, ws = gamma.new_empty(D), gamma.new_empty(D), gamma.new_empty(floats)
     _check(lib.bsr_layernorm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, _dp(res), ldr, code, M, D, pm, ps, pg, _dp(dx), lddx, _dp(dg), _dp(db),
                                       _dp(ws), floats, stream))
@@ -606,14 +623,14 @@ def _distill_dz(z, row_grad, dz):
         import torch
         pg = _flat(row_grad, "row_grad", z.shape[:1], torch.float32)
     if dz is None:
-        return pg, z.new_empty(z.shape), z.shape[1]
+        return pg, _like(z), z.shape[1]
     return pg, dz, _rows_of(dz, "dz", z.shape, z.dtype)
 
 
 def _distill_workspace(z, code):
     """-> (scratch of the forward or None, its floats)"""
     rows, classes = z.shape
-    floats = load_library().bsr_distill_workspace_floats(code, rows, classes)
+    floats = _scratch_size("bsr_distill_workspace_floats", code, rows, classes)
     if not floats:
         return None, 0
     import torch
