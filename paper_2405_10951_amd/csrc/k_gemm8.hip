@@ -53,7 +53,7 @@ template <typename T> __device__ __forceinline__ void put16(T* p, int n, bool ve
 
 // What follows the products of a wave tile: bias, GELU (with its stored input) or GELU', residual.  Bias and GELU are finished where the
 // accumulators are; 32 rows at a time then go through a patch of LDS, rounded where nothing is to be added any more, and come back with a lane owning
-// 16 bytes of a row.  bias: that of the wave tile's columns, in LDS.  What is added or multiplied there is asked for ahead of the patch.  The row blocks are a
+// 16 bytes of a row.  bias: that of the wave tile's columns, in LDS.  What is added or multiplied there is asked for a row block ahead.  The row blocks are a
 // loop: code that is written out once is fetched once.
 // Stores.  A row of a wave tile is one or two 128-byte lines, or half of one, where rows lie on lines; such stores go past the caches, which
 // otherwise lose the operands' panels to results that nobody reads here (16384 x 4096 x 8192: 509 -> 460 us; 6304 x 768 x 2304: 17.7 -> 15.7).  Smaller pieces of lines must not:
@@ -92,6 +92,16 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
     fence();
   };
   const T* extra = (const T*)(ACT == ACT_GELU_BWD ? g.aux : g.res);
+  const bool add = ACT == ACT_GELU_BWD || g.res;
+  vecT next[NPASS];                                  // of the row block after this one
+  auto ask = [&](int mi) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < NPASS; ++p) {
+      const int m = row0 + mi * 32 + p * RPP + my_row;
+      if (m < g.M && n > 0) next[p] = get16(extra + (int64_t)m * g.ldc + col, n, vec);
+    }
+  };
+  if (add) ask(0);
 #pragma nounroll
   for (int mi = 0; mi < MI; ++mi) {
     f32x16 blk[NI];
@@ -102,13 +112,9 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
         for (int ni = 0; ni < NI; ++ni) blk[ni] = acc[i][ni];
     });
     vecT more[NPASS];
-    const bool add = ACT == ACT_GELU_BWD || g.res;
-    if (add)
 #pragma unroll
-      for (int p = 0; p < NPASS; ++p) {
-        const int m = row0 + mi * 32 + p * RPP + my_row;
-        if (m < g.M && n > 0) more[p] = get16(extra + (int64_t)m * g.ldc + col, n, vec);
-      }
+    for (int p = 0; p < NPASS; ++p) more[p] = next[p];
+    if (add && mi + 1 < MI) ask(mi + 1);
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
