@@ -180,8 +180,13 @@ __device__ __forceinline__ void place(int t, int ntm, int ntn, int& tm, int& tn)
 // A stage is (BM + BN) rows of 128 bytes (eight chunks of 16, chunk c of row r in slot c ^ swz(r)) and behind them a dword of scales for
 // each row: the scales of four k-tiles, of which each k-tile reads its byte (each k-tile fetches the dword anew, 1/32 more bytes, so that
 // every k-tile is the same number of loads and can be waited for by count).
+template <int BM, int BN, int NT, int NST> constexpr size_t lds_of() {      // of a workgroup: stages and bias
+  return (size_t)NST * ((BM + BN) * 128 + (BM + BN + NT - 1) / NT * NT * 4) + BN * 4;
+}
+// (held to the registers that let as many workgroups share a CU as its LDS has room for, up to three)
 template <int BM, int BN, int WM, int WN, int NST, typename T, int ACT, bool EXACT>
-__global__ __launch_bounds__(WM * WN * 64, 1) void gemm8_kernel(const void* hA, const void* hB, const void* hsa, const void* hsb, int hM, int hN, int hK,
+__global__ __launch_bounds__(WM * WN * 64, std::max<int>(1, std::min<int>(3, 160 * 1024 / lds_of<BM, BN, WM * WN * 64, NST>()) * WM * WN / 4))
+void gemm8_kernel(const void* hA, const void* hB, const void* hsa, const void* hsb, int hM, int hN, int hK,
                                                                 int tiles, Gemm8Desc g) {
   constexpr int NW = WM * WN, NT = NW * 64, ROWS = BM + BN;
   constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 32, NI = TN / 32, NMF = MI * NI;
@@ -579,7 +584,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
 template <int BM, int BN, int WM, int WN, int NST, typename T, int ACT, bool EXACT>
 void launch_tiled(const Gemm8Desc& g, hipStream_t s) {
   constexpr int NT = WM * WN * 64;
-  constexpr size_t stages = (size_t)NST * ((BM + BN) * 128 + (BM + BN + NT - 1) / NT * NT * 4) + BN * 4;
+  constexpr size_t stages = lds_of<BM, BN, NT, NST>();
   static_assert(BN <= NT, "a thread for each column of the bias");
   constexpr size_t patches = (size_t)WM * WN * 32 * (BN / WN + 4) * 4;
   static_assert(patches <= stages && stages <= 160 * 1024, "the epilogue patches live in the stages");
