@@ -30,24 +30,21 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-// 16 bytes of a row of results: PIECE columns
-template <typename T> struct Piece16 { static constexpr int N = 16 / sizeof(T); typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)))); };
-// a piece of which n columns exist; vec: all of them do, and the address is aligned to 16 bytes
-template <typename T> __device__ __forceinline__ typename Piece16<T>::vec get16(const T* p, int n, bool vec) {
-  typedef typename Piece16<T>::vec V;
-  if (vec) return *(const V*)p;
-  V o;
+// 16 bytes of a row of results, at the address of any element, of which n columns exist
+template <typename T> __device__ __forceinline__ typename Chunk<T>::vec get16(const T* p, int n) {
+  if (n >= Chunk<T>::V) return *(const typename Loose<T>::vec*)p;
+  typename Chunk<T>::vec o;
 #pragma unroll
-  for (int i = 0; i < Piece16<T>::N; ++i) o[i] = i < n ? p[i] : (T)0.f;
+  for (int i = 0; i < Chunk<T>::V; ++i) o[i] = i < n ? p[i] : (T)0.f;
   return o;
 }
 // past: past the caches, where rows lie on lines
-template <typename T> __device__ __forceinline__ void put16(T* p, int n, bool vec, bool past, typename Piece16<T>::vec v) {
-  if (vec && past) __builtin_nontemporal_store(__builtin_bit_cast(i32x4, v), (i32x4*)p);
-  else if (vec) *(i32x4*)p = __builtin_bit_cast(i32x4, v);
+template <typename T> __device__ __forceinline__ void put16(T* p, int n, bool past, typename Chunk<T>::vec v) {
+  if (n >= Chunk<T>::V && past) __builtin_nontemporal_store(__builtin_bit_cast(i32x4, v), (i32x4*)p);
+  else if (n >= Chunk<T>::V) *(typename Loose<T>::vec*)p = v;
   else
 #pragma unroll
-    for (int i = 0; i < Piece16<T>::N; ++i)
+    for (int i = 0; i < Chunk<T>::V; ++i)
       if (i < n) p[i] = v[i];
 }
 
@@ -61,10 +58,9 @@ template <typename T> __device__ __forceinline__ void put16(T* p, int n, bool ve
 template <int MI, int NI, typename T, int ACT>
 __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][NI], int row0, int col0, int lane, unsigned char* patch,
                                           const float* bias) {
-  typedef typename Piece16<T>::vec vecT;
-  constexpr int P = Piece16<T>::N, TN = NI * 32, CPR = TN / P, RPP = 64 / CPR, NPASS = 32 / RPP, LDF = (TN + 4) * 4, LDT = TN * (int)sizeof(T) + 16;
+  typedef typename Chunk<T>::vec vecT;
+  constexpr int P = Chunk<T>::V, TN = NI * 32, CPR = TN / P, RPP = 64 / CPR, NPASS = 32 / RPP, LDF = (TN + 4) * 4, LDT = TN * (int)sizeof(T) + 16;
   const int lr = lane & 31, lh = lane >> 5, my_row = lane / CPR, col = col0 + lane % CPR * P, n = g.N - col;
-  const bool vec = g.ldc * (int64_t)sizeof(T) % 16 == 0 && n >= P;
   const bool past = g.ldc * (int64_t)sizeof(T) % 128 == 0;
   auto fence = [&]() __attribute__((always_inline)) {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -87,7 +83,7 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
     for (int p = 0; p < NPASS; ++p) {
       const int r = p * RPP + my_row, m = row0 + mi * 32 + r;
       const vecT v = *(const vecT*)(patch + r * LDT + lane % CPR * 16);
-      if (m < g.M && n > 0) put16(dst + (int64_t)m * g.ldc + col, n, vec, past, v);
+      if (m < g.M && n > 0) put16(dst + (int64_t)m * g.ldc + col, n, past, v);
     }
     fence();
   };
@@ -98,7 +94,7 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
 #pragma unroll
     for (int p = 0; p < NPASS; ++p) {
       const int m = row0 + mi * 32 + p * RPP + my_row;
-      if (m < g.M && n > 0) next[p] = get16(extra + (int64_t)m * g.ldc + col, n, vec);
+      if (m < g.M && n > 0) next[p] = get16(extra + (int64_t)m * g.ldc + col, n);
     }
   };
   if (add) ask(0);
@@ -147,13 +143,14 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
       vecT v;
 #pragma unroll
       for (int i = 0; i < P; ++i) v[i] = (T)(ACT == ACT_GELU_BWD ? src[i] * gelu_grad_f((float)more[p][i]) : src[i] + (float)more[p][i]);
-      if (m < g.M && n > 0) put16((T*)g.C + (int64_t)m * g.ldc + col, n, vec, past, v);
+      if (m < g.M && n > 0) put16((T*)g.C + (int64_t)m * g.ldc + col, n, past, v);
     }
     fence();
   }
 }
 
 constexpr int EXACT_BELOW = 768;
+static_assert(EXACT_BELOW >= 32, "rows shorter than a piece have the exact form alone");
 
 // eight e4m3 values (two dwords) times the power of two whose E8M0 byte is s8: exact in bf16
 __device__ __forceinline__ bf16x8 widen8(int lo, int hi, int s8) {
@@ -470,18 +467,29 @@ __device__ __forceinline__ int quantize32(const typename Chunk<T>::vec (&v)[32 /
   return s8;
 }
 
+// 32 bytes without the first n (< 32), zeros behind them
+__device__ __forceinline__ i32x8 bytes_down(i32x8 q, int n) {
+#pragma unroll
+  for (int step = 4; step > 0; step /= 2)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = n & 4 * step ? (i + step < 8 ? q[i + step] : 0) : q[i];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = (int)__builtin_amdgcn_alignbyte(i < 7 ? q[i + 1] : 0, q[i], n & 3);
+  return q;
+}
+
 // Few rows: what counts is that the weights come once and at once.  A workgroup owns 16 columns and all rows (16 MI of them); its eight
 // wavefronts share the k-tiles, each with its own straight from global memory into registers (a weight row's 128 bytes of a k-tile are a
 // cache line that four lanes read whole), AHEAD of them asked for before the first is looked at, and their sums meet in LDS in wavefront
-// order.  Rows of bf16 or fp32 (X: X_VEC where they are whole, aligned pieces of 32 values) are brought to 8 bits here by every workgroup for itself: they are few, and
-// it saves the launch.  Bound by the latency of one trip to memory, then by the weights' bytes.
-enum { X_E4, X_BF16, X_BF16_VEC, X_F32, X_F32_VEC };
+// order.  Rows of bf16 or fp32 are brought to 8 bits here by every workgroup for itself: they are
+// few, and it saves the launch.  Bound by the latency of one trip to memory, then by the weights' bytes.
+enum { X_E4, X_BF16, X_F32 };                      // type of the rows
+enum { ROWS_WHOLE, ROWS_PART, ROWS_SHORT };        // of whole pieces of 32 values; with a part of one at the end; of less than one
 constexpr int FEW_WAVES = 8, FEW_ROWS = 32;
-template <int X, int MI, bool EXACT>
+template <int X, int MI, bool EXACT, int ROWS>
 __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void* hA, const void* hB, const void* hsa, const void* hsb, int hM, int hN,
                                                                       int hK, int64_t lda, Gemm8Desc g) {
-  constexpr bool VEC = X == X_BF16_VEC || X == X_F32_VEC, F32 = X == X_F32 || X == X_F32_VEC;
-  typedef typename std::conditional<F32, float, bf16>::type TX;
+  typedef typename std::conditional<X == X_F32, float, bf16>::type TX;
   constexpr int V = Chunk<TX>::V, AHEAD = X == X_E4 ? 4 : 4 / MI;
   __shared__ float part[FEW_WAVES][MI * 16][16 + 1];
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
@@ -497,7 +505,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
   for (int kt0 = wave; kt0 < nk; kt0 += FEW_WAVES * AHEAD) {
     i32x8 w[AHEAD], x8[X == X_E4 ? AHEAD : 1][MI];
     int ws[AHEAD], xs[X == X_E4 ? AHEAD : 1][MI];
-    typename Chunk<TX>::vec raw[VEC ? AHEAD : 1][MI][32 / V];
+    typename Chunk<TX>::vec raw[X == X_E4 ? 1 : AHEAD][MI][32 / V];
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {                      // (past the end: the last k-tile again, not used)
       const int kt = min(kt0 + a * FEW_WAVES, nk - 1);
@@ -510,10 +518,13 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
           const uint8_t* p = (const uint8_t*)hA + m * ld + (int64_t)kt * BLOCK8 + lg * 32;
           x8[a][mi] = join8(*(const i32x4*)p, *(const i32x4*)(p + 16));
           xs[a][mi] = ((const uint8_t*)hsa)[m * lds + kt];
-        } else if constexpr (VEC) {
+        } else if constexpr (ROWS != ROWS_SHORT) {         // (a piece past the end: the last 32 values)
           const TX* p = (const TX*)hA + m * lda + min(kt * BLOCK8 + lg * 32, hK - 32);
 #pragma unroll
-          for (int i = 0; i < 32 / V; ++i) raw[a][mi][i] = *(const typename Chunk<TX>::vec*)(p + i * V);
+          for (int i = 0; i < 32 / V; ++i) raw[a][mi][i] = *(const typename Loose<TX>::vec*)(p + i * V);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) raw[a][mi][i / V][i % V] = ((const TX*)hA)[m * lda + min(i, hK - 1)];
         }
       }
     }
@@ -531,15 +542,22 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
         } else {
           const int k0 = kt * BLOCK8 + lg * 32;
           typename Chunk<TX>::vec v[32 / V];
-          if constexpr (VEC) {
 #pragma unroll
-            for (int i = 0; i < 32 / V; ++i) v[i] = k0 < hK ? raw[a][mi][i] : typename Chunk<TX>::vec{};
+          for (int i = 0; i < 32 / V; ++i) v[i] = ROWS == ROWS_WHOLE && k0 >= hK ? typename Chunk<TX>::vec{} : raw[a][mi][i];
+          if constexpr (ROWS == ROWS_WHOLE) {
+            s8 = quantize32<TX>(v, x);
+          } else if constexpr (ROWS == ROWS_PART) {        // the values that are another piece's do not count, and leave
+            const int skip = min(max(k0 - (hK - 32), 0), 32);
+            if (kt == nk - 1)
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i / V][i % V] = i < skip ? (TX)0.f : v[i / V][i % V];
+            s8 = quantize32<TX>(v, x);
+            if (kt == nk - 1) x = bytes_down(x, skip & 31);
           } else {
-            const TX* p = (const TX*)hA + (int64_t)min(mi * 16 + lr, hM - 1) * lda + k0;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i / V][i % V] = k0 + i < hK ? p[i] : (TX)0.f;
+            for (int i = 0; i < 32; ++i) v[i / V][i % V] = k0 + i < hK ? v[i / V][i % V] : (TX)0.f;
+            s8 = quantize32<TX>(v, x);
           }
-          s8 = quantize32<TX>(v, x);
         }
         if constexpr (EXACT) {
 #pragma unroll
@@ -650,23 +668,26 @@ void tiled(const Gemm8Desc& g, hipStream_t s) {
   }
 }
 
-template <int X, bool EXACT>
+template <int X, bool EXACT, int ROWS>
 void few_as(const Gemm8Desc& g, hipStream_t s) {
   const unsigned grid = (unsigned)((g.N + 15) / 16);
   auto go = [&](auto MI) {
-    gemm8_few_kernel<X, decltype(MI)::value, EXACT><<<grid, FEW_WAVES * 64, 0, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, g.lda, g);
+    gemm8_few_kernel<X, decltype(MI)::value, EXACT, ROWS><<<grid, FEW_WAVES * 64, 0, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, g.lda, g);
   };
   if (g.M <= 16) go(IC<1>{});
   else go(IC<2>{});
 }
 template <bool EXACT>
 void few(const Gemm8Desc& g, hipStream_t s) {
-  const bool vec = ((uintptr_t)g.A & 15) == 0 && g.lda * (g.a_type == 1 ? 4 : 2) % 16 == 0 && g.K % 32 == 0;
-  if (g.a_type == 2) few_as<X_E4, EXACT>(g, s);
-  else if (g.a_type == 1 && vec) few_as<X_F32_VEC, EXACT>(g, s);
-  else if (g.a_type == 1) few_as<X_F32, EXACT>(g, s);
-  else if (vec) few_as<X_BF16_VEC, EXACT>(g, s);
-  else few_as<X_BF16, EXACT>(g, s);
+  auto of = [&](auto X) {
+    constexpr int x = decltype(X)::value;
+    if (g.K % 32 == 0) few_as<x, EXACT, ROWS_WHOLE>(g, s);
+    else if (g.K > 32) few_as<x, EXACT, ROWS_PART>(g, s);
+    else if constexpr (EXACT) few_as<x, EXACT, ROWS_SHORT>(g, s);          // (short sums are)
+  };
+  if (g.a_type == 2) few_as<X_E4, EXACT, ROWS_WHOLE>(g, s);
+  else if (g.a_type == 1) of(IC<X_F32>{});
+  else of(IC<X_BF16>{});
 }
 
 template <typename T, bool EXACT>

@@ -25,7 +25,7 @@ struct NormRowsBwd {
   float *dgamma = nullptr, *dbeta = nullptr;        // both or none
   float* partial = nullptr;                         // scratch of norm_rows_bwd_floats(D), where dgamma is given
 };
-inline size_t norm_rows_bwd_floats(int D) { return (size_t)NORM_PARTIALS * 2 * (size_t)D; }
+inline size_t norm_rows_bwd_floats(int D) { return (size_t)NORM_PARTIALS * 2 * (((size_t)D + 7) / 8 * 8); }      // (partial rows are whole chunks)
 void norm_rows_bwd(const NormRowsBwd& a, hipStream_t s);
 
 }  // namespace bsr

@@ -9,6 +9,8 @@ constexpr int WAVE = 64;
 constexpr int ROW_MAX = 2048;       // longest row these kernels take
 
 template <typename T> struct Chunk { static constexpr int V = 16 / sizeof(T); typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)))); };
+// the same 16 bytes at the address of any element: global loads and stores of gfx950 take any address
+template <typename T> struct Loose { typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T)))); };
 
 // Sums and maxima over a wavefront, in every lane; the pairs are those of an exchange with lane ^ 32, ^ 16, ... ^ 1.  They stay on the vector
 // unit: gfx950 swaps half waves and rows of 16 lanes, and once lanes 8 (then 4) apart hold the same value, a rotation by 8 (by 4)
