@@ -177,12 +177,14 @@ __device__ __forceinline__ void place(int t, int ntm, int ntn, int& tm, int& tn)
 // A stage is (BM + BN) rows of 128 bytes (eight chunks of 16, chunk c of row r in slot c ^ swz(r)) and behind them a dword of scales for
 // each row: the scales of four k-tiles, of which each k-tile reads its byte (each k-tile fetches the dword anew, 1/32 more bytes, so that
 // every k-tile is the same number of loads and can be waited for by count).
-template <int BM, int BN, int NT, int NST> constexpr size_t lds_of() {      // of a workgroup: stages and bias
-  return (size_t)NST * ((BM + BN) * 128 + (BM + BN + NT - 1) / NT * NT * 4) + BN * 4;
+// KG groups of wavefronts, each with stages of its own, share the k-tiles of a block tile (few tiles, long sums); the groups behind the first leave their
+// sums in LDS, and the first adds them in their order.
+template <int BM, int BN, int NT, int NST, int KG> constexpr size_t lds_of() {      // of a workgroup: stages and bias
+  return (size_t)KG * NST * ((BM + BN) * 128 + (BM + BN + NT - 1) / NT * NT * 4) + BN * 4;
 }
 // (held to the registers that let as many workgroups share a CU as its LDS has room for, up to three)
-template <int BM, int BN, int WM, int WN, int NST, typename T, int ACT, bool EXACT>
-__global__ __launch_bounds__(WM * WN * 64, std::max<int>(1, std::min<int>(3, 160 * 1024 / lds_of<BM, BN, WM * WN * 64, NST>()) * WM * WN / 4))
+template <int BM, int BN, int WM, int WN, int NST, int KG, typename T, int ACT, bool EXACT>
+__global__ __launch_bounds__(WM * WN * KG * 64, std::max<int>(1, std::min<int>(3, 160 * 1024 / lds_of<BM, BN, WM * WN * 64, NST, KG>()) * WM * WN * KG / 4))
 void gemm8_kernel(const void* hA, const void* hB, const void* hsa, const void* hsb, int hM, int hN, int hK,
                                                                 int tiles, Gemm8Desc g) {
   constexpr int NW = WM * WN, NT = NW * 64, ROWS = BM + BN;
@@ -195,17 +197,23 @@ void gemm8_kernel(const void* hA, const void* hB, const void* hsa, const void* h
   constexpr int STAGE = SCALES + SL * NT * 4;
   static_assert(BM % RPI == 0 && BN % RPI == 0 && RPI % 16 == 0, "a load instruction covers whole groups of 16 rows");
   static_assert(NST >= 2 && NST <= 4 && (NST - 1) * LPT <= 60, "vmcnt has 6 bits");
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_all[];
   const int M = hM, N = hN;
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int group = KG > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
+  unsigned char* smem = smem_all + group * NST * STAGE;
+  float* bias = (float*)(smem_all + KG * NST * STAGE);
+  const int tid = threadIdx.x - group * NT, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
   const int tile = xcd_remap(blockIdx.x, tiles);
   int tm, tn;
   place(tile, (M + BM - 1) / BM, (N + BN - 1) / BN, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
-  const int nk = (hK + BLOCK8 - 1) / BLOCK8;
-  const unsigned ld = (unsigned)nk * BLOCK8, lds = (unsigned)(nk + 3) / 4 * 4;
+  const int nall = (hK + BLOCK8 - 1) / BLOCK8;
+  const unsigned ld = (unsigned)nall * BLOCK8, lds = (unsigned)(nall + 3) / 4 * 4;
+  // the group's k-tiles: `mine` from `first` on, in nk turns (the barriers are everybody's; a group with one k-tile less passes over the last turn)
+  const int first = KG > 1 ? group * (nall / KG) + min(group, nall % KG) : 0, mine = KG > 1 ? nall / KG + (group < nall % KG) : nall;
+  const int nk = KG > 1 ? (nall + KG - 1) / KG : nall;
   const uint8_t* __restrict__ A = (const uint8_t*)hA + (int64_t)m0 * ld;
   const uint8_t* __restrict__ B = (const uint8_t*)hB + (int64_t)n0 * ld;
 
@@ -226,8 +234,9 @@ void gemm8_kernel(const void* hA, const void* hB, const void* hsa, const void* h
     soff[i] = r < BM ? (const uint8_t*)hsa + (int64_t)min(m0 + r, M - 1) * lds
                      : (const uint8_t*)hsb + (int64_t)(min(n0 + r - BM, N - 1) / BLOCK8) * lds;
   }
-  auto issue1 = [&](auto I, int kt, int st) __attribute__((always_inline)) {
+  auto issue1 = [&](auto I, int turn, int st) __attribute__((always_inline)) {
     constexpr int i = decltype(I)::value;
+    const int kt = KG > 1 ? min(first + turn, nall - 1) : turn;
     unsigned char* base = smem + st * STAGE;
     if constexpr (i < AL + BL) {
       const uint8_t* src = (i < AL ? A : B) + (size_t)kt * BLOCK8;
@@ -278,11 +287,11 @@ void gemm8_kernel(const void* hA, const void* hB, const void* hsa, const void* h
   };
   auto rdsa = [&](auto I, int st, int kt) __attribute__((always_inline)) {
     constexpr int i = decltype(I)::value;
-    sa[i] = smem[st * STAGE + as_at + i * 128 + (kt & 3)];
+    sa[i] = smem[st * STAGE + as_at + i * 128 + (first + kt & 3)];
   };
   auto rdsb = [&](int st, int kt) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) sbn[i] = smem[st * STAGE + bs_at + i * 128 + (kt & 3)];
+    for (int i = 0; i < NI; ++i) sbn[i] = smem[st * STAGE + bs_at + i * 128 + (first + kt & 3)];
   };
   auto next_scales = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -367,9 +376,9 @@ void gemm8_kernel(const void* hA, const void* hB, const void* hsa, const void* h
 
   // the bias goes behind the stages, ahead of the first k-tile: it has landed when that has
   if (g.bias) {
-    if (wave < BN / 64) __builtin_amdgcn_global_load_lds(BSR_GLOBAL_PTR(g.bias + min(n0 + tid, N - 1)), BSR_LDS_VOID(smem + NST * STAGE + wave * 256), 4, 0, 0);
-  } else if (tid < BN) {
-    ((float*)(smem + NST * STAGE))[tid] = 0.f;
+    if (group == 0 && wave < BN / 64) __builtin_amdgcn_global_load_lds(BSR_GLOBAL_PTR(g.bias + min(n0 + tid, N - 1)), BSR_LDS_VOID(bias + wave * 64), 4, 0, 0);
+  } else if (group == 0 && tid < BN) {
+    bias[tid] = 0.f;
   }
 #pragma unroll
   for (int j = 0; j < NST; ++j)
@@ -400,10 +409,41 @@ void gemm8_kernel(const void* hA, const void* hB, const void* hsa, const void* h
   } else {
     while (kt + NST < nk) ktile(IC<0>{}, steady);
   }
-  while (kt < nk) ktile(IC<0>{}, IC<-1>{});                       // nothing left to issue
+  if constexpr (KG == 1) {
+    while (kt < nk) ktile(IC<0>{}, IC<-1>{});                     // nothing left to issue
+  } else {
+    static_assert(!LATE, "loads end with the k-tiles that issue them");
+    while (kt < nk - 1) ktile(IC<0>{}, IC<-1>{});
+    if (mine == nk) {
+      kfirst(IC<0>{}, st, 0, 0);
+      widen(IC<1>{});
+      sfor<NMF>([&](auto J) __attribute__((always_inline)) { mf1(IC<1>{}, J); });
+    }
+    // behind the patches of the epilogue: [group - 1][wave][accumulator][16 floats in fours][lane]
+    constexpr int PATCHES = NW * 32 * (TN + 4) * 4, PART = BM * BN * 4;
+    static_assert(PATCHES + (KG - 1) * PART <= KG * NST * STAGE, "the sums of the groups lie in the stages");
+    __syncthreads();
+    auto part = [&](int of, int mi, int ni, int q) __attribute__((always_inline)) {
+      return (f32x4*)(smem_all + PATCHES + (of - 1) * PART) + (((wave * MI + mi) * NI + ni) * 4 + q) * 64 + lane;
+    };
+    if (group > 0)
+      sfor<MI * NI * 4>([&](auto I) __attribute__((always_inline)) {
+        constexpr int q = decltype(I)::value % 4, ni = decltype(I)::value / 4 % NI, mi = decltype(I)::value / 4 / NI;
+        *part(group, mi, ni, q) = f32x4{acc[mi][ni][4 * q], acc[mi][ni][4 * q + 1], acc[mi][ni][4 * q + 2], acc[mi][ni][4 * q + 3]};
+      });
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int of = 1; of < KG; ++of)
+      sfor<MI * NI * 4>([&](auto I) __attribute__((always_inline)) {
+        constexpr int q = decltype(I)::value % 4, ni = decltype(I)::value / 4 % NI, mi = decltype(I)::value / 4 / NI;
+        const f32x4 p = *part(of, mi, ni, q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[mi][ni][4 * q + e] += p[e];
+      });
+  }
   // every wavefront is past the last barrier: the stages are free, a patch of them for each wavefront
-  epilogue8<MI, NI, T, ACT>(g, acc, m0 + wm * TM, n0 + wn * TN, lane, smem + wave * (32 * (TN + 4) * 4),
-                            (const float*)(smem + NST * STAGE) + wn * TN);
+  epilogue8<MI, NI, T, ACT>(g, acc, m0 + wm * TM, n0 + wn * TN, lane, smem_all + wave * (32 * (TN + 4) * 4), bias + wn * TN);
 }
 
 // maximum over lanes l, l ^ 16, l ^ 32, l ^ 48
@@ -599,50 +639,58 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
   }
 }
 
-template <int BM, int BN, int WM, int WN, int NST, typename T, int ACT, bool EXACT>
+template <int BM, int BN, int WM, int WN, int NST, int KG, typename T, int ACT, bool EXACT>
 void launch_tiled(const Gemm8Desc& g, hipStream_t s) {
   constexpr int NT = WM * WN * 64;
-  constexpr size_t stages = lds_of<BM, BN, NT, NST>();
+  constexpr size_t stages = lds_of<BM, BN, NT, NST, KG>();
   static_assert(BN <= NT, "a thread for each column of the bias");
   constexpr size_t patches = (size_t)WM * WN * 32 * (BN / WN + 4) * 4;
   static_assert(patches <= stages && stages <= 160 * 1024, "the epilogue patches live in the stages");
-  auto kern = gemm8_kernel<BM, BN, WM, WN, NST, T, ACT, EXACT>;
+  auto kern = gemm8_kernel<BM, BN, WM, WN, NST, KG, T, ACT, EXACT>;
   static bool attr_set = false;
   if (!attr_set) {
     (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)stages);
     attr_set = true;
   }
   const int tiles = (int)((int64_t)((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN));
-  kern<<<tiles, NT, stages, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, tiles, g);
+  kern<<<tiles, NT * KG, stages, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, tiles, g);
 }
 
-// What a product takes in each block tile, in microseconds: c[0] + rounds (c[1] + c[2] k) + tiles per CU (c[3] + c[4] k), k the k-tiles and rounds the
+// What a product takes in each block tile, in microseconds: c[0] + rounds (c[1] + c[2] k) + tiles per CU (c[3] + c[4] k), k the k-tiles (of a group) and rounds the
 // turns of workgroups that the tiles make over the CUs, `sharing` of them on one at a time.  Least squares over 67 products timed in every tile
 // (65 .. 16384 rows, 128 .. 8192 by 64 .. 8192, in chains of launches), one table for each arithmetic and type of result; the tile that comes out
 // best took 1.01 times as long as the fastest of ten tiles on the mean, 1.20, 1.20 and 1.13 times at worst.
-struct Tile8 { int bm, bn, sharing; float c[5]; };
+// Tiles whose k-tiles `groups` of wavefronts share (fitted over 60 products of up to 8 M results) are for one round of sums of two turns and more: with more tiles the
+// CUs are full without them.  64 x 64 tiles, one group -> shared: 100 x 4096 x 4096 9.7 -> 8.4 us and, to fp32, 15.7 -> 11.6; 64 x 8192 x 1024 15.9 -> 13.5 and
+// 27.7 -> 19.0; over the 60 products 5 % and 7 % on the mean.
+struct Tile8 { int bm, bn, sharing, groups; float c[5]; };
 constexpr Tile8 TILES_FAST[] = {
-    {256, 256, 1, {0.591f, 5.94f, 1.04f, 0.f, 0.544f}},
-    {256, 128, 1, {1.48f, 3.06f, 0.546f, 0.256f, 0.366f}},
-    {128, 128, 2, {2.04f, 0.f, 0.496f, 1.08f, 0.315f}},
-    {128, 64, 2, {1.32f, 1.44f, 0.315f, 0.f, 0.178f}},
-    {64, 64, 3, {1.77f, 0.697f, 0.19f, 0.0343f, 0.137f}}};
+    {256, 256, 1, 1, {0.591f, 5.94f, 1.04f, 0.f, 0.544f}},
+    {256, 128, 1, 1, {1.48f, 3.06f, 0.546f, 0.256f, 0.366f}},
+    {128, 128, 2, 1, {2.04f, 0.f, 0.496f, 1.08f, 0.315f}},
+    {128, 64, 2, 1, {1.32f, 1.44f, 0.315f, 0.f, 0.178f}},
+    {64, 64, 3, 1, {1.77f, 0.697f, 0.19f, 0.0343f, 0.137f}},
+    {64, 64, 1, 2, {0.f, 2.76f, 0.327f, 0.192f, 0.0601f}}};
 constexpr Tile8 TILES_EXACT_BF16[] = {
-    {128, 128, 2, {3.25f, 0.781f, 0.701f, 2.1f, 0.f}},
-    {128, 64, 3, {2.78f, 0.613f, 0.441f, 1.39f, 0.f}},
-    {64, 64, 3, {2.58f, 0.f, 0.358f, 0.651f, 0.112f}}};
+    {128, 128, 2, 1, {3.25f, 0.781f, 0.701f, 2.1f, 0.f}},
+    {128, 64, 3, 1, {2.78f, 0.613f, 0.441f, 1.39f, 0.f}},
+    {64, 64, 3, 1, {2.58f, 0.f, 0.358f, 0.651f, 0.112f}}};
 constexpr Tile8 TILES_EXACT_F32[] = {
-    {128, 128, 2, {1.04f, 3.67f, 0.718f, 0.695f, 0.478f}},
-    {128, 64, 3, {0.876f, 2.71f, 0.462f, 0.154f, 0.342f}},
-    {64, 64, 3, {2.61f, 0.152f, 0.335f, 0.525f, 0.186f}}};
+    {128, 128, 2, 1, {1.04f, 3.67f, 0.718f, 0.695f, 0.478f}},
+    {128, 64, 3, 1, {0.876f, 2.71f, 0.462f, 0.154f, 0.342f}},
+    {64, 64, 3, 1, {2.61f, 0.152f, 0.335f, 0.525f, 0.186f}},
+    {128, 64, 1, 2, {0.f, 3.81f, 0.814f, 0.692f, 0.126f}},
+    {64, 64, 1, 4, {0.f, 3.42f, 0.948f, 0.643f, 0.0971f}}};
 template <int N>
 int pick(const Tile8 (&table)[N], const Gemm8Desc& g) {
-  const float k = (float)((g.K + BLOCK8 - 1) / BLOCK8);
+  const int nk = (g.K + BLOCK8 - 1) / BLOCK8;
   int best = 0;
   float least = 0.f;
   for (int i = 0; i < N; ++i) {
     const Tile8& t = table[i];
     const int64_t tiles = (int64_t)((g.M + t.bm - 1) / t.bm) * ((g.N + t.bn - 1) / t.bn), slots = 256 * t.sharing;
+    if (t.groups > 1 && (tiles > slots || nk < 2 * t.groups)) continue;
+    const float k = (float)((nk + t.groups - 1) / t.groups);
     const float us = t.c[0] + (float)((tiles + slots - 1) / slots) * (t.c[1] + t.c[2] * k) + (float)tiles / 256.f * (t.c[3] + t.c[4] * k);
     if (i == 0 || us < least) { least = us; best = i; }
   }
@@ -653,17 +701,24 @@ template <typename T, int ACT, bool EXACT>
 void tiled(const Gemm8Desc& g, hipStream_t s) {
   if constexpr (!EXACT) {
     switch (pick(TILES_FAST, g)) {
-      case 0: launch_tiled<256, 256, 2, 4, 2, T, ACT, false>(g, s); break;
-      case 1: launch_tiled<256, 128, 4, 2, 3, T, ACT, false>(g, s); break;
-      case 2: launch_tiled<128, 128, 2, 4, 2, T, ACT, false>(g, s); break;
-      case 3: launch_tiled<128, 64, 4, 1, 3, T, ACT, false>(g, s); break;
-      default: launch_tiled<64, 64, 2, 2, 3, T, ACT, false>(g, s); break;
+      case 0: launch_tiled<256, 256, 2, 4, 2, 1, T, ACT, false>(g, s); break;
+      case 1: launch_tiled<256, 128, 4, 2, 3, 1, T, ACT, false>(g, s); break;
+      case 2: launch_tiled<128, 128, 2, 4, 2, 1, T, ACT, false>(g, s); break;
+      case 3: launch_tiled<128, 64, 4, 1, 3, 1, T, ACT, false>(g, s); break;
+      case 4: launch_tiled<64, 64, 2, 2, 3, 1, T, ACT, false>(g, s); break;
+      default: launch_tiled<64, 64, 2, 2, 3, 2, T, ACT, false>(g, s); break;
     }
   } else {
-    switch (g.out_f32 ? pick(TILES_EXACT_F32, g) : pick(TILES_EXACT_BF16, g)) {
-      case 0: launch_tiled<128, 128, 2, 2, 2, T, ACT, true>(g, s); break;
-      case 1: launch_tiled<128, 64, 2, 2, 2, T, ACT, true>(g, s); break;
-      default: launch_tiled<64, 64, 2, 2, 3, T, ACT, true>(g, s); break;
+    const int tile = sizeof(T) == 4 ? pick(TILES_EXACT_F32, g) : pick(TILES_EXACT_BF16, g);
+    switch (tile) {
+      case 0: launch_tiled<128, 128, 2, 2, 2, 1, T, ACT, true>(g, s); break;
+      case 1: launch_tiled<128, 64, 2, 2, 2, 1, T, ACT, true>(g, s); break;
+      case 2: launch_tiled<64, 64, 2, 2, 3, 1, T, ACT, true>(g, s); break;
+      default:
+        if constexpr (sizeof(T) == 4) {                    // (sums for bf16 results are short here)
+          if (tile == 3) launch_tiled<128, 64, 2, 2, 2, 2, T, ACT, true>(g, s);
+          else launch_tiled<64, 64, 2, 2, 2, 4, T, ACT, true>(g, s);
+        }
     }
   }
 }

@@ -268,3 +268,14 @@ def test_refusals(env):
         P.bsr_quantize8_rows(x.half())
     with pytest.raises(P.BsrError):
         P.bsr_linear8_forward(x, layer, act=2)
+
+
+# few tiles and long sums, whose k-tiles several groups of wavefronts share: as many for each, one or more left over, the fewest that are shared
+SHARED = [(33, 400, 64), (40, 897, 70), (64, 1100, 128), (90, 1300, 200), (50, 1920, 96), (130, 2048, 300), (257, 5000, 1030), (512, 4096, 2048)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", SHARED)
+def test_sums_shared_by_groups(env, M, K, N, dtype):
+    test_forward(env, M, K, N, dtype)
+    test_input_gradient(env, M, N, K, dtype)
