@@ -470,7 +470,8 @@ int32_t bsr_attention_backward(const void* qkv, const void* out, const void* dou
  * length) and the first may start anywhere.  Types are BSR_BF16 or BSR_FP32; statistics, sums over rows, products and losses are fp32 inside whatever
  * the type.  Tensors without a stride are aligned to 16 bytes; rows of whole 16-byte pieces on 16-byte boundaries are the fast ones.  Zero rows are no error: nothing is
  * launched but what zeroes a sum over them.  Results are bit-reproducible (no atomics).  All launches go to `stream`, nothing waits.
- * Errors: INVALID_ARG (NULL or misaligned pointer, a negative row count, a length < 1, a stride shorter than a row, an unknown type), HIP.
+ * Limits: rows of up to 2^30 elements, frozen layers of up to 2^23 inputs and outputs.
+ * Errors: INVALID_ARG (NULL or misaligned pointer, a negative row count, a length < 1 or past its limit, a stride shorter than a row, an unknown type), HIP.
  *
  * LayerNorm.
  * bsr_layernorm_forward: y = (x - mean) rstd gamma + beta over rows of D, mean and biased variance per row, rstd = 1 / sqrt(var + eps).

@@ -1758,6 +1758,8 @@ int32_t bsr_destroy(bsr_ctx* c) {
 }
 
 // ---- operators on the caller's own tensors ------------------------------------------------------------------------------------------
+constexpr int32_t LONGEST_ROW = 1 << 30;            // (a kernel's index may run past the end by a workgroup's stride)
+constexpr int32_t WIDEST_LAYER = 1 << 23;           // (offsets of 32 bits within the rows of a block tile)
 static bool known_type(int32_t t) { return t == BSR_BF16 || t == BSR_FP32; }
 // a matrix with a row stride: there, aligned to its elements, rows that do not overlap
 static bool rows_ok(const void* p, int32_t type, int64_t ld, int64_t row) {
@@ -1770,7 +1772,7 @@ size_t bsr_layernorm_workspace_floats(int32_t D) { return D < 1 ? 0 : norm_rows_
 int32_t bsr_layernorm_forward(const void* x, int32_t type, int64_t M, int32_t D, int64_t ldx, const float* gamma, const float* beta, float eps,
                               void* y, int64_t ldy, void* values, uint8_t* scales, float* mean, float* rstd, void* stream) {
   const char* w = "bsr_layernorm_forward";
-  if (!known_type(type) || M < 0 || D < 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, D %d", w, type, (long long)M, D);
+  if (!known_type(type) || M < 0 || D < 1 || D > LONGEST_ROW) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, D %d", w, type, (long long)M, D);
   if (!aligned16(gamma) || !aligned16(beta)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: gamma or beta is NULL or not 16-byte aligned", w);
   if (!(eps >= 0.f)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: eps %g", w, eps);
   if (M == 0) return BSR_OK;                         // (and tensors without elements have no address)
@@ -1790,7 +1792,7 @@ int32_t bsr_layernorm_backward(const void* dy, int64_t lddy, const void* x, int6
                                int32_t D, const float* mean, const float* rstd, const float* gamma, void* dx, int64_t lddx, float* dgamma,
                                float* dbeta, float* workspace, size_t workspace_floats, void* stream) {
   const char* w = "bsr_layernorm_backward";
-  if (!known_type(type) || M < 0 || D < 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, D %d", w, type, (long long)M, D);
+  if (!known_type(type) || M < 0 || D < 1 || D > LONGEST_ROW) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, D %d", w, type, (long long)M, D);
   if (!dgamma != !dbeta || (M > 0 && !dx && !dgamma)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dx, or dgamma and dbeta, or all three", w);
   if (dgamma && (!aligned4(dgamma) || !aligned4(dbeta) || !aligned16(workspace)))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: misaligned dgamma or dbeta, or workspace NULL or not 16-byte aligned", w);
@@ -1815,7 +1817,7 @@ void bsr_block8_strides(int32_t K, int64_t* ldv, int64_t* lds) {
 
 int32_t bsr_quantize8_rows(const void* x, int32_t type, int64_t M, int32_t K, int64_t ldx, void* values, uint8_t* scales, void* stream) {
   const char* w = "bsr_quantize8_rows";
-  if (!known_type(type) || M < 0 || K < 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, K %d", w, type, (long long)M, K);
+  if (!known_type(type) || M < 0 || K < 1 || K > LONGEST_ROW) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, K %d", w, type, (long long)M, K);
   if (M == 0) return BSR_OK;
   if (!rows_ok(x, type, ldx, K)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: x is NULL, misaligned or has rows closer than %d", w, K);
   if (!aligned16(values) || !aligned4(scales)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: values or scales is NULL or misaligned", w);
@@ -1826,7 +1828,8 @@ int32_t bsr_quantize8_rows(const void* x, int32_t type, int64_t M, int32_t K, in
 int32_t bsr_quantize8_weight(const void* weight, int32_t type, int32_t in, int32_t out, int64_t ldw, void* values, uint8_t* scales, void* values_back,
                              uint8_t* scales_back, void* stream) {
   const char* w = "bsr_quantize8_weight";
-  if (!known_type(type) || in < 1 || out < 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, in %d, out %d", w, type, in, out);
+  if (!known_type(type) || in < 1 || out < 1 || in > WIDEST_LAYER || out > WIDEST_LAYER)
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, in %d, out %d (1 .. %d)", w, type, in, out, WIDEST_LAYER);
   if (!rows_ok(weight, type, ldw, out)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: w is NULL, misaligned or has rows closer than %d", w, out);
   if (!aligned16(values) || !aligned4(scales) || !values_back != !scales_back || (values_back && (!aligned16(values_back) || !aligned4(scales_back))))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: values or scales is NULL or misaligned", w);
@@ -1843,8 +1846,8 @@ size_t bsr_linear8_workspace_bytes(int32_t M, int32_t K) {
 static int32_t linear8(const char* w, const void* x, int32_t x_type, int64_t ldx, const uint8_t* x_scales, int32_t M, int32_t K, int32_t N,
                        const void* values, const uint8_t* scales, Gemm8Desc& g, int32_t y_type, void* workspace, size_t workspace_bytes,
                        void* stream) {
-  if (!known_type(y_type) || (!x_scales && !known_type(x_type)) || M < 0 || K < 1 || N < 1)
-    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: types %d and %d, M %d, in or out < 1", w, x_type, y_type, M);
+  if (!known_type(y_type) || (!x_scales && !known_type(x_type)) || M < 0 || M > LONGEST_ROW || K < 1 || N < 1 || K > WIDEST_LAYER || N > WIDEST_LAYER)
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: types %d and %d, M %d, rows of %d and %d (1 .. %d)", w, x_type, y_type, M, K, N, WIDEST_LAYER);
   if (!aligned16(values) || !aligned4(scales)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: values or scales is NULL or misaligned", w);
   if ((g.bias && !aligned4(g.bias)) || (g.aux && !aligned16(g.aux)) || (g.res && !aligned16(g.res)))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: bias, u or res is misaligned", w);
@@ -1891,7 +1894,7 @@ int32_t bsr_linear8_dgrad(const void* dy, int32_t dy_type, int64_t lddy, const u
 static int32_t distill_args(const char* w, DistillArgs& a, const void* z, int32_t type, int64_t rows, int32_t classes, int64_t ldz, const int32_t* index,
                             int64_t ldi, const void* logits, int32_t logits_type, int64_t ldt, int32_t top, const int32_t* labels,
                             float temperature, float hard_weight, const float* row_grad, float grad_scale, void* dz, int64_t ldd) {
-  if (!known_type(type) || !known_type(logits_type) || rows < 0 || rows > INT32_MAX || classes < 1 || top < 1 || top > DISTILL_MAX_TOP)
+  if (!known_type(type) || !known_type(logits_type) || rows < 0 || rows > INT32_MAX || classes < 1 || classes > LONGEST_ROW || top < 1 || top > DISTILL_MAX_TOP)
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: types %d and %d, rows %lld, classes %d, top %d (1 .. %d)", w, type, logits_type, (long long)rows, classes, top,
                 DISTILL_MAX_TOP);
   if (!(temperature > 0.f) || !(temperature <= 3.4e38f) || !(hard_weight >= 0.f && hard_weight <= 1.f))

@@ -17,6 +17,7 @@ namespace bsr {
 namespace {
 
 constexpr int FINAL_WAVES = 16;
+constexpr int64_t ROWS_A_LAUNCH = 1 << 21;                 // (a launch has fewer than 2^32 threads, and a row up to 1024)
 
 // Results go past the caches, a wavefront's store being whole lines (16384 x 8192: forward 130 -> 94 us, backward 174 -> 170; 25216 x 768 backward 32 -> 26)
 // A row lies in chunks of 16 bytes.  WHOLE: it is whole chunks on 16-byte boundaries; otherwise chunks lie at any element's address, and what is left
@@ -498,14 +499,17 @@ void bwd(const NormRowsBwd& a, hipStream_t s) {
     const bool done = whole ? with_row_chunks_of(n, [&](auto TPR, auto C) { shaped(RowC<1>{}, TPR, C); })
                             : a.D >= Chunk<T>::V && with_row_chunks_of(n, [&](auto TPR, auto C) { shaped(RowC<0>{}, TPR, C); });
     if (!done) {
-      if (a.dx)
-        rows_bwd_dx_any_kernel<T><<<(unsigned)((a.M + 3) / 4), 256, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, (const T*)a.res, a.ldr, a.M,
-                                                                          a.D, a.mean, a.rstd, a.gamma, (T*)a.dx, a.lddx);
-      if (params) {
+      if (params) {                                       // (first: dx may take the place of dy)
         const int64_t per_chunk = (a.M + 63) / 64;
         rows = (int)((a.M + per_chunk - 1) / per_chunk);
         rows_bwd_params_any_kernel<T><<<dim3((a.D + WAVE - 1) / WAVE, rows), 256, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.M, a.D,
                                                                                         a.mean, a.rstd, per_chunk, P, a.partial);
+      }
+      for (int64_t m = 0; a.dx && m < a.M; m += ROWS_A_LAUNCH) {
+        const int64_t here = std::min(ROWS_A_LAUNCH, a.M - m);
+        rows_bwd_dx_any_kernel<T><<<(unsigned)((here + 3) / 4), 256, 0, s>>>((const T*)a.dy + m * a.lddy, a.lddy, (const T*)a.x + m * a.ldx, a.ldx,
+                                                                           a.res ? (const T*)a.res + m * a.ldr : nullptr, a.ldr, here, a.D, a.mean + m,
+                                                                           a.rstd + m, a.gamma, (T*)a.dx + m * a.lddx, a.lddx);
       }
     }
   }
@@ -515,14 +519,39 @@ void bwd(const NormRowsBwd& a, hipStream_t s) {
 }  // namespace
 
 void norm_rows_fwd(const NormRows& a, hipStream_t s) {
-  if (a.M <= 0) return;
-  if (a.f32) fwd<float>(a, s);
-  else fwd<bf16>(a, s);
+  const int64_t size = a.f32 ? 4 : 2;
+  for (int64_t m = 0; m < a.M; m += ROWS_A_LAUNCH) {
+    NormRows b = a;
+    b.M = std::min(ROWS_A_LAUNCH, a.M - m);
+    b.x = (const char*)a.x + m * a.ldx * size;
+    if (a.y) b.y = (char*)a.y + m * a.ldy * size;
+    if (a.q) { b.q = (uint8_t*)a.q + m * ld8(a.D); b.scale = a.scale + m * ld8s(a.D); }
+    if (a.mean) b.mean = a.mean + m;
+    if (a.rstd) b.rstd = a.rstd + m;
+    if (a.f32) fwd<float>(b, s);
+    else fwd<bf16>(b, s);
+  }
 }
 
 void norm_rows_bwd(const NormRowsBwd& a, hipStream_t s) {
-  if (a.f32) bwd<float>(a, s);
-  else bwd<bf16>(a, s);
+  const int64_t size = a.f32 ? 4 : 2;
+  if (a.dgamma || a.M <= ROWS_A_LAUNCH) {                  // (with sums the workgroups are few and walk the rows)
+    if (a.f32) bwd<float>(a, s);
+    else bwd<bf16>(a, s);
+    return;
+  }
+  for (int64_t m = 0; m < a.M; m += ROWS_A_LAUNCH) {
+    NormRowsBwd b = a;
+    b.M = std::min(ROWS_A_LAUNCH, a.M - m);
+    b.dy = (const char*)a.dy + m * a.lddy * size;
+    b.x = (const char*)a.x + m * a.ldx * size;
+    if (a.res) b.res = (const char*)a.res + m * a.ldr * size;
+    b.dx = (char*)a.dx + m * a.lddx * size;
+    b.mean = a.mean + m;
+    b.rstd = a.rstd + m;
+    if (a.f32) bwd<float>(b, s);
+    else bwd<bf16>(b, s);
+  }
 }
 
 }  // namespace bsr

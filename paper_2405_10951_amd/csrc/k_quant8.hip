@@ -1,4 +1,6 @@
 // Rows and weight matrices brought to 8 bits (fp8.h).  Bound by memory: 3 bytes move per bf16 element.
+#include <algorithm>
+
 #include "fp8.h"
 
 namespace bsr {
@@ -127,9 +129,12 @@ __global__ __launch_bounds__(256) void quantize8_weight_kernel(const T* __restri
 template <typename T>
 void rows_t(const void* x, int64_t M, int K, int64_t ldx, void* q, uint8_t* scale, hipStream_t s) {
   const int per_row = (int)ld8s(K), real = (int)(ld8(K) / BLOCK8);
-  const int64_t blocks = M * per_row;
-  const unsigned grid = (unsigned)((blocks * 8 + 255) / 256);
-  quantize8_rows_kernel<T><<<grid, 256, 0, s>>>((const T*)x, blocks, K, ldx, per_row, real, (uint8_t*)q, scale);
+  const int64_t step = std::max<int64_t>(1, (int64_t(1) << 28) / per_row);          // (a launch has fewer than 2^32 threads, and a block eight)
+  for (int64_t m = 0; m < M; m += step) {
+    const int64_t blocks = std::min(step, M - m) * per_row;
+    quantize8_rows_kernel<T><<<(unsigned)((blocks * 8 + 255) / 256), 256, 0, s>>>((const T*)x + m * ldx, blocks, K, ldx, per_row, real,
+                                                                                (uint8_t*)q + m * ld8(K), scale + m * per_row);
+  }
 }
 
 }  // namespace

@@ -60,6 +60,23 @@ def test_layernorm(env, D, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", WIDTHS)
+def test_layernorm_gradient_in_place(env, D, dtype):
+    """dx in the place of dy, and of the residual's gradient: the same dx and the same sums"""
+    torch, P = env
+    torch.manual_seed(D + 1)
+    x, dy, res = (torch.randn(41, D, device="cuda").to(types(torch)[dtype]) for _ in range(3))
+    gamma, beta = torch.randn(D, device="cuda"), torch.randn(D, device="cuda")
+    _, mean, rstd = P.bsr_layernorm_forward(x, gamma, beta)
+    want = P.bsr_layernorm_backward(dy, x, mean, rstd, gamma, res=res)
+    for place in (0, 1):
+        mine = [dy.clone(), res.clone()]
+        got = P.bsr_layernorm_backward(mine[0], x, mean, rstd, gamma, res=mine[1], dx=mine[place])
+        assert got[0].data_ptr() == mine[place].data_ptr()
+        assert all(torch.equal(g, w) for g, w in zip(got, want)), "in the place of " + ("dy", "res")[place]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("K", WIDTHS[:12])
 def test_to_8_bits_and_few_rows(env, K, dtype):
     torch, P = env

@@ -88,3 +88,16 @@ def test_the_reference_of_8_bit_blocks():
     assert list(to_e4m3([17.0, 19.0, 21.0, 2 ** -10, 3 * 2 ** -10, -17.0, 448.0, 0.0])) == [16.0, 20.0, 20.0, 0.0, 2 ** -8, -16.0, 448.0, 0.0]
     v, e = blocks8([[896.0, 1.0, 3.1]], 1, 128)
     assert e[0, 0] == 1 and list(v[0]) == [896.0, 1.0, 3.0]
+
+
+BIG, WIDE = (1 << 30) + 1, (1 << 23) + 1
+
+
+@pytest.mark.parametrize("name,good,bad", [
+    ("bsr_layernorm_forward", LN, dict(D=BIG, ldx=BIG, ldy=BIG)), ("bsr_layernorm_backward", LNB, dict(D=BIG, lddy=BIG, ldx=BIG, lddx=BIG, ws_floats=1 << 50)),
+    ("bsr_quantize8_rows", QR, dict(K=BIG, ldx=BIG)), ("bsr_quantize8_weight", QW, dict(n_in=WIDE)), ("bsr_quantize8_weight", QW, dict(n_out=WIDE, ldw=WIDE)),
+    ("bsr_linear8_forward", LF, dict(n_in=WIDE, ldx=WIDE, ws_bytes=1 << 50)), ("bsr_linear8_forward", LF, dict(n_out=WIDE)),
+    ("bsr_linear8_dgrad", LD, dict(n_out=WIDE, lddy=WIDE, ws_bytes=1 << 50)), ("bsr_linear8_dgrad", LD, dict(n_in=WIDE)),
+    ("bsr_distill_forward", DF, dict(classes=BIG, ldz=BIG)), ("bsr_distill_backward", DB, dict(classes=BIG, ldz=BIG, ldd=BIG))])
+def test_lengths_past_their_limits(name, good, bad):
+    test_refused_before_a_launch(name, good, bad)
