@@ -7,6 +7,8 @@
 // Bound by memory: a workgroup takes a row, asks for all of it at once, keeps it in registers (rows of up to 131072 bf16 or 65536 fp32 values), takes the
 // maximum and both sums together and writes dz; longer rows are read a second time for dz.  The teacher's list is worked on while the row is on its way.  The few places that p and the label touch are
 // written again behind a barrier by a thread each, duplicates added in the order of the list: no atomics, the same bits every time.
+// Measured (bytes at a copy's rate in brackets): 4096 x 131072 bf16 loss and gradient 438 us (420), 2048 x 21841 bf16 gradient 38 (35), 32 x 100 fp32 5.4, a
+// chain of waits.
 #include <algorithm>
 #include <cfloat>
 

@@ -12,6 +12,10 @@
 // power of two is one) to 24 bits, at half the rate.  So there are two forms: EXACT brings the operands to bf16 on the way from LDS to the
 // instruction, for fp32 results, and for bf16 results of short sums (K < EXACT_BELOW), where an fp32 sum would be closer than the cut; longer sums for bf16 results
 // take the 8-bit instructions, whose error is then below the bound of an fp32 sum in any order (K 2^-24 sum |a b|) and 60 times below the rounding of the result.
+//
+// Measured, in chains of launches: 8192^3 410 us (2683 TFLOP/s; to fp32 905, 1216), 16384 x 4096 x 8192 434 us (2532; with GELU 480, times GELU' 533), 4096^3 57 us,
+// 6304 x 768 x 2304 15.4, 100 x 4096 x 4096 8.2.  Large products are bound by the card's power (on zeros they run 25 % faster at the same instructions
+// and bytes), short ones by the way into LDS and out of the registers, few rows by the latency of a k-tile.
 #include <algorithm>
 #include <type_traits>
 
@@ -522,7 +526,8 @@ __device__ __forceinline__ i32x8 bytes_down(i32x8 q, int n) {
 // wavefronts share the k-tiles, each with its own straight from global memory into registers (a weight row's 128 bytes of a k-tile are a
 // cache line that four lanes read whole), AHEAD of them asked for before the first is looked at, and their sums meet in LDS in wavefront
 // order.  Rows of bf16 or fp32 are brought to 8 bits here by every workgroup for itself: they are
-// few, and it saves the launch.  Bound by the latency of one trip to memory, then by the weights' bytes.
+// few, and it saves the launch.  Bound by the latency of one trip to memory, then by the weights' bytes:
+// 1 x 4096 x 4096 6.4 us from bf16 and 5.6 from 8-bit rows (the weights' bytes at a copy's rate: 3.3), 1 x 8192 x 8192 16.5 and 14.0 (13.2), 16 x 4096 x 4096 8.4 and 6.8.
 enum { X_E4, X_BF16, X_F32 };                      // type of the rows
 enum { ROWS_WHOLE, ROWS_PART, ROWS_SHORT };        // of whole pieces of 32 values; with a part of one at the end; of less than one
 constexpr int FEW_WAVES = 8, FEW_ROWS = 32;
