@@ -664,7 +664,7 @@ void launch_tiled(const Gemm8Desc& g, hipStream_t s) {
 // What a product takes in each block tile, in microseconds: c[0] + rounds (c[1] + c[2] k) + tiles per CU (c[3] + c[4] k), k the k-tiles (of a group) and rounds the
 // turns of workgroups that the tiles make over the CUs, `sharing` of them on one at a time.  Least squares over 67 products timed in every tile
 // (65 .. 16384 rows, 128 .. 8192 by 64 .. 8192, in chains of launches), one table for each arithmetic and type of result; the tile that comes out
-// best took 1.01 times as long as the fastest of ten tiles on the mean, 1.20, 1.20 and 1.13 times at worst.
+// best took 1.01 times as long as the fastest of ten tiles on the mean, 1.20 times at worst (to fp32 1.13).
 // Tiles whose k-tiles `groups` of wavefronts share (fitted over 60 products of up to 8 M results) are for one round of sums of two turns and more: with more tiles the
 // CUs are full without them.  64 x 64 tiles, one group -> shared: 100 x 4096 x 4096 9.7 -> 8.4 us and, to fp32, 15.7 -> 11.6; 64 x 8192 x 1024 15.9 -> 13.5 and
 // 27.7 -> 19.0; over the 60 products 5 % and 7 % on the mean.
@@ -676,10 +676,10 @@ constexpr Tile8 TILES_FAST[] = {
     {128, 64, 2, 1, {1.32f, 1.44f, 0.315f, 0.f, 0.178f}},
     {64, 64, 3, 1, {1.77f, 0.697f, 0.19f, 0.0343f, 0.137f}},
     {64, 64, 1, 2, {0.f, 2.76f, 0.327f, 0.192f, 0.0601f}}};
-constexpr Tile8 TILES_EXACT_BF16[] = {
-    {128, 128, 2, 1, {3.25f, 0.781f, 0.701f, 2.1f, 0.f}},
-    {128, 64, 3, 1, {2.78f, 0.613f, 0.441f, 1.39f, 0.f}},
-    {64, 64, 3, 1, {2.58f, 0.f, 0.358f, 0.651f, 0.112f}}};
+constexpr Tile8 TILES_EXACT_BF16[] = {                        // (68 products of sums up to 767, with and without a residual: 1.004, 1.09 at worst)
+    {128, 128, 2, 1, {1.25f, 3.19f, 0.715f, 0.613f, 0.339f}},
+    {64, 128, 3, 1, {1.53f, 1.63f, 0.517f, 0.242f, 0.314f}},
+    {64, 64, 3, 1, {2.51f, 0.11f, 0.34f, 0.332f, 0.16f}}};
 constexpr Tile8 TILES_EXACT_F32[] = {
     {128, 128, 2, 1, {1.04f, 3.67f, 0.718f, 0.695f, 0.478f}},
     {128, 64, 3, 1, {0.876f, 2.71f, 0.462f, 0.154f, 0.342f}},
@@ -714,16 +714,20 @@ void tiled(const Gemm8Desc& g, hipStream_t s) {
       default: launch_tiled<64, 64, 2, 2, 3, 2, T, ACT, false>(g, s); break;
     }
   } else {
-    const int tile = sizeof(T) == 4 ? pick(TILES_EXACT_F32, g) : pick(TILES_EXACT_BF16, g);
-    switch (tile) {
-      case 0: launch_tiled<128, 128, 2, 2, 2, 1, T, ACT, true>(g, s); break;
-      case 1: launch_tiled<128, 64, 2, 2, 2, 1, T, ACT, true>(g, s); break;
-      case 2: launch_tiled<64, 64, 2, 2, 3, 1, T, ACT, true>(g, s); break;
-      default:
-        if constexpr (sizeof(T) == 4) {                    // (sums for bf16 results are short here)
-          if (tile == 3) launch_tiled<128, 64, 2, 2, 2, 2, T, ACT, true>(g, s);
-          else launch_tiled<64, 64, 2, 2, 2, 4, T, ACT, true>(g, s);
-        }
+    if constexpr (sizeof(T) == 2) {
+      switch (pick(TILES_EXACT_BF16, g)) {
+        case 0: launch_tiled<128, 128, 2, 2, 2, 1, T, ACT, true>(g, s); break;
+        case 1: launch_tiled<64, 128, 2, 2, 2, 1, T, ACT, true>(g, s); break;
+        default: launch_tiled<64, 64, 2, 2, 2, 1, T, ACT, true>(g, s); break;
+      }
+    } else {
+      switch (pick(TILES_EXACT_F32, g)) {
+        case 0: launch_tiled<128, 128, 2, 2, 2, 1, T, ACT, true>(g, s); break;
+        case 1: launch_tiled<128, 64, 2, 2, 2, 1, T, ACT, true>(g, s); break;
+        case 2: launch_tiled<64, 64, 2, 2, 3, 1, T, ACT, true>(g, s); break;
+        case 3: launch_tiled<128, 64, 2, 2, 2, 2, T, ACT, true>(g, s); break;
+        default: launch_tiled<64, 64, 2, 2, 2, 4, T, ACT, true>(g, s); break;
+      }
     }
   }
 }
