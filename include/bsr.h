@@ -54,6 +54,7 @@ enum {
 };
 
 enum { BSR_BF16 = 0, BSR_FP32 = 1 };          /* activation / compute dtype                       */
+enum { BSR_SUMS_CUT = 256 };                  /* beside BSR_BF16 as the type of bsr_linear8_*'s result: see there */
 enum { BSR_LOSS_CE = 0, BSR_LOSS_MEAN_SQ = 1 }; /* cross-entropy on the head, or mean of squared
                                                    outputs of the last block (no head)            */
 
@@ -509,9 +510,13 @@ int32_t bsr_layernorm_backward(const void* dy, int64_t lddy, const void* x, int6
  *   values, scales  the layer
  *   bias          fp32 [out], may be NULL;  act 0: none, 1: exact-erf GELU
  *   u_out, res, y [M,out] of y_type, contiguous; u_out (the pre-activation, act = 1) and res may be NULL
+ *   y_type        BSR_BF16 or BSR_FP32: the products are exact and added in fp32.  BSR_BF16 | BSR_SUMS_CUT lets the 8-bit matrix instructions add them, at about
+ *                 twice the rate where sums are long: of the eight or so products that these add at a time, what lies below 2^-13 of the largest is cut, so an element may be off by
+ *                 2^-6 of the largest |x w| of each block of 128 columns (by 3e-5 of its size on random data; where outliers cancel, by all that is left).
+ *                 A value of x or W that rounds to 2^128 in 8 bits counts as infinite.
  * bsr_linear8_dgrad: dx[M,in] = dy[M,out] . W^T, optionally times GELU'(u) element-wise; values, scales are the layer's values_back, scales_back
  *   dy            as x above, of `out` columns;  workspace: bsr_linear8_workspace_bytes(M, out)
- *   u, dx         [M,in] of dx_type, contiguous; u may be NULL
+ *   u, dx         [M,in] of dx_type (as y_type), contiguous; u may be NULL
  */
 void bsr_block8_strides(int32_t K, int64_t* ldv, int64_t* lds);
 int32_t bsr_quantize8_rows(const void* x, int32_t type, int64_t M, int32_t K, int64_t ldx, void* values, uint8_t* scales, void* stream);

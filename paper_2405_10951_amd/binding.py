@@ -8,6 +8,7 @@ import os
 
 MAX_BLOCKS = 16
 BSR_BF16, BSR_FP32 = 0, 1
+BSR_SUMS_CUT = 256
 BSR_LOSS_CE, BSR_LOSS_MEAN_SQ = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -518,9 +519,19 @@ def _linear8_out(x, t, y, what, shape, out_dtype):
     return y
 
 
-def bsr_linear8_forward(x, w: Weight8, bias=None, act=0, u_out=None, res=None, y=None, out_dtype=None):
+def _linear8_type(t, what, cut_sums):
+    """The result's type code, with how its sums are held."""
+    code = _type_code(t, what)
+    if not cut_sums:
+        return code
+    if code != BSR_BF16:
+        raise ValueError(f"cut_sums: {what} in bfloat16 is needed, got {t.dtype}")
+    return code | BSR_SUMS_CUT
+
+
+def bsr_linear8_forward(x, w: Weight8, bias=None, act=0, u_out=None, res=None, y=None, out_dtype=None, cut_sums=False):
     """x [M,in] (Rows8, or bf16 / fp32 with any row stride) -> y [M,out] = act(x W + bias) (+ res), of out_dtype (that of x, bf16 for Rows8).
-    act 1: GELU, u_out [M,out] receives its input."""
+    act 1: GELU, u_out [M,out] receives its input.  cut_sums: faster sums of fewer bits for a bf16 result (BSR_SUMS_CUT in bsr.h)."""
     t, M, rows, ws, size, stream = _linear8(x, w.n_in, "x", w.values, bias, u_out, res, y)
     shape = (M, w.n_out)
     y = _linear8_out(x, t, y, "y", shape, out_dtype)
@@ -530,12 +541,13 @@ def bsr_linear8_forward(x, w: Weight8, bias=None, act=0, u_out=None, res=None, y
     pu = None if u_out is None else _flat(u_out, "u_out", shape, y.dtype)
     pr = None if res is None else _flat(res, "res", shape, y.dtype)
     _check(load_library().bsr_linear8_forward(*rows, M, w.n_in, w.n_out, w.values.data_ptr(), w.scales.data_ptr(), _dp(bias), act, pu, pr,
-                                              _flat(y, "y", shape, y.dtype), _type_code(y, "y"), _dp(ws), size, stream))
+                                              _flat(y, "y", shape, y.dtype), _linear8_type(y, "y", cut_sums), _dp(ws), size, stream))
     return y
 
 
-def bsr_linear8_dgrad(dy, w: Weight8, u=None, dx=None, out_dtype=None):
-    """dy [M,out] (Rows8, or bf16 / fp32 with any row stride) -> dx [M,in] = dy W^T, times GELU'(u) where u [M,in] is given."""
+def bsr_linear8_dgrad(dy, w: Weight8, u=None, dx=None, out_dtype=None, cut_sums=False):
+    """dy [M,out] (Rows8, or bf16 / fp32 with any row stride) -> dx [M,in] = dy W^T, times GELU'(u) where u [M,in] is given.  cut_sums: as in
+    bsr_linear8_forward."""
     if w.values_back is None:
         raise ValueError("the layer was laid out without backward")
     t, M, rows, ws, size, stream = _linear8(dy, w.n_out, "dy", w.values_back, u, dx)
@@ -543,7 +555,7 @@ def bsr_linear8_dgrad(dy, w: Weight8, u=None, dx=None, out_dtype=None):
     dx = _linear8_out(dy, t, dx, "dx", shape, out_dtype)
     pu = None if u is None else _flat(u, "u", shape, dx.dtype)
     _check(load_library().bsr_linear8_dgrad(*rows, M, w.n_in, w.n_out, w.values_back.data_ptr(), w.scales_back.data_ptr(), pu,
-                                            _flat(dx, "dx", shape, dx.dtype), _type_code(dx, "dx"), _dp(ws), size, stream))
+                                            _flat(dx, "dx", shape, dx.dtype), _linear8_type(dx, "dx", cut_sums), _dp(ws), size, stream))
     return dx
 
 

@@ -1846,6 +1846,8 @@ size_t bsr_linear8_workspace_bytes(int32_t M, int32_t K) {
 static int32_t linear8(const char* w, const void* x, int32_t x_type, int64_t ldx, const uint8_t* x_scales, int32_t M, int32_t K, int32_t N,
                        const void* values, const uint8_t* scales, Gemm8Desc& g, int32_t y_type, void* workspace, size_t workspace_bytes,
                        void* stream) {
+  const bool cut = y_type == (BSR_BF16 | BSR_SUMS_CUT);
+  if (cut) y_type = BSR_BF16;
   if (!known_type(y_type) || (!x_scales && !known_type(x_type)) || M < 0 || M > LONGEST_ROW || K < 1 || N < 1 || K > WIDEST_LAYER || N > WIDEST_LAYER)
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: types %d and %d, M %d, rows of %d and %d (1 .. %d)", w, x_type, y_type, M, K, N, WIDEST_LAYER);
   if (!aligned16(values) || !aligned4(scales)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: values or scales is NULL or misaligned", w);
@@ -1855,7 +1857,7 @@ static int32_t linear8(const char* w, const void* x, int32_t x_type, int64_t ldx
   if (!aligned16(g.C)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: the result is NULL or not 16-byte aligned", w);
   if (x_scales ? !aligned16(x) || !aligned4(x_scales) : !rows_ok(x, x_type, ldx, K))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: the rows are NULL, misaligned or closer than %d", w, K);
-  g.M = M; g.K = K; g.N = N; g.ldc = N; g.out_f32 = y_type == BSR_FP32;
+  g.M = M; g.K = K; g.N = N; g.ldc = N; g.out_f32 = y_type == BSR_FP32; g.cut = cut;
   g.A = x; g.a_scale = x_scales; g.B = values; g.b_scale = scales;
   if (!x_scales && gemm8_few_takes(M)) {
     g.a_type = x_type == BSR_FP32 ? 1 : 0;

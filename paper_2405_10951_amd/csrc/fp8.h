@@ -46,6 +46,7 @@ struct Gemm8Desc {
   int64_t lda = 0;                 // elements between rows of A (few-row form with a_type other than 8 bits)
   int a_type = 2;                  // 0 bf16, 1 fp32 (few-row form: brought to 8 bits on the way in), 2 e4m3
   bool out_f32 = false;            // type of C, res and aux: fp32, else bf16; all of row stride ldc
+  bool cut = false;                // bf16 results: the 8-bit instructions may add the products (k_gemm8.hip: what that cuts)
   void* C = nullptr; int64_t ldc = 0;
   const float* bias = nullptr;     // [N]
   int act = 0;                     // Act

@@ -8,14 +8,17 @@
 //
 // How exactly that adds up (measured, one large product among small ones in an instruction): of the products that the 8-bit instructions add at
 // a time, those smaller than 2^-13 of the largest are cut to nothing and the others to that place; between such groups, and to the accumulator, the sum is fp32.
-// The result is off by about 3e-5 of its size, whatever K.  The bf16 instructions add the same products (exact in bf16: an e4m3 value times a
-// power of two is one) to 24 bits, at half the rate.  So there are two forms: EXACT brings the operands to bf16 on the way from LDS to the
-// instruction, for fp32 results, and for bf16 results of short sums (K < EXACT_BELOW), where an fp32 sum would be closer than the cut; longer sums for bf16 results
-// take the 8-bit instructions, whose error is then below the bound of an fp32 sum in any order (K 2^-24 sum |a b|) and 60 times below the rounding of the result.
+// On random operands the result is off by about 3e-5 of its size, whatever K, but one outlier takes up to all of its group's small products with it: where two
+// outliers cancel, what is left may be gone.  An element can be off by 2^-13 of the largest product for each product, 2^-6 of the largest in each block of
+// 128.  The bf16 instructions add the same products (exact in bf16: an e4m3 value times a power of two is one, but for a value that rounds to
+// 2^128, which is infinite there) to 24 bits, at half the rate.  So there are two forms: EXACT brings the operands to bf16 on the way from LDS to the instruction, and is what
+// runs unless the caller chose the other one (BSR_SUMS_CUT, for bf16 results: 16384 x 4096 x 8192 434 us against 909, 6304 x 768 x 2304 15.3 against 25.6).  Few rows
+// have the exact form alone, trips to memory being what they wait for: 1 x 4096 x 4096 5.5 us against 5.7 from 8-bit rows and 6.5 against 6.3 from bf16.
 //
-// Measured, in chains of launches: 8192^3 410 us (2683 TFLOP/s; to fp32 905, 1216), 16384 x 4096 x 8192 434 us (2532; with GELU 480, times GELU' 533), 4096^3 57 us,
-// 6304 x 768 x 2304 15.4, 100 x 4096 x 4096 8.2.  Large products are bound by the card's power (on zeros they run 25 % faster at the same instructions
-// and bytes), short ones by the way into LDS and out of the registers, few rows by the latency of a k-tile.
+// Measured, in chains of launches, exact and cut: 8192^3 893 us (1231 TFLOP/s; to fp32 900) and 409 (2688), 16384 x 4096 x 8192 909 (with GELU 958) and
+// 434 (479), 4096^3 117 and 57, 6304 x 768 x 2304 25.6 and 15.3, 100 x 4096 x 4096 11.4 and 8.2.  Large cut products are bound by the card's power (on zeros they run 25 %
+// faster at the same instructions and bytes), large exact ones reach 86 % of the rate of the library's largest bf16 product, the conversions standing in front of the products;
+// short ones are bound by the way into LDS and out of the registers, few rows by the latency of a k-tile.
 #include <algorithm>
 #include <type_traits>
 
@@ -152,9 +155,6 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
     fence();
   }
 }
-
-constexpr int EXACT_BELOW = 768;
-static_assert(EXACT_BELOW >= 32, "rows shorter than a piece have the exact form alone");
 
 // eight e4m3 values (two dwords) times the power of two whose E8M0 byte is s8: exact in bf16
 __device__ __forceinline__ bf16x8 widen8(int lo, int hi, int s8) {
@@ -527,11 +527,11 @@ __device__ __forceinline__ i32x8 bytes_down(i32x8 q, int n) {
 // cache line that four lanes read whole), AHEAD of them asked for before the first is looked at, and their sums meet in LDS in wavefront
 // order.  Rows of bf16 or fp32 are brought to 8 bits here by every workgroup for itself: they are
 // few, and it saves the launch.  Bound by the latency of one trip to memory, then by the weights' bytes:
-// 1 x 4096 x 4096 6.4 us from bf16 and 5.6 from 8-bit rows (the weights' bytes at a copy's rate: 3.3), 1 x 8192 x 8192 16.5 and 14.0 (13.2), 16 x 4096 x 4096 8.4 and 6.8.
+// 1 x 4096 x 4096 6.5 us from bf16 and 5.5 from 8-bit rows (the weights' bytes at a copy's rate: 3.3), 1 x 8192 x 8192 17.6 and 13.9 (13.2), 16 x 4096 x 4096 8.6 and 6.8.
 enum { X_E4, X_BF16, X_F32 };                      // type of the rows
 enum { ROWS_WHOLE, ROWS_PART, ROWS_SHORT };        // of whole pieces of 32 values; with a part of one at the end; of less than one
 constexpr int FEW_WAVES = 8, FEW_ROWS = 32;
-template <int X, int MI, bool EXACT, int ROWS>
+template <int X, int MI, int ROWS>
 __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void* hA, const void* hB, const void* hsa, const void* hsb, int hM, int hN,
                                                                       int hK, int64_t lda, Gemm8Desc g) {
   typedef typename std::conditional<X == X_F32, float, bf16>::type TX;
@@ -604,13 +604,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
             s8 = quantize32<TX>(v, x);
           }
         }
-        if constexpr (EXACT) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            acc[mi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[a][2 * q], w[a][2 * q + 1], ws[a]), widen8(x[2 * q], x[2 * q + 1], s8), acc[mi], 0, 0, 0);
-        } else {
-          acc[mi] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[a], x, acc[mi], 0, 0, 0, ws[a], 0, s8);
-        }
+        for (int q = 0; q < 4; ++q)
+          acc[mi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[a][2 * q], w[a][2 * q + 1], ws[a]), widen8(x[2 * q], x[2 * q + 1], s8), acc[mi], 0, 0, 0);
       }
     }
   }
@@ -666,20 +662,22 @@ void launch_tiled(const Gemm8Desc& g, hipStream_t s) {
 // (65 .. 16384 rows, 128 .. 8192 by 64 .. 8192, in chains of launches), one table for each arithmetic and type of result; the tile that comes out
 // best took 1.01 times as long as the fastest of ten tiles on the mean, 1.20 times at worst (to fp32 1.13).
 // Tiles whose k-tiles `groups` of wavefronts share (fitted over 60 products of up to 8 M results) are for one round of sums of two turns and more: with more tiles the
-// CUs are full without them.  64 x 64 tiles, one group -> shared: 100 x 4096 x 4096 9.7 -> 8.4 us and, to fp32, 15.7 -> 11.6; 64 x 8192 x 1024 15.9 -> 13.5 and
-// 27.7 -> 19.0; over the 60 products 5 % and 7 % on the mean.
+// CUs are full without them.  64 x 64 tiles, one group -> shared: 100 x 4096 x 4096 9.7 -> 8.4 us cut, 15.0 -> 11.6 exact and, to fp32, 15.7 -> 11.6; 64 x 8192 x 1024 15.9 -> 13.5 cut
+// and 27.7 -> 19.0 to fp32; over the 60 products 5 % and 7 % on the mean.
 struct Tile8 { int bm, bn, sharing, groups; float c[5]; };
-constexpr Tile8 TILES_FAST[] = {
+constexpr Tile8 TILES_CUT[] = {
     {256, 256, 1, 1, {0.591f, 5.94f, 1.04f, 0.f, 0.544f}},
     {256, 128, 1, 1, {1.48f, 3.06f, 0.546f, 0.256f, 0.366f}},
     {128, 128, 2, 1, {2.04f, 0.f, 0.496f, 1.08f, 0.315f}},
     {128, 64, 2, 1, {1.32f, 1.44f, 0.315f, 0.f, 0.178f}},
     {64, 64, 3, 1, {1.77f, 0.697f, 0.19f, 0.0343f, 0.137f}},
     {64, 64, 1, 2, {0.f, 2.76f, 0.327f, 0.192f, 0.0601f}}};
-constexpr Tile8 TILES_EXACT_BF16[] = {                        // (68 products of sums up to 767, with and without a residual: 1.004, 1.09 at worst)
-    {128, 128, 2, 1, {1.25f, 3.19f, 0.715f, 0.613f, 0.339f}},
-    {64, 128, 3, 1, {1.53f, 1.63f, 0.517f, 0.242f, 0.314f}},
-    {64, 64, 3, 1, {2.51f, 0.11f, 0.34f, 0.332f, 0.16f}}};
+constexpr Tile8 TILES_EXACT_BF16[] = {                        // (106 products of 64 .. 7430 by 64 .. 8192: 1.01, 1.11 at worst)
+    {128, 128, 2, 1, {1.87f, 2.09f, 0.685f, 0.683f, 0.447f}},
+    {64, 128, 3, 1, {1.49f, 1.17f, 0.526f, 0.517f, 0.264f}},
+    {64, 64, 3, 1, {2.05f, 0.334f, 0.362f, 0.356f, 0.154f}},
+    {128, 64, 1, 2, {0.f, 3.52f, 0.821f, 0.f, 0.199f}},
+    {64, 64, 1, 4, {3.22f, 0.f, 0.957f, 0.f, 0.186f}}};
 constexpr Tile8 TILES_EXACT_F32[] = {
     {128, 128, 2, 1, {1.04f, 3.67f, 0.718f, 0.695f, 0.478f}},
     {128, 64, 3, 1, {0.876f, 2.71f, 0.462f, 0.154f, 0.342f}},
@@ -705,7 +703,7 @@ int pick(const Tile8 (&table)[N], const Gemm8Desc& g) {
 template <typename T, int ACT, bool EXACT>
 void tiled(const Gemm8Desc& g, hipStream_t s) {
   if constexpr (!EXACT) {
-    switch (pick(TILES_FAST, g)) {
+    switch (pick(TILES_CUT, g)) {
       case 0: launch_tiled<256, 256, 2, 4, 2, 1, T, ACT, false>(g, s); break;
       case 1: launch_tiled<256, 128, 4, 2, 3, 1, T, ACT, false>(g, s); break;
       case 2: launch_tiled<128, 128, 2, 4, 2, 1, T, ACT, false>(g, s); break;
@@ -718,7 +716,9 @@ void tiled(const Gemm8Desc& g, hipStream_t s) {
       switch (pick(TILES_EXACT_BF16, g)) {
         case 0: launch_tiled<128, 128, 2, 2, 2, 1, T, ACT, true>(g, s); break;
         case 1: launch_tiled<64, 128, 2, 2, 2, 1, T, ACT, true>(g, s); break;
-        default: launch_tiled<64, 64, 2, 2, 2, 1, T, ACT, true>(g, s); break;
+        case 2: launch_tiled<64, 64, 2, 2, 2, 1, T, ACT, true>(g, s); break;
+        case 3: launch_tiled<128, 64, 2, 2, 2, 2, T, ACT, true>(g, s); break;
+        default: launch_tiled<64, 64, 2, 2, 2, 4, T, ACT, true>(g, s); break;
       }
     } else {
       switch (pick(TILES_EXACT_F32, g)) {
@@ -732,24 +732,23 @@ void tiled(const Gemm8Desc& g, hipStream_t s) {
   }
 }
 
-template <int X, bool EXACT, int ROWS>
+template <int X, int ROWS>
 void few_as(const Gemm8Desc& g, hipStream_t s) {
   const unsigned grid = (unsigned)((g.N + 15) / 16);
   auto go = [&](auto MI) {
-    gemm8_few_kernel<X, decltype(MI)::value, EXACT, ROWS><<<grid, FEW_WAVES * 64, 0, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, g.lda, g);
+    gemm8_few_kernel<X, decltype(MI)::value, ROWS><<<grid, FEW_WAVES * 64, 0, s>>>(g.A, g.B, g.a_scale, g.b_scale, g.M, g.N, g.K, g.lda, g);
   };
   if (g.M <= 16) go(IC<1>{});
   else go(IC<2>{});
 }
-template <bool EXACT>
 void few(const Gemm8Desc& g, hipStream_t s) {
   auto of = [&](auto X) {
     constexpr int x = decltype(X)::value;
-    if (g.K % 32 == 0) few_as<x, EXACT, ROWS_WHOLE>(g, s);
-    else if (g.K > 32) few_as<x, EXACT, ROWS_PART>(g, s);
-    else if constexpr (EXACT) few_as<x, EXACT, ROWS_SHORT>(g, s);          // (short sums are)
+    if (g.K % 32 == 0) few_as<x, ROWS_WHOLE>(g, s);
+    else if (g.K > 32) few_as<x, ROWS_PART>(g, s);
+    else few_as<x, ROWS_SHORT>(g, s);
   };
-  if (g.a_type == 2) few_as<X_E4, EXACT, ROWS_WHOLE>(g, s);
+  if (g.a_type == 2) few_as<X_E4, ROWS_WHOLE>(g, s);
   else if (g.a_type == 1) of(IC<X_F32>{});
   else of(IC<X_BF16>{});
 }
@@ -767,11 +766,10 @@ bool gemm8_few_takes(int64_t M) { return M <= FEW_ROWS; }
 
 void gemm8(const Gemm8Desc& g, hipStream_t s) {
   if (g.M <= 0) return;
-  const bool exact = g.out_f32 || g.K < EXACT_BELOW;
-  if (g.M <= FEW_ROWS) exact ? few<true>(g, s) : few<false>(g, s);
+  if (g.M <= FEW_ROWS) few(g, s);
   else if (g.out_f32) tiled_act<float, true>(g, s);
-  else if (exact) tiled_act<bf16, true>(g, s);
-  else tiled_act<bf16, false>(g, s);
+  else if (g.cut) tiled_act<bf16, false>(g, s);
+  else tiled_act<bf16, true>(g, s);
 }
 
 }  // namespace bsr

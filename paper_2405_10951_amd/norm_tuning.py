@@ -25,10 +25,12 @@ EPS = 1e-6
 
 class FrozenStack:
     """`weights`: [(fc1 [width,hidden], b1 [hidden], fc2 [hidden,width], b2 [width]) per block] and (head [width,classes], bias [classes]);
-    matrices bf16 or fp32, biases fp32, all on one GPU.  `norms`: [gamma, beta] per block and of the final LayerNorm, fp32, learned."""
+    matrices bf16 or fp32, biases fp32, all on one GPU.  `norms`: [gamma, beta] per block and of the final LayerNorm, fp32, learned.
+    cut_sums: the products' sums faster and of fewer bits."""
 
-    def __init__(self, blocks, head):
+    def __init__(self, blocks, head, cut_sums=False):
         import torch
+        self.sums = dict(cut_sums=cut_sums)
         self.blocks = [(P.bsr_quantize8_weight(fc1), b1, P.bsr_quantize8_weight(fc2), b2) for fc1, b1, fc2, b2 in blocks]
         self.head, self.head_bias = P.bsr_quantize8_weight(head[0]), head[1]
         width = self.head.n_in
@@ -41,23 +43,23 @@ class FrozenStack:
         for (fc1, b1, fc2, b2), (gamma, beta) in zip(self.blocks, self.norms):
             h, mean, rstd = P.bsr_layernorm_forward8(x, gamma, beta, EPS)
             u = torch.empty((x.shape[0], fc1.n_out), dtype=x.dtype, device=x.device)
-            g = P.bsr_linear8_forward(h, fc1, bias=b1, act=1, u_out=u, out_dtype=x.dtype)
+            g = P.bsr_linear8_forward(h, fc1, bias=b1, act=1, u_out=u, out_dtype=x.dtype, **self.sums)
             kept.append((x, mean, rstd, u))
-            x = P.bsr_linear8_forward(g, fc2, bias=b2, res=x)
+            x = P.bsr_linear8_forward(g, fc2, bias=b2, res=x, **self.sums)
         h, mean, rstd = P.bsr_layernorm_forward8(x, *self.norms[-1], EPS)
         kept.append((x, mean, rstd, None))
-        return P.bsr_linear8_forward(h, self.head, bias=self.head_bias, out_dtype=x.dtype), kept
+        return P.bsr_linear8_forward(h, self.head, bias=self.head_bias, out_dtype=x.dtype, **self.sums), kept
 
     def backward(self, dlogits, kept):
         """-> [[dgamma, dbeta] per norm]"""
         grads = []
         x, mean, rstd, _ = kept[-1]
-        dx, *grad = P.bsr_layernorm_backward(P.bsr_linear8_dgrad(dlogits, self.head), x, mean, rstd, self.norms[-1][0])
+        dx, *grad = P.bsr_layernorm_backward(P.bsr_linear8_dgrad(dlogits, self.head, **self.sums), x, mean, rstd, self.norms[-1][0])
         grads.append(grad)
         for i in reversed(range(len(self.blocks))):
             fc1, _, fc2, _ = self.blocks[i]
             x, mean, rstd, u = kept[i]
-            dh = P.bsr_linear8_dgrad(P.bsr_linear8_dgrad(dx, fc2, u=u), fc1)
+            dh = P.bsr_linear8_dgrad(P.bsr_linear8_dgrad(dx, fc2, u=u, **self.sums), fc1, **self.sums)
             dx, *grad = P.bsr_layernorm_backward(dh, x, mean, rstd, self.norms[i][0], res=dx if i else None, need_dx=i > 0)
             grads.append(grad)
         return grads[::-1]
@@ -75,7 +77,7 @@ class FrozenStack:
         return loss, grads
 
 
-def random_stack(width, hidden, depth, classes, seed=0, device="cuda"):
+def random_stack(width, hidden, depth, classes, seed=0, device="cuda", cut_sums=False):
     """A stack of random frozen matrices, scaled as trained ones are."""
     import torch
     gen = torch.Generator(device=device).manual_seed(seed)
@@ -85,7 +87,7 @@ def random_stack(width, hidden, depth, classes, seed=0, device="cuda"):
 
     blocks = [(normal(width, hidden, scale=width ** -0.5, dtype=torch.bfloat16), normal(hidden, scale=0.1),
                normal(hidden, width, scale=hidden ** -0.5, dtype=torch.bfloat16), normal(width, scale=0.1)) for _ in range(depth)]
-    return FrozenStack(blocks, (normal(width, classes, scale=2 * width ** -0.5, dtype=torch.bfloat16), torch.zeros(classes, device=device)))
+    return FrozenStack(blocks, (normal(width, classes, scale=2 * width ** -0.5, dtype=torch.bfloat16), torch.zeros(classes, device=device)), cut_sums)
 
 
 def main():
@@ -94,8 +96,9 @@ def main():
     for name, default in (("rows", 6304), ("width", 768), ("hidden", 1536), ("depth", 4), ("classes", 1000), ("top", 16), ("steps", 60)):
         ap.add_argument("--" + name, type=int, default=default)
     ap.add_argument("--lr", type=float, default=2.0)
+    ap.add_argument("--cut-sums", action="store_true", help="let the 8-bit matrix instructions add the products")
     a = ap.parse_args()
-    student, teacher = (random_stack(a.width, a.hidden, a.depth, a.classes) for _ in range(2))
+    student, teacher = (random_stack(a.width, a.hidden, a.depth, a.classes, cut_sums=a.cut_sums) for _ in range(2))
     gen = torch.Generator(device="cuda").manual_seed(1)
     for gamma, beta in teacher.norms:                      # the same frozen matrices under other norms
         gamma.add_(torch.randn(a.width, generator=gen, device="cuda"), alpha=0.3)

@@ -101,3 +101,10 @@ BIG, WIDE = (1 << 30) + 1, (1 << 23) + 1
     ("bsr_distill_forward", DF, dict(classes=BIG, ldz=BIG)), ("bsr_distill_backward", DB, dict(classes=BIG, ldz=BIG, ldd=BIG))])
 def test_lengths_past_their_limits(name, good, bad):
     test_refused_before_a_launch(name, good, bad)
+
+
+@pytest.mark.parametrize("name,good,bad", [("bsr_linear8_forward", LF, dict(y_type=1 | 256)), ("bsr_linear8_dgrad", LD, dict(dx_type=1 | 256)),
+                                           ("bsr_linear8_forward", LF, dict(x_type=256)), ("bsr_linear8_forward", LF, dict(y_type=2 | 256))])
+def test_cut_sums_are_for_bf16_results(name, good, bad):
+    assert P.BSR_SUMS_CUT == 256
+    test_refused_before_a_launch(name, good, bad)
