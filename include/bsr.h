@@ -537,8 +537,8 @@ int32_t bsr_linear8_dgrad(const void* dy, int32_t dy_type, int64_t lddy, const u
  *   loss = (1 - a) T^2 sum_j p_j (log p_j - log q_{c_j}) + a (-log r_label)
  *   dz_v = g ((1 - a) T (q_v - sum_{j: c_j = v} p_j) + a (r_v - [v = label])),   g = grad_scale * row_grad[row]
  * An entry whose class lies outside 0 .. classes-1 is absent, one whose logit is -inf has p = 0; a row without entries of p > 0 lacks the first part, one
- * whose label lies outside 0 .. classes-1 the second; a row whose logits are all -inf has loss and gradient 0.  A class with z = -inf that the teacher
- * gives weight makes the loss +inf and leaves the gradient finite.  NaN and +inf in z make a row NaN.
+ * whose label lies outside 0 .. classes-1 the second; at a = 1 every row lacks the first (the entries are not read), at a = 0 the second.  A row whose logits are all -inf has loss
+ * and gradient 0.  A class with z = -inf that the teacher gives weight (at a < 1) makes the loss +inf and leaves the gradient finite.  NaN and +inf in z make a row NaN.
  *   z            [rows, classes] of `type`, stride ldz
  *   index        int32 [rows, top], stride ldi: c_j;  top <= 1024
  *   logits       [rows, top] of logits_type, stride ldt: t_j

@@ -3,7 +3,8 @@
 //   p = softmax(t / T) over the entries,  q = softmax(z / T),  r = softmax(z)
 //   L = (1 - a) T^2 sum_j p_j (log p_j - log q_{c_j}) + a (-log r_label)
 //   dL/dz_v = (1 - a) T (q_v - sum_{j: c_j = v} p_j) + a (r_v - [v = label])
-// A row without entries lacks the first part, one without a label the second; one whose logits are all -inf has loss and gradient 0.
+// A row without entries lacks the first part, one without a label the second; one whose logits are all -inf has loss and gradient 0.  At a = 1 no row has the first part, and the
+// list is not looked at: the student may give a class of it no weight at all, and 0 times that infinity is no loss.
 // Bound by memory: a workgroup takes a row, asks for all of it at once, keeps it in registers (rows of up to 131072 bf16 or 65536 fp32 values), takes the
 // maximum and both sums together and writes dz; longer rows are read a second time for dz.  The teacher's list is worked on while the row is on its way.  The few places that p and the label touch are
 // written again behind a barrier by a thread each, duplicates added in the order of the list: no atomics, the same bits every time.
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   float* lp = (float*)(li + a.k);                   // [k] first t, then p
   float* lz = lp + a.k;                             // [k] the student's logits there
   constexpr int LIST = NT < 256 ? NT : 256;         // threads that go through the list: a sum over it is the same whatever NT
-  const int tid = threadIdx.x, n = a.classes, my_k = tid < LIST ? a.k : 0;
+  const int tid = threadIdx.x, n = a.classes, k = a.hard < 1.f ? a.k : 0, my_k = tid < LIST ? k : 0;
   const int64_t row = FROM == OWN ? (int64_t)blockIdx.x : (int64_t)(blockIdx.x / (unsigned)a.writers);
   const int seg = FROM == OWN ? 0 : (int)(blockIdx.x % (unsigned)a.writers);
   const T* z = (const T*)a.z + row * a.ldz;
@@ -264,7 +265,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   if (FROM != STATS && seg == 0) {
     if (a.loss) {
       part = block_sum<NT>(part, red_l);
-      float loss = (1.f - a.hard) * a.temperature * a.temperature * part;
+      float loss = k > 0 ? (1.f - a.hard) * a.temperature * a.temperature * part : 0.f;
       if (labelled) loss += a.hard * (l1 - (zl - st.m));
       if (tid == 0) a.loss[row] = empty ? 0.f : loss;
     }
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
     if (c < at.lo || c >= at.hi) continue;
     float p = 0.f;
     bool first = true;
-    for (int i = 0; i < a.k; ++i)
+    for (int i = 0; i < k; ++i)
       if (li[i] == c) {
         p += lp[i];
         if (i < j) first = false;
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
   }
   if (labelled && label >= at.lo && label < at.hi && tid == 0) {
     bool listed = false;
-    for (int i = 0; i < a.k; ++i) listed |= li[i] == label;
+    for (int i = 0; i < k; ++i) listed |= li[i] == label;
     if (!listed) dz[label] = (T)(grad(zl) - mix);
   }
 }

@@ -216,3 +216,41 @@ def test_no_rows_and_refusals(env):
                  lambda: P.bsr_distill_forward(z, torch.zeros(6, 1025, dtype=torch.int32, device="cuda"), torch.zeros(6, 1025, device="cuda"))):
         with pytest.raises(P.BsrError):
             call()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [50, 3001, 30001, 140000])
+def test_hard_weight_one_is_the_cross_entropy(env, n, dtype):
+    """the teacher has no say then: not where it weights classes at -inf, nor with infinities and NaN of its own"""
+    torch, P = env
+    rows = 9
+    z, index, t, labels = make(torch, rows, n, 6, dtype, 8)
+    index[0], z[0, int(index[0, 0])] = index[0, 0], -float("inf")       # all of the weight on a class at -inf
+    z[1, 10:] = -float("inf")
+    index[1], labels[1] = torch.arange(6, 12), 4
+    t[2], t[3, 2], t[4] = float("nan"), float("inf"), -float("inf")
+    index[5] = -1
+    labels[6] = -1
+    z[7, int(labels[7])] = -float("inf")
+    z[8] = -float("inf")
+    labels[0] = (int(index[0, 0]) + 1) % n
+    zd, lab = host(z), labels.cpu().numpy()
+    for T in (1.0, 2.0, 0.7):
+        how = dict(labels=labels, temperature=T, hard_weight=1.0)
+        loss, stats = P.bsr_distill_forward(z, index, t, **how)
+        both, dz = P.bsr_distill_forward_backward(z, index, t, **how)
+        apart = P.bsr_distill_backward(z, index, t, stats, **how)
+        assert torch.equal(loss, both)
+        for r in range(rows):
+            if r in (6, 8):
+                assert loss[r] == 0 and not dz[r].any() and not apart[r].any()
+                continue
+            lr = log_softmax(zd[r:r + 1])[0]
+            want = -lr[lab[r]]
+            assert float(loss[r]) == want if r == 7 else abs(float(loss[r]) - want) <= 1e-4 + 1e-5 * want
+            q = np.exp(lr)
+            size = q.copy()
+            q[lab[r]] -= 1
+            size[lab[r]] += 1
+            for d in (dz, apart):
+                assert (np.abs(host(d[r]) - q) <= 1e-4 * size + 1e-30 + (2.0 ** -8 * np.abs(q) + 1e-38 if dtype == "bf16" else 0)).all(), r
