@@ -267,7 +267,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillArgs a) {
       part = block_sum<NT>(part, red_l);
       float loss = k > 0 ? (1.f - a.hard) * a.temperature * a.temperature * part : 0.f;
       if (labelled) loss += a.hard * (l1 - (zl - st.m));
-      if (tid == 0) a.loss[row] = empty ? 0.f : loss;
+      if (tid == 0) a.loss[row] = empty ? 0.f : lt != lt ? lt : loss;          // (NaN in z shows, with or without entries)
     }
     if (a.stats && tid == 0) {
       a.stats[3 * row] = st.m;

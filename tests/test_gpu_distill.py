@@ -254,3 +254,22 @@ def test_hard_weight_one_is_the_cross_entropy(env, n, dtype):
             size[lab[r]] += 1
             for d in (dz, apart):
                 assert (np.abs(host(d[r]) - q) <= 1e-4 * size + 1e-30 + (2.0 ** -8 * np.abs(q) + 1e-38 if dtype == "bf16" else 0)).all(), r
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [50, 3001, 140000])
+def test_nan_shows_in_rows_without_entries_and_label(env, n, dtype):
+    """in loss and gradient alike; rows beside them have neither"""
+    torch, P = env
+    z, index, t, labels = make(torch, 4, n, 5, dtype, 9)
+    index[:], labels[:] = -1, -1
+    z[1, n // 2], z[2, 0] = float("nan"), float("inf")
+    for T, a in ((1.0, 0.0), (2.0, 0.3), (1.5, 1.0)):
+        how = dict(labels=labels, temperature=T, hard_weight=a)
+        loss, stats = P.bsr_distill_forward(z, index, t, **how)
+        both, dz = P.bsr_distill_forward_backward(z, index, t, **how)
+        apart = P.bsr_distill_backward(z, index, t, stats, **how)
+        for l in (loss, both):
+            assert l[0] == 0 and l[3] == 0 and bool(torch.isnan(l[1:3]).all())
+        for d in (dz, apart):
+            assert not d[0].any() and not d[3].any() and bool(torch.isnan(d[1:3]).all())
