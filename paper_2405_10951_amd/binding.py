@@ -347,13 +347,13 @@ def bsr_linear_wgrad_static(x, dy, dw=None, db=None):
     return dw, used.value
 
 
-def bsr_attention_forward(qkv, heads, want_stats=True, want_cls=True):
+def bsr_attention_forward(qkv, heads, want_lse=True, want_cls=True):
     """qkv [B,T,3D] bf16 -> (out [B,T,D] bf16, lse [B,H,T] | None, cls_prob [B,H,T] | None, used_mfma)."""
     import torch
     B, T, D3 = qkv.shape
     D = D3 // 3
     out = torch.empty((B, T, D), dtype=torch.bfloat16, device=qkv.device)
-    lse = torch.empty((B, heads, T), dtype=torch.float32, device=qkv.device) if want_stats else None
+    lse = torch.empty((B, heads, T), dtype=torch.float32, device=qkv.device) if want_lse else None
     cls = torch.empty((B, heads, T), dtype=torch.float32, device=qkv.device) if want_cls else None
     used = C.c_int32(-1)
     _check(load_library().bsr_attention_forward(_dp(qkv), B, T, heads, D // heads, _dp(out), _dp(lse), _dp(cls),

@@ -228,3 +228,10 @@ def test_tensor_names_are_taken_and_refused_as_the_struct_takes_them():
     for name, error in (("blocks", TypeError), ("blocks.16.w_qkv", IndexError), ("blocks.w_qkv", ValueError)):
         with pytest.raises(error):
             binding._params_struct({name: t})
+
+
+def test_attention_forward_keeps_its_argument_names():
+    import inspect
+
+    import paper_2405_10951_amd as P
+    assert list(inspect.signature(P.bsr_attention_forward).parameters) == ["qkv", "heads", "want_lse", "want_cls"]
