@@ -379,21 +379,40 @@ size_t distill_parts_floats(bool f32, int64_t rows, int classes) {
   return n < 3 ? 0 : (size_t)rows * n * 3;
 }
 
+// f on slices of the rows: a launch has fewer than 2^32 threads, and a row up to 1024 of them.  (Rows are split over workgroups, with scratch for it, only where they are few.)
+constexpr int64_t ROWS_A_LAUNCH = 1 << 21;
+template <class F> static void in_slices(const DistillArgs& all, F&& f) {
+  const int64_t z_size = all.f32 ? 4 : 2, t_size = all.top_f32 ? 4 : 2;
+  for (int64_t m = 0; m < all.rows; m += ROWS_A_LAUNCH) {
+    DistillArgs a = all;
+    a.rows = std::min(ROWS_A_LAUNCH, all.rows - m);
+    a.z = (const char*)all.z + m * all.ldz * z_size;
+    a.index = all.index + m * all.ldi;
+    a.top = (const char*)all.top + m * all.ldt * t_size;
+    if (all.labels) a.labels = all.labels + m;
+    if (all.loss) a.loss = all.loss + m;
+    if (all.stats) a.stats = all.stats + 3 * m;
+    if (all.row_grad) a.row_grad = all.row_grad + m;
+    if (all.dz) a.dz = (char*)all.dz + m * all.ldd * z_size;
+    f(a);
+  }
+}
+
 void distill_forward(const DistillArgs& given, hipStream_t s) {
-  if (given.rows <= 0) return;
-  DistillArgs a = given;
-  a.segments = a.parts ? segments_of(a) : 1;
+  DistillArgs all = given;
+  all.segments = all.parts ? segments_of(all) : 1;
   // (where dz takes the place of z, other segments' logits would be gone: one workgroup writes a row then, from the same parts)
-  a.writers = a.dz && a.dz != a.z ? a.segments : 1;
-  if (a.parts) a.f32 ? go_size<float, PARTS>(a, s) : go_size<bf16, PARTS>(a, s);
-  else a.f32 ? go_size<float, OWN>(a, s) : go_size<bf16, OWN>(a, s);
+  all.writers = all.dz && all.dz != all.z ? all.segments : 1;
+  in_slices(all, [&](const DistillArgs& a) {
+    if (a.parts) a.f32 ? go_size<float, PARTS>(a, s) : go_size<bf16, PARTS>(a, s);
+    else a.f32 ? go_size<float, OWN>(a, s) : go_size<bf16, OWN>(a, s);
+  });
 }
 
 void distill_backward(const DistillArgs& given, hipStream_t s) {
-  if (given.rows <= 0) return;
-  DistillArgs a = given;
-  a.writers = a.dz != a.z ? segments_of(a) : 1;
-  a.f32 ? go_size<float, STATS>(a, s) : go_size<bf16, STATS>(a, s);
+  DistillArgs all = given;
+  all.writers = all.dz != all.z ? segments_of(all) : 1;
+  in_slices(all, [&](const DistillArgs& a) { a.f32 ? go_size<float, STATS>(a, s) : go_size<bf16, STATS>(a, s); });
 }
 
 }  // namespace bsr

@@ -85,3 +85,48 @@ def test_more_logits_than_31_bits(env):
     want, wdz = P.bsr_distill_forward_backward(z[-600:], index[-600:], logits[-600:], labels[-600:], 1.0, 0.5)
     got, dz = P.bsr_distill_forward_backward(z, index, logits, labels, 1.0, 0.5, dz=z)
     assert torch.equal(got[-600:], want) and torch.equal(dz[-600:], wdz)
+
+
+# more rows than a launch takes (2^21 of them), and than a launch of 64 threads a row could have threads for (2^26)
+@pytest.mark.parametrize("rows,classes,top,kind", [((1 << 21) + 3, 9, 3, "f32"), ((1 << 21) + 3, 1100, 2, "bf16"), ((1 << 26) + 5, 2, 1, "bf16")])
+def test_distillation_of_many_rows(env, rows, classes, top, kind):
+    torch, P = env
+    torch.manual_seed(rows)
+    dt = {"bf16": torch.bfloat16, "f32": torch.float32}[kind]
+    z = torch.empty(rows, classes, dtype=dt, device="cuda").normal_()
+    index = torch.randint(classes, (rows, top), device="cuda", dtype=torch.int32)
+    logits = torch.empty(rows, top, dtype=torch.bfloat16 if kind == "f32" else torch.float32, device="cuda").normal_()
+    labels, weight = torch.randint(classes, (rows,), device="cuda", dtype=torch.int32), torch.rand(rows, device="cuda")
+    how = dict(temperature=2.0, hard_weight=0.25)
+    loss, stats = P.bsr_distill_forward(z, index, logits, labels, **how)
+    both, dz = P.bsr_distill_forward_backward(z, index, logits, labels, row_grad=weight, **how)
+    apart = P.bsr_distill_backward(z, index, logits, stats, row_grad=weight, labels=labels, **how)
+    assert torch.equal(both, loss)
+    for first in {0, (1 << 21) - 64, (rows - 64) // 64 * 64}:
+        part = slice(first, first + 128)
+        some = [t[part] for t in (z, index, logits, labels, weight)]
+        want, wstats = P.bsr_distill_forward(*some[:4], **how)
+        wboth, wdz = P.bsr_distill_forward_backward(*some[:4], row_grad=some[4], **how)
+        assert torch.equal(loss[part], want) and torch.equal(stats[part], wstats) and torch.equal(dz[part], wdz)
+        assert torch.equal(apart[part], P.bsr_distill_backward(*some[:3], wstats, row_grad=some[4], labels=some[3], **how))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [5, 8, 3])
+def test_layernorm_of_many_rows(env, D, kind):
+    """more than a launch takes: forward, to 8 bits, and dx alone"""
+    torch, P = env
+    torch.manual_seed(D)
+    M = (1 << 21) + 3
+    x, dy, res = (torch.randn(M, D, device="cuda").to({"bf16": torch.bfloat16, "f32": torch.float32}[kind]) for _ in range(3))
+    gamma, beta = torch.randn(D, device="cuda"), torch.randn(D, device="cuda")
+    y, mean, rstd = P.bsr_layernorm_forward(x, gamma, beta)
+    r8, mean8, rstd8 = P.bsr_layernorm_forward8(x, gamma, beta)
+    dx, _, _ = P.bsr_layernorm_backward(dy, x, mean, rstd, gamma, res=res, need_params=False)
+    assert torch.equal(mean, mean8) and torch.equal(rstd, rstd8)
+    for part in (slice(0, 100), slice((1 << 21) - 50, M), slice(M - 1, M)):
+        wy, wm, wr = P.bsr_layernorm_forward(x[part], gamma, beta)
+        w8, _, _ = P.bsr_layernorm_forward8(x[part], gamma, beta)
+        wdx, _, _ = P.bsr_layernorm_backward(dy[part], x[part], wm, wr, gamma, res=res[part], need_params=False)
+        assert torch.equal(y[part], wy) and torch.equal(mean[part], wm) and torch.equal(rstd[part], wr) and torch.equal(dx[part], wdx)
+        assert torch.equal(r8.values[part], w8.values) and torch.equal(r8.scales[part], w8.scales)
