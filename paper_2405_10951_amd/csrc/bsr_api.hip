@@ -1879,8 +1879,9 @@ int32_t bsr_linear8_forward(const void* x, int32_t x_type, int64_t ldx, const ui
                             const void* values, const uint8_t* scales, const float* bias, int32_t act, void* u_out, const void* res, void* y,
                             int32_t y_type, void* workspace, size_t workspace_bytes, void* stream) {
   if (act != 0 && act != 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "bsr_linear8_forward: act %d (0: none, 1: GELU)", act);
+  if (u_out && act != 1) return fail(nullptr, BSR_ERR_INVALID_ARG, "bsr_linear8_forward: u_out is the input of the GELU, act is %d", act);
   Gemm8Desc g;
-  g.bias = bias; g.act = act ? ACT_GELU : ACT_NONE; g.aux = act ? u_out : nullptr; g.res = res; g.C = y;
+  g.bias = bias; g.act = act ? ACT_GELU : ACT_NONE; g.aux = u_out; g.res = res; g.C = y;
   return linear8("bsr_linear8_forward", x, x_type, ldx, x_scales, M, in, out, values, scales, g, y_type, workspace, workspace_bytes, stream);
 }
 

@@ -108,3 +108,9 @@ def test_lengths_past_their_limits(name, good, bad):
 def test_cut_sums_are_for_bf16_results(name, good, bad):
     assert P.BSR_SUMS_CUT == 256
     test_refused_before_a_launch(name, good, bad)
+
+
+@pytest.mark.parametrize("rows", [4, 400, 0])
+def test_a_stored_input_needs_its_gelu(rows):
+    """u_out would stay as it was"""
+    test_refused_before_a_launch("bsr_linear8_forward", LF, dict(M=rows, act=0, u=A))
