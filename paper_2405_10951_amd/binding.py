@@ -373,8 +373,9 @@ def bsr_attention_backward(qkv, out, dout, lse, heads):
                                                  _dp(delta), _dp(dqkv), C.byref(used), _cur_stream(qkv)))
     return dqkv, used.value
 
+
 class Rows8:
-    """Rows in 8 bits: `values` uint8 [M, ldv] (e4m3), `scales` uint8 [M, lds], `cols` columns (see bsr.h)."""
+    """Rows in 8 bits: `values` uint8 [M, ldv] (e4m3), `scales` uint8 [M, lds], contiguous, `cols` columns (see bsr.h).  Looked at where they are used."""
     __slots__ = ("values", "scales", "cols")
 
     def __init__(self, values, scales, cols):
@@ -383,12 +384,29 @@ class Rows8:
 
 class Weight8:
     """A frozen linear layer in 8 bits, laid out once: `values` / `scales` for the forward product, `values_back` / `scales_back`
-    (None without) for the input gradient; n_in, n_out (see bsr.h)."""
+    (None without) for the input gradient; n_in, n_out (see bsr.h).  Looked at once, here: its parts stay what they are."""
     __slots__ = ("values", "scales", "values_back", "scales_back", "n_in", "n_out")
 
     def __init__(self, values, scales, values_back, scales_back, n_in, n_out):
-        self.values, self.scales, self.values_back, self.scales_back = values, scales, values_back, scales_back
-        self.n_in, self.n_out = int(n_in), int(n_out)
+        import torch
+        n_in, n_out = int(n_in), int(n_out)
+        if n_in < 1 or n_out < 1 or (values_back is None) != (scales_back is None):
+            raise ValueError(f"a layer of {n_in} inputs and {n_out} outputs, with values_back and scales_back or without both")
+        for v, s, rows, cols, what in ((values, scales, n_out, n_in, ""), (values_back, scales_back, n_in, n_out, "_back")):
+            if v is not None:
+                ldv, lds = _block8_strides(cols)
+                _flat(v, "values" + what, (rows, ldv), torch.uint8)
+                _flat(s, "scales" + what, (-(-rows // 128), lds), torch.uint8)
+                if v.device != values.device or s.device != values.device:
+                    raise ValueError(f"tensors on {values.device}, {v.device} and {s.device}")
+        for name, part in zip(self.__slots__, (values, scales, values_back, scales_back, n_in, n_out)):
+            object.__setattr__(self, name, part)
+
+    def __setattr__(self, name, value):
+        raise AttributeError("the parts of a frozen layer are set when it is made")
+
+    def __reduce__(self):                  # copies and pickles are made, and looked at, like the first one
+        return Weight8, tuple(getattr(self, name) for name in self.__slots__)
 
 
 # The wrappers below are on the path of calls that take the GPU a few microseconds, so what they look at they look at once and cheaply.
@@ -455,10 +473,16 @@ def _like(t):
     return t.new_empty(t.shape)
 
 
+def _block8_strides(cols):
+    """bsr_block8_strides: of a row's values, of its scales"""
+    nk = -(-cols // 128)
+    return nk * 128, (nk + 3) // 4 * 4
+
+
 def _rows8_new(M, K, like):
     import torch
-    nk = -(-K // 128)
-    return Rows8(like.new_empty((M, nk * 128), dtype=torch.uint8), like.new_empty((M, (nk + 3) // 4 * 4), dtype=torch.uint8), K)
+    ldv, lds = _block8_strides(K)
+    return Rows8(like.new_empty((M, ldv), dtype=torch.uint8), like.new_empty((M, lds), dtype=torch.uint8), K)
 
 
 def bsr_quantize8_rows(x) -> Rows8:
@@ -478,8 +502,8 @@ def bsr_quantize8_weight(w, backward=True) -> Weight8:
 
     def new(rows, cols):
         import torch
-        nk = -(-cols // 128)
-        return w.new_empty((rows, nk * 128), dtype=torch.uint8), w.new_empty((-(-rows // 128), (nk + 3) // 4 * 4), dtype=torch.uint8)
+        ldv, lds = _block8_strides(cols)
+        return w.new_empty((rows, ldv), dtype=torch.uint8), w.new_empty((-(-rows // 128), lds), dtype=torch.uint8)
 
     v, s = new(n_out, n_in)
     vb, sb = new(n_in, n_out) if backward else (None, None)
@@ -492,8 +516,12 @@ def _linear8(x, cols, what, *others):
     if type(x) is Rows8:
         if x.cols != cols:
             raise ValueError(f"{what}: {x.cols} columns, the layer has {cols}")
-        t = x.values
-        return t, t.shape[0], (t.data_ptr(), BSR_BF16, 0, x.scales.data_ptr()), None, 0, _together(t, x.scales, *others)
+        import torch
+        t, u8 = x.values, torch.uint8
+        M = t.shape[0] if t.dim() else 0
+        ldv, lds = _block8_strides(cols)
+        p, s = _flat(t, what + ".values", (M, ldv), u8), _flat(x.scales, what + ".scales", (M, lds), u8)
+        return t, M, (p, BSR_BF16, 0, s), None, 0, _together(t, x.scales, *others)
     ld = _rows_of(x, what)
     M, k = x.shape
     if k != cols:

@@ -1,6 +1,8 @@
 """The operators on a caller's own tensors without a GPU: exported, bound, and refusing bad arguments before anything is launched (the
 addresses below are never read)."""
+import copy
 import ctypes as C
+import pickle
 
 import pytest
 
@@ -114,3 +116,45 @@ def test_cut_sums_are_for_bf16_results(name, good, bad):
 def test_a_stored_input_needs_its_gelu(rows):
     """u_out would stay as it was"""
     test_refused_before_a_launch("bsr_linear8_forward", LF, dict(M=rows, act=0, u=A))
+
+
+def blocks(rows, cols, rows_per_scale, **how):
+    import torch
+    how = dict(dict(dtype=torch.uint8), **how)
+    return torch.zeros(rows, -(-cols // 128) * 128, **how), torch.zeros(-(-rows // rows_per_scale), -(-cols // 512) * 4, **how)
+
+
+def test_parts_of_a_layer_are_looked_at():
+    """tensors of other shapes, types or strides would be read past their ends"""
+    import torch
+    v, s = blocks(300, 200, 128)
+    vb, sb = blocks(200, 300, 128)
+    layer = P.Weight8(v, s, vb, sb, 200, 300)
+    assert layer.values is v and layer.scales_back is sb and (layer.n_in, layer.n_out) == (200, 300)
+    assert P.Weight8(v, s, None, None, 200, 300).values_back is None
+    for bad in ((v[:299], s, vb, sb), (v[:, :128], s, vb, sb), (v, s[:2], vb, sb), (v, s[:, :2], vb, sb), (v.view(torch.int8), s, vb, sb), (v, s.int(), vb, sb),
+                (v.t(), s, vb, sb), (v, s, v, sb), (v, s, vb, s), (v, s, vb, None), (v, s, None, sb), (v, s, vb.to("meta"), sb),
+                (torch.zeros(600, 256, dtype=torch.uint8)[::2], s, vb, sb)):
+        with pytest.raises(ValueError):
+            P.Weight8(*bad, 200, 300)
+    for n_in, n_out in ((0, 300), (200, 0), (300, 200), (257, 300), (200, 385)):
+        with pytest.raises(ValueError):
+            P.Weight8(v, s, vb, sb, n_in, n_out)
+    with pytest.raises(AttributeError):
+        layer.values = v[:10]
+    for again in (copy.copy(layer), copy.deepcopy(layer), pickle.loads(pickle.dumps(layer))):
+        assert again.n_out == 300 and again.values.shape == v.shape and torch.equal(again.scales_back, sb)
+
+
+@pytest.mark.parametrize("call", ["forward", "dgrad"])
+def test_rows_in_8_bits_are_looked_at(call):
+    import torch
+    v, s = blocks(20, 200, 1)
+    layer = P.Weight8(*blocks(200, 200, 128), *blocks(200, 200, 128), 200, 200)
+    product = P.bsr_linear8_forward if call == "forward" else P.bsr_linear8_dgrad
+    for bad in ((v[:, :128], s), (v[::2], s[::2]), (v, s[:19]), (v, s[:, :2]), (v, s.view(torch.int8)), (v.short(), s), (v.view(-1), s), (v[0, 0], s),
+                (torch.zeros(20, 512, dtype=torch.uint8)[:, :256], s)):
+        with pytest.raises(ValueError, match="(values|scales): contiguous"):
+            product(P.Rows8(*bad, 200), layer)
+    with pytest.raises(ValueError, match="GPU"):
+        product(P.Rows8(v, s, 200), layer)
