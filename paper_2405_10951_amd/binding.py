@@ -423,6 +423,15 @@ def _type_code(t, what):
     return code
 
 
+_LONGEST = 0x7fffffff              # of the lengths that the library takes in 32 bits, which would wrap around
+
+
+def _in_32_bits(n, what):
+    if n > _LONGEST:
+        raise ValueError(f"{what}: {n}, at most {_LONGEST}")
+    return n
+
+
 def _rows_of(t, what, shape=None, dtype=None):
     """A tensor of two dimensions whose rows are contiguous -> its row stride."""
     s = t.shape
@@ -432,6 +441,8 @@ def _rows_of(t, what, shape=None, dtype=None):
         raise TypeError(f"{what}: {dtype} is needed, got {t.dtype}")
     ld, step = t.stride()
     cols = s[1]
+    if cols > _LONGEST:
+        _in_32_bits(cols, what + ": columns")
     if step != 1 and cols > 1:
         raise ValueError(f"{what}: the elements of a row have to lie together, stride {step}")
     if ld < cols:
@@ -497,8 +508,10 @@ def bsr_quantize8_rows(x) -> Rows8:
 def bsr_quantize8_weight(w, backward=True) -> Weight8:
     """w [in,out] bf16 or fp32 (any row stride) -> a frozen 8-bit layer, a scale for each 128 x 128; backward: with the copy that the input
     gradient reads."""
-    ld, code, stream = _rows_of(w, "w"), _type_code(w, "w"), _together(w)
+    ld, code = _rows_of(w, "w"), _type_code(w, "w")
     n_in, n_out = w.shape
+    _in_32_bits(n_in, "w: rows")
+    stream = _together(w)
 
     def new(rows, cols):
         import torch
@@ -518,7 +531,7 @@ def _linear8(x, cols, what, *others):
             raise ValueError(f"{what}: {x.cols} columns, the layer has {cols}")
         import torch
         t, u8 = x.values, torch.uint8
-        M = t.shape[0] if t.dim() else 0
+        M = _in_32_bits(t.shape[0], what + ": rows") if t.dim() else 0
         ldv, lds = _block8_strides(cols)
         p, s = _flat(t, what + ".values", (M, ldv), u8), _flat(x.scales, what + ".scales", (M, lds), u8)
         return t, M, (p, BSR_BF16, 0, s), None, 0, _together(t, x.scales, *others)
@@ -526,6 +539,8 @@ def _linear8(x, cols, what, *others):
     M, k = x.shape
     if k != cols:
         raise ValueError(f"{what}: {k} columns, the layer has {cols}")
+    if M > _LONGEST:
+        _in_32_bits(M, what + ": rows")
     stream = _together(x, *others)
     size, ws = _scratch_size("bsr_linear8_workspace_bytes", M, cols), None
     if size:

@@ -158,3 +158,23 @@ def test_rows_in_8_bits_are_looked_at(call):
             product(P.Rows8(*bad, 200), layer)
     with pytest.raises(ValueError, match="GPU"):
         product(P.Rows8(v, s, 200), layer)
+
+
+def test_lengths_past_32_bits_are_refused_not_wrapped():
+    """the library's columns, and the rows of its products, are 32-bit numbers (tensors without memory: nothing is launched)"""
+    import torch
+
+    def big(*shape, dtype=torch.bfloat16):
+        return torch.empty(*shape, dtype=dtype, device="meta")
+
+    wrapped = (1 << 32) + 64                    # 64 in 32 bits
+    v64 = big(64, dtype=torch.float32)
+    layer = P.Weight8(*blocks(48, 64, 128), *blocks(64, 48, 128), 64, 48)
+    for call in (lambda: P.bsr_quantize8_rows(big(4, wrapped)), lambda: P.bsr_quantize8_weight(big(wrapped, 64)), lambda: P.bsr_quantize8_weight(big(64, wrapped)),
+                 lambda: P.bsr_linear8_forward(big(wrapped, 64), layer), lambda: P.bsr_linear8_dgrad(big(wrapped, 48), layer),
+                 lambda: P.bsr_linear8_forward(P.Rows8(big(wrapped, 128, dtype=torch.uint8), big(wrapped, 4, dtype=torch.uint8), 64), layer),
+                 lambda: P.bsr_layernorm_forward(big(4, wrapped), v64, v64), lambda: P.bsr_layernorm_forward8(big(4, wrapped), v64, v64),
+                 lambda: P.binding._distill_args(big(4, wrapped), big(4, 3, dtype=torch.int32), big(4, 3), None, 1.0, 0.0),
+                 lambda: P.binding._distill_args(big(4, 64), big(4, wrapped, dtype=torch.int32), big(4, wrapped), None, 1.0, 0.0)):
+        with pytest.raises(ValueError, match="2147483647"):
+            call()
