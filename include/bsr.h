@@ -482,7 +482,7 @@ int32_t bsr_attention_backward(const void* qkv, const void* out, const void* dou
  *   mean, rstd    fp32 [M], may be NULL
  * bsr_layernorm_backward: dx = res + rstd (g - mean(g) - xhat mean(g xhat)), g = dy gamma, xhat = (x - mean) rstd; dgamma = sum over rows of
  *   dy xhat, dbeta = sum of dy.  For a forward that left 8-bit rows the rounding counts as the identity.
- *   dy, x, res, dx  [M,D] of `type`, with strides; res may be NULL (no residual gradient to add); dx may be NULL (parameters only), dy or res
+ *   dy, x, res, dx  [M,D] of `type`, with strides; res may be NULL (no residual gradient to add); dx may be NULL (parameters only), dy or res (same stride)
  *   dgamma, dbeta fp32 [D], both or neither
  *   workspace     device fp32 scratch of bsr_layernorm_workspace_floats(D) floats, needed with dgamma
  */

@@ -1765,6 +1765,10 @@ static bool known_type(int32_t t) { return t == BSR_BF16 || t == BSR_FP32; }
 static bool rows_ok(const void* p, int32_t type, int64_t ld, int64_t row) {
   return p && ((uintptr_t)p & (type == BSR_FP32 ? 3 : 1)) == 0 && ld >= row;
 }
+// a result in the place of an input whose rows it would run over before they are read
+static bool in_place_apart(int64_t rows, const void* result, int64_t ldr, const void* input, int64_t ldi) {
+  return rows > 1 && result && result == input && ldr != ldi;
+}
 static bool aligned4(const void* p) { return p && ((uintptr_t)p & 3) == 0; }
 
 size_t bsr_layernorm_workspace_floats(int32_t D) { return D < 1 ? 0 : norm_rows_bwd_floats(D); }
@@ -1779,6 +1783,7 @@ int32_t bsr_layernorm_forward(const void* x, int32_t type, int64_t M, int32_t D,
   if (!values != !scales || (!y && !values)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: y, or values and scales, or all three", w);
   if (!rows_ok(x, type, ldx, D) || (y && !rows_ok(y, type, ldy, D)))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: x or y is NULL, misaligned or has rows closer than %d", w, D);
+  if (in_place_apart(M, y, ldy, x, ldx)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: y in the place of x needs its stride", w);
   if ((values && !aligned16(values)) || (mean && !aligned4(mean)) || (rstd && !aligned4(rstd)))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: misaligned output", w);
   NormRows a;
@@ -1801,6 +1806,8 @@ int32_t bsr_layernorm_backward(const void* dy, int64_t lddy, const void* x, int6
   if (!aligned16(gamma)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: gamma is NULL or not 16-byte aligned", w);
   if (M > 0 && (!rows_ok(dy, type, lddy, D) || !rows_ok(x, type, ldx, D) || (res && !rows_ok(res, type, ldr, D)) || (dx && !rows_ok(dx, type, lddx, D))))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dy, x, res or dx is NULL, misaligned or has rows closer than %d", w, D);
+  if (in_place_apart(M, dx, lddx, dy, lddy) || in_place_apart(M, dx, lddx, x, ldx) || in_place_apart(M, dx, lddx, res, ldr))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dx in the place of dy, x or res needs its stride", w);
   if (M > 0 && (!aligned4(mean) || !aligned4(rstd))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: mean or rstd is NULL or misaligned", w);
   if (M == 0 && !dgamma) return BSR_OK;
   NormRowsBwd a;
@@ -1905,7 +1912,7 @@ static int32_t distill_args(const char* w, DistillArgs& a, const void* z, int32_
   if (rows > 0 && (!rows_ok(z, type, ldz, classes) || !rows_ok(index, BSR_FP32, ldi, top) || !rows_ok(logits, logits_type, ldt, top) ||
                    (dz && !rows_ok(dz, type, ldd, classes))))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: z, index, logits or dz is NULL, misaligned or has rows too close", w);
-  if (rows > 0 && dz == z && ldd != ldz) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dz in the place of z needs its stride", w);
+  if (in_place_apart(rows, dz, ldd, z, ldz)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dz in the place of z needs its stride", w);
   if ((labels && !aligned4(labels)) || (row_grad && !aligned4(row_grad))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: labels or row_grad is misaligned", w);
   a.z = z; a.f32 = type == BSR_FP32; a.rows = rows; a.classes = classes; a.ldz = ldz; a.index = index; a.ldi = ldi;
   a.top = logits; a.top_f32 = logits_type == BSR_FP32; a.ldt = ldt; a.k = top; a.labels = labels; a.temperature = temperature; a.hard = hard_weight;

@@ -178,3 +178,11 @@ def test_lengths_past_32_bits_are_refused_not_wrapped():
                  lambda: P.binding._distill_args(big(4, 64), big(4, wrapped, dtype=torch.int32), big(4, wrapped), None, 1.0, 0.0)):
         with pytest.raises(ValueError, match="2147483647"):
             call()
+
+
+@pytest.mark.parametrize("name,good,bad", [
+    ("bsr_layernorm_forward", LN, dict(y=A, ldx=80, ldy=72)), ("bsr_layernorm_backward", LNB, dict(dy=A, lddy=72, x=2 * A, dx=A, lddx=64)),
+    ("bsr_layernorm_backward", LNB, dict(dy=2 * A, x=2 * A, res=A, ldr=72, dx=A)), ("bsr_layernorm_backward", LNB, dict(dy=2 * A, x=A, ldx=72, dx=A))])
+def test_results_in_the_place_of_an_input_need_its_stride(name, good, bad):
+    """rows would be written over others that have not been read yet"""
+    test_refused_before_a_launch(name, good, bad)
