@@ -508,7 +508,7 @@ int32_t bsr_layernorm_backward(const void* dy, int64_t lddy, const void* x, int6
  *   x             x_scales given: 8-bit rows of `in` columns (x_type and ldx are ignored); NULL: [M,in] of x_type, stride ldx, brought to 8 bits on the way
  *   workspace     device scratch, 16-byte aligned, of bsr_linear8_workspace_bytes(M, in), which is 0 where none is needed (a few rows); for x that is not in 8 bits yet
  *   values, scales  the layer
- *   bias          fp32 [out], may be NULL;  act 0: none, 1: exact-erf GELU
+ *   bias          fp32 [out], may be NULL;  act 0: none, 1: GELU, u Phi(u) (to fp32: Phi to a few units in its last place; to bf16: within 5e-7, an absolute error); GELU' alike
  *   u_out, res, y [M,out] of y_type, contiguous; u_out (the pre-activation, only with act = 1) and res may be NULL
  *   y_type        BSR_BF16 or BSR_FP32: the products are exact and added in fp32.  BSR_BF16 | BSR_SUMS_CUT lets the 8-bit matrix instructions add them, at about
  *                 twice the rate where sums are long: of the eight or so products that these add at a time, what lies below 2^-13 of the largest is cut, so an element may be off by

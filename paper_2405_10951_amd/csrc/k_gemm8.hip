@@ -131,7 +131,7 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) blk[ni][r] = gelu_f(blk[ni][r]);
+        for (int r = 0; r < 16; ++r) blk[ni][r] = gelu_to<sizeof(T) == 4>(blk[ni][r]);
     }
     if (!add) {
       out(blk, (T*)g.C, mi);
@@ -149,7 +149,7 @@ __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][
       const float* src = (const float*)(patch + r * LDF) + lane % CPR * P;
       vecT v;
 #pragma unroll
-      for (int i = 0; i < P; ++i) v[i] = (T)(ACT == ACT_GELU_BWD ? src[i] * gelu_grad_f((float)more[p][i]) : src[i] + (float)more[p][i]);
+      for (int i = 0; i < P; ++i) v[i] = (T)(ACT == ACT_GELU_BWD ? src[i] * gelu_grad_to<sizeof(T) == 4>((float)more[p][i]) : src[i] + (float)more[p][i]);
       if (m < g.M && n > 0) put16((T*)g.C + (int64_t)m * g.ldc + col, n, past, v);
     }
     fence();
@@ -631,9 +631,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void gemm8_few_kernel(const void
     if (g.bias) v += g.bias[col];
     if (g.act == ACT_GELU) {
       if (g.aux) put(g.aux, at, v);
-      v = gelu_f(v);
+      v = g.out_f32 ? gelu_fp32(v) : gelu_f(v);
     } else if (g.act == ACT_GELU_BWD) {
-      v *= gelu_grad_f(get(g.aux, at));
+      v *= g.out_f32 ? gelu_grad_fp32(get(g.aux, at)) : gelu_grad_f(get(g.aux, at));
     }
     if (g.res) v += get(g.res, at);
     put(g.C, at, v);
