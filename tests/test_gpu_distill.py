@@ -273,3 +273,13 @@ def test_nan_shows_in_rows_without_entries_and_label(env, n, dtype):
             assert l[0] == 0 and l[3] == 0 and bool(torch.isnan(l[1:3]).all())
         for d in (dz, apart):
             assert not d[0].any() and not d[3].any() and bool(torch.isnan(d[1:3]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,a", [(0.7, 0.3), (1.5, 0.5), (10.0, 0.1), (3.0, 0.4), (4.0, 0.25), (2.0, 0.5), (1.5, 1.0)])
+@pytest.mark.parametrize("rows,n,k", [(5, 100, 10), (3, 1000, 7), (4, 7777, 33), (3, 30003, 16), (5, 50001, 8), (2, 100001, 64), (520, 9000, 4), (2, 270001, 12)])
+def test_every_temperature_with_a_hard_part(env, rows, n, k, T, a, dtype):
+    """those whose second exponential is a power of the first, and those whose is one of its own, at every way to take a row"""
+    torch, P = env
+    z, index, t, labels = make(torch, rows, n, k, dtype, 10)
+    check(torch, P, z, index, t, labels, T, a, dtype)
