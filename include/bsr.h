@@ -471,7 +471,7 @@ int32_t bsr_attention_backward(const void* qkv, const void* out, const void* dou
  * length) and the first may start anywhere.  Types are BSR_BF16 or BSR_FP32; statistics, sums over rows, products and losses are fp32 inside whatever
  * the type.  Tensors without a stride are aligned to 16 bytes; rows of whole 16-byte pieces on 16-byte boundaries are the fast ones.  Zero rows are no error: nothing is
  * launched but what zeroes a sum over them.  Results are bit-reproducible (no atomics).  All launches go to `stream`, nothing waits.
- * Limits: rows of up to 2^30 elements, frozen layers of up to 2^23 inputs and outputs.
+ * Limits: rows of up to 2^30 elements, frozen layers of up to 2^23 inputs and outputs, products of up to 2^30 rows, losses of up to 2^31 - 1.
  * Errors: INVALID_ARG (NULL or misaligned pointer, a negative row count, a length < 1 or past its limit, a stride shorter than a row, an unknown type), HIP.
  *
  * LayerNorm.
@@ -538,7 +538,8 @@ int32_t bsr_linear8_dgrad(const void* dy, int32_t dy_type, int64_t lddy, const u
  *   dz_v = g ((1 - a) T (q_v - sum_{j: c_j = v} p_j) + a (r_v - [v = label])),   g = grad_scale * row_grad[row]
  * An entry whose class lies outside 0 .. classes-1 is absent, one whose logit is -inf has p = 0; a row without entries of p > 0 lacks the first part, one
  * whose label lies outside 0 .. classes-1 the second; at a = 1 every row lacks the first (the entries are not read), at a = 0 the second.  A row whose logits are all -inf has loss
- * and gradient 0.  A class with z = -inf that the teacher gives weight (at a < 1) makes the loss +inf and leaves the gradient finite.  NaN and +inf in z make a row NaN.
+ * and gradient 0.  A class with z = -inf that the teacher gives weight (at a < 1) makes the loss +inf and leaves the gradient finite.  NaN and +inf in z make a row NaN;
+ * among the logits of a row's entries (at a < 1) they make its loss NaN, and its gradient at their classes.
  *   z            [rows, classes] of `type`, stride ldz
  *   index        int32 [rows, top], stride ldi: c_j;  top <= 1024
  *   logits       [rows, top] of logits_type, stride ldt: t_j

@@ -409,7 +409,9 @@ class Weight8:
         return Weight8, tuple(getattr(self, name) for name in self.__slots__)
 
 
-# The wrappers below are on the path of calls that take the GPU a few microseconds, so what they look at they look at once and cheaply.
+# The operators on a caller's own tensors.  As everywhere in this module the library computes and nothing is recorded for autograd: results carry no graph, whether or not an argument
+# asks for a gradient; gradients are what the backward calls return.
+# The wrappers are on the path of calls that take the GPU a few microseconds, so what they look at they look at once and cheaply.
 _types: dict = {}                  # torch type -> type code
 
 

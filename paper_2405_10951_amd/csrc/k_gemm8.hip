@@ -1,24 +1,24 @@
 // Products of 8-bit operands with a scale for each block of 128 (fp8.h): forward and input gradient of frozen linear layers.
 //
-// C(m,n) = epilogue(sum over blocks b of 2^(ea(m,b) + eb(n/128,b)) sum_{k in b} A(m,k) B(n,k)), fp32 accumulation, in
-// v_mfma_scale_f32_32x32x64_f8f6f4 (16x16x128 for few rows), which multiplies by the scales of its operands on the way: a scale is a byte that
-// each lane passes for its row.  A k-tile is one block of 128, so the bytes of a tile row (128) and the LDS layout are those of the bf16
+// C(m,n) = epilogue(sum over blocks b of 2^(ea(m,b) + eb(n/128,b)) sum_{k in b} A(m,k) B(n,k)), fp32 accumulation, in two forms:
+//   exact  v_mfma_f32_32x32x16_bf16 (16x16x32 for few rows) on operands that are brought to bf16, scale and all, on the way from LDS to the instruction
+//   cut    v_mfma_scale_f32_32x32x64_f8f6f4, which multiplies by the scales of its operands on the way: a scale is a byte that each lane passes for its row
+// A k-tile is one block of 128, so the bytes of a tile row (128) and the LDS layout are those of the bf16
 // products with their k-tiles of 64, and so is the way operands come: straight from global memory into LDS.  Any order of k within a block
 // is as good as another as long as both operands use it, the scale being one for all of it.
 //
-// How exactly that adds up (measured, one large product among small ones in an instruction): of the products that the 8-bit instructions add at
+// How exactly that adds up (measured, one large product among small ones in an instruction).  Of the products that the 8-bit instructions add at
 // a time, those smaller than 2^-13 of the largest are cut to nothing and the others to that place; between such groups, and to the accumulator, the sum is fp32.
-// On random operands the result is off by about 3e-5 of its size, whatever K, but one outlier takes up to all of its group's small products with it: where two
+// On random operands the result is off by about 3e-5 of its size, whatever K, but an outlier takes up to all of its group's small products with it: where two
 // outliers cancel, what is left may be gone.  An element can be off by 2^-13 of the largest product for each product, 2^-6 of the largest in each block of
-// 128.  The bf16 instructions add the same products (exact in bf16: an e4m3 value times a power of two is one, but for a value that rounds to
-// 2^128, which is infinite there) to 24 bits, at half the rate.  So there are two forms: EXACT brings the operands to bf16 on the way from LDS to the instruction, and is what
-// runs unless the caller chose the other one (BSR_SUMS_CUT, for bf16 results: 16384 x 4096 x 8192 434 us against 909, 6304 x 768 x 2304 15.3 against 25.6).  Few rows
+// 128.  The bf16 instructions add the same products to 24 bits, at half the rate; an e4m3 value times a power of two is a bf16 value, but at the ends of the range (2^128 is infinite,
+// below 2^-126 there are fewer bits).  So exact sums are what runs, and a caller who wants bf16 results may choose the others (BSR_SUMS_CUT).  Few rows
 // have the exact form alone, trips to memory being what they wait for: 1 x 4096 x 4096 5.5 us against 5.7 from 8-bit rows and 6.5 against 6.3 from bf16.
 //
-// Measured, in chains of launches, exact and cut: 8192^3 893 us (1231 TFLOP/s; to fp32 900) and 409 (2688), 16384 x 4096 x 8192 909 (with GELU 958) and
-// 434 (479), 4096^3 117 and 57, 6304 x 768 x 2304 25.6 and 15.3, 100 x 4096 x 4096 11.4 and 8.2.  Large cut products are bound by the card's power (on zeros they run 25 %
-// faster at the same instructions and bytes), large exact ones reach 86 % of the rate of the library's largest bf16 product, the conversions standing in front of the products;
-// short ones are bound by the way into LDS and out of the registers, few rows by the latency of a k-tile.
+// Measured, in chains of launches, exact and cut: 8192^3 889 us (1237 TFLOP/s; to fp32 902) and 409 (2690), 16384 x 4096 x 8192 909 (with GELU 953, times GELU' 987) and
+// 435 (480, 534), 4096^3 116 and 57, 6304 x 768 x 2304 26 and 15.5, 100 x 4096 x 4096 11.4 and 8.2.  Large products are bound by the card's power: on zeros 16384 x 4096 x 8192
+// takes 688 us exact and 341 cut, at the same instructions and bytes.  Exact ones reach 86 % of the rate of the library's largest bf16 product.  Short sums are bound by the way
+// into LDS, the conversions and the way out of the registers, few rows by the latency of a k-tile.
 #include <algorithm>
 #include <type_traits>
 
@@ -60,7 +60,7 @@ template <typename T> __device__ __forceinline__ void put16(T* p, int n, bool pa
 // 16 bytes of a row.  bias: that of the wave tile's columns, in LDS.  What is added or multiplied there is asked for a row block ahead.  The row blocks are a
 // loop: code that is written out once is fetched once.
 // Stores.  A row of a wave tile is one or two 128-byte lines, or half of one, where rows lie on lines; such stores go past the caches, which
-// otherwise lose the operands' panels to results that nobody reads here (16384 x 4096 x 8192: 509 -> 460 us; 6304 x 768 x 2304: 17.7 -> 15.7).  Smaller pieces of lines must not:
+// otherwise lose the operands' panels to results that nobody reads here (cut sums, 16384 x 4096 x 8192: 509 -> 460 us; 6304 x 768 x 2304: 17.7 -> 15.7).  Smaller pieces of lines must not:
 // results stored 32 bytes of a row at a time straight from the accumulators took 509 us the ordinary way and 688 past the caches.
 template <int MI, int NI, typename T, int ACT>
 __device__ __forceinline__ void epilogue8(const Gemm8Desc& g, f32x16 (&acc)[MI][NI], int row0, int col0, int lane, unsigned char* patch,

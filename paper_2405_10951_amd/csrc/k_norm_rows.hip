@@ -149,7 +149,7 @@ __global__ __launch_bounds__(block_threads<TPR>()) void rows_fwd_kernel(const T*
       put_chunk<WHOLE>(y + m * ldy, c, D, c < nch, skip, w);
     }
     if constexpr (OUT8) {                          // BLOCK8 / V neighbouring lanes hold a block
-      // (8-bit rows stay in the caches for the product behind: past them 16384 x 8192 takes 108 us against 127, but 25216 x 768 with its product 47 against 44)
+      // (8-bit rows stay in the caches for the product behind: past them 16384 x 8192 takes 108 us against 127, but 25216 x 768 with its product, cut sums, 47 against 44)
       if (i * TPR * V < ldq) {
         // (fmaxf passes NaN over; a block with an infinity goes through its values again)
         float most = 0.f;

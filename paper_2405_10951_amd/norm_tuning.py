@@ -9,7 +9,7 @@ the final norm and the head, bsr_distill_forward_backward on the logits, and bac
 
     bsr_linear8_dgrad (GELU' of the kept input) -> bsr_linear8_dgrad -> bsr_layernorm_backward (residual gradient added; dgamma, dbeta)
 
-with the 8-bit rounding of activations counted as the identity.
+with the 8-bit rounding of activations counted as the identity.  The products' sums are exact; --cut-sums takes the faster ones of fewer bits.
 
     python -m paper_2405_10951_amd.norm_tuning --rows 6304 --width 768 --hidden 1536 --depth 4 --classes 1000 --steps 60
 """
