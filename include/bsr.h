@@ -532,7 +532,7 @@ int32_t bsr_linear8_dgrad(const void* dy, int32_t dy_type, int64_t lddy, const u
 
 /*
  * Distillation: loss of a classifier against a teacher's top logits, mixed with the label's cross-entropy.  Per row, with the student's logits
- * z [classes], the teacher's entries (class c_j, logit t_j), temperature T > 0 and hard weight a in [0,1]:
+ * z [classes], the teacher's entries (class c_j, logit t_j), temperature T in [1.2e-38, 1.8e19] (1 / T and T^2 are fp32) and hard weight a in [0,1]:
  *   p = softmax(t / T) over the entries,  q = softmax(z / T),  r = softmax(z)
  *   loss = (1 - a) T^2 sum_j p_j (log p_j - log q_{c_j}) + a (-log r_label)
  *   dz_v = g ((1 - a) T (q_v - sum_{j: c_j = v} p_j) + a (r_v - [v = label])),   g = grad_scale * row_grad[row]

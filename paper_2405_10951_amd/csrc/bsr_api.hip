@@ -1907,8 +1907,8 @@ static int32_t distill_args(const char* w, DistillArgs& a, const void* z, int32_
   if (!known_type(type) || !known_type(logits_type) || rows < 0 || rows > INT32_MAX || classes < 1 || classes > LONGEST_ROW || top < 1 || top > DISTILL_MAX_TOP)
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: types %d and %d, rows %lld, classes %d, top %d (1 .. %d)", w, type, logits_type, (long long)rows, classes, top,
                 DISTILL_MAX_TOP);
-  if (!(temperature > 0.f) || !(temperature <= 3.4e38f) || !(hard_weight >= 0.f && hard_weight <= 1.f))
-    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: temperature %g, hard_weight %g", w, temperature, hard_weight);
+  if (!(temperature >= 1.2e-38f && temperature <= 1.8e19f) || !(hard_weight >= 0.f && hard_weight <= 1.f))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: temperature %g (1.2e-38 .. 1.8e19), hard_weight %g (0 .. 1)", w, temperature, hard_weight);
   if (rows > 0 && (!rows_ok(z, type, ldz, classes) || !rows_ok(index, BSR_FP32, ldi, top) || !rows_ok(logits, logits_type, ldt, top) ||
                    (dz && !rows_ok(dz, type, ldd, classes))))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: z, index, logits or dz is NULL, misaligned or has rows too close", w);

@@ -186,3 +186,10 @@ def test_lengths_past_32_bits_are_refused_not_wrapped():
 def test_results_in_the_place_of_an_input_need_its_stride(name, good, bad):
     """rows would be written over others that have not been read yet"""
     test_refused_before_a_launch(name, good, bad)
+
+
+@pytest.mark.parametrize("name,good", [("bsr_distill_forward", DF), ("bsr_distill_backward", DB)])
+@pytest.mark.parametrize("T", [1e-39, 1e-45, 2e19, 3e38])
+def test_temperatures_whose_square_or_reciprocal_overflows(name, good, T):
+    """their losses and gradients would be 0 times infinity"""
+    test_refused_before_a_launch(name, good, dict(T=T))
