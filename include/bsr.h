@@ -508,11 +508,12 @@ int32_t bsr_layernorm_backward(const void* dy, int64_t lddy, const void* x, int6
  *   x             x_scales given: 8-bit rows of `in` columns (x_type and ldx are ignored); NULL: [M,in] of x_type, stride ldx, brought to 8 bits on the way
  *   workspace     device scratch, 16-byte aligned, of bsr_linear8_workspace_bytes(M, in), which is 0 where none is needed (a few rows); for x that is not in 8 bits yet
  *   values, scales  the layer
- *   bias          fp32 [out], may be NULL;  act 0: none, 1: GELU, u Phi(u) (to fp32: Phi to a few units in its last place; to bf16: within 5e-7, an absolute error); GELU' alike
+ *   bias          fp32 [out], may be NULL;  act 0: none, 1: GELU, u Phi(u) (to fp32: Phi within 6.3e-8, below 0 to u^2 2^-24 of itself and a few units in its last place; to bf16: within 5e-7); GELU' alike
  *   u_out, res, y [M,out] of y_type, contiguous; u_out (the pre-activation, only with act = 1) and res may be NULL
  *   y_type        BSR_BF16 or BSR_FP32: the products are exact and added in fp32.  BSR_BF16 | BSR_SUMS_CUT lets the 8-bit matrix instructions add them, at about
  *                 twice the rate where sums are long: of the eight or so products that these add at a time, what lies below 2^-13 of the largest is cut, so an element may be off by
- *                 2^-6 of the largest |x w| of each block of 128 columns (by 3e-5 of its size on random data; where outliers cancel, by all that is left).
+ *                 2^-6 of the largest |x w| of each block of 128 columns (by 3e-5 of its size on random data; where outliers cancel, by all that is left).  Up to 32 rows
+ *                 are exact all the same.
  *                 A value of x or W that rounds to 2^128 in 8 bits counts as infinite.
  * bsr_linear8_dgrad: dx[M,in] = dy[M,out] . W^T, optionally times GELU'(u) element-wise; values, scales are the layer's values_back, scales_back
  *   dy            as x above, of `out` columns;  workspace: bsr_linear8_workspace_bytes(M, out)
@@ -539,7 +540,7 @@ int32_t bsr_linear8_dgrad(const void* dy, int32_t dy_type, int64_t lddy, const u
  * An entry whose class lies outside 0 .. classes-1 is absent, one whose logit is -inf has p = 0; a row without entries of p > 0 lacks the first part, one
  * whose label lies outside 0 .. classes-1 the second; at a = 1 every row lacks the first (the entries are not read), at a = 0 the second.  A row whose logits are all -inf has loss
  * and gradient 0.  A class with z = -inf that the teacher gives weight (at a < 1) makes the loss +inf and leaves the gradient finite.  NaN and +inf in z make a row NaN;
- * among the logits of a row's entries (at a < 1) they make its loss NaN, and its gradient at their classes.
+ * among the logits of a row's entries (at a < 1) they make its loss NaN, and its gradient at the entries' classes.
  *   z            [rows, classes] of `type`, stride ldz
  *   index        int32 [rows, top], stride ldi: c_j;  top <= 1024
  *   logits       [rows, top] of logits_type, stride ldt: t_j

@@ -283,3 +283,20 @@ def test_every_temperature_with_a_hard_part(env, rows, n, k, T, a, dtype):
     torch, P = env
     z, index, t, labels = make(torch, rows, n, k, dtype, 10)
     check(torch, P, z, index, t, labels, T, a, dtype)
+
+
+@pytest.mark.parametrize("n", [50, 3001])
+def test_nan_and_infinity_in_the_teachers_list(env, n):
+    """they show in the loss and in the gradient at the classes of the row's entries; those of absent entries do not count"""
+    torch, P = env
+    z, index, t, labels = make(torch, 5, n, 6, "f32", 11)
+    clean, _ = P.bsr_distill_forward_backward(z, torch.cat([index[:, :5], torch.full_like(index[:, 5:], -1)], 1), t, labels, 2.0, 0.3)
+    index[:3, 5] = -1
+    t[0, 5], t[1, 5], t[2, 5] = float("nan"), float("inf"), 0.0
+    t[3, 2], t[4, 2] = float("nan"), float("inf")
+    loss, dz = P.bsr_distill_forward_backward(z, index, t, labels, 2.0, 0.3)
+    assert torch.equal(loss[:3], clean[:3]) and bool(torch.isfinite(dz[:3]).all())
+    for r in (3, 4):
+        listed = torch.zeros(n, dtype=torch.bool, device="cuda")
+        listed[index[r].long()] = True
+        assert bool(torch.isnan(loss[r])) and bool(torch.isnan(dz[r][listed]).all()) and bool(torch.isfinite(dz[r][~listed]).all())
