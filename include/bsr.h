@@ -465,8 +465,8 @@ int32_t bsr_attention_backward(const void* qkv, const void* out, const void* dou
                                int32_t* used_mfma, void* stream);
 
 /*
- * Operators on the caller's own tensors (no context): LayerNorm, frozen linear layers in 8 bits, distillation from a teacher's top
- * logits.  A program that tunes the norms of a frozen model against a teacher runs them one after the other
+ * Operators on the caller's own tensors (no context): LayerNorm, RMSNorm, frozen linear layers in 8 bits, distillation from a teacher's top
+ * logits, cross-entropy of a linear layer, clipping of gradients.  A program that tunes the norms of a frozen model against a teacher runs them one after the other
  * (paper_2405_10951_amd/norm_tuning.py).  Rows are contiguous; between rows there is a stride ("ld...", in elements, at least the row's
  * length) and the first may start anywhere.  Types are BSR_BF16 or BSR_FP32; statistics, sums over rows, products and losses are fp32 inside whatever
  * the type.  Tensors without a stride are aligned to 16 bytes; rows of whole 16-byte pieces on 16-byte boundaries are the fast ones.  Zero rows are no error: nothing is
@@ -492,6 +492,28 @@ int32_t bsr_layernorm_forward(const void* x, int32_t type, int64_t M, int32_t D,
 int32_t bsr_layernorm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* res, int64_t ldr, int32_t type, int64_t M,
                                int32_t D, const float* mean, const float* rstd, const float* gamma, void* dx, int64_t lddx, float* dgamma,
                                float* dbeta, float* workspace, size_t workspace_floats, void* stream);
+
+/*
+ * RMSNorm of rows with the residual's addition in front: s = x + res, y = s rstd gamma, rstd = 1 / sqrt(mean(s^2) + eps).  (Sums of squares are fp32: rows of values past
+ * 1e19 / sqrt(D) or so have rstd 0.)
+ * bsr_rmsnorm_forward
+ *   x [M,D] stride ldx, res [M,D] stride ldr (NULL: none), y [M,D] stride ldy: of `type`; y may be NULL when values is given
+ *   sum           [M,D] of `type`, stride lds: s, rounded once, which the norm does not see; NULL: not wanted (NULL without res).  sum and y may each take the place of x or res (same
+ *                 stride), not one another's
+ *   gamma         fp32 [D]
+ *   values, scales  both or neither: the result, unrounded, as 8-bit rows (below)
+ *   rstd          fp32 [M], may be NULL
+ * bsr_rmsnorm_backward: dx = res + rstd (g - xhat mean(g xhat)), g = dy gamma, xhat = x rstd, with x what the norm was of (sum, where there was a residual: dx is then the
+ *   gradient of x and of res alike); dgamma = sum over rows of dy xhat.  For a forward that left 8-bit rows the rounding counts as the identity.
+ *   dy, x, res, dx  [M,D] of `type`, with strides; res may be NULL (no gradient of sum from elsewhere to add); dx may be NULL (dgamma only), dy, x or res (same stride)
+ *   dgamma        fp32 [D], may be NULL
+ *   workspace     device fp32 scratch of bsr_rmsnorm_workspace_floats(D) floats, needed with dgamma
+ */
+size_t bsr_rmsnorm_workspace_floats(int32_t D);
+int32_t bsr_rmsnorm_forward(const void* x, int64_t ldx, const void* res, int64_t ldr, int32_t type, int64_t M, int32_t D, const float* gamma, float eps, void* sum,
+                            int64_t lds, void* y, int64_t ldy, void* values, uint8_t* scales, float* rstd, void* stream);
+int32_t bsr_rmsnorm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* res, int64_t ldr, int32_t type, int64_t M, int32_t D,
+                             const float* rstd, const float* gamma, void* dx, int64_t lddx, float* dgamma, float* workspace, size_t workspace_floats, void* stream);
 
 /*
  * Frozen linear layers in 8 bits.  A block of 128 holds e4m3 values (1 sign, 4 exponent, 3 mantissa bits, largest 448) and one scale, a power
@@ -563,6 +585,20 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
                              const void* logits, int32_t logits_type, int64_t ldt, int32_t top, const int32_t* labels, float temperature,
                              float hard_weight, const float* stats, const float* row_grad, float grad_scale, void* dz, int64_t ldd,
                              void* stream);
+
+/*
+ * The norm of many gradients taken together, and the gradients brought down to a largest norm: norm = sqrt(sum over tensors and values of g^2),
+ * out = g min(1, max_norm / norm).  Squares and their sum are fp64.  A norm that is infinite or no number is given as it is and scales nothing.
+ *   grads, types, lengths  host arrays of `count` (1 or more) entries: device address (aligned to the values), BSR_BF16 or BSR_FP32, values (0 .. 2^36; any address
+ *                where it is 0).  They are read before the call returns
+ *   max_norm     0 or more; infinite: nothing is scaled
+ *   out          host array of device addresses, of the gradients' types; out[i] may be grads[i], and results may not touch one another or another gradient.  NULL: the norm alone
+ *   norm         device fp32 scalar; may be NULL with out
+ *   workspace    device scratch of bsr_clip_workspace_bytes(count) bytes, aligned to 8
+ */
+size_t bsr_clip_workspace_bytes(int32_t count);
+int32_t bsr_clip_grads(const void* const* grads, const int32_t* types, const int64_t* lengths, int32_t count, float max_norm, void* const* out, float* norm,
+                       void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Profiling mode, for measurement only.  Between bsr_profile_begin and bsr_profile_end every launch

@@ -136,6 +136,9 @@ def load_library():
     for name, args in {
             "bsr_layernorm_forward": (p, i32, i64, i32, i64, p, p, f32, p, i64, p, p, p, p, p),
             "bsr_layernorm_backward": (p, i64, p, i64, p, i64, i32, i64, i32, p, p, p, p, i64, p, p, p, C.c_size_t, p),
+            "bsr_rmsnorm_forward": (p, i64, p, i64, i32, i64, i32, p, f32, p, i64, p, i64, p, p, p, p),
+            "bsr_rmsnorm_backward": (p, i64, p, i64, p, i64, i32, i64, i32, p, p, p, i64, p, p, C.c_size_t, p),
+            "bsr_clip_grads": (p, p, p, i32, f32, p, p, p, C.c_size_t, p),
             "bsr_quantize8_rows": (p, i32, i64, i32, i64, p, p, p),
             "bsr_quantize8_weight": (p, i32, i32, i32, i64, p, p, p, p, p),
             "bsr_linear8_forward": (p, i32, i64, p, i32, i32, i32, p, p, p, i32, p, p, p, i32, p, C.c_size_t, p),
@@ -145,6 +148,8 @@ def load_library():
         getattr(lib, name).restype, getattr(lib, name).argtypes = i32, args
     lib.bsr_block8_strides.restype, lib.bsr_block8_strides.argtypes = None, (i32, p, p)
     lib.bsr_layernorm_workspace_floats.restype, lib.bsr_layernorm_workspace_floats.argtypes = C.c_size_t, (i32,)
+    lib.bsr_rmsnorm_workspace_floats.restype, lib.bsr_rmsnorm_workspace_floats.argtypes = C.c_size_t, (i32,)
+    lib.bsr_clip_workspace_bytes.restype, lib.bsr_clip_workspace_bytes.argtypes = C.c_size_t, (i32,)
     lib.bsr_distill_workspace_floats.restype, lib.bsr_distill_workspace_floats.argtypes = C.c_size_t, (i32, i64, i32)
     lib.bsr_linear8_workspace_bytes.restype, lib.bsr_linear8_workspace_bytes.argtypes = C.c_size_t, (i32, i32)
     lib.bsr_profile_begin.argtypes = [C.c_void_p]
@@ -661,6 +666,70 @@ def bsr_layernorm_backward(dy, x, mean, rstd, gamma, res=None, dx=None, need_dx=
     return dx, dg, db
 
 
+def _rmsnorm_forward(x, gamma, eps, res, y, sum_out, r8):
+    ldx, code, stream = _rows_of(x, "x"), _type_code(x, "x"), _together(x, gamma, res, y, sum_out)
+    shape, dtype = x.shape, x.dtype
+    M, D = shape
+    import torch
+    pg = _flat(gamma, "gamma", (D,), torch.float32)
+    ldy = 0 if y is None else _rows_of(y, "y", shape, dtype)
+    ldr = lds = 0
+    if res is not None:
+        ldr = _rows_of(res, "res", shape, dtype)
+        if sum_out is None:
+            sum_out, lds = _like(x), D
+        else:
+            lds = _rows_of(sum_out, "sum_out", shape, dtype)
+    elif sum_out is not None:
+        raise ValueError("sum_out is the sum of x and res, there is no res")
+    rstd = gamma.new_empty(M)
+    pq, ps = (None, None) if r8 is None else (r8.values.data_ptr(), r8.scales.data_ptr())
+    _check(load_library().bsr_rmsnorm_forward(x.data_ptr(), ldx, _dp(res), ldr, code, M, D, pg, eps, _dp(sum_out), lds, _dp(y), ldy, pq, ps, rstd.data_ptr(), stream))
+    return rstd, x if res is None else sum_out
+
+
+def bsr_rmsnorm_forward(x, gamma, eps=1e-6, res=None, y=None, sum_out=None):
+    """x, res [M,D] bf16 or fp32 (any row stride; res None: none), gamma [D] fp32 -> (y [M,D], rstd [M], what the norm is of: x + res [M,D], rounded once, or x itself)."""
+    if y is None:
+        y = _like(x)
+    rstd, total = _rmsnorm_forward(x, gamma, eps, res, y, sum_out, None)
+    return y, rstd, total
+
+
+def bsr_rmsnorm_forward8(x, gamma, eps=1e-6, res=None, y=None, sum_out=None):
+    """The same with the result in 8 bits -> (Rows8, rstd, x + res or x); y given: rounded to the type of x as well."""
+    _rows_of(x, "x")
+    r8 = _rows8_new(*x.shape, x)
+    rstd, total = _rmsnorm_forward(x, gamma, eps, res, y, sum_out, r8)
+    return r8, rstd, total
+
+
+def bsr_rmsnorm_backward(dy, x, rstd, gamma, res=None, dx=None, need_dx=True, need_params=True):
+    """dy [M,D], x [M,D] (what the norm was of), rstd [M] of the forward, gamma [D] -> (dx [M,D] | None, dgamma [D] | None).  res [M,D]: added to dx."""
+    lib = load_library()
+    ldx, code, stream = _rows_of(x, "x"), _type_code(x, "x"), _together(x, dy, rstd, gamma, res, dx)
+    shape, dtype = x.shape, x.dtype
+    M, D = shape
+    import torch
+    f32 = torch.float32
+    lddy = _rows_of(dy, "dy", shape, dtype)
+    ldr = 0 if res is None else _rows_of(res, "res", shape, dtype)
+    ps, pg = _flat(rstd, "rstd", (M,), f32), _flat(gamma, "gamma", (D,), f32)
+    if dx is None:
+        lddx = D
+        if need_dx:
+            dx = _like(x)
+    else:
+        lddx = _rows_of(dx, "dx", shape, dtype)
+    dg = ws = None
+    floats = 0
+    if need_params:
+        floats = _scratch_size("bsr_rmsnorm_workspace_floats", D)
+        dg, ws = gamma.new_empty(D), gamma.new_empty(floats)
+    _check(lib.bsr_rmsnorm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, _dp(res), ldr, code, M, D, ps, pg, _dp(dx), lddx, _dp(dg), _dp(ws), floats, stream))
+    return dx, dg
+
+
 def _distill_args(z, index, logits, labels, temperature, hard_weight):
     import torch
     ldz, code = _rows_of(z, "z"), _type_code(z, "z")
@@ -727,6 +796,44 @@ def bsr_distill_backward(z, index, logits, stats, row_grad=None, labels=None, te
     pg, dz, ldd = _distill_dz(z, row_grad, dz)
     _check(load_library().bsr_distill_backward(*args, ps, pg, grad_scale, dz.data_ptr(), ldd, stream))
     return dz
+
+
+def _clip(grads, max_norm, out):
+    import torch
+    n = len(grads)
+    if n == 0:
+        raise ValueError("no gradients")
+    stream = _together(*grads, *(out or ()))
+    types = [_type_code(g, "a gradient") for g in grads]
+    for g in grads:
+        if not g.is_contiguous():
+            raise ValueError(f"gradients have to be contiguous, got shape {tuple(g.shape)}, strides {g.stride()}")
+    addresses = None
+    if out is not None:
+        if len(out) != n:
+            raise ValueError(f"{n} gradients, {len(out)} results")
+        if out is not grads:
+            for g, o in zip(grads, out):
+                if o.shape != g.shape or o.dtype is not g.dtype or not o.is_contiguous():
+                    raise ValueError(f"out: contiguous {g.dtype} {tuple(g.shape)} expected, got {o.dtype} {tuple(o.shape)}, strides {o.stride()}")
+        addresses = (C.c_void_p * n)(*[o.data_ptr() for o in out])
+    size = _scratch_size("bsr_clip_workspace_bytes", n)
+    norm, ws = grads[0].new_empty((), dtype=torch.float32), grads[0].new_empty(size, dtype=torch.uint8)
+    _check(load_library().bsr_clip_grads((C.c_void_p * n)(*[g.data_ptr() for g in grads]), (C.c_int32 * n)(*types), (C.c_int64 * n)(*[g.numel() for g in grads]), n,
+                                         max_norm, addresses, norm.data_ptr(), ws.data_ptr(), size, stream))
+    return norm
+
+
+def bsr_grad_norm(grads):
+    """The norm of all gradients (a list of contiguous bf16 or fp32 tensors) taken together -> fp32 scalar on their GPU."""
+    return _clip(list(grads), 0.0, None)
+
+
+def bsr_clip_grads(grads, max_norm, out=None):
+    """grads (a list of contiguous bf16 or fp32 tensors) times min(1, max_norm / their norm taken together), in place or to `out` (a list of tensors like them)
+    -> the norm before, fp32 scalar on their GPU."""
+    grads = list(grads)
+    return _clip(grads, max_norm, grads if out is None else list(out))
 
 
 _PointerTable = C.c_uint64 * (C.sizeof(bsr_params) // 8)       # a bsr_params, which holds nothing but pointers, by position
@@ -914,6 +1021,11 @@ class Context:
         self._chk(self.lib.bsr_adamw_step(self.ctx, C.byref(gs), C.byref(ms), C.byref(vs), C.c_float(lr),
                                           C.c_float(beta1), C.c_float(beta2), C.c_float(eps),
                                           C.c_float(weight_decay), C.c_int32(step), self._stream()))
+
+    def bsr_clip_grads(self, grads: dict, max_norm: float):
+        """The trainable tensors' gradients brought down to a largest norm, all of them taken together, in place, for bsr_sgd_step or bsr_adamw_step
+        behind it; -> the norm before (a scalar on the GPU)."""
+        return bsr_clip_grads(list(grads.values()), max_norm)
 
     def bsr_profile_begin(self):
         self._chk(self.lib.bsr_profile_begin(self.ctx))

@@ -13,9 +13,11 @@
 
 #include "../../include/bsr.h"
 #include "bsr_internal.h"
+#include "clip.h"
 #include "distill.h"
 #include "fp8.h"
 #include "norm_rows.h"
+#include "rms_rows.h"
 
 using namespace bsr;
 
@@ -1759,6 +1761,7 @@ int32_t bsr_destroy(bsr_ctx* c) {
 
 // ---- operators on the caller's own tensors ------------------------------------------------------------------------------------------
 constexpr int32_t LONGEST_ROW = 1 << 30;            // (a kernel's index may run past the end by a workgroup's stride)
+constexpr int64_t LONGEST_TENSOR = (int64_t)1 << 36;  // (its pieces are counted in 32 bits)
 constexpr int32_t WIDEST_LAYER = 1 << 23;           // (offsets of 32 bits within the rows of a block tile)
 static bool known_type(int32_t t) { return t == BSR_BF16 || t == BSR_FP32; }
 // a matrix with a row stride: there, aligned to its elements, rows that do not overlap
@@ -1957,6 +1960,102 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
   a.stats = const_cast<float*>(stats);
   distill_backward(a, (hipStream_t)stream);
   return check_hip(nullptr, "bsr_distill_backward");
+}
+
+size_t bsr_rmsnorm_workspace_floats(int32_t D) { return D < 1 ? 0 : rms_rows_bwd_floats(D); }
+
+int32_t bsr_rmsnorm_forward(const void* x, int64_t ldx, const void* res, int64_t ldr, int32_t type, int64_t M, int32_t D, const float* gamma, float eps,
+                            void* sum, int64_t lds, void* y, int64_t ldy, void* values, uint8_t* scales, float* rstd, void* stream) {
+  const char* w = "bsr_rmsnorm_forward";
+  if (!known_type(type) || M < 0 || D < 1 || D > LONGEST_ROW) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, D %d", w, type, (long long)M, D);
+  if (!aligned16(gamma)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: gamma is NULL or not 16-byte aligned", w);
+  if (!(eps >= 0.f)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: eps %g (0 or more)", w, eps);
+  if (M == 0) return BSR_OK;
+  if (!values != !scales || (!y && !values)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: y, or values and scales, or all three", w);
+  if (sum && !res) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: sum is that of x and res, there is no res", w);
+  if (!rows_ok(x, type, ldx, D) || (res && !rows_ok(res, type, ldr, D)) || (sum && !rows_ok(sum, type, lds, D)) || (y && !rows_ok(y, type, ldy, D)))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: x, res, sum or y is NULL, misaligned or has rows closer than %d", w, D);
+  if (in_place_apart(M, y, ldy, x, ldx) || in_place_apart(M, sum, lds, x, ldx) || (res && (in_place_apart(M, y, ldy, res, ldr) || in_place_apart(M, sum, lds, res, ldr))))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: y or sum in the place of x or res needs its stride", w);
+  if (sum && sum == y) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: sum and y are one place", w);
+  if ((values && !aligned16(values)) || (rstd && !aligned4(rstd))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: misaligned output", w);
+  RmsRows a;
+  a.x = x; a.ldx = ldx; a.res = res; a.ldr = ldr; a.M = M; a.D = D; a.f32 = type == BSR_FP32; a.gamma = gamma; a.eps = eps;
+  a.sum = sum; a.lds = lds; a.y = y; a.ldy = ldy; a.q = values; a.scale = scales; a.rstd = rstd;
+  rms_rows_fwd(a, (hipStream_t)stream);
+  return check_hip(nullptr, w);
+}
+
+int32_t bsr_rmsnorm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* res, int64_t ldr, int32_t type, int64_t M, int32_t D,
+                             const float* rstd, const float* gamma, void* dx, int64_t lddx, float* dgamma, float* workspace, size_t workspace_floats, void* stream) {
+  const char* w = "bsr_rmsnorm_backward";
+  if (!known_type(type) || M < 0 || D < 1 || D > LONGEST_ROW) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, M %lld, D %d", w, type, (long long)M, D);
+  if (M > 0 && !dx && !dgamma) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dx, or dgamma, or both", w);
+  if (dgamma && (!aligned4(dgamma) || !aligned16(workspace)))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: misaligned dgamma, or workspace NULL or not 16-byte aligned", w);
+  if (dgamma && workspace_floats < rms_rows_bwd_floats(D))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: workspace of %zu floats, %zu are needed", w, workspace_floats, rms_rows_bwd_floats(D));
+  if (!aligned16(gamma)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: gamma is NULL or not 16-byte aligned", w);
+  if (M > 0 && (!rows_ok(dy, type, lddy, D) || !rows_ok(x, type, ldx, D) || (res && !rows_ok(res, type, ldr, D)) || (dx && !rows_ok(dx, type, lddx, D))))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dy, x, res or dx is NULL, misaligned or has rows closer than %d", w, D);
+  if (in_place_apart(M, dx, lddx, dy, lddy) || in_place_apart(M, dx, lddx, x, ldx) || (res && in_place_apart(M, dx, lddx, res, ldr)))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dx in the place of dy, x or res needs its stride", w);
+  if (M > 0 && !aligned4(rstd)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: rstd is NULL or misaligned", w);
+  if (M == 0 && !dgamma) return BSR_OK;
+  RmsRowsBwd a;
+  a.dy = dy; a.x = x; a.res = res; a.lddy = lddy; a.ldx = ldx; a.ldr = ldr; a.M = M; a.D = D; a.f32 = type == BSR_FP32;
+  a.rstd = rstd; a.gamma = gamma; a.dx = dx; a.lddx = lddx; a.dgamma = dgamma; a.partial = workspace;
+  rms_rows_bwd(a, (hipStream_t)stream);
+  return check_hip(nullptr, w);
+}
+
+size_t bsr_clip_workspace_bytes(int32_t count) { return clip_workspace_bytes(count); }
+
+// whether results lie apart: from each other, and from every gradient but the one that they are
+static bool clip_apart(const void* const* grads, const int32_t* types, const int64_t* lengths, int32_t count, void* const* out) {
+  struct Range { uintptr_t from, to; int32_t i; bool result; };
+  std::vector<Range> r;
+  r.reserve(2 * (size_t)count);
+  for (int32_t i = 0; i < count; ++i) {
+    const uintptr_t bytes = (uintptr_t)lengths[i] * (types[i] == BSR_FP32 ? 4 : 2), g = (uintptr_t)grads[i], o = (uintptr_t)out[i];
+    if (bytes == 0) continue;
+    r.push_back({o, o + bytes, i, true});
+    if (g != o) r.push_back({g, g + bytes, i, false});
+  }
+  std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+  uintptr_t result_to = 0, any_to = 0;              // ends of what came before
+  for (const Range& a : r) {
+    if (a.from < (a.result ? any_to : result_to)) return false;
+    any_to = std::max(any_to, a.to);
+    if (a.result) result_to = std::max(result_to, a.to);
+  }
+  return true;
+}
+
+int32_t bsr_clip_grads(const void* const* grads, const int32_t* types, const int64_t* lengths, int32_t count, float max_norm, void* const* out, float* norm,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  const char* w = "bsr_clip_grads";
+  if (count < 1 || !grads || !types || !lengths) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: %d tensors, or a table is NULL", w, count);
+  if (out && !(max_norm >= 0.f)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: max_norm %g (0 or more)", w, max_norm);
+  for (int32_t i = 0; i < count; ++i) {
+    if (!known_type(types[i]) || lengths[i] < 0 || lengths[i] > LONGEST_TENSOR)
+      return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: tensor %d: type %d, %lld values", w, i, types[i], (long long)lengths[i]);
+    const uintptr_t mask = types[i] == BSR_FP32 ? 3 : 1;
+    if (lengths[i] > 0 && (!grads[i] || ((uintptr_t)grads[i] & mask) || (out && (!out[i] || ((uintptr_t)out[i] & mask)))))
+      return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: tensor %d or its result is NULL or misaligned", w, i);
+  }
+  if (out ? norm && !aligned4(norm) : !aligned4(norm)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: norm is NULL or misaligned", w);
+  if (((uintptr_t)workspace & 7) || !workspace || workspace_bytes < clip_workspace_bytes(count))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: workspace NULL, misaligned or of %zu bytes, %zu are needed", w, workspace_bytes, clip_workspace_bytes(count));
+  try {
+    if (out && !clip_apart(grads, types, lengths, count, out)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: a result lies on another one or on another gradient", w);
+  } catch (const std::bad_alloc&) {
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: no host memory for %d tensors", w, count);
+  }
+  ClipArgs a;
+  a.g = grads; a.f32 = types; a.n = lengths; a.count = count; a.out = out; a.max_norm = max_norm; a.norm = norm; a.parts = (double*)workspace;
+  clip(a, (hipStream_t)stream);
+  return check_hip(nullptr, w);
 }
 
 const char* bsr_last_error(const bsr_ctx* c) { return c ? c->err : g_err; }
