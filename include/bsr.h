@@ -587,6 +587,31 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
                              void* stream);
 
 /*
+ * Softmax cross-entropy of a linear layer over many classes, z = x w^T + bias, whose logits are never kept: they are made in tiles, a piece of the classes at a time, and once more
+ * for the gradients.  Per row loss = log sum exp z - z_label; with g = grad_scale * row_grad[row] and G = g (softmax(z) - onehot(label)):
+ *   dx = G w,   dw = G^T x,   db = sum over rows of G
+ * A row whose label lies outside 0 .. classes-1 has loss 0 and counts for no gradient (its dx is 0), whatever its x holds; so does, for the gradients, one of weight 0.  A class with
+ * bias -inf has probability 0; a row whose logits are all -inf has loss and gradient 0, one whose label's is has loss +inf and a finite gradient.  NaN and +inf in z make a row NaN, and with it dw.
+ * bf16 x and w are multiplied as they are; G is held in 11 bits (fp16, off by 2^-11 of itself, or by 2^-39 where it is below 2^-28), x and w beside it exactly down to 2^-29 of a feature's
+ * largest value (with row_grad x in 11 bits too).  fp32 values are held in two terms of 11 bits each, off by 2^-22 of themselves, or by 2^-39 of the largest of their row, or of their feature, where they are below 2^-17 of it.  Sums
+ * are fp32.
+ *   x            [rows, width] of `type`, stride ldx;  w [classes, width] of `type`, stride ldw (a row for each class)
+ *   bias         fp32 [classes], may be NULL;  labels int32 [rows]
+ *   loss         fp32 [rows], may be NULL with stats
+ *   stats        fp32 [rows, 2], 8-byte aligned: max z and log sum exp(z - max z), what the backward needs; may be NULL with loss
+ *   row_grad     fp32 [rows], may be NULL (1 for every row)
+ *   dx           [rows, width] of `type`, stride lddx;  dw [classes, width], stride lddw, of dw_type: BSR_FP32, or BSR_BF16 where w is;  db fp32 [classes];  each may be NULL
+ *   workspace    device scratch of bsr_linear_ce_workspace_bytes() bytes, 256-byte aligned
+ * Limits: rows up to 2^23, width up to 2^20, their product up to 2^33; classes up to 2^30.
+ */
+size_t bsr_linear_ce_workspace_bytes(int32_t type, int64_t rows, int32_t width, int32_t classes, int32_t backward);
+int32_t bsr_linear_ce_forward(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t type, int64_t rows, int32_t width, int32_t classes, const float* bias,
+                              const int32_t* labels, float* loss, float* stats, void* workspace, size_t workspace_bytes, void* stream);
+int32_t bsr_linear_ce_backward(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t type, int64_t rows, int32_t width, int32_t classes, const float* bias,
+                               const int32_t* labels, const float* stats, const float* row_grad, float grad_scale, void* dx, int64_t lddx, void* dw, int64_t lddw, int32_t dw_type,
+                               float* db, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The norm of many gradients taken together, and the gradients brought down to a largest norm: norm = sqrt(sum over tensors and values of g^2),
  * out = g min(1, max_norm / norm).  Squares and their sum are fp64.  A norm that is infinite or no number is given as it is and scales nothing.
  *   grads, types, lengths  host arrays of `count` (1 or more) entries: device address (aligned to the values), BSR_BF16 or BSR_FP32, values (0 .. 2^36; any address

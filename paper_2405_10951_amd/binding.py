@@ -138,6 +138,8 @@ def load_library():
             "bsr_layernorm_backward": (p, i64, p, i64, p, i64, i32, i64, i32, p, p, p, p, i64, p, p, p, C.c_size_t, p),
             "bsr_rmsnorm_forward": (p, i64, p, i64, i32, i64, i32, p, f32, p, i64, p, i64, p, p, p, p),
             "bsr_rmsnorm_backward": (p, i64, p, i64, p, i64, i32, i64, i32, p, p, p, i64, p, p, C.c_size_t, p),
+            "bsr_linear_ce_forward": (p, i64, p, i64, i32, i64, i32, i32, p, p, p, p, p, C.c_size_t, p),
+            "bsr_linear_ce_backward": (p, i64, p, i64, i32, i64, i32, i32, p, p, p, p, f32, p, i64, p, i64, i32, p, p, C.c_size_t, p),
             "bsr_clip_grads": (p, p, p, i32, f32, p, p, p, C.c_size_t, p),
             "bsr_quantize8_rows": (p, i32, i64, i32, i64, p, p, p),
             "bsr_quantize8_weight": (p, i32, i32, i32, i64, p, p, p, p, p),
@@ -149,6 +151,7 @@ def load_library():
     lib.bsr_block8_strides.restype, lib.bsr_block8_strides.argtypes = None, (i32, p, p)
     lib.bsr_layernorm_workspace_floats.restype, lib.bsr_layernorm_workspace_floats.argtypes = C.c_size_t, (i32,)
     lib.bsr_rmsnorm_workspace_floats.restype, lib.bsr_rmsnorm_workspace_floats.argtypes = C.c_size_t, (i32,)
+    lib.bsr_linear_ce_workspace_bytes.restype, lib.bsr_linear_ce_workspace_bytes.argtypes = C.c_size_t, (i32, i64, i32, i32, i32)
     lib.bsr_clip_workspace_bytes.restype, lib.bsr_clip_workspace_bytes.argtypes = C.c_size_t, (i32,)
     lib.bsr_distill_workspace_floats.restype, lib.bsr_distill_workspace_floats.argtypes = C.c_size_t, (i32, i64, i32)
     lib.bsr_linear8_workspace_bytes.restype, lib.bsr_linear8_workspace_bytes.argtypes = C.c_size_t, (i32, i32)
@@ -796,6 +799,70 @@ def bsr_distill_backward(z, index, logits, stats, row_grad=None, labels=None, te
     pg, dz, ldd = _distill_dz(z, row_grad, dz)
     _check(load_library().bsr_distill_backward(*args, ps, pg, grad_scale, dz.data_ptr(), ldd, stream))
     return dz
+
+
+def _linear_ce_args(x, w, labels, bias):
+    """-> the arguments that both calls begin with"""
+    import torch
+    ldx, code = _rows_of(x, "x"), _type_code(x, "x")
+    ldw = _rows_of(w, "w", dtype=x.dtype)
+    rows, width = x.shape
+    classes = w.shape[0]
+    if w.shape[1] != width:
+        raise ValueError(f"w: {w.shape[1]} columns, x has {width}")
+    _in_32_bits(classes, "w: rows")
+    pb = None if bias is None else _flat(bias, "bias", (classes,), torch.float32)
+    return x.data_ptr(), ldx, w.data_ptr(), ldw, code, rows, width, classes, pb, _flat(labels, "labels", (rows,), torch.int32)
+
+
+def _linear_ce_workspace(x, args, backward):
+    """-> (scratch or None, its bytes); torch's allocations are aligned to 512 bytes"""
+    import torch
+    size = _scratch_size("bsr_linear_ce_workspace_bytes", *args[4:8], backward)
+    return (x.new_empty(size, dtype=torch.uint8), size) if size else (None, 0)
+
+
+def bsr_linear_ce_forward(x, w, labels, bias=None):
+    """Cross-entropy of the logits x w^T + bias, which nobody keeps: x [rows,width] bf16 or fp32, w [classes,width] of the same type (any row strides), labels [rows] int32 (-1: the row
+    counts for nothing), bias [classes] fp32 -> (loss [rows], stats [rows,2] for bsr_linear_ce_backward)."""
+    import torch
+    stream = _together(x, w, labels, bias)
+    args = _linear_ce_args(x, w, labels, bias)
+    f32 = torch.float32
+    loss, stats = x.new_empty(x.shape[0], dtype=f32), x.new_empty((x.shape[0], 2), dtype=f32)
+    ws, size = _linear_ce_workspace(x, args, 0)
+    _check(load_library().bsr_linear_ce_forward(*args, loss.data_ptr(), stats.data_ptr(), _dp(ws), size, stream))
+    return loss, stats
+
+
+def bsr_linear_ce_backward(x, w, labels, stats, bias=None, row_grad=None, grad_scale=1.0, dx=None, dw=None, need_dx=True, need_dw=True, need_db=True):
+    """The gradients of grad_scale * sum(row_grad * loss) (row_grad [rows] fp32, None: 1 for each) from the stats of the forward -> (dx [rows,width] | None, dw [classes,width] | None,
+    db [classes] | None).  dw is of the type of w, or fp32 where a tensor of that type is given; there is no db without a bias."""
+    import torch
+    stream = _together(x, w, labels, bias, stats, row_grad, dx, dw)
+    args = _linear_ce_args(x, w, labels, bias)
+    f32 = torch.float32
+    ps = _flat(stats, "stats", (x.shape[0], 2), f32)
+    pg = None if row_grad is None else _flat(row_grad, "row_grad", (x.shape[0],), f32)
+    lddx = lddw = x.shape[1]
+    if dx is not None:
+        lddx = _rows_of(dx, "dx", x.shape, x.dtype)
+    elif need_dx:
+        dx = _like(x)
+    if dw is not None:
+        lddw = _rows_of(dw, "dw", w.shape)
+    elif need_dw:
+        dw = _like(w)
+    db = None if bias is None or not need_db else bias.new_empty(w.shape[0])
+    ws, size = _linear_ce_workspace(x, args, 1)
+    _check(load_library().bsr_linear_ce_backward(*args, ps, pg, grad_scale, _dp(dx), lddx, _dp(dw), lddw, 0 if dw is None else _type_code(dw, "dw"), _dp(db), _dp(ws), size, stream))
+    return dx, dw, db
+
+
+def bsr_linear_ce_forward_backward(x, w, labels, bias=None, row_grad=None, grad_scale=1.0, dx=None, dw=None, need_dx=True, need_dw=True, need_db=True):
+    """-> (loss [rows], dx, dw, db), both calls one after the other."""
+    loss, stats = bsr_linear_ce_forward(x, w, labels, bias)
+    return loss, *bsr_linear_ce_backward(x, w, labels, stats, bias, row_grad, grad_scale, dx, dw, need_dx, need_dw, need_db)
 
 
 def _clip(grads, max_norm, out):

@@ -1,0 +1,24 @@
+// Softmax cross-entropy of a linear layer whose logits nobody keeps, and its gradients (k_linear_ce.hip): raw device pointers and a stream, no allocation, no wait.
+#pragma once
+#include "bsr_internal.h"
+
+namespace bsr {
+
+struct LinearCe {
+  const void* x = nullptr; int64_t ldx = 0; int N = 0;          // [N, D]
+  const void* w = nullptr; int64_t ldw = 0; int V = 0, D = 0;   // [V, D]
+  bool f32 = false;                                             // type of x, w and dx
+  const float* bias = nullptr;                                  // [V]; null: none
+  const int32_t* labels = nullptr;                              // [N], outside 0 .. V - 1: the row counts for nothing
+  float *loss = nullptr, *stats = nullptr;                      // forward: [N], [N, 2]; either may be null.  Backward: stats is read
+  const float* row_grad = nullptr; float grad_scale = 1.f;      // [N], null: 1 for each
+  void* dx = nullptr; int64_t lddx = 0;                         // null: not wanted
+  void* dw = nullptr; int64_t lddw = 0; bool dw_f32 = false;    // null: not wanted
+  float* db = nullptr;                                          // [V]; null: not wanted
+  void* workspace = nullptr;                                    // 256-byte aligned
+};
+size_t linear_ce_workspace_bytes(bool f32, int N, int D, int V, bool backward);
+void linear_ce_forward(const LinearCe& a, hipStream_t s);
+void linear_ce_backward(const LinearCe& a, hipStream_t s);
+
+}  // namespace bsr
