@@ -30,14 +30,14 @@ constexpr int BK = 64;
 constexpr int G_SHIFT = 14;                        // G is kept times 2^14
 
 // ------------------------------------------------------------------------------------------ the products
-enum Mode { STATS, GRAD, OUT };
+enum Mode { STATS, GRAD };
 
 // C(m,n) = sum_k A(m,k) B(n,k): rows of 64-element k-tiles, whole ones, 16-byte aligned.  SEG = 3: two terms each, ta and tb elements apart, products h h, h l, l h.
 struct CeGemm {
   const void *A = nullptr, *B = nullptr;
   int64_t lda = 0, ldb = 0, ta = 0, tb = 0;
   int M = 0, N = 0, nk = 0;                        // nk: k-tiles of a term
-  int splits = 1, per = 0;                         // workgroups over the k-tiles of a tile, k-tiles (of all terms) of each
+  int splits = 1, per = 0;                         // products of G: workgroups over the k-tiles of a tile, k-tiles (of all terms) of each
   const int *ea = nullptr, *eb = nullptr;          // powers of two of A's and B's rows, null: 0
   // STATS, GRAD: m is a token, n a class of the piece that begins at class v0
   const float* bias = nullptr;                     // of the piece
@@ -47,19 +47,19 @@ struct CeGemm {
   const float2* stats = nullptr; const float* row_grad = nullptr;          // GRAD: [M] maximum, log of the sum; weights or null
   f16 *G = nullptr, *GT = nullptr;                 // GRAD: [terms][M][ldg], [terms][N][ldgt], columns behind the last one zero; null: not wanted
   int64_t ldg = 0, ldgt = 0, tg = 0, tgt = 0;
-  float* dbp = nullptr;                            // GRAD: [tile of tokens][N] sums of g G; null: not wanted
-  // OUT
+  float* dbp = nullptr; int64_t ldd = 0;           // GRAD: [tile of tokens][ldd] sums of g G; null: not wanted
+  // products of G
   float* part = nullptr; int64_t ldp = 0, tp = 0; bool add = false;        // [split][M][ldp] fp32 (of what was there as well)
-  void* out = nullptr; int64_t ldo = 0; bool out_f32 = false, out_vec = false;   // or the result itself: times scale and, where given, its row's weight
-  float scale = 1.f; const float* row_scale = nullptr;
+  void* out = nullptr; int64_t ldo = 0; bool out_f32 = false, out_vec = false;   // or the result itself, times scale
+  float scale = 1.f;
 };
 
 template <int BM_, int BN_, int WM_, int WN_, int NST_> struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NST = NST_, NT = WM * WN * 64;
   static constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 32, NI = TN / 32;
   static constexpr size_t stages = (size_t)NST * (BM + BN) * 128;
-  static constexpr int LDT = TM * 2 + 16, LDR = TN * 2 + 16, LDF = TN * 4 + 16;           // patch rows in bytes
-  static constexpr int patch = TN * LDT > 32 * LDF ? TN * LDT : 32 * LDF;                  // of a wavefront
+  static constexpr int LDR = TN * 2 + 16, LDF = TN * 4 + 16;     // patch rows in bytes: fp16, fp32
+  static constexpr int patch = 32 * (2 * LDR > LDF ? 2 * LDR : LDF);                       // of a wavefront: 32 rows, of one or two terms
   static constexpr size_t lds = stages > (size_t)patch * WM * WN ? stages : (size_t)patch * WM * WN;
 };
 typedef Shape<256, 256, 2, 4, 2> Large;
@@ -207,224 +207,296 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
   wait_lgkmcnt0();
 }
 
-template <class S, Mode MODE, bool F16, int SEG>
-__global__ __launch_bounds__(S::NT, S::lds <= 80 * 1024 ? S::NT / 128 : 1) void ce_kernel(CeGemm g, int mt, int nt) {
-  constexpr int MI = S::MI, NI = S::NI, TM = S::TM, TN = S::TN;
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN, wn = wave % S::WN;
-  const int lm = lane & 31, lh = lane >> 5;
-  const int id = xcd_remap(blockIdx.x, gridDim.x), split = MODE == OUT ? id / (mt * nt) : 0;
-  int tm, tn;
-  tile_at(MODE == OUT ? id - split * mt * nt : id, mt, nt, tm, tn);
-  const int m0 = tm * S::BM, n0 = tn * S::BN;
-  const int kt0 = MODE == OUT ? split * g.per : 0, nk = MODE == OUT ? min(g.per, SEG * g.nk - kt0) : m0 < g.M ? SEG * g.nk : 0;      // (tokens that only fill GT's last k-tile: zeros)
-  f32x16 acc[MI][NI];
-  multiply<S, F16, SEG>(g, m0, n0, kt0, nk, smem, acc);
-  __syncthreads();
-  unsigned char* patch = smem + wave * S::patch;
-  const int row0 = m0 + wm * TM, col0 = n0 + wn * TN;
+template <class S> struct Wave {                   // where a wavefront's part of a tile lies
+  int lane, lm, lh, wm, wn, row0, col0;
+  __device__ __forceinline__ Wave(int m0, int n0) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lane = threadIdx.x & 63; lm = lane & 31; lh = lane >> 5; wm = wave / S::WN; wn = wave % S::WN;
+    row0 = m0 + wm * S::TM; col0 = n0 + wn * S::TN;
+  }
+  // column (in the wavefront's part) of element r of acc[..][ni]
+  __device__ __forceinline__ int col(int ni, int r) const { return ni * 32 + 8 * (r / 4) + 4 * lh + r % 4; }
+  __device__ __forceinline__ unsigned char* patch(unsigned char* smem) const { return smem + (wm * S::WN + wn) * S::patch; }
+};
 
-  if constexpr (MODE == STATS || MODE == GRAD) {
-    // a lane has 16 NI classes of MI tokens: what belongs to the classes, once
-    float b[NI][16];
-    int e[F16 ? NI : 1][16];
+// bias and powers of two of a lane's 16 NI classes; classes past the last one: -inf
+template <class S, bool F16> struct Classes {
+  float b[S::NI][16];
+  int e[F16 ? S::NI : 1][16];
+  bool edge;                                       // some lie past the last one (of the whole wavefront)
+  __device__ __forceinline__ Classes(const CeGemm& g, const Wave<S>& w) {
+    edge = w.col0 + S::TN > g.N;
+#pragma unroll
+    for (int ni = 0; ni < S::NI; ++ni)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int n = w.col0 + w.col(ni, r), nc = min(n, g.N - 1);
+        b[ni][r] = g.bias ? g.bias[nc] : 0.f;
+        if constexpr (F16) e[ni][r] = g.eb[nc];
+      }
+  }
+  __device__ __forceinline__ float logit(float acc, int ea, int ni, int r) const {
+    if constexpr (F16) acc = ldexpf(acc, ea + e[ni][r]);
+    return acc + b[ni][r];
+  }
+};
+
+constexpr float LOG2E = 1.4426950408889634f;
+__device__ __forceinline__ float2 joined(float2 p, float2 q) {   // two maxima with their sums of exp(z - maximum)
+  const float most = fmaxf(p.x, q.x), ref = most == -INFINITY ? 0.f : most;
+  return make_float2(most, p.y * __expf(p.x - ref) + q.y * __expf(q.x - ref));
+}
+
+// Forward: a row's maximum and sum over the tile's classes.  (fmaxf passes NaN over, the sum does not; a row of -inf alone has sum 0.)
+template <class S, bool F16>
+__device__ __forceinline__ void end_stats(const CeGemm& g, f32x16 (&acc)[S::MI][S::NI], int m0, int n0, int tn, unsigned char* smem) {
+  const Wave<S> w(m0, n0);
+  const Classes<S, F16> cl(g, w);
+  float2* red = (float2*)smem;                     // [WN][BM]
+#pragma unroll
+  for (int mi = 0; mi < S::MI; ++mi) {
+    const int m = w.row0 + mi * 32 + w.lm;
+    const int at = m < g.M ? max(g.labels[m], -1) - g.v0 - w.col0 : -1, ea = F16 && m < g.M ? g.ea[m] : 0;
+    float most = -INFINITY;
+#pragma unroll
+    for (int ni = 0; ni < S::NI; ++ni)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[mi][ni][r] = cl.logit(acc[mi][ni][r], ea, ni, r);
+    if (cl.edge)                                   // (whatever the product of a repeated row is, it does not count)
+#pragma unroll
+      for (int ni = 0; ni < S::NI; ++ni)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (w.col0 + w.col(ni, r) >= g.N) acc[mi][ni][r] = -INFINITY;
+#pragma unroll
+    for (int ni = 0; ni < S::NI; ++ni)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) most = fmaxf(most, acc[mi][ni][r]);
+    if (__any(at >= 0 && at < S::TN))              // (few wavefronts hold a label)
+#pragma unroll
+      for (int ni = 0; ni < S::NI; ++ni)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (at == w.col(ni, r) && at + w.col0 < g.N) g.zlabel[m] = acc[mi][ni][r];
+    most = half_max(most);
+    const float ref = most == -INFINITY ? 0.f : most;
+    float s = 0.f;
+#pragma unroll
+    for (int ni = 0; ni < S::NI; ++ni)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[mi][ni][r] - ref) * LOG2E);
+    s = half_sum(s);
+    if (w.lh == 0) red[w.wn * S::BM + w.wm * S::TM + mi * 32 + w.lm] = make_float2(most, s);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < S::BM && m0 + i < g.M; i += S::NT) {
+    float2 p = red[i];
+#pragma unroll
+    for (int j = 1; j < S::WN; ++j) p = joined(p, red[j * S::BM + i]);
+    g.parts[(int64_t)tn * g.M + m0 + i] = p;
+  }
+}
+
+// sums of 32 (or 16) values over the 32 lanes of each half of the wavefront: lane l of a half gets that of value l (l % 16).  Each step halves the values a lane holds
+template <int N> __device__ __forceinline__ float half_sums(float (&v)[N]) {
+  static_assert(N == 32 || N == 16, "");
+  const int l = threadIdx.x;
+  if constexpr (N == 32) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {                 // (swapping rows of 16 lanes leaves both addends of the value that stays)
+      const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 16]), false, false);
+      v[i] = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+      v[i] = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (l & 8 ? v[i + 8] : v[i]) + dpp_move<0x128>(l & 8 ? v[i] : v[i + 8]);          // lane ^ 8
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (l & 4 ? v[i + 4] : v[i]) + dpp_move<0x141>(l & 4 ? v[i] : v[i + 4]);          // lane ^ 7, which holds the same values so far
+#pragma unroll
+  for (int i = 0; i < 2; ++i) v[i] = (l & 2 ? v[i + 2] : v[i]) + dpp_move<0x4E>(l & 2 ? v[i] : v[i + 2]);           // lane ^ 2
+  return (l & 1 ? v[1] : v[0]) + dpp_move<0xB1>(l & 1 ? v[0] : v[1]);                                              // lane ^ 1
+}
+
+// Backward: the tile as G, in fp16 times 2^14, rows of 32 tokens at a time through a patch of LDS, from which rows are read as they lie and, with the transposing reads, columns
+template <class S, bool F16, int SEG, bool DB>
+__device__ __forceinline__ void end_grad(const CeGemm& g, f32x16 (&acc)[S::MI][S::NI], int m0, int n0, int tm, unsigned char* smem) {
+  constexpr int NI = S::NI, TERMS = SEG == 3 ? 2 : 1, TERM = 32 * S::LDR;
+  const Wave<S> w(m0, n0);
+  const Classes<S, F16> cl(g, w);
+  unsigned char* patch = w.patch(smem);
+  float sum[DB ? NI * 16 : 1];
+  if constexpr (DB)
+#pragma unroll
+    for (int i = 0; i < NI * 16; ++i) sum[i] = 0.f;
+#pragma unroll
+  for (int mi = 0; mi < S::MI; ++mi) {
+    const int m = w.row0 + mi * 32 + w.lm, mc = min(m, g.M - 1);
+    const int label = max(g.labels[mc], -1), ea = F16 ? g.ea[mc] : 0, at = label - g.v0 - w.col0;
+    const float2 st = g.stats[mc];
+    const float weight = g.row_grad ? g.row_grad[mc] : 1.f;
+    // (label: of the whole layer; a row of logits that are all -inf has no gradient; of those that are all NaN the logarithm is NaN)
+    const bool counts = m < g.M && label >= 0 && label < g.classes && weight != 0.f && !(st.x == -INFINITY && st.y == 0.f);
+    const float c = fmaf(st.y, -LOG2E, (float)G_SHIFT);
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int n = col0 + ni * 32 + 8 * (r / 4) + 4 * lh + r % 4;
-        b[ni][r] = n < g.N ? (g.bias ? g.bias[n] : 0.f) : -INFINITY;
-        if constexpr (F16) e[ni][r] = n < g.N ? g.eb[n] : 0;
-      }
-    if constexpr (MODE == STATS) {
-      float2* red = (float2*)smem;                 // [WN][BM]
-#pragma unroll
-      for (int mi = 0; mi < MI; ++mi) {
-        const int m = row0 + mi * 32 + lm;
-        const int at = m < g.M ? max(g.labels[m], -1) - g.v0 - col0 : -1, ea = F16 && m < g.M ? g.ea[m] : 0;
-        float most = -INFINITY, zl = 0.f;
-        bool mine = false;
-#pragma unroll
-        for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            float z = acc[mi][ni][r];
-            if constexpr (F16) z = ldexpf(z, ea + e[ni][r]);
-            z += b[ni][r];
-            // (a class past the last one: whatever the product of a repeated row is, it does not count)
-            if (b[ni][r] == -INFINITY && col0 + ni * 32 + 8 * (r / 4) + 4 * lh + r % 4 >= g.N) z = -INFINITY;
-            acc[mi][ni][r] = z;
-            most = fmaxf(most, z);
-            const bool here = at == ni * 32 + 8 * (r / 4) + 4 * lh + r % 4;
-            zl = here ? z : zl;
-            mine |= here;
-          }
-        most = half_max(most);
-        const float ref = most == -INFINITY ? 0.f : most;
-        float s = 0.f;
-#pragma unroll
-        for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s += __expf(acc[mi][ni][r] - ref);
-        s = half_sum(s);
-        if (lh == 0) red[wn * S::BM + wm * TM + mi * 32 + lm] = make_float2(most, s);
-        if (mine && at + col0 < g.N) g.zlabel[m] = zl;
-      }
-      __syncthreads();
-      for (int i = threadIdx.x; i < S::BM && m0 + i < g.M; i += S::NT) {
-        float2 p = red[i];
-#pragma unroll
-        for (int j = 1; j < S::WN; ++j) {
-          const float2 q = red[j * S::BM + i];
-          const float most = fmaxf(p.x, q.x), ref = most == -INFINITY ? 0.f : most;
-          p = make_float2(most, p.y * __expf(p.x - ref) + q.y * __expf(q.x - ref));
-        }
-        g.parts[(int64_t)tn * g.M + m0 + i] = p;
-      }
-    } else {
-      constexpr int TERMS = SEG == 3 ? 2 : 1;
-      f16x4 t[TERMS][MI][NI][4];
-      float sum[NI][16];
+      for (int r = 0; r < 16; ++r) acc[mi][ni][r] = __builtin_amdgcn_exp2f(fmaf(cl.logit(acc[mi][ni][r], ea, ni, r) - st.x, LOG2E, c));
+    if (__any(at >= 0 && at < S::TN))              // (few wavefronts hold a label)
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum[ni][r] = 0.f;
+        for (int r = 0; r < 16; ++r) acc[mi][ni][r] -= at == w.col(ni, r) ? (float)(1 << G_SHIFT) : 0.f;
+    if (!__all(counts) || cl.edge)
 #pragma unroll
-      for (int mi = 0; mi < MI; ++mi) {
-        const int m = row0 + mi * 32 + lm, mc = min(m, g.M - 1);
-        const int label = g.labels[mc], ea = F16 ? g.ea[mc] : 0, at = max(label, -1) - g.v0 - col0;
-        const float2 st = g.stats[mc];
-        const float weight = g.row_grad ? g.row_grad[mc] : 1.f;
-        // (label: of the whole layer; a row of logits that are all -inf has no gradient; of those that are all NaN the logarithm is NaN)
-        const bool counts = m < g.M && label >= 0 && label < g.classes && weight != 0.f && !(st.x == -INFINITY && st.y == 0.f);
+      for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-        for (int ni = 0; ni < NI; ++ni)
+        for (int r = 0; r < 16; ++r) acc[mi][ni][r] = counts && w.col0 + w.col(ni, r) < g.N ? acc[mi][ni][r] : 0.f;
+    if constexpr (DB)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int c = ni * 32 + 8 * (r / 4) + 4 * lh + r % 4;
-            float z = acc[mi][ni][r];
-            if constexpr (F16) z = ldexpf(z, ea + e[ni][r]);
-            z += b[ni][r];
-            float p = __expf((z - st.x) - st.y) - (at == c ? 1.f : 0.f);
-            p = counts && col0 + c < g.N ? p : 0.f;
-            sum[ni][r] += weight * p;
-            p *= (float)(1 << G_SHIFT);
-            const f16 h = (f16)p;
-            t[0][mi][ni][r / 4][r % 4] = h;
-            if constexpr (TERMS == 2) t[TERMS - 1][mi][ni][r / 4][r % 4] = (f16)(p - (float)h);
-          }
-      }
-      (void)sum;
+      for (int i = 0; i < NI * 16; ++i) sum[i] = counts ? fmaf(weight, acc[mi][i / 16][i % 16], sum[i]) : sum[i];
 #pragma unroll
-      for (int term = 0; term < TERMS; ++term) {
-        if (g.GT) {
+    for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-          for (int mi = 0; mi < MI; ++mi)
+      for (int q = 0; q < 4; ++q) {
+        f16x4 h, l;
 #pragma unroll
-            for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                *(f16*)(patch + (ni * 32 + 8 * (r / 4) + 4 * lh + r % 4) * S::LDT + (mi * 32 + lm) * 2) = t[term][mi][ni][r / 4][r % 4];
-          wave_fence();
-          constexpr int CPR = TM / 8, RPP = 64 / CPR;            // 16-byte chunks of a patch row, rows at a time
-          f16* to = g.GT + term * g.tgt;
-          const int c = lane % CPR;
-#pragma unroll 4
-          for (int p = 0; p < TN / RPP; ++p) {
-            const int r = p * RPP + lane / CPR, n = col0 + r, m = row0 + c * 8;
-            if (n < g.N && m < g.ldgt) *(f16x8*)(to + (int64_t)n * g.ldgt + m) = *(const f16x8*)(patch + r * S::LDT + c * 16);
-          }
-          wave_fence();
+        for (int j = 0; j < 4; ++j) {
+          const float p = acc[mi][ni][4 * q + j];
+          h[j] = (f16)p;
+          if constexpr (TERMS == 2) l[j] = (f16)(p - (float)h[j]);
         }
-        if (g.G) {
-          constexpr int CPR = TN / 8, RPP = 64 / CPR;
-          f16* to = g.G + term * g.tg;
-          const int c = lane % CPR;
+        unsigned char* to = patch + w.lm * S::LDR + (ni * 32 + 8 * q + 4 * w.lh) * 2;
+        *(f16x4*)to = h;
+        if constexpr (TERMS == 2) *(f16x4*)(to + TERM) = l;
+      }
+    wave_fence();
 #pragma unroll
-          for (int mi = 0; mi < MI; ++mi) {
+    for (int term = 0; term < TERMS; ++term) {
+      if (g.G) {
+        constexpr int CPR = S::TN / 8, RPP = 64 / CPR;           // 16-byte chunks of a patch row, rows at a time
+        const int k = w.lane % CPR, n = w.col0 + k * 8;
+        f16* to = g.G + term * g.tg;
 #pragma unroll
-            for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-              for (int q = 0; q < 4; ++q) *(f16x4*)(patch + lm * S::LDR + (ni * 32 + 8 * q + 4 * lh) * 2) = t[term][mi][ni][q];
-            wave_fence();
-#pragma unroll
-            for (int p = 0; p < 32 / RPP; ++p) {
-              const int r = p * RPP + lane / CPR, m = row0 + mi * 32 + r, n = col0 + c * 8;
-              if (m < g.M && n < g.ldg) *(f16x8*)(to + (int64_t)m * g.ldg + n) = *(const f16x8*)(patch + r * S::LDR + c * 16);
-            }
-            wave_fence();
-          }
+        for (int p = 0; p < 32 / RPP; ++p) {
+          const int r = p * RPP + w.lane / CPR, row = w.row0 + mi * 32 + r;
+          if (row < g.M && n < g.ldg) *(f16x8*)(to + (int64_t)row * g.ldg + n) = *(const f16x8*)(patch + term * TERM + r * S::LDR + k * 16);
         }
       }
-      if (g.dbp) {
-        // sums over the tile's tokens: the 32 lanes of a half, then the wavefronts, in order
-        __syncthreads();
-        float* red = (float*)smem;                 // [WM][BN]
+      if (g.GT) {
+        // 16 lanes read 4 tokens x 16 classes (lane 4 e + q names the address of classes 4 q .. of token e) and get a class each, four tokens of it; two such reads are 16 bytes of GT
+        const int j = w.lane & 15, octet = w.lane >> 4, token = w.row0 + mi * 32 + octet * 8;
+        const unsigned char* from = patch + term * TERM + (octet * 8 + (j >> 2)) * S::LDR + (j & 3) * 8;
+        f16* to = g.GT + term * g.tgt;
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
 #pragma unroll
-        for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            float v = sum[ni][r];
-#pragma unroll
-            for (int d = 16; d > 0; d /= 2) v += __shfl_xor(v, d);
-            if (lm == 0) red[wm * S::BN + wn * TN + ni * 32 + 8 * (r / 4) + 4 * lh + r % 4] = v;
-          }
-        __syncthreads();
-        for (int i = threadIdx.x; i < S::BN && n0 + i < g.N; i += S::NT) {
-          float v = red[i];
-#pragma unroll
-          for (int j = 1; j < S::WM; ++j) v += red[j * S::BN + i];
-          g.dbp[(int64_t)tm * g.N + n0 + i] = v;
+        for (int cb = 0; cb < S::TN / 16; ++cb) {
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(from + cb * 32));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(from + cb * 32 + 4 * S::LDR));
+          const int n = w.col0 + cb * 16 + j;
+          if (n < g.N && token < g.ldgt) *(s16x8*)(to + (int64_t)n * g.ldgt + token) = s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         }
       }
     }
-  } else {
-    constexpr int CPR = TN / 4, RPP = 64 / CPR;                  // 4-column chunks of a patch row, rows at a time
-    const int c = lane % CPR, n = col0 + c * 4;
-    int e[4];
+    wave_fence();
+  }
+  if constexpr (DB) {
+    // sums over the tile's tokens: the lanes of each half, then the wavefronts in order
+    const float v = half_sums<NI * 16>(sum);
+    __syncthreads();
+    float* red = (float*)smem;                     // [WM][BN]
+    if (NI == 2 || w.lm < 16) red[w.wm * S::BN + w.wn * S::TN + w.col(w.lm / 16, w.lm % 16)] = v;
+    __syncthreads();
+    for (int i = threadIdx.x; i < S::BN && n0 + i < g.N; i += S::NT) {
+      float t = red[i];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) e[j] = (n + j < g.N ? g.eb[n + j] : 0) - G_SHIFT;
+      for (int j = 1; j < S::WM; ++j) t += red[j * S::BN + i];
+      g.dbp[tm * g.ldd + n0 + i] = ldexpf(t, -G_SHIFT);
+    }
+  }
+}
+
+template <class S, Mode MODE, bool F16, int SEG, bool DB>
+__global__ __launch_bounds__(S::NT, 1) void ce_logits_kernel(CeGemm g, int mt, int nt) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  int tm, tn;
+  tile_at(xcd_remap(blockIdx.x, gridDim.x), mt, nt, tm, tn);
+  const int m0 = tm * S::BM, n0 = tn * S::BN;
+  f32x16 acc[S::MI][S::NI];
+  multiply<S, F16, SEG>(g, m0, n0, 0, m0 < g.M ? SEG * g.nk : 0, smem, acc);      // (tokens that only fill GT's last k-tile: zeros)
+  __syncthreads();
+  if constexpr (MODE == STATS) end_stats<S, F16>(g, acc, m0, n0, tn, smem);
+  else end_grad<S, F16, SEG, DB>(g, acc, m0, n0, tm, smem);
+}
+
+// Up to two products of G in one launch (a, then b, na workgroups of the first): dx and dw of a piece fill the CUs together
+template <class S, int SEG>
+__global__ __launch_bounds__(S::NT, 1) void ce_grads_kernel(CeGemm a, CeGemm b, int na) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const bool first = (int)blockIdx.x < na;
+  CeGemm g;
+  if (first) g = a;
+  else g = b;
+  const int mt = (g.M + S::BM - 1) / S::BM, nt = (g.N + S::BN - 1) / S::BN, here = first ? na : (int)gridDim.x - na;
+  const int id = xcd_remap(first ? blockIdx.x : blockIdx.x - na, here), split = id / (mt * nt);
+  int tm, tn;
+  tile_at(id - split * mt * nt, mt, nt, tm, tn);
+  const int m0 = tm * S::BM, n0 = tn * S::BN, kt0 = split * g.per;
+  f32x16 acc[S::MI][S::NI];
+  multiply<S, true, SEG>(g, m0, n0, kt0, min(g.per, SEG * g.nk - kt0), smem, acc);
+  __syncthreads();
+  const Wave<S> w(m0, n0);
+  unsigned char* patch = w.patch(smem);
+  constexpr int CPR = S::TN / 4, RPP = 64 / CPR;                 // 4-column chunks of a patch row, rows at a time
+  const int c = w.lane % CPR, n = w.col0 + c * 4;
+  int e[4];
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) {
+  for (int j = 0; j < 4; ++j) e[j] = (n + j < g.N ? g.eb[n + j] : 0) - G_SHIFT;
 #pragma unroll
-      for (int ni = 0; ni < NI; ++ni)
+  for (int mi = 0; mi < S::MI; ++mi) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          *(f32x4*)(patch + lm * S::LDF + (ni * 32 + 8 * q + 4 * lh) * 4) = f32x4{acc[mi][ni][4 * q], acc[mi][ni][4 * q + 1], acc[mi][ni][4 * q + 2], acc[mi][ni][4 * q + 3]};
-      wave_fence();
+    for (int ni = 0; ni < S::NI; ++ni)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(f32x4*)(patch + w.lm * S::LDF + (ni * 32 + 8 * q + 4 * w.lh) * 4) = f32x4{acc[mi][ni][4 * q], acc[mi][ni][4 * q + 1], acc[mi][ni][4 * q + 2], acc[mi][ni][4 * q + 3]};
+    wave_fence();
 #pragma unroll 4
-      for (int p = 0; p < 32 / RPP; ++p) {
-        const int r = p * RPP + lane / CPR, m = row0 + mi * 32 + r;
-        f32x4 v = *(const f32x4*)(patch + r * S::LDF + c * 16);
+    for (int p = 0; p < 32 / RPP; ++p) {
+      const int r = p * RPP + w.lane / CPR, m = w.row0 + mi * 32 + r;
+      f32x4 v = *(const f32x4*)(patch + r * S::LDF + c * 16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = ldexpf(v[j], e[j]);
-        if (m < g.M && n < g.N) {
-          if (g.part) {
-            f32x4* to = (f32x4*)(g.part + split * g.tp + (int64_t)m * g.ldp + n);
-            *to = g.add ? *to + v : v;
+      for (int j = 0; j < 4; ++j) v[j] = ldexpf(v[j], e[j]);
+      if (m < g.M && n < g.N) {
+        if (g.part) {
+          f32x4* to = (f32x4*)(g.part + split * g.tp + (int64_t)m * g.ldp + n);
+          *to = g.add ? *to + v : v;
+        } else {
+          v *= g.scale;
+          if (g.out_f32) {
+            float* to = (float*)g.out + (int64_t)m * g.ldo + n;
+            if (g.out_vec) *(f32x4*)to = v;
+            else
+              for (int j = 0; j < 4; ++j)
+                if (n + j < g.N) to[j] = v[j];
           } else {
-            const float by = g.row_scale ? g.scale * g.row_scale[m] : g.scale;
-            v *= by;
-            if (g.out_f32) {
-              float* to = (float*)g.out + (int64_t)m * g.ldo + n;
-              if (g.out_vec) *(f32x4*)to = v;
-              else
-                for (int j = 0; j < 4; ++j)
-                  if (n + j < g.N) to[j] = v[j];
-            } else {
-              bf16* to = (bf16*)g.out + (int64_t)m * g.ldo + n;
-              typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
-              const bf16x4 o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
-              if (g.out_vec) *(bf16x4*)to = o;
-              else
-                for (int j = 0; j < 4; ++j)
-                  if (n + j < g.N) to[j] = o[j];
-            }
+            bf16* to = (bf16*)g.out + (int64_t)m * g.ldo + n;
+            typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+            const bf16x4 o = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+            if (g.out_vec) *(bf16x4*)to = o;
+            else
+              for (int j = 0; j < 4; ++j)
+                if (n + j < g.N) to[j] = o[j];
           }
         }
       }
-      wave_fence();
     }
+    wave_fence();
   }
 }
 
@@ -436,82 +508,169 @@ __device__ __forceinline__ uint32_t bits_if_finite(float v) {
   return b < 0x7f800000u ? b : 0u;
 }
 
+// x, w or both (a launch handles up to two; the first `blocks` workgroups the first)
+struct PackJob { const void* x = nullptr; int64_t ldx = 0, rows = 0; uint16_t* to = nullptr; int64_t term = 0; int* exps = nullptr; };
 // rows of D values to rows of whole k-tiles: bf16 as they are, fp32 in two fp16 terms (`term` elements apart) with a power of two a row.  A wavefront a row
 template <typename T>
-__global__ __launch_bounds__(256) void ce_pack_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int D, int Dp, uint16_t* __restrict__ to, int64_t term, int* __restrict__ exps) {
+__global__ __launch_bounds__(256) void ce_pack_kernel(PackJob a, PackJob b, int blocks, int D, int Dp) {
+  const bool first = (int)blockIdx.x < blocks;
+  const PackJob j = first ? a : b;
   const int lane = threadIdx.x % WAVE;
-  const int64_t m = (int64_t)blockIdx.x * 4 + threadIdx.x / WAVE;
-  if (m >= rows) return;
-  const T* row = x + m * ldx;
-  uint16_t* out = to + m * Dp;
+  const int64_t m = (int64_t)(first ? blockIdx.x : blockIdx.x - blocks) * 4 + threadIdx.x / WAVE;
+  if (m >= j.rows) return;
+  const T* row = (const T*)j.x + m * j.ldx;
+  uint16_t* out = j.to + m * Dp;
   if constexpr (sizeof(T) == 2) {
-    for (int j = lane; j < Dp; j += WAVE) out[j] = j < D ? __builtin_bit_cast(uint16_t, row[j]) : (uint16_t)0;
+#pragma unroll 4
+    for (int k = lane; k < Dp; k += WAVE) out[k] = k < D ? __builtin_bit_cast(uint16_t, row[k]) : (uint16_t)0;
   } else {
-    float most = 0.f;
-    for (int j = lane; j < D; j += WAVE) most = fmaxf(most, __uint_as_float(bits_if_finite(row[j])));
+    // rows of up to 1024 values stay in registers, longer ones are read twice
+    constexpr int KEEP = 16;
+    float v[KEEP], most = 0.f;
+    if (Dp <= KEEP * WAVE) {
+#pragma unroll
+      for (int i = 0; i < KEEP; ++i) v[i] = lane + i * WAVE < D ? row[lane + i * WAVE] : 0.f;
+#pragma unroll
+      for (int i = 0; i < KEEP; ++i) most = fmaxf(most, __uint_as_float(bits_if_finite(v[i])));
+    } else {
+#pragma unroll 8
+      for (int k = lane; k < D; k += WAVE) most = fmaxf(most, __uint_as_float(bits_if_finite(row[k])));
+    }
     const int e = exponent_of(__float_as_uint(wave_max(most)));
-    if (lane == 0) exps[m] = e;
-    for (int j = lane; j < Dp; j += WAVE) {
-      const float v = j < D ? ldexpf(row[j], -e) : 0.f;
-      const f16 h = (f16)v, l = (f16)(v - (float)h);
-      out[j] = __builtin_bit_cast(uint16_t, h);
-      out[term + j] = __builtin_bit_cast(uint16_t, l);
+    if (lane == 0) j.exps[m] = e;
+    auto put = [&](int k, float x) __attribute__((always_inline)) {
+      x = ldexpf(x, -e);
+      const f16 h = (f16)x, l = (f16)(x - (float)h);
+      out[k] = __builtin_bit_cast(uint16_t, h);
+      out[j.term + k] = __builtin_bit_cast(uint16_t, l);
+    };
+    if (Dp <= KEEP * WAVE) {
+#pragma unroll
+      for (int i = 0; i < KEEP; ++i)
+        if (lane + i * WAVE < Dp) put(lane + i * WAVE, v[i]);
+    } else {
+#pragma unroll 8
+      for (int k = lane; k < Dp; k += WAVE) put(k, k < D ? row[k] : 0.f);
     }
   }
 }
 
 // what a row of x counts with in dw
-struct RowWeights { const int32_t* labels; const float* row_grad; int classes; };
+struct RowWeights { const int32_t* labels = nullptr; const float* row_grad = nullptr; int classes = 0; };
 __device__ __forceinline__ float weight_of(const RowWeights& w, int64_t m) {
   if (!w.labels) return 1.f;
   const int label = w.labels[m];
   return label >= 0 && label < w.classes ? w.row_grad ? w.row_grad[m] : 1.f : 0.f;
 }
-template <typename T> __device__ __forceinline__ float weighted(T v, float by) { return by == 0.f ? 0.f : (float)v * by; }
+__device__ __forceinline__ float weighted(float v, float by) { return by == 0.f ? 0.f : v * by; }
 
-__global__ __launch_bounds__(256) void ce_zero_kernel(uint32_t* p, int n) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < n) p[i] = 0u;
-}
+// [rows, D] -> [terms][D][ld] fp16, a power of two each of the D rows; what lies between rows and ld is zero.  In two launches, each for x, w or both: the columns' maxima, `chunks`
+// parts of the rows apart, then the rest
+struct TransposeJob {
+  const void* x = nullptr; int64_t ldx = 0; int rows = 0; RowWeights rw;
+  int per = 1, chunks = 0;                         // rows of a part; parts (0: no job)
+  uint32_t* most = nullptr;                        // [chunks][D] bits of the largest finite |value|
+  f16* to = nullptr; int64_t ld = 0, term = 0; int* exps = nullptr;
+};
+constexpr int CHUNKS = 64;
 
-// bits of the largest |value| of each column (maxima: their order changes nothing)
 template <typename T>
-__global__ __launch_bounds__(256) void ce_colmax_kernel(const T* __restrict__ x, int64_t ldx, int rows, int D, int per, RowWeights rw, uint32_t* __restrict__ most) {
-  __shared__ uint32_t red[4][WAVE];
-  const int lane = threadIdx.x % WAVE, w = threadIdx.x / WAVE, col = blockIdx.x * WAVE + lane, r1 = min((int)(blockIdx.y + 1) * per, rows);
-  uint32_t b = 0;
-  if (col < D)
-#pragma unroll 8
-    for (int m = blockIdx.y * per + w; m < r1; m += 4) b = max(b, bits_if_finite(weighted(x[m * ldx + col], weight_of(rw, m))));
-  red[w][lane] = b;
-  __syncthreads();
-  if (w == 0 && col < D) atomicMax(most + col, max(max(red[0][lane], red[1][lane]), max(red[2][lane], red[3][lane])));
-}
-
-// [rows, D] -> [terms][D][ld] fp16, a power of two each of the D rows; what lies between rows and ld is zero
-template <typename T>
-__global__ __launch_bounds__(256) void ce_transpose_kernel(const T* __restrict__ x, int64_t ldx, int rows, int D, RowWeights rw, const uint32_t* __restrict__ most, f16* __restrict__ to,
-                                                           int64_t ld, int64_t term, int* __restrict__ exps) {
-  constexpr int TERMS = sizeof(T) / 2;
-  __shared__ f16 tile[TERMS][64][64 + 8];
-  const int lane = threadIdx.x % WAVE, w = threadIdx.x / WAVE, c0 = blockIdx.y * 64, col = c0 + lane;
-  const int m0 = blockIdx.x * 64, e = col < D ? exponent_of(most[col]) : 0;
-  if (blockIdx.x == 0 && w == 0 && col < D) exps[col] = e;
+__global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, TransposeJob b, int D) {
+  constexpr int V = Chunk<T>::V;
+  __shared__ uint32_t red[256][V + 1];
+  const bool first = (int)blockIdx.y < a.chunks;
+  const TransposeJob j = first ? a : b;
+  const int chunk = first ? blockIdx.y : blockIdx.y - a.chunks, r0 = chunk * j.per, r1 = min(r0 + j.per, j.rows);
+  const T* x = (const T*)j.x;
+  uint32_t* most = j.most + (int64_t)chunk * D;
+  if (D < V) {                                     // (no whole piece to read)
+    if (threadIdx.x < D) {
+      uint32_t m = 0;
+      for (int r = r0; r < r1; ++r) m = max(m, bits_if_finite(weighted((float)x[r * j.ldx + threadIdx.x], weight_of(j.rw, r))));
+      most[threadIdx.x] = m;
+    }
+    return;
+  }
+  // pieces of V columns (the last one ends with the row), 8 .. 64 of them side by side, the rows among the threads above each other
+  const int pieces = (D + V - 1) / V, side = pieces > 32 ? 64 : pieces > 16 ? 32 : pieces > 8 ? 16 : 8, above = 256 / side;
+  const int p = blockIdx.x * side + threadIdx.x % side, col = min(p * V, D - V);
+  uint32_t m[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) m[e] = 0;
+  if (p < pieces)
 #pragma unroll 4
-  for (int r = w; r < 64; r += 4) {
-    const int m = m0 + r;
-    const float v = m < rows && col < D ? ldexpf(weighted(x[m * ldx + col], weight_of(rw, m)), -e) : 0.f;
-    const f16 h = (f16)v;
-    tile[0][lane][r] = h;
-    if constexpr (TERMS == 2) tile[TERMS - 1][lane][r] = (f16)(v - (float)h);
+    for (int r = r0 + threadIdx.x / side; r < r1; r += above) {
+      const typename Loose<T>::vec v = *(const typename Loose<T>::vec*)(x + r * j.ldx + col);
+      const float by = weight_of(j.rw, r);
+#pragma unroll
+      for (int e = 0; e < V; ++e) m[e] = max(m[e], bits_if_finite(weighted((float)v[e], by)));
+    }
+#pragma unroll
+  for (int e = 0; e < V; ++e) red[threadIdx.x][e] = m[e];
+  __syncthreads();
+  if ((int)threadIdx.x < side && p < pieces) {
+    for (int i = 1; i < above; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) m[e] = max(m[e], red[threadIdx.x + i * side][e]);
+#pragma unroll
+    for (int e = 0; e < V; ++e) most[col + e] = m[e];            // (columns that two pieces hold: the same from both)
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, TransposeJob b, int blocks, int D) {
+  constexpr int TERMS = sizeof(T) / 2, V = Chunk<T>::V, PER_ROW = 64 / V, LD = 66;
+  __shared__ f16 tile[TERMS][64][LD];              // (rows of 33 words: neither the writes down nor the reads across meet in a bank)
+  __shared__ uint32_t red[4][64];
+  __shared__ int exps[64];
+  const bool first = (int)blockIdx.x < blocks;
+  const TransposeJob j = first ? a : b;
+  const int lane = threadIdx.x % WAVE, w = threadIdx.x / WAVE, c0 = blockIdx.y * 64, m0 = (first ? blockIdx.x : blockIdx.x - blocks) * 64;
+  const T* x = (const T*)j.x;
+  // the tile's rows on their way first
+  typename Loose<T>::vec v[PER_ROW / 4];
+  float by[PER_ROW / 4];
+  const int c = threadIdx.x % PER_ROW * V;
+  const bool whole = c0 + 64 <= D;
+#pragma unroll
+  for (int i = 0; i < PER_ROW / 4; ++i) {
+    const int m = m0 + (int)threadIdx.x / PER_ROW + i * (256 / PER_ROW);
+    by[i] = m < j.rows ? weight_of(j.rw, m) : 0.f;
+    if (whole) v[i] = *(const typename Loose<T>::vec*)(x + (int64_t)min(m, j.rows - 1) * j.ldx + c0 + c);
+    else
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[i][e] = m < j.rows && c0 + c + e < D ? x[(int64_t)m * j.ldx + c0 + c + e] : (T)0.f;
+  }
+  uint32_t most = 0;
+  if (c0 + lane < D)
+    for (int k = w; k < j.chunks; k += 4) most = max(most, j.most[(int64_t)k * D + c0 + lane]);
+  red[w][lane] = most;
+  __syncthreads();
+  if (w == 0) {
+    const int e = exponent_of(max(max(red[0][lane], red[1][lane]), max(red[2][lane], red[3][lane])));
+    exps[lane] = e;
+    if (m0 == 0 && c0 + lane < D) j.exps[c0 + lane] = e;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER_ROW / 4; ++i) {
+    const int r = (int)threadIdx.x / PER_ROW + i * (256 / PER_ROW);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float s = ldexpf(weighted((float)v[i][e], by[i]), -exps[c + e]);
+      const f16 h = (f16)s;
+      tile[0][c + e][r] = h;
+      if constexpr (TERMS == 2) tile[TERMS - 1][c + e][r] = (f16)(s - (float)h);
+    }
   }
   __syncthreads();
 #pragma unroll
   for (int t = 0; t < TERMS; ++t)
 #pragma unroll
     for (int i = threadIdx.x; i < 512; i += 256) {
-      const int c = i / 8, m = m0 + i % 8 * 8;
-      if (c0 + c < D && m < ld) *(f16x8*)(to + t * term + (int64_t)(c0 + c) * ld + m) = *(const f16x8*)&tile[t][c][i % 8 * 8];
+      const int col = i / 8, k = i % 8 * 8;
+      const uint32_t* from = (const uint32_t*)&tile[t][col][k];
+      if (c0 + col < D && m0 + k < j.ld) *(uint4*)(j.to + t * j.term + (int64_t)(c0 + col) * j.ld + m0 + k) = make_uint4(from[0], from[1], from[2], from[3]);
     }
 }
 
@@ -521,19 +680,15 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* __restrict_
                                                        const int32_t* __restrict__ labels, int classes, float* __restrict__ loss, float2* __restrict__ stats) {
   __shared__ float2 red[16][WAVE];
   const int lane = threadIdx.x % WAVE, w = threadIdx.x / WAVE, m = blockIdx.x * WAVE + lane, mc = min(m, M - 1);
-  auto join = [](float2 p, float2 q) __attribute__((always_inline)) {
-    const float most = fmaxf(p.x, q.x), ref = most == -INFINITY ? 0.f : most;
-    return make_float2(most, p.y * __expf(p.x - ref) + q.y * __expf(q.x - ref));
-  };
   float2 p = make_float2(-INFINITY, 0.f);
 #pragma unroll 8
-  for (int t = w; t < tiles; t += 16) p = join(p, parts[(int64_t)t * M + mc]);
+  for (int t = w; t < tiles; t += 16) p = joined(p, parts[(int64_t)t * M + mc]);
   red[w][lane] = p;
   __syncthreads();
   if (w != 0 || m >= M) return;
-  if (!begin) p = join(run[m], p);
+  if (!begin) p = joined(run[m], p);
 #pragma unroll
-  for (int i = 1; i < 16; ++i) p = join(p, red[i][lane]);
+  for (int i = 1; i < 16; ++i) p = joined(p, red[i][lane]);
   if (!end) {
     run[m] = p;
     return;
@@ -548,33 +703,44 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* __restrict_
   }
 }
 
-// out = scale row_scale[m] (sum over the parts, in order)
-template <typename T>
-__global__ __launch_bounds__(256) void ce_reduce_kernel(const float* __restrict__ part, int splits, int64_t tp, int64_t ldp, int64_t M, int N, float scale, const float* __restrict__ row_scale,
-                                                        T* __restrict__ out, int64_t ldo) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, chunks = (N + 3) / 4, m = i / chunks;
-  const int n = (int)(i - m * chunks) * 4;
-  if (m >= M) return;
-  f32x4 v = *(const f32x4*)(part + m * ldp + n);
-  for (int s = 1; s < splits; ++s) v += *(const f32x4*)(part + s * tp + m * ldp + n);
-  v *= row_scale ? scale * row_scale[m] : scale;
-  T* to = out + m * ldo + n;
-  if (n + 4 <= N && ((uintptr_t)to & (4 * sizeof(T) - 1)) == 0) {
+// out = scale row_scale[m] (sum over the parts, in order); parts of db are rows of tokens
+struct SumJob {
+  const float* part = nullptr; int parts = 0; int64_t tp = 0, ldp = 0, rows = 0; int cols = 0;
+  float scale = 1.f; const float* row_scale = nullptr;
+  void* out = nullptr; int64_t ldo = 0; bool f32 = false;
+  int blocks = 0;
+};
+template <typename T> __device__ __forceinline__ void put_four(T* to, f32x4 v, int have) {
+  if (have >= 4 && ((uintptr_t)to & (4 * sizeof(T) - 1)) == 0) {
     typedef T vec __attribute__((ext_vector_type(4)));
     *(vec*)to = vec{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
   } else {
     for (int j = 0; j < 4; ++j)
-      if (n + j < N) to[j] = (T)v[j];
+      if (j < have) to[j] = (T)v[j];
   }
 }
-
-__global__ __launch_bounds__(256) void ce_db_kernel(const float* __restrict__ dbp, int tiles, int n, float scale, float* __restrict__ db) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  float v = 0.f;
-#pragma unroll 8
-  for (int t = 0; t < tiles; ++t) v += dbp[(int64_t)t * n + i];
-  db[i] = scale * v;
+// dx, dw and db, or some of them, in one launch
+__global__ __launch_bounds__(256) void ce_sums_kernel(SumJob a, SumJob b, SumJob c) {
+  int block = blockIdx.x;
+  SumJob j = a;
+  if (block >= a.blocks) {
+    block -= a.blocks;
+    j = b;
+    if (block >= b.blocks) {
+      block -= b.blocks;
+      j = c;
+    }
+  }
+  const int64_t i = (int64_t)block * 256 + threadIdx.x, chunks = (j.cols + 3) / 4, m = i / chunks;
+  const int n = (int)(i - m * chunks) * 4;
+  if (m >= j.rows) return;
+  const float* at = j.part + m * j.ldp + n;
+  f32x4 v = *(const f32x4*)at;
+#pragma unroll 4
+  for (int s = 1; s < j.parts; ++s) v += *(const f32x4*)(at + s * j.tp);
+  v *= j.row_scale ? j.scale * j.row_scale[m] : j.scale;
+  if (j.f32) put_four((float*)j.out + m * j.ldo + n, v, j.cols - n);
+  else put_four((bf16*)j.out + m * j.ldo + n, v, j.cols - n);
 }
 
 // no tokens: no gradients
@@ -587,41 +753,84 @@ template <typename T> __global__ __launch_bounds__(256) void ce_fill_kernel(T* _
 int up(int64_t n, int to) { return (int)((n + to - 1) / to * to); }
 int over(int64_t n, int by) { return (int)((n + by - 1) / by); }
 
-template <class S, Mode MODE, bool F16, int SEG> void launch(const CeGemm& g, int mt, int nt, hipStream_t s) {
-  auto kern = ce_kernel<S, MODE, F16, SEG>;
-  static uint64_t known = 0;                       // devices on which the kernel has its LDS
+// a kernel has its LDS, once a device
+template <auto KERNEL> void with_lds(size_t bytes) {
+  static uint64_t known = 0;
   int dev = 0;
   (void)hipGetDevice(&dev);
   if (!(__atomic_load_n(&known, __ATOMIC_RELAXED) >> (dev & 63) & 1)) {
-    (void)hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::lds);
+    (void)hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     __atomic_fetch_or(&known, (uint64_t)1 << (dev & 63), __ATOMIC_RELAXED);
   }
-  kern<<<mt * nt * g.splits, S::NT, S::lds, s>>>(g, mt, nt);
 }
 enum { LARGE, SMALL, FEW };
-template <Mode MODE, bool F16, int SEG> void launch_as(int shape, const CeGemm& g, int rows, hipStream_t s) {
-  // (rows: those that tiles have to cover)
-  if (shape == FEW) launch<Few, MODE, F16, SEG>(g, over(rows, Few::BM), over(g.N, Few::BN), s);
-  else if (shape == SMALL || (SEG == 3 && MODE == GRAD)) launch<Small, MODE, F16, SEG>(g, over(rows, Small::BM), over(g.N, Small::BN), s);
-  else if constexpr (SEG == 1 || MODE != GRAD) launch<Large, MODE, F16, SEG>(g, over(rows, Large::BM), over(g.N, Large::BN), s);
-}
 int rows_of(int shape) { return shape == FEW ? Few::BM : shape == SMALL ? Small::BM : Large::BM; }
 int cols_of(int shape) { return shape == FEW ? Few::BN : shape == SMALL ? Small::BN : Large::BN; }
 
-// the shape and the workgroups over k of a product, by a model of its time in rounds over the 256 CUs (us)
-struct Pick { int shape, splits, per; };
-Pick pick(int64_t M, int64_t N, int kt, bool split, bool large) {
-  static const double tile[3] = {1.15, 0.40, 0.30}, start[3] = {7, 4, 4};
-  Pick best = {SMALL, 1, kt};
+template <class S, Mode MODE, bool F16, int SEG, bool DB> void launch_logits(const CeGemm& g, int rows, hipStream_t s) {
+  with_lds<ce_logits_kernel<S, MODE, F16, SEG, DB>>(S::lds);
+  const int mt = over(rows, S::BM), nt = over(g.N, S::BN);
+  ce_logits_kernel<S, MODE, F16, SEG, DB><<<mt * nt, S::NT, S::lds, s>>>(g, mt, nt);
+}
+// rows: those that tiles have to cover
+template <Mode MODE, bool F16, int SEG, bool DB> void logits(int shape, const CeGemm& g, int rows, hipStream_t s) {
+  if (shape == FEW) launch_logits<Few, MODE, F16, SEG, DB>(g, rows, s);
+  else if (shape == SMALL) launch_logits<Small, MODE, F16, SEG, DB>(g, rows, s);
+  else launch_logits<Large, MODE, F16, SEG, DB>(g, rows, s);
+}
+template <class S, int SEG> void launch_grads(const CeGemm& a, const CeGemm& b, hipStream_t s) {
+  auto blocks = [](const CeGemm& g) { return g.A ? over(g.M, S::BM) * over(g.N, S::BN) * g.splits : 0; };
+  with_lds<ce_grads_kernel<S, SEG>>(S::lds);
+  ce_grads_kernel<S, SEG><<<blocks(a) + blocks(b), S::NT, S::lds, s>>>(a, b, blocks(a));
+}
+
+// Models of a launch, in us: a workgroup takes a CU for start + k-tiles * tile
+struct Cost { double tile, start; };
+constexpr Cost COST[3] = {{1.7, 8}, {0.6, 4}, {0.5, 4}};
+int logits_shape(int64_t M, int64_t N, int kt) {
+  int best = SMALL;
   double least = 1e30;
   for (int shape = 0; shape < 3; ++shape) {
-    if ((shape == FEW && M > 32) || (shape == LARGE && !large)) continue;
+    if (shape == FEW && M > Few::BM) continue;
     const int64_t tiles = (int64_t)over(M, rows_of(shape)) * over(N, cols_of(shape));
-    for (int n = 1; n <= (split ? 64 : 1); ++n) {
-      const int per = over(kt, n), splits = over(kt, per);
-      if (splits != n || (n > 1 && per < 4)) continue;
-      const double us = (double)((tiles * n + 255) / 256) * (per * tile[shape] + start[shape]) + (n > 1 ? 3 + n * M * N * 8e-6 / 4 : 0);
-      if (us < least) { least = us; best = {shape, n, per}; }
+    const double us = (double)((tiles + 255) / 256) * (COST[shape].start + kt * COST[shape].tile);
+    if (us < least) { least = us; best = shape; }
+  }
+  return best;
+}
+// shape and workgroups over k of dx (M x D, kx k-tiles) and dw (n x D, kw k-tiles) together; either may be missing (0 k-tiles).  dx's workgroups go first
+struct Split { int shape, x, w; };
+Split grads_split(int64_t M, int64_t n, int64_t D, int kx, int kw) {
+  Split best = {SMALL, 1, 1};
+  double least = 1e30;
+  for (int shape = LARGE; shape <= SMALL; ++shape) {
+    const int64_t tx = kx ? (int64_t)over(M, rows_of(shape)) * over(D, cols_of(shape)) : 0, tw = kw ? (int64_t)over(n, rows_of(shape)) * over(D, cols_of(shape)) : 0;
+    const Cost c = COST[shape];
+    for (int x = 1; x <= (kx ? 64 : 1); ++x) {
+      if (x > 1 && (kx < 4 * x || tx * x > 1024)) break;
+      for (int w = 1; w <= (kw ? 16 : 1); ++w) {
+        if (w > 1 && (kw < 4 * w || tw * w > 1024)) break;
+        const double a = c.start + over(kx, x) * c.tile, b = c.start + over(kw, w) * c.tile;
+        // dx in rounds over the CUs, dw on those that are free
+        const int64_t nx = tx * x, nw = tw * w, full = nx / 256, rest = nx % 256;
+        double us = full * a + (rest ? a : 0);
+        if (nw) {
+          int64_t left = nw;
+          double early = full * a, late = full * a + a;           // when 256 - rest CUs, and the rest, take the next
+          us = std::max(us, 0.0);
+          const int64_t rounds = std::max<int64_t>(0, (nw - 1024) / 256);      // (many: whole rounds at once)
+          left -= rounds * 256;
+          early += rounds * b;
+          late += rounds * b;
+          while (left > 0) {
+            if (rest == 0 || early <= late) { left -= 256 - rest; early += b; us = std::max(us, early); }
+            else { left -= rest; late += b; us = std::max(us, late); }
+          }
+        }
+        // partial sums leave and come back
+        us += ((kx ? x * M * D : 0) + (w > 1 ? w * n * D : 0)) * 8e-6 / 4;
+        if (us < least * 0.999) { least = us; best = {shape, x, w}; }
+      }
     }
   }
   return best;
@@ -629,8 +838,9 @@ Pick pick(int64_t M, int64_t N, int kt, bool split, bool large) {
 
 // sizes, and places in the workspace
 struct Plan {
-  int T, Dp, Np, Vs, Vp, Vc, dx_parts, dw_parts, Dq;
-  size_t xp, ex, wp, ew, parts, run, zlabel, G, GT, xT, wT, exT, ewT, most, dxp, dwp, dbp, bytes;
+  int T, Dp, Np, Vs, Vp, Vc, Dq, ldd;
+  Split split = {};
+  size_t xp, ex, wp, ew, parts, run, zlabel, G, GT, xT, wT, exT, ewT, mostx, mostw, dxp, dwp, dbp, bytes;
   Plan(bool f32, int N, int D, int V, bool backward) {
     T = f32 ? 2 : 1;
     Dp = up(D, BK); Np = up(N, BK); Dq = up(D, 4);
@@ -644,6 +854,7 @@ struct Plan {
     Vs = piece(64 * MB * 128 / (8.0 * N));
     Vp = std::min(Vs, piece(256 * MB / (2.0 * T * Dp)));
     Vc = std::min(piece(256 * MB / (4.0 * T * Np)), piece(256 * MB / (2.0 * T * Dp)));
+    ldd = Vc;
     bytes = 0;
     auto take = [&](size_t n) { const size_t at = bytes; bytes += (n + 255) / 256 * 256; return at; };
     const int Vm = backward ? Vc : Vp;
@@ -656,35 +867,50 @@ struct Plan {
     G = take((size_t)2 * T * N * Vc); GT = take((size_t)2 * T * Vc * Np);
     xT = take((size_t)2 * T * D * Np); exT = take(sizeof(int) * (size_t)D);
     wT = take((size_t)2 * T * D * Vc); ewT = take(sizeof(int) * (size_t)D);
-    most = take(sizeof(uint32_t) * (size_t)D);
-    dx_parts = pick(N, D, over(std::min(Vc, up(V, BK)), BK) * (T == 2 ? 3 : 1), true, true).splits;
-    dw_parts = pick(std::min(V, Vc), D, Np / BK * (T == 2 ? 3 : 1), true, true).splits;
-    dxp = take(sizeof(float) * (size_t)dx_parts * N * Dq);
-    dwp = take(dw_parts > 1 ? sizeof(float) * (size_t)dw_parts * Vc * Dq : 0);
-    dbp = take(sizeof(float) * (size_t)over(Np, 32) * Vc);
+    mostx = take(sizeof(uint32_t) * (size_t)CHUNKS * D); mostw = take(sizeof(uint32_t) * (size_t)CHUNKS * D);
+    const int seg = T == 2 ? 3 : 1;
+    // (for the first piece; the others take as many workgroups over k)
+    split = grads_split(N, std::min(V, Vc), D, std::min(Vc, up(V, BK)) / BK * seg, Np / BK * seg);
+    dxp = take(sizeof(float) * (size_t)split.x * N * Dq);
+    dwp = take(split.w > 1 ? sizeof(float) * (size_t)split.w * Vc * Dq : 0);
+    dbp = take(sizeof(float) * (size_t)over(Np, 32) * ldd);
   }
 };
 
 // (a tile's rows are addressed in 32 bits)
 bool whole_rows(const void* p, int64_t ld, int D) { return D % BK == 0 && ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld <= 1 << 23; }
 
-// An operand of the logits: as it lies, or packed
+// An operand of the logits: as it lies, or packed by what `job` then describes
 struct Rows { const void* p; int64_t ld, term; const int* exps; };
-Rows rows_operand(const void* p, int64_t ld, bool f32, int64_t rows, int D, int Dp, void* packed, int* exps, bool as_it_lies, hipStream_t s) {
+Rows rows_operand(const void* p, int64_t ld, bool f32, int64_t rows, int Dp, void* packed, int* exps, bool as_it_lies, PackJob& job) {
   if (as_it_lies) return {p, ld, 0, nullptr};
-  const int64_t term = rows * Dp;
-  const unsigned grid = (unsigned)((rows + 3) / 4);
-  if (f32) ce_pack_kernel<float><<<grid, 256, 0, s>>>((const float*)p, ld, rows, D, Dp, (uint16_t*)packed, term, exps);
-  else ce_pack_kernel<bf16><<<grid, 256, 0, s>>>((const bf16*)p, ld, rows, D, Dp, (uint16_t*)packed, term, nullptr);
-  return {packed, Dp, term, f32 ? exps : nullptr};
+  job.x = p; job.ldx = ld; job.rows = rows; job.to = (uint16_t*)packed; job.term = rows * Dp; job.exps = exps;
+  return {packed, Dp, job.term, f32 ? exps : nullptr};
+}
+void pack(const PackJob& a, const PackJob& b, bool f32, int D, int Dp, hipStream_t s) {
+  const int na = over(a.rows, 4), nb = over(b.rows, 4);
+  if (na + nb == 0) return;
+  if (f32) ce_pack_kernel<float><<<na + nb, 256, 0, s>>>(a, b, na, D, Dp);
+  else ce_pack_kernel<bf16><<<na + nb, 256, 0, s>>>(a, b, na, D, Dp);
 }
 
-template <typename T>
-void transposed(const void* x, int64_t ldx, int rows, int D, const RowWeights& rw, uint32_t* most, f16* to, int64_t ld, int64_t term, int* exps, hipStream_t s) {
-  ce_zero_kernel<<<over(D, 256), 256, 0, s>>>(most, D);
-  const int per = std::max(64, over(rows, std::max(1, 2048 / over(D, 64))));
-  ce_colmax_kernel<T><<<dim3(over(D, 64), over(rows, per)), 256, 0, s>>>((const T*)x, ldx, rows, D, per, rw, most);
-  ce_transpose_kernel<T><<<dim3(over(ld, 64), over(D, 64)), 256, 0, s>>>((const T*)x, ldx, rows, D, rw, most, to, ld, term, exps);
+template <typename T> void transpose(const TransposeJob& a, const TransposeJob& b, int D, hipStream_t s) {
+  if (a.chunks + b.chunks == 0) return;
+  const int pieces = over(D, Chunk<T>::V), side = pieces > 32 ? 64 : pieces > 16 ? 32 : pieces > 8 ? 16 : 8;
+  ce_colmax_kernel<T><<<dim3(over(pieces, side), a.chunks + b.chunks), 256, 0, s>>>(a, b, D);
+  const int na = a.chunks ? over(a.ld, 64) : 0, nb = b.chunks ? over(b.ld, 64) : 0;
+  ce_transpose_kernel<T><<<dim3(na + nb, over(D, 64)), 256, 0, s>>>(a, b, na, D);
+}
+void set_chunks(TransposeJob& j) {
+  j.per = std::max(64, over(j.rows, CHUNKS));
+  j.chunks = over(j.rows, j.per);
+}
+
+CeGemm logits_gemm(const LinearCe& a, const Plan& p, const Rows& x, const Rows& w, int v0, int n) {
+  CeGemm g;
+  g.A = x.p; g.lda = x.ld; g.ta = x.term; g.ea = x.exps; g.B = w.p; g.ldb = w.ld; g.tb = w.term; g.eb = w.exps;
+  g.M = a.N; g.N = n; g.nk = p.Dp / BK; g.bias = a.bias ? a.bias + v0 : nullptr; g.labels = a.labels; g.v0 = v0; g.classes = a.V;
+  return g;
 }
 
 }  // namespace
@@ -696,19 +922,20 @@ void linear_ce_forward(const LinearCe& a, hipStream_t s) {
   char* ws = (char*)a.workspace;
   const int64_t size = a.f32 ? 4 : 2;
   const bool direct_x = !a.f32 && whole_rows(a.x, a.ldx, a.D), direct_w = !a.f32 && whole_rows(a.w, a.ldw, a.D);
-  const Rows x = rows_operand(a.x, a.ldx, a.f32, a.N, a.D, p.Dp, ws + p.xp, (int*)(ws + p.ex), direct_x, s);
+  PackJob px;
+  const Rows x = rows_operand(a.x, a.ldx, a.f32, a.N, p.Dp, ws + p.xp, (int*)(ws + p.ex), direct_x, px);
   const int step = direct_w ? p.Vs : p.Vp;
   for (int v0 = 0; v0 < a.V; v0 += step) {
     const int n = std::min(step, a.V - v0);
-    const Rows w = rows_operand((const char*)a.w + v0 * a.ldw * size, a.ldw, a.f32, n, a.D, p.Dp, ws + p.wp, (int*)(ws + p.ew), direct_w, s);
-    CeGemm g;
-    g.A = x.p; g.lda = x.ld; g.ta = x.term; g.ea = x.exps; g.B = w.p; g.ldb = w.ld; g.tb = w.term; g.eb = w.exps;
-    g.M = a.N; g.N = n; g.nk = p.Dp / BK; g.bias = a.bias ? a.bias + v0 : nullptr; g.labels = a.labels; g.v0 = v0; g.classes = a.V;
+    PackJob pw;
+    const Rows w = rows_operand((const char*)a.w + v0 * a.ldw * size, a.ldw, a.f32, n, p.Dp, ws + p.wp, (int*)(ws + p.ew), direct_w, pw);
+    pack(v0 == 0 ? px : PackJob(), pw, a.f32, a.D, p.Dp, s);
+    CeGemm g = logits_gemm(a, p, x, w, v0, n);
     g.parts = (float2*)(ws + p.parts); g.zlabel = (float*)(ws + p.zlabel);
-    const Pick k = pick(a.N, n, g.nk * (a.f32 ? 3 : 1), false, true);
-    if (a.f32) launch_as<STATS, true, 3>(k.shape, g, a.N, s);
-    else launch_as<STATS, false, 1>(k.shape, g, a.N, s);
-    ce_join_kernel<<<over(a.N, WAVE), 1024, 0, s>>>(g.parts, over(n, cols_of(k.shape)), a.N, (float2*)(ws + p.run), v0 == 0, v0 + n == a.V, g.zlabel, a.labels, a.V, a.loss, (float2*)a.stats);
+    const int shape = logits_shape(a.N, n, g.nk * (a.f32 ? 3 : 1));
+    if (a.f32) logits<STATS, true, 3, false>(shape, g, a.N, s);
+    else logits<STATS, false, 1, false>(shape, g, a.N, s);
+    ce_join_kernel<<<over(a.N, WAVE), 1024, 0, s>>>(g.parts, over(n, cols_of(shape)), a.N, (float2*)(ws + p.run), v0 == 0, v0 + n == a.V, g.zlabel, a.labels, a.V, a.loss, (float2*)a.stats);
   }
 }
 
@@ -719,55 +946,67 @@ void backward_as(const LinearCe& a, hipStream_t s) {
   const Plan p(F32, a.N, a.D, a.V, true);
   char* ws = (char*)a.workspace;
   const bool direct_x = !F32 && whole_rows(a.x, a.ldx, a.D), direct_w = !F32 && whole_rows(a.w, a.ldw, a.D);
-  const Rows x = rows_operand(a.x, a.ldx, F32, a.N, a.D, p.Dp, ws + p.xp, (int*)(ws + p.ex), direct_x, s);
+  PackJob px;
+  const Rows x = rows_operand(a.x, a.ldx, F32, a.N, p.Dp, ws + p.xp, (int*)(ws + p.ex), direct_x, px);
   f16 *xT = (f16*)(ws + p.xT), *wT = (f16*)(ws + p.wT), *G = (f16*)(ws + p.G), *GT = (f16*)(ws + p.GT);
-  if (a.dw) transposed<T>(a.x, a.ldx, a.N, a.D, {a.labels, a.row_grad, a.V}, (uint32_t*)(ws + p.most), xT, p.Np, (int64_t)a.D * p.Np, (int*)(ws + p.exT), s);
-  Pick kx = {SMALL, 1, 1};
   for (int v0 = 0; v0 < a.V; v0 += p.Vc) {
     const int n = std::min(p.Vc, a.V - v0), np = up(n, BK);
+    const bool begin = v0 == 0, end = v0 + n == a.V;
     const T* wv = (const T*)a.w + v0 * a.ldw;
-    const Rows w = rows_operand(wv, a.ldw, F32, n, a.D, p.Dp, ws + p.wp, (int*)(ws + p.ew), direct_w, s);
-    CeGemm g;
-    g.A = x.p; g.lda = x.ld; g.ta = x.term; g.ea = x.exps; g.B = w.p; g.ldb = w.ld; g.tb = w.term; g.eb = w.exps;
-    g.M = a.N; g.N = n; g.nk = p.Dp / BK; g.bias = a.bias ? a.bias + v0 : nullptr; g.labels = a.labels; g.v0 = v0; g.classes = a.V;
+    PackJob pw;
+    const Rows w = rows_operand(wv, a.ldw, F32, n, p.Dp, ws + p.wp, (int*)(ws + p.ew), direct_w, pw);
+    pack(begin ? px : PackJob(), pw, F32, a.D, p.Dp, s);
+    TransposeJob tx, tw;
+    if (a.dw && begin) {
+      tx.x = a.x; tx.ldx = a.ldx; tx.rows = a.N; tx.rw.labels = a.labels; tx.rw.row_grad = a.row_grad; tx.rw.classes = a.V;
+      tx.most = (uint32_t*)(ws + p.mostx); tx.to = xT; tx.ld = p.Np; tx.term = (int64_t)a.D * p.Np; tx.exps = (int*)(ws + p.exT);
+      set_chunks(tx);
+    }
+    if (a.dx) {
+      tw.x = wv; tw.ldx = a.ldw; tw.rows = n; tw.most = (uint32_t*)(ws + p.mostw); tw.to = wT; tw.ld = np; tw.term = (int64_t)a.D * np; tw.exps = (int*)(ws + p.ewT);
+      set_chunks(tw);
+    }
+    transpose<T>(tx, tw, a.D, s);
+    CeGemm g = logits_gemm(a, p, x, w, v0, n);
     g.stats = (const float2*)a.stats; g.row_grad = a.row_grad;
     if (a.dx) { g.G = G; g.ldg = np; g.tg = (int64_t)a.N * np; }
     if (a.dw) { g.GT = GT; g.ldgt = p.Np; g.tgt = (int64_t)n * p.Np; }
-    if (a.db) g.dbp = (float*)(ws + p.dbp);
-    const Pick kg = pick(a.N, n, g.nk * SEG, false, !F32);
-    launch_as<GRAD, F32, SEG>(kg.shape, g, a.dw ? p.Np : a.N, s);
-    if (a.db) ce_db_kernel<<<over(n, 256), 256, 0, s>>>(g.dbp, over(a.dw ? p.Np : a.N, rows_of(kg.shape)), n, a.grad_scale, a.db + v0);
+    if (a.db) { g.dbp = (float*)(ws + p.dbp); g.ldd = p.ldd; }
+    const int shape = logits_shape(a.N, n, g.nk * SEG), rows = a.dw ? p.Np : a.N;
+    if (a.db) logits<GRAD, F32, SEG, true>(shape, g, rows, s);
+    else logits<GRAD, F32, SEG, false>(shape, g, rows, s);
+    CeGemm ox, ow;
+    SumJob sx, sw, sb;
     if (a.dx) {
-      transposed<T>(wv, a.ldw, n, a.D, {nullptr, nullptr, 0}, (uint32_t*)(ws + p.most), wT, np, (int64_t)a.D * np, (int*)(ws + p.ewT), s);
-      CeGemm o;
-      o.A = G; o.lda = np; o.ta = g.tg; o.B = wT; o.ldb = np; o.tb = (int64_t)a.D * np; o.eb = (int*)(ws + p.ewT);
-      o.M = a.N; o.N = a.D; o.nk = np / BK;
-      // one shape and number of parts for all pieces: the parts are added to
-      if (v0 == 0) kx = pick(a.N, a.D, o.nk * SEG, true, true);
-      o.splits = kx.splits; o.per = over(o.nk * SEG, kx.splits);
-      o.part = (float*)(ws + p.dxp); o.ldp = p.Dq; o.tp = (int64_t)a.N * p.Dq; o.add = v0 > 0;
-      launch_as<OUT, true, SEG>(kx.shape, o, a.N, s);
-    }
-    if (a.dw) {
-      CeGemm o;
-      o.A = GT; o.lda = p.Np; o.ta = g.tgt; o.B = xT; o.ldb = p.Np; o.tb = (int64_t)a.D * p.Np; o.eb = (int*)(ws + p.exT);
-      o.M = n; o.N = a.D; o.nk = p.Np / BK;
-      const Pick k = pick(std::min(a.V, p.Vc), a.D, o.nk * SEG, true, true);
-      o.splits = k.splits; o.per = k.per; o.scale = a.grad_scale;
-      char* dw = (char*)a.dw + v0 * a.lddw * (a.dw_f32 ? 4 : 2);
-      if (k.splits > 1) { o.part = (float*)(ws + p.dwp); o.ldp = p.Dq; o.tp = (int64_t)n * p.Dq; }
-      else { o.out = dw; o.ldo = a.lddw; o.out_f32 = a.dw_f32; o.out_vec = a.D % 4 == 0 && a.lddw % 4 == 0 && ((uintptr_t)dw & (a.dw_f32 ? 15 : 7)) == 0; }
-      launch_as<OUT, true, SEG>(k.shape, o, n, s);
-      if (k.splits > 1) {
-        const unsigned grid = (unsigned)over((int64_t)n * over(a.D, 4), 256);
-        if (a.dw_f32) ce_reduce_kernel<float><<<grid, 256, 0, s>>>(o.part, k.splits, o.tp, o.ldp, n, a.D, a.grad_scale, nullptr, (float*)dw, a.lddw);
-        else ce_reduce_kernel<bf16><<<grid, 256, 0, s>>>(o.part, k.splits, o.tp, o.ldp, n, a.D, a.grad_scale, nullptr, (bf16*)dw, a.lddw);
+      ox.A = G; ox.lda = np; ox.ta = g.tg; ox.B = wT; ox.ldb = np; ox.tb = tw.term; ox.eb = tw.exps;
+      ox.M = a.N; ox.N = a.D; ox.nk = np / BK; ox.splits = p.split.x; ox.per = over(ox.nk * SEG, ox.splits);
+      ox.part = (float*)(ws + p.dxp); ox.ldp = p.Dq; ox.tp = (int64_t)a.N * p.Dq; ox.add = !begin;
+      if (end) {
+        sx.part = ox.part; sx.parts = ox.splits; sx.tp = ox.tp; sx.ldp = p.Dq; sx.rows = a.N; sx.cols = a.D; sx.scale = a.grad_scale; sx.row_scale = a.row_grad;
+        sx.out = a.dx; sx.ldo = a.lddx; sx.f32 = F32; sx.blocks = over((int64_t)a.N * over(a.D, 4), 256);
       }
     }
+    if (a.dw) {
+      ow.A = GT; ow.lda = p.Np; ow.ta = g.tgt; ow.B = xT; ow.ldb = p.Np; ow.tb = (int64_t)a.D * p.Np; ow.eb = (int*)(ws + p.exT);
+      ow.M = n; ow.N = a.D; ow.nk = p.Np / BK; ow.splits = p.split.w; ow.per = over(ow.nk * SEG, ow.splits); ow.scale = a.grad_scale;
+      char* dw = (char*)a.dw + v0 * a.lddw * (a.dw_f32 ? 4 : 2);
+      if (ow.splits > 1) {
+        ow.part = (float*)(ws + p.dwp); ow.ldp = p.Dq; ow.tp = (int64_t)n * p.Dq;
+        sw.part = ow.part; sw.parts = ow.splits; sw.tp = ow.tp; sw.ldp = p.Dq; sw.rows = n; sw.cols = a.D; sw.scale = a.grad_scale;
+        sw.out = dw; sw.ldo = a.lddw; sw.f32 = a.dw_f32; sw.blocks = over((int64_t)n * over(a.D, 4), 256);
+      } else {
+        ow.out = dw; ow.ldo = a.lddw; ow.out_f32 = a.dw_f32; ow.out_vec = a.D % 4 == 0 && a.lddw % 4 == 0 && ((uintptr_t)dw & (a.dw_f32 ? 15 : 7)) == 0;
+      }
+    }
+    if (a.dx || a.dw) {
+      if (p.split.shape == SMALL) launch_grads<Small, SEG>(ox, ow, s);
+      else launch_grads<Large, SEG>(ox, ow, s);
+    }
+    if (a.db) {
+      sb.part = g.dbp; sb.parts = over(rows, rows_of(shape)); sb.tp = p.ldd; sb.rows = 1; sb.cols = n; sb.scale = a.grad_scale; sb.out = a.db + v0; sb.f32 = true; sb.blocks = over(over(n, 4), 256);
+    }
+    if (sx.blocks + sw.blocks + sb.blocks > 0) ce_sums_kernel<<<sx.blocks + sw.blocks + sb.blocks, 256, 0, s>>>(sx, sw, sb);
   }
-  if (a.dx)
-    ce_reduce_kernel<T><<<(unsigned)over((int64_t)a.N * over(a.D, 4), 256), 256, 0, s>>>((const float*)(ws + p.dxp), kx.splits, (int64_t)a.N * p.Dq, p.Dq, a.N, a.D, a.grad_scale, a.row_grad,
-                                                                                       (T*)a.dx, a.lddx);
 }
 void linear_ce_backward(const LinearCe& a, hipStream_t s) {
   if (a.N == 0) {
