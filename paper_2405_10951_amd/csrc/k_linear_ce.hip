@@ -19,7 +19,6 @@ namespace bsr {
 
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16;
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
@@ -56,7 +55,7 @@ struct CeGemm {
 
 template <int BM_, int BN_, int WM_, int WN_, int NST_> struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NST = NST_, NT = WM * WN * 64;
-  static constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 32, NI = TN / 32;
+  static constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;              // a wavefront's part, in tiles of 16 x 16
   static constexpr size_t stages = (size_t)NST * (BM + BN) * 128;
   static constexpr int LDR = TN * 2 + 16, LDF = TN * 4 + 16;     // patch rows in bytes: fp16, fp32
   static constexpr int patch = 32 * (2 * LDR > LDF ? 2 * LDR : LDF);                       // of a wavefront: 32 rows, of one or two terms
@@ -79,19 +78,28 @@ __device__ __forceinline__ void tile_at(int t, int mt, int nt, int& m, int& n) {
   m = band * BAND + in - n * rows;
 }
 
-// The k-loop is the one of the step's products (operands straight into LDS, one barrier a k-tile, every matrix instruction followed by at most one
-// fragment read or a few loads, the order pinned): accumulators hold transposed 32 x 32 tiles, element r of acc[mi][ni] is row mi 32 + lane % 32, column ni 32 + 8 (r / 4) + 4 (lane / 32) + r % 4.
+// Where a row's chunks of 16 bytes lie in LDS: chunk kc at position kc ^ place(row).  A fragment is read 16 lanes at a time, of which some have one chunk and some its neighbour (lanes 0 - 3, 12 - 15
+// and 20 - 27 go together), of 16 different rows: all 64 banks once.
+__device__ __forceinline__ int place(int row) { return row >> 1 & 7; }
+
+// Operands go straight into LDS (global_load_lds: rows of 8 chunks of 16 bytes, their order in LDS made by the address that a lane reads), NST stages of a
+// k-tile of 64, one barrier a k-tile.  A k-tile is 2 MI groups of NI matrix instructions 16 x 16 x 32, each group with one fragment of A: fragments of A come DIST groups ahead through a ring of
+// RING, those of B a k-step ahead.  DIST groups before the k-tile's end every wavefront has read all of it: there is the barrier, and behind it the loads of k-tile kt + NST go out into its stage, one or two a group.
+// 16 x 16 x 32, not 32 x 32 x 16: under full load the clock is what the power allows, and the smaller tile, which touches half as many accumulators a product, draws less.
+// The operands are swapped (B's rows first): accumulators hold transposed tiles, element r of acc[mi][ni] is row mi 16 + lane % 16, column ni 16 + 4 (lane / 16) + r.
 template <class S, bool F16, int SEG>
-__device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt0, int nk, unsigned char* smem, f32x16 (&acc)[S::MI][S::NI]) {
-  constexpr int BM = S::BM, WN = S::WN, NST = S::NST, TM = S::TM, TN = S::TN, MI = S::MI, NI = S::NI, NMF = MI * NI, NFR = MI + NI;
+__device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt0, int nk, unsigned char* smem, f32x4 (&acc)[S::MI][S::NI]) {
+  constexpr int BM = S::BM, WN = S::WN, NST = S::NST, TM = S::TM, TN = S::TN, MI = S::MI, NI = S::NI, NG = 2 * MI;
   constexpr int RPI = S::NT / 8, AL = BM / RPI, BL = S::BN / RPI, LPT = AL + BL, STAGE = (BM + S::BN) * 128;
+  constexpr int RING = 4, DIST = 3;
   static_assert(BM % RPI == 0 && S::BN % RPI == 0 && RPI % 16 == 0, "a load instruction covers whole groups of 16 rows");
-  static_assert(NST >= 2 && NST <= 4 && (NST - 1) * LPT <= 60 && NMF >= 2, "vmcnt has 6 bits");
+  static_assert(NST >= 2 && NST <= 4 && (NST - 1) * LPT <= 60, "vmcnt has 6 bits");
+  static_assert(NG % RING == 0 && NG > DIST, "the ring comes round with the k-tile");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
   const f16* __restrict__ A = (const f16*)g.A + (int64_t)m0 * g.lda;
   const f16* __restrict__ B = (const f16*)g.B + (int64_t)n0 * g.ldb;
   // rows past the last one repeat it: they only feed accumulators that count for nothing
-  const int lrow = tid >> 3, kc = (tid & 7) ^ swz(lrow);
+  const int lrow = tid >> 3, kc = (tid & 7) ^ place(lrow);
   unsigned off[LPT];
 #pragma unroll
   for (int i = 0; i < AL; ++i) off[i] = (unsigned)min(i * RPI + lrow, g.M - 1 - m0) * (unsigned)g.lda + kc * 8;
@@ -111,67 +119,62 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[mi][ni][r] = 0.f;
-  // fragments: read order A0, B0 .. B(NI-1), A1 .. A(MI-1), so that the first matrix instructions of a k-step can start early
-  const int lr = lane & 31, lh = lane >> 5, sw = swz(lr);
-  int offr[NFR];
-  f16x8 fr[2][NFR];
-#pragma unroll
-  for (int j = 0; j < NFR; ++j) {
-    const bool isA = j == 0 || j > NI;
-    const int idx = j == 0 ? 0 : (j <= NI ? j - 1 : j - NI);
-    offr[j] = isA ? (wm * TM + idx * 32 + lr) * 128 : BM * 128 + (wn * TN + idx * 32 + lr) * 128;
-  }
-  auto rd1 = [&](auto SET, auto J, int st, int ks) __attribute__((always_inline)) {
-    constexpr int set = decltype(SET)::value, j = decltype(J)::value;
-    fr[set][j] = *(const f16x8*)(smem + st * STAGE + (((ks * 2 + lh) ^ sw) << 4) + offr[j]);
+    for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // a fragment: 16 rows, a lane 8 k of one: chunk 4 ks + lane / 16 of row lane % 16
+  const int lr = lane & 15, lq = lane >> 4, sw = place(lr);
+  const unsigned char *fa = smem + (wm * TM + lr) * 128, *fb = smem + BM * 128 + (wn * TN + lr) * 128;
+  f16x8 a[RING], b[2][NI];
+  // group gi (0 .. 2 MI - 1) of a k-tile takes A's fragment (ks, mi) = (gi / MI, gi % MI)
+  auto read_a = [&](auto GI, int st) __attribute__((always_inline)) {
+    constexpr int gi = decltype(GI)::value, ks = gi / MI, mi = gi % MI;
+    a[gi % RING] = *(const f16x8*)(fa + st * STAGE + mi * 16 * 128 + (((ks * 4 + lq) ^ sw) << 4));
   };
-  auto mf1 = [&](auto SET, auto J) __attribute__((always_inline)) {
-    constexpr int set = decltype(SET)::value, j = decltype(J)::value, mi = j / NI, ni = j % NI, ja = mi == 0 ? 0 : NI + mi, jb = 1 + ni;
-    if constexpr (F16) acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fr[set][jb], fr[set][ja], acc[mi][ni], 0, 0, 0);
-    else acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fr[set][jb]), __builtin_bit_cast(bf16x8, fr[set][ja]), acc[mi][ni], 0, 0, 0);
+  auto read_b = [&](auto KS, auto J, int st) __attribute__((always_inline)) {
+    constexpr int ks = decltype(KS)::value, j = decltype(J)::value;
+    b[ks][j] = *(const f16x8*)(fb + st * STAGE + j * 16 * 128 + (((ks * 4 + lq) ^ sw) << 4));
   };
-  constexpr int PRE = NMF >= 16 ? 4 : (NMF >= 8 ? 2 : 1), POST = NMF - PRE;          // matrix instructions of the last k-step in front of the barrier, and behind it
-  constexpr int SPAN = POST + (NST == 2 ? NMF >= 8 : NMF >= 4 ? 3 : NMF == 3 ? 2 : 0) * NMF;    // over which the loads of a k-tile are spread
-  auto loads_at = [&](auto P, int kt, int st) __attribute__((always_inline)) {
+  // loads of k-tile ktl's number p .. : spread evenly over SPAN groups behind the barrier
+  constexpr int SPAN = NG > 8 ? 8 : NG;
+  auto loads = [&](auto P, int kt, int st) __attribute__((always_inline)) {
     constexpr int p = decltype(P)::value, lo = p >= SPAN ? LPT : (p * LPT + SPAN - 1) / SPAN, hi = p + 1 >= SPAN ? LPT : ((p + 1) * LPT + SPAN - 1) / SPAN;
     sfor<hi - lo>([&](auto L) __attribute__((always_inline)) { issue1(IC<lo + decltype(L)::value>{}, kt, st); });
   };
-  constexpr bool LATE = SPAN > POST;
-  auto kstep = [&](auto SET, auto LOADS, auto KS, int st, int ktl, int stl) __attribute__((always_inline)) {
-    constexpr int set = decltype(SET)::value, ks = decltype(KS)::value;
-    sfor<NMF>([&](auto J) __attribute__((always_inline)) {
-      constexpr int j = decltype(J)::value, RPM = (NFR + NMF - 1) / NMF;
-      mf1(IC<set>{}, J);
-      sfor<RPM>([&](auto R) __attribute__((always_inline)) {
-        constexpr int r = j * RPM + decltype(R)::value;
-        if constexpr (r < NFR) rd1(IC<set ^ 1>{}, IC<r>{}, st, ks);
+  // A k-tile in stage st; its successor in stn.  EARLY: the rest of the loads of k-tile kt + NST - 1 goes out into stage stl (the one in front of st);  VMW: loads that may stay in flight at the
+  // barrier, behind which the first loads of k-tile kt + NST follow;  < 0: nothing more to load, the count follows from rem, the number of k-tiles behind this one
+  auto ktile = [&](auto EARLY, auto VMW, int kt, int st, int stn, int stl, int rem) __attribute__((always_inline)) {
+    constexpr int vmw = decltype(VMW)::value, LAST = NG - DIST;
+    sfor<NG>([&](auto GI) __attribute__((always_inline)) {
+      constexpr int gi = decltype(GI)::value, ks = gi / MI, mi = gi % MI;
+      if constexpr (gi == LAST) {
+        wait_lgkmcnt0();
+        if constexpr (vmw >= 0) wait_vmcnt<vmw>();
+        else if (rem >= 3) wait_vmcnt<2 * LPT>();
+        else if (rem == 2) wait_vmcnt<LPT>();
+        else wait_vmcnt<0>();
+        __builtin_amdgcn_s_barrier();
+        BSR_SCHED_FENCE();
+      }
+      sfor<NI>([&](auto J) __attribute__((always_inline)) {
+        constexpr int j = decltype(J)::value;
+        if constexpr (F16) acc[mi][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[ks][j], a[gi % RING], acc[mi][j], 0, 0, 0);
+        else acc[mi][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[ks][j]), __builtin_bit_cast(bf16x8, a[gi % RING]), acc[mi][j], 0, 0, 0);
+        if constexpr (j == 0) {                    // (into the place of the group before, whose instructions have been issued)
+          if constexpr (gi + DIST < NG) read_a(IC<gi + DIST>{}, st);
+          else read_a(IC<gi + DIST - NG>{}, stn);
+        }
+        // the next k-step's fragments of B: two a group, those of the next k-tile right behind the barrier, those of this one's second half in the middle of its first
+        constexpr int at = ks == 0 ? gi - (MI / 2 - 1) : gi - (LAST > MI ? LAST : MI);
+        constexpr int jb = 2 * at + j;
+        if constexpr (j < 2 && at >= 0 && jb < NI && (ks == 1 || MI >= 4)) {
+          if constexpr (ks == 0) read_b(IC<1>{}, IC<jb>{}, st);
+          else read_b(IC<0>{}, IC<jb>{}, stn);
+        }
+        if constexpr (MI < 4 && ks == 0 && gi == 0 && j == NI - 1) sfor<NI>([&](auto Q) __attribute__((always_inline)) { read_b(IC<1>{}, Q, st); });
+        BSR_SCHED_FENCE();
       });
-      if constexpr (decltype(LOADS)::value) loads_at(IC<POST + (ks - 1) * NMF + j>{}, ktl, stl);
-      BSR_SCHED_FENCE();
-    });
-  };
-  // the last k-step of k-tile kt, with the barrier.  VMW >= 0: loads that may stay in flight there; < 0: nothing is issued any more, the count follows from what is left
-  auto klast = [&](auto VMW, int kt, int st, int stn, int rem) __attribute__((always_inline)) {
-    constexpr int vmw = decltype(VMW)::value, RPP = (NFR + POST - 1) / POST;
-    sfor<PRE>([&](auto J) __attribute__((always_inline)) { mf1(IC<1>{}, J); BSR_SCHED_FENCE(); });
-    wait_lgkmcnt0();
-    if constexpr (vmw >= 0) wait_vmcnt<vmw>();
-    else if (rem >= 3) wait_vmcnt<2 * LPT>();
-    else if (rem == 2) wait_vmcnt<LPT>();
-    else wait_vmcnt<0>();
-    __builtin_amdgcn_s_barrier();
-    BSR_SCHED_FENCE();
-    sfor<POST>([&](auto P) __attribute__((always_inline)) {
-      constexpr int p = decltype(P)::value;
-      mf1(IC<1>{}, IC<PRE + p>{});
-      sfor<RPP>([&](auto R) __attribute__((always_inline)) {
-        constexpr int r = p * RPP + decltype(R)::value;
-        if constexpr (r < NFR) rd1(IC<0>{}, IC<r>{}, stn, 0);
-      });
-      if constexpr (vmw >= 0) loads_at(P, kt + NST, st);
+      if constexpr (gi >= LAST) {
+        if constexpr (vmw >= 0) loads(IC<gi - LAST>{}, kt + NST, st);
+      } else if constexpr (decltype(EARLY)::value) loads(IC<gi + DIST>{}, kt + NST - 1, stl);
       BSR_SCHED_FENCE();
     });
   };
@@ -183,53 +186,47 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
     if (fl >= 3) wait_vmcnt<3 * LPT>(); else if (fl == 2) wait_vmcnt<2 * LPT>(); else if (fl == 1) wait_vmcnt<LPT>(); else wait_vmcnt<0>();
   }
   __builtin_amdgcn_s_barrier();
-  sfor<NFR>([&](auto J) __attribute__((always_inline)) { rd1(IC<0>{}, J, 0, 0); });
+  sfor<DIST>([&](auto I) __attribute__((always_inline)) { read_a(I, 0); });
+  sfor<NI>([&](auto J) __attribute__((always_inline)) { read_b(IC<0>{}, J, 0); });
   int st = 0, kt = 0;
-  auto ktile = [&](auto LOADS, auto VMW) __attribute__((always_inline)) {
-    const int stn = (st + 1 == NST) ? 0 : st + 1, stl = st == 0 ? NST - 1 : st - 1;
-    kstep(IC<0>{}, LOADS, IC<1>{}, st, kt + NST - 1, stl);
-    kstep(IC<1>{}, LOADS, IC<2>{}, st, kt + NST - 1, stl);
-    kstep(IC<0>{}, LOADS, IC<3>{}, st, kt + NST - 1, stl);
-    klast(VMW, kt, st, stn, nk - 1 - kt);
+  auto step = [&](auto EARLY, auto VMW) __attribute__((always_inline)) {
+    const int stn = st + 1 == NST ? 0 : st + 1, stl = st == 0 ? NST - 1 : st - 1;
+    ktile(EARLY, VMW, kt, st, stn, stl, nk - 1 - kt);
     st = stn;
     ++kt;
   };
   constexpr IC<(NST - 2) * LPT> steady{};
-  if constexpr (LATE) {
-    if (kt + NST < nk) ktile(IC<0>{}, steady);
-    while (kt + NST < nk) ktile(IC<1>{}, steady);
-    if (kt > 0) ktile(IC<1>{}, IC<-1>{});
-  } else {
-    while (kt + NST < nk) ktile(IC<0>{}, steady);
-  }
-  while (kt < nk) ktile(IC<0>{}, IC<-1>{});
+  if (kt + NST < nk) step(IC<0>{}, steady);        // (the first stages' loads are all out)
+  while (kt + NST < nk) step(IC<1>{}, steady);
+  if (kt > 0 && kt < nk) step(IC<1>{}, IC<-1>{});  // the rest of the last loads
+  while (kt < nk) step(IC<0>{}, IC<-1>{});
   // every wavefront is past the last barrier, i.e. has read its last fragments of the tiles (the reads behind it are idle): wait for those before the stages are used for anything else
   wait_lgkmcnt0();
 }
 
 template <class S> struct Wave {                   // where a wavefront's part of a tile lies
-  int lane, lm, lh, wm, wn, row0, col0;
+  int lane, lm, lq, wm, wn, row0, col0;
   __device__ __forceinline__ Wave(int m0, int n0) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    lane = threadIdx.x & 63; lm = lane & 31; lh = lane >> 5; wm = wave / S::WN; wn = wave % S::WN;
+    lane = threadIdx.x & 63; lm = lane & 15; lq = lane >> 4; wm = wave / S::WN; wn = wave % S::WN;
     row0 = m0 + wm * S::TM; col0 = n0 + wn * S::TN;
   }
   // column (in the wavefront's part) of element r of acc[..][ni]
-  __device__ __forceinline__ int col(int ni, int r) const { return ni * 32 + 8 * (r / 4) + 4 * lh + r % 4; }
+  __device__ __forceinline__ int col(int ni, int r) const { return ni * 16 + 4 * lq + r; }
   __device__ __forceinline__ unsigned char* patch(unsigned char* smem) const { return smem + (wm * S::WN + wn) * S::patch; }
 };
 
-// bias and powers of two of a lane's 16 NI classes; classes past the last one: -inf
+// bias and powers of two of a lane's 4 NI classes; classes past the last one: -inf
 template <class S, bool F16> struct Classes {
-  float b[S::NI][16];
-  int e[F16 ? S::NI : 1][16];
+  float b[S::NI][4];
+  int e[F16 ? S::NI : 1][4];
   bool edge;                                       // some lie past the last one (of the whole wavefront)
   __device__ __forceinline__ Classes(const CeGemm& g, const Wave<S>& w) {
     edge = w.col0 + S::TN > g.N;
 #pragma unroll
     for (int ni = 0; ni < S::NI; ++ni)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
+      for (int r = 0; r < 4; ++r) {
         const int n = w.col0 + w.col(ni, r), nc = min(n, g.N - 1);
         b[ni][r] = g.bias ? g.bias[nc] : 0.f;
         if constexpr (F16) e[ni][r] = g.eb[nc];
@@ -241,6 +238,13 @@ template <class S, bool F16> struct Classes {
   }
 };
 
+// of lanes l, l ^ 16, l ^ 32 and l ^ 48
+template <class Op> __device__ __forceinline__ float quarters_all(float v, Op op) {
+  v = halves_all(v, op);
+  const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
+}
+
 constexpr float LOG2E = 1.4426950408889634f;
 __device__ __forceinline__ float2 joined(float2 p, float2 q) {   // two maxima with their sums of exp(z - maximum)
   const float most = fmaxf(p.x, q.x), ref = most == -INFINITY ? 0.f : most;
@@ -249,44 +253,44 @@ __device__ __forceinline__ float2 joined(float2 p, float2 q) {   // two maxima w
 
 // Forward: a row's maximum and sum over the tile's classes.  (fmaxf passes NaN over, the sum does not; a row of -inf alone has sum 0.)
 template <class S, bool F16>
-__device__ __forceinline__ void end_stats(const CeGemm& g, f32x16 (&acc)[S::MI][S::NI], int m0, int n0, int tn, unsigned char* smem) {
+__device__ __forceinline__ void end_stats(const CeGemm& g, f32x4 (&acc)[S::MI][S::NI], int m0, int n0, int tn, unsigned char* smem) {
   const Wave<S> w(m0, n0);
   const Classes<S, F16> cl(g, w);
   float2* red = (float2*)smem;                     // [WN][BM]
 #pragma unroll
   for (int mi = 0; mi < S::MI; ++mi) {
-    const int m = w.row0 + mi * 32 + w.lm;
+    const int m = w.row0 + mi * 16 + w.lm;
     const int at = m < g.M ? max(g.labels[m], -1) - g.v0 - w.col0 : -1, ea = F16 && m < g.M ? g.ea[m] : 0;
     float most = -INFINITY;
 #pragma unroll
     for (int ni = 0; ni < S::NI; ++ni)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[mi][ni][r] = cl.logit(acc[mi][ni][r], ea, ni, r);
+      for (int r = 0; r < 4; ++r) acc[mi][ni][r] = cl.logit(acc[mi][ni][r], ea, ni, r);
     if (cl.edge)                                   // (whatever the product of a repeated row is, it does not count)
 #pragma unroll
       for (int ni = 0; ni < S::NI; ++ni)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
+        for (int r = 0; r < 4; ++r)
           if (w.col0 + w.col(ni, r) >= g.N) acc[mi][ni][r] = -INFINITY;
 #pragma unroll
     for (int ni = 0; ni < S::NI; ++ni)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) most = fmaxf(most, acc[mi][ni][r]);
+      for (int r = 0; r < 4; ++r) most = fmaxf(most, acc[mi][ni][r]);
     if (__any(at >= 0 && at < S::TN))              // (few wavefronts hold a label)
 #pragma unroll
       for (int ni = 0; ni < S::NI; ++ni)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
+        for (int r = 0; r < 4; ++r)
           if (at == w.col(ni, r) && at + w.col0 < g.N) g.zlabel[m] = acc[mi][ni][r];
-    most = half_max(most);
+    most = quarters_all(most, [](float p, float q) { return fmaxf(p, q); });
     const float ref = most == -INFINITY ? 0.f : most;
     float s = 0.f;
 #pragma unroll
     for (int ni = 0; ni < S::NI; ++ni)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f((acc[mi][ni][r] - ref) * LOG2E);
-    s = half_sum(s);
-    if (w.lh == 0) red[w.wn * S::BM + w.wm * S::TM + mi * 32 + w.lm] = make_float2(most, s);
+      for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f((acc[mi][ni][r] - ref) * LOG2E);
+    s = quarters_all(s, [](float p, float q) { return p + q; });
+    if (w.lq == 0) red[w.wn * S::BM + w.wm * S::TM + mi * 16 + w.lm] = make_float2(most, s);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < S::BM && m0 + i < g.M; i += S::NT) {
@@ -297,25 +301,16 @@ __device__ __forceinline__ void end_stats(const CeGemm& g, f32x16 (&acc)[S::MI][
   }
 }
 
-// sums of 32 (or 16) values over the 32 lanes of each half of the wavefront: lane l of a half gets that of value l (l % 16).  Each step halves the values a lane holds
-template <int N> __device__ __forceinline__ float half_sums(float (&v)[N]) {
-  static_assert(N == 32 || N == 16, "");
+// sums of 16 (or 8) values over each 16 lanes: lane l gets that of value l % 16 (l % 8).  Each step halves the values a lane holds
+template <int N> __device__ __forceinline__ float lanes16_sums(float (&v)[N]) {
+  static_assert(N == 16 || N == 8, "");
   const int l = threadIdx.x;
-  if constexpr (N == 32) {
+  if constexpr (N == 16)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {                 // (swapping rows of 16 lanes leaves both addends of the value that stays)
-      const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 16]), false, false);
-      v[i] = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
-    }
-  } else {
+    for (int i = 0; i < 8; ++i) v[i] = (l & 8 ? v[i + 8] : v[i]) + dpp_move<0x128>(l & 8 ? v[i] : v[i + 8]);        // lane ^ 8
+  else
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
-      v[i] = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = (l & 8 ? v[i + 8] : v[i]) + dpp_move<0x128>(l & 8 ? v[i] : v[i + 8]);          // lane ^ 8
+    for (int i = 0; i < 8; ++i) v[i] += dpp_move<0x128>(v[i]);
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = (l & 4 ? v[i + 4] : v[i]) + dpp_move<0x141>(l & 4 ? v[i] : v[i + 4]);          // lane ^ 7, which holds the same values so far
 #pragma unroll
@@ -325,18 +320,18 @@ template <int N> __device__ __forceinline__ float half_sums(float (&v)[N]) {
 
 // Backward: the tile as G, in fp16 times 2^14, rows of 32 tokens at a time through a patch of LDS, from which rows are read as they lie and, with the transposing reads, columns
 template <class S, bool F16, int SEG, bool DB>
-__device__ __forceinline__ void end_grad(const CeGemm& g, f32x16 (&acc)[S::MI][S::NI], int m0, int n0, int tm, unsigned char* smem) {
+__device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S::NI], int m0, int n0, int tm, unsigned char* smem) {
   constexpr int NI = S::NI, TERMS = SEG == 3 ? 2 : 1, TERM = 32 * S::LDR;
   const Wave<S> w(m0, n0);
   const Classes<S, F16> cl(g, w);
   unsigned char* patch = w.patch(smem);
-  float sum[DB ? NI * 16 : 1];
+  float sum[DB ? NI * 4 : 1];
   if constexpr (DB)
 #pragma unroll
-    for (int i = 0; i < NI * 16; ++i) sum[i] = 0.f;
+    for (int i = 0; i < NI * 4; ++i) sum[i] = 0.f;
 #pragma unroll
   for (int mi = 0; mi < S::MI; ++mi) {
-    const int m = w.row0 + mi * 32 + w.lm, mc = min(m, g.M - 1);
+    const int m = w.row0 + mi * 16 + w.lm, mc = min(m, g.M - 1);
     const int label = max(g.labels[mc], -1), ea = F16 ? g.ea[mc] : 0, at = label - g.v0 - w.col0;
     const float2 st = g.stats[mc];
     const float weight = g.row_grad ? g.row_grad[mc] : 1.f;
@@ -346,35 +341,35 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x16 (&acc)[S::MI][S
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[mi][ni][r] = __builtin_amdgcn_exp2f(fmaf(cl.logit(acc[mi][ni][r], ea, ni, r) - st.x, LOG2E, c));
+      for (int r = 0; r < 4; ++r) acc[mi][ni][r] = __builtin_amdgcn_exp2f(fmaf(cl.logit(acc[mi][ni][r], ea, ni, r) - st.x, LOG2E, c));
     if (__any(at >= 0 && at < S::TN))              // (few wavefronts hold a label)
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[mi][ni][r] -= at == w.col(ni, r) ? (float)(1 << G_SHIFT) : 0.f;
+        for (int r = 0; r < 4; ++r) acc[mi][ni][r] -= at == w.col(ni, r) ? (float)(1 << G_SHIFT) : 0.f;
     if (!__all(counts) || cl.edge)
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[mi][ni][r] = counts && w.col0 + w.col(ni, r) < g.N ? acc[mi][ni][r] : 0.f;
+        for (int r = 0; r < 4; ++r) acc[mi][ni][r] = counts && w.col0 + w.col(ni, r) < g.N ? acc[mi][ni][r] : 0.f;
     if constexpr (DB)
 #pragma unroll
-      for (int i = 0; i < NI * 16; ++i) sum[i] = counts ? fmaf(weight, acc[mi][i / 16][i % 16], sum[i]) : sum[i];
+      for (int i = 0; i < NI * 4; ++i) sum[i] = counts ? fmaf(weight, acc[mi][i / 4][i % 4], sum[i]) : sum[i];
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni)
+    for (int ni = 0; ni < NI; ++ni) {
+      f16x4 h, l;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        f16x4 h, l;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p = acc[mi][ni][4 * q + j];
-          h[j] = (f16)p;
-          if constexpr (TERMS == 2) l[j] = (f16)(p - (float)h[j]);
-        }
-        unsigned char* to = patch + w.lm * S::LDR + (ni * 32 + 8 * q + 4 * w.lh) * 2;
-        *(f16x4*)to = h;
-        if constexpr (TERMS == 2) *(f16x4*)(to + TERM) = l;
+      for (int j = 0; j < 4; ++j) {
+        const float p = acc[mi][ni][j];
+        h[j] = (f16)p;
+        if constexpr (TERMS == 2) l[j] = (f16)(p - (float)h[j]);
       }
+      unsigned char* to = patch + (mi % 2 * 16 + w.lm) * S::LDR + w.col(ni, 0) * 2;
+      *(f16x4*)to = h;
+      if constexpr (TERMS == 2) *(f16x4*)(to + TERM) = l;
+    }
+    if (mi % 2 == 0) continue;
+    const int first = w.row0 + (mi - 1) * 16;      // the patch's 32 tokens
     wave_fence();
 #pragma unroll
     for (int term = 0; term < TERMS; ++term) {
@@ -384,13 +379,13 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x16 (&acc)[S::MI][S
         f16* to = g.G + term * g.tg;
 #pragma unroll
         for (int p = 0; p < 32 / RPP; ++p) {
-          const int r = p * RPP + w.lane / CPR, row = w.row0 + mi * 32 + r;
+          const int r = p * RPP + w.lane / CPR, row = first + r;
           if (row < g.M && n < g.ldg) *(f16x8*)(to + (int64_t)row * g.ldg + n) = *(const f16x8*)(patch + term * TERM + r * S::LDR + k * 16);
         }
       }
       if (g.GT) {
         // 16 lanes read 4 tokens x 16 classes (lane 4 e + q names the address of classes 4 q .. of token e) and get a class each, four tokens of it; two such reads are 16 bytes of GT
-        const int j = w.lane & 15, octet = w.lane >> 4, token = w.row0 + mi * 32 + octet * 8;
+        const int j = w.lane & 15, octet = w.lane >> 4, token = first + octet * 8;
         const unsigned char* from = patch + term * TERM + (octet * 8 + (j >> 2)) * S::LDR + (j & 3) * 8;
         f16* to = g.GT + term * g.tgt;
         typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -407,11 +402,11 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x16 (&acc)[S::MI][S
     wave_fence();
   }
   if constexpr (DB) {
-    // sums over the tile's tokens: the lanes of each half, then the wavefronts in order
-    const float v = half_sums<NI * 16>(sum);
+    // sums over the tile's tokens: lanes, then the wavefronts in order
+    const float v = lanes16_sums<NI * 4>(sum);
     __syncthreads();
     float* red = (float*)smem;                     // [WM][BN]
-    if (NI == 2 || w.lm < 16) red[w.wm * S::BN + w.wn * S::TN + w.col(w.lm / 16, w.lm % 16)] = v;
+    if (w.lm < NI * 4) red[w.wm * S::BN + w.wn * S::TN + w.col(w.lm / 4, w.lm % 4)] = v;
     __syncthreads();
     for (int i = threadIdx.x; i < S::BN && n0 + i < g.N; i += S::NT) {
       float t = red[i];
@@ -428,7 +423,7 @@ __global__ __launch_bounds__(S::NT, 1) void ce_logits_kernel(CeGemm g, int mt, i
   int tm, tn;
   tile_at(xcd_remap(blockIdx.x, gridDim.x), mt, nt, tm, tn);
   const int m0 = tm * S::BM, n0 = tn * S::BN;
-  f32x16 acc[S::MI][S::NI];
+  f32x4 acc[S::MI][S::NI];
   multiply<S, F16, SEG>(g, m0, n0, 0, m0 < g.M ? SEG * g.nk : 0, smem, acc);      // (tokens that only fill GT's last k-tile: zeros)
   __syncthreads();
   if constexpr (MODE == STATS) end_stats<S, F16>(g, acc, m0, n0, tn, smem);
@@ -448,7 +443,7 @@ __global__ __launch_bounds__(S::NT, 1) void ce_grads_kernel(CeGemm a, CeGemm b, 
   int tm, tn;
   tile_at(id - split * mt * nt, mt, nt, tm, tn);
   const int m0 = tm * S::BM, n0 = tn * S::BN, kt0 = split * g.per;
-  f32x16 acc[S::MI][S::NI];
+  f32x4 acc[S::MI][S::NI];
   multiply<S, true, SEG>(g, m0, n0, kt0, min(g.per, SEG * g.nk - kt0), smem, acc);
   __syncthreads();
   const Wave<S> w(m0, n0);
@@ -462,13 +457,12 @@ __global__ __launch_bounds__(S::NT, 1) void ce_grads_kernel(CeGemm a, CeGemm b, 
   for (int mi = 0; mi < S::MI; ++mi) {
 #pragma unroll
     for (int ni = 0; ni < S::NI; ++ni)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *(f32x4*)(patch + w.lm * S::LDF + (ni * 32 + 8 * q + 4 * w.lh) * 4) = f32x4{acc[mi][ni][4 * q], acc[mi][ni][4 * q + 1], acc[mi][ni][4 * q + 2], acc[mi][ni][4 * q + 3]};
+      *(f32x4*)(patch + (mi % 2 * 16 + w.lm) * S::LDF + w.col(ni, 0) * 4) = acc[mi][ni];
+    if (mi % 2 == 0) continue;
     wave_fence();
 #pragma unroll 4
     for (int p = 0; p < 32 / RPP; ++p) {
-      const int r = p * RPP + w.lane / CPR, m = w.row0 + mi * 32 + r;
+      const int r = p * RPP + w.lane / CPR, m = w.row0 + (mi - 1) * 16 + r;
       f32x4 v = *(const f32x4*)(patch + r * S::LDF + c * 16);
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = ldexpf(v[j], e[j]);
