@@ -44,8 +44,8 @@ struct CeGemm {
   int v0 = 0, classes = 0;                         // classes of the whole layer
   float2* parts = nullptr; float* zlabel = nullptr;                        // STATS: [tile of classes][M] maximum and sum; [M]
   const float2* stats = nullptr; const float* row_grad = nullptr;          // GRAD: [M] maximum, log of the sum; weights or null
-  f16 *G = nullptr, *GT = nullptr;                 // GRAD: [terms][M][ldg], [terms][N][ldgt], columns behind the last one zero; null: not wanted
-  int64_t ldg = 0, ldgt = 0, tg = 0, tgt = 0;
+  f16 *G = nullptr, *GT = nullptr;                 // GRAD: [terms][M][ldg], [terms][N][ldgt], of which kg and kgt columns are written, zero behind the last one; null: not wanted
+  int64_t ldg = 0, ldgt = 0, tg = 0, tgt = 0; int kg = 0, kgt = 0;
   float* dbp = nullptr; int64_t ldd = 0;           // GRAD: [tile of tokens][ldd] sums of g G; null: not wanted
   // products of G
   float* part = nullptr; int64_t ldp = 0, tp = 0; bool add = false;        // [split][M][ldp] fp32 (of what was there as well)
@@ -62,6 +62,7 @@ template <int BM_, int BN_, int WM_, int WN_, int NST_> struct Shape {
   static constexpr size_t lds = stages > (size_t)patch * WM * WN ? stages : (size_t)patch * WM * WN;
 };
 typedef Shape<256, 256, 2, 4, 2> Large;
+typedef Shape<256, 256, 2, 2, 2> LargeForward;     // (four wavefronts read a third less of LDS for the product, eight share the work of ending a tile)
 typedef Shape<128, 128, 2, 4, 3> Small;
 typedef Shape<32, 256, 1, 4, 4> Few;
 
@@ -100,21 +101,27 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
   const f16* __restrict__ B = (const f16*)g.B + (int64_t)n0 * g.ldb;
   // rows past the last one repeat it: they only feed accumulators that count for nothing
   const int lrow = tid >> 3, kc = (tid & 7) ^ place(lrow);
-  unsigned off[LPT];
+  unsigned off[LPT];                               // in bytes: beside an address that the wavefront shares they cost no arithmetic
 #pragma unroll
-  for (int i = 0; i < AL; ++i) off[i] = (unsigned)min(i * RPI + lrow, g.M - 1 - m0) * (unsigned)g.lda + kc * 8;
+  for (int i = 0; i < AL; ++i) off[i] = (unsigned)min(i * RPI + lrow, g.M - 1 - m0) * (unsigned)g.lda * 2 + kc * 16;
 #pragma unroll
-  for (int i = 0; i < BL; ++i) off[AL + i] = (unsigned)min(i * RPI + lrow, g.N - 1 - n0) * (unsigned)g.ldb + kc * 8;
+  for (int i = 0; i < BL; ++i) off[AL + i] = (unsigned)min(i * RPI + lrow, g.N - 1 - n0) * (unsigned)g.ldb * 2 + kc * 16;
   auto issue1 = [&](auto I, int kt, int st) __attribute__((always_inline)) {
     constexpr int i = decltype(I)::value;
-    const f16* src;
-    if constexpr (SEG == 1) src = (i < AL ? A : B) + (int64_t)(kt0 + kt) * BK;
-    else {
-      const int k = kt0 + kt, seg = (k >= g.nk) + (k >= 2 * g.nk);
-      src = (i < AL ? A + (seg == 2 ? g.ta : 0) : B + (seg == 1 ? g.tb : 0)) + (int64_t)(k - seg * g.nk) * BK;
+    const f16* src = i < AL ? A : B;
+    int k = kt0 + kt;
+    if constexpr (SEG == 3) {
+      const int seg = (k >= g.nk) + (k >= 2 * g.nk);
+      src += i < AL ? (seg == 2 ? g.ta : 0) : (seg == 1 ? g.tb : 0);
+      k -= seg * g.nk;
     }
+    // (a buffer: address of the tile in scalar registers, the row's bytes in a vector register, the k-tile's in a scalar one, and no arithmetic)
     unsigned char* dst = smem + st * STAGE + wave * 1024 + (i < AL ? i * RPI * 128 : BM * 128 + (i - AL) * RPI * 128);
-    __builtin_amdgcn_global_load_lds(BSR_GLOBAL_PTR(src + off[i]), BSR_LDS_VOID(dst), 16, 0, 0);
+#ifdef __HIP_DEVICE_COMPILE__
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)src, 0, -1, 0x00020000), BSR_LDS_VOID(dst), 16, off[i], k * BK * 2, 0, 0);
+#else
+    (void)src; (void)dst; (void)k;                 // (the host's pass does not know these instructions)
+#endif
   };
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi)
@@ -162,10 +169,10 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
           if constexpr (gi + DIST < NG) read_a(IC<gi + DIST>{}, st);
           else read_a(IC<gi + DIST - NG>{}, stn);
         }
-        // the next k-step's fragments of B: two a group, those of the next k-tile right behind the barrier, those of this one's second half in the middle of its first
+        // the next k-step's fragments of B: a few a group, those of the next k-tile right behind the barrier, those of this one's second half in the middle of its first
         constexpr int at = ks == 0 ? gi - (MI / 2 - 1) : gi - (LAST > MI ? LAST : MI);
-        constexpr int jb = 2 * at + j;
-        if constexpr (j < 2 && at >= 0 && jb < NI && (ks == 1 || MI >= 4)) {
+        constexpr int BPG = (NI + DIST - 1) / DIST, jb = BPG * at + j;
+        if constexpr (j < BPG && at >= 0 && jb < NI && (ks == 1 || MI >= 4)) {
           if constexpr (ks == 0) read_b(IC<1>{}, IC<jb>{}, st);
           else read_b(IC<0>{}, IC<jb>{}, stn);
         }
@@ -380,7 +387,7 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
 #pragma unroll
         for (int p = 0; p < 32 / RPP; ++p) {
           const int r = p * RPP + w.lane / CPR, row = first + r;
-          if (row < g.M && n < g.ldg) *(f16x8*)(to + (int64_t)row * g.ldg + n) = *(const f16x8*)(patch + term * TERM + r * S::LDR + k * 16);
+          if (row < g.M && n < g.kg) *(f16x8*)(to + (int64_t)row * g.ldg + n) = *(const f16x8*)(patch + term * TERM + r * S::LDR + k * 16);
         }
       }
       if (g.GT) {
@@ -395,7 +402,7 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
           const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(from + cb * 32));
           const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(from + cb * 32 + 4 * S::LDR));
           const int n = w.col0 + cb * 16 + j;
-          if (n < g.N && token < g.ldgt) *(s16x8*)(to + (int64_t)n * g.ldgt + token) = s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          if (n < g.N && token < g.kgt) *(s16x8*)(to + (int64_t)n * g.ldgt + token) = s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         }
       }
     }
@@ -403,10 +410,17 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
   }
   if constexpr (DB) {
     // sums over the tile's tokens: lanes, then the wavefronts in order
-    const float v = lanes16_sums<NI * 4>(sum);
+    constexpr int K = NI * 4 > 16 ? 16 : NI * 4;   // values at a time
     __syncthreads();
     float* red = (float*)smem;                     // [WM][BN]
-    if (w.lm < NI * 4) red[w.wm * S::BN + w.wn * S::TN + w.col(w.lm / 4, w.lm % 4)] = v;
+#pragma unroll
+    for (int i = 0; i < NI * 4; i += K) {
+      float part[K];
+#pragma unroll
+      for (int j = 0; j < K; ++j) part[j] = sum[i + j];
+      const float v = lanes16_sums<K>(part);
+      if (w.lm < K) red[w.wm * S::BN + w.wn * S::TN + w.col((i + w.lm) / 4, w.lm % 4)] = v;
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < S::BN && n0 + i < g.N; i += S::NT) {
       float t = red[i];
@@ -564,7 +578,7 @@ struct TransposeJob {
   const void* x = nullptr; int64_t ldx = 0; int rows = 0; RowWeights rw;
   int per = 1, chunks = 0;                         // rows of a part; parts (0: no job)
   uint32_t* most = nullptr;                        // [chunks][D] bits of the largest finite |value|
-  f16* to = nullptr; int64_t ld = 0, term = 0; int* exps = nullptr;
+  f16* to = nullptr; int cols = 0; int64_t ld = 0, term = 0; int* exps = nullptr;           // cols of a row are written
 };
 constexpr int CHUNKS = 64;
 
@@ -592,7 +606,7 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
 #pragma unroll
   for (int e = 0; e < V; ++e) m[e] = 0;
   if (p < pieces)
-#pragma unroll 4
+#pragma unroll 8
     for (int r = r0 + threadIdx.x / side; r < r1; r += above) {
       const typename Loose<T>::vec v = *(const typename Loose<T>::vec*)(x + r * j.ldx + col);
       const float by = weight_of(j.rw, r);
@@ -611,61 +625,67 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
   }
 }
 
+// `down` tiles of 64 x 64 a workgroup, below one another: their columns' powers of two are worked out once, and the next tile's rows are on their way while one is turned
 template <typename T>
-__global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, TransposeJob b, int blocks, int D) {
-  constexpr int TERMS = sizeof(T) / 2, V = Chunk<T>::V, PER_ROW = 64 / V, LD = 66;
+__global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, TransposeJob b, int blocks, int down, int D) {
+  constexpr int TERMS = sizeof(T) / 2, V = Chunk<T>::V, PER_ROW = 64 / V, K = PER_ROW / 4, LD = 66;
   __shared__ f16 tile[TERMS][64][LD];              // (rows of 33 words: neither the writes down nor the reads across meet in a bank)
   __shared__ uint32_t red[4][64];
   __shared__ int exps[64];
   const bool first = (int)blockIdx.x < blocks;
   const TransposeJob j = first ? a : b;
-  const int lane = threadIdx.x % WAVE, w = threadIdx.x / WAVE, c0 = blockIdx.y * 64, m0 = (first ? blockIdx.x : blockIdx.x - blocks) * 64;
+  const int lane = threadIdx.x % WAVE, w = threadIdx.x / WAVE, c0 = blockIdx.y * 64, begin = (first ? blockIdx.x : blockIdx.x - blocks) * 64 * down, end = min(begin + 64 * down, j.cols);
   const T* x = (const T*)j.x;
-  // the tile's rows on their way first
-  typename Loose<T>::vec v[PER_ROW / 4];
-  float by[PER_ROW / 4];
-  const int c = threadIdx.x % PER_ROW * V;
+  const int c = threadIdx.x % PER_ROW * V, r0 = threadIdx.x / PER_ROW;
   const bool whole = c0 + 64 <= D;
+  typename Loose<T>::vec v[K];
+  float by[K];
+  auto fetch = [&](int m0) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < PER_ROW / 4; ++i) {
-    const int m = m0 + (int)threadIdx.x / PER_ROW + i * (256 / PER_ROW);
-    by[i] = m < j.rows ? weight_of(j.rw, m) : 0.f;
-    if (whole) v[i] = *(const typename Loose<T>::vec*)(x + (int64_t)min(m, j.rows - 1) * j.ldx + c0 + c);
-    else
+    for (int i = 0; i < K; ++i) {
+      const int m = m0 + r0 + i * (256 / PER_ROW);
+      by[i] = m < j.rows ? weight_of(j.rw, m) : 0.f;
+      if (whole) v[i] = *(const typename Loose<T>::vec*)(x + (int64_t)min(m, j.rows - 1) * j.ldx + c0 + c);
+      else
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[i][e] = m < j.rows && c0 + c + e < D ? x[(int64_t)m * j.ldx + c0 + c + e] : (T)0.f;
-  }
+        for (int e = 0; e < V; ++e) v[i][e] = m < j.rows && c0 + c + e < D ? x[(int64_t)m * j.ldx + c0 + c + e] : (T)0.f;
+    }
+  };
+  fetch(begin);
   uint32_t most = 0;
   if (c0 + lane < D)
+#pragma unroll 4
     for (int k = w; k < j.chunks; k += 4) most = max(most, j.most[(int64_t)k * D + c0 + lane]);
   red[w][lane] = most;
   __syncthreads();
   if (w == 0) {
     const int e = exponent_of(max(max(red[0][lane], red[1][lane]), max(red[2][lane], red[3][lane])));
     exps[lane] = e;
-    if (m0 == 0 && c0 + lane < D) j.exps[c0 + lane] = e;
+    if (begin == 0 && c0 + lane < D) j.exps[c0 + lane] = e;
   }
   __syncthreads();
+  for (int m0 = begin; m0 < end; m0 += 64) {
 #pragma unroll
-  for (int i = 0; i < PER_ROW / 4; ++i) {
-    const int r = (int)threadIdx.x / PER_ROW + i * (256 / PER_ROW);
+    for (int i = 0; i < K; ++i)
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float s = ldexpf(weighted((float)v[i][e], by[i]), -exps[c + e]);
-      const f16 h = (f16)s;
-      tile[0][c + e][r] = h;
-      if constexpr (TERMS == 2) tile[TERMS - 1][c + e][r] = (f16)(s - (float)h);
-    }
+      for (int e = 0; e < V; ++e) {
+        const float s = ldexpf(weighted((float)v[i][e], by[i]), -exps[c + e]);
+        const f16 h = (f16)s;
+        tile[0][c + e][r0 + i * (256 / PER_ROW)] = h;
+        if constexpr (TERMS == 2) tile[TERMS - 1][c + e][r0 + i * (256 / PER_ROW)] = (f16)(s - (float)h);
+      }
+    if (m0 + 64 < end) fetch(m0 + 64);
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int i = threadIdx.x; i < 512; i += 256) {
+        const int col = i / 8, k = i % 8 * 8;
+        const uint32_t* from = (const uint32_t*)&tile[t][col][k];
+        if (c0 + col < D && m0 + k < j.cols) *(uint4*)(j.to + t * j.term + (int64_t)(c0 + col) * j.ld + m0 + k) = make_uint4(from[0], from[1], from[2], from[3]);
+      }
+    __syncthreads();
   }
-  __syncthreads();
-#pragma unroll
-  for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-    for (int i = threadIdx.x; i < 512; i += 256) {
-      const int col = i / 8, k = i % 8 * 8;
-      const uint32_t* from = (const uint32_t*)&tile[t][col][k];
-      if (c0 + col < D && m0 + k < j.ld) *(uint4*)(j.to + t * j.term + (int64_t)(c0 + col) * j.ld + m0 + k) = make_uint4(from[0], from[1], from[2], from[3]);
-    }
 }
 
 // ------------------------------------------------------------------------------------------ joining
@@ -770,7 +790,7 @@ template <class S, Mode MODE, bool F16, int SEG, bool DB> void launch_logits(con
 template <Mode MODE, bool F16, int SEG, bool DB> void logits(int shape, const CeGemm& g, int rows, hipStream_t s) {
   if (shape == FEW) launch_logits<Few, MODE, F16, SEG, DB>(g, rows, s);
   else if (shape == SMALL) launch_logits<Small, MODE, F16, SEG, DB>(g, rows, s);
-  else launch_logits<Large, MODE, F16, SEG, DB>(g, rows, s);
+  else launch_logits<std::conditional_t<MODE == STATS, LargeForward, Large>, MODE, F16, SEG, DB>(g, rows, s);
 }
 template <class S, int SEG> void launch_grads(const CeGemm& a, const CeGemm& b, hipStream_t s) {
   auto blocks = [](const CeGemm& g) { return g.A ? over(g.M, S::BM) * over(g.N, S::BN) * g.splits : 0; };
@@ -892,8 +912,10 @@ template <typename T> void transpose(const TransposeJob& a, const TransposeJob& 
   if (a.chunks + b.chunks == 0) return;
   const int pieces = over(D, Chunk<T>::V), side = pieces > 32 ? 64 : pieces > 16 ? 32 : pieces > 8 ? 16 : 8;
   ce_colmax_kernel<T><<<dim3(over(pieces, side), a.chunks + b.chunks), 256, 0, s>>>(a, b, D);
-  const int na = a.chunks ? over(a.ld, 64) : 0, nb = b.chunks ? over(b.ld, 64) : 0;
-  ce_transpose_kernel<T><<<dim3(na + nb, over(D, 64)), 256, 0, s>>>(a, b, na, D);
+  const int tiles = (a.chunks ? over(a.cols, 64) : 0) + (b.chunks ? over(b.cols, 64) : 0);
+  const int down = (int)std::min<int64_t>(8, std::max<int64_t>(1, (int64_t)tiles * over(D, 64) / 2048));
+  const int na = a.chunks ? over(a.cols, 64 * down) : 0, nb = b.chunks ? over(b.cols, 64 * down) : 0;
+  ce_transpose_kernel<T><<<dim3(na + nb, over(D, 64)), 256, 0, s>>>(a, b, na, down, D);
 }
 void set_chunks(TransposeJob& j) {
   j.per = std::max(64, over(j.rows, CHUNKS));
@@ -953,18 +975,18 @@ void backward_as(const LinearCe& a, hipStream_t s) {
     TransposeJob tx, tw;
     if (a.dw && begin) {
       tx.x = a.x; tx.ldx = a.ldx; tx.rows = a.N; tx.rw.labels = a.labels; tx.rw.row_grad = a.row_grad; tx.rw.classes = a.V;
-      tx.most = (uint32_t*)(ws + p.mostx); tx.to = xT; tx.ld = p.Np; tx.term = (int64_t)a.D * p.Np; tx.exps = (int*)(ws + p.exT);
+      tx.most = (uint32_t*)(ws + p.mostx); tx.to = xT; tx.cols = p.Np; tx.ld = p.Np; tx.term = a.D * tx.ld; tx.exps = (int*)(ws + p.exT);
       set_chunks(tx);
     }
     if (a.dx) {
-      tw.x = wv; tw.ldx = a.ldw; tw.rows = n; tw.most = (uint32_t*)(ws + p.mostw); tw.to = wT; tw.ld = np; tw.term = (int64_t)a.D * np; tw.exps = (int*)(ws + p.ewT);
+      tw.x = wv; tw.ldx = a.ldw; tw.rows = n; tw.most = (uint32_t*)(ws + p.mostw); tw.to = wT; tw.cols = np; tw.ld = np; tw.term = a.D * tw.ld; tw.exps = (int*)(ws + p.ewT);
       set_chunks(tw);
     }
     transpose<T>(tx, tw, a.D, s);
     CeGemm g = logits_gemm(a, p, x, w, v0, n);
     g.stats = (const float2*)a.stats; g.row_grad = a.row_grad;
-    if (a.dx) { g.G = G; g.ldg = np; g.tg = (int64_t)a.N * np; }
-    if (a.dw) { g.GT = GT; g.ldgt = p.Np; g.tgt = (int64_t)n * p.Np; }
+    if (a.dx) { g.G = G; g.kg = np; g.ldg = np; g.tg = a.N * g.ldg; }
+    if (a.dw) { g.GT = GT; g.kgt = p.Np; g.ldgt = p.Np; g.tgt = n * g.ldgt; }
     if (a.db) { g.dbp = (float*)(ws + p.dbp); g.ldd = p.ldd; }
     const int shape = logits_shape(a.N, n, g.nk * SEG), rows = a.dw ? p.Np : a.N;
     if (a.db) logits<GRAD, F32, SEG, true>(shape, g, rows, s);
@@ -972,7 +994,7 @@ void backward_as(const LinearCe& a, hipStream_t s) {
     CeGemm ox, ow;
     SumJob sx, sw, sb;
     if (a.dx) {
-      ox.A = G; ox.lda = np; ox.ta = g.tg; ox.B = wT; ox.ldb = np; ox.tb = tw.term; ox.eb = tw.exps;
+      ox.A = G; ox.lda = g.ldg; ox.ta = g.tg; ox.B = wT; ox.ldb = tw.ld; ox.tb = tw.term; ox.eb = tw.exps;
       ox.M = a.N; ox.N = a.D; ox.nk = np / BK; ox.splits = p.split.x; ox.per = over(ox.nk * SEG, ox.splits);
       ox.part = (float*)(ws + p.dxp); ox.ldp = p.Dq; ox.tp = (int64_t)a.N * p.Dq; ox.add = !begin;
       if (end) {
@@ -981,7 +1003,7 @@ void backward_as(const LinearCe& a, hipStream_t s) {
       }
     }
     if (a.dw) {
-      ow.A = GT; ow.lda = p.Np; ow.ta = g.tgt; ow.B = xT; ow.ldb = p.Np; ow.tb = (int64_t)a.D * p.Np; ow.eb = (int*)(ws + p.exT);
+      ow.A = GT; ow.lda = g.ldgt; ow.ta = g.tgt; ow.B = xT; ow.ldb = p.Np; ow.tb = a.D * ow.ldb; ow.eb = (int*)(ws + p.exT);
       ow.M = n; ow.N = a.D; ow.nk = p.Np / BK; ow.splits = p.split.w; ow.per = over(ow.nk * SEG, ow.splits); ow.scale = a.grad_scale;
       char* dw = (char*)a.dw + v0 * a.lddw * (a.dw_f32 ? 4 : 2);
       if (ow.splits > 1) {
