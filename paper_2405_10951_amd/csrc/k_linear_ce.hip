@@ -582,10 +582,11 @@ struct TransposeJob {
 };
 constexpr int CHUNKS = 64;
 
-template <typename T>
+// SIDE pieces of 16 bytes side by side: a cache line, or four where that leaves enough workgroups (131072 x 4096 bf16, eight pieces: 47 against 40 us; 21841 x 768 12 against 21)
+template <typename T, int SIDE>
 __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, TransposeJob b, int D) {
-  constexpr int V = Chunk<T>::V;
-  __shared__ uint32_t red[256][V + 1];
+  constexpr int V = Chunk<T>::V, ABOVE = 256 / SIDE;
+  __shared__ uint32_t red[4][SIDE][V];
   const bool first = (int)blockIdx.y < a.chunks;
   const TransposeJob j = first ? a : b;
   const int chunk = first ? blockIdx.y : blockIdx.y - a.chunks, r0 = chunk * j.per, r1 = min(r0 + j.per, j.rows);
@@ -599,29 +600,33 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
     }
     return;
   }
-  // pieces of V columns (the last one ends with the row), 8 .. 64 of them side by side, the rows among the threads above each other
-  const int pieces = (D + V - 1) / V, side = pieces > 32 ? 64 : pieces > 16 ? 32 : pieces > 8 ? 16 : 8, above = 256 / side;
-  const int p = blockIdx.x * side + threadIdx.x % side, col = min(p * V, D - V);
+  // the last piece of V columns ends with the row; the rows among the threads above each other
+  const int s = threadIdx.x % SIDE, p = blockIdx.x * SIDE + s, col = min(p * V, D - V);
   uint32_t m[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) m[e] = 0;
-  if (p < pieces)
-#pragma unroll 8
-    for (int r = r0 + threadIdx.x / side; r < r1; r += above) {
-      const typename Loose<T>::vec v = *(const typename Loose<T>::vec*)(x + r * j.ldx + col);
-      const float by = weight_of(j.rw, r);
+#pragma unroll 4
+  for (int r = r0 + threadIdx.x / SIDE; r < r1; r += ABOVE) {
+    const typename Loose<T>::vec v = *(const typename Loose<T>::vec*)(x + r * j.ldx + col);
+    const float by = weight_of(j.rw, r);
 #pragma unroll
-      for (int e = 0; e < V; ++e) m[e] = max(m[e], bits_if_finite(weighted((float)v[e], by)));
-    }
+    for (int e = 0; e < V; ++e) m[e] = max(m[e], bits_if_finite(weighted((float)v[e], by)));
+  }
 #pragma unroll
-  for (int e = 0; e < V; ++e) red[threadIdx.x][e] = m[e];
+  for (int e = 0; e < V; ++e) {
+    float f = __uint_as_float(m[e]);               // (finite and not negative: the bits' order is the values')
+    const auto op = [](float p, float q) { return fmaxf(p, q); };
+    if constexpr (SIDE == 8) f = quarters_all(fmaxf(f, dpp_move<0x128>(f)), op);      // lanes ^ 8, ^ 16, ^ 32
+    else f = halves_all(f, op);
+    m[e] = __float_as_uint(f);
+  }
+  if (threadIdx.x % WAVE < SIDE)
+#pragma unroll
+    for (int e = 0; e < V; ++e) red[threadIdx.x / WAVE][s][e] = m[e];
   __syncthreads();
-  if ((int)threadIdx.x < side && p < pieces) {
-    for (int i = 1; i < above; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) m[e] = max(m[e], red[threadIdx.x + i * side][e]);
-#pragma unroll
-    for (int e = 0; e < V; ++e) most[col + e] = m[e];            // (columns that two pieces hold: the same from both)
+  if ((int)threadIdx.x < SIDE * V) {               // (SIDE V <= 256)
+    const int at = threadIdx.x / V, e = threadIdx.x % V, c = min((blockIdx.x * SIDE + at) * V, (unsigned)(D - V)) + e;
+    most[c] = max(max(red[0][at][e], red[1][at][e]), max(red[2][at][e], red[3][at][e]));      // (columns that two pieces hold: the same from both)
   }
 }
 
@@ -910,8 +915,9 @@ void pack(const PackJob& a, const PackJob& b, bool f32, int D, int Dp, hipStream
 
 template <typename T> void transpose(const TransposeJob& a, const TransposeJob& b, int D, hipStream_t s) {
   if (a.chunks + b.chunks == 0) return;
-  const int pieces = over(D, Chunk<T>::V), side = pieces > 32 ? 64 : pieces > 16 ? 32 : pieces > 8 ? 16 : 8;
-  ce_colmax_kernel<T><<<dim3(over(pieces, side), a.chunks + b.chunks), 256, 0, s>>>(a, b, D);
+  constexpr int LINE = 8 * Chunk<T>::V;
+  if (over(D, 4 * LINE) * (a.chunks + b.chunks) >= 1024) ce_colmax_kernel<T, 32><<<dim3(over(D, 4 * LINE), a.chunks + b.chunks), 256, 0, s>>>(a, b, D);
+  else ce_colmax_kernel<T, 8><<<dim3(over(D, LINE), a.chunks + b.chunks), 256, 0, s>>>(a, b, D);
   const int tiles = (a.chunks ? over(a.cols, 64) : 0) + (b.chunks ? over(b.cols, 64) : 0);
   const int down = (int)std::min<int64_t>(8, std::max<int64_t>(1, (int64_t)tiles * over(D, 64) / 2048));
   const int na = a.chunks ? over(a.cols, 64 * down) : 0, nb = b.chunks ? over(b.cols, 64 * down) : 0;
