@@ -693,6 +693,57 @@ __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, Trans
   }
 }
 
+// G in fp32 (from k_linear_ce_small.hip, without weights) to what the tiles leave of it: 64 tokens x 64 classes a workgroup
+template <int TERMS>
+__global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ from, int64_t ldz, CeGemm g) {
+  __shared__ float tile[64][65];
+  const int t = threadIdx.x, m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, a = t / 4, b = t % 4 * 16;      // a row (or a column) and 16 of its values
+  auto half = [](float p, f16& h, f16& l) __attribute__((always_inline)) {
+    p *= (float)(1 << G_SHIFT);
+    h = (f16)p;
+    l = (f16)(p - (float)h);
+  };
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) {
+    const bool there = m0 + a < g.M && n0 + b + i < g.N;
+    const f32x4 p = there ? *(const f32x4*)(from + (int64_t)(m0 + a) * ldz + n0 + b + i) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) tile[a][b + i + j] = v[i + j] = n0 + b + i + j < g.N ? p[j] : 0.f;
+  }
+  auto put = [&](f16* to, int64_t term) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 8) {
+      f16x8 h, l;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        f16 hj, lj;
+        half(v[i + j], hj, lj);
+        h[j] = hj;
+        l[j] = lj;
+      }
+      *(f16x8*)(to + i) = h;
+      if constexpr (TERMS == 2) *(f16x8*)(to + term + i) = l;
+    }
+  };
+  if (g.G && m0 + a < g.M) put(g.G + (int64_t)(m0 + a) * g.ldg + n0 + b, g.tg);
+  if (!g.GT && !g.dbp) return;
+  __syncthreads();
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    v[i] = tile[b + i][a];
+    const int m = m0 + b + i;
+    sum += m < g.M && g.row_grad && v[i] != 0.f ? g.row_grad[m] * v[i] : v[i];
+  }
+  if (g.GT && n0 + a < g.N) put(g.GT + (int64_t)(n0 + a) * g.ldgt + m0 + b, g.tgt);
+  if (g.dbp) {
+    sum += __shfl_xor(sum, 1);
+    sum += __shfl_xor(sum, 2);
+    if (t % 4 == 0 && n0 + a < g.N) g.dbp[blockIdx.y * g.ldd + n0 + a] = sum;
+  }
+}
+
 // ------------------------------------------------------------------------------------------ joining
 // 64 rows a workgroup: wavefront w joins tiles w, w + 16, ..., then the wavefronts in order; first and last piece of the classes: begin, end
 __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* __restrict__ parts, int tiles, int M, float2* __restrict__ run, int begin, int end, const float* __restrict__ zlabel,
@@ -855,11 +906,18 @@ Split grads_split(int64_t M, int64_t n, int64_t D, int kx, int kw) {
   return best;
 }
 
+// What goes to k_linear_ce_small.hip: little work, where the launches count; few rows backward (w is read and dw written once there), and forward where they would have to be packed first.  Its
+// logits take 16 MB at most
+constexpr size_t SMALL_BYTES = 16 << 20;
+constexpr double SMALL_WORK = 1 << 28;             // tokens x features x classes
+bool is_small(int N, int D, int V) { return small_ce_bytes(N, V) <= SMALL_BYTES && (double)N * D * V <= SMALL_WORK; }
+bool is_few(int N, int V) { return N <= 32 && small_ce_bytes(N, V) <= SMALL_BYTES; }
+
 // sizes, and places in the workspace
 struct Plan {
   int T, Dp, Np, Vs, Vp, Vc, Dq, ldd;
   Split split = {};
-  size_t xp, ex, wp, ew, parts, run, zlabel, G, GT, xT, wT, exT, ewT, mostx, mostw, dxp, dwp, dbp, bytes;
+  size_t xp, ex, wp, ew, parts, run, zlabel, G, GT, xT, wT, exT, ewT, mostx, mostw, dxp, dwp, dbp, z, bytes;
   Plan(bool f32, int N, int D, int V, bool backward) {
     T = f32 ? 2 : 1;
     Dp = up(D, BK); Np = up(N, BK); Dq = up(D, 4);
@@ -893,6 +951,7 @@ struct Plan {
     dxp = take(sizeof(float) * (size_t)split.x * N * Dq);
     dwp = take(split.w > 1 ? sizeof(float) * (size_t)split.w * Vc * Dq : 0);
     dbp = take(sizeof(float) * (size_t)over(Np, 32) * ldd);
+    z = take(is_small(N, D, V) ? small_ce_bytes(N, V) : 0);
   }
 };
 
@@ -928,6 +987,12 @@ void set_chunks(TransposeJob& j) {
   j.chunks = over(j.rows, j.per);
 }
 
+// whether tiles of the logits would leave most CUs idle, each behind a long chain of k-tiles
+bool few_tiles(int N, int V, int kt) {
+  const int shape = logits_shape(N, V, kt);
+  return (int64_t)over(N, rows_of(shape)) * over(V, cols_of(shape)) < 64;
+}
+
 CeGemm logits_gemm(const LinearCe& a, const Plan& p, const Rows& x, const Rows& w, int v0, int n) {
   CeGemm g;
   g.A = x.p; g.lda = x.ld; g.ta = x.term; g.ea = x.exps; g.B = w.p; g.ldb = w.ld; g.tb = w.term; g.eb = w.exps;
@@ -937,13 +1002,22 @@ CeGemm logits_gemm(const LinearCe& a, const Plan& p, const Rows& x, const Rows& 
 
 }  // namespace
 
-size_t linear_ce_workspace_bytes(bool f32, int N, int D, int V, bool backward) { return Plan(f32, N, D, V, backward).bytes; }
+size_t linear_ce_workspace_bytes(bool f32, int N, int D, int V, bool backward) {
+  if (backward && is_few(N, V)) return few_ce_bytes(f32, N, V, D);
+  const size_t bytes = Plan(f32, N, D, V, backward).bytes;
+  return !backward && (is_small(N, D, V) || is_few(N, V)) ? std::max(bytes, small_ce_bytes(N, V)) : bytes;
+}
 
 void linear_ce_forward(const LinearCe& a, hipStream_t s) {
+  const bool direct_x = !a.f32 && whole_rows(a.x, a.ldx, a.D), direct_w = !a.f32 && whole_rows(a.w, a.ldw, a.D);
+  const bool direct = direct_x && direct_w;
+  if ((is_small(a.N, a.D, a.V) && (!direct || few_tiles(a.N, a.V, over(a.D, BK)))) || (!direct_w && is_few(a.N, a.V))) {
+    small_ce_forward(a, s);
+    return;
+  }
   const Plan p(a.f32, a.N, a.D, a.V, false);
   char* ws = (char*)a.workspace;
   const int64_t size = a.f32 ? 4 : 2;
-  const bool direct_x = !a.f32 && whole_rows(a.x, a.ldx, a.D), direct_w = !a.f32 && whole_rows(a.w, a.ldw, a.D);
   PackJob px;
   const Rows x = rows_operand(a.x, a.ldx, a.f32, a.N, p.Dp, ws + p.xp, (int*)(ws + p.ex), direct_x, px);
   const int step = direct_w ? p.Vs : p.Vp;
@@ -970,6 +1044,8 @@ void backward_as(const LinearCe& a, hipStream_t s) {
   const bool direct_x = !F32 && whole_rows(a.x, a.ldx, a.D), direct_w = !F32 && whole_rows(a.w, a.ldw, a.D);
   PackJob px;
   const Rows x = rows_operand(a.x, a.ldx, F32, a.N, p.Dp, ws + p.xp, (int*)(ws + p.ex), direct_x, px);
+  // (little work: the logits straight from x and w, and turned into G in a launch of its own; one piece of the classes then.  Whether tiles would be the faster: few_tiles)
+  const bool turned = is_small(a.N, a.D, a.V) && p.Vc >= a.V && (!direct_x || !direct_w || few_tiles(a.N, a.V, p.Dp / BK * SEG));
   f16 *xT = (f16*)(ws + p.xT), *wT = (f16*)(ws + p.wT), *G = (f16*)(ws + p.G), *GT = (f16*)(ws + p.GT);
   for (int v0 = 0; v0 < a.V; v0 += p.Vc) {
     const int n = std::min(p.Vc, a.V - v0), np = up(n, BK);
@@ -977,7 +1053,7 @@ void backward_as(const LinearCe& a, hipStream_t s) {
     const T* wv = (const T*)a.w + v0 * a.ldw;
     PackJob pw;
     const Rows w = rows_operand(wv, a.ldw, F32, n, p.Dp, ws + p.wp, (int*)(ws + p.ew), direct_w, pw);
-    pack(begin ? px : PackJob(), pw, F32, a.D, p.Dp, s);
+    if (!turned) pack(begin ? px : PackJob(), pw, F32, a.D, p.Dp, s);
     TransposeJob tx, tw;
     if (a.dw && begin) {
       tx.x = a.x; tx.ldx = a.ldx; tx.rows = a.N; tx.rw.labels = a.labels; tx.rw.row_grad = a.row_grad; tx.rw.classes = a.V;
@@ -994,9 +1070,16 @@ void backward_as(const LinearCe& a, hipStream_t s) {
     if (a.dx) { g.G = G; g.kg = np; g.ldg = np; g.tg = a.N * g.ldg; }
     if (a.dw) { g.GT = GT; g.kgt = p.Np; g.ldgt = p.Np; g.tgt = n * g.ldgt; }
     if (a.db) { g.dbp = (float*)(ws + p.dbp); g.ldd = p.ldd; }
-    const int shape = logits_shape(a.N, n, g.nk * SEG), rows = a.dw ? p.Np : a.N;
-    if (a.db) logits<GRAD, F32, SEG, true>(shape, g, rows, s);
-    else logits<GRAD, F32, SEG, false>(shape, g, rows, s);
+    const int shape = logits_shape(a.N, n, g.nk * SEG), rows = a.dw ? p.Np : a.N, tall = turned ? 64 : rows_of(shape);
+    if (turned) {
+      float* z = (float*)(ws + p.z);
+      small_ce_gradient(a, false, z, s);
+      ce_turn_kernel<F32 ? 2 : 1><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(z, up(a.V, 4), g);
+    } else if (a.db) {
+      logits<GRAD, F32, SEG, true>(shape, g, rows, s);
+    } else {
+      logits<GRAD, F32, SEG, false>(shape, g, rows, s);
+    }
     CeGemm ox, ow;
     SumJob sx, sw, sb;
     if (a.dx) {
@@ -1025,7 +1108,7 @@ void backward_as(const LinearCe& a, hipStream_t s) {
       else launch_grads<Large, SEG>(ox, ow, s);
     }
     if (a.db) {
-      sb.part = g.dbp; sb.parts = over(rows, rows_of(shape)); sb.tp = p.ldd; sb.rows = 1; sb.cols = n; sb.scale = a.grad_scale; sb.out = a.db + v0; sb.f32 = true; sb.blocks = over(over(n, 4), 256);
+      sb.part = g.dbp; sb.parts = over(rows, tall); sb.tp = p.ldd; sb.rows = 1; sb.cols = n; sb.scale = a.grad_scale; sb.out = a.db + v0; sb.f32 = true; sb.blocks = over(over(n, 4), 256);
     }
     if (sx.blocks + sw.blocks + sb.blocks > 0) ce_sums_kernel<<<sx.blocks + sw.blocks + sb.blocks, 256, 0, s>>>(sx, sw, sb);
   }
@@ -1038,7 +1121,8 @@ void linear_ce_backward(const LinearCe& a, hipStream_t s) {
     if (a.db) ce_fill_kernel<float><<<1, 256, 0, s>>>(a.db, 0, 1, a.V);
     return;
   }
-  if (a.f32) backward_as<float>(a, s);
+  if (is_few(a.N, a.V)) few_ce_backward(a, s);
+  else if (a.f32) backward_as<float>(a, s);
   else backward_as<bf16>(a, s);
 }
 
