@@ -64,6 +64,7 @@ template <int BM_, int BN_, int WM_, int WN_, int NST_> struct Shape {
 typedef Shape<256, 256, 2, 4, 2> Large;
 typedef Shape<256, 256, 2, 2, 2> LargeForward;     // (four wavefronts read a third less of LDS for the product, eight share the work of ending a tile)
 typedef Shape<128, 128, 2, 4, 3> Small;
+typedef Shape<64, 128, 2, 2, 3> Mid;                  // (logits only: where larger tiles would leave CUs idle)
 typedef Shape<32, 256, 1, 4, 4> Few;
 
 __device__ __forceinline__ void wave_fence() {
@@ -833,9 +834,9 @@ template <auto KERNEL> void with_lds(size_t bytes) {
     __atomic_fetch_or(&known, (uint64_t)1 << (dev & 63), __ATOMIC_RELAXED);
   }
 }
-enum { LARGE, SMALL, FEW };
-int rows_of(int shape) { return shape == FEW ? Few::BM : shape == SMALL ? Small::BM : Large::BM; }
-int cols_of(int shape) { return shape == FEW ? Few::BN : shape == SMALL ? Small::BN : Large::BN; }
+enum { LARGE, SMALL, MID, FEW };
+int rows_of(int shape) { return shape == FEW ? Few::BM : shape == MID ? Mid::BM : shape == SMALL ? Small::BM : Large::BM; }
+int cols_of(int shape) { return shape == FEW ? Few::BN : shape == MID ? Mid::BN : shape == SMALL ? Small::BN : Large::BN; }
 
 template <class S, Mode MODE, bool F16, int SEG, bool DB> void launch_logits(const CeGemm& g, int rows, hipStream_t s) {
   with_lds<ce_logits_kernel<S, MODE, F16, SEG, DB>>(S::lds);
@@ -845,6 +846,7 @@ template <class S, Mode MODE, bool F16, int SEG, bool DB> void launch_logits(con
 // rows: those that tiles have to cover
 template <Mode MODE, bool F16, int SEG, bool DB> void logits(int shape, const CeGemm& g, int rows, hipStream_t s) {
   if (shape == FEW) launch_logits<Few, MODE, F16, SEG, DB>(g, rows, s);
+  else if (shape == MID) launch_logits<Mid, MODE, F16, SEG, DB>(g, rows, s);
   else if (shape == SMALL) launch_logits<Small, MODE, F16, SEG, DB>(g, rows, s);
   else launch_logits<std::conditional_t<MODE == STATS, LargeForward, Large>, MODE, F16, SEG, DB>(g, rows, s);
 }
@@ -856,11 +858,11 @@ template <class S, int SEG> void launch_grads(const CeGemm& a, const CeGemm& b, 
 
 // Models of a launch, in us: a workgroup takes a CU for start + k-tiles * tile
 struct Cost { double tile, start; };
-constexpr Cost COST[3] = {{1.7, 8}, {0.6, 4}, {0.5, 4}};
+constexpr Cost COST[4] = {{1.7, 8}, {0.6, 4}, {0.4, 4}, {0.5, 4}};
 int logits_shape(int64_t M, int64_t N, int kt) {
   int best = SMALL;
   double least = 1e30;
-  for (int shape = 0; shape < 3; ++shape) {
+  for (int shape = LARGE; shape <= FEW; ++shape) {
     if (shape == FEW && M > Few::BM) continue;
     const int64_t tiles = (int64_t)over(M, rows_of(shape)) * over(N, cols_of(shape));
     const double us = (double)((tiles + 255) / 256) * (COST[shape].start + kt * COST[shape].tile);
