@@ -865,29 +865,44 @@ def bsr_linear_ce_forward_backward(x, w, labels, bias=None, row_grad=None, grad_
     return loss, *bsr_linear_ce_backward(x, w, labels, stats, bias, row_grad, grad_scale, dx, dw, need_dx, need_dw, need_db)
 
 
-def _clip(grads, max_norm, out):
+def _clip_tensors(tensors, what):
+    """-> (addresses, numbers of values, types) of contiguous tensors on one GPU.  (Lists through map: a call walks hundreds of tensors, and the GPU is done with ViT-B's in 55 us.)"""
     import torch
+    t = torch.Tensor
+    gpu = set(map(t.get_device, tensors))
+    if len(gpu) != 1 or min(gpu) < 0:
+        raise ValueError(f"{what}: tensors on one GPU are needed, these are on {sorted({str(g.device) for g in tensors})}")
+    if not all(map(t.is_contiguous, tensors)):
+        raise ValueError(f"{what}: contiguous tensors are needed")
+    kinds = [g.dtype for g in tensors]
+    for g in tensors if not _types or not _types.keys() >= set(kinds) else ():
+        _type_code(g, what)
+    return list(map(t.data_ptr, tensors)), list(map(t.numel, tensors)), kinds
+
+
+def _clip(grads, max_norm, out):
     n = len(grads)
     if n == 0:
         raise ValueError("no gradients")
-    stream = _together(*grads, *(out or ()))
-    types = [_type_code(g, "a gradient") for g in grads]
-    for g in grads:
-        if not g.is_contiguous():
-            raise ValueError(f"gradients have to be contiguous, got shape {tuple(g.shape)}, strides {g.stride()}")
-    addresses = None
-    if out is not None:
+    at, lengths, kinds = _clip_tensors(grads, "gradients")
+    first, to = grads[0], None
+    gpu = first.get_device()
+    if out is grads:
+        to = at
+    elif out is not None:
         if len(out) != n:
             raise ValueError(f"{n} gradients, {len(out)} results")
-        if out is not grads:
-            for g, o in zip(grads, out):
-                if o.shape != g.shape or o.dtype is not g.dtype or not o.is_contiguous():
-                    raise ValueError(f"out: contiguous {g.dtype} {tuple(g.shape)} expected, got {o.dtype} {tuple(o.shape)}, strides {o.stride()}")
-        addresses = (C.c_void_p * n)(*[o.data_ptr() for o in out])
+        to, more, same = _clip_tensors(out, "out")
+        if more != lengths or same != kinds:
+            raise ValueError("out: tensors of the gradients' types and numbers of values are needed")
+        if out[0].get_device() != gpu:
+            raise ValueError(f"tensors on {first.device} and {out[0].device}")
+    import torch
     size = _scratch_size("bsr_clip_workspace_bytes", n)
-    norm, ws = grads[0].new_empty((), dtype=torch.float32), grads[0].new_empty(size, dtype=torch.uint8)
-    _check(load_library().bsr_clip_grads((C.c_void_p * n)(*[g.data_ptr() for g in grads]), (C.c_int32 * n)(*types), (C.c_int64 * n)(*[g.numel() for g in grads]), n,
-                                         max_norm, addresses, norm.data_ptr(), ws.data_ptr(), size, stream))
+    norm, ws = first.new_empty((), dtype=torch.float32), first.new_empty(size, dtype=torch.uint8)
+    addresses = C.c_void_p * n
+    _check(load_library().bsr_clip_grads(addresses(*at), (C.c_int32 * n)(*[_types[k] for k in kinds]), (C.c_int64 * n)(*lengths), n, max_norm,
+                                         None if to is None else addresses(*to), norm.data_ptr(), ws.data_ptr(), size, _raw_stream(gpu)))
     return norm
 
 
@@ -897,7 +912,8 @@ def bsr_grad_norm(grads):
 
 
 def bsr_clip_grads(grads, max_norm, out=None):
-    """grads (a list of contiguous bf16 or fp32 tensors) times min(1, max_norm / their norm taken together), in place or to `out` (a list of tensors like them)
+    """grads (a list of contiguous bf16 or fp32 tensors) times min(1, max_norm / their norm taken together), in place or to `out` (a list of contiguous tensors of
+    as many values and the same types)
     -> the norm before, fp32 scalar on their GPU."""
     grads = list(grads)
     return _clip(grads, max_norm, grads if out is None else list(out))

@@ -14,9 +14,10 @@ struct ClipTable {
   int count = 0, pieces = 0;
 };
 constexpr int CLIP_PIECE = 16384;                   // values of a piece
-constexpr int CLIP_PARTS = 1024;                    // workgroups of the first pass, together (a launch has one at least)
 inline int clip_launches(int count) { return (count + CLIP_TENSORS - 1) / CLIP_TENSORS; }
-inline size_t clip_workspace_bytes(int count) { return count < 1 ? 0 : sizeof(double) * ((size_t)CLIP_PARTS + clip_launches(count)); }
+// workgroups of a launch of the first pass, which leave a part each
+inline int clip_share(int count) { const int n = 4096 / clip_launches(count); return n < 64 ? 64 : n > 2048 ? 2048 : n; }
+inline size_t clip_workspace_bytes(int count) { return count < 1 ? 0 : sizeof(double) * (size_t)clip_share(count) * clip_launches(count); }
 
 struct ClipArgs {
   const void* const* g = nullptr; const int32_t* f32 = nullptr; const int64_t* n = nullptr; int count = 0;      // host arrays; f32: not 0 where a tensor is fp32

@@ -1,5 +1,5 @@
 // The norm of many tensors taken together, sqrt(sum over tensors, sum over values of g^2), and out = g min(1, max_norm / norm).
-// Bound by memory: every value is read twice and written once.  Pass one: at most 1024 workgroups walk the pieces of all tensors and leave a sum of squares each; pass
+// Bound by memory: every value is read twice and written once.  Pass one: at most 2048 workgroups a launch walk the pieces of all tensors and leave a sum of squares each; pass
 // two: every workgroup adds these up for itself, in the same order, while its first piece is on its way (a launch between the passes would cost as much as a few MB), and walks the pieces
 // backwards, the last read first, for what the caches still hold.  Results that lie where the gradients do are left alone when nothing is to be scaled.
 // Squares and sums are fp64: squares of fp32 gradients leave fp32's range, and sums of 10^9 of them its precision; the vector unit does them at several times the rate
@@ -137,7 +137,7 @@ int fill(ClipTable& t, const ClipArgs& a, int from) {
 }  // namespace
 
 void clip(const ClipArgs& a, hipStream_t s) {
-  const int launches = clip_launches(a.count), share = std::max(1, CLIP_PARTS / launches);
+  const int launches = clip_launches(a.count), share = clip_share(a.count);
   ClipTable t;
   int parts = 0;
   for (int l = 0; l < launches; ++l) {
@@ -152,7 +152,7 @@ void clip(const ClipArgs& a, hipStream_t s) {
   bool told = false;
   for (int l = launches - 1; l >= 0; --l) {
     if (launches > 1 && fill(t, a, l * CLIP_TENSORS) == 0) continue;
-    clip_scale_kernel<<<std::min(t.pieces, 2 * CLIP_PARTS), NT, 0, s>>>(t, a.parts, parts, a.max_norm, told ? nullptr : a.norm);
+    clip_scale_kernel<<<std::min(t.pieces, 2048), NT, 0, s>>>(t, a.parts, parts, a.max_norm, told ? nullptr : a.norm);
     told = true;
   }
 }
