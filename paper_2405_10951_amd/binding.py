@@ -140,6 +140,7 @@ def load_library():
             "bsr_rmsnorm_backward": (p, i64, p, i64, p, i64, i32, i64, i32, p, p, p, i64, p, p, C.c_size_t, p),
             "bsr_linear_ce_forward": (p, i64, p, i64, i32, i64, i32, i32, p, p, p, p, p, C.c_size_t, p),
             "bsr_linear_ce_backward": (p, i64, p, i64, i32, i64, i32, i32, p, p, p, p, f32, p, i64, p, i64, i32, p, p, C.c_size_t, p),
+            "bsr_linear_ce_forward_backward": (p, i64, p, i64, i32, i64, i32, i32, p, p, p, p, f32, p, i64, p, i64, i32, p, p, C.c_size_t, p),
             "bsr_clip_grads": (p, p, p, i32, f32, p, p, p, C.c_size_t, p),
             "bsr_quantize8_rows": (p, i32, i64, i32, i64, p, p, p),
             "bsr_quantize8_weight": (p, i32, i32, i32, i64, p, p, p, p, p),
@@ -815,11 +816,13 @@ def _linear_ce_args(x, w, labels, bias):
     return x.data_ptr(), ldx, w.data_ptr(), ldw, code, rows, width, classes, pb, _flat(labels, "labels", (rows,), torch.int32)
 
 
-def _linear_ce_workspace(x, args, backward):
+def _linear_ce_workspace(x, args, what):
     """-> (scratch or None, its bytes); torch's allocations are aligned to 512 bytes"""
+    size = _scratch_size("bsr_linear_ce_workspace_bytes", *args[4:8], what)
+    if not size:
+        return None, 0
     import torch
-    size = _scratch_size("bsr_linear_ce_workspace_bytes", *args[4:8], backward)
-    return (x.new_empty(size, dtype=torch.uint8), size) if size else (None, 0)
+    return x.new_empty(size, dtype=torch.uint8), size
 
 
 def bsr_linear_ce_forward(x, w, labels, bias=None):
@@ -828,11 +831,29 @@ def bsr_linear_ce_forward(x, w, labels, bias=None):
     import torch
     stream = _together(x, w, labels, bias)
     args = _linear_ce_args(x, w, labels, bias)
-    f32 = torch.float32
-    loss, stats = x.new_empty(x.shape[0], dtype=f32), x.new_empty((x.shape[0], 2), dtype=f32)
+    rows, f32 = x.shape[0], torch.float32
+    loss, stats = x.new_empty(rows, dtype=f32), x.new_empty((rows, 2), dtype=f32)
     ws, size = _linear_ce_workspace(x, args, 0)
     _check(load_library().bsr_linear_ce_forward(*args, loss.data_ptr(), stats.data_ptr(), _dp(ws), size, stream))
     return loss, stats
+
+
+def _linear_ce_grads(x, w, bias, row_grad, dx, dw, need_dx, need_dw, need_db):
+    """-> (dx, dw, db, row_grad's address, dx's, dx's stride, dw's address, dw's stride, dw's type code, db's address)"""
+    import torch
+    shape = x.shape
+    pg = None if row_grad is None else _flat(row_grad, "row_grad", shape[:1], torch.float32)
+    lddx = lddw = shape[1]
+    if dx is not None:
+        lddx = _rows_of(dx, "dx", shape, x.dtype)
+    elif need_dx:
+        dx = _like(x)
+    if dw is not None:
+        lddw = _rows_of(dw, "dw", w.shape)
+    elif need_dw:
+        dw = _like(w)
+    db = None if bias is None or not need_db else bias.new_empty(bias.shape)
+    return dx, dw, db, pg, _dp(dx), lddx, _dp(dw), lddw, 0 if dw is None else _type_code(dw, "dw"), _dp(db)
 
 
 def bsr_linear_ce_backward(x, w, labels, stats, bias=None, row_grad=None, grad_scale=1.0, dx=None, dw=None, need_dx=True, need_dw=True, need_db=True):
@@ -841,28 +862,23 @@ def bsr_linear_ce_backward(x, w, labels, stats, bias=None, row_grad=None, grad_s
     import torch
     stream = _together(x, w, labels, bias, stats, row_grad, dx, dw)
     args = _linear_ce_args(x, w, labels, bias)
-    f32 = torch.float32
-    ps = _flat(stats, "stats", (x.shape[0], 2), f32)
-    pg = None if row_grad is None else _flat(row_grad, "row_grad", (x.shape[0],), f32)
-    lddx = lddw = x.shape[1]
-    if dx is not None:
-        lddx = _rows_of(dx, "dx", x.shape, x.dtype)
-    elif need_dx:
-        dx = _like(x)
-    if dw is not None:
-        lddw = _rows_of(dw, "dw", w.shape)
-    elif need_dw:
-        dw = _like(w)
-    db = None if bias is None or not need_db else bias.new_empty(w.shape[0])
+    ps = _flat(stats, "stats", (x.shape[0], 2), torch.float32)
+    dx, dw, db, pg, *out = _linear_ce_grads(x, w, bias, row_grad, dx, dw, need_dx, need_dw, need_db)
     ws, size = _linear_ce_workspace(x, args, 1)
-    _check(load_library().bsr_linear_ce_backward(*args, ps, pg, grad_scale, _dp(dx), lddx, _dp(dw), lddw, 0 if dw is None else _type_code(dw, "dw"), _dp(db), _dp(ws), size, stream))
+    _check(load_library().bsr_linear_ce_backward(*args, ps, pg, grad_scale, *out, _dp(ws), size, stream))
     return dx, dw, db
 
 
 def bsr_linear_ce_forward_backward(x, w, labels, bias=None, row_grad=None, grad_scale=1.0, dx=None, dw=None, need_dx=True, need_dw=True, need_db=True):
-    """-> (loss [rows], dx, dw, db), both calls one after the other."""
-    loss, stats = bsr_linear_ce_forward(x, w, labels, bias)
-    return loss, *bsr_linear_ce_backward(x, w, labels, stats, bias, row_grad, grad_scale, dx, dw, need_dx, need_dw, need_db)
+    """-> (loss [rows], dx, dw, db) in one call."""
+    import torch
+    stream = _together(x, w, labels, bias, row_grad, dx, dw)
+    args = _linear_ce_args(x, w, labels, bias)
+    loss = x.new_empty(x.shape[0], dtype=torch.float32)
+    dx, dw, db, pg, *out = _linear_ce_grads(x, w, bias, row_grad, dx, dw, need_dx, need_dw, need_db)
+    ws, size = _linear_ce_workspace(x, args, 2)
+    _check(load_library().bsr_linear_ce_forward_backward(*args, loss.data_ptr(), pg, grad_scale, *out, _dp(ws), size, stream))
+    return loss, dx, dw, db
 
 
 def _clip_tensors(tensors, what):

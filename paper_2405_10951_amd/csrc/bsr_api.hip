@@ -2015,18 +2015,22 @@ int32_t bsr_rmsnorm_backward(const void* dy, int64_t lddy, const void* x, int64_
 static bool linear_ce_takes(int32_t type, int64_t rows, int32_t width, int32_t classes) {
   return known_type(type) && rows >= 0 && rows <= MOST_TOKENS && width >= 1 && width <= WIDEST_CE && classes >= 1 && classes <= LONGEST_ROW && rows * width <= MOST_TOKENS * 1024;
 }
-size_t bsr_linear_ce_workspace_bytes(int32_t type, int64_t rows, int32_t width, int32_t classes, int32_t backward) {
-  return rows < 1 || !linear_ce_takes(type, rows, width, classes) ? 0 : linear_ce_workspace_bytes(type == BSR_FP32, (int)rows, width, classes, backward != 0);
+// what: 0 forward, 1 backward, 2 both, with the statistics between them
+static size_t linear_ce_stats_at(bool f32, int32_t rows, int32_t width, int32_t classes) { return (linear_ce_both_bytes(f32, rows, width, classes) + 255) / 256 * 256; }
+size_t bsr_linear_ce_workspace_bytes(int32_t type, int64_t rows, int32_t width, int32_t classes, int32_t what) {
+  if (rows < 1 || what < 0 || what > 2 || !linear_ce_takes(type, rows, width, classes)) return 0;
+  const bool f32 = type == BSR_FP32;
+  return what == 2 ? linear_ce_stats_at(f32, (int)rows, width, classes) + 8 * (size_t)rows : linear_ce_workspace_bytes(f32, (int)rows, width, classes, what == 1);
 }
 
 static int32_t linear_ce_args(const char* what, LinearCe& a, const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t type, int64_t rows, int32_t width, int32_t classes,
-                              const float* bias, const int32_t* labels, void* workspace, size_t workspace_bytes, bool backward) {
+                              const float* bias, const int32_t* labels, void* workspace, size_t workspace_bytes, int32_t part) {
   if (!linear_ce_takes(type, rows, width, classes))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, rows %lld, width %d, classes %d", what, type, (long long)rows, width, classes);
   if (!rows_ok(w, type, ldw, width) || (rows > 0 && !rows_ok(x, type, ldx, width)))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: x or w is NULL, misaligned or has rows closer than %d", what, width);
   if ((bias && !aligned4(bias)) || (rows > 0 && !aligned4(labels))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: bias is misaligned, or labels NULL or misaligned", what);
-  const size_t need = rows > 0 ? linear_ce_workspace_bytes(type == BSR_FP32, (int)rows, width, classes, backward) : 0;
+  const size_t need = bsr_linear_ce_workspace_bytes(type, rows, width, classes, part);
   if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need))
     return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: workspace NULL, not aligned to 256 bytes or of %zu bytes, %zu are needed", what, workspace_bytes, need);
   a.x = x; a.ldx = ldx; a.N = (int)rows; a.w = w; a.ldw = ldw; a.V = classes; a.D = width; a.f32 = type == BSR_FP32; a.bias = bias; a.labels = labels; a.workspace = workspace;
@@ -2036,7 +2040,7 @@ static int32_t linear_ce_args(const char* what, LinearCe& a, const void* x, int6
 int32_t bsr_linear_ce_forward(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t type, int64_t rows, int32_t width, int32_t classes, const float* bias,
                               const int32_t* labels, float* loss, float* stats, void* workspace, size_t workspace_bytes, void* stream) {
   LinearCe a;
-  const int32_t rc = linear_ce_args("bsr_linear_ce_forward", a, x, ldx, w, ldw, type, rows, width, classes, bias, labels, workspace, workspace_bytes, false);
+  const int32_t rc = linear_ce_args("bsr_linear_ce_forward", a, x, ldx, w, ldw, type, rows, width, classes, bias, labels, workspace, workspace_bytes, 0);
   if (rc != BSR_OK) return rc;
   if (rows == 0) return BSR_OK;
   if ((!loss && !stats) || (loss && !aligned4(loss)) || (stats && ((uintptr_t)stats & 7)))
@@ -2046,22 +2050,44 @@ int32_t bsr_linear_ce_forward(const void* x, int64_t ldx, const void* w, int64_t
   return check_hip(nullptr, "bsr_linear_ce_forward");
 }
 
+static int32_t linear_ce_grads(const char* what, LinearCe& a, const float* row_grad, float grad_scale, void* dx, int64_t lddx, void* dw, int64_t lddw, int32_t dw_type, float* db) {
+  const int32_t type = a.f32 ? BSR_FP32 : BSR_BF16;
+  if (!dx && !dw && !db) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: none of dx, dw, db", what);
+  if (dw && (!known_type(dw_type) || (a.f32 && dw_type != BSR_FP32))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dw of type %d for w of type %d", what, dw_type, type);
+  if ((a.N > 0 && dx && !rows_ok(dx, type, lddx, a.D)) || (dw && !rows_ok(dw, dw_type, lddw, a.D)) || (db && !aligned4(db)))
+    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dx, dw or db is misaligned or has rows closer than %d", what, a.D);
+  if (a.N > 0 && row_grad && !aligned4(row_grad)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: row_grad is misaligned", what);
+  if (a.N > 0 && ((dx && (dx == a.x || dx == a.w)) || (dw && (dw == a.w || dw == a.x || dw == dx)))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dx or dw in the place of x, w or one another", what);
+  a.row_grad = row_grad; a.grad_scale = grad_scale; a.dx = a.N > 0 ? dx : nullptr; a.lddx = lddx; a.dw = dw; a.lddw = lddw; a.dw_f32 = dw_type == BSR_FP32; a.db = db;
+  return BSR_OK;
+}
+
 int32_t bsr_linear_ce_backward(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t type, int64_t rows, int32_t width, int32_t classes, const float* bias,
                                const int32_t* labels, const float* stats, const float* row_grad, float grad_scale, void* dx, int64_t lddx, void* dw, int64_t lddw, int32_t dw_type,
                                float* db, void* workspace, size_t workspace_bytes, void* stream) {
   const char* what = "bsr_linear_ce_backward";
   LinearCe a;
-  const int32_t rc = linear_ce_args(what, a, x, ldx, w, ldw, type, rows, width, classes, bias, labels, workspace, workspace_bytes, true);
+  int32_t rc = linear_ce_args(what, a, x, ldx, w, ldw, type, rows, width, classes, bias, labels, workspace, workspace_bytes, 1);
+  if (rc == BSR_OK) rc = linear_ce_grads(what, a, row_grad, grad_scale, dx, lddx, dw, lddw, dw_type, db);
   if (rc != BSR_OK) return rc;
-  if (!dx && !dw && !db) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: none of dx, dw, db", what);
-  if (dw && (!known_type(dw_type) || (type == BSR_FP32 && dw_type != BSR_FP32))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dw of type %d for w of type %d", what, dw_type, type);
-  if ((rows > 0 && dx && !rows_ok(dx, type, lddx, width)) || (dw && !rows_ok(dw, dw_type, lddw, width)) || (db && !aligned4(db)))
-    return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dx, dw or db is misaligned or has rows closer than %d", what, width);
-  if (rows > 0 && (!stats || ((uintptr_t)stats & 7) || (row_grad && !aligned4(row_grad)))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: stats is NULL or misaligned, or row_grad is", what);
-  if (rows > 0 && ((dx && (dx == x || dx == w)) || (dw && (dw == w || dw == x || dw == dx)))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dx or dw in the place of x, w or one another", what);
-  a.stats = const_cast<float*>(stats); a.row_grad = row_grad; a.grad_scale = grad_scale;
-  a.dx = rows > 0 ? dx : nullptr; a.lddx = lddx; a.dw = dw; a.lddw = lddw; a.dw_f32 = dw_type == BSR_FP32; a.db = db;
+  if (rows > 0 && (!stats || ((uintptr_t)stats & 7))) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: stats is NULL or misaligned", what);
+  a.stats = const_cast<float*>(stats);
   linear_ce_backward(a, (hipStream_t)stream);
+  return check_hip(nullptr, what);
+}
+
+int32_t bsr_linear_ce_forward_backward(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t type, int64_t rows, int32_t width, int32_t classes, const float* bias,
+                                       const int32_t* labels, float* loss, const float* row_grad, float grad_scale, void* dx, int64_t lddx, void* dw, int64_t lddw, int32_t dw_type,
+                                       float* db, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* what = "bsr_linear_ce_forward_backward";
+  LinearCe a;
+  int32_t rc = linear_ce_args(what, a, x, ldx, w, ldw, type, rows, width, classes, bias, labels, workspace, workspace_bytes, 2);
+  if (rc == BSR_OK) rc = linear_ce_grads(what, a, row_grad, grad_scale, dx, lddx, dw, lddw, dw_type, db);
+  if (rc != BSR_OK) return rc;
+  if (rows > 0 && !aligned4(loss)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: loss is NULL or misaligned", what);
+  a.loss = loss;
+  if (rows > 0) a.stats = (float*)((char*)workspace + linear_ce_stats_at(a.f32, (int)rows, width, classes));
+  linear_ce_both(a, (hipStream_t)stream);
   return check_hip(nullptr, what);
 }
 

@@ -1010,11 +1010,21 @@ size_t linear_ce_workspace_bytes(bool f32, int N, int D, int V, bool backward) {
   return !backward && (is_small(N, D, V) || is_few(N, V)) ? std::max(bytes, small_ce_bytes(N, V)) : bytes;
 }
 
+// How x and w lie, and what follows from it: the logits (or G) of little work straight from x and w, in a launch of its own, not in tiles
+struct Way {
+  bool x, w, little;                               // rows of whole 16-byte pieces; little work
+  explicit Way(const LinearCe& a) {
+    x = !a.f32 && whole_rows(a.x, a.ldx, a.D);
+    w = !a.f32 && whole_rows(a.w, a.ldw, a.D);
+    little = is_small(a.N, a.D, a.V) && (!x || !w || few_tiles(a.N, a.V, over(a.D, BK) * (a.f32 ? 3 : 1)));
+  }
+};
+
 void linear_ce_forward(const LinearCe& a, hipStream_t s) {
-  const bool direct_x = !a.f32 && whole_rows(a.x, a.ldx, a.D), direct_w = !a.f32 && whole_rows(a.w, a.ldw, a.D);
-  const bool direct = direct_x && direct_w;
-  if ((is_small(a.N, a.D, a.V) && (!direct || few_tiles(a.N, a.V, over(a.D, BK)))) || (!direct_w && is_few(a.N, a.V))) {
-    small_ce_forward(a, s);
+  const Way way(a);
+  const bool direct_x = way.x, direct_w = way.w;
+  if (way.little || (!direct_w && is_few(a.N, a.V))) {
+    small_ce_forward(a, (float*)a.workspace, GRAD_NONE, s);
     return;
   }
   const Plan p(a.f32, a.N, a.D, a.V, false);
@@ -1037,17 +1047,22 @@ void linear_ce_forward(const LinearCe& a, hipStream_t s) {
   }
 }
 
+// little work: G in fp32 first, then turned into what the tiles leave (in one piece)
+bool takes_turn(const LinearCe& a, const Plan& p, const Way& way) { return way.little && p.Vc >= a.V; }
+
+// What a forward on the same workspace has left: nothing, the packed operands (of one piece), or G of little work
+enum Ready { NOTHING, PACKED, TURNED };
 template <typename T>
-void backward_as(const LinearCe& a, hipStream_t s) {
+void backward_as(const LinearCe& a, Ready ready, hipStream_t s) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int SEG = F32 ? 3 : 1;
   const Plan p(F32, a.N, a.D, a.V, true);
   char* ws = (char*)a.workspace;
-  const bool direct_x = !F32 && whole_rows(a.x, a.ldx, a.D), direct_w = !F32 && whole_rows(a.w, a.ldw, a.D);
+  const Way way(a);
+  const bool direct_x = way.x, direct_w = way.w;
   PackJob px;
   const Rows x = rows_operand(a.x, a.ldx, F32, a.N, p.Dp, ws + p.xp, (int*)(ws + p.ex), direct_x, px);
-  // (little work: the logits straight from x and w, and turned into G in a launch of its own; one piece of the classes then.  Whether tiles would be the faster: few_tiles)
-  const bool turned = is_small(a.N, a.D, a.V) && p.Vc >= a.V && (!direct_x || !direct_w || few_tiles(a.N, a.V, p.Dp / BK * SEG));
+  const bool turned = takes_turn(a, p, way);
   f16 *xT = (f16*)(ws + p.xT), *wT = (f16*)(ws + p.wT), *G = (f16*)(ws + p.G), *GT = (f16*)(ws + p.GT);
   for (int v0 = 0; v0 < a.V; v0 += p.Vc) {
     const int n = std::min(p.Vc, a.V - v0), np = up(n, BK);
@@ -1055,7 +1070,7 @@ void backward_as(const LinearCe& a, hipStream_t s) {
     const T* wv = (const T*)a.w + v0 * a.ldw;
     PackJob pw;
     const Rows w = rows_operand(wv, a.ldw, F32, n, p.Dp, ws + p.wp, (int*)(ws + p.ew), direct_w, pw);
-    if (!turned) pack(begin ? px : PackJob(), pw, F32, a.D, p.Dp, s);
+    if (!turned && ready != PACKED) pack(begin ? px : PackJob(), pw, F32, a.D, p.Dp, s);
     TransposeJob tx, tw;
     if (a.dw && begin) {
       tx.x = a.x; tx.ldx = a.ldx; tx.rows = a.N; tx.rw.labels = a.labels; tx.rw.row_grad = a.row_grad; tx.rw.classes = a.V;
@@ -1075,7 +1090,7 @@ void backward_as(const LinearCe& a, hipStream_t s) {
     const int shape = logits_shape(a.N, n, g.nk * SEG), rows = a.dw ? p.Np : a.N, tall = turned ? 64 : rows_of(shape);
     if (turned) {
       float* z = (float*)(ws + p.z);
-      small_ce_gradient(a, false, z, s);
+      if (ready != TURNED) small_ce_gradient(a, false, z, s);
       ce_turn_kernel<F32 ? 2 : 1><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(z, up(a.V, 4), g);
     } else if (a.db) {
       logits<GRAD, F32, SEG, true>(shape, g, rows, s);
@@ -1115,17 +1130,45 @@ void backward_as(const LinearCe& a, hipStream_t s) {
     if (sx.blocks + sw.blocks + sb.blocks > 0) ce_sums_kernel<<<sx.blocks + sw.blocks + sb.blocks, 256, 0, s>>>(sx, sw, sb);
   }
 }
+static void backward_with(const LinearCe& a, Ready ready, hipStream_t s) {
+  if (a.f32) backward_as<float>(a, ready, s);
+  else backward_as<bf16>(a, ready, s);
+}
+static void no_tokens(const LinearCe& a, hipStream_t s) {
+  const unsigned grid = (unsigned)std::min(a.V, 4096);
+  if (a.dw && a.dw_f32) ce_fill_kernel<float><<<grid, 256, 0, s>>>((float*)a.dw, a.lddw, a.V, a.D);
+  else if (a.dw) ce_fill_kernel<bf16><<<grid, 256, 0, s>>>((bf16*)a.dw, a.lddw, a.V, a.D);
+  if (a.db) ce_fill_kernel<float><<<1, 256, 0, s>>>(a.db, 0, 1, a.V);
+}
 void linear_ce_backward(const LinearCe& a, hipStream_t s) {
+  if (a.N == 0) no_tokens(a, s);
+  else if (is_few(a.N, a.V)) few_ce_backward(a, false, s);
+  else backward_with(a, NOTHING, s);
+}
+
+size_t linear_ce_both_bytes(bool f32, int N, int D, int V) { return std::max(linear_ce_workspace_bytes(f32, N, D, V, false), linear_ce_workspace_bytes(f32, N, D, V, true)); }
+void linear_ce_both(const LinearCe& a, hipStream_t s) {
+  const Way way(a);
   if (a.N == 0) {
-    const unsigned grid = (unsigned)std::min(a.V, 4096);
-    if (a.dw && a.dw_f32) ce_fill_kernel<float><<<grid, 256, 0, s>>>((float*)a.dw, a.lddw, a.V, a.D);
-    else if (a.dw) ce_fill_kernel<bf16><<<grid, 256, 0, s>>>((bf16*)a.dw, a.lddw, a.V, a.D);
-    if (a.db) ce_fill_kernel<float><<<1, 256, 0, s>>>(a.db, 0, 1, a.V);
-    return;
+    no_tokens(a, s);
+  } else if (is_few(a.N, a.V) && (way.little || !way.w)) {
+    small_ce_forward(a, (float*)a.workspace, GRAD_WEIGHTED, s);
+    few_ce_backward(a, true, s);
+  } else if (is_few(a.N, a.V)) {
+    linear_ce_forward(a, s);
+    few_ce_backward(a, false, s);
+  } else {
+    const Plan f(a.f32, a.N, a.D, a.V, false), p(a.f32, a.N, a.D, a.V, true);
+    if (takes_turn(a, p, way)) {
+      small_ce_forward(a, (float*)((char*)a.workspace + p.z), GRAD_PLAIN, s);
+      backward_with(a, TURNED, s);
+    } else {
+      linear_ce_forward(a, s);
+      // (one piece in both: the packed operands lie at the same places)
+      const bool packed = !way.little && (!way.x || !way.w) && p.Vc >= a.V && (way.w ? f.Vs : f.Vp) >= a.V && f.xp == p.xp && f.ex == p.ex && f.wp == p.wp && f.ew == p.ew;
+      backward_with(a, packed ? PACKED : NOTHING, s);
+    }
   }
-  if (is_few(a.N, a.V)) few_ce_backward(a, s);
-  else if (a.f32) backward_as<float>(a, s);
-  else backward_as<bf16>(a, s);
 }
 
 }  // namespace bsr

@@ -1,6 +1,6 @@
 // Softmax cross-entropy of a linear layer and its gradients where there is little to do, or few rows: a few launches instead of tiles that fill the chip.  (The other sizes: k_linear_ce.hip.)
 // The logits, or G, are left in scratch in fp32, 16 MB at most; the products take their fragments straight from the caller's tensors, whatever their type, stride and alignment.
-//   logits   16 classes x 16 or 32 tokens a workgroup, the features split over its four wavefronts, whole cache lines each (bf16 16 x 16 x 32, fp32 16 x 16 x 4 matrix instructions, both exact products
+//   logits   16 classes x 16 or 32 tokens a workgroup, the features split over its eight wavefronts, whole cache lines each (bf16 16 x 16 x 32, fp32 16 x 16 x 4 matrix instructions, both exact products
 //            added in fp32); for the gradients they leave as G
 //   rows     a workgroup a token: maximum, sum, loss
 //   grads    up to 32 tokens: dx and dw in one pass over w, multiplied in fp32 (16 x 16 x 4)
@@ -50,12 +50,13 @@ struct Tokens {
 };
 
 // z or G [N, ldz]: lane l has V features of class l % 16 and of token l % 16
+constexpr int LOGIT_WAVES = 8;
 template <typename T, int TILES>
-__global__ __launch_bounds__(256) void small_logits_kernel(const T* __restrict__ x, int64_t ldx, const T* __restrict__ w, int64_t ldw, int D, const float* __restrict__ bias, Tokens tk,
+__global__ __launch_bounds__(LOGIT_WAVES * WAVE) void small_logits_kernel(const T* __restrict__ x, int64_t ldx, const T* __restrict__ w, int64_t ldw, int D, const float* __restrict__ bias, Tokens tk,
                                                            float* __restrict__ z, int64_t ldz) {
   constexpr int C = Chunk<T>::V, STEP = 4 * C, AT_ONCE = 4;
   typedef typename Chunk<T>::vec vec;
-  __shared__ f32x4 red[3][TILES][WAVE];
+  __shared__ f32x4 red[LOGIT_WAVES - 1][TILES][WAVE];
   const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, v0 = blockIdx.x * 16, n0 = blockIdx.y * 16 * TILES, part = lane / 16 * C, N = tk.N, V = tk.V;
   const T* wr = w + (int64_t)min(v0 + lane % 16, V - 1) * ldw;
   const T* xr[TILES];
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(256) void small_logits_kernel(const T* __restrict__
   f32x4 acc[TILES];
 #pragma unroll
   for (int t = 0; t < TILES; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int k = wave * STEP * AT_ONCE; k < D; k += 4 * STEP * AT_ONCE) {
+  for (int k = wave * STEP * AT_ONCE; k < D; k += LOGIT_WAVES * STEP * AT_ONCE) {
     vec a[AT_ONCE], b[AT_ONCE][TILES];
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
@@ -91,7 +92,10 @@ __global__ __launch_bounds__(256) void small_logits_kernel(const T* __restrict__
   for (int t = 0; t < TILES; ++t) {
     const int n = n0 + t * 16 + lane % 16;
     if (n >= N || v >= V) continue;
-    f32x4 o = (((acc[t] + red[0][t][lane]) + red[1][t][lane]) + red[2][t][lane]) + b;
+    f32x4 o = acc[t];
+#pragma unroll
+    for (int i = 0; i < LOGIT_WAVES - 1; ++i) o += red[i][t][lane];
+    o += b;
     if (tk.stats) {
       const bool counts = tk.counts(n);
       const float2 st = tk.stats[n];
@@ -104,11 +108,11 @@ __global__ __launch_bounds__(256) void small_logits_kernel(const T* __restrict__
   }
 }
 
-// a workgroup a token
-__global__ __launch_bounds__(256) void small_rows_kernel(const float* __restrict__ z, int64_t ldz, int V, const int32_t* __restrict__ labels, float* __restrict__ loss, float2* __restrict__ stats) {
+// a workgroup a token.  grad: the logits become G
+__global__ __launch_bounds__(256) void small_rows_kernel(float* __restrict__ z, int64_t ldz, Tokens tk, float* __restrict__ loss, float2* __restrict__ stats, bool grad) {
   __shared__ float red[2][4];
-  const int m = blockIdx.x, wave = threadIdx.x / WAVE;
-  const float* row = z + m * ldz;
+  const int m = blockIdx.x, wave = threadIdx.x / WAVE, V = tk.V;
+  float* row = z + m * ldz;
   float most = -INFINITY;
 #pragma unroll 4
   for (int v = threadIdx.x; v < V; v += 256) most = fmaxf(most, row[v]);
@@ -124,14 +128,20 @@ __global__ __launch_bounds__(256) void small_rows_kernel(const float* __restrict
   s = wave_sum(s);
   if (threadIdx.x % WAVE == 0) red[1][wave] = s;
   __syncthreads();
-  if (threadIdx.x != 0) return;
   s = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
   const float ls = s == 0.f ? 0.f : logf(s);
-  if (stats) stats[m] = make_float2(most, ls);
-  if (loss) {
-    const int label = labels[m];
-    loss[m] = label >= 0 && label < V && !(most == -INFINITY && s == 0.f) ? (most - row[label]) + ls : 0.f;
+  const int label = tk.labels[m];
+  const bool there = label >= 0 && label < V && !(most == -INFINITY && s == 0.f);
+  const float mine = there && threadIdx.x == 0 ? row[label] : 0.f;       // (before it becomes G)
+  if (threadIdx.x == 0) {
+    if (stats) stats[m] = make_float2(most, ls);
+    if (loss) loss[m] = there ? (most - mine) + ls : 0.f;
   }
+  if (!grad) return;
+  __syncthreads();
+  const float weight = tk.row_grad ? tk.row_grad[m] : 1.f, by = tk.weighted ? tk.scale * weight : 1.f;
+#pragma unroll 4
+  for (int v = threadIdx.x; v < V; v += 256) row[v] = there && weight != 0.f ? by * (__builtin_amdgcn_exp2f(fmaf(row[v] - most, LOG2E, -ls * LOG2E)) - (v == label ? 1.f : 0.f)) : 0.f;
 }
 
 // K values of a row from d on, zero past its end
@@ -294,8 +304,8 @@ template <typename T> __global__ __launch_bounds__(256) void few_sums_kernel(con
 
 int64_t small_ldz(const LinearCe& a) { return ((int64_t)a.V + 3) / 4 * 4; }
 template <typename T> void logits_as(const LinearCe& a, const Tokens& tk, float* z, hipStream_t s) {
-  if (a.N <= 16) small_logits_kernel<T, 1><<<dim3(over(a.V, 16), 1), 256, 0, s>>>((const T*)a.x, a.ldx, (const T*)a.w, a.ldw, a.D, a.bias, tk, z, small_ldz(a));
-  else small_logits_kernel<T, 2><<<dim3(over(a.V, 16), over(a.N, 32)), 256, 0, s>>>((const T*)a.x, a.ldx, (const T*)a.w, a.ldw, a.D, a.bias, tk, z, small_ldz(a));
+  if (a.N <= 16) small_logits_kernel<T, 1><<<dim3(over(a.V, 16), 1), LOGIT_WAVES * WAVE, 0, s>>>((const T*)a.x, a.ldx, (const T*)a.w, a.ldw, a.D, a.bias, tk, z, small_ldz(a));
+  else small_logits_kernel<T, 2><<<dim3(over(a.V, 16), over(a.N, 32)), LOGIT_WAVES * WAVE, 0, s>>>((const T*)a.x, a.ldx, (const T*)a.w, a.ldw, a.D, a.bias, tk, z, small_ldz(a));
 }
 // workgroups over the classes
 int few_wide(bool f32, int N) { return 16 * (N > 16 ? few_features<float>(2) : f32 ? few_features<float>(1) : few_features<bf16>(1)); }
@@ -314,30 +324,35 @@ template <typename T, typename TW> void grads_as(const LinearCe& a, const Tokens
 
 }  // namespace
 
-void small_ce_forward(const LinearCe& a, hipStream_t s) {
-  float* z = (float*)a.workspace;
+static Tokens tokens_of(const LinearCe& a, bool weighted) {
   Tokens tk;
-  tk.N = a.N; tk.V = a.V;
+  tk.N = a.N; tk.V = a.V; tk.labels = a.labels; tk.row_grad = a.row_grad; tk.weighted = weighted; tk.scale = weighted ? a.grad_scale : 1.f;
+  return tk;
+}
+static void logits_of(const LinearCe& a, const Tokens& tk, float* z, hipStream_t s) {
   if (a.f32) logits_as<float>(a, tk, z, s);
   else logits_as<bf16>(a, tk, z, s);
-  small_rows_kernel<<<a.N, 256, 0, s>>>(z, small_ldz(a), a.V, a.labels, a.loss, (float2*)a.stats);
+}
+
+void small_ce_forward(const LinearCe& a, float* z, SmallGrad grad, hipStream_t s) {
+  const Tokens tk = tokens_of(a, grad == GRAD_WEIGHTED);
+  logits_of(a, tk, z, s);
+  small_rows_kernel<<<a.N, 256, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad != GRAD_NONE);
 }
 
 void small_ce_gradient(const LinearCe& a, bool weighted, float* G, hipStream_t s) {
-  Tokens tk;
-  tk.weighted = weighted;
-  tk.N = a.N; tk.V = a.V; tk.labels = a.labels; tk.stats = (const float2*)a.stats; tk.row_grad = a.row_grad; tk.scale = weighted ? a.grad_scale : 1.f;
-  if (a.f32) logits_as<float>(a, tk, G, s);
-  else logits_as<bf16>(a, tk, G, s);
+  Tokens tk = tokens_of(a, weighted);
+  tk.stats = (const float2*)a.stats;
+  logits_of(a, tk, G, s);
 }
 
 static size_t few_parts_at(int N, int V) { return (small_ce_bytes(N, V) + 255) / 256 * 256; }
 size_t few_ce_bytes(bool f32, int N, int V, int D) { return few_parts_at(N, V) + sizeof(float) * (size_t)few_ranges(f32, N, V, D) * N * (((size_t)D + 3) / 4 * 4); }
-void few_ce_backward(const LinearCe& a, hipStream_t s) {
+void few_ce_backward(const LinearCe& a, bool ready, hipStream_t s) {
   float *G = (float*)a.workspace, *parts = (float*)((char*)a.workspace + few_parts_at(a.N, a.V));
-  small_ce_gradient(a, true, G, s);
-  Tokens tk;
-  tk.N = a.N; tk.V = a.V; tk.labels = a.labels; tk.stats = (const float2*)a.stats; tk.row_grad = a.row_grad;
+  if (!ready) small_ce_gradient(a, true, G, s);
+  Tokens tk = tokens_of(a, true);
+  tk.stats = (const float2*)a.stats;
   if (a.f32) grads_as<float, float>(a, tk, G, parts, s);
   else if (a.dw_f32) grads_as<bf16, float>(a, tk, G, parts, s);
   else grads_as<bf16, bf16>(a, tk, G, parts, s);

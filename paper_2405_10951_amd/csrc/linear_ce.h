@@ -20,12 +20,16 @@ struct LinearCe {
 size_t linear_ce_workspace_bytes(bool f32, int N, int D, int V, bool backward);
 void linear_ce_forward(const LinearCe& a, hipStream_t s);
 void linear_ce_backward(const LinearCe& a, hipStream_t s);
+// one after the other, the second with what the first leaves; stats (not null) is written
+size_t linear_ce_both_bytes(bool f32, int N, int D, int V);
+void linear_ce_both(const LinearCe& a, hipStream_t s);
 
 // k_linear_ce_small.hip: scratch of small_ce_bytes() for the logits, or for G [N, V in whole fours], weighted: with grad_scale and the rows' weights; the gradients of few rows (32 at most) with few_ce_bytes()
 inline size_t small_ce_bytes(int N, int V) { return sizeof(float) * (size_t)N * (((size_t)V + 3) / 4 * 4); }
-void small_ce_forward(const LinearCe& a, hipStream_t s);
+enum SmallGrad { GRAD_NONE, GRAD_PLAIN, GRAD_WEIGHTED };
+void small_ce_forward(const LinearCe& a, float* z, SmallGrad grad, hipStream_t s);      // grad: G in the logits' place
 void small_ce_gradient(const LinearCe& a, bool weighted, float* G, hipStream_t s);
 size_t few_ce_bytes(bool f32, int N, int V, int D);
-void few_ce_backward(const LinearCe& a, hipStream_t s);
+void few_ce_backward(const LinearCe& a, bool ready, hipStream_t s);                     // ready: G is there
 
 }  // namespace bsr
