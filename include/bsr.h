@@ -603,7 +603,7 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
  *   dx           [rows, width] of `type`, stride lddx;  dw [classes, width], stride lddw, of dw_type: BSR_FP32, or BSR_BF16 where w is;  db fp32 [classes];  each may be NULL
  *   workspace    device scratch of bsr_linear_ce_workspace_bytes() bytes, 256-byte aligned; what: 0 for the forward, 1 for the backward, 2 for both in one call
  * bsr_linear_ce_forward_backward: one after the other, the second with what the first leaves.
- * Limits: rows up to 2^23, width up to 2^20, their product up to 2^33; classes up to 2^30.
+ * Limits: rows up to 2^22, width up to 2^20, their product up to 2^33; classes up to 2^30.
  */
 size_t bsr_linear_ce_workspace_bytes(int32_t type, int64_t rows, int32_t width, int32_t classes, int32_t what);
 int32_t bsr_linear_ce_forward(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t type, int64_t rows, int32_t width, int32_t classes, const float* bias,

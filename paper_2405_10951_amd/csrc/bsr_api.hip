@@ -1763,7 +1763,7 @@ int32_t bsr_destroy(bsr_ctx* c) {
 // ---- operators on the caller's own tensors ------------------------------------------------------------------------------------------
 constexpr int32_t LONGEST_ROW = 1 << 30;            // (a kernel's index may run past the end by a workgroup's stride)
 constexpr int64_t LONGEST_TENSOR = (int64_t)1 << 36;  // (its pieces are counted in 32 bits)
-constexpr int64_t MOST_TOKENS = 1 << 23;            // (offsets of 32 bits within the rows of a tile of what is transposed)
+constexpr int64_t MOST_TOKENS = 1 << 22;            // (offsets of 32 bits within the rows of a tile of what is transposed)
 constexpr int32_t WIDEST_CE = 1 << 20;
 constexpr int32_t WIDEST_LAYER = 1 << 23;           // (offsets of 32 bits within the rows of a block tile)
 static bool known_type(int32_t t) { return t == BSR_BF16 || t == BSR_FP32; }
@@ -2013,7 +2013,7 @@ int32_t bsr_rmsnorm_backward(const void* dy, int64_t lddy, const void* x, int64_
 }
 
 static bool linear_ce_takes(int32_t type, int64_t rows, int32_t width, int32_t classes) {
-  return known_type(type) && rows >= 0 && rows <= MOST_TOKENS && width >= 1 && width <= WIDEST_CE && classes >= 1 && classes <= LONGEST_ROW && rows * width <= MOST_TOKENS * 1024;
+  return known_type(type) && rows >= 0 && rows <= MOST_TOKENS && width >= 1 && width <= WIDEST_CE && classes >= 1 && classes <= LONGEST_ROW && rows * width <= (int64_t)1 << 33;
 }
 // what: 0 forward, 1 backward, 2 both, with the statistics between them
 static size_t linear_ce_stats_at(bool f32, int32_t rows, int32_t width, int32_t classes) { return (linear_ce_both_bytes(f32, rows, width, classes) + 255) / 256 * 256; }

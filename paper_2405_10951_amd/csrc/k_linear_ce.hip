@@ -912,7 +912,7 @@ Split grads_split(int64_t M, int64_t n, int64_t D, int kx, int kw) {
 // logits take 16 MB at most
 constexpr size_t SMALL_BYTES = 16 << 20;
 constexpr double SMALL_WORK = 1 << 28;             // tokens x features x classes
-bool is_small(int N, int D, int V) { return small_ce_bytes(N, V) <= SMALL_BYTES && (double)N * D * V <= SMALL_WORK; }
+bool is_small(int N, int D, int V) { return N <= 1 << 20 && small_ce_bytes(N, V) <= SMALL_BYTES && (double)N * D * V <= SMALL_WORK; }      // (a launch has up to 65535 workgroups one way)
 bool is_few(int N, int V) { return N <= 32 && small_ce_bytes(N, V) <= SMALL_BYTES; }
 
 // sizes, and places in the workspace
@@ -927,7 +927,8 @@ struct Plan {
     // Backward: G, twice, takes at most 256 MB, and so does the transposed piece of w.
     auto piece = [&](double most) {
       const int64_t c = std::max<int64_t>(256, (int64_t)std::min(most, 1e9) / 256 * 256);
-      return up(over(V, over(V, (int)c)), 256);
+      const int pieces = over(V, (int)c);
+      return pieces == 1 ? up(V, BK) : up(over(V, pieces), 256);
     };
     constexpr double MB = 1 << 20;
     Vs = piece(64 * MB * 128 / (8.0 * N));
@@ -957,8 +958,8 @@ struct Plan {
   }
 };
 
-// (a tile's rows are addressed in 32 bits)
-bool whole_rows(const void* p, int64_t ld, int D) { return D % BK == 0 && ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld <= 1 << 23; }
+// (255 rows of a tile, and k behind them, are addressed in 32 bits; so are those of what is packed and transposed here: rows of 2^20 features or 2^22 tokens at most)
+bool whole_rows(const void* p, int64_t ld, int D) { return D % BK == 0 && ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld <= 1 << 22; }
 
 // An operand of the logits: as it lies, or packed by what `job` then describes
 struct Rows { const void* p; int64_t ld, term; const int* exps; };
