@@ -64,12 +64,14 @@ class FrozenStack:
             grads.append(grad)
         return grads[::-1]
 
-    def step(self, x, top_index, top_logits, labels=None, temperature=2.0, hard_weight=0.0, lr=0.0):
-        """One step of gradient descent on the mean loss -> (loss of every row [rows], gradients)"""
+    def step(self, x, top_index, top_logits, labels=None, temperature=2.0, hard_weight=0.0, lr=0.0, max_norm=None):
+        """One step of gradient descent on the mean loss -> (loss of every row [rows], gradients); max_norm: all of them taken together are brought down to that norm first"""
         logits, kept = self.forward(x)
         loss, dlogits = P.bsr_distill_forward_backward(logits, top_index, top_logits, labels, temperature, hard_weight,
                                                        grad_scale=1.0 / x.shape[0], dz=logits)
         grads = self.backward(dlogits, kept)
+        if max_norm is not None:
+            P.bsr_clip_grads([g for grad in grads for g in grad], max_norm)
         if lr:
             for norm, grad in zip(self.norms, grads):
                 for p, g in zip(norm, grad):
@@ -96,6 +98,7 @@ def main():
     for name, default in (("rows", 6304), ("width", 768), ("hidden", 1536), ("depth", 4), ("classes", 1000), ("top", 16), ("steps", 60)):
         ap.add_argument("--" + name, type=int, default=default)
     ap.add_argument("--lr", type=float, default=2.0)
+    ap.add_argument("--max-norm", type=float, default=None, help="clip the gradients, all taken together, to this norm")
     ap.add_argument("--cut-sums", action="store_true", help="let the 8-bit matrix instructions add the products")
     a = ap.parse_args()
     student, teacher = (random_stack(a.width, a.hidden, a.depth, a.classes, cut_sums=a.cut_sums) for _ in range(2))
@@ -109,7 +112,7 @@ def main():
     torch.cuda.synchronize()
     start = time.perf_counter()
     for i in range(a.steps):
-        loss, _ = student.step(x, top_index, top_logits, lr=a.lr)
+        loss, _ = student.step(x, top_index, top_logits, lr=a.lr, max_norm=a.max_norm)
         if i % 10 == 0 or i == a.steps - 1:
             print(f"step {i}: loss {loss.mean().item():.4f}", flush=True)
     torch.cuda.synchronize()
