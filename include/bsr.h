@@ -590,7 +590,7 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
  * Softmax cross-entropy of a linear layer over many classes, z = x w^T + bias, whose logits are never kept: they are made in tiles, a piece of the classes at a time, and once more
  * for the gradients.  Per row loss = log sum exp z - z_label; with g = grad_scale * row_grad[row] and G = g (softmax(z) - onehot(label)):
  *   dx = G w,   dw = G^T x,   db = sum over rows of G
- * A row whose label lies outside 0 .. classes-1 has loss 0 and counts for no gradient (its dx is 0), whatever its x holds; so does, for the gradients, one of weight 0.  A class with
+ * A row whose label lies outside 0 .. classes-1 has loss 0 and counts for no gradient (its dx is 0), whatever its x and its row_grad hold; so does, for the gradients, one of weight 0.  A class with
  * bias -inf has probability 0; a row whose logits are all -inf has loss and gradient 0, one whose label's is has loss +inf and a finite gradient.  NaN and +inf in z make a row NaN, and with it dw.
  * bf16 x and w are multiplied as they are; G is held in 11 bits (fp16, off by 2^-11 of itself, or by 2^-39 where it is below 2^-28), x and w beside it exactly down to 2^-29 of a feature's
  * largest value (with row_grad x in 11 bits too).  fp32 values are held in two terms of 11 bits each, off by 2^-22 of themselves, or by 2^-39 of the largest of their row, or of their feature, where they are below 2^-17 of it.  Sums
@@ -602,6 +602,7 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
  *   row_grad     fp32 [rows], may be NULL (1 for every row)
  *   dx           [rows, width] of `type`, stride lddx;  dw [classes, width], stride lddw, of dw_type: BSR_FP32, or BSR_BF16 where w is;  db fp32 [classes];  each may be NULL
  *   workspace    device scratch of bsr_linear_ce_workspace_bytes() bytes, 256-byte aligned; what: 0 for the forward, 1 for the backward, 2 for both in one call
+ * No result may touch an input, another result or the workspace.
  * bsr_linear_ce_forward_backward: one after the other, the second with what the first leaves.
  * Limits: rows up to 2^22, width up to 2^20, their product up to 2^33; classes up to 2^30.
  */

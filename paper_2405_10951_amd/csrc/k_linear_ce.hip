@@ -774,10 +774,10 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* __restrict_
   }
 }
 
-// out = scale row_scale[m] (sum over the parts, in order); parts of db are rows of tokens
+// out = scale weight[m] (sum over the parts, in order), 0 for rows that do not count, whatever w and their weight hold; parts of db are rows of tokens
 struct SumJob {
   const float* part = nullptr; int parts = 0; int64_t tp = 0, ldp = 0, rows = 0; int cols = 0;
-  float scale = 1.f; const float* row_scale = nullptr;
+  float scale = 1.f; RowWeights rw;                // rows by their weights
   void* out = nullptr; int64_t ldo = 0; bool f32 = false;
   int blocks = 0;
 };
@@ -809,7 +809,8 @@ __global__ __launch_bounds__(256) void ce_sums_kernel(SumJob a, SumJob b, SumJob
   f32x4 v = *(const f32x4*)at;
 #pragma unroll 4
   for (int s = 1; s < j.parts; ++s) v += *(const f32x4*)(at + s * j.tp);
-  v *= j.row_scale ? j.scale * j.row_scale[m] : j.scale;
+  const float by = weight_of(j.rw, m);
+  v = by == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : v * (j.scale * by);
   if (j.f32) put_four((float*)j.out + m * j.ldo + n, v, j.cols - n);
   else put_four((bf16*)j.out + m * j.ldo + n, v, j.cols - n);
 }
@@ -1105,7 +1106,7 @@ void backward_as(const LinearCe& a, Ready ready, hipStream_t s) {
       ox.M = a.N; ox.N = a.D; ox.nk = np / BK; ox.splits = p.split.x; ox.per = over(ox.nk * SEG, ox.splits);
       ox.part = (float*)(ws + p.dxp); ox.ldp = p.Dq; ox.tp = (int64_t)a.N * p.Dq; ox.add = !begin;
       if (end) {
-        sx.part = ox.part; sx.parts = ox.splits; sx.tp = ox.tp; sx.ldp = p.Dq; sx.rows = a.N; sx.cols = a.D; sx.scale = a.grad_scale; sx.row_scale = a.row_grad;
+        sx.part = ox.part; sx.parts = ox.splits; sx.tp = ox.tp; sx.ldp = p.Dq; sx.rows = a.N; sx.cols = a.D; sx.scale = a.grad_scale; sx.rw.labels = a.labels; sx.rw.row_grad = a.row_grad; sx.rw.classes = a.V;
         sx.out = a.dx; sx.ldo = a.lddx; sx.f32 = F32; sx.blocks = over((int64_t)a.N * over(a.D, 4), 256);
       }
     }

@@ -134,6 +134,22 @@ def test_weights_of_rows(env, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,D,V", [(20, 96, 400), (70, 96, 400), (300, 128, 9000)])
+def test_rows_without_a_label_whose_weight_is_no_number(env, N, D, V, dtype):
+    """1 / 0 for a sequence that has no labels, for instance"""
+    torch, P = env
+    x, w, labels, b = make(torch, N, D, V, dtype, 40)
+    weight = torch.rand(N, generator=torch.Generator().manual_seed(41)).cuda()
+    want = P.bsr_linear_ce_forward_backward(x, w, labels, bias=b, row_grad=weight, grad_scale=0.5)
+    none = (labels < 0) | (labels >= V)
+    weight[none] = torch.where(torch.arange(int(none.sum()), device="cuda") % 2 == 0, float("inf"), float("nan"))
+    got = P.bsr_linear_ce_forward_backward(x, w, labels, bias=b, row_grad=weight, grad_scale=0.5)
+    _, stats = P.bsr_linear_ce_forward(x, w, labels, bias=b)
+    apart = P.bsr_linear_ce_backward(x, w, labels, stats, bias=b, row_grad=weight, grad_scale=0.5)
+    assert not got[1][none].any() and all(torch.equal(g, r) for g, r in zip(got, want)) and not apart[0][none].any() and all(t.isfinite().all() for t in apart)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_features_of_different_sizes(env, dtype):
     """over a factor of 10^5 or so"""
     torch, P = env
