@@ -587,7 +587,7 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
                              void* stream);
 
 /*
- * Softmax cross-entropy of a linear layer over many classes, z = x w^T + bias, whose logits are never kept: they are made in tiles, a piece of the classes at a time, and once more
+ * Softmax cross-entropy of a linear layer over many classes, z = x w^T + bias, whose logits the caller never holds: they are made in tiles, a piece of the classes at a time, and once more
  * for the gradients.  Per row loss = log sum exp z - z_label; with g = grad_scale * row_grad[row] and G = g (softmax(z) - onehot(label)):
  *   dx = G w,   dw = G^T x,   db = sum over rows of G
  * A row whose label lies outside 0 .. classes-1 has loss 0 and counts for no gradient (its dx is 0), whatever its x and its row_grad hold; so does, for the gradients, one of weight 0.  A class with
@@ -603,7 +603,7 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
  *   dx           [rows, width] of `type`, stride lddx;  dw [classes, width], stride lddw, of dw_type: BSR_FP32, or BSR_BF16 where w is;  db fp32 [classes];  each may be NULL
  *   workspace    device scratch of bsr_linear_ce_workspace_bytes() bytes, 256-byte aligned; what: 0 for the forward, 1 for the backward, 2 for both in one call
  * No result may touch an input, another result or the workspace.
- * bsr_linear_ce_forward_backward: one after the other, the second with what the first leaves.
+ * bsr_linear_ce_forward_backward: one after the other, the second with what the first leaves in the workspace: packed operands, and logits where 16 MB hold them all.
  * Limits: rows up to 2^22, width up to 2^20, their product up to 2^33; classes up to 2^30.
  */
 size_t bsr_linear_ce_workspace_bytes(int32_t type, int64_t rows, int32_t width, int32_t classes, int32_t what);

@@ -1,7 +1,7 @@
 // Softmax cross-entropy of a linear layer over many classes, and its gradients, without keeping the logits:
 //   z = x w^T + b;   loss = log sum exp z - z_label;   G = softmax(z) - onehot(label);   dx = g G w;   dw = G^T (g x);   db = G^T g
 // Forward: tiles of z stay in the accumulators of the product; a tile leaves each row's maximum and its sum of exp(z - maximum), and a second kernel joins the tiles of a row.
-// Backward: z is made again, a piece of the classes at a time; the tile's end turns it into G and leaves that as it lies and transposed, so that both products behind it
+// Backward: z is made again (or, in one call for both, read where 16 MB hold it), a piece of the classes at a time; the tile's end turns it into G and leaves that as it lies and transposed, so that both products behind it
 // contract over contiguous memory like the first.  What they need transposed beside it (x once, the piece's rows of w) is transposed in a pass of its own.
 //
 // Numbers.  bf16 x and w are multiplied as they are and added in fp32.  G is kept in fp16, not bf16: it lies within -1 .. 1, and scaled by 2^14 its values keep 11 bits down to
@@ -43,6 +43,7 @@ struct CeGemm {
   const int32_t* labels = nullptr;
   int v0 = 0, classes = 0;                         // classes of the whole layer
   float2* parts = nullptr; float* zlabel = nullptr;                        // STATS: [tile of classes][M] maximum and sum; [M]
+  float* z = nullptr; int64_t ldz = 0;             // STATS: the logits as well, [M][ldz], ldz whole fours; null: not wanted
   const float2* stats = nullptr; const float* row_grad = nullptr;          // GRAD: [M] maximum, log of the sum; weights or null
   f16 *G = nullptr, *GT = nullptr;                 // GRAD: [terms][M][ldg], [terms][N][ldgt], of which kg and kgt columns are written, zero behind the last one; null: not wanted
   int64_t ldg = 0, ldgt = 0, tg = 0, tgt = 0; int kg = 0, kgt = 0;
@@ -274,6 +275,10 @@ __device__ __forceinline__ void end_stats(const CeGemm& g, f32x4 (&acc)[S::MI][S
     for (int ni = 0; ni < S::NI; ++ni)
 #pragma unroll
       for (int r = 0; r < 4; ++r) acc[mi][ni][r] = cl.logit(acc[mi][ni][r], ea, ni, r);
+    if (g.z && m < g.M)
+#pragma unroll
+      for (int ni = 0; ni < S::NI; ++ni)
+        if (w.col0 + w.col(ni, 0) < g.N) *(f32x4*)(g.z + (int64_t)m * g.ldz + w.col0 + w.col(ni, 0)) = acc[mi][ni];
     if (cl.edge)                                   // (whatever the product of a repeated row is, it does not count)
 #pragma unroll
       for (int ni = 0; ni < S::NI; ++ni)
@@ -694,8 +699,8 @@ __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, Trans
   }
 }
 
-// G in fp32 (from k_linear_ce_small.hip, without weights) to what the tiles leave of it: 64 tokens x 64 classes a workgroup
-template <int TERMS>
+// G in fp32 (from k_linear_ce_small.hip, without weights), or logits, to what the tiles leave of G: 64 tokens x 64 classes a workgroup
+template <int TERMS, bool LOGITS>
 __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ from, int64_t ldz, CeGemm g) {
   __shared__ float tile[64][65];
   const int t = threadIdx.x, m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, a = t / 4, b = t % 4 * 16;      // a row (or a column) and 16 of its values
@@ -705,12 +710,23 @@ __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ 
     l = (f16)(p - (float)h);
   };
   float v[16];
+  bool counts = m0 + a < g.M;                      // (as at a tile's end)
+  float2 st = {0.f, 0.f};
+  int label = -1;
+  if (LOGITS && counts) {
+    label = g.labels[m0 + a];
+    st = g.stats[m0 + a];
+    counts = label >= 0 && label < g.classes && (!g.row_grad || g.row_grad[m0 + a] != 0.f) && !(st.x == -INFINITY && st.y == 0.f);
+  }
 #pragma unroll
   for (int i = 0; i < 16; i += 4) {
-    const bool there = m0 + a < g.M && n0 + b + i < g.N;
-    const f32x4 p = there ? *(const f32x4*)(from + (int64_t)(m0 + a) * ldz + n0 + b + i) : f32x4{0.f, 0.f, 0.f, 0.f};
+    const bool there = counts && n0 + b + i < g.N;
+    f32x4 p = there ? *(const f32x4*)(from + (int64_t)(m0 + a) * ldz + n0 + b + i) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) tile[a][b + i + j] = v[i + j] = n0 + b + i + j < g.N ? p[j] : 0.f;
+    for (int j = 0; j < 4; ++j) {
+      if (LOGITS) p[j] = __builtin_amdgcn_exp2f(fmaf(p[j] - st.x, LOG2E, -st.y * LOG2E)) - (n0 + b + i + j == label ? 1.f : 0.f);
+      tile[a][b + i + j] = v[i + j] = there && n0 + b + i + j < g.N ? p[j] : 0.f;
+    }
   }
   auto put = [&](f16* to, int64_t term) __attribute__((always_inline)) {
 #pragma unroll
@@ -1022,7 +1038,8 @@ struct Way {
   }
 };
 
-void linear_ce_forward(const LinearCe& a, hipStream_t s) {
+// z: where the logits are kept as well (in one piece, and not of little work), or null
+static void forward_with(const LinearCe& a, float* z, hipStream_t s) {
   const Way way(a);
   const bool direct_x = way.x, direct_w = way.w;
   if (way.little || (!direct_w && is_few(a.N, a.V))) {
@@ -1041,7 +1058,7 @@ void linear_ce_forward(const LinearCe& a, hipStream_t s) {
     const Rows w = rows_operand((const char*)a.w + v0 * a.ldw * size, a.ldw, a.f32, n, p.Dp, ws + p.wp, (int*)(ws + p.ew), direct_w, pw);
     pack(v0 == 0 ? px : PackJob(), pw, a.f32, a.D, p.Dp, s);
     CeGemm g = logits_gemm(a, p, x, w, v0, n);
-    g.parts = (float2*)(ws + p.parts); g.zlabel = (float*)(ws + p.zlabel);
+    g.parts = (float2*)(ws + p.parts); g.zlabel = (float*)(ws + p.zlabel); g.z = z; g.ldz = up(a.V, 4);
     const int shape = logits_shape(a.N, n, g.nk * (a.f32 ? 3 : 1));
     if (a.f32) logits<STATS, true, 3, false>(shape, g, a.N, s);
     else logits<STATS, false, 1, false>(shape, g, a.N, s);
@@ -1049,13 +1066,19 @@ void linear_ce_forward(const LinearCe& a, hipStream_t s) {
   }
 }
 
+void linear_ce_forward(const LinearCe& a, hipStream_t s) { forward_with(a, nullptr, s); }
+
+// Loss and gradients in one call: the logits stay in scratch between the passes where they fit it and cost more to make again than to read.  (333 x 1001 x 5003 fp32 110 against 128 us, 1024 x 4096 x
+// 4000 bf16 153 against 177, 1000 x 768 x 1000 40 against 43; 400 x 64 x 10000 51 against 48)
+bool keeps(bool f32, int N, int D, int V) { return small_ce_bytes(N, V) <= SMALL_BYTES && over(D, BK) * (f32 ? 3 : 1) >= 8; }
+
 // little work: G in fp32 first, then turned into what the tiles leave (in one piece)
 bool takes_turn(const LinearCe& a, const Plan& p, const Way& way) { return way.little && p.Vc >= a.V; }
 
-// What a forward on the same workspace has left: nothing, the packed operands (of one piece), or G of little work
-enum Ready { NOTHING, PACKED, TURNED };
+// What a forward on the same workspace has left: nothing, the packed operands (of one piece), G of little work, or the logits (z)
+enum Ready { NOTHING, PACKED, TURNED, KEPT };
 template <typename T>
-void backward_as(const LinearCe& a, Ready ready, hipStream_t s) {
+void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int SEG = F32 ? 3 : 1;
   const Plan p(F32, a.N, a.D, a.V, true);
@@ -1064,7 +1087,7 @@ void backward_as(const LinearCe& a, Ready ready, hipStream_t s) {
   const bool direct_x = way.x, direct_w = way.w;
   PackJob px;
   const Rows x = rows_operand(a.x, a.ldx, F32, a.N, p.Dp, ws + p.xp, (int*)(ws + p.ex), direct_x, px);
-  const bool turned = takes_turn(a, p, way);
+  const bool turned = ready == KEPT || takes_turn(a, p, way);
   f16 *xT = (f16*)(ws + p.xT), *wT = (f16*)(ws + p.wT), *G = (f16*)(ws + p.G), *GT = (f16*)(ws + p.GT);
   for (int v0 = 0; v0 < a.V; v0 += p.Vc) {
     const int n = std::min(p.Vc, a.V - v0), np = up(n, BK);
@@ -1090,10 +1113,11 @@ void backward_as(const LinearCe& a, Ready ready, hipStream_t s) {
     if (a.dw) { g.GT = GT; g.kgt = p.Np; g.ldgt = p.Np; g.tgt = n * g.ldgt; }
     if (a.db) { g.dbp = (float*)(ws + p.dbp); g.ldd = p.ldd; }
     const int shape = logits_shape(a.N, n, g.nk * SEG), rows = a.dw ? p.Np : a.N, tall = turned ? 64 : rows_of(shape);
-    if (turned) {
-      float* z = (float*)(ws + p.z);
-      if (ready != TURNED) small_ce_gradient(a, false, z, s);
-      ce_turn_kernel<F32 ? 2 : 1><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(z, up(a.V, 4), g);
+    if (ready == KEPT) {
+      ce_turn_kernel<F32 ? 2 : 1, true><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(z, up(a.V, 4), g);
+    } else if (turned) {
+      if (ready != TURNED) small_ce_gradient(a, false, (float*)(ws + p.z), s);
+      ce_turn_kernel<F32 ? 2 : 1, false><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>((const float*)(ws + p.z), up(a.V, 4), g);
     } else if (a.db) {
       logits<GRAD, F32, SEG, true>(shape, g, rows, s);
     } else {
@@ -1132,9 +1156,9 @@ void backward_as(const LinearCe& a, Ready ready, hipStream_t s) {
     if (sx.blocks + sw.blocks + sb.blocks > 0) ce_sums_kernel<<<sx.blocks + sw.blocks + sb.blocks, 256, 0, s>>>(sx, sw, sb);
   }
 }
-static void backward_with(const LinearCe& a, Ready ready, hipStream_t s) {
-  if (a.f32) backward_as<float>(a, ready, s);
-  else backward_as<bf16>(a, ready, s);
+static void backward_with(const LinearCe& a, Ready ready, const float* z, hipStream_t s) {
+  if (a.f32) backward_as<float>(a, ready, z, s);
+  else backward_as<bf16>(a, ready, z, s);
 }
 static void no_tokens(const LinearCe& a, hipStream_t s) {
   const unsigned grid = (unsigned)std::min(a.V, 4096);
@@ -1145,10 +1169,13 @@ static void no_tokens(const LinearCe& a, hipStream_t s) {
 void linear_ce_backward(const LinearCe& a, hipStream_t s) {
   if (a.N == 0) no_tokens(a, s);
   else if (is_few(a.N, a.V)) few_ce_backward(a, false, s);
-  else backward_with(a, NOTHING, s);
+  else backward_with(a, NOTHING, nullptr, s);
 }
 
-size_t linear_ce_both_bytes(bool f32, int N, int D, int V) { return std::max(linear_ce_workspace_bytes(f32, N, D, V, false), linear_ce_workspace_bytes(f32, N, D, V, true)); }
+static size_t both_kept_at(bool f32, int N, int D, int V) {
+  return (std::max(linear_ce_workspace_bytes(f32, N, D, V, false), linear_ce_workspace_bytes(f32, N, D, V, true)) + 255) / 256 * 256;
+}
+size_t linear_ce_both_bytes(bool f32, int N, int D, int V) { return both_kept_at(f32, N, D, V) + (keeps(f32, N, D, V) && !is_few(N, V) ? small_ce_bytes(N, V) : 0); }
 void linear_ce_both(const LinearCe& a, hipStream_t s) {
   const Way way(a);
   if (a.N == 0) {
@@ -1161,14 +1188,19 @@ void linear_ce_both(const LinearCe& a, hipStream_t s) {
     few_ce_backward(a, false, s);
   } else {
     const Plan f(a.f32, a.N, a.D, a.V, false), p(a.f32, a.N, a.D, a.V, true);
+    const bool one = p.Vc >= a.V && (way.w ? f.Vs : f.Vp) >= a.V;        // one piece in both
     if (takes_turn(a, p, way)) {
       small_ce_forward(a, (float*)((char*)a.workspace + p.z), GRAD_PLAIN, s);
-      backward_with(a, TURNED, s);
+      backward_with(a, TURNED, nullptr, s);
+    } else if (one && keeps(a.f32, a.N, a.D, a.V) && !way.little) {
+      float* z = (float*)((char*)a.workspace + both_kept_at(a.f32, a.N, a.D, a.V));
+      forward_with(a, z, s);
+      backward_with(a, KEPT, z, s);
     } else {
       linear_ce_forward(a, s);
-      // (one piece in both: the packed operands lie at the same places)
-      const bool packed = !way.little && (!way.x || !way.w) && p.Vc >= a.V && (way.w ? f.Vs : f.Vp) >= a.V && f.xp == p.xp && f.ex == p.ex && f.wp == p.wp && f.ew == p.ew;
-      backward_with(a, packed ? PACKED : NOTHING, s);
+      // (the packed operands lie at the same places)
+      const bool packed = !way.little && (!way.x || !way.w) && one && f.xp == p.xp && f.ex == p.ex && f.wp == p.wp && f.ew == p.ew;
+      backward_with(a, packed ? PACKED : NOTHING, nullptr, s);
     }
   }
 }
