@@ -68,11 +68,6 @@ typedef Shape<128, 128, 2, 4, 3> Small;
 typedef Shape<64, 128, 2, 2, 3> Mid;                  // (logits only: where larger tiles would leave CUs idle)
 typedef Shape<32, 256, 1, 4, 4> Few;
 
-__device__ __forceinline__ void wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // tiles band after band of eight row tiles, row tile fastest: what an XCD works on at a time shares rows of A and of B
 constexpr int BAND = 8;
 __device__ __forceinline__ void tile_at(int t, int mt, int nt, int& m, int& n) {
@@ -762,17 +757,19 @@ __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ 
 }
 
 // ------------------------------------------------------------------------------------------ joining
-// 64 rows a workgroup: wavefront w joins tiles w, w + 16, ..., then the wavefronts in order; first and last piece of the classes: begin, end
+// 16 rows a workgroup, whose 64 quarters of wavefronts join every 64th tile each and then, in order, what they have; first and last piece of the classes: begin, end
 __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* __restrict__ parts, int tiles, int M, float2* __restrict__ run, int begin, int end, const float* __restrict__ zlabel,
                                                        const int32_t* __restrict__ labels, int classes, float* __restrict__ loss, float2* __restrict__ stats) {
-  __shared__ float2 red[16][WAVE];
-  const int lane = threadIdx.x % WAVE, w = threadIdx.x / WAVE, m = blockIdx.x * WAVE + lane, mc = min(m, M - 1);
+  __shared__ float2 red[16][16];
+  const int lane = threadIdx.x % WAVE, w = threadIdx.x / WAVE, m = blockIdx.x * 16 + lane % 16, mc = min(m, M - 1);
   float2 p = make_float2(-INFINITY, 0.f);
 #pragma unroll 8
-  for (int t = w; t < tiles; t += 16) p = joined(p, parts[(int64_t)t * M + mc]);
-  red[w][lane] = p;
+  for (int t = threadIdx.x / 16; t < tiles; t += 64) p = joined(p, parts[(int64_t)t * M + mc]);
+#pragma unroll
+  for (int d = 16; d < WAVE; d *= 2) p = joined(p, make_float2(__shfl_xor(p.x, d), __shfl_xor(p.y, d)));
+  if (lane < 16) red[w][lane] = p;
   __syncthreads();
-  if (w != 0 || m >= M) return;
+  if (threadIdx.x >= 16 || m >= M) return;
   if (!begin) p = joined(run[m], p);
 #pragma unroll
   for (int i = 1; i < 16; ++i) p = joined(p, red[i][lane]);
@@ -926,18 +923,20 @@ Split grads_split(int64_t M, int64_t n, int64_t D, int kx, int kw) {
 }
 
 // What goes to k_linear_ce_small.hip: little work, where the launches count; few rows backward (w is read and dw written once there), and forward where they would have to be packed first.  Its
-// logits take 16 MB at most
-constexpr size_t SMALL_BYTES = 16 << 20;
+// logits take 16 MB at most, those of few rows, of which there is room for 16, 32 or 64, 256
+constexpr size_t SMALL_BYTES = 16 << 20, FEW_BYTES = 256 << 20;
 constexpr double SMALL_WORK = 1 << 28;             // tokens x features x classes
 bool is_small(int N, int D, int V) { return N <= 1 << 20 && small_ce_bytes(N, V) <= SMALL_BYTES && (double)N * D * V <= SMALL_WORK; }      // (a launch has up to 65535 workgroups one way)
-bool is_few(int N, int V) { return N <= 32 && small_ce_bytes(N, V) <= SMALL_BYTES; }
+// (more than 32 rows of a w that would have to be packed: 48 x 1001 x 50000 bf16 318 us here, 291 by tiles)
+bool is_few(bool f32, int N, int V) { return N <= (f32 ? FEW_ROWS_F32 : FEW_ROWS_BF16) && few_parts_at(N, V) <= FEW_BYTES; }
+bool always_few(int N) { return N <= 32; }
 
 // sizes, and places in the workspace
 struct Plan {
   int T, Dp, Np, Vs, Vp, Vc, Dq, ldd;
   Split split = {};
   size_t xp, ex, wp, ew, parts, run, zlabel, G, GT, xT, wT, exT, ewT, mostx, mostw, dxp, dwp, dbp, z, bytes;
-  Plan(bool f32, int N, int D, int V, bool backward) {
+  Plan(bool f32, int N, int D, int V, bool backward, bool packs = true) {      // packs: room for w packed
     T = f32 ? 2 : 1;
     Dp = up(D, BK); Np = up(N, BK); Dq = up(D, 4);
     // Pieces of the classes, whole tiles and alike in size.  Forward: the tiles' maxima and sums take at most 64 MB (Vs) and what is packed 256 (Vp, where something is).
@@ -954,7 +953,7 @@ struct Plan {
     ldd = Vc;
     bytes = 0;
     auto take = [&](size_t n) { const size_t at = bytes; bytes += (n + 255) / 256 * 256; return at; };
-    const int Vm = backward ? Vc : Vp;
+    const int Vm = packs ? backward ? Vc : Vp : 0;
     xp = take((size_t)2 * T * N * Dp); ex = take(sizeof(int) * (size_t)N);
     wp = take((size_t)2 * T * Vm * Dp); ew = take(sizeof(int) * (size_t)Vm);
     if (!backward) {
@@ -1023,30 +1022,33 @@ CeGemm logits_gemm(const LinearCe& a, const Plan& p, const Rows& x, const Rows& 
 }  // namespace
 
 size_t linear_ce_workspace_bytes(bool f32, int N, int D, int V, bool backward) {
-  if (backward && is_few(N, V)) return few_ce_bytes(f32, N, V, D);
-  const size_t bytes = Plan(f32, N, D, V, backward).bytes;
-  return !backward && (is_small(N, D, V) || is_few(N, V)) ? std::max(bytes, small_ce_bytes(N, V)) : bytes;
+  // (few rows: the logits may come from tiles, whose scratch lies where the parts of dx do afterwards)
+  const size_t few = is_few(f32, N, V) ? few_parts_at(N, V) + std::max(few_ce_bytes(f32, N, V, D), f32 ? 0 : Plan(f32, N, D, V, false, false).bytes) : 0;
+  if (backward && few && always_few(N)) return few;
+  const size_t bytes = std::max(Plan(f32, N, D, V, backward).bytes, backward ? few : 0);
+  return !backward && (is_small(N, D, V) || (few && always_few(N))) ? std::max(bytes, small_ce_bytes(N, V)) : bytes;
 }
 
 // How x and w lie, and what follows from it: the logits (or G) of little work straight from x and w, in a launch of its own, not in tiles
 struct Way {
-  bool x, w, little;                               // rows of whole 16-byte pieces; little work
+  bool x, w, little, few;                          // rows of whole 16-byte pieces; little work; gradients of few rows
   explicit Way(const LinearCe& a) {
     x = !a.f32 && whole_rows(a.x, a.ldx, a.D);
     w = !a.f32 && whole_rows(a.w, a.ldw, a.D);
     little = is_small(a.N, a.D, a.V) && (!x || !w || few_tiles(a.N, a.V, over(a.D, BK) * (a.f32 ? 3 : 1)));
+    few = is_few(a.f32, a.N, a.V) && (always_few(a.N) || w || little);
   }
 };
 
-// z: where the logits are kept as well (in one piece, and not of little work), or null
-static void forward_with(const LinearCe& a, float* z, hipStream_t s) {
+// z: where the logits are kept as well (in one piece, and not of little work), or null;  packs: whether the workspace has room for w packed
+static void forward_with(const LinearCe& a, float* z, bool packs, hipStream_t s) {
   const Way way(a);
   const bool direct_x = way.x, direct_w = way.w;
-  if (way.little || (!direct_w && is_few(a.N, a.V))) {
+  if (way.little || (way.few && !way.w)) {
     small_ce_forward(a, (float*)a.workspace, GRAD_NONE, s);
     return;
   }
-  const Plan p(a.f32, a.N, a.D, a.V, false);
+  const Plan p(a.f32, a.N, a.D, a.V, false, packs);
   char* ws = (char*)a.workspace;
   const int64_t size = a.f32 ? 4 : 2;
   PackJob px;
@@ -1058,15 +1060,16 @@ static void forward_with(const LinearCe& a, float* z, hipStream_t s) {
     const Rows w = rows_operand((const char*)a.w + v0 * a.ldw * size, a.ldw, a.f32, n, p.Dp, ws + p.wp, (int*)(ws + p.ew), direct_w, pw);
     pack(v0 == 0 ? px : PackJob(), pw, a.f32, a.D, p.Dp, s);
     CeGemm g = logits_gemm(a, p, x, w, v0, n);
-    g.parts = (float2*)(ws + p.parts); g.zlabel = (float*)(ws + p.zlabel); g.z = z; g.ldz = up(a.V, 4);
+    g.parts = (float2*)(ws + p.parts); g.zlabel = (float*)(ws + p.zlabel); g.z = z; g.ldz = small_ce_stride(a.N, a.V);
     const int shape = logits_shape(a.N, n, g.nk * (a.f32 ? 3 : 1));
     if (a.f32) logits<STATS, true, 3, false>(shape, g, a.N, s);
     else logits<STATS, false, 1, false>(shape, g, a.N, s);
-    ce_join_kernel<<<over(a.N, WAVE), 1024, 0, s>>>(g.parts, over(n, cols_of(shape)), a.N, (float2*)(ws + p.run), v0 == 0, v0 + n == a.V, g.zlabel, a.labels, a.V, a.loss, (float2*)a.stats);
+    if (a.loss || a.stats)
+      ce_join_kernel<<<over(a.N, 16), 1024, 0, s>>>(g.parts, over(n, cols_of(shape)), a.N, (float2*)(ws + p.run), v0 == 0, v0 + n == a.V, g.zlabel, a.labels, a.V, a.loss, (float2*)a.stats);
   }
 }
 
-void linear_ce_forward(const LinearCe& a, hipStream_t s) { forward_with(a, nullptr, s); }
+void linear_ce_forward(const LinearCe& a, hipStream_t s) { forward_with(a, nullptr, true, s); }
 
 // Loss and gradients in one call: the logits stay in scratch between the passes where they fit it and cost more to make again than to read.  (333 x 1001 x 5003 fp32 110 against 128 us, 1024 x 4096 x
 // 4000 bf16 153 against 177, 1000 x 768 x 1000 40 against 43; 400 x 64 x 10000 51 against 48)
@@ -1114,10 +1117,10 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
     if (a.db) { g.dbp = (float*)(ws + p.dbp); g.ldd = p.ldd; }
     const int shape = logits_shape(a.N, n, g.nk * SEG), rows = a.dw ? p.Np : a.N, tall = turned ? 64 : rows_of(shape);
     if (ready == KEPT) {
-      ce_turn_kernel<F32 ? 2 : 1, true><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(z, up(a.V, 4), g);
+      ce_turn_kernel<F32 ? 2 : 1, true><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(z, small_ce_stride(a.N, a.V), g);
     } else if (turned) {
       if (ready != TURNED) small_ce_gradient(a, false, (float*)(ws + p.z), s);
-      ce_turn_kernel<F32 ? 2 : 1, false><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>((const float*)(ws + p.z), up(a.V, 4), g);
+      ce_turn_kernel<F32 ? 2 : 1, false><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>((const float*)(ws + p.z), small_ce_stride(a.N, a.V), g);
     } else if (a.db) {
       logits<GRAD, F32, SEG, true>(shape, g, rows, s);
     } else {
@@ -1166,26 +1169,36 @@ static void no_tokens(const LinearCe& a, hipStream_t s) {
   else if (a.dw) ce_fill_kernel<bf16><<<grid, 256, 0, s>>>((bf16*)a.dw, a.lddw, a.V, a.D);
   if (a.db) ce_fill_kernel<float><<<1, 256, 0, s>>>(a.db, 0, 1, a.V);
 }
+// few rows; both: the forward as well
+static void few_backward(const LinearCe& a, bool both, hipStream_t s) {
+  const Way way(a);
+  if (way.little || !way.w) {
+    if (both) small_ce_forward(a, (float*)a.workspace, GRAD_WEIGHTED, s);
+    few_ce_backward(a, both ? FEW_GRADIENT : FEW_NOTHING, s);
+  } else {
+    LinearCe f = a;
+    f.workspace = (char*)a.workspace + few_parts_at(a.N, a.V);
+    if (!both) f.loss = f.stats = nullptr;
+    forward_with(f, (float*)a.workspace, false, s);
+    few_ce_backward(a, FEW_LOGITS, s);
+  }
+}
 void linear_ce_backward(const LinearCe& a, hipStream_t s) {
   if (a.N == 0) no_tokens(a, s);
-  else if (is_few(a.N, a.V)) few_ce_backward(a, false, s);
+  else if (Way(a).few) few_backward(a, false, s);
   else backward_with(a, NOTHING, nullptr, s);
 }
 
 static size_t both_kept_at(bool f32, int N, int D, int V) {
   return (std::max(linear_ce_workspace_bytes(f32, N, D, V, false), linear_ce_workspace_bytes(f32, N, D, V, true)) + 255) / 256 * 256;
 }
-size_t linear_ce_both_bytes(bool f32, int N, int D, int V) { return both_kept_at(f32, N, D, V) + (keeps(f32, N, D, V) && !is_few(N, V) ? small_ce_bytes(N, V) : 0); }
+size_t linear_ce_both_bytes(bool f32, int N, int D, int V) { return both_kept_at(f32, N, D, V) + (keeps(f32, N, D, V) && !(is_few(f32, N, V) && always_few(N)) ? small_ce_bytes(N, V) : 0); }
 void linear_ce_both(const LinearCe& a, hipStream_t s) {
   const Way way(a);
   if (a.N == 0) {
     no_tokens(a, s);
-  } else if (is_few(a.N, a.V) && (way.little || !way.w)) {
-    small_ce_forward(a, (float*)a.workspace, GRAD_WEIGHTED, s);
-    few_ce_backward(a, true, s);
-  } else if (is_few(a.N, a.V)) {
-    linear_ce_forward(a, s);
-    few_ce_backward(a, false, s);
+  } else if (way.few) {
+    few_backward(a, true, s);
   } else {
     const Plan f(a.f32, a.N, a.D, a.V, false), p(a.f32, a.N, a.D, a.V, true);
     const bool one = p.Vc >= a.V && (way.w ? f.Vs : f.Vp) >= a.V;        // one piece in both
@@ -1194,7 +1207,7 @@ void linear_ce_both(const LinearCe& a, hipStream_t s) {
       backward_with(a, TURNED, nullptr, s);
     } else if (one && keeps(a.f32, a.N, a.D, a.V) && !way.little) {
       float* z = (float*)((char*)a.workspace + both_kept_at(a.f32, a.N, a.D, a.V));
-      forward_with(a, z, s);
+      forward_with(a, z, true, s);
       backward_with(a, KEPT, z, s);
     } else {
       linear_ce_forward(a, s);

@@ -3,7 +3,7 @@
 //   logits   16 classes x 16 or 32 tokens a workgroup, the features split over its eight wavefronts, whole cache lines each (bf16 16 x 16 x 32, fp32 16 x 16 x 4 matrix instructions, both exact products
 //            added in fp32); for the gradients they leave as G
 //   rows     a workgroup a token: maximum, sum, loss
-//   grads    up to 32 tokens: dx and dw in one pass over w, multiplied in fp32 (16 x 16 x 4)
+//   grads    up to 32 tokens in fp32, 64 in bf16: dx and dw in one pass over w, multiplied in fp32 (16 x 16 x 4), or with G in two bf16 terms (16 x 16 x 16)
 // A launch is a chain of a few trips to memory; that, the calls and, for few rows of many classes, the bytes of w and dw are what bounds it.
 #include <algorithm>
 
@@ -42,6 +42,7 @@ struct Tokens {
   const int32_t* labels = nullptr; const float2* stats = nullptr; const float* row_grad = nullptr; float scale = 1.f;      // stats null: the logits stay what they are
   bool weighted = true;                            // G with its row's weight
   int N = 0, V = 0;
+  int rows = 0;                                    // of G; those from N on, and classes from V on, are zero
   __device__ __forceinline__ bool counts(int n) const {
     const int m = min(n, N - 1), label = labels[m];
     const float2 st = stats[m];
@@ -91,28 +92,33 @@ __global__ __launch_bounds__(LOGIT_WAVES * WAVE) void small_logits_kernel(const 
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
     const int n = n0 + t * 16 + lane % 16;
-    if (n >= N || v >= V) continue;
+    if (n >= tk.rows || v >= ldz) continue;
     f32x4 o = acc[t];
 #pragma unroll
     for (int i = 0; i < LOGIT_WAVES - 1; ++i) o += red[i][t][lane];
     o += b;
     if (tk.stats) {
       const bool counts = tk.counts(n);
-      const float2 st = tk.stats[n];
-      const float by = tk.scale * (tk.weighted && tk.row_grad ? tk.row_grad[n] : 1.f);
+      const int m = min(n, N - 1);
+      const float2 st = tk.stats[m];
+      const float by = tk.scale * (tk.weighted && tk.row_grad ? tk.row_grad[m] : 1.f);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        o[j] = counts ? by * (__builtin_amdgcn_exp2f(fmaf(o[j] - st.x, LOG2E, -st.y * LOG2E)) - (v + j == tk.labels[n] ? 1.f : 0.f)) : 0.f;
+        o[j] = counts && v + j < V ? by * (__builtin_amdgcn_exp2f(fmaf(o[j] - st.x, LOG2E, -st.y * LOG2E)) - (v + j == tk.labels[m] ? 1.f : 0.f)) : 0.f;
     }
-    *(f32x4*)(z + n * ldz + v) = o;                          // (ldz: whole fours)
+    *(f32x4*)(z + n * ldz + v) = o;                          // (ldz: whole fours at least)
   }
 }
 
-// a workgroup a token.  grad: the logits become G
+// a workgroup a token.  grad: the logits become G (of tk.rows rows)
 __global__ __launch_bounds__(256) void small_rows_kernel(float* __restrict__ z, int64_t ldz, Tokens tk, float* __restrict__ loss, float2* __restrict__ stats, bool grad) {
   __shared__ float red[2][4];
   const int m = blockIdx.x, wave = threadIdx.x / WAVE, V = tk.V;
   float* row = z + m * ldz;
+  if (m >= tk.N) {
+    for (int v = threadIdx.x; v < ldz; v += 256) row[v] = 0.f;
+    return;
+  }
   float most = -INFINITY;
 #pragma unroll 4
   for (int v = threadIdx.x; v < V; v += 256) most = fmaxf(most, row[v]);
@@ -142,6 +148,21 @@ __global__ __launch_bounds__(256) void small_rows_kernel(float* __restrict__ z, 
   const float weight = tk.row_grad ? tk.row_grad[m] : 1.f, by = tk.weighted ? tk.scale * weight : 1.f;
 #pragma unroll 4
   for (int v = threadIdx.x; v < V; v += 256) row[v] = there && weight != 0.f ? by * (__builtin_amdgcn_exp2f(fmaf(row[v] - most, LOG2E, -ls * LOG2E)) - (v == label ? 1.f : 0.f)) : 0.f;
+  if (V + (int)threadIdx.x < ldz) row[V + threadIdx.x] = 0.f;
+}
+
+// logits to G in their place, with the row's weight: four classes a thread
+__global__ __launch_bounds__(256) void small_turn_kernel(float* __restrict__ z, int64_t ldz, Tokens tk) {
+  const int n = blockIdx.y, v = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (v >= ldz) return;
+  const bool counts = tk.counts(n);
+  const int m = min(n, tk.N - 1);
+  const float2 st = tk.stats[m];
+  const float by = tk.scale * (tk.weighted && tk.row_grad ? tk.row_grad[m] : 1.f);
+  f32x4 p = *(const f32x4*)(z + n * ldz + v);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) p[j] = counts && v + j < tk.V ? by * (__builtin_amdgcn_exp2f(fmaf(p[j] - st.x, LOG2E, -st.y * LOG2E)) - (v + j == tk.labels[m] ? 1.f : 0.f)) : 0.f;
+  *(f32x4*)(z + n * ldz + v) = p;
 }
 
 // K values of a row from d on, zero past its end
@@ -161,21 +182,54 @@ template <int K, typename T> __device__ __forceinline__ void put(T* row, int d, 
       if (d + e < D) row[d + e] = v[e];
 }
 
-// features of a lane: 16 bytes; with two tiles of tokens 8, or they would not leave registers for a second wavefront a SIMD
-template <typename T> constexpr int few_features(int tiles) { return tiles == 2 ? 4 : Chunk<T>::V; }
+// features of a lane; wavefronts that a SIMD has registers for
+constexpr int few_features(bool f32, int tiles) { return f32 || tiles > 2 ? 4 : 8; }
+constexpr int few_wavefronts(int tiles) { return 2; }
+
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+// Four values of G, and what they are multiplied by, of the four k of a lane.  fp32: as they are, four products of 16 x 16 x 4.  Beside bf16: G in two bf16 terms, off by 2^-17 of itself, which take
+// the eight k of one product of 16 x 16 x 32 and meet the other operand twice
+template <typename T> struct Four;
+template <> struct Four<float> {
+  typedef f32x4 Other;
+  f32x4 v;
+  Four() = default;
+  __device__ __forceinline__ explicit Four(f32x4 g) : v(g) {}
+};
+template <> struct Four<bf16> {
+  typedef bf16x4 Other;
+  bf16x8 v;
+  Four() = default;
+  __device__ __forceinline__ bf16x4 high() const { return bf16x4{v[0], v[1], v[2], v[3]}; }
+  __device__ __forceinline__ bf16x4 low() const { return bf16x4{v[4], v[5], v[6], v[7]}; }
+  __device__ __forceinline__ Four(bf16x4 h, bf16x4 l) : v{h[0], h[1], h[2], h[3], l[0], l[1], l[2], l[3]} {}
+  __device__ __forceinline__ explicit Four(f32x4 g) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float h = __uint_as_float(__float_as_uint(g[j]) & 0xffff0000u);
+      v[j] = (bf16)h;
+      v[4 + j] = (bf16)(g[j] - h);
+    }
+  }
+};
+__device__ __forceinline__ f32x4 times(const Four<float>& g, f32x4 b, f32x4 c) { return multiplied(g.v, b, c); }
+__device__ __forceinline__ f32x4 times(const Four<bf16>& g, bf16x4 b, f32x4 c) { return multiplied(g.v, bf16x8{b[0], b[1], b[2], b[3], b[0], b[1], b[2], b[3]}, c); }
 
 // dx = G w, dw = G^T x and db of up to 16 TILES tokens and any number of classes, w read and dw written once.  A workgroup takes 16 K features and a range of the classes, a wavefront every
 // fourth 16 of these, in products of 16 x 16 whose column l % 16 of product i is feature K (l % 16) + i: a lane reads and writes K features together.  x's part stays in
-// registers; dx's is added up over the range and leaves as a part.
+// registers; dx's is added up over the range and leaves as a part.  G: [16 TILES, ldz], ldz whole sixteens, zero behind the last token and class.
 template <typename T, typename TW, int TILES>
-__global__ __launch_bounds__(256) void few_grads_kernel(const float* __restrict__ G, int64_t ldz, Tokens tk, int D, const T* __restrict__ x, int64_t ldx, const T* __restrict__ w, int64_t ldw,
-                                                        float* __restrict__ parts, int64_t ldp, int per, TW* __restrict__ dw, int64_t lddw, float* __restrict__ db) {
-  constexpr int K = few_features<T>(TILES);
+__global__ __launch_bounds__(256, few_wavefronts(TILES)) void few_grads_kernel(const float* __restrict__ G, int64_t ldz, Tokens tk, int D, const T* __restrict__ x, int64_t ldx,
+                                                                               const T* __restrict__ w, int64_t ldw, float* __restrict__ parts, int64_t ldp, int per, TW* __restrict__ dw,
+                                                                               int64_t lddw, float* __restrict__ db) {
+  constexpr int K = few_features(sizeof(T) == 4, TILES), STEP = 64;
   typedef typename Some<K, T>::vec vec;
+  typedef typename Four<T>::Other other;
   __shared__ f32x4 red[3][K][WAVE];
   const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, lm = lane % 16, lq = lane / 16, d = (blockIdx.x * 16 + lm) * K, N = tk.N, V = tk.V;
   const int begin = blockIdx.y * per, end = min(begin + per, V);
-  float xb[TILES][4][K];
+  const bool whole = (int)(blockIdx.x + 1) * 16 * K <= D;        // no feature of the workgroup lies behind the last
+  other xb[TILES][K];                              // of four tokens
   f32x4 acc[TILES][K];
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
@@ -185,83 +239,103 @@ __global__ __launch_bounds__(256) void few_grads_kernel(const float* __restrict_
       const bool counts = tk.counts(n);                            // (a row that does not count may hold anything)
       const vec v = some<K>(x + (int64_t)min(n, N - 1) * ldx, d, D);
 #pragma unroll
-      for (int i = 0; i < K; ++i) xb[t][j][i] = counts ? (float)v[i] : 0.f;
+      for (int i = 0; i < K; ++i) xb[t][i][j] = counts ? v[i] : (T)0.f;
     }
 #pragma unroll
     for (int i = 0; i < K; ++i) acc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // G by rows (four classes of token l % 16) and by columns (four tokens of class l % 16)
-  const float* gr[TILES];
-#pragma unroll
-  for (int t = 0; t < TILES; ++t) gr[t] = G + (int64_t)min(t * 16 + lm, N - 1) * ldz;
+  // G by rows (four classes of token l % 16) and by columns (four tokens of class l % 16), 256 MB at most: places in 32 bits
+  // (by columns in bf16: from the rows' terms, through LDS and its transposing reads)
+  constexpr bool TURN = sizeof(T) == 2;
+  __shared__ __attribute__((aligned(16))) bf16 turn[TURN ? 4 : 1][TURN ? TILES : 1][2][16][16];
+  const unsigned ld = (unsigned)ldz, by_row = lm * ld + 4 * lq, by_col = 4 * lq * ld + lm;
   vec nb[4];
-  f32x4 nr[TILES];
-  float nc[TILES][4];
+  f32x4 nr[TILES], nc[TURN ? 1 : TILES];
   auto fetch = [&](int v0) __attribute__((always_inline)) {        // (a step ahead)
-    const int v = v0 + 4 * lq, vc = min(v0 + lm, V - 1);
+    if (v0 >= end) return;
     if (parts) {
+      if (whole)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) nb[j] = some<K>(w + (int64_t)min(v + j, V - 1) * ldw, d, D);
+        for (int j = 0; j < 4; ++j) nb[j] = *(const vec*)(w + (int64_t)min(v0 + 4 * lq + j, V - 1) * ldw + d);
+      else
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) nr[t] = v < V ? *(const f32x4*)(gr[t] + v) : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < 4; ++j) nb[j] = some<K>(w + (int64_t)min(v0 + 4 * lq + j, V - 1) * ldw, d, D);
     }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) nr[t] = *(const f32x4*)(G + (size_t)t * 16 * ldz + (by_row + (unsigned)v0));
+    if constexpr (!TURN)
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) nc[t][j] = G[(int64_t)min(t * 16 + 4 * lq + j, N - 1) * ldz + vc];
+      for (int j = 0; j < 4; ++j) nc[t][j] = (G + (size_t)(t * 16 + j) * ldz)[by_col + (unsigned)v0];
   };
-  if (begin + wave * 16 < end) fetch(begin + wave * 16);
-  for (int v0 = begin + wave * 16; v0 < end; v0 += 64) {
+  fetch(begin + wave * 16);
+  for (int v0 = begin + wave * 16; v0 < end; v0 += STEP) {
     const int v = v0 + 4 * lq;
-    vec b[4];
-    f32x4 row[TILES];
-    float col[TILES][4];
+    other b[K];                                    // of four classes
 #pragma unroll
-    for (int j = 0; j < 4; ++j) b[j] = nb[j];
+    for (int i = 0; i < K; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[i][j] = nb[j][i];
+    Four<T> row[TILES];
+    f32x4 col[TURN ? 1 : TILES], sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
-      row[t] = nr[t];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) col[t][j] = t * 16 + 4 * lq + j < N ? nc[t][j] : 0.f;
+      row[t] = Four<T>(nr[t]);
+      sum += nr[t];
+      if constexpr (TURN) {
+        *(bf16x4*)&turn[wave][t][0][lm][4 * lq] = row[t].high();
+        *(bf16x4*)&turn[wave][t][1][lm][4 * lq] = row[t].low();
+      } else col[t] = nc[t];
     }
-    if (v0 + 64 < end) fetch(v0 + 64);
+    fetch(v0 + STEP);
     if (parts)
 #pragma unroll
       for (int t = 0; t < TILES; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float g = v + j < end ? row[t][j] : 0.f;           // (what lies behind the last class is not written)
-#pragma unroll
-          for (int i = 0; i < K; ++i) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(g, (float)b[j][i], acc[t][i], 0, 0, 0);
-        }
+        for (int i = 0; i < K; ++i) acc[t][i] = times(row[t], b[i], acc[t][i]);
     if (dw) {
       f32x4 out[K];
 #pragma unroll
       for (int i = 0; i < K; ++i) out[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (TURN) wave_fence();
 #pragma unroll
-      for (int t = 0; t < TILES; ++t)
+      for (int t = 0; t < TILES; ++t) {
+        Four<T> g;
+        if constexpr (TURN) {
+          // (lanes 4 e + q of 16 name the address of classes 4 q .. of token e, and get a class each, four tokens of it)
+          typedef short s16x4 __attribute__((ext_vector_type(4)));
+          typedef s16x4 __attribute__((address_space(3))) * at;
+          g = Four<T>(__builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)&turn[wave][t][0][4 * lq + lm / 4][lm % 4 * 4])),
+                      __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)&turn[wave][t][1][4 * lq + lm / 4][lm % 4 * 4])));
+        } else g = Four<T>(col[t]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int i = 0; i < K; ++i) out[i] = times(g, xb[t][i], out[i]);
+      }
+      if constexpr (TURN) wave_fence();
+      auto put_row = [&](int r, bool all) __attribute__((always_inline)) {
+        typename Some<K, TW>::vec o;
 #pragma unroll
-          for (int i = 0; i < K; ++i) out[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(col[t][j], xb[t][j][i], out[i], 0, 0, 0);
+        for (int i = 0; i < K; ++i) o[i] = (TW)out[i][r];
+        TW* to = dw + (int64_t)(v + r) * lddw;
+        if (all) *(typename Some<K, TW>::vec*)(to + d) = o;
+        else if (v + r < end) put<K>(to, d, D, o);
+      };
+      const bool all = whole && v0 + 16 <= end;
+      if (all)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (v + r < end) {
-          typename Some<K, TW>::vec o;
+        for (int r = 0; r < 4; ++r) put_row(r, true);
+      else
 #pragma unroll
-          for (int i = 0; i < K; ++i) o[i] = (TW)out[i][r];
-          put<K>(dw + (int64_t)(v + r) * lddw, d, D, o);
-        }
+        for (int r = 0; r < 4; ++r) put_row(r, false);
     }
-    if (db && blockIdx.x == 0) {
-      float sum = 0.f;
+    if (db && blockIdx.x == 0) {                   // over the tokens, 16 lanes
 #pragma unroll
-      for (int t = 0; t < TILES; ++t)
+      for (int j = 0; j < 4; ++j) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum += col[t][j];
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
-      if (lq == 0 && v0 + lm < end) db[v0 + lm] = sum;
+        for (int o = 1; o < 16; o *= 2) sum[j] += __shfl_xor(sum[j], o);
+        if (lm == j && v + j < end) db[v + j] = sum[j];
+      }
     }
   }
   if (!parts) return;
@@ -302,13 +376,14 @@ template <typename T> __global__ __launch_bounds__(256) void few_sums_kernel(con
   put<4>(dx + n * lddx, d, D, typename Some<4, T>::vec{(T)v[0], (T)v[1], (T)v[2], (T)v[3]});
 }
 
-int64_t small_ldz(const LinearCe& a) { return ((int64_t)a.V + 3) / 4 * 4; }
+int64_t small_ldz(const LinearCe& a) { return small_ce_stride(a.N, a.V); }
 template <typename T> void logits_as(const LinearCe& a, const Tokens& tk, float* z, hipStream_t s) {
   if (a.N <= 16) small_logits_kernel<T, 1><<<dim3(over(a.V, 16), 1), LOGIT_WAVES * WAVE, 0, s>>>((const T*)a.x, a.ldx, (const T*)a.w, a.ldw, a.D, a.bias, tk, z, small_ldz(a));
   else small_logits_kernel<T, 2><<<dim3(over(a.V, 16), over(a.N, 32)), LOGIT_WAVES * WAVE, 0, s>>>((const T*)a.x, a.ldx, (const T*)a.w, a.ldw, a.D, a.bias, tk, z, small_ldz(a));
 }
+int few_tiles_of(int N) { return N > 32 ? 4 : N > 16 ? 2 : 1; }
+int few_wide(bool f32, int N) { return 16 * few_features(f32, few_tiles_of(N)); }
 // workgroups over the classes
-int few_wide(bool f32, int N) { return 16 * (N > 16 ? few_features<float>(2) : f32 ? few_features<float>(1) : few_features<bf16>(1)); }
 int few_ranges(bool f32, int N, int V, int D) { return std::min(over(V, 64), std::max(1, 1024 / over(D, few_wide(f32, N)))); }
 
 template <typename T, typename TW> void grads_as(const LinearCe& a, const Tokens& tk, const float* G, float* parts, hipStream_t s) {
@@ -317,8 +392,10 @@ template <typename T, typename TW> void grads_as(const LinearCe& a, const Tokens
   const int per = over(over(a.V, few_ranges(a.f32, a.N, a.V, a.D)), 64) * 64, ranges = over(a.V, per);
   if (!a.dx) parts = nullptr;
   const dim3 grid(a.dx || a.dw ? over(a.D, wide) : 1, ranges);
+  if constexpr (sizeof(T) == 2)
+    if (a.N > 32) few_grads_kernel<T, TW, 4><<<grid, 256, 0, s>>>(G, small_ldz(a), tk, a.D, (const T*)a.x, a.ldx, (const T*)a.w, a.ldw, parts, ldp, per, (TW*)a.dw, a.lddw, a.db);
   if (a.N <= 16) few_grads_kernel<T, TW, 1><<<grid, 256, 0, s>>>(G, small_ldz(a), tk, a.D, (const T*)a.x, a.ldx, (const T*)a.w, a.ldw, parts, ldp, per, (TW*)a.dw, a.lddw, a.db);
-  else few_grads_kernel<T, TW, 2><<<grid, 256, 0, s>>>(G, small_ldz(a), tk, a.D, (const T*)a.x, a.ldx, (const T*)a.w, a.ldw, parts, ldp, per, (TW*)a.dw, a.lddw, a.db);
+  else if (a.N <= 32) few_grads_kernel<T, TW, 2><<<grid, 256, 0, s>>>(G, small_ldz(a), tk, a.D, (const T*)a.x, a.ldx, (const T*)a.w, a.ldw, parts, ldp, per, (TW*)a.dw, a.lddw, a.db);
   if (a.dx) few_sums_kernel<T><<<dim3(over(a.D, 256), a.N), 256, 0, s>>>(parts, ranges, ldp, tk, a.D, (T*)a.dx, a.lddx);
 }
 
@@ -326,7 +403,7 @@ template <typename T, typename TW> void grads_as(const LinearCe& a, const Tokens
 
 static Tokens tokens_of(const LinearCe& a, bool weighted) {
   Tokens tk;
-  tk.N = a.N; tk.V = a.V; tk.labels = a.labels; tk.row_grad = a.row_grad; tk.weighted = weighted; tk.scale = weighted ? a.grad_scale : 1.f;
+  tk.N = tk.rows = a.N; tk.V = a.V; tk.labels = a.labels; tk.row_grad = a.row_grad; tk.weighted = weighted; tk.scale = weighted ? a.grad_scale : 1.f;
   return tk;
 }
 static void logits_of(const LinearCe& a, const Tokens& tk, float* z, hipStream_t s) {
@@ -335,24 +412,28 @@ static void logits_of(const LinearCe& a, const Tokens& tk, float* z, hipStream_t
 }
 
 void small_ce_forward(const LinearCe& a, float* z, SmallGrad grad, hipStream_t s) {
-  const Tokens tk = tokens_of(a, grad == GRAD_WEIGHTED);
+  Tokens tk = tokens_of(a, grad == GRAD_WEIGHTED);
   logits_of(a, tk, z, s);
-  small_rows_kernel<<<a.N, 256, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad != GRAD_NONE);
+  if (grad == GRAD_WEIGHTED) tk.rows = 16 * few_tiles_of(a.N);
+  small_rows_kernel<<<tk.rows, 256, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad != GRAD_NONE);
 }
 
 void small_ce_gradient(const LinearCe& a, bool weighted, float* G, hipStream_t s) {
   Tokens tk = tokens_of(a, weighted);
   tk.stats = (const float2*)a.stats;
+  if (weighted) tk.rows = 16 * few_tiles_of(a.N);
   logits_of(a, tk, G, s);
 }
 
-static size_t few_parts_at(int N, int V) { return (small_ce_bytes(N, V) + 255) / 256 * 256; }
-size_t few_ce_bytes(bool f32, int N, int V, int D) { return few_parts_at(N, V) + sizeof(float) * (size_t)few_ranges(f32, N, V, D) * N * (((size_t)D + 3) / 4 * 4); }
-void few_ce_backward(const LinearCe& a, bool ready, hipStream_t s) {
+size_t few_parts_at(int N, int V) { return (small_ce_bytes(16 * few_tiles_of(N), V) + 255) / 256 * 256; }
+size_t few_ce_bytes(bool f32, int N, int V, int D) { return sizeof(float) * (size_t)few_ranges(f32, N, V, D) * N * (((size_t)D + 3) / 4 * 4); }
+void few_ce_backward(const LinearCe& a, Few there, hipStream_t s) {
   float *G = (float*)a.workspace, *parts = (float*)((char*)a.workspace + few_parts_at(a.N, a.V));
-  if (!ready) small_ce_gradient(a, true, G, s);
+  if (there == FEW_NOTHING) small_ce_gradient(a, true, G, s);
   Tokens tk = tokens_of(a, true);
   tk.stats = (const float2*)a.stats;
+  tk.rows = 16 * few_tiles_of(a.N);
+  if (there == FEW_LOGITS) small_turn_kernel<<<dim3(over(small_ldz(a), 1024), tk.rows), 256, 0, s>>>(G, small_ldz(a), tk);
   if (a.f32) grads_as<float, float>(a, tk, G, parts, s);
   else if (a.dw_f32) grads_as<bf16, float>(a, tk, G, parts, s);
   else grads_as<bf16, bf16>(a, tk, G, parts, s);

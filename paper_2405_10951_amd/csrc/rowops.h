@@ -12,6 +12,12 @@ template <typename T> struct Chunk { static constexpr int V = 16 / sizeof(T); ty
 // the same 16 bytes at the address of any element: global loads and stores of gfx950 take any address
 template <typename T> struct Loose { typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T)))); };
 
+// between what a wavefront's lanes write to LDS and what other lanes of it read
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Sums and maxima over a wavefront, in every lane; the pairs are those of an exchange with lane ^ 32, ^ 16, ... ^ 1.  They stay on the vector
 // unit: gfx950 swaps half waves and rows of 16 lanes, and once lanes 8 (then 4) apart hold the same value, a rotation by 8 (by 4)
 // within a row is the exchange with lane ^ 8 (lane ^ 4).  A row kernel waits for two such sums one after the other, and through LDS (ds_bpermute)
