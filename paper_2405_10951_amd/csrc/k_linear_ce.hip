@@ -1173,8 +1173,9 @@ static void no_tokens(const LinearCe& a, hipStream_t s) {
 static void few_backward(const LinearCe& a, bool both, hipStream_t s) {
   const Way way(a);
   if (way.little || !way.w) {
-    if (both) small_ce_forward(a, (float*)a.workspace, GRAD_WEIGHTED, s);
-    few_ce_backward(a, both ? FEW_GRADIENT : FEW_NOTHING, s);
+    const bool fused = both && few_fused(a.f32, a.V);
+    if (both && !fused) small_ce_forward(a, (float*)a.workspace, GRAD_WEIGHTED, s);
+    few_ce_backward(a, fused ? FEW_FUSED : both ? FEW_GRADIENT : FEW_NOTHING, s);
   } else {
     LinearCe f = a;
     f.workspace = (char*)a.workspace + few_parts_at(a.N, a.V);

@@ -34,7 +34,9 @@ void small_ce_gradient(const LinearCe& a, bool weighted, float* G, hipStream_t s
 constexpr int FEW_ROWS_F32 = 32, FEW_ROWS_BF16 = 64;
 size_t few_parts_at(int N, int V);
 size_t few_ce_bytes(bool f32, int N, int V, int D);
-enum Few { FEW_NOTHING, FEW_LOGITS, FEW_GRADIENT };
+// what G holds: nothing, logits, or G; fused: nothing, and the forward is wanted as well (of few_fused() classes)
+enum Few { FEW_NOTHING, FEW_LOGITS, FEW_GRADIENT, FEW_FUSED };
+bool few_fused(bool f32, int V);
 void few_ce_backward(const LinearCe& a, Few there, hipStream_t s);
 
 }  // namespace bsr
