@@ -618,7 +618,7 @@ int32_t bsr_linear_ce_forward_backward(const void* x, int64_t ldx, const void* w
 
 /*
  * The norm of many gradients taken together, and the gradients brought down to a largest norm: norm = sqrt(sum over tensors and values of g^2),
- * out = g min(1, max_norm / norm).  Squares and their sum are fp64.  A norm that is infinite or no number is given as it is and scales nothing.
+ * out = g min(1, max_norm / norm).  Squares, their sum and the factor are fp64.  A norm that is no number, or infinite or past fp32's range, is given as it is (as infinity) and scales nothing.
  *   grads, types, lengths  host arrays of `count` (1 or more) entries: device address (aligned to the values), BSR_BF16 or BSR_FP32, values (0 .. 2^36; any address
  *                where it is 0).  They are read before the call returns
  *   max_norm     0 or more; infinite: nothing is scaled

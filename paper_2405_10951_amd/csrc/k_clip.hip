@@ -92,19 +92,19 @@ __global__ __launch_bounds__(NT) void clip_scale_kernel(ClipTable t, const doubl
   __shared__ double red[WAVES];
   const double length = norm_of(parts, nparts, red);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)length;
-  // (a norm that is no number or infinite scales nothing)
-  const float by = length > (double)max_norm && length < INFINITY ? (float)((double)max_norm / length) : 1.f;
+  // (a norm that is no number, or infinite where it is told, scales nothing; fp64: the factor may lie below fp32's normal numbers)
+  const double by = length > (double)max_norm && (float)length < INFINITY ? (double)max_norm / length : 1.0;
   for (int k = blockIdx.x; k < t.pieces; k += gridDim.x) {
     const int p = t.pieces - 1 - k, i = tensor_of(t, p);
-    if (by == 1.f && t.out[i] == t.g[i]) continue;
+    if (by == 1.0 && t.out[i] == t.g[i]) continue;
     const int64_t at = (int64_t)(p - t.start[i]) * CLIP_PIECE, n = t.n[i];
     auto put = [&](auto* out) __attribute__((always_inline)) {
       return [=](auto v, int j) __attribute__((always_inline)) {
         typedef decltype(v) V;
-        if constexpr (sizeof(V) < 16) out[j] = (V)((float)v * by);
+        if constexpr (sizeof(V) < 16) out[j] = (V)(float)((double)(float)v * by);
         else {
 #pragma unroll
-          for (int e = 0; e < (int)(16 / sizeof(v[0])); ++e) v[e] = (float)v[e] * by;
+          for (int e = 0; e < (int)(16 / sizeof(v[0])); ++e) v[e] = (float)((double)(float)v[e] * by);
           *(typename Loose<std::remove_reference_t<decltype(*out)>>::vec*)(out + j) = v;
         }
       };

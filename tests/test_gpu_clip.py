@@ -88,6 +88,17 @@ def test_squares_past_the_range_of_fp32(env, scale):
     check(torch, P, gradients(torch, [1000, 333], 3, scale, kinds=("f32",)), 1e-3 * scale)
 
 
+def test_a_factor_below_the_normal_numbers_of_fp32(env):
+    torch, P = env
+    check(torch, P, gradients(torch, [1000, 333], 3, 1e36, kinds=("f32",)), 1e-3)
+
+
+def test_a_norm_past_the_range_of_fp32_scales_nothing(env):
+    torch, P = env
+    grads = [torch.full((n,), 3e38, device="cuda") for n in (100, 3000)]
+    assert torch.isinf(P.bsr_clip_grads(grads, 1.0)) and all((g == 3e38).all() for g in grads)
+
+
 def test_a_norm_that_is_no_number_scales_nothing(env):
     torch, P = env
     for bad in (float("nan"), float("inf"), -float("inf")):
