@@ -5,6 +5,8 @@
 //   rows     a workgroup a token: maximum, sum, loss
 //   grads    up to 32 tokens in fp32, 64 in bf16: dx and dw in one pass over w, multiplied in fp32 (16 x 16 x 4), or with G in two bf16 terms (16 x 16 x 16)
 // A launch is a chain of a few trips to memory; that, the calls and, for few rows of many classes, the bytes of w and dw are what bounds it.
+// Measured: 32 x 768 x 100 fp32 8 + 11 us; gradients of 32 x 4096 x 100000 bf16 348 (1.6 GB of w and dw: 4.7 TB/s; with fp32 products 728), of 64 rows 580 (two wavefronts a SIMD, of which each waits for a
+// half as long rows' piece; G by columns from memory instead of LDS: 673; 8 features a lane and one wavefront: 660; four wavefronts side by side on G: 690).
 #include <algorithm>
 
 #include "linear_ce.h"
@@ -186,9 +188,8 @@ template <int K, typename T> __device__ __forceinline__ void put(T* row, int d, 
 // Classes that a workgroup takes alone, with the maxima and sums of its rows: two launches instead of four.  (Loss and gradients of 32 x 768 x 100 fp32 18.7 us against 21.5, of 250 classes 23.7 against
 // 22.5; 64 x 4096 x 250 bf16 33 against 37)
 constexpr int fused_classes(bool f32) { return f32 ? 128 : 256; }
-// features of a lane; wavefronts that a SIMD has registers for
+// features of a lane: as many as leave registers for two wavefronts a SIMD
 constexpr int few_features(bool f32, int tiles) { return f32 || tiles > 2 ? 4 : 8; }
-constexpr int few_wavefronts(int tiles) { return 2; }
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 // Four values of G, and what they are multiplied by, of the four k of a lane.  fp32: as they are, four products of 16 x 16 x 4.  Beside bf16: G in two bf16 terms, off by 2^-17 of itself, which take
@@ -224,7 +225,7 @@ __device__ __forceinline__ f32x4 times(const Four<bf16>& g, bf16x4 b, f32x4 c) {
 // registers; dx's is added up over the range and leaves as a part, or, of one range, as it is.  G: [16 TILES, ldz], ldz whole sixteens, zero behind the last token and class.
 // LOGITS (of fused_classes() at most): G is still logits; every workgroup works out the rows' maxima and sums for itself, the first one leaves them and the losses.
 template <typename T, typename TW, int TILES, bool LOGITS>
-__global__ __launch_bounds__(256, few_wavefronts(TILES)) void few_grads_kernel(const float* __restrict__ G, int64_t ldz, Tokens tk, int D, const T* __restrict__ x, int64_t ldx,
+__global__ __launch_bounds__(256, 2) void few_grads_kernel(const float* __restrict__ G, int64_t ldz, Tokens tk, int D, const T* __restrict__ x, int64_t ldx,
                                                                                const T* __restrict__ w, int64_t ldw, float* __restrict__ parts, int64_t ldp, int per, T* __restrict__ dx,
                                                                                int64_t lddx, TW* __restrict__ dw, int64_t lddw, float* __restrict__ db) {
   constexpr int K = few_features(sizeof(T) == 4, TILES), STEP = 64;

@@ -5,6 +5,8 @@
 // activations in 16 bits).
 // Bound by memory: a row is read once, into registers, by 64 to 1024 threads (two 16-byte chunks each at most), sums are fp32, over rows in a fixed order.
 // Rows longer than the registers take (16384 bf16, 8192 fp32), or shorter than a chunk, are read again for every pass over them (`any` kernels).
+// Measured: 16384 x 8192 bf16 with the residual, forward 182 us, backward 204, each 1.07 GB (5.9 and 5.3 TB/s; a copy of 2 GiB 4.96: more of this is reading); 6304 x 768 bf16 with residual to 8-bit
+// rows 8.0; 1031 x 1777 fp32 backward 6.4 and 4.6 for the sums over its 512 partial rows; 1 x 4096 bf16 1.9.
 #include <algorithm>
 
 #include "rms_rows.h"
