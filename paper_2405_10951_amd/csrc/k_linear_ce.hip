@@ -28,6 +28,9 @@ typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+int up(int64_t n, int to) { return (int)((n + to - 1) / to * to); }
+int over(int64_t n, int by) { return (int)((n + by - 1) / by); }
+
 constexpr int BK = 64;
 constexpr int G_SHIFT = 14;                        // G is kept times 2^14
 
@@ -64,11 +67,13 @@ template <int BM_, int BN_, int WM_, int WN_, int NST_> struct Shape {
   static constexpr int LDR = TN * 2 + 16, LDF = TN * 4 + 16;     // patch rows in bytes: fp16, fp32
   static constexpr int patch = 32 * (2 * LDR > LDF ? 2 * LDR : LDF);                       // of a wavefront: 32 rows, of one or two terms
   static constexpr size_t lds = stages > (size_t)patch * WM * WN ? stages : (size_t)patch * WM * WN;
+  static constexpr int at_once = (int)(160 * 1024 / lds), wavefronts = at_once * (NT / 64) / 4;       // workgroups a CU, wavefronts a SIMD
 };
 typedef Shape<256, 256, 2, 4, 2> Large;
 typedef Shape<256, 256, 2, 2, 2> LargeForward;     // (four wavefronts read a third less of LDS for the product, eight share the work of ending a tile)
 typedef Shape<128, 128, 2, 4, 3> Small;
 typedef Shape<64, 128, 2, 2, 3> Mid;                  // (logits only: where larger tiles would leave CUs idle)
+typedef Shape<128, 128, 2, 4, 2> Short;               // (logits only: of few k-tiles, two workgroups a CU, so that one's products cover the other's beginning and end)
 typedef Shape<32, 256, 1, 4, 4> Few;
 
 // tiles band after band of eight row tiles, row tile fastest: what an XCD works on at a time shares rows of A and of B
@@ -436,7 +441,7 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
 }
 
 template <class S, Mode MODE, bool F16, int SEG, bool DB>
-__global__ __launch_bounds__(S::NT, 1) void ce_logits_kernel(CeGemm g, int mt, int nt) {
+__global__ __launch_bounds__(S::NT, S::wavefronts) void ce_logits_kernel(CeGemm g, int mt, int nt) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int tm, tn;
   tile_at(xcd_remap(blockIdx.x, gridDim.x), mt, nt, tm, tn);
@@ -522,47 +527,74 @@ __device__ __forceinline__ uint32_t bits_if_finite(float v) {
 
 // x, w or both (a launch handles up to two; the first `blocks` workgroups the first)
 struct PackJob { const void* x = nullptr; int64_t ldx = 0, rows = 0; uint16_t* to = nullptr; int64_t term = 0; int* exps = nullptr; };
-// rows of D values to rows of whole k-tiles: bf16 as they are, fp32 in two fp16 terms (`term` elements apart) with a power of two a row.  A wavefront a row
-template <typename T>
+// rows of D values to rows of whole k-tiles: bf16 as they are, a thread 8 of them, fp32 in two fp16 terms (`term` elements apart) with a power of two a row, LANES lanes a row
+template <typename T, int LANES> int pack_blocks(int64_t rows, int Dp) { return sizeof(T) == 2 ? over(rows * (Dp / 8), 256) : over(rows, 256 / LANES); }
+template <typename T, int LANES>
 __global__ __launch_bounds__(256) void ce_pack_kernel(PackJob a, PackJob b, int blocks, int D, int Dp) {
   const bool first = (int)blockIdx.x < blocks;
   const PackJob j = first ? a : b;
-  const int lane = threadIdx.x % WAVE;
-  const int64_t m = (int64_t)(first ? blockIdx.x : blockIdx.x - blocks) * 4 + threadIdx.x / WAVE;
-  if (m >= j.rows) return;
-  const T* row = (const T*)j.x + m * j.ldx;
-  uint16_t* out = j.to + m * Dp;
+  const int block = first ? blockIdx.x : blockIdx.x - blocks;
+  constexpr int V = Chunk<T>::V;
+  auto load = [&](const T* row, int k) __attribute__((always_inline)) {
+    typename Chunk<T>::vec v;
+    if (k + V <= D) v = *(const typename Loose<T>::vec*)(row + k);
+    else
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] = k + e < D ? row[k + e] : (T)0.f;
+    return v;
+  };
   if constexpr (sizeof(T) == 2) {
-#pragma unroll 4
-    for (int k = lane; k < Dp; k += WAVE) out[k] = k < D ? __builtin_bit_cast(uint16_t, row[k]) : (uint16_t)0;
+    const unsigned chunks = Dp / V, i = (unsigned)block * 256 + threadIdx.x, m = i / chunks;       // (2^33 values at most)
+    if (m < j.rows) *(typename Chunk<T>::vec*)(j.to + (int64_t)m * Dp + (i - m * chunks) * V) = load((const T*)j.x + (int64_t)m * j.ldx, (i - m * chunks) * V);
   } else {
-    // rows of up to 1024 values stay in registers, longer ones are read twice
-    constexpr int KEEP = 16;
-    float v[KEEP], most = 0.f;
-    if (Dp <= KEEP * WAVE) {
+    const int lane = threadIdx.x % LANES;
+    const int64_t m = (int64_t)block * (256 / LANES) + threadIdx.x / LANES;
+    const bool there = m < j.rows;                 // (lanes of other rows take part in the maximum)
+    const T* row = (const T*)j.x + (there ? m : j.rows - 1) * j.ldx;
+    uint16_t* out = j.to + m * Dp;
+    // rows of up to 2048 values stay in registers, longer ones are read twice
+    constexpr int KEEP = LANES == WAVE ? 8 : 1;
+    f32x4 v[KEEP];
+    float most = 0.f;
+    const bool kept = LANES < WAVE || Dp <= KEEP * WAVE * V;      // (fewer lanes: of rows that they hold)
+    auto most_of = [&](f32x4 p) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < KEEP; ++i) v[i] = lane + i * WAVE < D ? row[lane + i * WAVE] : 0.f;
-#pragma unroll
-      for (int i = 0; i < KEEP; ++i) most = fmaxf(most, __uint_as_float(bits_if_finite(v[i])));
-    } else {
-#pragma unroll 8
-      for (int k = lane; k < D; k += WAVE) most = fmaxf(most, __uint_as_float(bits_if_finite(row[k])));
-    }
-    const int e = exponent_of(__float_as_uint(wave_max(most)));
-    if (lane == 0) j.exps[m] = e;
-    auto put = [&](int k, float x) __attribute__((always_inline)) {
-      x = ldexpf(x, -e);
-      const f16 h = (f16)x, l = (f16)(x - (float)h);
-      out[k] = __builtin_bit_cast(uint16_t, h);
-      out[j.term + k] = __builtin_bit_cast(uint16_t, l);
+      for (int e = 0; e < V; ++e) most = fmaxf(most, __uint_as_float(bits_if_finite(p[e])));
     };
-    if (Dp <= KEEP * WAVE) {
+    if (kept) {
+#pragma unroll
+      for (int i = 0; i < KEEP; ++i) v[i] = load(row, (lane + i * LANES) * V);
+#pragma unroll
+      for (int i = 0; i < KEEP; ++i) most_of(v[i]);
+    } else {
+#pragma unroll 4
+      for (int k = lane * V; k < D; k += WAVE * V) most_of(load(row, k));
+    }
+    if constexpr (LANES == WAVE) most = wave_max(most);
+    else
+#pragma unroll
+      for (int d = 1; d < LANES; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    if (!there) return;
+    const int e = exponent_of(__float_as_uint(most));
+    if (lane == 0) j.exps[m] = e;
+    auto put = [&](int k, f32x4 x) __attribute__((always_inline)) {
+      f16x4 h, l;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float s = ldexpf(x[i], -e);
+        h[i] = (f16)s;
+        l[i] = (f16)(s - (float)h[i]);
+      }
+      *(f16x4*)(out + k) = h;
+      *(f16x4*)(out + j.term + k) = l;
+    };
+    if (kept) {
 #pragma unroll
       for (int i = 0; i < KEEP; ++i)
-        if (lane + i * WAVE < Dp) put(lane + i * WAVE, v[i]);
+        if ((lane + i * LANES) * V < Dp) put((lane + i * LANES) * V, v[i]);
     } else {
-#pragma unroll 8
-      for (int k = lane; k < Dp; k += WAVE) put(k, k < D ? row[k] : 0.f);
+#pragma unroll 4
+      for (int k = lane * V; k < Dp; k += WAVE * V) put(k, load(row, k));
     }
   }
 }
@@ -838,8 +870,6 @@ template <typename T> __global__ __launch_bounds__(256) void ce_fill_kernel(T* _
 }
 
 // ------------------------------------------------------------------------------------------ host
-int up(int64_t n, int to) { return (int)((n + to - 1) / to * to); }
-int over(int64_t n, int by) { return (int)((n + by - 1) / by); }
 
 // a kernel has its LDS, once a device
 template <auto KERNEL> void with_lds(size_t bytes) {
@@ -851,9 +881,9 @@ template <auto KERNEL> void with_lds(size_t bytes) {
     __atomic_fetch_or(&known, (uint64_t)1 << (dev & 63), __ATOMIC_RELAXED);
   }
 }
-enum { LARGE, SMALL, MID, FEW };
-int rows_of(int shape) { return shape == FEW ? Few::BM : shape == MID ? Mid::BM : shape == SMALL ? Small::BM : Large::BM; }
-int cols_of(int shape) { return shape == FEW ? Few::BN : shape == MID ? Mid::BN : shape == SMALL ? Small::BN : Large::BN; }
+enum { LARGE, SMALL, MID, FEW, SHORT };
+int rows_of(int shape) { return shape == FEW ? Few::BM : shape == SHORT ? Short::BM : shape == MID ? Mid::BM : shape == SMALL ? Small::BM : Large::BM; }
+int cols_of(int shape) { return shape == FEW ? Few::BN : shape == SHORT ? Short::BN : shape == MID ? Mid::BN : shape == SMALL ? Small::BN : Large::BN; }
 
 template <class S, Mode MODE, bool F16, int SEG, bool DB> void launch_logits(const CeGemm& g, int rows, hipStream_t s) {
   with_lds<ce_logits_kernel<S, MODE, F16, SEG, DB>>(S::lds);
@@ -863,6 +893,7 @@ template <class S, Mode MODE, bool F16, int SEG, bool DB> void launch_logits(con
 // rows: those that tiles have to cover
 template <Mode MODE, bool F16, int SEG, bool DB> void logits(int shape, const CeGemm& g, int rows, hipStream_t s) {
   if (shape == FEW) launch_logits<Few, MODE, F16, SEG, DB>(g, rows, s);
+  else if (shape == SHORT) launch_logits<Short, MODE, F16, SEG, DB>(g, rows, s);
   else if (shape == MID) launch_logits<Mid, MODE, F16, SEG, DB>(g, rows, s);
   else if (shape == SMALL) launch_logits<Small, MODE, F16, SEG, DB>(g, rows, s);
   else launch_logits<std::conditional_t<MODE == STATS, LargeForward, Large>, MODE, F16, SEG, DB>(g, rows, s);
@@ -873,16 +904,17 @@ template <class S, int SEG> void launch_grads(const CeGemm& a, const CeGemm& b, 
   ce_grads_kernel<S, SEG><<<blocks(a) + blocks(b), S::NT, S::lds, s>>>(a, b, blocks(a));
 }
 
-// Models of a launch, in us: a workgroup takes a CU for start + k-tiles * tile
-struct Cost { double tile, start; };
-constexpr Cost COST[4] = {{1.7, 8}, {0.6, 4}, {0.4, 4}, {0.5, 4}};
+// Models of a launch, in us: a workgroup, or the two of a shape that a CU takes at once, has a CU for start + k-tiles * tile.  (Short against large, forward: 600 x 100 x 100000 bf16 60 against 75 us, 2000 x 512 x
+// 50000 128 against 136, 2048 x 768 x 21841 80 against 79)
+struct Cost { double tile, start; int at_once; };
+constexpr Cost COST[5] = {{1.7, 8, 1}, {0.6, 4, 1}, {0.4, 4, 1}, {0.5, 4, 1}, {1.03, 2.3, 2}};
 int logits_shape(int64_t M, int64_t N, int kt) {
   int best = SMALL;
   double least = 1e30;
-  for (int shape = LARGE; shape <= FEW; ++shape) {
+  for (int shape = LARGE; shape <= SHORT; ++shape) {
     if (shape == FEW && M > Few::BM) continue;
     const int64_t tiles = (int64_t)over(M, rows_of(shape)) * over(N, cols_of(shape));
-    const double us = (double)((tiles + 255) / 256) * (COST[shape].start + kt * COST[shape].tile);
+    const double us = (double)over(tiles, 256 * COST[shape].at_once) * (COST[shape].start + kt * COST[shape].tile);
     if (us < least) { least = us; best = shape; }
   }
   return best;
@@ -928,11 +960,11 @@ Split grads_split(int64_t M, int64_t n, int64_t D, int kx, int kw) {
 // What goes to k_linear_ce_small.hip: little work, where the launches count; few rows backward (w is read and dw written once there), and forward where they would have to be packed first.  Its
 // logits take 16 MB at most, those of few rows, of which there is room for 16, 32 or 64, 256
 constexpr size_t SMALL_BYTES = 16 << 20, FEW_BYTES = 256 << 20;
-constexpr double SMALL_WORK = 1 << 28;             // tokens x features x classes
-bool is_small(int N, int D, int V) { return N <= 1 << 20 && small_ce_bytes(N, V) <= SMALL_BYTES && (double)N * D * V <= SMALL_WORK; }      // (a launch has up to 65535 workgroups one way)
+constexpr double SMALL_WORK = 1 << 28, MOST_SMALL_WORK = 1 << 30;        // tokens x features x classes; where tiles would leave most CUs idle
+bool is_small(int N, int D, int V) { return N <= 1 << 20 && small_ce_bytes(N, V) <= SMALL_BYTES && (double)N * D * V <= MOST_SMALL_WORK; }      // (a launch has up to 65535 workgroups one way)
 // (more than 32 rows of a w that would have to be packed: 48 x 1001 x 50000 bf16 318 us here, 291 by tiles)
-bool is_few(bool f32, int N, int V) { return N <= (f32 ? FEW_ROWS_F32 : FEW_ROWS_BF16) && few_parts_at(N, V) <= FEW_BYTES; }
-bool always_few(int N) { return N <= 32; }
+bool is_few(int N, int V) { return N <= FEW_ROWS && few_parts_at(N, V) <= FEW_BYTES; }
+bool always_few(bool f32, int N) { return f32 || N <= 32; }
 
 // sizes, and places in the workspace
 struct Plan {
@@ -988,10 +1020,12 @@ Rows rows_operand(const void* p, int64_t ld, bool f32, int64_t rows, int Dp, voi
   return {packed, Dp, job.term, f32 ? exps : nullptr};
 }
 void pack(const PackJob& a, const PackJob& b, bool f32, int D, int Dp, hipStream_t s) {
-  const int na = over(a.rows, 4), nb = over(b.rows, 4);
-  if (na + nb == 0) return;
-  if (f32) ce_pack_kernel<float><<<na + nb, 256, 0, s>>>(a, b, na, D, Dp);
-  else ce_pack_kernel<bf16><<<na + nb, 256, 0, s>>>(a, b, na, D, Dp);
+  if (a.rows + b.rows == 0) return;
+  auto go = [&](auto kernel, int na, int nb) { kernel<<<na + nb, 256, 0, s>>>(a, b, na, D, Dp); };
+  if (!f32) go(ce_pack_kernel<bf16, WAVE>, pack_blocks<bf16, WAVE>(a.rows, Dp), pack_blocks<bf16, WAVE>(b.rows, Dp));
+  else if (Dp <= 64) go(ce_pack_kernel<float, 16>, pack_blocks<float, 16>(a.rows, Dp), pack_blocks<float, 16>(b.rows, Dp));
+  else if (Dp <= 128) go(ce_pack_kernel<float, 32>, pack_blocks<float, 32>(a.rows, Dp), pack_blocks<float, 32>(b.rows, Dp));
+  else go(ce_pack_kernel<float, WAVE>, pack_blocks<float, WAVE>(a.rows, Dp), pack_blocks<float, WAVE>(b.rows, Dp));
 }
 
 template <typename T> void transpose(const TransposeJob& a, const TransposeJob& b, int D, hipStream_t s) {
@@ -1026,10 +1060,10 @@ CeGemm logits_gemm(const LinearCe& a, const Plan& p, const Rows& x, const Rows& 
 
 size_t linear_ce_workspace_bytes(bool f32, int N, int D, int V, bool backward) {
   // (few rows: the logits may come from tiles, whose scratch lies where the parts of dx do afterwards)
-  const size_t few = is_few(f32, N, V) ? few_parts_at(N, V) + std::max(few_ce_bytes(f32, N, V, D), f32 ? 0 : Plan(f32, N, D, V, false, false).bytes) : 0;
-  if (backward && few && always_few(N)) return few;
+  const size_t few = is_few(N, V) ? few_parts_at(N, V) + std::max(few_ce_bytes(f32, N, V, D), f32 ? 0 : Plan(f32, N, D, V, false, false).bytes) : 0;
+  if (backward && few && always_few(f32, N)) return few;
   const size_t bytes = std::max(Plan(f32, N, D, V, backward).bytes, backward ? few : 0);
-  return !backward && (is_small(N, D, V) || (few && always_few(N))) ? std::max(bytes, small_ce_bytes(N, V)) : bytes;
+  return !backward && (is_small(N, D, V) || (few && always_few(f32, N))) ? std::max(bytes, small_ce_bytes(N, V)) : bytes;
 }
 
 // How x and w lie, and what follows from it: the logits (or G) of little work straight from x and w, in a launch of its own, not in tiles
@@ -1038,8 +1072,9 @@ struct Way {
   explicit Way(const LinearCe& a) {
     x = !a.f32 && whole_rows(a.x, a.ldx, a.D);
     w = !a.f32 && whole_rows(a.w, a.ldw, a.D);
-    little = is_small(a.N, a.D, a.V) && (!x || !w || few_tiles(a.N, a.V, over(a.D, BK) * (a.f32 ? 3 : 1)));
-    few = is_few(a.f32, a.N, a.V) && (always_few(a.N) || w || little);
+    little = is_small(a.N, a.D, a.V) &&
+             ((double)a.N * a.D * a.V <= SMALL_WORK && (!x || !w) || few_tiles(a.N, a.V, over(a.D, BK) * (a.f32 ? 3 : 1)));
+    few = is_few(a.N, a.V) && (always_few(a.f32, a.N) || w || little);
   }
 };
 
@@ -1177,8 +1212,9 @@ static void few_backward(const LinearCe& a, bool both, hipStream_t s) {
   const Way way(a);
   if (way.little || !way.w) {
     const bool fused = both && few_fused(a.f32, a.V);
-    if (both && !fused) small_ce_forward(a, (float*)a.workspace, GRAD_WEIGHTED, s);
-    few_ce_backward(a, fused ? FEW_FUSED : both ? FEW_GRADIENT : FEW_NOTHING, s);
+    const bool many = a.V > 4096;                  // (a workgroup a row turns those into G more slowly than a launch of its own)
+    if (both && !fused) small_ce_forward(a, (float*)a.workspace, many ? GRAD_NONE : GRAD_WEIGHTED, s);
+    few_ce_backward(a, fused ? FEW_FUSED : !both ? FEW_NOTHING : many ? FEW_LOGITS : FEW_GRADIENT, s);
   } else {
     LinearCe f = a;
     f.workspace = (char*)a.workspace + few_parts_at(a.N, a.V);
@@ -1196,7 +1232,7 @@ void linear_ce_backward(const LinearCe& a, hipStream_t s) {
 static size_t both_kept_at(bool f32, int N, int D, int V) {
   return (std::max(linear_ce_workspace_bytes(f32, N, D, V, false), linear_ce_workspace_bytes(f32, N, D, V, true)) + 255) / 256 * 256;
 }
-size_t linear_ce_both_bytes(bool f32, int N, int D, int V) { return both_kept_at(f32, N, D, V) + (keeps(f32, N, D, V) && !(is_few(f32, N, V) && always_few(N)) ? small_ce_bytes(N, V) : 0); }
+size_t linear_ce_both_bytes(bool f32, int N, int D, int V) { return both_kept_at(f32, N, D, V) + (keeps(f32, N, D, V) && !(is_few(N, V) && always_few(f32, N)) ? small_ce_bytes(N, V) : 0); }
 void linear_ce_both(const LinearCe& a, hipStream_t s) {
   const Way way(a);
   if (a.N == 0) {

@@ -5,7 +5,7 @@
 //   rows     a workgroup a token: maximum, sum, loss
 //   grads    up to 32 tokens in fp32, 64 in bf16: dx and dw in one pass over w, multiplied in fp32 (16 x 16 x 4), or with G in two bf16 terms (16 x 16 x 16)
 // A launch is a chain of a few trips to memory; that, the calls and, for few rows of many classes, the bytes of w and dw are what bounds it.
-// Measured: 32 x 768 x 100 fp32 8 + 11 us; gradients of 32 x 4096 x 100000 bf16 348 (1.6 GB of w and dw: 4.7 TB/s; with fp32 products 728), of 64 rows 580 (two wavefronts a SIMD, of which each waits for a
+// Measured: 32 x 768 x 100 fp32 8 + 11 us; loss and gradients of 48 x 2048 x 100000 fp32 987 (by tiles 2360), of 1 x 100 x 100000 bf16 50; gradients of 32 x 4096 x 100000 bf16 348 (1.6 GB of w and dw: 4.7 TB/s; with fp32 products 728), of 64 rows 580 (two wavefronts a SIMD, of which each waits for a
 // half as long rows' piece; G by columns from memory instead of LDS: 673; 8 features a lane and one wavefront: 660; four wavefronts side by side on G: 690).
 #include <algorithm>
 
@@ -53,91 +53,128 @@ struct Tokens {
   }
 };
 
-// z or G [N, ldz]: lane l has V features of class l % 16 and of token l % 16
+// z or G [N, ldz]: lane l has V features of CT classes l % 16 and of TILES tokens l % 16.  KW of the eight wavefronts share the features of 16 CT classes.  (Every workgroup reads x from the caches: with many
+// tokens for several classes at a time, or that would take longer than w's bytes: forward of 48 x 2048 x 100000 fp32 465 us with two times 16 classes and four times 16 tokens, 582 with one times 16
+// classes, 32 x 2048 x 100000 328 and 387)
 constexpr int LOGIT_WAVES = 8;
-template <typename T, int TILES>
+template <typename T, int TILES, int KW, int CT>
 __global__ __launch_bounds__(LOGIT_WAVES * WAVE) void small_logits_kernel(const T* __restrict__ x, int64_t ldx, const T* __restrict__ w, int64_t ldw, int D, const float* __restrict__ bias, Tokens tk,
                                                            float* __restrict__ z, int64_t ldz) {
-  constexpr int C = Chunk<T>::V, STEP = 4 * C, AT_ONCE = 4;
+  constexpr int C = Chunk<T>::V, STEP = 4 * C, AT_ONCE = TILES * CT > 4 ? 2 : 4;
   typedef typename Chunk<T>::vec vec;
-  __shared__ f32x4 red[LOGIT_WAVES - 1][TILES][WAVE];
-  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, v0 = blockIdx.x * 16, n0 = blockIdx.y * 16 * TILES, part = lane / 16 * C, N = tk.N, V = tk.V;
-  const T* wr = w + (int64_t)min(v0 + lane % 16, V - 1) * ldw;
-  const T* xr[TILES];
+  __shared__ f32x4 red[KW > 1 ? KW - 1 : 1][CT][TILES][WAVE];
+  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE % KW, v0 = (blockIdx.x * (LOGIT_WAVES / KW) + threadIdx.x / WAVE / KW) * 16 * CT, n0 = blockIdx.y * 16 * TILES,
+            part = lane / 16 * C, N = tk.N, V = tk.V;
+  const T *wr[CT], *xr[TILES];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) wr[c] = w + (int64_t)min(v0 + c * 16 + lane % 16, V - 1) * ldw;
 #pragma unroll
   for (int t = 0; t < TILES; ++t) xr[t] = x + (int64_t)min(n0 + t * 16 + lane % 16, N - 1) * ldx;
-  f32x4 acc[TILES];
+  f32x4 acc[CT][TILES];
 #pragma unroll
-  for (int t = 0; t < TILES; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int k = wave * STEP * AT_ONCE; k < D; k += LOGIT_WAVES * STEP * AT_ONCE) {
-    vec a[AT_ONCE], b[AT_ONCE][TILES];
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) acc[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int k = wave * STEP * AT_ONCE; k < D; k += KW * STEP * AT_ONCE) {
+    vec a[AT_ONCE][CT], b[AT_ONCE][TILES];
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
       const int at = k + i * STEP + part;
-      a[i] = piece(wr, at, D);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) a[i][c] = piece(wr[c], at, D);
 #pragma unroll
       for (int t = 0; t < TILES; ++t) b[i][t] = piece(xr[t], at, D);
     }
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) acc[t] = multiplied(a[i], b[i][t], acc[t]);
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) acc[c][t] = multiplied(a[i][c], b[i][t], acc[c][t]);
   }
-  if (wave > 0)
+  static_assert(KW == 1 || KW == LOGIT_WAVES, "");
+  if constexpr (KW > 1) {
+    if (wave > 0)
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) red[wave - 1][t][lane] = acc[t];
-  __syncthreads();
-  if (wave > 0) return;
-  const int v = v0 + lane / 16 * 4;
-  f32x4 b;
+      for (int c = 0; c < CT; ++c)
 #pragma unroll
-  for (int j = 0; j < 4; ++j) b[j] = bias && v + j < V ? bias[v + j] : 0.f;
+        for (int t = 0; t < TILES; ++t) red[wave - 1][c][t][lane] = acc[c][t];
+    __syncthreads();
+    if (wave > 0) return;
+  }
 #pragma unroll
-  for (int t = 0; t < TILES; ++t) {
-    const int n = n0 + t * 16 + lane % 16;
-    if (n >= tk.rows || v >= ldz) continue;
-    f32x4 o = acc[t];
+  for (int c = 0; c < CT; ++c) {
+    const int v = v0 + c * 16 + lane / 16 * 4;
+    f32x4 b;
 #pragma unroll
-    for (int i = 0; i < LOGIT_WAVES - 1; ++i) o += red[i][t][lane];
-    o += b;
-    if (tk.stats) {
-      const bool counts = tk.counts(n);
-      const int m = min(n, N - 1);
-      const float2 st = tk.stats[m];
-      const float by = tk.scale * (tk.weighted && tk.row_grad ? tk.row_grad[m] : 1.f);
+    for (int j = 0; j < 4; ++j) b[j] = bias && v + j < V ? bias[v + j] : 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        o[j] = counts && v + j < V ? by * (__builtin_amdgcn_exp2f(fmaf(o[j] - st.x, LOG2E, -st.y * LOG2E)) - (v + j == tk.labels[m] ? 1.f : 0.f)) : 0.f;
+    for (int t = 0; t < TILES; ++t) {
+      const int n = n0 + t * 16 + lane % 16;
+      if (n >= tk.rows || v >= ldz) continue;
+      f32x4 o = acc[c][t];
+      if constexpr (KW > 1)
+#pragma unroll
+        for (int i = 0; i < KW - 1; ++i) o += red[i][c][t][lane];
+      o += b;
+      if (tk.stats) {
+        const bool counts = tk.counts(n);
+        const int m = min(n, N - 1);
+        const float2 st = tk.stats[m];
+        const float by = tk.scale * (tk.weighted && tk.row_grad ? tk.row_grad[m] : 1.f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          o[j] = counts && v + j < V ? by * (__builtin_amdgcn_exp2f(fmaf(o[j] - st.x, LOG2E, -st.y * LOG2E)) - (v + j == tk.labels[m] ? 1.f : 0.f)) : 0.f;
+      }
+      *(f32x4*)(z + n * ldz + v) = o;                        // (ldz: whole fours)
     }
-    *(f32x4*)(z + n * ldz + v) = o;                          // (ldz: whole fours at least)
   }
 }
 
 // a workgroup a token.  grad: the logits become G (of tk.rows rows)
-__global__ __launch_bounds__(256) void small_rows_kernel(float* __restrict__ z, int64_t ldz, Tokens tk, float* __restrict__ loss, float2* __restrict__ stats, bool grad) {
-  __shared__ float red[2][4];
+template <int NT>
+__global__ __launch_bounds__(NT) void small_rows_kernel(float* __restrict__ z, int64_t ldz, Tokens tk, float* __restrict__ loss, float2* __restrict__ stats, bool grad) {
+  constexpr int WAVES = NT / WAVE;
+  __shared__ float red[2][WAVES];
   const int m = blockIdx.x, wave = threadIdx.x / WAVE, V = tk.V;
   float* row = z + m * ldz;
   if (m >= tk.N) {
-    for (int v = threadIdx.x; v < ldz; v += 256) row[v] = 0.f;
+    for (int v = threadIdx.x; v < ldz; v += NT) row[v] = 0.f;
     return;
   }
+  auto four = [&](int v) __attribute__((always_inline)) {          // (ldz: whole fours)
+    f32x4 p = *(const f32x4*)(row + v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = v + j < V ? p[j] : -INFINITY;
+    return p;
+  };
   float most = -INFINITY;
 #pragma unroll 4
-  for (int v = threadIdx.x; v < V; v += 256) most = fmaxf(most, row[v]);
+  for (int v = threadIdx.x * 4; v < V; v += NT * 4) {
+    const f32x4 p = four(v);
+    most = fmaxf(most, fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])));
+  }
   most = wave_max(most);
   if (threadIdx.x % WAVE == 0) red[0][wave] = most;
   __syncthreads();
-  most = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  most = red[0][0];
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) most = fmaxf(most, red[0][i]);
   // (fmaxf passes NaN over, the sum does not; a row of -inf alone has sum 0)
   const float ref = most == -INFINITY ? 0.f : most;
   float s = 0.f;
 #pragma unroll 4
-  for (int v = threadIdx.x; v < V; v += 256) s += __builtin_amdgcn_exp2f((row[v] - ref) * LOG2E);
+  for (int v = threadIdx.x * 4; v < V; v += NT * 4) {
+    const f32x4 p = four(v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s += __builtin_amdgcn_exp2f((p[j] - ref) * LOG2E);
+  }
   s = wave_sum(s);
   if (threadIdx.x % WAVE == 0) red[1][wave] = s;
   __syncthreads();
-  s = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+  s = red[1][0];
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) s += red[1][i];
   const float ls = s == 0.f ? 0.f : logf(s);
   const int label = tk.labels[m];
   const bool there = label >= 0 && label < V && !(most == -INFINITY && s == 0.f);
@@ -149,9 +186,14 @@ __global__ __launch_bounds__(256) void small_rows_kernel(float* __restrict__ z, 
   if (!grad) return;
   __syncthreads();
   const float weight = tk.row_grad ? tk.row_grad[m] : 1.f, by = tk.weighted ? tk.scale * weight : 1.f;
+  const bool counts = there && weight != 0.f;
 #pragma unroll 4
-  for (int v = threadIdx.x; v < V; v += 256) row[v] = there && weight != 0.f ? by * (__builtin_amdgcn_exp2f(fmaf(row[v] - most, LOG2E, -ls * LOG2E)) - (v == label ? 1.f : 0.f)) : 0.f;
-  if (V + (int)threadIdx.x < ldz) row[V + threadIdx.x] = 0.f;
+  for (int v = threadIdx.x * 4; v < ldz; v += NT * 4) {
+    f32x4 p = *(const f32x4*)(row + v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = counts && v + j < V ? by * (__builtin_amdgcn_exp2f(fmaf(p[j] - most, LOG2E, -ls * LOG2E)) - (v + j == label ? 1.f : 0.f)) : 0.f;
+    *(f32x4*)(row + v) = p;
+  }
 }
 
 // logits to G in their place, with the row's weight: four classes a thread
@@ -200,14 +242,29 @@ template <> struct Four<float> {
   f32x4 v;
   Four() = default;
   __device__ __forceinline__ explicit Four(f32x4 g) : v(g) {}
+  // four classes of token lm to a tile; four tokens of class lm from it
+  __device__ __forceinline__ void put(float (*tile)[16][20], int lm, int lq) const { *(f32x4*)&tile[0][lm][4 * lq] = v; }
+  __device__ __forceinline__ Four(const float (*tile)[16][20], int lm, int lq) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = tile[0][4 * lq + j][lm];
+  }
 };
 template <> struct Four<bf16> {
   typedef bf16x4 Other;
   bf16x8 v;
   Four() = default;
-  __device__ __forceinline__ bf16x4 high() const { return bf16x4{v[0], v[1], v[2], v[3]}; }
-  __device__ __forceinline__ bf16x4 low() const { return bf16x4{v[4], v[5], v[6], v[7]}; }
-  __device__ __forceinline__ Four(bf16x4 h, bf16x4 l) : v{h[0], h[1], h[2], h[3], l[0], l[1], l[2], l[3]} {}
+  __device__ __forceinline__ void put(bf16 (*tile)[16][16], int lm, int lq) const {
+    *(bf16x4*)&tile[0][lm][4 * lq] = bf16x4{v[0], v[1], v[2], v[3]};
+    *(bf16x4*)&tile[1][lm][4 * lq] = bf16x4{v[4], v[5], v[6], v[7]};
+  }
+  // (lanes 4 e + q of 16 name the address of classes 4 q .. of token e, and get a class each, four tokens of it)
+  __device__ __forceinline__ Four(bf16 (*tile)[16][16], int lm, int lq) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef s16x4 __attribute__((address_space(3))) * at;
+    const bf16x4 h = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)&tile[0][4 * lq + lm / 4][lm % 4 * 4]));
+    const bf16x4 l = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)&tile[1][4 * lq + lm / 4][lm % 4 * 4]));
+    v = bf16x8{h[0], h[1], h[2], h[3], l[0], l[1], l[2], l[3]};
+  }
   __device__ __forceinline__ explicit Four(f32x4 g) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -302,13 +359,12 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(const float* __restri
 #pragma unroll
     for (int i = 0; i < K; ++i) acc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // G by rows (four classes of token l % 16) and by columns (four tokens of class l % 16), 256 MB at most: places in 32 bits
-  // (by columns in bf16: from the rows' terms, through LDS and its transposing reads)
-  constexpr bool TURN = sizeof(T) == 2;
-  __shared__ __attribute__((aligned(16))) bf16 turn[TURN ? 4 : 1][TURN ? TILES : 1][2][16][16];
-  const unsigned ld = (unsigned)ldz, by_row = lm * ld + 4 * lq, by_col = 4 * lq * ld + lm;
+  // G by rows (four classes of token l % 16), 256 MB at most: places in 32 bits; by columns (four tokens of class l % 16) through LDS, in bf16 with its transposing reads
+  constexpr int TERMS = sizeof(T) == 2 ? 2 : 1, LD = sizeof(T) == 2 ? 16 : 20;
+  __shared__ __attribute__((aligned(16))) T turn[4][TILES][TERMS][16][LD];
+  const unsigned by_row = lm * (unsigned)ldz + 4 * lq;
   vec nb[4];
-  f32x4 nr[TILES], nc[TURN ? 1 : TILES];
+  f32x4 nr[TILES];
   auto fetch = [&](int v0) __attribute__((always_inline)) {        // (a step ahead)
     if (v0 >= end) return;
     if (want_dx) {
@@ -321,11 +377,6 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(const float* __restri
     }
 #pragma unroll
     for (int t = 0; t < TILES; ++t) nr[t] = *(const f32x4*)(G + (size_t)t * 16 * ldz + (by_row + (unsigned)v0));
-    if constexpr (!TURN)
-#pragma unroll
-    for (int t = 0; t < TILES; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) nc[t][j] = (G + (size_t)(t * 16 + j) * ldz)[by_col + (unsigned)v0];
   };
   fetch(begin + wave * 16);
   for (int v0 = begin + wave * 16; v0 < end; v0 += STEP) {
@@ -336,23 +387,17 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(const float* __restri
 #pragma unroll
       for (int j = 0; j < 4; ++j) b[i][j] = nb[j][i];
     Four<T> row[TILES];
-    f32x4 col[TURN ? 1 : TILES], sum = {0.f, 0.f, 0.f, 0.f};
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     if constexpr (LOGITS)
 #pragma unroll
       for (int t = 0; t < TILES; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          nr[t][j] = gradient(nr[t][j], t * 16 + lm, v + j);
-          if constexpr (!TURN) nc[t][j] = gradient(nc[t][j], t * 16 + 4 * lq + j, v0 + lm);
-        }
+        for (int j = 0; j < 4; ++j) nr[t][j] = gradient(nr[t][j], t * 16 + lm, v + j);
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
       row[t] = Four<T>(nr[t]);
       sum += nr[t];
-      if constexpr (TURN) {
-        *(bf16x4*)&turn[wave][t][0][lm][4 * lq] = row[t].high();
-        *(bf16x4*)&turn[wave][t][1][lm][4 * lq] = row[t].low();
-      } else col[t] = nc[t];
+      row[t].put(turn[wave][t], lm, lq);
     }
     fetch(v0 + STEP);
     if (want_dx)
@@ -364,21 +409,14 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(const float* __restri
       f32x4 out[K];
 #pragma unroll
       for (int i = 0; i < K; ++i) out[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (TURN) wave_fence();
+      wave_fence();
 #pragma unroll
       for (int t = 0; t < TILES; ++t) {
-        Four<T> g;
-        if constexpr (TURN) {
-          // (lanes 4 e + q of 16 name the address of classes 4 q .. of token e, and get a class each, four tokens of it)
-          typedef short s16x4 __attribute__((ext_vector_type(4)));
-          typedef s16x4 __attribute__((address_space(3))) * at;
-          g = Four<T>(__builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)&turn[wave][t][0][4 * lq + lm / 4][lm % 4 * 4])),
-                      __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)&turn[wave][t][1][4 * lq + lm / 4][lm % 4 * 4])));
-        } else g = Four<T>(col[t]);
+        const Four<T> g(turn[wave][t], lm, lq);
 #pragma unroll
         for (int i = 0; i < K; ++i) out[i] = times(g, xb[t][i], out[i]);
       }
-      if constexpr (TURN) wave_fence();
+      wave_fence();
       auto put_row = [&](int r, bool all) __attribute__((always_inline)) {
         typename Some<K, TW>::vec o;
 #pragma unroll
@@ -432,25 +470,35 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(const float* __restri
   }
 }
 // dx from its parts, in order
-template <typename T> __global__ __launch_bounds__(256) void few_sums_kernel(const float* __restrict__ parts, int count, int64_t ldp, Tokens tk, int D, T* __restrict__ dx, int64_t lddx) {
-  const int d = (blockIdx.x * 64 + threadIdx.x % 64) * 4, n = blockIdx.y;
-  __shared__ f32x4 red[3][64];
+template <typename T> __global__ __launch_bounds__(1024) void few_sums_kernel(const float* __restrict__ parts, int count, int64_t ldp, Tokens tk, int D, T* __restrict__ dx, int64_t lddx) {
+  constexpr int WAVES = 16;
+  const int t = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, d = (blockIdx.x * WAVE + t) * 4, n = blockIdx.y;
+  __shared__ f32x4 red[WAVES][WAVE];
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (d < D)
 #pragma unroll 8
-    for (int p = threadIdx.x / 64; p < count; p += 4) v += *(const f32x4*)(parts + ((int64_t)p * tk.N + n) * ldp + d);
-  if (threadIdx.x >= 64) red[threadIdx.x / 64 - 1][threadIdx.x % 64] = v;
+    for (int p = wave; p < count; p += WAVES) v += *(const f32x4*)(parts + ((int64_t)p * tk.N + n) * ldp + d);
+  red[wave][t] = v;
   __syncthreads();
-  if (threadIdx.x >= 64 || d >= D) return;
-  v = ((v + red[0][threadIdx.x]) + red[1][threadIdx.x]) + red[2][threadIdx.x];
+  if (wave > 0 || d >= D) return;
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) v += red[i][t];
   if (!tk.counts(n)) v = f32x4{0.f, 0.f, 0.f, 0.f};                // (whatever w holds)
   put<4>(dx + n * lddx, d, D, typename Some<4, T>::vec{(T)v[0], (T)v[1], (T)v[2], (T)v[3]});
 }
 
 int64_t small_ldz(const LinearCe& a) { return small_ce_stride(a.N, a.V); }
+// (KW 1 where the classes fill the CUs and few features would leave wavefronts without any)
 template <typename T> void logits_as(const LinearCe& a, const Tokens& tk, float* z, hipStream_t s) {
-  if (a.N <= 16) small_logits_kernel<T, 1><<<dim3(over(a.V, 16), 1), LOGIT_WAVES * WAVE, 0, s>>>((const T*)a.x, a.ldx, (const T*)a.w, a.ldw, a.D, a.bias, tk, z, small_ldz(a));
-  else small_logits_kernel<T, 2><<<dim3(over(a.V, 16), over(a.N, 32)), LOGIT_WAVES * WAVE, 0, s>>>((const T*)a.x, a.ldx, (const T*)a.w, a.ldw, a.D, a.bias, tk, z, small_ldz(a));
+  auto go = [&](auto kernel, int classes, int tokens) {
+    kernel<<<dim3(over(a.V, classes), over(a.N, tokens)), LOGIT_WAVES * WAVE, 0, s>>>((const T*)a.x, a.ldx, (const T*)a.w, a.ldw, a.D, a.bias, tk, z, small_ldz(a));
+  };
+  const bool many = a.V >= 1 << 15, narrow = many && a.D <= 256;
+  if constexpr (sizeof(T) == 4)                    // (as many tokens beside bf16 rows of more features: tiles)
+    if (a.N > 32 && many && !narrow) return go(small_logits_kernel<T, 4, 8, 2>, 32, 64);
+  if (a.N <= 16) narrow ? go(small_logits_kernel<T, 1, 1, 1>, 128, 16) : many ? go(small_logits_kernel<T, 1, 8, 2>, 32, 16) : go(small_logits_kernel<T, 1, 8, 1>, 16, 16);
+  else if (a.N > 32 && narrow) go(small_logits_kernel<T, 4, 1, 1>, 128, 64);
+  else narrow ? go(small_logits_kernel<T, 2, 1, 1>, 128, 32) : many ? go(small_logits_kernel<T, 2, 8, 2>, 32, 32) : go(small_logits_kernel<T, 2, 8, 1>, 16, 32);
 }
 int few_tiles_of(int N) { return N > 32 ? 4 : N > 16 ? 2 : 1; }
 int few_wide(bool f32, int N) { return 16 * few_features(f32, few_tiles_of(N)); }
@@ -469,8 +517,8 @@ template <typename T, typename TW, bool LOGITS> void grads_as(const LinearCe& a,
   };
   if (a.N <= 16) go(few_grads_kernel<T, TW, 1, LOGITS>);
   else if (a.N <= 32) go(few_grads_kernel<T, TW, 2, LOGITS>);
-  else if constexpr (sizeof(T) == 2) go(few_grads_kernel<T, TW, 4, LOGITS>);
-  if (parts) few_sums_kernel<T><<<dim3(over(a.D, 256), a.N), 256, 0, s>>>(parts, ranges, ldp, tk, a.D, (T*)a.dx, a.lddx);
+  else go(few_grads_kernel<T, TW, 4, LOGITS>);
+  if (parts) few_sums_kernel<T><<<dim3(over(a.D, 256), a.N), 1024, 0, s>>>(parts, ranges, ldp, tk, a.D, (T*)a.dx, a.lddx);
 }
 template <bool LOGITS> void grads(const LinearCe& a, const Tokens& tk, const float* G, float* parts, hipStream_t s) {
   if (a.f32) grads_as<float, float, LOGITS>(a, tk, G, parts, s);
@@ -494,7 +542,8 @@ void small_ce_forward(const LinearCe& a, float* z, SmallGrad grad, hipStream_t s
   Tokens tk = tokens_of(a, grad == GRAD_WEIGHTED);
   logits_of(a, tk, z, s);
   if (grad == GRAD_WEIGHTED) tk.rows = 16 * few_tiles_of(a.N);
-  small_rows_kernel<<<tk.rows, 256, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad != GRAD_NONE);
+  if (a.V > 4096) small_rows_kernel<1024><<<tk.rows, 1024, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad != GRAD_NONE);
+  else small_rows_kernel<256><<<tk.rows, 256, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad != GRAD_NONE);
 }
 
 void small_ce_gradient(const LinearCe& a, bool weighted, float* G, hipStream_t s) {

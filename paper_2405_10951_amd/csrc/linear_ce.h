@@ -30,8 +30,8 @@ inline size_t small_ce_bytes(int N, int V) { return sizeof(float) * (size_t)N * 
 enum SmallGrad { GRAD_NONE, GRAD_PLAIN, GRAD_WEIGHTED };
 void small_ce_forward(const LinearCe& a, float* z, SmallGrad grad, hipStream_t s);      // grad: G in the logits' place
 void small_ce_gradient(const LinearCe& a, bool weighted, float* G, hipStream_t s);
-// N up to FEW_ROWS_...: G (or the logits) at the workspace's beginning, few_ce_bytes() more at few_parts_at()
-constexpr int FEW_ROWS_F32 = 32, FEW_ROWS_BF16 = 64;
+// N up to FEW_ROWS: G (or the logits) at the workspace's beginning, few_ce_bytes() more at few_parts_at()
+constexpr int FEW_ROWS = 64;
 size_t few_parts_at(int N, int V);
 size_t few_ce_bytes(bool f32, int N, int V, int D);
 // what G holds: nothing, logits, or G; fused: nothing, and the forward is wanted as well (of few_fused() classes)

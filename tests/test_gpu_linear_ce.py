@@ -117,6 +117,7 @@ def test_against_64_bits(env, N, D, V, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("N,D,V", [(16, 1024, 20000), (17, 65, 70000), (32, 512, 20003), (33, 65, 129), (48, 100, 3000), (49, 576, 20001), (64, 1000, 9000), (64, 4096, 1031),
+                                   (9, 300, 33000), (20, 300, 40000), (40, 300, 33001), (40, 100, 50000), (12, 100, 40000), (64, 2048, 300),
                                    (1, 64, 3), (7, 100, 256), (32, 768, 100), (40, 193, 200)])
 def test_few_rows_of_many_classes(env, N, D, V, dtype):
     torch, P = env
