@@ -641,7 +641,7 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
   uint32_t m[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) m[e] = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int r = r0 + threadIdx.x / SIDE; r < r1; r += ABOVE) {
     const typename Loose<T>::vec v = *(const typename Loose<T>::vec*)(x + r * j.ldx + col);
     const float by = weight_of(j.rw, r);

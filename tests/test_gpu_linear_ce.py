@@ -285,17 +285,18 @@ def test_nothing_to_do(env):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_replayed(env, dtype):
+@pytest.mark.parametrize("N,D,V", [(300, 192, 1000), (20, 192, 100), (40, 512, 20000), (700, 512, 1500)])
+def test_replayed(env, N, D, V, dtype):
     """recorded once, replayed on new inputs with the program's own work between"""
     torch, P = env
-    held = make(torch, 300, 192, 1000, dtype, 13)
+    held = make(torch, N, D, V, dtype, 13)
     P.bsr_linear_ce_forward_backward(*held[:3], bias=held[3], grad_scale=0.01)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         recorded = P.bsr_linear_ce_forward_backward(*held[:3], bias=held[3], grad_scale=0.01)
     for k in range(4):
-        now = make(torch, 300, 192, 1000, dtype, 14 + k)
+        now = make(torch, N, D, V, dtype, 14 + k)
         want = [t.clone() for t in P.bsr_linear_ce_forward_backward(*now[:3], bias=now[3], grad_scale=0.01)]
         for h, n in zip(held, now):
             h.copy_(n)
@@ -319,7 +320,7 @@ def test_two_streams_at_once(env):
         assert all(torch.equal(p, q) for g, w in zip(got, want) for p, q in zip(g, w))
 
 
-@pytest.mark.parametrize("N,D,V", [(9000, 64, 20000), (40, 512, 300000)])
+@pytest.mark.parametrize("N,D,V", [(9000, 64, 20000), (40, 512, 300000), (3, 64, 4300000), (60, 64, 1100000), (130, 72, 200000)])
 def test_several_pieces(env, N, D, V):
     """more classes than a piece holds, against torch in 64 bits on the GPU; the bound: that of a few elements' norms"""
     torch, P = env
