@@ -7,7 +7,7 @@
 // Numbers.  bf16 x and w are multiplied as they are and added in fp32.  G is kept in fp16, not bf16: it lies within -1 .. 1, and scaled by 2^14 its values keep 11 bits down to
 // 2^-28 and are off by 2^-39 at most below, where bf16 would keep 8; x and w join it in fp16, each feature (a row of the transposed operand) scaled by a power of two so that its
 // largest value lies in 2^14 .. 2^15, which is exact for bf16 values down to 2^-29 of the feature's largest.  The matrix instructions take both types at one rate.  fp32 operands are two fp16 terms each,
-// h + l with h = fp16(v), l = fp16(v - h), off by 2^-22 of the value, and the products h h, h l, l h, added in fp32, are three runs over the contraction index.
+// h + l with h = fp16(v), l = fp16(v - h), off by 2^-22 of the value, and the products h h, h l, l h are added in fp32, three k-tiles after one another for each of the operands.
 // Bound by the matrix unit's power where it is large: at 4096 x 4096 x 131072 bf16 a tile of 16 x 16 x 32 instructions runs at 1.7 - 1.8 GHz (32 x 32 x 16 at 1.46, 6 % slower in all), the forward at
 // 1350 TFLOP/s (3.25 ms), a piece's G at 1225 (450 us), both products of G at 1250 (880 us); transposing a piece takes 38 + 59 us.  2048 x 768 x 21841, gradients: maxima 12, transposing 17, G 100 (688 tiles of
 // 12 k-tiles on 256 CUs: beginnings and ends count as much as the products), products 137, sums 9.  333 x 1001 x 5003 fp32: packing 10, logits 26, joining 5, maxima 9, transposing 12, G 9, products 40, sums 4.
@@ -116,9 +116,9 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
     const f16* src = i < AL ? A : B;
     int k = kt0 + kt;
     if constexpr (SEG == 3) {
-      const int seg = (k >= g.nk) + (k >= 2 * g.nk);
+      const int seg = (unsigned)k % 3;             // (the three products of a k-tile follow one another: the caches still hold the terms that are read twice)
       src += i < AL ? (seg == 2 ? g.ta : 0) : (seg == 1 ? g.tb : 0);
-      k -= seg * g.nk;
+      k = (unsigned)k / 3;
     }
     // (a buffer: address of the tile in scalar registers, the row's bytes in a vector register, the k-tile's in a scalar one, and no arithmetic)
     unsigned char* dst = smem + st * STAGE + wave * 1024 + (i < AL ? i * RPI * 128 : BM * 128 + (i - AL) * RPI * 128);
