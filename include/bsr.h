@@ -604,7 +604,7 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
  *   workspace    device scratch of bsr_linear_ce_workspace_bytes() bytes, 256-byte aligned; what: 0 for the forward, 1 for the backward, 2 for both in one call
  * No result may touch an input, another result or the workspace.
  * bsr_linear_ce_forward_backward: one after the other, the second with what the first leaves in the workspace: packed operands, and logits where 16 MB hold them all.
- * Limits: rows up to 2^22, width up to 2^20, their product up to 2^33; classes up to 2^30.
+ * Limits: rows up to 2^22 (2^21 fp32), width up to 2^20, their product up to 2^33; classes up to 2^30.
  */
 size_t bsr_linear_ce_workspace_bytes(int32_t type, int64_t rows, int32_t width, int32_t classes, int32_t what);
 int32_t bsr_linear_ce_forward(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t type, int64_t rows, int32_t width, int32_t classes, const float* bias,

@@ -2013,7 +2013,7 @@ int32_t bsr_rmsnorm_backward(const void* dy, int64_t lddy, const void* x, int64_
 }
 
 static bool linear_ce_takes(int32_t type, int64_t rows, int32_t width, int32_t classes) {
-  return known_type(type) && rows >= 0 && rows <= MOST_TOKENS && width >= 1 && width <= WIDEST_CE && classes >= 1 && classes <= LONGEST_ROW && rows * width <= (int64_t)1 << 33;
+  return known_type(type) && rows >= 0 && rows <= (type == BSR_FP32 ? MOST_TOKENS / 2 : MOST_TOKENS) && width >= 1 && width <= WIDEST_CE && classes >= 1 && classes <= LONGEST_ROW && rows * width <= (int64_t)1 << 33;
 }
 // what: 0 forward, 1 backward, 2 both, with the statistics between them
 static size_t linear_ce_stats_at(bool f32, int32_t rows, int32_t width, int32_t classes) { return (linear_ce_both_bytes(f32, rows, width, classes) + 255) / 256 * 256; }

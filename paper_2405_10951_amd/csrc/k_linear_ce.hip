@@ -7,10 +7,12 @@
 // Numbers.  bf16 x and w are multiplied as they are and added in fp32.  G is kept in fp16, not bf16: it lies within -1 .. 1, and scaled by 2^14 its values keep 11 bits down to
 // 2^-28 and are off by 2^-39 at most below, where bf16 would keep 8; x and w join it in fp16, each feature (a row of the transposed operand) scaled by a power of two so that its
 // largest value lies in 2^14 .. 2^15, which is exact for bf16 values down to 2^-29 of the feature's largest.  The matrix instructions take both types at one rate.  fp32 operands are two fp16 terms each,
-// h + l with h = fp16(v), l = fp16(v - h), off by 2^-22 of the value, and the products h h, h l, l h are added in fp32, three k-tiles after one another for each of the operands.
+// h + l with h = fp16(v), l = fp16(v - h), off by 2^-22 of the value, and the products h h, l h, h l are added in fp32.  A k-tile holds both terms of 32 k: it is loaded
+// once for the three of them (333 x 1001 x 5003 loss and gradients 93 us; one product after another over the whole contraction 109, k-tile by k-tile 107).
 // Bound by the matrix unit's power where it is large: at 4096 x 4096 x 131072 bf16 a tile of 16 x 16 x 32 instructions runs at 1.7 - 1.8 GHz (32 x 32 x 16 at 1.46, 6 % slower in all), the forward at
 // 1350 TFLOP/s (3.25 ms), a piece's G at 1225 (450 us), both products of G at 1250 (880 us); transposing a piece takes 38 + 59 us.  2048 x 768 x 21841, gradients: maxima 12, transposing 17, G 100 (688 tiles of
-// 12 k-tiles on 256 CUs: beginnings and ends count as much as the products), products 137, sums 9.  333 x 1001 x 5003 fp32: packing 10, logits 26, joining 5, maxima 9, transposing 12, G 9, products 40, sums 4.
+// 12 k-tiles on 256 CUs: beginnings and ends count as much as the products), products 137, sums 9.  333 x 1001 x 5003 fp32: packing 11, logits 20, joining 5, maxima 9, transposing 13, G 9, products 35,
+// sums 4.
 // The row's weight g scales x in dw and the result in dx; rows whose label is absent or whose weight is 0 have G = 0 and, in the transposed x, zeros.
 #include <algorithm>
 
@@ -32,17 +34,19 @@ int up(int64_t n, int to) { return (int)((n + to - 1) / to * to); }
 int over(int64_t n, int by) { return (int)((n + by - 1) / by); }
 
 constexpr int BK = 64;
+// where element k of a row lies: of two terms 32 h and 32 l in turn
+template <int TERMS> __host__ __device__ constexpr int64_t spot(int64_t k, int term = 0) { return TERMS == 2 ? k / 32 * 64 + k % 32 + 32 * term : k; }
 constexpr int G_SHIFT = 14;                        // G is kept times 2^14
 
 // ------------------------------------------------------------------------------------------ the products
 enum Mode { STATS, GRAD };
 
-// C(m,n) = sum_k A(m,k) B(n,k): rows of 64-element k-tiles, whole ones, 16-byte aligned.  SEG = 3: two terms each, ta and tb elements apart, products h h, h l, l h.
+// C(m,n) = sum_k A(m,k) B(n,k): rows of 64-element k-tiles, whole ones, 16-byte aligned.  TERMS 2: a k-tile holds 32 k, first their h, then their l, and the products are h h, l h, h l.
 struct CeGemm {
   const void *A = nullptr, *B = nullptr;
-  int64_t lda = 0, ldb = 0, ta = 0, tb = 0;
-  int M = 0, N = 0, nk = 0;                        // nk: k-tiles of a term
-  int splits = 1, per = 0;                         // products of G: workgroups over the k-tiles of a tile, k-tiles (of all terms) of each
+  int64_t lda = 0, ldb = 0;
+  int M = 0, N = 0, nk = 0;                        // nk: k-tiles
+  int splits = 1, per = 0;                         // products of G: workgroups over the k-tiles of a tile, k-tiles of each
   const int *ea = nullptr, *eb = nullptr;          // powers of two of A's and B's rows, null: 0
   // STATS, GRAD: m is a token, n a class of the piece that begins at class v0
   const float* bias = nullptr;                     // of the piece
@@ -51,8 +55,8 @@ struct CeGemm {
   float2* parts = nullptr; float* zlabel = nullptr;                        // STATS: [tile of classes][M] maximum and sum; [M]
   float* z = nullptr; int64_t ldz = 0;             // STATS: the logits as well, [M][ldz], ldz whole fours; null: not wanted
   const float2* stats = nullptr; const float* row_grad = nullptr;          // GRAD: [M] maximum, log of the sum; weights or null
-  f16 *G = nullptr, *GT = nullptr;                 // GRAD: [terms][M][ldg], [terms][N][ldgt], of which kg and kgt columns are written, zero behind the last one; null: not wanted
-  int64_t ldg = 0, ldgt = 0, tg = 0, tgt = 0; int kg = 0, kgt = 0;
+  f16 *G = nullptr, *GT = nullptr;                 // GRAD: [M][ldg], [N][ldgt], of which kg and kgt columns (of one or both terms) are written, zero behind the last one; null: not wanted
+  int64_t ldg = 0, ldgt = 0; int kg = 0, kgt = 0;
   float* dbp = nullptr; int64_t ldd = 0;           // GRAD: [tile of tokens][ldd] sums of g G; null: not wanted
   // products of G
   float* part = nullptr; int64_t ldp = 0, tp = 0; bool add = false;        // [split][M][ldp] fp32 (of what was there as well)
@@ -89,15 +93,15 @@ __device__ __forceinline__ void tile_at(int t, int mt, int nt, int& m, int& n) {
 __device__ __forceinline__ int place(int row) { return row >> 1 & 7; }
 
 // Operands go straight into LDS (global_load_lds: rows of 8 chunks of 16 bytes, their order in LDS made by the address that a lane reads), NST stages of a
-// k-tile of 64, one barrier a k-tile.  A k-tile is 2 MI groups of NI matrix instructions 16 x 16 x 32, each group with one fragment of A: fragments of A come DIST groups ahead through a ring of
-// RING, those of B a k-step ahead.  DIST groups before the k-tile's end every wavefront has read all of it: there is the barrier, and behind it the loads of k-tile kt + NST go out into its stage, one or two a group.
+// k-tile of 64, one barrier a k-tile.  A k-tile is 2 MI groups (of two terms: 3 MI, h and l of each with B's h, then h again with B's l) of NI matrix instructions 16 x 16 x 32, each group with one fragment
+// of A: fragments of A come DIST groups ahead through a ring of RING, those of B a half ahead.  DIST groups before the k-tile's end every wavefront has read all of it: there is the barrier, and behind it the loads of k-tile kt + NST go out into its stage, one or two a group.
 // 16 x 16 x 32, not 32 x 32 x 16: under full load the clock is what the power allows, and the smaller tile, which touches half as many accumulators a product, draws less.
 // The operands are swapped (B's rows first): accumulators hold transposed tiles, element r of acc[mi][ni] is row mi 16 + lane % 16, column ni 16 + 4 (lane / 16) + r.
-template <class S, bool F16, int SEG>
+template <class S, bool F16, int TERMS>
 __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt0, int nk, unsigned char* smem, f32x4 (&acc)[S::MI][S::NI]) {
-  constexpr int BM = S::BM, WN = S::WN, NST = S::NST, TM = S::TM, TN = S::TN, MI = S::MI, NI = S::NI, NG = 2 * MI;
+  constexpr int BM = S::BM, WN = S::WN, NST = S::NST, TM = S::TM, TN = S::TN, MI = S::MI, NI = S::NI, HALF = TERMS * MI, NG = HALF + MI;
   constexpr int RPI = S::NT / 8, AL = BM / RPI, BL = S::BN / RPI, LPT = AL + BL, STAGE = (BM + S::BN) * 128;
-  constexpr int RING = 4, DIST = 3;
+  constexpr int RING = NG % 4 == 0 ? 4 : 3, DIST = RING - 1;
   static_assert(BM % RPI == 0 && S::BN % RPI == 0 && RPI % 16 == 0, "a load instruction covers whole groups of 16 rows");
   static_assert(NST >= 2 && NST <= 4 && (NST - 1) * LPT <= 60, "vmcnt has 6 bits");
   static_assert(NG % RING == 0 && NG > DIST, "the ring comes round with the k-tile");
@@ -114,12 +118,7 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
   auto issue1 = [&](auto I, int kt, int st) __attribute__((always_inline)) {
     constexpr int i = decltype(I)::value;
     const f16* src = i < AL ? A : B;
-    int k = kt0 + kt;
-    if constexpr (SEG == 3) {
-      const int seg = (unsigned)k % 3;             // (the three products of a k-tile follow one another: the caches still hold the terms that are read twice)
-      src += i < AL ? (seg == 2 ? g.ta : 0) : (seg == 1 ? g.tb : 0);
-      k = (unsigned)k / 3;
-    }
+    const int k = kt0 + kt;
     // (a buffer: address of the tile in scalar registers, the row's bytes in a vector register, the k-tile's in a scalar one, and no arithmetic)
     unsigned char* dst = smem + st * STAGE + wave * 1024 + (i < AL ? i * RPI * 128 : BM * 128 + (i - AL) * RPI * 128);
 #ifdef __HIP_DEVICE_COMPILE__
@@ -136,9 +135,12 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
   const int lr = lane & 15, lq = lane >> 4, sw = place(lr);
   const unsigned char *fa = smem + (wm * TM + lr) * 128, *fb = smem + BM * 128 + (wn * TN + lr) * 128;
   f16x8 a[RING], b[2][NI];
-  // group gi (0 .. 2 MI - 1) of a k-tile takes A's fragment (ks, mi) = (gi / MI, gi % MI)
+  // group gi (0 .. NG - 1) of a k-tile: half of B, 32 k of A (or its term), rows of A
+  auto half_of = [](int gi) constexpr { return gi >= HALF; };
+  auto ks_of = [](int gi) constexpr { return TERMS == 2 ? (gi < HALF ? gi % 2 : 0) : gi / MI; };
+  auto mi_of = [](int gi) constexpr { return gi >= HALF ? gi - HALF : TERMS == 2 ? gi / 2 : gi; };
   auto read_a = [&](auto GI, int st) __attribute__((always_inline)) {
-    constexpr int gi = decltype(GI)::value, ks = gi / MI, mi = gi % MI;
+    constexpr int gi = decltype(GI)::value, ks = ks_of(gi), mi = mi_of(gi);
     a[gi % RING] = *(const f16x8*)(fa + st * STAGE + mi * 16 * 128 + (((ks * 4 + lq) ^ sw) << 4));
   };
   auto read_b = [&](auto KS, auto J, int st) __attribute__((always_inline)) {
@@ -156,7 +158,7 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
   auto ktile = [&](auto EARLY, auto VMW, int kt, int st, int stn, int stl, int rem) __attribute__((always_inline)) {
     constexpr int vmw = decltype(VMW)::value, LAST = NG - DIST;
     sfor<NG>([&](auto GI) __attribute__((always_inline)) {
-      constexpr int gi = decltype(GI)::value, ks = gi / MI, mi = gi % MI;
+      constexpr int gi = decltype(GI)::value, ks = half_of(gi), mi = mi_of(gi);
       if constexpr (gi == LAST) {
         wait_lgkmcnt0();
         if constexpr (vmw >= 0) wait_vmcnt<vmw>();
@@ -175,13 +177,13 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
           else read_a(IC<gi + DIST - NG>{}, stn);
         }
         // the next k-step's fragments of B: a few a group, those of the next k-tile right behind the barrier, those of this one's second half in the middle of its first
-        constexpr int at = ks == 0 ? gi - (MI / 2 - 1) : gi - (LAST > MI ? LAST : MI);
+        constexpr int at = ks == 0 ? gi - (HALF / 2 - 1) : gi - (LAST > HALF ? LAST : HALF);
         constexpr int BPG = (NI + DIST - 1) / DIST, jb = BPG * at + j;
-        if constexpr (j < BPG && at >= 0 && jb < NI && (ks == 1 || MI >= 4)) {
+        if constexpr (j < BPG && at >= 0 && jb < NI && (ks == 1 || HALF >= 4)) {
           if constexpr (ks == 0) read_b(IC<1>{}, IC<jb>{}, st);
           else read_b(IC<0>{}, IC<jb>{}, stn);
         }
-        if constexpr (MI < 4 && ks == 0 && gi == 0 && j == NI - 1) sfor<NI>([&](auto Q) __attribute__((always_inline)) { read_b(IC<1>{}, Q, st); });
+        if constexpr (HALF < 4 && ks == 0 && gi == 0 && j == NI - 1) sfor<NI>([&](auto Q) __attribute__((always_inline)) { read_b(IC<1>{}, Q, st); });
         BSR_SCHED_FENCE();
       });
       if constexpr (gi >= LAST) {
@@ -335,9 +337,9 @@ template <int N> __device__ __forceinline__ float lanes16_sums(float (&v)[N]) {
 }
 
 // Backward: the tile as G, in fp16 times 2^14, rows of 32 tokens at a time through a patch of LDS, from which rows are read as they lie and, with the transposing reads, columns
-template <class S, bool F16, int SEG, bool DB>
+template <class S, bool F16, int TERMS, bool DB>
 __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S::NI], int m0, int n0, int tm, unsigned char* smem) {
-  constexpr int NI = S::NI, TERMS = SEG == 3 ? 2 : 1, TERM = 32 * S::LDR;
+  constexpr int NI = S::NI, TERM = 32 * S::LDR;
   const Wave<S> w(m0, n0);
   const Classes<S, F16> cl(g, w);
   unsigned char* patch = w.patch(smem);
@@ -392,18 +394,16 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
       if (g.G) {
         constexpr int CPR = S::TN / 8, RPP = 64 / CPR;           // 16-byte chunks of a patch row, rows at a time
         const int k = w.lane % CPR, n = w.col0 + k * 8;
-        f16* to = g.G + term * g.tg;
 #pragma unroll
         for (int p = 0; p < 32 / RPP; ++p) {
           const int r = p * RPP + w.lane / CPR, row = first + r;
-          if (row < g.M && n < g.kg) *(f16x8*)(to + (int64_t)row * g.ldg + n) = *(const f16x8*)(patch + term * TERM + r * S::LDR + k * 16);
+          if (row < g.M && n < g.kg) *(f16x8*)(g.G + (int64_t)row * g.ldg + spot<TERMS>(n, term)) = *(const f16x8*)(patch + term * TERM + r * S::LDR + k * 16);
         }
       }
       if (g.GT) {
         // 16 lanes read 4 tokens x 16 classes (lane 4 e + q names the address of classes 4 q .. of token e) and get a class each, four tokens of it; two such reads are 16 bytes of GT
         const int j = w.lane & 15, octet = w.lane >> 4, token = first + octet * 8;
         const unsigned char* from = patch + term * TERM + (octet * 8 + (j >> 2)) * S::LDR + (j & 3) * 8;
-        f16* to = g.GT + term * g.tgt;
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef short s16x8 __attribute__((ext_vector_type(8)));
 #pragma unroll
@@ -411,7 +411,7 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
           const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(from + cb * 32));
           const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(from + cb * 32 + 4 * S::LDR));
           const int n = w.col0 + cb * 16 + j;
-          if (n < g.N && token < g.kgt) *(s16x8*)(to + (int64_t)n * g.ldgt + token) = s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          if (n < g.N && token < g.kgt) *(s16x8*)(g.GT + (int64_t)n * g.ldgt + spot<TERMS>(token, term)) = s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         }
       }
     }
@@ -440,21 +440,21 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
   }
 }
 
-template <class S, Mode MODE, bool F16, int SEG, bool DB>
+template <class S, Mode MODE, bool F16, int TERMS, bool DB>
 __global__ __launch_bounds__(S::NT, S::wavefronts) void ce_logits_kernel(CeGemm g, int mt, int nt) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int tm, tn;
   tile_at(xcd_remap(blockIdx.x, gridDim.x), mt, nt, tm, tn);
   const int m0 = tm * S::BM, n0 = tn * S::BN;
   f32x4 acc[S::MI][S::NI];
-  multiply<S, F16, SEG>(g, m0, n0, 0, m0 < g.M ? SEG * g.nk : 0, smem, acc);      // (tokens that only fill GT's last k-tile: zeros)
+  multiply<S, F16, TERMS>(g, m0, n0, 0, m0 < g.M ? g.nk : 0, smem, acc);      // (tokens that only fill GT's last k-tile: zeros)
   __syncthreads();
   if constexpr (MODE == STATS) end_stats<S, F16>(g, acc, m0, n0, tn, smem);
-  else end_grad<S, F16, SEG, DB>(g, acc, m0, n0, tm, smem);
+  else end_grad<S, F16, TERMS, DB>(g, acc, m0, n0, tm, smem);
 }
 
 // Up to two products of G in one launch (a, then b, na workgroups of the first): dx and dw of a piece fill the CUs together
-template <class S, int SEG>
+template <class S, int TERMS>
 __global__ __launch_bounds__(S::NT, 1) void ce_grads_kernel(CeGemm a, CeGemm b, int na) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const bool first = (int)blockIdx.x < na;
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(S::NT, 1) void ce_grads_kernel(CeGemm a, CeGemm b, 
   tile_at(id - split * mt * nt, mt, nt, tm, tn);
   const int m0 = tm * S::BM, n0 = tn * S::BN, kt0 = split * g.per;
   f32x4 acc[S::MI][S::NI];
-  multiply<S, true, SEG>(g, m0, n0, kt0, min(g.per, SEG * g.nk - kt0), smem, acc);
+  multiply<S, true, TERMS>(g, m0, n0, kt0, min(g.per, g.nk - kt0), smem, acc);
   __syncthreads();
   const Wave<S> w(m0, n0);
   unsigned char* patch = w.patch(smem);
@@ -526,8 +526,8 @@ __device__ __forceinline__ uint32_t bits_if_finite(float v) {
 }
 
 // x, w or both (a launch handles up to two; the first `blocks` workgroups the first)
-struct PackJob { const void* x = nullptr; int64_t ldx = 0, rows = 0; uint16_t* to = nullptr; int64_t term = 0; int* exps = nullptr; };
-// rows of D values to rows of whole k-tiles: bf16 as they are, a thread 8 of them, fp32 in two fp16 terms (`term` elements apart) with a power of two a row, LANES lanes a row
+struct PackJob { const void* x = nullptr; int64_t ldx = 0, rows = 0; uint16_t* to = nullptr; int* exps = nullptr; };
+// rows of D values to rows of whole k-tiles: bf16 as they are, a thread 8 of them, fp32 in two fp16 terms with a power of two a row, LANES lanes a row
 template <typename T, int LANES> int pack_blocks(int64_t rows, int Dp) { return sizeof(T) == 2 ? over(rows * (Dp / 8), 256) : over(rows, 256 / LANES); }
 template <typename T, int LANES>
 __global__ __launch_bounds__(256) void ce_pack_kernel(PackJob a, PackJob b, int blocks, int D, int Dp) {
@@ -551,7 +551,7 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(PackJob a, PackJob b, int 
     const int64_t m = (int64_t)block * (256 / LANES) + threadIdx.x / LANES;
     const bool there = m < j.rows;                 // (lanes of other rows take part in the maximum)
     const T* row = (const T*)j.x + (there ? m : j.rows - 1) * j.ldx;
-    uint16_t* out = j.to + m * Dp;
+    uint16_t* out = j.to + m * Dp * 2;
     // rows of up to 2048 values stay in registers, longer ones are read twice
     constexpr int KEEP = LANES == WAVE ? 8 : 1;
     f32x4 v[KEEP];
@@ -585,8 +585,8 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(PackJob a, PackJob b, int 
         h[i] = (f16)s;
         l[i] = (f16)(s - (float)h[i]);
       }
-      *(f16x4*)(out + k) = h;
-      *(f16x4*)(out + j.term + k) = l;
+      *(f16x4*)(out + spot<2>(k)) = h;
+      *(f16x4*)(out + spot<2>(k, 1)) = l;
     };
     if (kept) {
 #pragma unroll
@@ -608,13 +608,13 @@ __device__ __forceinline__ float weight_of(const RowWeights& w, int64_t m) {
 }
 __device__ __forceinline__ float weighted(float v, float by) { return by == 0.f ? 0.f : v * by; }
 
-// [rows, D] -> [terms][D][ld] fp16, a power of two each of the D rows; what lies between rows and ld is zero.  In two launches, each for x, w or both: the columns' maxima, `chunks`
+// [rows, D] -> [D][ld] fp16 in one or two terms, a power of two each of the D rows; what lies between rows and ld is zero.  In two launches, each for x, w or both: the columns' maxima, `chunks`
 // parts of the rows apart, then the rest
 struct TransposeJob {
   const void* x = nullptr; int64_t ldx = 0; int rows = 0; RowWeights rw;
   int per = 1, chunks = 0;                         // rows of a part; parts (0: no job)
   uint32_t* most = nullptr;                        // [chunks][D] bits of the largest finite |value|
-  f16* to = nullptr; int cols = 0; int64_t ld = 0, term = 0; int* exps = nullptr;           // cols of a row are written
+  f16* to = nullptr; int cols = 0; int64_t ld = 0; int* exps = nullptr;           // cols (of one or both terms) of a row are written
 };
 constexpr int CHUNKS = 64;
 
@@ -723,7 +723,7 @@ __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, Trans
       for (int i = threadIdx.x; i < 512; i += 256) {
         const int col = i / 8, k = i % 8 * 8;
         const uint32_t* from = (const uint32_t*)&tile[t][col][k];
-        if (c0 + col < D && m0 + k < j.cols) *(uint4*)(j.to + t * j.term + (int64_t)(c0 + col) * j.ld + m0 + k) = make_uint4(from[0], from[1], from[2], from[3]);
+        if (c0 + col < D && m0 + k < j.cols) *(uint4*)(j.to + (int64_t)(c0 + col) * j.ld + spot<TERMS>(m0 + k, t)) = make_uint4(from[0], from[1], from[2], from[3]);
       }
     __syncthreads();
   }
@@ -758,7 +758,7 @@ __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ 
       tile[a][b + i + j] = v[i + j] = there && n0 + b + i + j < g.N ? p[j] : 0.f;
     }
   }
-  auto put = [&](f16* to, int64_t term) __attribute__((always_inline)) {
+  auto put = [&](f16* row, int at) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 16; i += 8) {
       f16x8 h, l;
@@ -769,11 +769,11 @@ __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ 
         h[j] = hj;
         l[j] = lj;
       }
-      *(f16x8*)(to + i) = h;
-      if constexpr (TERMS == 2) *(f16x8*)(to + term + i) = l;
+      *(f16x8*)(row + spot<TERMS>(at + i)) = h;
+      if constexpr (TERMS == 2) *(f16x8*)(row + spot<TERMS>(at + i, 1)) = l;
     }
   };
-  if (g.G && m0 + a < g.M) put(g.G + (int64_t)(m0 + a) * g.ldg + n0 + b, g.tg);
+  if (g.G && m0 + a < g.M) put(g.G + (int64_t)(m0 + a) * g.ldg, n0 + b);
   if (!g.GT && !g.dbp) return;
   __syncthreads();
   float sum = 0.f;
@@ -783,7 +783,7 @@ __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ 
     const int m = m0 + b + i;
     sum += m < g.M && g.row_grad && v[i] != 0.f ? g.row_grad[m] * v[i] : v[i];
   }
-  if (g.GT && n0 + a < g.N) put(g.GT + (int64_t)(n0 + a) * g.ldgt + m0 + b, g.tgt);
+  if (g.GT && n0 + a < g.N) put(g.GT + (int64_t)(n0 + a) * g.ldgt, m0 + b);
   if (g.dbp) {
     sum += __shfl_xor(sum, 1);
     sum += __shfl_xor(sum, 2);
@@ -885,30 +885,33 @@ enum { LARGE, SMALL, MID, FEW, SHORT };
 int rows_of(int shape) { return shape == FEW ? Few::BM : shape == SHORT ? Short::BM : shape == MID ? Mid::BM : shape == SMALL ? Small::BM : Large::BM; }
 int cols_of(int shape) { return shape == FEW ? Few::BN : shape == SHORT ? Short::BN : shape == MID ? Mid::BN : shape == SMALL ? Small::BN : Large::BN; }
 
-template <class S, Mode MODE, bool F16, int SEG, bool DB> void launch_logits(const CeGemm& g, int rows, hipStream_t s) {
-  with_lds<ce_logits_kernel<S, MODE, F16, SEG, DB>>(S::lds);
+template <class S, Mode MODE, bool F16, int TERMS, bool DB> void launch_logits(const CeGemm& g, int rows, hipStream_t s) {
+  with_lds<ce_logits_kernel<S, MODE, F16, TERMS, DB>>(S::lds);
   const int mt = over(rows, S::BM), nt = over(g.N, S::BN);
-  ce_logits_kernel<S, MODE, F16, SEG, DB><<<mt * nt, S::NT, S::lds, s>>>(g, mt, nt);
+  ce_logits_kernel<S, MODE, F16, TERMS, DB><<<mt * nt, S::NT, S::lds, s>>>(g, mt, nt);
 }
 // rows: those that tiles have to cover
-template <Mode MODE, bool F16, int SEG, bool DB> void logits(int shape, const CeGemm& g, int rows, hipStream_t s) {
-  if (shape == FEW) launch_logits<Few, MODE, F16, SEG, DB>(g, rows, s);
-  else if (shape == SHORT) launch_logits<Short, MODE, F16, SEG, DB>(g, rows, s);
-  else if (shape == MID) launch_logits<Mid, MODE, F16, SEG, DB>(g, rows, s);
-  else if (shape == SMALL) launch_logits<Small, MODE, F16, SEG, DB>(g, rows, s);
-  else launch_logits<std::conditional_t<MODE == STATS, LargeForward, Large>, MODE, F16, SEG, DB>(g, rows, s);
+template <Mode MODE, bool F16, int TERMS, bool DB> void logits(int shape, const CeGemm& g, int rows, hipStream_t s) {
+  if (shape == FEW) launch_logits<Few, MODE, F16, TERMS, DB>(g, rows, s);
+  else if (shape == SHORT) launch_logits<Short, MODE, F16, TERMS, DB>(g, rows, s);
+  else if (shape == MID) launch_logits<Mid, MODE, F16, TERMS, DB>(g, rows, s);
+  else if (shape == SMALL) launch_logits<Small, MODE, F16, TERMS, DB>(g, rows, s);
+  else launch_logits<std::conditional_t<MODE == STATS, LargeForward, Large>, MODE, F16, TERMS, DB>(g, rows, s);
 }
-template <class S, int SEG> void launch_grads(const CeGemm& a, const CeGemm& b, hipStream_t s) {
+template <class S, int TERMS> void launch_grads(const CeGemm& a, const CeGemm& b, hipStream_t s) {
   auto blocks = [](const CeGemm& g) { return g.A ? over(g.M, S::BM) * over(g.N, S::BN) * g.splits : 0; };
-  with_lds<ce_grads_kernel<S, SEG>>(S::lds);
-  ce_grads_kernel<S, SEG><<<blocks(a) + blocks(b), S::NT, S::lds, s>>>(a, b, blocks(a));
+  with_lds<ce_grads_kernel<S, TERMS>>(S::lds);
+  ce_grads_kernel<S, TERMS><<<blocks(a) + blocks(b), S::NT, S::lds, s>>>(a, b, blocks(a));
 }
 
 // Models of a launch, in us: a workgroup, or the two of a shape that a CU takes at once, has a CU for start + k-tiles * tile.  (Short against large, forward: 600 x 100 x 100000 bf16 60 against 75 us, 2000 x 512 x
 // 50000 128 against 136, 2048 x 768 x 21841 80 against 79)
 struct Cost { double tile, start; int at_once; };
 constexpr Cost COST[5] = {{1.7, 8, 1}, {0.6, 4, 1}, {0.4, 4, 1}, {0.5, 4, 1}, {1.03, 2.3, 2}};
-int logits_shape(int64_t M, int64_t N, int kt) {
+// of a k-tile, which two terms make longer; of a row of so many times 64 features
+double tile_work(bool f32) { return f32 ? 1.25 : 1; }
+double logits_work(bool f32, int kt) { return kt * (f32 ? 2 : 1) * tile_work(f32); }
+int logits_shape(int64_t M, int64_t N, double kt) {
   int best = SMALL;
   double least = 1e30;
   for (int shape = LARGE; shape <= SHORT; ++shape) {
@@ -921,7 +924,7 @@ int logits_shape(int64_t M, int64_t N, int kt) {
 }
 // shape and workgroups over k of dx (M x D, kx k-tiles) and dw (n x D, kw k-tiles) together; either may be missing (0 k-tiles).  dx's workgroups go first
 struct Split { int shape, x, w; };
-Split grads_split(int64_t M, int64_t n, int64_t D, int kx, int kw) {
+Split grads_split(int64_t M, int64_t n, int64_t D, int kx, int kw, double work) {
   Split best = {SMALL, 1, 1};
   double least = 1e30;
   for (int shape = LARGE; shape <= SMALL; ++shape) {
@@ -931,7 +934,7 @@ Split grads_split(int64_t M, int64_t n, int64_t D, int kx, int kw) {
       if (x > 1 && (kx < 4 * x || tx * x > 1024)) break;
       for (int w = 1; w <= (kw ? 16 : 1); ++w) {
         if (w > 1 && (kw < 4 * w || tw * w > 1024)) break;
-        const double a = c.start + over(kx, x) * c.tile, b = c.start + over(kw, w) * c.tile;
+        const double a = c.start + over(kx, x) * c.tile * work, b = c.start + over(kw, w) * c.tile * work;
         // dx in rounds over the CUs, dw on those that are free
         const int64_t nx = tx * x, nw = tw * w, full = nx / 256, rest = nx % 256;
         double us = full * a + (rest ? a : 0);
@@ -999,9 +1002,8 @@ struct Plan {
     xT = take((size_t)2 * T * D * Np); exT = take(sizeof(int) * (size_t)D);
     wT = take((size_t)2 * T * D * Vc); ewT = take(sizeof(int) * (size_t)D);
     mostx = take(sizeof(uint32_t) * (size_t)CHUNKS * D); mostw = take(sizeof(uint32_t) * (size_t)CHUNKS * D);
-    const int seg = T == 2 ? 3 : 1;
     // (for the first piece; the others take as many workgroups over k)
-    split = grads_split(N, std::min(V, Vc), D, std::min(Vc, up(V, BK)) / BK * seg, Np / BK * seg);
+    split = grads_split(N, std::min(V, Vc), D, std::min(Vc, up(V, BK)) / BK * T, Np / BK * T, tile_work(f32));
     dxp = take(sizeof(float) * (size_t)split.x * N * Dq);
     dwp = take(split.w > 1 ? sizeof(float) * (size_t)split.w * Vc * Dq : 0);
     dbp = take(sizeof(float) * (size_t)over(Np, 32) * ldd);
@@ -1009,15 +1011,15 @@ struct Plan {
   }
 };
 
-// (255 rows of a tile, and k behind them, are addressed in 32 bits; so are those of what is packed and transposed here: rows of 2^20 features or 2^22 tokens at most)
+// (255 rows of a tile, and k behind them, are addressed in 32 bits; so are those of what is packed and transposed here: rows of 2^20 features or 2^22 tokens at most, of two terms of 2^20 or 2^21)
 bool whole_rows(const void* p, int64_t ld, int D) { return D % BK == 0 && ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld <= 1 << 22; }
 
 // An operand of the logits: as it lies, or packed by what `job` then describes
-struct Rows { const void* p; int64_t ld, term; const int* exps; };
+struct Rows { const void* p; int64_t ld; const int* exps; };
 Rows rows_operand(const void* p, int64_t ld, bool f32, int64_t rows, int Dp, void* packed, int* exps, bool as_it_lies, PackJob& job) {
-  if (as_it_lies) return {p, ld, 0, nullptr};
-  job.x = p; job.ldx = ld; job.rows = rows; job.to = (uint16_t*)packed; job.term = rows * Dp; job.exps = exps;
-  return {packed, Dp, job.term, f32 ? exps : nullptr};
+  if (as_it_lies) return {p, ld, nullptr};
+  job.x = p; job.ldx = ld; job.rows = rows; job.to = (uint16_t*)packed; job.exps = exps;
+  return {packed, f32 ? 2 * Dp : Dp, f32 ? exps : nullptr};
 }
 void pack(const PackJob& a, const PackJob& b, bool f32, int D, int Dp, hipStream_t s) {
   if (a.rows + b.rows == 0) return;
@@ -1044,15 +1046,15 @@ void set_chunks(TransposeJob& j) {
 }
 
 // whether tiles of the logits would leave most CUs idle, each behind a long chain of k-tiles
-bool few_tiles(int N, int V, int kt) {
+bool few_tiles(int N, int V, double kt) {
   const int shape = logits_shape(N, V, kt);
   return (int64_t)over(N, rows_of(shape)) * over(V, cols_of(shape)) < 64;
 }
 
 CeGemm logits_gemm(const LinearCe& a, const Plan& p, const Rows& x, const Rows& w, int v0, int n) {
   CeGemm g;
-  g.A = x.p; g.lda = x.ld; g.ta = x.term; g.ea = x.exps; g.B = w.p; g.ldb = w.ld; g.tb = w.term; g.eb = w.exps;
-  g.M = a.N; g.N = n; g.nk = p.Dp / BK; g.bias = a.bias ? a.bias + v0 : nullptr; g.labels = a.labels; g.v0 = v0; g.classes = a.V;
+  g.A = x.p; g.lda = x.ld; g.ea = x.exps; g.B = w.p; g.ldb = w.ld; g.eb = w.exps;
+  g.M = a.N; g.N = n; g.nk = (a.f32 ? 2 : 1) * p.Dp / BK; g.bias = a.bias ? a.bias + v0 : nullptr; g.labels = a.labels; g.v0 = v0; g.classes = a.V;
   return g;
 }
 
@@ -1073,7 +1075,7 @@ struct Way {
     x = !a.f32 && whole_rows(a.x, a.ldx, a.D);
     w = !a.f32 && whole_rows(a.w, a.ldw, a.D);
     little = is_small(a.N, a.D, a.V) &&
-             ((double)a.N * a.D * a.V <= SMALL_WORK && (!x || !w) || few_tiles(a.N, a.V, over(a.D, BK) * (a.f32 ? 3 : 1)));
+             ((double)a.N * a.D * a.V <= SMALL_WORK && (!x || !w) || few_tiles(a.N, a.V, logits_work(a.f32, over(a.D, BK))));
     few = is_few(a.N, a.V) && (always_few(a.f32, a.N) || w || little);
   }
 };
@@ -1099,8 +1101,8 @@ static void forward_with(const LinearCe& a, float* z, bool packs, hipStream_t s)
     pack(v0 == 0 ? px : PackJob(), pw, a.f32, a.D, p.Dp, s);
     CeGemm g = logits_gemm(a, p, x, w, v0, n);
     g.parts = (float2*)(ws + p.parts); g.zlabel = (float*)(ws + p.zlabel); g.z = z; g.ldz = small_ce_stride(a.N, a.V);
-    const int shape = logits_shape(a.N, n, g.nk * (a.f32 ? 3 : 1));
-    if (a.f32) logits<STATS, true, 3, false>(shape, g, a.N, s);
+    const int shape = logits_shape(a.N, n, g.nk * tile_work(a.f32));
+    if (a.f32) logits<STATS, true, 2, false>(shape, g, a.N, s);
     else logits<STATS, false, 1, false>(shape, g, a.N, s);
     if (a.loss || a.stats)
       ce_join_kernel<<<over(a.N, 16), 1024, 0, s>>>(g.parts, over(n, cols_of(shape)), a.N, (float2*)(ws + p.run), v0 == 0, v0 + n == a.V, g.zlabel, a.labels, a.V, a.loss, (float2*)a.stats);
@@ -1121,7 +1123,7 @@ enum Ready { NOTHING, PACKED, TURNED, KEPT };
 template <typename T>
 void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) {
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int SEG = F32 ? 3 : 1;
+  constexpr int TERMS = F32 ? 2 : 1;
   const Plan p(F32, a.N, a.D, a.V, true);
   char* ws = (char*)a.workspace;
   const Way way(a);
@@ -1140,35 +1142,35 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
     TransposeJob tx, tw;
     if (a.dw && begin) {
       tx.x = a.x; tx.ldx = a.ldx; tx.rows = a.N; tx.rw.labels = a.labels; tx.rw.row_grad = a.row_grad; tx.rw.classes = a.V;
-      tx.most = (uint32_t*)(ws + p.mostx); tx.to = xT; tx.cols = p.Np; tx.ld = p.Np; tx.term = a.D * tx.ld; tx.exps = (int*)(ws + p.exT);
+      tx.most = (uint32_t*)(ws + p.mostx); tx.to = xT; tx.cols = p.Np; tx.ld = TERMS * p.Np; tx.exps = (int*)(ws + p.exT);
       set_chunks(tx);
     }
     if (a.dx) {
-      tw.x = wv; tw.ldx = a.ldw; tw.rows = n; tw.most = (uint32_t*)(ws + p.mostw); tw.to = wT; tw.cols = np; tw.ld = np; tw.term = a.D * tw.ld; tw.exps = (int*)(ws + p.ewT);
+      tw.x = wv; tw.ldx = a.ldw; tw.rows = n; tw.most = (uint32_t*)(ws + p.mostw); tw.to = wT; tw.cols = np; tw.ld = TERMS * np; tw.exps = (int*)(ws + p.ewT);
       set_chunks(tw);
     }
     transpose<T>(tx, tw, a.D, s);
     CeGemm g = logits_gemm(a, p, x, w, v0, n);
     g.stats = (const float2*)a.stats; g.row_grad = a.row_grad;
-    if (a.dx) { g.G = G; g.kg = np; g.ldg = np; g.tg = a.N * g.ldg; }
-    if (a.dw) { g.GT = GT; g.kgt = p.Np; g.ldgt = p.Np; g.tgt = n * g.ldgt; }
+    if (a.dx) { g.G = G; g.kg = np; g.ldg = TERMS * np; }
+    if (a.dw) { g.GT = GT; g.kgt = p.Np; g.ldgt = TERMS * p.Np; }
     if (a.db) { g.dbp = (float*)(ws + p.dbp); g.ldd = p.ldd; }
-    const int shape = logits_shape(a.N, n, g.nk * SEG), rows = a.dw ? p.Np : a.N, tall = turned ? 64 : rows_of(shape);
+    const int shape = logits_shape(a.N, n, g.nk * tile_work(F32)), rows = a.dw ? p.Np : a.N, tall = turned ? 64 : rows_of(shape);
     if (ready == KEPT) {
       ce_turn_kernel<F32 ? 2 : 1, true><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(z, small_ce_stride(a.N, a.V), g);
     } else if (turned) {
       if (ready != TURNED) small_ce_gradient(a, false, (float*)(ws + p.z), s);
       ce_turn_kernel<F32 ? 2 : 1, false><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>((const float*)(ws + p.z), small_ce_stride(a.N, a.V), g);
     } else if (a.db) {
-      logits<GRAD, F32, SEG, true>(shape, g, rows, s);
+      logits<GRAD, F32, TERMS, true>(shape, g, rows, s);
     } else {
-      logits<GRAD, F32, SEG, false>(shape, g, rows, s);
+      logits<GRAD, F32, TERMS, false>(shape, g, rows, s);
     }
     CeGemm ox, ow;
     SumJob sx, sw, sb;
     if (a.dx) {
-      ox.A = G; ox.lda = g.ldg; ox.ta = g.tg; ox.B = wT; ox.ldb = tw.ld; ox.tb = tw.term; ox.eb = tw.exps;
-      ox.M = a.N; ox.N = a.D; ox.nk = np / BK; ox.splits = p.split.x; ox.per = over(ox.nk * SEG, ox.splits);
+      ox.A = G; ox.lda = g.ldg; ox.B = wT; ox.ldb = tw.ld; ox.eb = tw.exps;
+      ox.M = a.N; ox.N = a.D; ox.nk = TERMS * np / BK; ox.splits = p.split.x; ox.per = over(ox.nk, ox.splits);
       ox.part = (float*)(ws + p.dxp); ox.ldp = p.Dq; ox.tp = (int64_t)a.N * p.Dq; ox.add = !begin;
       if (end) {
         sx.part = ox.part; sx.parts = ox.splits; sx.tp = ox.tp; sx.ldp = p.Dq; sx.rows = a.N; sx.cols = a.D; sx.scale = a.grad_scale; sx.rw.labels = a.labels; sx.rw.row_grad = a.row_grad; sx.rw.classes = a.V;
@@ -1176,8 +1178,8 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
       }
     }
     if (a.dw) {
-      ow.A = GT; ow.lda = g.ldgt; ow.ta = g.tgt; ow.B = xT; ow.ldb = p.Np; ow.tb = a.D * ow.ldb; ow.eb = (int*)(ws + p.exT);
-      ow.M = n; ow.N = a.D; ow.nk = p.Np / BK; ow.splits = p.split.w; ow.per = over(ow.nk * SEG, ow.splits); ow.scale = a.grad_scale;
+      ow.A = GT; ow.lda = g.ldgt; ow.B = xT; ow.ldb = TERMS * p.Np; ow.eb = (int*)(ws + p.exT);
+      ow.M = n; ow.N = a.D; ow.nk = TERMS * p.Np / BK; ow.splits = p.split.w; ow.per = over(ow.nk, ow.splits); ow.scale = a.grad_scale;
       char* dw = (char*)a.dw + v0 * a.lddw * (a.dw_f32 ? 4 : 2);
       if (ow.splits > 1) {
         ow.part = (float*)(ws + p.dwp); ow.ldp = p.Dq; ow.tp = (int64_t)n * p.Dq;
@@ -1188,8 +1190,8 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
       }
     }
     if (a.dx || a.dw) {
-      if (p.split.shape == SMALL) launch_grads<Small, SEG>(ox, ow, s);
-      else launch_grads<Large, SEG>(ox, ow, s);
+      if (p.split.shape == SMALL) launch_grads<Small, TERMS>(ox, ow, s);
+      else launch_grads<Large, TERMS>(ox, ow, s);
     }
     if (a.db) {
       sb.part = g.dbp; sb.parts = over(rows, tall); sb.tp = p.ldd; sb.rows = 1; sb.cols = n; sb.scale = a.grad_scale; sb.out = a.db + v0; sb.f32 = true; sb.blocks = over(over(n, 4), 256);

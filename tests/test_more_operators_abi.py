@@ -30,7 +30,7 @@ CB = dict(x=A, ldx=64, w=2 * A, ldw=64, type=0, rows=4, width=64, classes=10, bi
           ws=A, ws_bytes=1 << 40, stream=None)
 CFB = dict(x=A, ldx=64, w=2 * A, ldw=64, type=0, rows=4, width=64, classes=10, bias=A, labels=A, loss=A, row_grad=None, scale=1.0, dx=3 * A, lddx=64, dw=4 * A, lddw=64, dw_type=1, db=A,
            ws=A, ws_bytes=1 << 40, stream=None)
-CE_BAD = [dict(x=None), dict(x=A + 1), dict(ldx=63), dict(w=None), dict(ldw=9), dict(type=2), dict(rows=-1), dict(rows=(1 << 22) + 1), dict(width=0), dict(width=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21,
+CE_BAD = [dict(x=None), dict(x=A + 1), dict(ldx=63), dict(w=None), dict(ldw=9), dict(type=2), dict(rows=-1), dict(rows=(1 << 22) + 1), dict(type=1, dw_type=1, rows=(1 << 21) + 1), dict(width=0), dict(width=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21,
           lddx=1 << 21, lddw=1 << 21), dict(rows=1 << 22, width=2049, ldx=2049, ldw=2049, lddx=2049, lddw=2049), dict(classes=0), dict(classes=BIG), dict(bias=A + 2), dict(labels=None),
           dict(labels=A + 1), dict(ws=None), dict(ws=A + 128), dict(ws_bytes=100)]
 CE_GRADS = [dict(row_grad=A + 1), dict(dx=None, dw=None, db=None), dict(dw_type=2), dict(type=1, dw_type=0), dict(dx=3 * A + 1), dict(lddx=5), dict(dw=4 * A + 2), dict(lddw=60), dict(db=A + 2),
@@ -92,7 +92,7 @@ def test_workspaces():
     assert lib.bsr_clip_workspace_bytes(0) == lib.bsr_clip_workspace_bytes(-4) == 0
     assert lib.bsr_linear_ce_workspace_bytes(0, 0, 64, 10, 0) == lib.bsr_linear_ce_workspace_bytes(2, 4, 64, 10, 0) == 0
     for kind in (0, 1):
-        for rows, width, classes in ((1, 1, 1), (4096, 4096, 131072), (1 << 22, 64, 1 << 30), (33, 1 << 20, 100), (1, 64, 1 << 30)):
+        for rows, width, classes in ((1, 1, 1), (4096, 4096, 131072), ((1 << 22) >> kind, 64, 1 << 30), (33, 1 << 20, 100), (1, 64, 1 << 30)):
             one = [lib.bsr_linear_ce_workspace_bytes(kind, rows, width, classes, what) for what in (0, 1, 2)]
             assert min(one) > 0 and one[2] >= max(one) and lib.bsr_linear_ce_workspace_bytes(kind, rows, width, classes, 3) == 0
     assert 0 < lib.bsr_clip_workspace_bytes(1) <= lib.bsr_clip_workspace_bytes(1000)
