@@ -629,9 +629,16 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
   const T* x = (const T*)j.x;
   uint32_t* most = j.most + (int64_t)chunk * D;
   if (D < V) {                                     // (no whole piece to read)
-    if (threadIdx.x < D) {
-      uint32_t m = 0;
-      for (int r = r0; r < r1; ++r) m = max(m, bits_if_finite(weighted((float)x[r * j.ldx + threadIdx.x], weight_of(j.rw, r))));
+    __shared__ uint32_t part[256 / V][V];
+    const int c = threadIdx.x % V, i = threadIdx.x / V;
+    uint32_t m = 0;
+    if (c < D)
+#pragma unroll 4
+      for (int r = r0 + i; r < r1; r += 256 / V) m = max(m, bits_if_finite(weighted((float)x[r * j.ldx + c], weight_of(j.rw, r))));
+    part[i][c] = m;
+    __syncthreads();
+    if ((int)threadIdx.x < D) {
+      for (int k = 1; k < 256 / V; ++k) m = max(m, part[k][threadIdx.x]);
       most[threadIdx.x] = m;
     }
     return;

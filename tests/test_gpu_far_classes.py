@@ -77,3 +77,28 @@ def test_the_last_rows_of_many(env):
     assert (loss[-L:] - want[0]).abs().max() < 2.0 ** -6 and not loss[:-L].any() and not dx[:-L].any()
     for got, ref in ((dx[-L:], want[1]), (dw, want[2])):
         assert (got.double() - ref.double()).norm() < 2.0 ** -6 * ref.double().norm()
+
+
+@pytest.mark.parametrize("N,D,dtype", [(1 << 22, 16, "bf16"), (1 << 21, 5, "f32"), ((1 << 20) + 7, 3, "bf16")])
+def test_the_most_rows(env, N, D, dtype):
+    """Labels all alike, so that the sums over the rows grow with them: fp32 sums of N rows are off by (N / 16 + 60) 2^-24 of their terms' sizes, 2^-6, of which a class's sum keeps more than half here; the
+    tensors of other signs, and half a step of bf16, take it to 2^-4 in the 2-norm.  What is off by a row or a tile misses by far more in dx and loss, which have a row each."""
+    torch, P = env
+    torch.manual_seed(D)
+    kind = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    V = 5
+    x, w = (1 + 0.25 * torch.randn(N, D, device="cuda")).to(kind), (torch.randn(V, D, device="cuda") / D ** 0.5).to(kind)
+    labels = torch.zeros(N, device="cuda", dtype=torch.int32)
+    labels[1::3] = -1
+    loss, dx, dw, _ = P.bsr_linear_ce_forward_backward(x, w, labels, dw=torch.empty(V, D, device="cuda"))
+    z = x.double() @ w.double().t()
+    some = (labels >= 0).double()
+    G = torch.softmax(z, 1)
+    G[:, 0] -= 1
+    G *= some[:, None]
+    ref = (torch.logsumexp(z, 1) - z[:, 0]) * some
+    assert (loss - ref).abs().max() < 2.0 ** -16
+    want = G @ w.double()
+    assert (dx.double() - want).abs().max() < {"bf16": 2.0 ** -7, "f32": 2.0 ** -16}[dtype] * want.abs().max()
+    want = G.t() @ x.double()
+    assert (dw.double() - want).norm() < 2.0 ** -4 * want.norm()

@@ -203,3 +203,29 @@ def test_far_rows(env):
     dx, dg = P.bsr_rmsnorm_backward(x, x, want[1], gamma, res=x)
     dx2, dg2 = P.bsr_rmsnorm_backward(near, near, want[1], gamma, res=near)
     assert torch.equal(dx, dx2) and torch.equal(dg, dg2)
+
+
+@pytest.mark.parametrize("D", [16, 5])
+def test_rows_past_one_launch(env, D):
+    """2^21 rows are a launch: the rows around its end and the last ones as by themselves"""
+    torch, P = env
+    M = (1 << 21) + 3
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x, r, dy = (torch.randn(M, D, generator=g, device="cuda").bfloat16() for _ in range(3))
+    gamma = gains(torch, D)
+    y, rstd, total = P.bsr_rmsnorm_forward(x, gamma, EPS, res=r)
+    r8, _, _ = P.bsr_rmsnorm_forward8(x, gamma, EPS, res=r)
+    dx, none = P.bsr_rmsnorm_backward(dy, total, rstd, gamma, res=r, need_params=False)
+    dx2, dgamma = P.bsr_rmsnorm_backward(dy, total, rstd, gamma, res=r)
+    assert none is None and torch.equal(dx, dx2)
+    for part in (slice(0, 70), slice((1 << 21) - 50, M), slice(M - 1, M)):
+        a, b, c = (t[part].contiguous() for t in (x, r, dy))
+        want = P.bsr_rmsnorm_forward(a, gamma, EPS, res=b)
+        q, _, _ = P.bsr_rmsnorm_forward8(a, gamma, EPS, res=b)
+        assert torch.equal(y[part], want[0]) and torch.equal(rstd[part], want[1]) and torch.equal(total[part], want[2])
+        assert torch.equal(r8.values[part], q.values) and torch.equal(r8.scales[part], q.scales)
+        assert torch.equal(dx[part], P.bsr_rmsnorm_backward(c, want[2], want[1], gamma, res=b, need_params=False)[0])
+    xhat = total.double() * rstd.double()[:, None]
+    want = (dy.double() * xhat).sum(0)
+    # (at most 256 chains of 8192 additions, whose running sums of random signs stay below 512: each is off by 8192 x 512 x 2^-24 at the very most)
+    assert (dgamma.double() - want).abs().max() < 64
