@@ -102,3 +102,30 @@ def test_the_most_rows(env, N, D, dtype):
     assert (dx.double() - want).abs().max() < {"bf16": 2.0 ** -7, "f32": 2.0 ** -16}[dtype] * want.abs().max()
     want = G.t() @ x.double()
     assert (dw.double() - want).norm() < 2.0 ** -4 * want.norm()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [3, 40, 70])
+def test_the_widest_rows(env, N, dtype):
+    """2^20 features, of which 64 are not zero in x: sums of 64 terms, off by less than 64 2^-24 of their sizes (8 or so); gradients by 2^-12 (fp32) and half a step of bf16, 2^-8, as parts of their 2-norm"""
+    torch, P = env
+    torch.manual_seed(N)
+    kind = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    D, V = 1 << 20, 20
+    at = torch.randperm(D, device="cuda")[:64]
+    at[0] = D - 1
+    x, w = torch.zeros(N, D, dtype=kind, device="cuda"), torch.randn(V, D, device="cuda").to(kind)
+    x[:, at] = (torch.randn(N, 64, device="cuda") / 8).to(kind)
+    labels = torch.randint(V, (N,), device="cuda", dtype=torch.int32)
+    loss, dx, dw, _ = P.bsr_linear_ce_forward_backward(x, w, labels)
+    z = x[:, at].double() @ w[:, at].double().t()
+    assert (loss - torch.nn.functional.cross_entropy(z, labels.long(), reduction="none")).abs().max() < 2.0 ** -12
+    G = torch.softmax(z, 1)
+    G[torch.arange(N), labels.long()] -= 1
+    tol = {"bf16": 2.0 ** -8, "f32": 2.0 ** -12}[dtype]
+    want = G @ w.double()
+    assert (dx.double() - want).norm() < tol * want.norm()
+    want = G.t() @ x[:, at].double()
+    assert (dw[:, at].double() - want).norm() < tol * want.norm()
+    dw[:, at] = 0
+    assert not dw.any()
