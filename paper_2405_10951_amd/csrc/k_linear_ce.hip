@@ -736,8 +736,8 @@ __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, Trans
   }
 }
 
-// G in fp32 (from k_linear_ce_small.hip, without weights), or logits, to what the tiles leave of G: 64 tokens x 64 classes a workgroup
-template <int TERMS, bool LOGITS>
+// logits to what the tiles leave of G: 64 tokens x 64 classes a workgroup
+template <int TERMS>
 __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ from, int64_t ldz, CeGemm g) {
   __shared__ float tile[64][65];
   const int t = threadIdx.x, m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, a = t / 4, b = t % 4 * 16;      // a row (or a column) and 16 of its values
@@ -750,7 +750,7 @@ __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ 
   bool counts = m0 + a < g.M;                      // (as at a tile's end)
   float2 st = {0.f, 0.f};
   int label = -1;
-  if (LOGITS && counts) {
+  if (counts) {
     label = g.labels[m0 + a];
     st = g.stats[m0 + a];
     counts = label >= 0 && label < g.classes && (!g.row_grad || g.row_grad[m0 + a] != 0.f) && !(st.x == -INFINITY && st.y == 0.f);
@@ -761,7 +761,7 @@ __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ 
     f32x4 p = there ? *(const f32x4*)(from + (int64_t)(m0 + a) * ldz + n0 + b + i) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (LOGITS) p[j] = __builtin_amdgcn_exp2f(fmaf(p[j] - st.x, LOG2E, -st.y * LOG2E)) - (n0 + b + i + j == label ? 1.f : 0.f);
+      p[j] = __builtin_amdgcn_exp2f(fmaf(p[j] - st.x, LOG2E, -st.y * LOG2E)) - (n0 + b + i + j == label ? 1.f : 0.f);
       tile[a][b + i + j] = v[i + j] = there && n0 + b + i + j < g.N ? p[j] : 0.f;
     }
   }
@@ -1092,7 +1092,7 @@ static void forward_with(const LinearCe& a, float* z, bool packs, hipStream_t s)
   const Way way(a);
   const bool direct_x = way.x, direct_w = way.w;
   if (way.little || (way.few && !way.w)) {
-    small_ce_forward(a, (float*)a.workspace, GRAD_NONE, s);
+    small_ce_forward(a, (float*)a.workspace, false, s);
     return;
   }
   const Plan p(a.f32, a.N, a.D, a.V, false, packs);
@@ -1122,11 +1122,11 @@ void linear_ce_forward(const LinearCe& a, hipStream_t s) { forward_with(a, nullp
 // 4000 bf16 153 against 177, 1000 x 768 x 1000 40 against 43; 400 x 64 x 10000 51 against 48)
 bool keeps(bool f32, int N, int D, int V) { return small_ce_bytes(N, V) <= SMALL_BYTES && over(D, BK) * (f32 ? 3 : 1) >= 8; }
 
-// little work: G in fp32 first, then turned into what the tiles leave (in one piece)
+// little work: its logits, in scratch, turned into what the tiles leave (in one piece)
 bool takes_turn(const LinearCe& a, const Plan& p, const Way& way) { return way.little && p.Vc >= a.V; }
 
-// What a forward on the same workspace has left: nothing, the packed operands (of one piece), G of little work, or the logits (z)
-enum Ready { NOTHING, PACKED, TURNED, KEPT };
+// What a forward on the same workspace has left: nothing, the packed operands (of one piece), or the logits (z)
+enum Ready { NOTHING, PACKED, KEPT };
 template <typename T>
 void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) {
   constexpr bool F32 = sizeof(T) == 4;
@@ -1163,11 +1163,9 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
     if (a.dw) { g.GT = GT; g.kgt = p.Np; g.ldgt = TERMS * p.Np; }
     if (a.db) { g.dbp = (float*)(ws + p.dbp); g.ldd = p.ldd; }
     const int shape = logits_shape(a.N, n, g.nk * tile_work(F32)), rows = a.dw ? p.Np : a.N, tall = turned ? 64 : rows_of(shape);
-    if (ready == KEPT) {
-      ce_turn_kernel<F32 ? 2 : 1, true><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(z, small_ce_stride(a.N, a.V), g);
-    } else if (turned) {
-      if (ready != TURNED) small_ce_gradient(a, false, (float*)(ws + p.z), s);
-      ce_turn_kernel<F32 ? 2 : 1, false><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>((const float*)(ws + p.z), small_ce_stride(a.N, a.V), g);
+    if (turned) {
+      if (ready != KEPT) small_ce_logits(a, (float*)(ws + p.z), s);
+      ce_turn_kernel<TERMS><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(ready == KEPT ? z : (const float*)(ws + p.z), small_ce_stride(a.N, a.V), g);
     } else if (a.db) {
       logits<GRAD, F32, TERMS, true>(shape, g, rows, s);
     } else {
@@ -1222,7 +1220,7 @@ static void few_backward(const LinearCe& a, bool both, hipStream_t s) {
   if (way.little || !way.w) {
     const bool fused = both && few_fused(a.f32, a.V);
     const bool many = a.V > 4096;                  // (a workgroup a row turns those into G more slowly than a launch of its own)
-    if (both && !fused) small_ce_forward(a, (float*)a.workspace, many ? GRAD_NONE : GRAD_WEIGHTED, s);
+    if (both && !fused) small_ce_forward(a, (float*)a.workspace, !many, s);
     few_ce_backward(a, fused ? FEW_FUSED : !both ? FEW_NOTHING : many ? FEW_LOGITS : FEW_GRADIENT, s);
   } else {
     LinearCe f = a;
@@ -1252,8 +1250,9 @@ void linear_ce_both(const LinearCe& a, hipStream_t s) {
     const Plan f(a.f32, a.N, a.D, a.V, false), p(a.f32, a.N, a.D, a.V, true);
     const bool one = p.Vc >= a.V && (way.w ? f.Vs : f.Vp) >= a.V;        // one piece in both
     if (takes_turn(a, p, way)) {
-      small_ce_forward(a, (float*)((char*)a.workspace + p.z), GRAD_PLAIN, s);
-      backward_with(a, TURNED, nullptr, s);
+      float* z = (float*)((char*)a.workspace + p.z);
+      small_ce_forward(a, z, false, s);
+      backward_with(a, KEPT, z, s);
     } else if (one && keeps(a.f32, a.N, a.D, a.V) && !way.little) {
       float* z = (float*)((char*)a.workspace + both_kept_at(a.f32, a.N, a.D, a.V));
       forward_with(a, z, true, s);

@@ -42,7 +42,6 @@ __device__ __forceinline__ f32x4 multiplied(f32x4 a, f32x4 b, f32x4 c) {
 // what a token's logits become G by; counts: whether it has a gradient at all
 struct Tokens {
   const int32_t* labels = nullptr; const float2* stats = nullptr; const float* row_grad = nullptr; float scale = 1.f;      // stats null: the logits stay what they are
-  bool weighted = true;                            // G with its row's weight
   int N = 0, V = 0;
   float* loss = nullptr; float2* stats_out = nullptr;            // where a kernel that makes them leaves them
   int rows = 0;                                    // of G; those from N on, and classes from V on, are zero
@@ -121,7 +120,7 @@ __global__ __launch_bounds__(LOGIT_WAVES * WAVE) void small_logits_kernel(const 
         const bool counts = tk.counts(n);
         const int m = min(n, N - 1);
         const float2 st = tk.stats[m];
-        const float by = tk.scale * (tk.weighted && tk.row_grad ? tk.row_grad[m] : 1.f);
+        const float by = tk.scale * (tk.row_grad ? tk.row_grad[m] : 1.f);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           o[j] = counts && v + j < V ? by * (__builtin_amdgcn_exp2f(fmaf(o[j] - st.x, LOG2E, -st.y * LOG2E)) - (v + j == tk.labels[m] ? 1.f : 0.f)) : 0.f;
@@ -185,7 +184,7 @@ __global__ __launch_bounds__(NT) void small_rows_kernel(float* __restrict__ z, i
   }
   if (!grad) return;
   __syncthreads();
-  const float weight = tk.row_grad ? tk.row_grad[m] : 1.f, by = tk.weighted ? tk.scale * weight : 1.f;
+  const float weight = tk.row_grad ? tk.row_grad[m] : 1.f, by = tk.scale * weight;
   const bool counts = there && weight != 0.f;
 #pragma unroll 4
   for (int v = threadIdx.x * 4; v < ldz; v += NT * 4) {
@@ -203,7 +202,7 @@ __global__ __launch_bounds__(256) void small_turn_kernel(float* __restrict__ z, 
   const bool counts = tk.counts(n);
   const int m = min(n, tk.N - 1);
   const float2 st = tk.stats[m];
-  const float by = tk.scale * (tk.weighted && tk.row_grad ? tk.row_grad[m] : 1.f);
+  const float by = tk.scale * (tk.row_grad ? tk.row_grad[m] : 1.f);
   f32x4 p = *(const f32x4*)(z + n * ldz + v);
 #pragma unroll
   for (int j = 0; j < 4; ++j) p[j] = counts && v + j < tk.V ? by * (__builtin_amdgcn_exp2f(fmaf(p[j] - st.x, LOG2E, -st.y * LOG2E)) - (v + j == tk.labels[m] ? 1.f : 0.f)) : 0.f;
@@ -528,9 +527,9 @@ template <bool LOGITS> void grads(const LinearCe& a, const Tokens& tk, const flo
 
 }  // namespace
 
-static Tokens tokens_of(const LinearCe& a, bool weighted) {
+static Tokens tokens_of(const LinearCe& a) {
   Tokens tk;
-  tk.N = tk.rows = a.N; tk.V = a.V; tk.labels = a.labels; tk.row_grad = a.row_grad; tk.weighted = weighted; tk.scale = weighted ? a.grad_scale : 1.f;
+  tk.N = tk.rows = a.N; tk.V = a.V; tk.labels = a.labels; tk.row_grad = a.row_grad; tk.scale = a.grad_scale;
   return tk;
 }
 static void logits_of(const LinearCe& a, const Tokens& tk, float* z, hipStream_t s) {
@@ -538,29 +537,24 @@ static void logits_of(const LinearCe& a, const Tokens& tk, float* z, hipStream_t
   else logits_as<bf16>(a, tk, z, s);
 }
 
-void small_ce_forward(const LinearCe& a, float* z, SmallGrad grad, hipStream_t s) {
-  Tokens tk = tokens_of(a, grad == GRAD_WEIGHTED);
-  logits_of(a, tk, z, s);
-  if (grad == GRAD_WEIGHTED) tk.rows = 16 * few_tiles_of(a.N);
-  if (a.V > 4096) small_rows_kernel<1024><<<tk.rows, 1024, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad != GRAD_NONE);
-  else small_rows_kernel<256><<<tk.rows, 256, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad != GRAD_NONE);
-}
+void small_ce_logits(const LinearCe& a, float* z, hipStream_t s) { logits_of(a, tokens_of(a), z, s); }
 
-void small_ce_gradient(const LinearCe& a, bool weighted, float* G, hipStream_t s) {
-  Tokens tk = tokens_of(a, weighted);
-  tk.stats = (const float2*)a.stats;
-  if (weighted) tk.rows = 16 * few_tiles_of(a.N);
-  logits_of(a, tk, G, s);
+void small_ce_forward(const LinearCe& a, float* z, bool grad, hipStream_t s) {
+  Tokens tk = tokens_of(a);
+  logits_of(a, tk, z, s);
+  if (grad) tk.rows = 16 * few_tiles_of(a.N);
+  if (a.V > 4096) small_rows_kernel<1024><<<tk.rows, 1024, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad);
+  else small_rows_kernel<256><<<tk.rows, 256, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad);
 }
 
 size_t few_parts_at(int N, int V) { return (small_ce_bytes(16 * few_tiles_of(N), V) + 255) / 256 * 256; }
 size_t few_ce_bytes(bool f32, int N, int V, int D) { return sizeof(float) * (size_t)few_ranges(f32, N, V, D) * N * (((size_t)D + 3) / 4 * 4); }
 void few_ce_backward(const LinearCe& a, Few there, hipStream_t s) {
   float *G = (float*)a.workspace, *parts = (float*)((char*)a.workspace + few_parts_at(a.N, a.V));
-  if (there == FEW_NOTHING) small_ce_gradient(a, true, G, s);
-  Tokens tk = tokens_of(a, true);
+  Tokens tk = tokens_of(a);
   tk.stats = (const float2*)a.stats;
   tk.rows = 16 * few_tiles_of(a.N);
+  if (there == FEW_NOTHING) logits_of(a, tk, G, s);
   if (there == FEW_LOGITS) small_turn_kernel<<<dim3(over(small_ldz(a), 1024), tk.rows), 256, 0, s>>>(G, small_ldz(a), tk);
   if (there == FEW_FUSED) {
     tk.stats = nullptr;                            // (and the logits as they are)

@@ -24,12 +24,11 @@ void linear_ce_backward(const LinearCe& a, hipStream_t s);
 size_t linear_ce_both_bytes(bool f32, int N, int D, int V);
 void linear_ce_both(const LinearCe& a, hipStream_t s);
 
-// k_linear_ce_small.hip: scratch of small_ce_bytes() for the logits, or for G [N, small_ce_stride()], weighted (few rows, below): with grad_scale and the rows' weights
+// k_linear_ce_small.hip: scratch of small_ce_bytes() for the logits, or for G, with grad_scale and the rows' weights, [N, small_ce_stride()]
 inline int64_t small_ce_stride(int N, int V) { return N <= 64 ? ((int64_t)V + 15) / 16 * 16 : ((int64_t)V + 3) / 4 * 4; }
 inline size_t small_ce_bytes(int N, int V) { return sizeof(float) * (size_t)N * small_ce_stride(N, V); }
-enum SmallGrad { GRAD_NONE, GRAD_PLAIN, GRAD_WEIGHTED };
-void small_ce_forward(const LinearCe& a, float* z, SmallGrad grad, hipStream_t s);      // grad: G in the logits' place
-void small_ce_gradient(const LinearCe& a, bool weighted, float* G, hipStream_t s);
+void small_ce_logits(const LinearCe& a, float* z, hipStream_t s);
+void small_ce_forward(const LinearCe& a, float* z, bool grad, hipStream_t s);      // grad (of few rows, below): G in the logits' place
 // N up to FEW_ROWS: G (or the logits) at the workspace's beginning, few_ce_bytes() more at few_parts_at()
 constexpr int FEW_ROWS = 64;
 size_t few_parts_at(int N, int V);
