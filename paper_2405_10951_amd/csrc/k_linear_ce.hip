@@ -9,6 +9,9 @@
 // largest value lies in 2^14 .. 2^15, which is exact for bf16 values down to 2^-29 of the feature's largest.  The matrix instructions take both types at one rate.  fp32 operands are two fp16 terms each,
 // h + l with h = fp16(v), l = fp16(v - h), off by 2^-22 of the value, and the products h h, l h, h l are added in fp32.  A k-tile holds both terms of 32 k: it is loaded
 // once for the three of them (333 x 1001 x 5003 loss and gradients 93 us; one product after another over the whole contraction 109, k-tile by k-tile 107).
+// dw in fp32 beside bf16 operands: one fp16 term of G would show in it (off by 1.3e-4 of its norm, two terms 4e-7 at 2048 x 768 x 21841), so the transposed G has two, and so has x times a weight; the products
+// h h, l h and, with weights, h l follow one another over a contraction of two or three times the tokens (6304 x 768 x 21841 loss and gradients 1423 us, with weights 1670; dw in bf16 1072).  In a bf16 result G's
+// one term does not show: 2048 x 768 x 21841 dw is off by 1.662e-3 of its norm, from exact G by 1.659e-3, the rounding of the result.
 // Bound by the matrix unit's power where it is large: at 4096 x 4096 x 131072 bf16 a tile of 16 x 16 x 32 instructions runs at 1.7 - 1.8 GHz (32 x 32 x 16 at 1.46, 6 % slower in all), the forward at
 // 1350 TFLOP/s (3.25 ms), a piece's G at 1225 (450 us), both products of G at 1250 (880 us); transposing a piece takes 38 + 59 us.  2048 x 768 x 21841, gradients: maxima 12, transposing 17, G 100 (688 tiles of
 // 12 k-tiles on 256 CUs: beginnings and ends count as much as the products), products 137, sums 9.  333 x 1001 x 5003 fp32: packing 11, logits 20, joining 5, maxima 9, transposing 13, G 9, products 35,
@@ -47,6 +50,7 @@ struct CeGemm {
   int64_t lda = 0, ldb = 0;
   int M = 0, N = 0, nk = 0;                        // nk: k-tiles
   int splits = 1, per = 0;                         // products of G: workgroups over the k-tiles of a tile, k-tiles of each
+  int pass = 0;                                    // PASSES: k-tiles of a pass; A's rows are h, then l, and so are B's where there are three passes: h h, l h, h l
   const int *ea = nullptr, *eb = nullptr;          // powers of two of A's and B's rows, null: 0
   // STATS, GRAD: m is a token, n a class of the piece that begins at class v0
   const float* bias = nullptr;                     // of the piece
@@ -97,7 +101,8 @@ __device__ __forceinline__ int place(int row) { return row >> 1 & 7; }
 // of A: fragments of A come DIST groups ahead through a ring of RING, those of B a half ahead.  DIST groups before the k-tile's end every wavefront has read all of it: there is the barrier, and behind it the loads of k-tile kt + NST go out into its stage, one or two a group.
 // 16 x 16 x 32, not 32 x 32 x 16: under full load the clock is what the power allows, and the smaller tile, which touches half as many accumulators a product, draws less.
 // The operands are swapped (B's rows first): accumulators hold transposed tiles, element r of acc[mi][ni] is row mi 16 + lane % 16, column ni 16 + 4 (lane / 16) + r.
-template <class S, bool F16, int TERMS>
+// PASSES: rows of two terms lie one term behind the other, and the contraction goes over them as one longer one of up to three passes.
+template <class S, bool F16, int TERMS, bool PASSES = false>
 __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt0, int nk, unsigned char* smem, f32x4 (&acc)[S::MI][S::NI]) {
   constexpr int BM = S::BM, WN = S::WN, NST = S::NST, TM = S::TM, TN = S::TN, MI = S::MI, NI = S::NI, HALF = TERMS * MI, NG = HALF + MI;
   constexpr int RPI = S::NT / 8, AL = BM / RPI, BL = S::BN / RPI, LPT = AL + BL, STAGE = (BM + S::BN) * 128;
@@ -118,7 +123,11 @@ __device__ __forceinline__ void multiply(const CeGemm& g, int m0, int n0, int kt
   auto issue1 = [&](auto I, int kt, int st) __attribute__((always_inline)) {
     constexpr int i = decltype(I)::value;
     const f16* src = i < AL ? A : B;
-    const int k = kt0 + kt;
+    int k = kt0 + kt;
+    if constexpr (PASSES) {
+      if (i < AL) k -= k >= 2 * g.pass ? 2 * g.pass : 0;
+      else k -= k >= g.pass ? g.pass : 0;
+    }
     // (a buffer: address of the tile in scalar registers, the row's bytes in a vector register, the k-tile's in a scalar one, and no arithmetic)
     unsigned char* dst = smem + st * STAGE + wave * 1024 + (i < AL ? i * RPI * 128 : BM * 128 + (i - AL) * RPI * 128);
 #ifdef __HIP_DEVICE_COMPILE__
@@ -337,9 +346,10 @@ template <int N> __device__ __forceinline__ float lanes16_sums(float (&v)[N]) {
 }
 
 // Backward: the tile as G, in fp16 times 2^14, rows of 32 tokens at a time through a patch of LDS, from which rows are read as they lie and, with the transposing reads, columns
-template <class S, bool F16, int TERMS, bool DB>
+// FINE (of bf16 operands): the transposed G in two terms, one behind the other.  dw is wanted in fp32, and one fp16 term would be off by up to 2^-12 of G's largest values
+template <class S, bool F16, int TERMS, bool DB, bool FINE>
 __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S::NI], int m0, int n0, int tm, unsigned char* smem) {
-  constexpr int NI = S::NI, TERM = 32 * S::LDR;
+  constexpr int NI = S::NI, TERM = 32 * S::LDR, KEPT = FINE ? 2 : TERMS;
   const Wave<S> w(m0, n0);
   const Classes<S, F16> cl(g, w);
   unsigned char* patch = w.patch(smem);
@@ -380,18 +390,18 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
       for (int j = 0; j < 4; ++j) {
         const float p = acc[mi][ni][j];
         h[j] = (f16)p;
-        if constexpr (TERMS == 2) l[j] = (f16)(p - (float)h[j]);
+        if constexpr (KEPT == 2) l[j] = (f16)(p - (float)h[j]);
       }
       unsigned char* to = patch + (mi % 2 * 16 + w.lm) * S::LDR + w.col(ni, 0) * 2;
       *(f16x4*)to = h;
-      if constexpr (TERMS == 2) *(f16x4*)(to + TERM) = l;
+      if constexpr (KEPT == 2) *(f16x4*)(to + TERM) = l;
     }
     if (mi % 2 == 0) continue;
     const int first = w.row0 + (mi - 1) * 16;      // the patch's 32 tokens
     wave_fence();
 #pragma unroll
-    for (int term = 0; term < TERMS; ++term) {
-      if (g.G) {
+    for (int term = 0; term < KEPT; ++term) {
+      if (term < TERMS && g.G) {
         constexpr int CPR = S::TN / 8, RPP = 64 / CPR;           // 16-byte chunks of a patch row, rows at a time
         const int k = w.lane % CPR, n = w.col0 + k * 8;
 #pragma unroll
@@ -411,7 +421,7 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
           const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(from + cb * 32));
           const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(from + cb * 32 + 4 * S::LDR));
           const int n = w.col0 + cb * 16 + j;
-          if (n < g.N && token < g.kgt) *(s16x8*)(g.GT + (int64_t)n * g.ldgt + spot<TERMS>(token, term)) = s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          if (n < g.N && token < g.kgt) *(s16x8*)(g.GT + (int64_t)n * g.ldgt + (FINE ? token + (int64_t)term * g.kgt : spot<TERMS>(token, term))) = s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         }
       }
     }
@@ -440,7 +450,7 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
   }
 }
 
-template <class S, Mode MODE, bool F16, int TERMS, bool DB>
+template <class S, Mode MODE, bool F16, int TERMS, bool DB, bool FINE>
 __global__ __launch_bounds__(S::NT, S::wavefronts) void ce_logits_kernel(CeGemm g, int mt, int nt) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int tm, tn;
@@ -450,11 +460,11 @@ __global__ __launch_bounds__(S::NT, S::wavefronts) void ce_logits_kernel(CeGemm 
   multiply<S, F16, TERMS>(g, m0, n0, 0, m0 < g.M ? g.nk : 0, smem, acc);      // (tokens that only fill GT's last k-tile: zeros)
   __syncthreads();
   if constexpr (MODE == STATS) end_stats<S, F16>(g, acc, m0, n0, tn, smem);
-  else end_grad<S, F16, TERMS, DB>(g, acc, m0, n0, tm, smem);
+  else end_grad<S, F16, TERMS, DB, FINE>(g, acc, m0, n0, tm, smem);
 }
 
 // Up to two products of G in one launch (a, then b, na workgroups of the first): dx and dw of a piece fill the CUs together
-template <class S, int TERMS>
+template <class S, int TERMS, bool PASSES>
 __global__ __launch_bounds__(S::NT, 1) void ce_grads_kernel(CeGemm a, CeGemm b, int na) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const bool first = (int)blockIdx.x < na;
@@ -467,7 +477,7 @@ __global__ __launch_bounds__(S::NT, 1) void ce_grads_kernel(CeGemm a, CeGemm b, 
   tile_at(id - split * mt * nt, mt, nt, tm, tn);
   const int m0 = tm * S::BM, n0 = tn * S::BN, kt0 = split * g.per;
   f32x4 acc[S::MI][S::NI];
-  multiply<S, true, TERMS>(g, m0, n0, kt0, min(g.per, g.nk - kt0), smem, acc);
+  multiply<S, true, TERMS, PASSES>(g, m0, n0, kt0, min(g.per, g.nk - kt0), smem, acc);
   __syncthreads();
   const Wave<S> w(m0, n0);
   unsigned char* patch = w.patch(smem);
@@ -615,6 +625,7 @@ struct TransposeJob {
   int per = 1, chunks = 0;                         // rows of a part; parts (0: no job)
   uint32_t* most = nullptr;                        // [chunks][D] bits of the largest finite |value|
   f16* to = nullptr; int cols = 0; int64_t ld = 0; int* exps = nullptr;           // cols (of one or both terms) of a row are written
+  bool both = false;                               // FINE: two terms, one behind the other (of x with weights, which bf16 values times them do not fit one of)
 };
 constexpr int CHUNKS = 64;
 
@@ -674,10 +685,10 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
 }
 
 // `down` tiles of 64 x 64 a workgroup, below one another: their columns' powers of two are worked out once, and the next tile's rows are on their way while one is turned
-template <typename T>
+template <typename T, bool FINE>
 __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, TransposeJob b, int blocks, int down, int D) {
-  constexpr int TERMS = sizeof(T) / 2, V = Chunk<T>::V, PER_ROW = 64 / V, K = PER_ROW / 4, LD = 66;
-  __shared__ f16 tile[TERMS][64][LD];              // (rows of 33 words: neither the writes down nor the reads across meet in a bank)
+  constexpr int TERMS = sizeof(T) / 2, KEPT = FINE ? 2 : TERMS, V = Chunk<T>::V, PER_ROW = 64 / V, K = PER_ROW / 4, LD = 66;
+  __shared__ f16 tile[KEPT][64][LD];              // (rows of 33 words: neither the writes down nor the reads across meet in a bank)
   __shared__ uint32_t red[4][64];
   __shared__ int exps[64];
   const bool first = (int)blockIdx.x < blocks;
@@ -720,24 +731,25 @@ __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, Trans
         const float s = ldexpf(weighted((float)v[i][e], by[i]), -exps[c + e]);
         const f16 h = (f16)s;
         tile[0][c + e][r0 + i * (256 / PER_ROW)] = h;
-        if constexpr (TERMS == 2) tile[TERMS - 1][c + e][r0 + i * (256 / PER_ROW)] = (f16)(s - (float)h);
+        if constexpr (KEPT == 2) tile[KEPT - 1][c + e][r0 + i * (256 / PER_ROW)] = (f16)(s - (float)h);
       }
     if (m0 + 64 < end) fetch(m0 + 64);
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < TERMS; ++t)
+    for (int t = 0; t < KEPT; ++t)
 #pragma unroll
       for (int i = threadIdx.x; i < 512; i += 256) {
+        if (FINE && t == 1 && !j.both) break;
         const int col = i / 8, k = i % 8 * 8;
         const uint32_t* from = (const uint32_t*)&tile[t][col][k];
-        if (c0 + col < D && m0 + k < j.cols) *(uint4*)(j.to + (int64_t)(c0 + col) * j.ld + spot<TERMS>(m0 + k, t)) = make_uint4(from[0], from[1], from[2], from[3]);
+        if (c0 + col < D && m0 + k < j.cols) *(uint4*)(j.to + (int64_t)(c0 + col) * j.ld + (FINE ? m0 + k + (int64_t)t * j.cols : spot<TERMS>(m0 + k, t))) = make_uint4(from[0], from[1], from[2], from[3]);
       }
     __syncthreads();
   }
 }
 
 // logits to what the tiles leave of G: 64 tokens x 64 classes a workgroup
-template <int TERMS>
+template <int TERMS, bool FINE>
 __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ from, int64_t ldz, CeGemm g) {
   __shared__ float tile[64][65];
   const int t = threadIdx.x, m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, a = t / 4, b = t % 4 * 16;      // a row (or a column) and 16 of its values
@@ -765,7 +777,8 @@ __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ 
       tile[a][b + i + j] = v[i + j] = there && n0 + b + i + j < g.N ? p[j] : 0.f;
     }
   }
-  auto put = [&](f16* row, int at) __attribute__((always_inline)) {
+  // (second: whether, and how far behind, the other term goes; 0: 32 and 32 of both in turn)
+  auto put = [&](f16* row, int at, auto BOTH, int64_t second) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 16; i += 8) {
       f16x8 h, l;
@@ -777,10 +790,10 @@ __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ 
         l[j] = lj;
       }
       *(f16x8*)(row + spot<TERMS>(at + i)) = h;
-      if constexpr (TERMS == 2) *(f16x8*)(row + spot<TERMS>(at + i, 1)) = l;
+      if constexpr (decltype(BOTH)::value != 0) *(f16x8*)(row + (second ? at + i + second : spot<TERMS>(at + i, 1))) = l;
     }
   };
-  if (g.G && m0 + a < g.M) put(g.G + (int64_t)(m0 + a) * g.ldg, n0 + b);
+  if (g.G && m0 + a < g.M) put(g.G + (int64_t)(m0 + a) * g.ldg, n0 + b, IC<TERMS - 1>{}, 0);
   if (!g.GT && !g.dbp) return;
   __syncthreads();
   float sum = 0.f;
@@ -790,7 +803,7 @@ __global__ __launch_bounds__(256) void ce_turn_kernel(const float* __restrict__ 
     const int m = m0 + b + i;
     sum += m < g.M && g.row_grad && v[i] != 0.f ? g.row_grad[m] * v[i] : v[i];
   }
-  if (g.GT && n0 + a < g.N) put(g.GT + (int64_t)(n0 + a) * g.ldgt, m0 + b);
+  if (g.GT && n0 + a < g.N) put(g.GT + (int64_t)(n0 + a) * g.ldgt, m0 + b, IC<FINE || TERMS == 2>{}, FINE ? g.kgt : 0);
   if (g.dbp) {
     sum += __shfl_xor(sum, 1);
     sum += __shfl_xor(sum, 2);
@@ -892,23 +905,23 @@ enum { LARGE, SMALL, MID, FEW, SHORT };
 int rows_of(int shape) { return shape == FEW ? Few::BM : shape == SHORT ? Short::BM : shape == MID ? Mid::BM : shape == SMALL ? Small::BM : Large::BM; }
 int cols_of(int shape) { return shape == FEW ? Few::BN : shape == SHORT ? Short::BN : shape == MID ? Mid::BN : shape == SMALL ? Small::BN : Large::BN; }
 
-template <class S, Mode MODE, bool F16, int TERMS, bool DB> void launch_logits(const CeGemm& g, int rows, hipStream_t s) {
-  with_lds<ce_logits_kernel<S, MODE, F16, TERMS, DB>>(S::lds);
+template <class S, Mode MODE, bool F16, int TERMS, bool DB, bool FINE> void launch_logits(const CeGemm& g, int rows, hipStream_t s) {
+  with_lds<ce_logits_kernel<S, MODE, F16, TERMS, DB, FINE>>(S::lds);
   const int mt = over(rows, S::BM), nt = over(g.N, S::BN);
-  ce_logits_kernel<S, MODE, F16, TERMS, DB><<<mt * nt, S::NT, S::lds, s>>>(g, mt, nt);
+  ce_logits_kernel<S, MODE, F16, TERMS, DB, FINE><<<mt * nt, S::NT, S::lds, s>>>(g, mt, nt);
 }
 // rows: those that tiles have to cover
-template <Mode MODE, bool F16, int TERMS, bool DB> void logits(int shape, const CeGemm& g, int rows, hipStream_t s) {
-  if (shape == FEW) launch_logits<Few, MODE, F16, TERMS, DB>(g, rows, s);
-  else if (shape == SHORT) launch_logits<Short, MODE, F16, TERMS, DB>(g, rows, s);
-  else if (shape == MID) launch_logits<Mid, MODE, F16, TERMS, DB>(g, rows, s);
-  else if (shape == SMALL) launch_logits<Small, MODE, F16, TERMS, DB>(g, rows, s);
-  else launch_logits<std::conditional_t<MODE == STATS, LargeForward, Large>, MODE, F16, TERMS, DB>(g, rows, s);
+template <Mode MODE, bool F16, int TERMS, bool DB, bool FINE = false> void logits(int shape, const CeGemm& g, int rows, hipStream_t s) {
+  if (shape == FEW) launch_logits<Few, MODE, F16, TERMS, DB, FINE>(g, rows, s);
+  else if (shape == SHORT) launch_logits<Short, MODE, F16, TERMS, DB, FINE>(g, rows, s);
+  else if (shape == MID) launch_logits<Mid, MODE, F16, TERMS, DB, FINE>(g, rows, s);
+  else if (shape == SMALL) launch_logits<Small, MODE, F16, TERMS, DB, FINE>(g, rows, s);
+  else launch_logits<std::conditional_t<MODE == STATS, LargeForward, Large>, MODE, F16, TERMS, DB, FINE>(g, rows, s);
 }
-template <class S, int TERMS> void launch_grads(const CeGemm& a, const CeGemm& b, hipStream_t s) {
+template <class S, int TERMS, bool PASSES> void launch_grads(const CeGemm& a, const CeGemm& b, hipStream_t s) {
   auto blocks = [](const CeGemm& g) { return g.A ? over(g.M, S::BM) * over(g.N, S::BN) * g.splits : 0; };
-  with_lds<ce_grads_kernel<S, TERMS>>(S::lds);
-  ce_grads_kernel<S, TERMS><<<blocks(a) + blocks(b), S::NT, S::lds, s>>>(a, b, blocks(a));
+  with_lds<ce_grads_kernel<S, TERMS, PASSES>>(S::lds);
+  ce_grads_kernel<S, TERMS, PASSES><<<blocks(a) + blocks(b), S::NT, S::lds, s>>>(a, b, blocks(a));
 }
 
 // Models of a launch, in us: a workgroup, or the two of a shape that a CU takes at once, has a CU for start + k-tiles * tile.  (Short against large, forward: 600 x 100 x 100000 bf16 60 against 75 us, 2000 x 512 x
@@ -934,7 +947,8 @@ struct Split { int shape, x, w; };
 Split grads_split(int64_t M, int64_t n, int64_t D, int kx, int kw, double work) {
   Split best = {SMALL, 1, 1};
   double least = 1e30;
-  for (int shape = LARGE; shape <= SMALL; ++shape) {
+  // (255 rows of two terms of more than 2^21 tokens would pass 32 bits)
+  for (int shape = kw > 1 << 16 ? SMALL : LARGE; shape <= SMALL; ++shape) {
     const int64_t tx = kx ? (int64_t)over(M, rows_of(shape)) * over(D, cols_of(shape)) : 0, tw = kw ? (int64_t)over(n, rows_of(shape)) * over(D, cols_of(shape)) : 0;
     const Cost c = COST[shape];
     for (int x = 1; x <= (kx ? 64 : 1); ++x) {
@@ -981,8 +995,10 @@ struct Plan {
   int T, Dp, Np, Vs, Vp, Vc, Dq, ldd;
   Split split = {};
   size_t xp, ex, wp, ew, parts, run, zlabel, G, GT, xT, wT, exT, ewT, mostx, mostw, dxp, dwp, dbp, z, bytes;
-  Plan(bool f32, int N, int D, int V, bool backward, bool packs = true) {      // packs: room for w packed
+  // packs: room for w packed; fine: x and G transposed in two terms
+  Plan(bool f32, int N, int D, int V, bool backward, bool packs = true, bool fine = false) {
     T = f32 ? 2 : 1;
+    const int TT = f32 || fine ? 2 : 1;            // terms of what is transposed of G and of x
     Dp = up(D, BK); Np = up(N, BK); Dq = up(D, 4);
     // Pieces of the classes, whole tiles and alike in size.  Forward: the tiles' maxima and sums take at most 64 MB (Vs) and what is packed 256 (Vp, where something is).
     // Backward: G, twice, takes at most 256 MB, and so does the transposed piece of w.
@@ -994,7 +1010,7 @@ struct Plan {
     constexpr double MB = 1 << 20;
     Vs = piece(64 * MB * 128 / (8.0 * N));
     Vp = std::min(Vs, piece(256 * MB / (2.0 * T * Dp)));
-    Vc = std::min(piece(256 * MB / (4.0 * T * Np)), piece(256 * MB / (2.0 * T * Dp)));
+    Vc = std::min(piece(256 * MB / (2.0 * (T + TT) * Np)), piece(256 * MB / (2.0 * T * Dp)));
     ldd = Vc;
     bytes = 0;
     auto take = [&](size_t n) { const size_t at = bytes; bytes += (n + 255) / 256 * 256; return at; };
@@ -1005,12 +1021,12 @@ struct Plan {
       parts = take(sizeof(float2) * (size_t)over(Vs, 128) * N); run = take(sizeof(float2) * (size_t)N); zlabel = take(sizeof(float) * (size_t)N);
       return;
     }
-    G = take((size_t)2 * T * N * Vc); GT = take((size_t)2 * T * Vc * Np);
-    xT = take((size_t)2 * T * D * Np); exT = take(sizeof(int) * (size_t)D);
+    G = take((size_t)2 * T * N * Vc); GT = take((size_t)2 * TT * Vc * Np);
+    xT = take((size_t)2 * TT * D * Np); exT = take(sizeof(int) * (size_t)D);
     wT = take((size_t)2 * T * D * Vc); ewT = take(sizeof(int) * (size_t)D);
     mostx = take(sizeof(uint32_t) * (size_t)CHUNKS * D); mostw = take(sizeof(uint32_t) * (size_t)CHUNKS * D);
     // (for the first piece; the others take as many workgroups over k)
-    split = grads_split(N, std::min(V, Vc), D, std::min(Vc, up(V, BK)) / BK * T, Np / BK * T, tile_work(f32));
+    split = grads_split(N, std::min(V, Vc), D, std::min(Vc, up(V, BK)) / BK * T, Np / BK * TT, tile_work(f32));
     dxp = take(sizeof(float) * (size_t)split.x * N * Dq);
     dwp = take(split.w > 1 ? sizeof(float) * (size_t)split.w * Vc * Dq : 0);
     dbp = take(sizeof(float) * (size_t)over(Np, 32) * ldd);
@@ -1037,7 +1053,7 @@ void pack(const PackJob& a, const PackJob& b, bool f32, int D, int Dp, hipStream
   else go(ce_pack_kernel<float, WAVE>, pack_blocks<float, WAVE>(a.rows, Dp), pack_blocks<float, WAVE>(b.rows, Dp));
 }
 
-template <typename T> void transpose(const TransposeJob& a, const TransposeJob& b, int D, hipStream_t s) {
+template <typename T, bool FINE> void transpose(const TransposeJob& a, const TransposeJob& b, int D, hipStream_t s) {
   if (a.chunks + b.chunks == 0) return;
   constexpr int LINE = 8 * Chunk<T>::V;
   if (over(D, 4 * LINE) * (a.chunks + b.chunks) >= 1024) ce_colmax_kernel<T, 32><<<dim3(over(D, 4 * LINE), a.chunks + b.chunks), 256, 0, s>>>(a, b, D);
@@ -1045,7 +1061,7 @@ template <typename T> void transpose(const TransposeJob& a, const TransposeJob& 
   const int tiles = (a.chunks ? over(a.cols, 64) : 0) + (b.chunks ? over(b.cols, 64) : 0);
   const int down = (int)std::min<int64_t>(8, std::max<int64_t>(1, (int64_t)tiles * over(D, 64) / 2048));
   const int na = a.chunks ? over(a.cols, 64 * down) : 0, nb = b.chunks ? over(b.cols, 64 * down) : 0;
-  ce_transpose_kernel<T><<<dim3(na + nb, over(D, 64)), 256, 0, s>>>(a, b, na, down, D);
+  ce_transpose_kernel<T, FINE><<<dim3(na + nb, over(D, 64)), 256, 0, s>>>(a, b, na, down, D);
 }
 void set_chunks(TransposeJob& j) {
   j.per = std::max(64, over(j.rows, CHUNKS));
@@ -1071,7 +1087,8 @@ size_t linear_ce_workspace_bytes(bool f32, int N, int D, int V, bool backward) {
   // (few rows: the logits may come from tiles, whose scratch lies where the parts of dx do afterwards)
   const size_t few = is_few(N, V) ? few_parts_at(N, V) + std::max(few_ce_bytes(f32, N, V, D), f32 ? 0 : Plan(f32, N, D, V, false, false).bytes) : 0;
   if (backward && few && always_few(f32, N)) return few;
-  const size_t bytes = std::max(Plan(f32, N, D, V, backward).bytes, backward ? few : 0);
+  // (backward: dw may be wanted in either type)
+  const size_t bytes = std::max({Plan(f32, N, D, V, backward).bytes, backward && !f32 ? Plan(f32, N, D, V, true, true, true).bytes : 0, backward ? few : 0});
   return !backward && (is_small(N, D, V) || (few && always_few(f32, N))) ? std::max(bytes, small_ce_bytes(N, V)) : bytes;
 }
 
@@ -1125,13 +1142,18 @@ bool keeps(bool f32, int N, int D, int V) { return small_ce_bytes(N, V) <= SMALL
 // little work: its logits, in scratch, turned into what the tiles leave (in one piece)
 bool takes_turn(const LinearCe& a, const Plan& p, const Way& way) { return way.little && p.Vc >= a.V; }
 
+// dw in fp32 beside bf16 operands
+bool is_fine(const LinearCe& a) { return !a.f32 && a.dw && a.dw_f32; }
+Plan backward_plan(const LinearCe& a) { return Plan(a.f32, a.N, a.D, a.V, true, true, is_fine(a)); }
+
 // What a forward on the same workspace has left: nothing, the packed operands (of one piece), or the logits (z)
 enum Ready { NOTHING, PACKED, KEPT };
-template <typename T>
+template <typename T, bool FINE>
 void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int TERMS = F32 ? 2 : 1;
-  const Plan p(F32, a.N, a.D, a.V, true);
+  const Plan p = backward_plan(a);
+  const int xterms = FINE && a.row_grad ? 2 : TERMS, gterms = FINE ? 2 : TERMS;             // of x and G transposed
   char* ws = (char*)a.workspace;
   const Way way(a);
   const bool direct_x = way.x, direct_w = way.w;
@@ -1149,33 +1171,35 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
     TransposeJob tx, tw;
     if (a.dw && begin) {
       tx.x = a.x; tx.ldx = a.ldx; tx.rows = a.N; tx.rw.labels = a.labels; tx.rw.row_grad = a.row_grad; tx.rw.classes = a.V;
-      tx.most = (uint32_t*)(ws + p.mostx); tx.to = xT; tx.cols = p.Np; tx.ld = TERMS * p.Np; tx.exps = (int*)(ws + p.exT);
+      tx.most = (uint32_t*)(ws + p.mostx); tx.to = xT; tx.cols = p.Np; tx.ld = xterms * p.Np; tx.exps = (int*)(ws + p.exT);
+      tx.both = xterms == 2;
       set_chunks(tx);
     }
     if (a.dx) {
       tw.x = wv; tw.ldx = a.ldw; tw.rows = n; tw.most = (uint32_t*)(ws + p.mostw); tw.to = wT; tw.cols = np; tw.ld = TERMS * np; tw.exps = (int*)(ws + p.ewT);
       set_chunks(tw);
     }
-    transpose<T>(tx, tw, a.D, s);
+    transpose<T, FINE>(tx, tw, a.D, s);
     CeGemm g = logits_gemm(a, p, x, w, v0, n);
     g.stats = (const float2*)a.stats; g.row_grad = a.row_grad;
     if (a.dx) { g.G = G; g.kg = np; g.ldg = TERMS * np; }
-    if (a.dw) { g.GT = GT; g.kgt = p.Np; g.ldgt = TERMS * p.Np; }
+    if (a.dw) { g.GT = GT; g.kgt = p.Np; g.ldgt = gterms * p.Np; }
     if (a.db) { g.dbp = (float*)(ws + p.dbp); g.ldd = p.ldd; }
     const int shape = logits_shape(a.N, n, g.nk * tile_work(F32)), rows = a.dw ? p.Np : a.N, tall = turned ? 64 : rows_of(shape);
     if (turned) {
       if (ready != KEPT) small_ce_logits(a, (float*)(ws + p.z), s);
-      ce_turn_kernel<TERMS><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(ready == KEPT ? z : (const float*)(ws + p.z), small_ce_stride(a.N, a.V), g);
+      ce_turn_kernel<TERMS, FINE><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(ready == KEPT ? z : (const float*)(ws + p.z), small_ce_stride(a.N, a.V), g);
     } else if (a.db) {
-      logits<GRAD, F32, TERMS, true>(shape, g, rows, s);
+      logits<GRAD, F32, TERMS, true, FINE>(shape, g, rows, s);
     } else {
-      logits<GRAD, F32, TERMS, false>(shape, g, rows, s);
+      logits<GRAD, F32, TERMS, false, FINE>(shape, g, rows, s);
     }
     CeGemm ox, ow;
     SumJob sx, sw, sb;
     if (a.dx) {
       ox.A = G; ox.lda = g.ldg; ox.B = wT; ox.ldb = tw.ld; ox.eb = tw.exps;
       ox.M = a.N; ox.N = a.D; ox.nk = TERMS * np / BK; ox.splits = p.split.x; ox.per = over(ox.nk, ox.splits);
+      ox.pass = ox.nk;
       ox.part = (float*)(ws + p.dxp); ox.ldp = p.Dq; ox.tp = (int64_t)a.N * p.Dq; ox.add = !begin;
       if (end) {
         sx.part = ox.part; sx.parts = ox.splits; sx.tp = ox.tp; sx.ldp = p.Dq; sx.rows = a.N; sx.cols = a.D; sx.scale = a.grad_scale; sx.rw.labels = a.labels; sx.rw.row_grad = a.row_grad; sx.rw.classes = a.V;
@@ -1183,8 +1207,8 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
       }
     }
     if (a.dw) {
-      ow.A = GT; ow.lda = g.ldgt; ow.B = xT; ow.ldb = TERMS * p.Np; ow.eb = (int*)(ws + p.exT);
-      ow.M = n; ow.N = a.D; ow.nk = TERMS * p.Np / BK; ow.splits = p.split.w; ow.per = over(ow.nk, ow.splits); ow.scale = a.grad_scale;
+      ow.A = GT; ow.lda = g.ldgt; ow.B = xT; ow.ldb = xterms * p.Np; ow.eb = (int*)(ws + p.exT);
+      ow.M = n; ow.N = a.D; ow.nk = (FINE ? 1 + xterms : TERMS) * p.Np / BK; ow.pass = p.Np / BK; ow.splits = p.split.w; ow.per = over(ow.nk, ow.splits); ow.scale = a.grad_scale;
       char* dw = (char*)a.dw + v0 * a.lddw * (a.dw_f32 ? 4 : 2);
       if (ow.splits > 1) {
         ow.part = (float*)(ws + p.dwp); ow.ldp = p.Dq; ow.tp = (int64_t)n * p.Dq;
@@ -1195,8 +1219,8 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
       }
     }
     if (a.dx || a.dw) {
-      if (p.split.shape == SMALL) launch_grads<Small, TERMS>(ox, ow, s);
-      else launch_grads<Large, TERMS>(ox, ow, s);
+      if (p.split.shape == SMALL) launch_grads<Small, TERMS, FINE>(ox, ow, s);
+      else launch_grads<Large, TERMS, FINE>(ox, ow, s);
     }
     if (a.db) {
       sb.part = g.dbp; sb.parts = over(rows, tall); sb.tp = p.ldd; sb.rows = 1; sb.cols = n; sb.scale = a.grad_scale; sb.out = a.db + v0; sb.f32 = true; sb.blocks = over(over(n, 4), 256);
@@ -1205,8 +1229,9 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
   }
 }
 static void backward_with(const LinearCe& a, Ready ready, const float* z, hipStream_t s) {
-  if (a.f32) backward_as<float>(a, ready, z, s);
-  else backward_as<bf16>(a, ready, z, s);
+  if (a.f32) backward_as<float, false>(a, ready, z, s);
+  else if (is_fine(a)) backward_as<bf16, true>(a, ready, z, s);
+  else backward_as<bf16, false>(a, ready, z, s);
 }
 static void no_tokens(const LinearCe& a, hipStream_t s) {
   const unsigned grid = (unsigned)std::min(a.V, 4096);
@@ -1247,7 +1272,7 @@ void linear_ce_both(const LinearCe& a, hipStream_t s) {
   } else if (way.few) {
     few_backward(a, true, s);
   } else {
-    const Plan f(a.f32, a.N, a.D, a.V, false), p(a.f32, a.N, a.D, a.V, true);
+    const Plan f(a.f32, a.N, a.D, a.V, false), p = backward_plan(a);
     const bool one = p.Vc >= a.V && (way.w ? f.Vs : f.Vp) >= a.V;        // one piece in both
     if (takes_turn(a, p, way)) {
       float* z = (float*)((char*)a.workspace + p.z);

@@ -1,0 +1,68 @@
+"""The weight's gradient of the cross-entropy of a linear layer in fp32 beside bf16 operands, against 64 bits: it keeps the bits that an fp32 sum of fp32 terms has, more than
+the one fp16 term of G that is enough for a bf16 result.
+
+Tolerances, from the arithmetic, as parts of 2-norms (|A B| <= |A| times the largest singular value of B).  A logit is off by e_z = (D / 16 + 20) 2^-24 of the sum of its terms' sizes, a probability by
+a factor 1 + 2 e_z + 2^-20 (1 + the distance to the maximum); G is two fp16 terms, off by 2^-22 of itself, or by 2^-39.  x is exact; times a weight it is two terms as well, off by 2^-22, and the product of the
+low terms that is left out is another 2^-22.  The sums have up to three products a row: (3 N / 16 + 60) 2^-24 of the terms' sizes.  Up to 64 rows G is two bf16 terms, off by 2^-17 of itself.
+One fp16 term would be off by 2^-12 of G over the root of three, which is more than all of that together but for the two sizes of many rows and few features."""
+import pytest
+
+from test_gpu_linear_ce import make
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a HIP device")
+    import paper_2405_10951_amd as P
+    return torch, P
+
+
+def check(torch, x, w, labels, bias, weight, scale, dw):
+    N, D = x.shape
+    V = len(w)
+    xd, wd = x.double(), w.double()
+    z = xd @ wd.t() + bias.double()
+    some = ((labels >= 0) & (labels < V))
+    by = torch.where(some, 1.0 if weight is None else weight.double(), 0.0)[:, None]
+    p = torch.softmax(z, 1)
+    G = p.clone()
+    G[torch.arange(N, device="cuda"), torch.where(some, labels, 0).long()] -= 1
+    ez = (D / 16 + 20) * 2.0 ** -24 * (xd.abs() @ wd.abs().t())
+    off = by.abs() * (p * (2 * ez + 2.0 ** -20 * (1 + z.amax(1, keepdim=True) - z)) + (2.0 ** -17 if N <= 64 else 2.0 ** -22) * G.abs() + 2.0 ** -39)
+    G *= by
+    want = G.t() @ xd
+    terms = (G.abs().t() @ xd.abs()).norm()
+    bound = off.norm() * torch.linalg.matrix_norm(xd, 2) + (2.0 ** -21 + (3 * N / 16 + 60) * 2.0 ** -24) * terms + 2.0 ** -24 * want.norm()
+    err = (dw.double() / scale - want).norm()
+    one_term = 2.0 ** -12 / 3 ** 0.5 * want.norm()
+    assert err <= bound, f"off by {err / want.norm():.3g} of the norm, {bound / want.norm():.3g} allowed"
+    return err, bound, one_term
+
+
+# little work, its logits turned into G; tiles of every shape, with x and w as they lie and packed; several workgroups over the rows; several pieces of classes; few rows
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("N,D,V", [(130, 96, 400), (300, 128, 9000), (700, 512, 1500), (333, 1000, 5003), (65, 64, 1000), (6304, 64, 300), (1100, 200, 2600), (9000, 64, 20000), (2048, 768, 21841),
+                                   (64, 512, 3000)])
+def test_dw_in_fp32_beside_bf16(env, N, D, V, weights):
+    torch, P = env
+    x, w, labels, b = make(torch, N, D, V, "bf16", 60)
+    weight = (0.5 + torch.rand(N, generator=torch.Generator().manual_seed(61))).cuda() if weights else None
+    scale = 2.0 ** -10
+    _, stats = P.bsr_linear_ce_forward(x, w, labels, bias=b)
+    dx, dw, db = P.bsr_linear_ce_backward(x, w, labels, stats, bias=b, row_grad=weight, grad_scale=scale, dw=torch.empty(V, D, device="cuda"))
+    err, bound, one_term = check(torch, x, w, labels, b, weight, scale, dw)
+    print(f"{N}x{D}x{V}: error {err:.3g}, allowed {bound:.3g}, of one term {one_term:.3g}")
+    # alone, and in one call with the loss
+    _, alone, _ = P.bsr_linear_ce_backward(x, w, labels, stats, bias=b, row_grad=weight, grad_scale=scale, dw=torch.empty(V, D, device="cuda"), need_dx=False, need_db=False)
+    check(torch, x, w, labels, b, weight, scale, alone)
+    _, dx2, dw2, db2 = P.bsr_linear_ce_forward_backward(x, w, labels, bias=b, row_grad=weight, grad_scale=scale, dw=torch.empty(V, D, device="cuda"))
+    check(torch, x, w, labels, b, weight, scale, dw2)
+    # the other results as beside a bf16 dw
+    ox, ow, ob = P.bsr_linear_ce_backward(x, w, labels, stats, bias=b, row_grad=weight, grad_scale=scale)
+    assert torch.equal(dw.bfloat16(), ow) or (dw.double() - ow.double()).norm() < 2.0 ** -8 * dw.double().norm()
+    for a, c in ((dx, ox), (dx2, ox), (db, ob), (db2, ob)):
+        assert (a.double() - c.double()).norm() <= 2.0 ** -8 * c.double().norm()
