@@ -9,7 +9,7 @@
 // largest value lies in 2^14 .. 2^15, which is exact for bf16 values down to 2^-29 of the feature's largest.  The matrix instructions take both types at one rate.  fp32 operands are two fp16 terms each,
 // h + l with h = fp16(v), l = fp16(v - h), off by 2^-22 of the value, and the products h h, l h, h l are added in fp32.  A k-tile holds both terms of 32 k: it is loaded
 // once for the three of them (333 x 1001 x 5003 loss and gradients 93 us; one product after another over the whole contraction 109, k-tile by k-tile 107).
-// dw in fp32 beside bf16 operands: one fp16 term of G would show in it (off by 1.3e-4 of its norm, two terms 4e-7 at 2048 x 768 x 21841), so the transposed G has two, and so has x times a weight; the products
+// dw in fp32 beside bf16 operands: one fp16 term of G would show in it (with weights off by 8e-5 of its norm, two terms by 4.5e-7, at 2048 x 768 x 21841), so the transposed G has two, and so has x times a weight; the products
 // h h, l h and, with weights, h l follow one another over a contraction of two or three times the tokens (6304 x 768 x 21841 loss and gradients 1423 us, with weights 1670; dw in bf16 1072).  In a bf16 result G's
 // one term does not show: 2048 x 768 x 21841 dw is off by 1.662e-3 of its norm, from exact G by 1.659e-3, the rounding of the result.
 // Bound by the matrix unit's power where it is large: at 4096 x 4096 x 131072 bf16 a tile of 16 x 16 x 32 instructions runs at 1.7 - 1.8 GHz (32 x 32 x 16 at 1.46, 6 % slower in all), the forward at
@@ -843,11 +843,13 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* __restrict_
 }
 
 // out = scale weight[m] (sum over the parts, in order), 0 for rows that do not count, whatever w and their weight hold; parts of db are rows of tokens
+// db has a part for each 64 to 256 tokens, 65536 at most: from 16 on several threads (ways) share four classes and add up in fp64, every ways-th part each and then those sums in order.
+// (Gradients of 4194304 x 16 x 20 bf16 4273 us, one thread a sum 7790; 200000 x 64 x 1000 1077 and 1830; 32768 x 64 x 131072 10870 and 13010; 4096 x 64 x 65536 600 and 611.)
 struct SumJob {
   const float* part = nullptr; int parts = 0; int64_t tp = 0, ldp = 0, rows = 0; int cols = 0;
   float scale = 1.f; RowWeights rw;                // rows by their weights
   void* out = nullptr; int64_t ldo = 0; bool f32 = false;
-  int blocks = 0;
+  int ways = 1, blocks = 0;
 };
 template <typename T> __device__ __forceinline__ void put_four(T* to, f32x4 v, int have) {
   if (have >= 4 && ((uintptr_t)to & (4 * sizeof(T) - 1)) == 0) {
@@ -859,6 +861,7 @@ template <typename T> __device__ __forceinline__ void put_four(T* to, f32x4 v, i
   }
 }
 // dx, dw and db, or some of them, in one launch
+template <bool WAYS>
 __global__ __launch_bounds__(256) void ce_sums_kernel(SumJob a, SumJob b, SumJob c) {
   int block = blockIdx.x;
   SumJob j = a;
@@ -869,6 +872,27 @@ __global__ __launch_bounds__(256) void ce_sums_kernel(SumJob a, SumJob b, SumJob
       block -= b.blocks;
       j = c;
     }
+  }
+  if constexpr (WAYS) if (j.ways > 1) {            // (one row, fp32)
+    __shared__ double red[4][256];
+    const int wide = 256 / j.ways, way = threadIdx.x / wide, n = (block * wide + threadIdx.x % wide) * 4;
+    double v[4] = {0.0, 0.0, 0.0, 0.0};
+    if (n < j.cols)
+#pragma unroll 8
+      for (int s = way; s < j.parts; s += j.ways) {
+        const f32x4 p = *(const f32x4*)(j.part + s * j.tp + n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += (double)p[e];
+      }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[e][threadIdx.x] = v[e];
+    __syncthreads();
+    if (way > 0 || n >= j.cols) return;
+    for (int i = 1; i < j.ways; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += red[e][i * wide + threadIdx.x];
+    put_four((float*)j.out + n, f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]} * j.scale, j.cols - n);
+    return;
   }
   const int64_t i = (int64_t)block * 256 + threadIdx.x, chunks = (j.cols + 3) / 4, m = i / chunks;
   const int n = (int)(i - m * chunks) * 4;
@@ -1223,9 +1247,12 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
       else launch_grads<Large, TERMS, FINE>(ox, ow, s);
     }
     if (a.db) {
-      sb.part = g.dbp; sb.parts = over(rows, tall); sb.tp = p.ldd; sb.rows = 1; sb.cols = n; sb.scale = a.grad_scale; sb.out = a.db + v0; sb.f32 = true; sb.blocks = over(over(n, 4), 256);
+      sb.part = g.dbp; sb.parts = over(rows, tall); sb.tp = p.ldd; sb.rows = 1; sb.cols = n; sb.scale = a.grad_scale; sb.out = a.db + v0; sb.f32 = true;
+      sb.ways = sb.parts < 16 ? 1 : sb.parts < 512 ? 16 : 64; sb.blocks = over(over(n, 4), 256 / sb.ways);
     }
-    if (sx.blocks + sw.blocks + sb.blocks > 0) ce_sums_kernel<<<sx.blocks + sw.blocks + sb.blocks, 256, 0, s>>>(sx, sw, sb);
+    const int blocks = sx.blocks + sw.blocks + sb.blocks;
+    if (sb.ways > 1) ce_sums_kernel<true><<<blocks, 256, 0, s>>>(sx, sw, sb);
+    else if (blocks > 0) ce_sums_kernel<false><<<blocks, 256, 0, s>>>(sx, sw, sb);
   }
 }
 static void backward_with(const LinearCe& a, Ready ready, const float* z, hipStream_t s) {
