@@ -592,7 +592,7 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
  *   dx = G w,   dw = G^T x,   db = sum over rows of G
  * A row whose label lies outside 0 .. classes-1 has loss 0 and counts for no gradient (its dx is 0), whatever its x and its row_grad hold; so does, for the gradients, one of weight 0.  A class with
  * bias -inf has probability 0; a row whose logits are all -inf has loss and gradient 0, one whose label's is has loss +inf and a finite gradient.  NaN and +inf in z make a row NaN, and with it dw.
- * bf16 x and w are multiplied as they are; G is held in 11 bits (fp16, off by 2^-12 of itself, or by 2^-39 where it is below 2^-28), x and w beside it exactly down to 2^-29 of a feature's
+ * bf16 x and w are multiplied as they are; G is held in 11 bits (fp16, off by 2^-11 of itself, or by 2^-39 where it is below 2^-28), x and w beside it exactly down to 2^-29 of a feature's
  * largest value (with row_grad x in 11 bits too).  For dw in fp32 G, and x times row_grad, have two terms, off by 2^-22 of themselves: half as long again for the products.  Of up to 64 rows G is two terms in
  * bf16 whatever dw is, off by 2^-17.  fp32 values are held in two terms of 11 bits each, off by 2^-22 of themselves, or by 2^-39 of the largest of their row, or of their feature, where they are below 2^-17 of it.  Sums
  * are fp32.
@@ -606,6 +606,11 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
  * No result may touch an input, another result or the workspace.
  * bsr_linear_ce_forward_backward: one after the other, the second with what the first leaves in the workspace: packed operands, and logits where 16 MB hold them all.
  * Limits: rows up to 2^22 (2^21 fp32), width up to 2^20, their product up to 2^33; classes up to 2^30.
+ * bsr_linear_ce_tiles: how the forward and the backward (each by itself) go about such sizes, for inspection and tests (host only).  aligned: whether rows of x and w start on 16-byte boundaries; dw_type: of a dw
+ *   that is wanted.  Writes up to `max` of nine numbers to out (host) and returns 9, or an error (below 0):
+ *   0 tile of the forward's logits (1000000 x stages + 1000 x rows + columns; 0: without tiles), 1 pieces of the classes, 2 tile of the last piece
+ *   3 tile of the backward's logits (0: without), 4 pieces (0: few rows, in one pass over w), 5 tile of the last piece
+ *   6 tile of the products for dx and dw, 7 and 8 workgroups over the contraction of a tile of each
  */
 size_t bsr_linear_ce_workspace_bytes(int32_t type, int64_t rows, int32_t width, int32_t classes, int32_t what);
 int32_t bsr_linear_ce_forward(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t type, int64_t rows, int32_t width, int32_t classes, const float* bias,
@@ -616,6 +621,7 @@ int32_t bsr_linear_ce_backward(const void* x, int64_t ldx, const void* w, int64_
 int32_t bsr_linear_ce_forward_backward(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t type, int64_t rows, int32_t width, int32_t classes, const float* bias,
                                        const int32_t* labels, float* loss, const float* row_grad, float grad_scale, void* dx, int64_t lddx, void* dw, int64_t lddw, int32_t dw_type,
                                        float* db, void* workspace, size_t workspace_bytes, void* stream);
+int32_t bsr_linear_ce_tiles(int32_t type, int64_t rows, int32_t width, int32_t classes, int32_t aligned, int32_t dw_type, int32_t* out, int32_t max);
 
 /*
  * The norm of many gradients taken together, and the gradients brought down to a largest norm: norm = sqrt(sum over tensors and values of g^2),

@@ -6,6 +6,6 @@ from .binding import (BSR_BF16, BSR_FP32, BSR_LOSS_CE, BSR_LOSS_MEAN_SQ, BSR_SUM
                       bsr_attention_backward, bsr_attention_forward, bsr_gemm_tile_shapes, bsr_linear_backward, bsr_linear_dgrad, bsr_linear_forward, bsr_linear_wgrad, bsr_linear_wgrad_static,
                       bsr_distill_backward, bsr_distill_forward, bsr_distill_forward_backward, bsr_layernorm_backward, bsr_layernorm_forward,
                       bsr_layernorm_forward8, bsr_linear8_dgrad, bsr_linear8_forward, bsr_quantize8_rows, bsr_quantize8_weight,
-                      bsr_clip_grads, bsr_grad_norm, bsr_linear_ce_backward, bsr_linear_ce_forward, bsr_linear_ce_forward_backward, bsr_rmsnorm_backward, bsr_rmsnorm_forward, bsr_rmsnorm_forward8,
+                      bsr_clip_grads, bsr_grad_norm, bsr_linear_ce_backward, bsr_linear_ce_forward, bsr_linear_ce_forward_backward, bsr_linear_ce_tiles, bsr_rmsnorm_backward, bsr_rmsnorm_forward, bsr_rmsnorm_forward8,
                       bsr_ln_linear_fold, bsr_ln_linear_forward, bsr_saved_activation_bytes, bsr_token_schedule,
                       bsr_workspace_bytes, lib_path, load_library, make_config)

@@ -2,6 +2,7 @@
 as device memory, the stream is torch's current HIP stream.  Same names as the C entry points."""
 from __future__ import annotations
 
+import collections
 import ctypes as C
 import functools
 import os
@@ -141,6 +142,7 @@ def load_library():
             "bsr_linear_ce_forward": (p, i64, p, i64, i32, i64, i32, i32, p, p, p, p, p, C.c_size_t, p),
             "bsr_linear_ce_backward": (p, i64, p, i64, i32, i64, i32, i32, p, p, p, p, f32, p, i64, p, i64, i32, p, p, C.c_size_t, p),
             "bsr_linear_ce_forward_backward": (p, i64, p, i64, i32, i64, i32, i32, p, p, p, p, f32, p, i64, p, i64, i32, p, p, C.c_size_t, p),
+            "bsr_linear_ce_tiles": (i32, i64, i32, i32, i32, i32, p, i32),
             "bsr_clip_grads": (p, p, p, i32, f32, p, p, p, C.c_size_t, p),
             "bsr_quantize8_rows": (p, i32, i64, i32, i64, p, p, p),
             "bsr_quantize8_weight": (p, i32, i32, i32, i64, p, p, p, p, p),
@@ -879,6 +881,18 @@ def bsr_linear_ce_forward_backward(x, w, labels, bias=None, row_grad=None, grad_
     ws, size = _linear_ce_workspace(x, args, 2)
     _check(load_library().bsr_linear_ce_forward_backward(*args, loss.data_ptr(), pg, grad_scale, *out, _dp(ws), size, stream))
     return loss, dx, dw, db
+
+
+LinearCeTiles = collections.namedtuple("LinearCeTiles", "forward forward_pieces forward_last gradient pieces gradient_last products splits_x splits_w")
+
+
+def bsr_linear_ce_tiles(rows, width, classes, dtype, aligned=True, dw_dtype=None):
+    """How bsr_linear_ce_forward and bsr_linear_ce_backward go about such sizes (see include/bsr.h); host only."""
+    code = {"bf16": BSR_BF16, "fp32": BSR_FP32}
+    out = (C.c_int32 * len(LinearCeTiles._fields))()
+    n = load_library().bsr_linear_ce_tiles(code[dtype], rows, width, classes, aligned, code[dw_dtype or dtype], out, len(out))
+    _check(min(n, 0))
+    return LinearCeTiles(*out)
 
 
 def _clip_tensors(tensors, what):

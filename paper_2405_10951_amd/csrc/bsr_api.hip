@@ -2091,6 +2091,23 @@ int32_t bsr_linear_ce_forward_backward(const void* x, int64_t ldx, const void* w
   return check_hip(nullptr, what);
 }
 
+int32_t bsr_linear_ce_tiles(int32_t type, int64_t rows, int32_t width, int32_t classes, int32_t aligned, int32_t dw_type, int32_t* out, int32_t max) {
+  const char* what = "bsr_linear_ce_tiles";
+  if (rows < 1 || !linear_ce_takes(type, rows, width, classes)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: type %d, rows %lld, width %d, classes %d", what, type, (long long)rows, width, classes);
+  if (!known_type(dw_type) || (type == BSR_FP32 && dw_type != BSR_FP32)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: dw of type %d for w of type %d", what, dw_type, type);
+  if (max < 0 || (max > 0 && !out)) return fail(nullptr, BSR_ERR_INVALID_ARG, "%s: %d places at NULL", what, max);
+  LinearCe a;
+  a.N = (int)rows; a.D = width; a.V = classes; a.f32 = type == BSR_FP32; a.dw_f32 = dw_type == BSR_FP32;
+  // (addresses that are only looked at)
+  a.x = a.w = a.dw = (void*)(uintptr_t)(aligned ? 256 : 2);
+  a.ldx = a.ldw = ((int64_t)width + 63) / 64 * 64;
+  LinearCeTiles t;
+  linear_ce_tiles(a, t);
+  const int32_t all[] = {t.forward, t.forward_pieces, t.forward_last, t.gradient, t.pieces, t.gradient_last, t.products, t.splits_x, t.splits_w};
+  for (int i = 0; i < max && i < (int)(sizeof(all) / sizeof(all[0])); ++i) out[i] = all[i];
+  return (int32_t)(sizeof(all) / sizeof(all[0]));
+}
+
 size_t bsr_clip_workspace_bytes(int32_t count) { return clip_workspace_bytes(count); }
 
 // whether results lie apart: from each other, and from every gradient but the one that they are

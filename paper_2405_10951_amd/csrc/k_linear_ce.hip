@@ -346,7 +346,7 @@ template <int N> __device__ __forceinline__ float lanes16_sums(float (&v)[N]) {
 }
 
 // Backward: the tile as G, in fp16 times 2^14, rows of 32 tokens at a time through a patch of LDS, from which rows are read as they lie and, with the transposing reads, columns
-// FINE (of bf16 operands): the transposed G in two terms, one behind the other.  dw is wanted in fp32, and one fp16 term would be off by up to 2^-12 of G's largest values
+// FINE (of bf16 operands): the transposed G in two terms, one behind the other.  dw is wanted in fp32, and one fp16 term would be off by up to 2^-11 of itself
 template <class S, bool F16, int TERMS, bool DB, bool FINE>
 __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S::NI], int m0, int n0, int tm, unsigned char* smem) {
   constexpr int NI = S::NI, TERM = 32 * S::LDR, KEPT = FINE ? 2 : TERMS;
@@ -1098,6 +1098,9 @@ bool few_tiles(int N, int V, double kt) {
   return (int64_t)over(N, rows_of(shape)) * over(V, cols_of(shape)) < 64;
 }
 
+// tiles of the logits of n classes
+int logits_shape(const LinearCe& a, const Plan& p, int n) { return logits_shape(a.N, n, (a.f32 ? 2 : 1) * p.Dp / BK * tile_work(a.f32)); }
+
 CeGemm logits_gemm(const LinearCe& a, const Plan& p, const Rows& x, const Rows& w, int v0, int n) {
   CeGemm g;
   g.A = x.p; g.lda = x.ld; g.ea = x.exps; g.B = w.p; g.ldb = w.ld; g.eb = w.exps;
@@ -1126,13 +1129,14 @@ struct Way {
              ((double)a.N * a.D * a.V <= SMALL_WORK && (!x || !w) || few_tiles(a.N, a.V, logits_work(a.f32, over(a.D, BK))));
     few = is_few(a.N, a.V) && (always_few(a.f32, a.N) || w || little);
   }
+  bool straight() const { return little || (few && !w); }        // the forward's logits without tiles
 };
 
 // z: where the logits are kept as well (in one piece, and not of little work), or null;  packs: whether the workspace has room for w packed
 static void forward_with(const LinearCe& a, float* z, bool packs, hipStream_t s) {
   const Way way(a);
   const bool direct_x = way.x, direct_w = way.w;
-  if (way.little || (way.few && !way.w)) {
+  if (way.straight()) {
     small_ce_forward(a, (float*)a.workspace, false, s);
     return;
   }
@@ -1149,7 +1153,7 @@ static void forward_with(const LinearCe& a, float* z, bool packs, hipStream_t s)
     pack(v0 == 0 ? px : PackJob(), pw, a.f32, a.D, p.Dp, s);
     CeGemm g = logits_gemm(a, p, x, w, v0, n);
     g.parts = (float2*)(ws + p.parts); g.zlabel = (float*)(ws + p.zlabel); g.z = z; g.ldz = small_ce_stride(a.N, a.V);
-    const int shape = logits_shape(a.N, n, g.nk * tile_work(a.f32));
+    const int shape = logits_shape(a, p, n);
     if (a.f32) logits<STATS, true, 2, false>(shape, g, a.N, s);
     else logits<STATS, false, 1, false>(shape, g, a.N, s);
     if (a.loss || a.stats)
@@ -1209,7 +1213,7 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
     if (a.dx) { g.G = G; g.kg = np; g.ldg = TERMS * np; }
     if (a.dw) { g.GT = GT; g.kgt = p.Np; g.ldgt = gterms * p.Np; }
     if (a.db) { g.dbp = (float*)(ws + p.dbp); g.ldd = p.ldd; }
-    const int shape = logits_shape(a.N, n, g.nk * tile_work(F32)), rows = a.dw ? p.Np : a.N, tall = turned ? 64 : rows_of(shape);
+    const int shape = logits_shape(a, p, n), rows = a.dw ? p.Np : a.N, tall = turned ? 64 : rows_of(shape);
     if (turned) {
       if (ready != KEPT) small_ce_logits(a, (float*)(ws + p.z), s);
       ce_turn_kernel<TERMS, FINE><<<dim3(np / 64, over(rows, 64)), 256, 0, s>>>(ready == KEPT ? z : (const float*)(ws + p.z), small_ce_stride(a.N, a.V), g);
@@ -1286,6 +1290,29 @@ void linear_ce_backward(const LinearCe& a, hipStream_t s) {
   if (a.N == 0) no_tokens(a, s);
   else if (Way(a).few) few_backward(a, false, s);
   else backward_with(a, NOTHING, nullptr, s);
+}
+
+void linear_ce_tiles(const LinearCe& a, LinearCeTiles& t) {
+  const Way way(a);
+  const int id[] = {2256256, 3128128, 3064128, 4032256, 2128128};
+  if (!way.straight()) {
+    const Plan p(a.f32, a.N, a.D, a.V, false);
+    const int step = std::min(a.V, way.w ? p.Vs : p.Vp);
+    t.forward_pieces = over(a.V, step);
+    t.forward = id[logits_shape(a, p, step)];
+    t.forward_last = id[logits_shape(a, p, a.V - (t.forward_pieces - 1) * step)];
+  }
+  if (way.few) return;
+  const Plan p = backward_plan(a);
+  const int step = std::min(a.V, p.Vc);
+  t.pieces = over(a.V, step);
+  if (!takes_turn(a, p, way)) {
+    t.gradient = id[logits_shape(a, p, step)];
+    t.gradient_last = id[logits_shape(a, p, a.V - (t.pieces - 1) * step)];
+  }
+  t.products = id[p.split.shape == SMALL ? SMALL : LARGE];
+  t.splits_x = p.split.x;
+  t.splits_w = p.split.w;
 }
 
 static size_t both_kept_at(bool f32, int N, int D, int V) {

@@ -23,6 +23,9 @@ void linear_ce_backward(const LinearCe& a, hipStream_t s);
 // one after the other, the second with what the first leaves; stats (not null) is written
 size_t linear_ce_both_bytes(bool f32, int N, int D, int V);
 void linear_ce_both(const LinearCe& a, hipStream_t s);
+// what the forward and the backward of their own take, as bsr.h says; host only
+struct LinearCeTiles { int32_t forward = 0, forward_pieces = 0, forward_last = 0, gradient = 0, pieces = 0, gradient_last = 0, products = 0, splits_x = 0, splits_w = 0; };
+void linear_ce_tiles(const LinearCe& a, LinearCeTiles& t);
 
 // k_linear_ce_small.hip: scratch of small_ce_bytes() for the logits, or for G, with grad_scale and the rows' weights, [N, small_ce_stride()]
 inline int64_t small_ce_stride(int N, int V) { return N <= 64 ? ((int64_t)V + 15) / 16 * 16 : ((int64_t)V + 3) / 4 * 4; }

@@ -4,7 +4,7 @@ the one fp16 term of G that is enough for a bf16 result.
 Tolerances, from the arithmetic, as parts of 2-norms (|A B| <= |A| times the largest singular value of B).  A logit is off by e_z = (D / 16 + 20) 2^-24 of the sum of its terms' sizes, a probability by
 a factor 1 + 2 e_z + 2^-20 (1 + the distance to the maximum); G is two fp16 terms, off by 2^-22 of itself, or by 2^-39.  x is exact; times a weight it is two terms as well, off by 2^-22, and the product of the
 low terms that is left out is another 2^-22.  The sums have up to three products a row: (3 N / 16 + 60) 2^-24 of the terms' sizes.  Up to 64 rows G is two bf16 terms, off by 2^-17 of itself.
-One fp16 term would be off by 2^-12 of G over the root of three, which is more than all of that together but for the two sizes of many rows and few features."""
+One fp16 term would be off by up to 2^-11 of itself, half of that over the root of three at least in the root mean square, which is more than all of that together but for the two sizes of many rows and few features."""
 import pytest
 
 from test_gpu_linear_ce import make
