@@ -78,7 +78,8 @@ template <int BM_, int BN_, int WM_, int WN_, int NST_> struct Shape {
   static constexpr int at_once = (int)(160 * 1024 / lds), wavefronts = at_once * (NT / 64) / 4;       // workgroups a CU, wavefronts a SIMD
 };
 typedef Shape<256, 256, 2, 4, 2> Large;
-typedef Shape<256, 256, 2, 2, 2> LargeForward;     // (four wavefronts read a third less of LDS for the product, eight share the work of ending a tile)
+typedef Shape<256, 256, 2, 2, 2> LargeForward;     // (bf16: four wavefronts read a third less of LDS for the product, eight share the work of ending a tile; of two terms eight are faster,
+                                                   // 2048 x 768 x 21841 196 us against 224, and need no register that four would spill)
 typedef Shape<128, 128, 2, 4, 3> Small;
 typedef Shape<64, 128, 2, 2, 3> Mid;                  // (logits only: where larger tiles would leave CUs idle)
 typedef Shape<128, 128, 2, 4, 2> Short;               // (logits only: of few k-tiles, two workgroups a CU, so that one's products cover the other's beginning and end)
@@ -380,9 +381,11 @@ __device__ __forceinline__ void end_grad(const CeGemm& g, f32x4 (&acc)[S::MI][S:
       for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[mi][ni][r] = counts && w.col0 + w.col(ni, r) < g.N ? acc[mi][ni][r] : 0.f;
-    if constexpr (DB)
+    if constexpr (DB) {
+      const float by = counts ? weight : 0.f;
 #pragma unroll
-      for (int i = 0; i < NI * 4; ++i) sum[i] = counts ? fmaf(weight, acc[mi][i / 4][i % 4], sum[i]) : sum[i];
+      for (int i = 0; i < NI * 4; ++i) sum[i] = fmaf(by, acc[mi][i / 4][i % 4], sum[i]);
+    }
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) {
       f16x4 h, l;
@@ -940,7 +943,7 @@ template <Mode MODE, bool F16, int TERMS, bool DB, bool FINE = false> void logit
   else if (shape == SHORT) launch_logits<Short, MODE, F16, TERMS, DB, FINE>(g, rows, s);
   else if (shape == MID) launch_logits<Mid, MODE, F16, TERMS, DB, FINE>(g, rows, s);
   else if (shape == SMALL) launch_logits<Small, MODE, F16, TERMS, DB, FINE>(g, rows, s);
-  else launch_logits<std::conditional_t<MODE == STATS, LargeForward, Large>, MODE, F16, TERMS, DB, FINE>(g, rows, s);
+  else launch_logits<std::conditional_t<MODE == STATS && TERMS == 1, LargeForward, Large>, MODE, F16, TERMS, DB, FINE>(g, rows, s);
 }
 template <class S, int TERMS, bool PASSES> void launch_grads(const CeGemm& a, const CeGemm& b, hipStream_t s) {
   auto blocks = [](const CeGemm& g) { return g.A ? over(g.M, S::BM) * over(g.N, S::BN) * g.splits : 0; };
