@@ -847,7 +847,8 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(const float2* __restrict_
 
 // out = scale weight[m] (sum over the parts, in order), 0 for rows that do not count, whatever w and their weight hold; parts of db are rows of tokens
 // db has a part for each 64 to 256 tokens, 65536 at most: from 16 on several threads (ways) share four classes and add up in fp64, every ways-th part each and then those sums in order.
-// (Gradients of 4194304 x 16 x 20 bf16 4273 us, one thread a sum 7790; 200000 x 64 x 1000 1077 and 1830; 32768 x 64 x 131072 10870 and 13010; 4096 x 64 x 65536 600 and 611.)
+// (Gradients of 4194304 x 16 x 20 bf16 4273 us, one thread a sum 7790; 200000 x 64 x 1000 1077 and 1830; 32768 x 64 x 131072 10870 and 13010; 4096 x 64 x 65536 600 and 611.  One, 16 and 64 ways: 1000 x 64 x 65536 162, 162, 168;
+// 32000 x 64 x 4096 381, 323, 320; 262144 x 64 x 4096 9606, 5687, 5610.)
 struct SumJob {
   const float* part = nullptr; int parts = 0; int64_t tp = 0, ldp = 0, rows = 0; int cols = 0;
   float scale = 1.f; RowWeights rw;                // rows by their weights
@@ -1011,7 +1012,11 @@ Split grads_split(int64_t M, int64_t n, int64_t D, int kx, int kw, double work) 
 // What goes to k_linear_ce_small.hip: little work, where the launches count; few rows backward (w is read and dw written once there), and forward where they would have to be packed first.  Its
 // logits take 16 MB at most, those of few rows, of which there is room for 16, 32 or 64, 256
 constexpr size_t SMALL_BYTES = 16 << 20, FEW_BYTES = 256 << 20;
-constexpr double SMALL_WORK = 1 << 28, MOST_SMALL_WORK = 1 << 30;        // tokens x features x classes; where tiles would leave most CUs idle
+// SMALL_WORK, tokens x features x classes: up to there where x or w would have to be packed (forward, without tiles and in tiles: 300 x 200 x 2000 fp32 14.6 and 18.0 us, bf16 17.8 and 18.3; 300 x 500 x 2000, just
+// above, 22.5 and 19.7, 23.2 and 18.3; gradients 100 x 200 x 2000 fp32 31.9 and 34.6, 300 x 500 x 2000 50 and 44).
+// MOST_SMALL_WORK: up to there where fewer than 64 tiles would leave most CUs idle behind long chains (forward, bf16 as it lies: 128 x 4096 x 512 15.7 and 24.5, 256 x 4096 x 512 16.0 and 24.7, 256 x 8192 x 512 26.5 and 42.1, 2^30;
+// with more tiles, 512 x 2048 x 1024, 26.6 and 16.3; with more work, 128 x 4096 x 4096, 48 and 25.4).
+constexpr double SMALL_WORK = 1 << 28, MOST_SMALL_WORK = 1 << 30;
 bool is_small(int N, int D, int V) { return N <= 1 << 20 && small_ce_bytes(N, V) <= SMALL_BYTES && (double)N * D * V <= MOST_SMALL_WORK; }      // (a launch has up to 65535 workgroups one way)
 // (more than 32 rows of a w that would have to be packed: 48 x 1001 x 50000 bf16 318 us here, 291 by tiles)
 bool is_few(int N, int V) { return N <= FEW_ROWS && few_parts_at(N, V) <= FEW_BYTES; }

@@ -487,12 +487,15 @@ template <typename T> __global__ __launch_bounds__(1024) void few_sums_kernel(co
 }
 
 int64_t small_ldz(const LinearCe& a) { return small_ce_stride(a.N, a.V); }
-// (KW 1 where the classes fill the CUs and few features would leave wavefronts without any)
+// Two times 16 classes a workgroup (and four times 16 tokens, fp32) from 2^13 classes on, which fill the CUs then: forward of 32 x 1024 fp32 and 4096 classes 16.1 us, one times 16 14.4; 8192 17.1 and 19.6;
+// 32768 52 and 61; 48 rows of 8192 24.0 and 30.6; 32 x 1000 x 8192 bf16 15.8 and 19.2.
+// Every wavefront with classes of its own (KW 1) for rows of up to 256 bytes of so many, which would leave most of eight without features: 48 x 64 x 100000 fp32 36 us against 42, 500 x 40 x 8192 22.4 and 34.4, 400 x 64
+// x 8192 bf16 23.7 and 34.9; longer rows 48 x 128 x 40000 fp32 29.4 and 24.9, 1 x 250 x 40000 bf16 19.0 and 15.7.
 template <typename T> void logits_as(const LinearCe& a, const Tokens& tk, float* z, hipStream_t s) {
   auto go = [&](auto kernel, int classes, int tokens) {
     kernel<<<dim3(over(a.V, classes), over(a.N, tokens)), LOGIT_WAVES * WAVE, 0, s>>>((const T*)a.x, a.ldx, (const T*)a.w, a.ldw, a.D, a.bias, tk, z, small_ldz(a));
   };
-  const bool many = a.V >= 1 << 15, narrow = many && a.D <= 256;
+  const bool many = a.V >= 1 << 13, narrow = many && a.D * sizeof(T) <= 256;
   if constexpr (sizeof(T) == 4)                    // (as many tokens beside bf16 rows of more features: tiles)
     if (a.N > 32 && many && !narrow) return go(small_logits_kernel<T, 4, 8, 2>, 32, 64);
   if (a.N <= 16) narrow ? go(small_logits_kernel<T, 1, 1, 1>, 128, 16) : many ? go(small_logits_kernel<T, 1, 8, 2>, 32, 16) : go(small_logits_kernel<T, 1, 8, 1>, 16, 16);
