@@ -546,6 +546,8 @@ void small_ce_forward(const LinearCe& a, float* z, bool grad, hipStream_t s) {
   Tokens tk = tokens_of(a);
   logits_of(a, tk, z, s);
   if (grad) tk.rows = 16 * few_tiles_of(a.N);
+  // (forward of 300 x 300 x 2000 fp32 15.5 us with 1024 threads a row, 15.2 with 256; 500 x 60 x 8192 23.2 and 22.8; 4 x 256 x 40000 18.2 and 21.7; 32 x 64 x 100000 27.9 and 35.2; loss and gradients of 16 x 512 x
+  // 8192 27.4 and 28.4, of 16384 36.4 and 40.1)
   if (a.V > 4096) small_rows_kernel<1024><<<tk.rows, 1024, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad);
   else small_rows_kernel<256><<<tk.rows, 256, 0, s>>>(z, small_ldz(a), tk, a.loss, (float2*)a.stats, grad);
 }

@@ -5,9 +5,9 @@ from test_gpu_linear_ce import check, make
 
 pytestmark = pytest.mark.gpu
 
-# (rows, width, classes): classes whose gradients take two launches; those that a row's workgroup of 1024 threads turns; those from which workgroups take two times 16 of them, beside rows of up to 256 bytes
+# (rows, width, classes): classes whose gradients take two launches; those whose rows have 1024 threads, and that a launch of its own turns; those from which workgroups take two times 16 of them, beside rows of up to 256 bytes
 # and longer ones; rows in tiles of 16, 32 and 64; little work by products, and by tiles; logits that are kept between the passes; tiles of rows that one thread or several add up for db
-SIZES = [(20, 100, 128), (20, 100, 129), (20, 100, 256), (20, 100, 257), (20, 70, 4096), (20, 70, 4097), (17, 64, 8191), (17, 64, 8192), (17, 65, 8192), (40, 128, 8192), (40, 129, 8192), (33, 64, 8200),
+SIZES = [(20, 100, 128), (20, 100, 129), (20, 100, 256), (20, 100, 257), (20, 70, 4096), (20, 70, 4097), (20, 70, 32768), (20, 70, 32769), (17, 64, 8191), (17, 64, 8192), (17, 65, 8192), (40, 128, 8192), (40, 129, 8192), (33, 64, 8200),
          (32, 130, 8200), (1, 63, 8192), (16, 300, 8193), (500, 40, 8192), (65, 100, 8193), (64, 200, 700), (65, 200, 700), (300, 200, 2000), (300, 448, 2000), (256, 1024, 512), (256, 1024, 1030), (512, 576, 1024),
          (500, 512, 8384), (500, 512, 8392), (600, 448, 3000), (960, 64, 2200), (1025, 64, 2200)]
 
