@@ -3,10 +3,11 @@
 //   logits   16 classes x 16 or 32 tokens a workgroup, the features split over its eight wavefronts, whole cache lines each (bf16 16 x 16 x 32, fp32 16 x 16 x 4 matrix instructions, both exact products
 //            added in fp32); for the gradients they leave as G
 //   rows     a workgroup a token: maximum, sum, loss
-//   grads    up to 32 tokens in fp32, 64 in bf16: dx and dw in one pass over w, multiplied in fp32 (16 x 16 x 4), or with G in two bf16 terms (16 x 16 x 16)
+//   grads    up to 64 tokens: dx and dw in one pass over w, multiplied in fp32 (16 x 16 x 4), or beside bf16 with G in two bf16 terms (16 x 16 x 32) and, for dw in fp32, a third (16 x 16 x 16)
 // A launch is a chain of a few trips to memory; that, the calls and, for few rows of many classes, the bytes of w and dw are what bounds it.
 // Measured: 32 x 768 x 100 fp32 8 + 11 us; loss and gradients of 48 x 2048 x 100000 fp32 987 (by tiles 2360), of 1 x 100 x 100000 bf16 50; gradients of 32 x 4096 x 100000 bf16 348 (1.6 GB of w and dw: 4.7 TB/s; with fp32 products 728), of 64 rows 580 (two wavefronts a SIMD, of which each waits for a
 // half as long rows' piece; G by columns from memory instead of LDS: 673; 8 features a lane and one wavefront: 660; four wavefronts side by side on G: 690).
+// The third term of G for dw in fp32: loss and gradients of 64 x 4096 x 100000 949 us, of two terms 930; 32 x 4096 x 100000 749 with either; 33 x 2048 x 8000, gradients, 64 and 62.
 #include <algorithm>
 
 #include "linear_ce.h"
@@ -273,6 +274,17 @@ template <> struct Four<bf16> {
     }
   }
 };
+// What two terms leave of G, 8 bits more, for dw in fp32 beside bf16: the third term, of four classes of a token to a tile, and of four tokens of a class from it (as above)
+__device__ __forceinline__ bf16x4 third(f32x4 g, const Four<bf16>& two) {
+  bf16x4 m;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) m[j] = (bf16)((g[j] - (float)two.v[j]) - (float)two.v[4 + j]);
+  return m;
+}
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ s16x4 third_from(bf16 (*tile)[16], int lm, int lq) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)&tile[4 * lq + lm / 4][lm % 4 * 4]);
+}
 __device__ __forceinline__ f32x4 times(const Four<float>& g, f32x4 b, f32x4 c) { return multiplied(g.v, b, c); }
 __device__ __forceinline__ f32x4 times(const Four<bf16>& g, bf16x4 b, f32x4 c) { return multiplied(g.v, bf16x8{b[0], b[1], b[2], b[3], b[0], b[1], b[2], b[3]}, c); }
 
@@ -359,7 +371,8 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(const float* __restri
     for (int i = 0; i < K; ++i) acc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   // G by rows (four classes of token l % 16), 256 MB at most: places in 32 bits; by columns (four tokens of class l % 16) through LDS, in bf16 with its transposing reads
-  constexpr int TERMS = sizeof(T) == 2 ? 2 : 1, LD = sizeof(T) == 2 ? 16 : 20;
+  constexpr bool FINE = sizeof(T) == 2 && sizeof(TW) == 4;         // dw keeps more bits than two terms of G have
+  constexpr int TERMS = sizeof(T) == 2 ? 2 + FINE : 1, LD = sizeof(T) == 2 ? 16 : 20;
   __shared__ __attribute__((aligned(16))) T turn[4][TILES][TERMS][16][LD];
   const unsigned by_row = lm * (unsigned)ldz + 4 * lq;
   vec nb[4];
@@ -397,6 +410,7 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(const float* __restri
       row[t] = Four<T>(nr[t]);
       sum += nr[t];
       row[t].put(turn[wave][t], lm, lq);
+      if constexpr (FINE) *(bf16x4*)&turn[wave][t][TERMS - 1][lm][4 * lq] = third(nr[t], row[t]);
     }
     fetch(v0 + STEP);
     if (want_dx)
@@ -414,6 +428,11 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(const float* __restri
         const Four<T> g(turn[wave][t], lm, lq);
 #pragma unroll
         for (int i = 0; i < K; ++i) out[i] = times(g, xb[t][i], out[i]);
+        if constexpr (FINE) {
+          const s16x4 m = third_from(turn[wave][t][TERMS - 1], lm, lq);
+#pragma unroll
+          for (int i = 0; i < K; ++i) out[i] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(m, __builtin_bit_cast(s16x4, xb[t][i]), out[i], 0, 0, 0);
+        }
       }
       wave_fence();
       auto put_row = [&](int r, bool all) __attribute__((always_inline)) {
