@@ -621,16 +621,31 @@ __device__ __forceinline__ float weight_of(const RowWeights& w, int64_t m) {
 }
 __device__ __forceinline__ float weighted(float v, float by) { return by == 0.f ? 0.f : v * by; }
 
+// A class whose bias is -inf has G 0 but where it is a row's label.  It counts with 0 in dx, so that whatever its row of w holds does not make the features' powers of two larger than the others need.
+// (Looking for such classes costs 2048 x 768 x 21841 3.5 us of 272 where there is a bias.)
+struct Masks { const float* bias = nullptr; const int32_t* labels = nullptr; int tokens = 0, v0 = 0; };      // bias of the piece; null: none is
+// bits of the classes r0 .. r1 that are labels (all threads, behind a barrier of their own)
+__device__ __forceinline__ void mark_labels(const Masks& k, int r0, int r1, uint32_t* bits) {
+  for (int i = threadIdx.x; i < (r1 - r0 + 31) / 32; i += blockDim.x) bits[i] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < k.tokens; i += blockDim.x) {
+    const int at = max(k.labels[i], -1) - k.v0 - r0;
+    if (at >= 0 && at < r1 - r0) atomicOr(bits + at / 32, 1u << at % 32);
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ bool is_masked(const Masks& k, int r, int r0, const uint32_t* bits) { return k.bias[r] == -INFINITY && !(bits[(r - r0) / 32] >> (r - r0) % 32 & 1); }
+
 // [rows, D] -> [D][ld] fp16 in one or two terms, a power of two each of the D rows; what lies between rows and ld is zero.  In two launches, each for x, w or both: the columns' maxima, `chunks`
 // parts of the rows apart, then the rest
 struct TransposeJob {
-  const void* x = nullptr; int64_t ldx = 0; int rows = 0; RowWeights rw;
+  const void* x = nullptr; int64_t ldx = 0; int rows = 0; RowWeights rw; Masks masks;
   int per = 1, chunks = 0;                         // rows of a part; parts (0: no job)
   uint32_t* most = nullptr;                        // [chunks][D] bits of the largest finite |value|
   f16* to = nullptr; int cols = 0; int64_t ld = 0; int* exps = nullptr;           // cols (of one or both terms) of a row are written
   bool both = false;                               // FINE: two terms, one behind the other (of x with weights, which bf16 values times them do not fit one of)
 };
-constexpr int CHUNKS = 64;
+constexpr int CHUNKS = 64, MOST_PART = 1 << 15;    // rows of a part: a piece has 2^21 classes at most (its rows of 64 features 256 MB)
 
 // SIDE pieces of 16 bytes side by side: a cache line, or four where that leaves enough workgroups (131072 x 4096 bf16, eight pieces: 47 against 40 us; 21841 x 768 12 against 21)
 template <typename T, int SIDE>
@@ -642,13 +657,29 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
   const int chunk = first ? blockIdx.y : blockIdx.y - a.chunks, r0 = chunk * j.per, r1 = min(r0 + j.per, j.rows);
   const T* x = (const T*)j.x;
   uint32_t* most = j.most + (int64_t)chunk * D;
+  // (masked classes are looked for beside the loads, the first 256 ahead of them; where there are some, the maxima are made once more without them)
+  const float first_bias = j.masks.bias ? j.masks.bias[min(r0 + (int)threadIdx.x, r1 - 1)] : 0.f;
+  __shared__ uint32_t label_bits[MOST_PART / 32];
+  __shared__ int found[4];
+  auto any_masked = [&]() __attribute__((always_inline)) {
+    if (!j.masks.bias) return false;
+    bool mine = first_bias == -INFINITY;
+    for (int r = r0 + 256 + threadIdx.x; r < r1; r += 256) mine |= j.masks.bias[r] == -INFINITY;
+    const bool wave = __any(mine);
+    if (threadIdx.x % WAVE == 0) found[threadIdx.x / WAVE] = wave;
+    __syncthreads();
+    if (!(found[0] | found[1] | found[2] | found[3])) return false;
+    mark_labels(j.masks, r0, r1, label_bits);
+    return true;
+  };
   if (D < V) {                                     // (no whole piece to read)
     __shared__ uint32_t part[256 / V][V];
     const int c = threadIdx.x % V, i = threadIdx.x / V;
+    const bool some = any_masked();
     uint32_t m = 0;
     if (c < D)
 #pragma unroll 4
-      for (int r = r0 + i; r < r1; r += 256 / V) m = max(m, bits_if_finite(weighted((float)x[r * j.ldx + c], weight_of(j.rw, r))));
+      for (int r = r0 + i; r < r1; r += 256 / V) m = max(m, bits_if_finite(weighted((float)x[r * j.ldx + c], some && is_masked(j.masks, r, r0, label_bits) ? 0.f : weight_of(j.rw, r))));
     part[i][c] = m;
     __syncthreads();
     if ((int)threadIdx.x < D) {
@@ -668,6 +699,16 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
     const float by = weight_of(j.rw, r);
 #pragma unroll
     for (int e = 0; e < V; ++e) m[e] = max(m[e], bits_if_finite(weighted((float)v[e], by)));
+  }
+  if (any_masked()) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) m[e] = 0;
+    for (int r = r0 + threadIdx.x / SIDE; r < r1; r += ABOVE) {
+      if (is_masked(j.masks, r, r0, label_bits)) continue;
+      const typename Loose<T>::vec v = *(const typename Loose<T>::vec*)(x + r * j.ldx + col);
+#pragma unroll
+      for (int e = 0; e < V; ++e) m[e] = max(m[e], bits_if_finite((float)v[e]));
+    }
   }
 #pragma unroll
   for (int e = 0; e < V; ++e) {
@@ -714,12 +755,22 @@ __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, Trans
     }
   };
   fetch(begin);
+  __shared__ uint32_t label_bits[16];              // (down: 8 at most)
+  __shared__ int found[4];
+  float bias[2] = {0.f, 0.f};                      // (of 512 classes)
+  if (j.masks.bias)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) bias[i] = j.masks.bias[min(begin + (int)threadIdx.x + 256 * i, j.rows - 1)];
   uint32_t most = 0;
   if (c0 + lane < D)
 #pragma unroll 4
     for (int k = w; k < j.chunks; k += 4) most = max(most, j.most[(int64_t)k * D + c0 + lane]);
   red[w][lane] = most;
+  const bool masked = __any(bias[0] == -INFINITY || bias[1] == -INFINITY);            // (or a class behind the workgroup's last: looked for in vain)
+  if (lane == 0) found[w] = masked;
   __syncthreads();
+  const bool some = found[0] | found[1] | found[2] | found[3];
+  if (some) mark_labels(j.masks, begin, min(end, j.rows), label_bits);
   if (w == 0) {
     const int e = exponent_of(max(max(red[0][lane], red[1][lane]), max(red[2][lane], red[3][lane])));
     exps[lane] = e;
@@ -727,6 +778,12 @@ __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, Trans
   }
   __syncthreads();
   for (int m0 = begin; m0 < end; m0 += 64) {
+    if (some)
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const int m = m0 + r0 + i * (256 / PER_ROW);
+        if (m < j.rows && is_masked(j.masks, m, begin, label_bits)) by[i] = 0.f;
+      }
 #pragma unroll
     for (int i = 0; i < K; ++i)
 #pragma unroll
@@ -1205,6 +1262,7 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
     PackJob pw;
     const Rows w = rows_operand(wv, a.ldw, F32, n, p.Dp, ws + p.wp, (int*)(ws + p.ew), direct_w, pw);
     if (!turned && ready != PACKED) pack(begin ? px : PackJob(), pw, F32, a.D, p.Dp, s);
+    CeGemm g = logits_gemm(a, p, x, w, v0, n);
     TransposeJob tx, tw;
     if (a.dw && begin) {
       tx.x = a.x; tx.ldx = a.ldx; tx.rows = a.N; tx.rw.labels = a.labels; tx.rw.row_grad = a.row_grad; tx.rw.classes = a.V;
@@ -1214,10 +1272,10 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
     }
     if (a.dx) {
       tw.x = wv; tw.ldx = a.ldw; tw.rows = n; tw.most = (uint32_t*)(ws + p.mostw); tw.to = wT; tw.cols = np; tw.ld = TERMS * np; tw.exps = (int*)(ws + p.ewT);
+      tw.masks.bias = g.bias; tw.masks.labels = a.labels; tw.masks.tokens = a.N; tw.masks.v0 = v0;
       set_chunks(tw);
     }
     transpose<T, FINE>(tx, tw, a.D, s);
-    CeGemm g = logits_gemm(a, p, x, w, v0, n);
     g.stats = (const float2*)a.stats; g.row_grad = a.row_grad;
     if (a.dx) { g.G = G; g.kg = np; g.ldg = TERMS * np; }
     if (a.dw) { g.GT = GT; g.kgt = p.Np; g.ldgt = gterms * p.Np; }
