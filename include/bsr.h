@@ -591,7 +591,7 @@ int32_t bsr_distill_backward(const void* z, int32_t type, int64_t rows, int32_t 
  * for the gradients.  Per row loss = log sum exp z - z_label; with g = grad_scale * row_grad[row] and G = g (softmax(z) - onehot(label)):
  *   dx = G w,   dw = G^T x,   db = sum over rows of G
  * A row whose label lies outside 0 .. classes-1 has loss 0 and counts for no gradient (its dx is 0), whatever its x and its row_grad hold; so does, for the gradients, one of weight 0.  A class with
- * bias -inf has probability 0 and, but for rows whose label it is, no part in dx, whatever finite values its row of w holds; a row whose logits are all -inf has loss and gradient 0, one whose label's is has loss +inf and a finite gradient.  NaN and +inf in z make a row NaN, and with it dw.
+ * bias -inf has probability 0 and, but for rows whose label it is, no part in dx, whatever finite values its row of w holds (nor has one below -2^120, where logits of all rows lie above -2^100); a row whose logits are all -inf has loss and gradient 0, one whose label's is has loss +inf and a finite gradient.  NaN and +inf in z make a row NaN, and with it dw.
  * bf16 x and w are multiplied as they are; G is held in 11 bits (fp16, off by 2^-11 of itself, or by 2^-39 where it is below 2^-28), x and w beside it exactly down to 2^-29 of a feature's
  * largest value (with row_grad x in 11 bits too).  For dw in fp32 G, and x times row_grad, have two terms, off by 2^-22 of themselves: half as long again for the products.  Of up to 64 rows G is two bf16 terms, off
  * by 2^-17 of itself, and for dw in fp32 three, by 2^-24.  fp32 values are held in two terms of 11 bits each, off by 2^-22 of themselves, or by 2^-39 of the largest of their row, or of their feature, where they are below 2^-17 of it.  Sums

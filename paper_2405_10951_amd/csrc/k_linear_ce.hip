@@ -621,20 +621,27 @@ __device__ __forceinline__ float weight_of(const RowWeights& w, int64_t m) {
 }
 __device__ __forceinline__ float weighted(float v, float by) { return by == 0.f ? 0.f : v * by; }
 
-// A class whose bias is -inf has G 0 but where it is a row's label.  It counts with 0 in dx, so that whatever its row of w holds does not make the features' powers of two larger than the others need.
-// (Looking for such classes costs 2048 x 768 x 21841 3.5 us of 272 where there is a bias.)
-struct Masks { const float* bias = nullptr; const int32_t* labels = nullptr; int tokens = 0, v0 = 0; };      // bias of the piece; null: none is
-// bits of the classes r0 .. r1 that are labels (all threads, behind a barrier of their own)
-__device__ __forceinline__ void mark_labels(const Masks& k, int r0, int r1, uint32_t* bits) {
-  for (int i = threadIdx.x; i < (r1 - r0 + 31) / 32; i += blockDim.x) bits[i] = 0;
+// A masked class has G 0 but where it is a row's label: its bias is -inf, or below -2^120 where the largest logit of every row with a label lies above -2^100 (its own would take 2^119 of x w to live).  It
+// counts with 0 in dx, so that whatever its row of w holds does not make the features' powers of two larger than the others need.
+// (Looking for such classes costs the gradients of 2048 x 768 x 21841 1.5 us of 270.5 where there is a bias.)
+struct Masks { const float* bias = nullptr; const int32_t* labels = nullptr; const float2* stats = nullptr; int tokens = 0, classes = 0, v0 = 0; };      // bias of the piece; null: none is
+constexpr float MAY_MASK = -0x1p120f;
+// bits of the classes r0 .. r1 that are labels -> the bias that masks (all 256 threads, behind a barrier of their own)
+__device__ __forceinline__ float look_at_rows(const Masks& k, int r0, int r1, uint32_t* bits, float* red) {
+  for (int i = threadIdx.x; i < (r1 - r0 + 31) / 32; i += 256) bits[i] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < k.tokens; i += blockDim.x) {
-    const int at = max(k.labels[i], -1) - k.v0 - r0;
+  float least = INFINITY;
+  for (int i = threadIdx.x; i < k.tokens; i += 256) {
+    const int label = k.labels[i], at = max(label, -1) - k.v0 - r0;
+    if (label >= 0 && label < k.classes) least = fminf(least, k.stats[i].x);
     if (at >= 0 && at < r1 - r0) atomicOr(bits + at / 32, 1u << at % 32);
   }
+  least = -wave_max(-least);
+  if (threadIdx.x % WAVE == 0) red[threadIdx.x / WAVE] = least;
   __syncthreads();
+  return fminf(fminf(red[0], red[1]), fminf(red[2], red[3])) > -0x1p100f ? MAY_MASK : -INFINITY;
 }
-__device__ __forceinline__ bool is_masked(const Masks& k, int r, int r0, const uint32_t* bits) { return k.bias[r] == -INFINITY && !(bits[(r - r0) / 32] >> (r - r0) % 32 & 1); }
+__device__ __forceinline__ bool is_masked(const Masks& k, int r, int r0, const uint32_t* bits, float limit) { return k.bias[r] <= limit && !(bits[(r - r0) / 32] >> (r - r0) % 32 & 1); }
 
 // [rows, D] -> [D][ld] fp16 in one or two terms, a power of two each of the D rows; what lies between rows and ld is zero.  In two launches, each for x, w or both: the columns' maxima, `chunks`
 // parts of the rows apart, then the rest
@@ -660,16 +667,18 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
   // (masked classes are looked for beside the loads, the first 256 ahead of them; where there are some, the maxima are made once more without them)
   const float first_bias = j.masks.bias ? j.masks.bias[min(r0 + (int)threadIdx.x, r1 - 1)] : 0.f;
   __shared__ uint32_t label_bits[MOST_PART / 32];
+  __shared__ float lows[4];
   __shared__ int found[4];
+  float limit = 0.f;
   auto any_masked = [&]() __attribute__((always_inline)) {
     if (!j.masks.bias) return false;
-    bool mine = first_bias == -INFINITY;
-    for (int r = r0 + 256 + threadIdx.x; r < r1; r += 256) mine |= j.masks.bias[r] == -INFINITY;
+    bool mine = first_bias <= MAY_MASK;
+    for (int r = r0 + 256 + threadIdx.x; r < r1; r += 256) mine |= j.masks.bias[r] <= MAY_MASK;
     const bool wave = __any(mine);
     if (threadIdx.x % WAVE == 0) found[threadIdx.x / WAVE] = wave;
     __syncthreads();
     if (!(found[0] | found[1] | found[2] | found[3])) return false;
-    mark_labels(j.masks, r0, r1, label_bits);
+    limit = look_at_rows(j.masks, r0, r1, label_bits, lows);
     return true;
   };
   if (D < V) {                                     // (no whole piece to read)
@@ -679,7 +688,7 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
     uint32_t m = 0;
     if (c < D)
 #pragma unroll 4
-      for (int r = r0 + i; r < r1; r += 256 / V) m = max(m, bits_if_finite(weighted((float)x[r * j.ldx + c], some && is_masked(j.masks, r, r0, label_bits) ? 0.f : weight_of(j.rw, r))));
+      for (int r = r0 + i; r < r1; r += 256 / V) m = max(m, bits_if_finite(weighted((float)x[r * j.ldx + c], some && is_masked(j.masks, r, r0, label_bits, limit) ? 0.f : weight_of(j.rw, r))));
     part[i][c] = m;
     __syncthreads();
     if ((int)threadIdx.x < D) {
@@ -704,7 +713,7 @@ __global__ __launch_bounds__(256) void ce_colmax_kernel(TransposeJob a, Transpos
 #pragma unroll
     for (int e = 0; e < V; ++e) m[e] = 0;
     for (int r = r0 + threadIdx.x / SIDE; r < r1; r += ABOVE) {
-      if (is_masked(j.masks, r, r0, label_bits)) continue;
+      if (is_masked(j.masks, r, r0, label_bits, limit)) continue;
       const typename Loose<T>::vec v = *(const typename Loose<T>::vec*)(x + r * j.ldx + col);
 #pragma unroll
       for (int e = 0; e < V; ++e) m[e] = max(m[e], bits_if_finite((float)v[e]));
@@ -756,6 +765,7 @@ __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, Trans
   };
   fetch(begin);
   __shared__ uint32_t label_bits[16];              // (down: 8 at most)
+  __shared__ float lows[4];
   __shared__ int found[4];
   float bias[2] = {0.f, 0.f};                      // (of 512 classes)
   if (j.masks.bias)
@@ -766,11 +776,11 @@ __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, Trans
 #pragma unroll 4
     for (int k = w; k < j.chunks; k += 4) most = max(most, j.most[(int64_t)k * D + c0 + lane]);
   red[w][lane] = most;
-  const bool masked = __any(bias[0] == -INFINITY || bias[1] == -INFINITY);            // (or a class behind the workgroup's last: looked for in vain)
+  const bool masked = __any(bias[0] <= MAY_MASK || bias[1] <= MAY_MASK);            // (or a class behind the workgroup's last: looked for in vain)
   if (lane == 0) found[w] = masked;
   __syncthreads();
   const bool some = found[0] | found[1] | found[2] | found[3];
-  if (some) mark_labels(j.masks, begin, min(end, j.rows), label_bits);
+  const float limit = some ? look_at_rows(j.masks, begin, min(end, j.rows), label_bits, lows) : 0.f;
   if (w == 0) {
     const int e = exponent_of(max(max(red[0][lane], red[1][lane]), max(red[2][lane], red[3][lane])));
     exps[lane] = e;
@@ -782,7 +792,7 @@ __global__ __launch_bounds__(256) void ce_transpose_kernel(TransposeJob a, Trans
 #pragma unroll
       for (int i = 0; i < K; ++i) {
         const int m = m0 + r0 + i * (256 / PER_ROW);
-        if (m < j.rows && is_masked(j.masks, m, begin, label_bits)) by[i] = 0.f;
+        if (m < j.rows && is_masked(j.masks, m, begin, label_bits, limit)) by[i] = 0.f;
       }
 #pragma unroll
     for (int i = 0; i < K; ++i)
@@ -1272,7 +1282,7 @@ void backward_as(const LinearCe& a, Ready ready, const float* z, hipStream_t s) 
     }
     if (a.dx) {
       tw.x = wv; tw.ldx = a.ldw; tw.rows = n; tw.most = (uint32_t*)(ws + p.mostw); tw.to = wT; tw.cols = np; tw.ld = TERMS * np; tw.exps = (int*)(ws + p.ewT);
-      tw.masks.bias = g.bias; tw.masks.labels = a.labels; tw.masks.tokens = a.N; tw.masks.v0 = v0;
+      tw.masks.bias = g.bias; tw.masks.labels = a.labels; tw.masks.stats = (const float2*)a.stats; tw.masks.tokens = a.N; tw.masks.classes = a.V; tw.masks.v0 = v0;
       set_chunks(tw);
     }
     transpose<T, FINE>(tx, tw, a.D, s);
