@@ -467,7 +467,7 @@ int32_t bsr_attention_backward(const void* qkv, const void* out, const void* dou
 /*
  * Operators on the caller's own tensors (no context): LayerNorm, RMSNorm, frozen linear layers in 8 bits, distillation from a teacher's top
  * logits, cross-entropy of a linear layer, clipping of gradients.  A program that tunes the norms of a frozen model against a teacher runs them one after the other
- * (paper_2405_10951_amd/norm_tuning.py).  Rows are contiguous; between rows there is a stride ("ld...", in elements, at least the row's
+ * (paper_2405_10951_amd/norm_tuning.py).  Kernels run on the current device, whose tensors and stream these have to be.  Rows are contiguous; between rows there is a stride ("ld...", in elements, at least the row's
  * length) and the first may start anywhere.  Types are BSR_BF16 or BSR_FP32; statistics, sums over rows, products and losses are fp32 inside whatever
  * the type.  Tensors without a stride are aligned to 16 bytes; rows of whole 16-byte pieces on 16-byte boundaries are the fast ones.  Zero rows are no error: nothing is
  * launched but what zeroes a sum over them.  Results are bit-reproducible (no atomics).  All launches go to `stream`, nothing waits.

@@ -247,9 +247,12 @@ def _gpu_index(device):
 
 
 def _raw_stream(index) -> int:
-    """torch's current stream of a GPU, without the object around it"""
+    """torch's current stream of a GPU, without the object around it.  The library launches on the current GPU: tensors on another one are refused."""
     import torch
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if index is None else index)
+    here = torch._C._cuda_getDevice()
+    if index is not None and index != here:
+        raise ValueError(f"tensors on cuda:{index}, the current GPU is cuda:{here} (torch.cuda.device or set_device)")
+    return torch._C._cuda_getCurrentRawStream(here)
 
 
 def _cur_stream(t):
