@@ -8,14 +8,14 @@
 // 2^-28 and are off by 2^-39 at most below, where bf16 would keep 8; x and w join it in fp16, each feature (a row of the transposed operand) scaled by a power of two so that its
 // largest value lies in 2^14 .. 2^15, which is exact for bf16 values down to 2^-29 of the feature's largest.  The matrix instructions take both types at one rate.  fp32 operands are two fp16 terms each,
 // h + l with h = fp16(v), l = fp16(v - h), off by 2^-22 of the value, and the products h h, l h, h l are added in fp32.  A k-tile holds both terms of 32 k: it is loaded
-// once for the three of them (333 x 1001 x 5003 loss and gradients 93 us; one product after another over the whole contraction 109, k-tile by k-tile 107).
+// once for the three of them (333 x 1001 x 5003 loss and gradients 93 us in the run in which one product after another over the whole contraction took 109 and k-tile by k-tile 107; 93 to 102 from card to card).
 // dw in fp32 beside bf16 operands: one fp16 term of G would show in it (with weights off by 8e-5 of its norm, two terms by 4.5e-7, at 2048 x 768 x 21841), so the transposed G has two, and so has x times a weight; the products
 // h h, l h and, with weights, h l follow one another over a contraction of two or three times the tokens (6304 x 768 x 21841 loss and gradients 1423 us, with weights 1670; dw in bf16 1072).  In a bf16 result G's
 // one term does not show: 2048 x 768 x 21841 dw is off by 1.662e-3 of its norm, from exact G by 1.659e-3, the rounding of the result.
 // Bound by the matrix unit's power where it is large: at 4096 x 4096 x 131072 bf16 a tile of 16 x 16 x 32 instructions runs at 1.7 - 1.8 GHz (32 x 32 x 16 at 1.46, 6 % slower in all), the forward at
-// 1350 TFLOP/s (3.25 ms), a piece's G at 1225 (450 us), both products of G at 1250 (880 us); transposing a piece takes 38 + 59 us.  2048 x 768 x 21841, gradients: maxima 12, transposing 17, G 100 (688 tiles of
-// 12 k-tiles on 256 CUs: beginnings and ends count as much as the products), products 137, sums 9.  333 x 1001 x 5003 fp32: packing 11, logits 20, joining 5, maxima 9, transposing 13, G 9, products 35,
-// sums 4.
+// 1350 TFLOP/s (3.25 ms), a piece's G at 1225 (450 us), both products of G at 1250 (880 us); transposing a piece takes 38 + 59 us.  2048 x 768 x 21841, gradients, best and median of
+// twenty: maxima 12 and 14, transposing 16 and 18, G 94 and 111 (688 tiles of 12 k-tiles on 256 CUs: beginnings and ends count as much as the products), products 121 and 147, sums 9.  333 x 1001 x 5003 fp32: packing 11,
+// logits 19, joining 5, maxima 10, transposing 13, G 9, products 35, sums 4.
 // The row's weight g scales x in dw and the result in dx; rows whose label is absent or whose weight is 0 have G = 0 and, in the transposed x, zeros.
 #include <algorithm>
 

@@ -5,7 +5,7 @@
 //   rows     a workgroup a token: maximum, sum, loss
 //   grads    up to 64 tokens: dx and dw in one pass over w, multiplied in fp32 (16 x 16 x 4), or beside bf16 with G in two bf16 terms (16 x 16 x 32) and, for dw in fp32, a third (16 x 16 x 16)
 // A launch is a chain of a few trips to memory; that, the calls and, for few rows of many classes, the bytes of w and dw are what bounds it.
-// Measured: 32 x 768 x 100 fp32 8 + 11 us; loss and gradients of 48 x 2048 x 100000 fp32 987 (by tiles 2360), of 1 x 100 x 100000 bf16 50; gradients of 32 x 4096 x 100000 bf16 348 (1.6 GB of w and dw: 4.7 TB/s; with fp32 products 728), of 64 rows 580 (two wavefronts a SIMD, of which each waits for a
+// Measured: 32 x 768 x 100 fp32 8 + 11 us; loss and gradients of 48 x 2048 x 100000 fp32 987 to 1062 (by tiles 2360), of 1 x 100 x 100000 bf16 50 to 54; gradients of 32 x 4096 x 100000 bf16 348 (1.6 GB of w and dw: 4.7 TB/s; with fp32 products 728), of 64 rows 580 (two wavefronts a SIMD, of which each waits for a
 // half as long rows' piece; G by columns from memory instead of LDS: 673; 8 features a lane and one wavefront: 660; four wavefronts side by side on G: 690).
 // The third term of G for dw in fp32: loss and gradients of 64 x 4096 x 100000 949 us, of two terms 930; 32 x 4096 x 100000 749 with either; 33 x 2048 x 8000, gradients, 64 and 62.
 #include <algorithm>
